@@ -72,7 +72,8 @@ typedef enum {
   MOL_OP_RERANK = 3,
   MOL_OP_TOPK_MAXDOT = 4,
   MOL_OP_TOPK_BOUNDED = 5,
-  MOL_OP_TOPK_TWO_PASS = 6
+  MOL_OP_TOPK_TWO_PASS = 6,
+  MOL_OP_SCORE_GRAD = 7  /* workspace size only: not timed                   */
 } mol_op;
 
 /* Threshold of the two-pass exact algorithm (mol_topk_two_pass). */
@@ -92,6 +93,8 @@ typedef enum {
 #define MOL_MAX_D 1024    /* component embedding width                       */
 #define MOL_MAX_K 8192    /* k of every top-k output                         */
 #define MOL_MAX_C 16384   /* candidates per query handed to mol_rerank       */
+#define MOL_MAX_ROW 65536 /* elements of an embedding table's row            */
+#define MOL_MAX_TABLES 64 /* component tables per embedding call             */
 
 /* One retrieval problem: shapes, storage type and device pointers (the
  * notation table of Section 2; gating parameters per Appendix A.3).
@@ -305,6 +308,147 @@ int mol_gap_bound_combined(int32_t B, int32_t P, int32_t m, const float *dots,
                            const int32_t *avg_ids, int32_t k_avg, int32_t k,
                            const float *scores, float *out_S, float *out_SK,
                            float *out_bound, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Learning the similarity.  One step of the paper's sampled-softmax
+ * objective (Section 2, Eq. 4) on the model that the calls above serve:
+ *   mol_embed_lookup  rows of the query's and the items' tables by id, laid
+ *                     out as a problem's Q and X;
+ *   mol_score         phi of every query against the sampled items;
+ *   mol_softmax_loss  the loss and dphi;
+ *   mol_score_grad    the gradient of every problem tensor;
+ *   mol_embed_grad    the tables' gradient, rows summed by id;
+ *   mol_adamw_step    the update.
+ * All of it is deterministic: the same inputs give the same bits. */
+
+/* Embedding rows by id: for each of C component tables
+ *   out[c][t][:] = scale * table[c][ids[t]][:],   t < T.
+ * table [C][V][d] (table_dtype), ids int32 [T], out [C][T][d] (out_dtype):
+ * C item tables give a problem's X [Px][T][d]; query rows of Pq components
+ * are one table, C = 1, of rows of Pq * d elements, and give Q [B][Pq][d].
+ * The product is formed in float32 and rounded once to out_dtype.  An id
+ * outside [0, V) (e.g. -1) is an empty slot: its row is zero, and its
+ * gradient is dropped by mol_embed_grad.  T == 0 is a no-op.  d up to
+ * MOL_MAX_ROW, C up to MOL_MAX_TABLES.  table and out must not overlap. */
+int mol_embed_lookup(const void *table, int32_t table_dtype, int32_t C,
+                     int32_t V, int32_t d, const int32_t *ids, int32_t T,
+                     float scale, void *out, int32_t out_dtype, void *stream);
+
+/* Gradient of mol_embed_lookup for its tables:
+ *   table_grad[c][v][:] (+)= scale * sum over t with ids[t] == v of
+ *                            grad[c][t][:].
+ * grad [C][T][d] (grad_dtype), table_grad [C][V][d] (out_dtype).  With
+ * accumulate == 0 every row is written, zero where no token has its id; with
+ * accumulate == 1 the sum is added to the rows that have tokens, and the
+ * others are neither read nor written (T == 0: nothing is).  The tokens are
+ * sorted by id, stably, and each row is summed in float32, in an order that
+ * only ids and the sizes fix, and rounded once.  Needs
+ * mol_embed_grad_workspace bytes of workspace (256-byte aligned). */
+int mol_embed_grad_workspace(int32_t C, int32_t V, int32_t d, int32_t T,
+                             size_t *bytes);
+int mol_embed_grad(const void *grad, int32_t grad_dtype, int32_t C, int32_t V,
+                   int32_t d, const int32_t *ids, int32_t T, float scale,
+                   int32_t accumulate, void *table_grad, int32_t out_dtype,
+                   void *ws, size_t ws_bytes, void *stream);
+
+/* Sampled-softmax loss of every query (Eq. 4) and its gradient, from scores
+ * phi float32 [B][N] (as mol_score writes them):
+ *   z_i     = inv_temp * phi[b][i]
+ *   loss[b] = log sum_{i kept} exp(z_i) - z_t,       t = target[b]
+ *   dphi[b][i] = row_weight[b] * inv_temp * (softmax(z)_i - [i == t]).
+ * target int32 [B]: the positive's column.  ids int32 [N] (may be NULL): the
+ * columns' items.  A column is left out (dphi 0, whatever its score holds)
+ * if its id is negative (an empty slot), or if it is another copy of the
+ * query's positive: i != t and ids[i] == ids[t].  A row whose target is
+ * outside [0, N), or whose target's id is negative, has loss 0 and gradient
+ * 0.  row_weight float32 [B] is the gradient of the total for loss[b] (NULL:
+ * 1 each); it does not scale loss.  loss may be NULL, and dphi may be NULL
+ * or phi itself.  Maximum, sum and loss are float32. */
+int mol_softmax_loss_workspace(int32_t B, int32_t N, size_t *bytes);
+int mol_softmax_loss(int32_t B, int32_t N, const float *phi,
+                     const int32_t *target, const int32_t *ids, float inv_temp,
+                     const float *row_weight, float *loss, float *dphi,
+                     void *ws, size_t ws_bytes, void *stream);
+
+/* Gradient of mol_score over the whole corpus for every tensor of the
+ * problem, given dphi float32 [B][N].  With g = dphi and the symbols of the
+ * problem above, sig = 1 / (1 + exp(-u)):
+ *   dl_p = g pi_p (s_p - phi)          da_q[b] = sum_n dl, da_x[n] = sum_b dl
+ *   dh   = W2^T dl                     dW2 = sum dl SiLU(u)^T,  db2 = sum dl
+ *   du   = dh sig (1 + u (1 - sig))    dW1 = sum du s^T,        db1 = sum du
+ *   ds   = g pi + W1^T du              dQ = sum ds X,           dX = sum ds Q
+ * Each output has its tensor's shape and type, and any may be NULL.  Every
+ * element is written.  The gating chain runs in float32 for float32 problems
+ * and in float32 or better than float32's rounding allows to tell for bf16
+ * ones whatever the flags say; sums are float32, rounded once to bf16 at the
+ * end.  Needs every problem pointer and
+ * mol_workspace_size(MOL_OP_SCORE_GRAD) bytes of workspace. */
+typedef struct mol_score_grads {
+  void *dQ;      /* [B][Pq][d]  dtype   */
+  void *dX;      /* [Px][N][d]  dtype   */
+  float *da_q;   /* [B][P]              */
+  float *da_x;   /* [N][P]              */
+  void *dW1;     /* [H][P]      dtype   */
+  float *db1;    /* [H]                 */
+  void *dW2;     /* [P][H]      dtype   */
+  float *db2;    /* [P]                 */
+} mol_score_grads;
+int mol_score_grad(const mol_problem *prob, const float *dphi,
+                   const mol_score_grads *grads, void *ws, size_t ws_bytes,
+                   void *stream);
+
+/* One AdamW step (decoupled weight decay) over many tensors at once:
+ *   g' = grad_scale g
+ *   m' = beta1 m + (1 - beta1) g',   v' = beta2 v + (1 - beta2) g'^2
+ *   p' = p (1 - lr weight_decay)
+ *        - lr (m' / (1 - beta1^step)) / (sqrt(v' / (1 - beta2^step)) + eps)
+ * in float32, from the new states before they are rounded.
+ *
+ * A tensor's states are float32 (MOL_STATE_F32) or 8-bit (MOL_STATE_E4M3):
+ * m and sqrt(v) as e4m3 codes with one float32 scale per run of
+ * MOL_STATE_BLOCK elements, the last run short; scale = largest magnitude /
+ * 448.  New codes are rounded up or down with the chance that makes the
+ * stored value right on average (beta2 = 0.999 moves v by less than half a
+ * code per step, so that rounding to nearest would leave it where it is).
+ * The chance comes from 16 bits of a 32-bit mix of the element's place
+ * (rng_offset + its index), seed and step.  A positive v is never stored as
+ * zero, which would make the element's next step unbounded.  A block that
+ * holds a NaN or an infinity stores NaN scales.  Codes start as zeros with
+ * zero scales.
+ *
+ * Each state is read from one buffer and written to another or the same one
+ * (in place); buffers overlap in no other way.  copy_out: NULL, or bf16 [n],
+ * the new parameter rounded to nearest (a bf16 problem's tensor of a float32
+ * master).  Any alignment of the element types is taken.  n == 0 is allowed.
+ * step_ptr and lr_ptr: NULL, or device memory read by the kernel in place of
+ * step and lr, so that a captured graph can be replayed for later steps
+ * (*step_ptr below 1 counts as 1).  grad_scale: NULL (1), or one float on the
+ * device, e.g. the factor that clips the gradients' norm.  The tensor
+ * descriptors are host memory, free for use when the call returns. */
+#define MOL_STATE_F32 0
+#define MOL_STATE_E4M3 1
+#define MOL_STATE_BLOCK 256
+typedef struct mol_adamw_tensor {
+  int64_t n;                              /* elements                        */
+  const void *p, *g, *m, *v;              /* param_dtype, grad_dtype, states */
+  const float *m_scale, *v_scale;         /* [ceil(n / 256)], 8-bit states   */
+  void *p_out, *m_out, *v_out;
+  float *m_scale_out, *v_scale_out;
+  void *copy_out;                         /* bf16 [n] or NULL                */
+  int32_t param_dtype, grad_dtype, state; /* mol_dtype, mol_dtype, MOL_STATE_* */
+  float weight_decay;
+  uint64_t rng_offset;
+} mol_adamw_tensor;
+typedef struct mol_adamw {
+  double lr, beta1, beta2, eps;
+  int32_t step;                           /* from 1                          */
+  uint32_t seed;
+  const float *grad_scale;
+  const float *lr_ptr;
+  const int32_t *step_ptr;
+} mol_adamw;
+int mol_adamw_step(const mol_adamw *opt, const mol_adamw_tensor *tensors,
+                   int32_t n_tensors, void *stream);
 
 /* Kernel timing, a diagnostic for throughput measurements.
  * mol_timing_enable(1) makes every later call record a pair of HIP events on

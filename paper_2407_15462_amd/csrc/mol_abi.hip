@@ -1,6 +1,7 @@
 // Host side of the C ABI declared in include/mol.h: argument validation,
 // workspace planning and kernel sequencing on the caller's stream.
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <cstdarg>
 #include <cstdio>
@@ -1103,6 +1104,10 @@ int mol_workspace_size(const mol_problem* prob, int op, int32_t k, int32_t kprim
       if ((rc = check_two_pass_k(prob, k))) return rc;
       *bytes = plan_two_pass(dev_prob(prob), k).ws.best;
       return MOL_OK;
+    case MOL_OP_SCORE_GRAD:
+      if ((rc = check_problem(prob, true))) return rc;
+      *bytes = score_grad_bytes(dev_prob(prob));
+      return MOL_OK;
     default:
       return fail(MOL_EINVAL, "unknown op %d", op);
   }
@@ -1262,6 +1267,131 @@ int mol_gap_bound_combined(int32_t B, int32_t P, int32_t m, const float* dots, c
   MOL_TRY_HIP(launch_gap_bound_combined(B, P, m, dots, ids, kprime, avg_ids, k_avg, k, scores, out_S, out_SK,
                                         out_bound, static_cast<hipStream_t>(stream)),
               "combined gap bound");
+  return MOL_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Learning the similarity.
+
+static int check_dtype(int32_t t, const char* name) {
+  if (t != MOL_F32 && t != MOL_BF16) return fail(MOL_EUNSUPPORTED, "%s = %d is not MOL_F32 or MOL_BF16", name, t);
+  return MOL_OK;
+}
+
+static int check_rows(int32_t C, int32_t V, int32_t d, int32_t T) {
+  if (C < 1 || V < 1 || d < 1 || T < 0)
+    return fail(MOL_EINVAL, "need C, V, d >= 1 and T >= 0 (C=%d V=%d d=%d T=%d)", C, V, d, T);
+  if (C > MOL_MAX_TABLES) return fail(MOL_EUNSUPPORTED, "C = %d tables exceed %d", C, MOL_MAX_TABLES);
+  if (d > MOL_MAX_ROW) return fail(MOL_EUNSUPPORTED, "d = %d exceeds %d", d, MOL_MAX_ROW);
+  // grids hold 2^32 threads; a block has 1024 elements at least
+  if (static_cast<int64_t>(T) * d * C >= (1ll << 33) || static_cast<int64_t>(V) * C >= (1ll << 33))
+    return fail(MOL_EUNSUPPORTED, "C T d = %lld elements or C V = %lld rows pass 2^33",
+                static_cast<long long>(T) * d * C, static_cast<long long>(V) * C);
+  return MOL_OK;
+}
+
+int mol_embed_lookup(const void* table, int32_t table_dtype, int32_t C, int32_t V, int32_t d, const int32_t* ids,
+                     int32_t T, float scale, void* out, int32_t out_dtype, void* stream) {
+  int rc;
+  if ((rc = check_rows(C, V, d, T))) return rc;
+  if ((rc = check_dtype(table_dtype, "table_dtype")) || (rc = check_dtype(out_dtype, "out_dtype"))) return rc;
+  if (T == 0) return MOL_OK;
+  if (!table || !ids || !out) return fail(MOL_EINVAL, "table, ids or out is NULL");
+  MOL_TRY_HIP(launch_embed_lookup(table, table_dtype, C, V, d, ids, T, scale, out, out_dtype,
+                                  static_cast<hipStream_t>(stream)),
+              "embedding lookup");
+  return MOL_OK;
+}
+
+int mol_embed_grad_workspace(int32_t C, int32_t V, int32_t d, int32_t T, size_t* bytes) {
+  int rc;
+  if ((rc = check_rows(C, V, d, T))) return rc;
+  if (!bytes) return fail(MOL_EINVAL, "bytes is NULL");
+  size_t off[4];
+  *bytes = embed_grad_bytes(C, V, d, T, off);
+  return MOL_OK;
+}
+
+int mol_embed_grad(const void* grad, int32_t grad_dtype, int32_t C, int32_t V, int32_t d, const int32_t* ids, int32_t T,
+                   float scale, int32_t accumulate, void* table_grad, int32_t out_dtype, void* ws, size_t ws_bytes,
+                   void* stream) {
+  int rc;
+  if ((rc = check_rows(C, V, d, T))) return rc;
+  if ((rc = check_dtype(grad_dtype, "grad_dtype")) || (rc = check_dtype(out_dtype, "out_dtype"))) return rc;
+  if (accumulate != 0 && accumulate != 1) return fail(MOL_EINVAL, "accumulate = %d is not 0 or 1", accumulate);
+  if (T == 0 && accumulate) return MOL_OK;
+  if (!table_grad || (T > 0 && (!grad || !ids))) return fail(MOL_EINVAL, "grad, ids or table_grad is NULL");
+  size_t off[4];
+  if ((rc = check_ws(ws, ws_bytes, embed_grad_bytes(C, V, d, T, off)))) return rc;
+  MOL_TRY_HIP(launch_embed_grad(grad, grad_dtype, C, V, d, ids, T, scale, accumulate, table_grad, out_dtype, ws,
+                                static_cast<hipStream_t>(stream)),
+              "embedding gradient");
+  return MOL_OK;
+}
+
+static int check_loss(int32_t B, int32_t N) {
+  if (B < 1 || N < 1) return fail(MOL_EINVAL, "sizes must be positive (B=%d N=%d)", B, N);
+  if (B > MOL_MAX_B) return fail(MOL_EUNSUPPORTED, "B = %d exceeds %d", B, MOL_MAX_B);
+  return MOL_OK;
+}
+
+int mol_softmax_loss_workspace(int32_t B, int32_t N, size_t* bytes) {
+  int rc;
+  if ((rc = check_loss(B, N))) return rc;
+  if (!bytes) return fail(MOL_EINVAL, "bytes is NULL");
+  *bytes = softmax_loss_bytes(B, N);
+  return MOL_OK;
+}
+
+int mol_softmax_loss(int32_t B, int32_t N, const float* phi, const int32_t* target, const int32_t* ids, float inv_temp,
+                     const float* row_weight, float* loss, float* dphi, void* ws, size_t ws_bytes, void* stream) {
+  int rc;
+  if ((rc = check_loss(B, N))) return rc;
+  if (!phi || !target) return fail(MOL_EINVAL, "phi or target is NULL");
+  if (!(inv_temp > 0.f) || inv_temp > FLT_MAX) return fail(MOL_EINVAL, "inv_temp = %g is not positive and finite", inv_temp);
+  if ((rc = check_ws(ws, ws_bytes, softmax_loss_bytes(B, N)))) return rc;
+  if (!loss && !dphi) return MOL_OK;
+  MOL_TRY_HIP(launch_softmax_loss(B, N, phi, target, ids, inv_temp, row_weight, loss, dphi, ws,
+                                  static_cast<hipStream_t>(stream)),
+              "softmax loss");
+  return MOL_OK;
+}
+
+int mol_score_grad(const mol_problem* prob, const float* dphi, const mol_score_grads* grads, void* ws, size_t ws_bytes,
+                   void* stream) {
+  int rc;
+  if ((rc = check_problem(prob, true))) return rc;
+  if (!dphi || !grads) return fail(MOL_EINVAL, "dphi or grads is NULL");
+  const DevProb pr = dev_prob(prob);
+  if ((rc = check_ws(ws, ws_bytes, score_grad_bytes(pr)))) return rc;
+  MOL_TRY_HIP(launch_score_grad(pr, dphi, *grads, ws, static_cast<hipStream_t>(stream)), "score gradient");
+  return MOL_OK;
+}
+
+int mol_adamw_step(const mol_adamw* opt, const mol_adamw_tensor* tensors, int32_t n_tensors, void* stream) {
+  if (!opt) return fail(MOL_EINVAL, "opt is NULL");
+  if (n_tensors < 0) return fail(MOL_EINVAL, "n_tensors = %d is negative", n_tensors);
+  if (n_tensors > 0 && !tensors) return fail(MOL_EINVAL, "tensors is NULL");
+  if (!(opt->beta1 >= 0 && opt->beta1 < 1 && opt->beta2 >= 0 && opt->beta2 < 1))
+    return fail(MOL_EINVAL, "beta1 = %g, beta2 = %g: need 0 <= beta < 1", opt->beta1, opt->beta2);
+  if (!(opt->eps > 0)) return fail(MOL_EINVAL, "eps = %g is not positive", opt->eps);
+  if (!opt->lr_ptr && !(opt->lr >= 0)) return fail(MOL_EINVAL, "lr = %g is negative", opt->lr);
+  if (!opt->step_ptr && opt->step < 1) return fail(MOL_EINVAL, "step = %d: steps count from 1", opt->step);
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    const mol_adamw_tensor& t = tensors[i];
+    if (t.n < 0 || t.n >= (1ll << 35)) return fail(MOL_EINVAL, "tensor %d: n = %lld outside [0, 2^35)", i, static_cast<long long>(t.n));
+    int rc;
+    if ((rc = check_dtype(t.param_dtype, "param_dtype")) || (rc = check_dtype(t.grad_dtype, "grad_dtype"))) return rc;
+    if (t.state != MOL_STATE_F32 && t.state != MOL_STATE_E4M3)
+      return fail(MOL_EUNSUPPORTED, "tensor %d: state = %d is not MOL_STATE_F32 or MOL_STATE_E4M3", i, t.state);
+    if (!(t.weight_decay >= 0)) return fail(MOL_EINVAL, "tensor %d: weight_decay = %g is negative", i, t.weight_decay);
+    if (t.n == 0) continue;
+    if (!t.p || !t.g || !t.m || !t.v || !t.p_out || !t.m_out || !t.v_out)
+      return fail(MOL_EINVAL, "tensor %d: a pointer (p, g, m, v, p_out, m_out, v_out) is NULL", i);
+    if (t.state == MOL_STATE_E4M3 && (!t.m_scale || !t.v_scale || !t.m_scale_out || !t.v_scale_out))
+      return fail(MOL_EINVAL, "tensor %d: a scale pointer of its 8-bit states is NULL", i);
+  }
+  MOL_TRY_HIP(launch_adamw(*opt, tensors, n_tensors, static_cast<hipStream_t>(stream)), "AdamW step");
   return MOL_OK;
 }
 

@@ -226,3 +226,28 @@ hipError_t launch_rerank(const DevProb& pr, const int32_t* uniq, const int32_t* 
                          long phi_stride, hipStream_t st);
 
 }  // namespace mol
+
+namespace mol {
+
+// Embedding rows by id and the gradient of their tables (mol_embed.hip).
+hipError_t launch_embed_lookup(const void* table, int table_dtype, int C, int V, int d, const int32_t* ids, int T,
+                               float scale, void* out, int out_dtype, hipStream_t st);
+// workspace of the gradient: bytes, and where its parts begin
+size_t embed_grad_bytes(int C, int V, int d, long T, size_t off[4]);
+hipError_t launch_embed_grad(const void* grad, int grad_dtype, int C, int V, int d, const int32_t* ids, int T,
+                             float scale, int accumulate, void* out, int out_dtype, void* ws, hipStream_t st);
+
+// Sampled-softmax loss and gradient (mol_loss.hip); ws: softmax_loss_bytes
+size_t softmax_loss_bytes(int B, int N);
+hipError_t launch_softmax_loss(int B, int N, const float* phi, const int32_t* target, const int32_t* ids,
+                               float inv_temp, const float* row_weight, float* loss, float* dphi, void* ws,
+                               hipStream_t st);
+
+// Gradient of the scores for every input (mol_score_grad.hip); ws: score_grad_bytes
+size_t score_grad_bytes(const DevProb& pr);
+hipError_t launch_score_grad(const DevProb& pr, const float* dphi, const mol_score_grads& o, void* ws, hipStream_t st);
+
+// AdamW over many tensors (mol_adamw.hip); arguments checked
+hipError_t launch_adamw(const mol_adamw& opt, const mol_adamw_tensor* tensors, int n_tensors, hipStream_t st);
+
+}  // namespace mol

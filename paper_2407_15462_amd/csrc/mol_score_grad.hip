@@ -1,0 +1,797 @@
+// Gradient of the MoL scores (Eq. 1 / Eq. 2 with the gating MLP of Appendix
+// A.3) for every input, any supported shape and both storage types.
+//
+// With g = dphi, per pair (query, item):
+//   dl_p = g pi_p (s_p - phi)             dh = W2^T dl
+//   du   = dh sig (1 + u (1 - sig))       ds = g pi + W1^T du
+// and sums of dl, du, du s^T, dl h^T, ds X and ds Q over pairs.
+//
+// 1. k_score_grad recomputes the chain and goes back through it.  A workgroup
+//    of 8 waves has TI items and walks over blocks of QB queries, QB TI = 128
+//    pairs: the waves form the tile's dot products (as k_mol_f32 does) in LDS,
+//    then each wave takes 16 items of one query through the chain on 16x16x4
+//    f32 MFMAs.  Lane (c = lane % 16, g = lane / 16) holds item c's components
+//    p = RUN g + mu, mu < RUN = PV / 4, the layout in which s, dl (K = p) and
+//    h, du (K = j, four hidden units of each 16) are B operands as they stand,
+//    so that the four products with W1, W2 and their transposes exchange
+//    nothing between lanes.  dW1 = sum du s^T and dW2 = sum dl h^T have K = the
+//    items: s and dl are read back from LDS, h and du go through a small block
+//    of the wave's, four items a lane.  The two sums stay in registers for the
+//    whole walk (JTG blocks of 16 hidden units; a wider MLP takes a launch for
+//    every JTG blocks, of which only the first writes ds, da_q and da_x), as
+//    does da_x.  The workgroup's sums go to the workspace.
+// 2. ds goes there too, [Px][B Pq][items], as float32 or, for bf16 problems, as
+//    two bf16 terms (16 significant bits, more than dQ and dX keep), and
+//    k_grad_gemm forms dQ = sum ds X and dX = sum ds Q on matrix cores from it,
+//    with X and Q transposed once.
+// 3. k_sum_parts adds the partial sums in a fixed order.
+// Items are taken in slabs, so that ds stays within kSlabBytes.
+//
+// What bounds it: the f32 matrix rate, 12 P H flop a pair (157 TFLOP/s).
+#include <algorithm>
+
+#include "mol_tile.h"
+
+namespace mol {
+
+using namespace tile;
+
+namespace {
+
+constexpr int kWaves = 8, kThreads = 64 * kWaves, kPairs = 16 * kWaves;
+constexpr size_t kSlabBytes = size_t(256) << 20;   // of ds
+
+template <int PV>
+constexpr int group_tiles() { return PV == 64 ? 4 : 8; }   // JTG
+
+__device__ __forceinline__ f32x4_t mfma_f32(float a, float b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4_t mfma_f32x4(float4 a, float4 b, f32x4_t c) {
+  c = mfma_f32(a.x, b.x, c);
+  c = mfma_f32(a.y, b.y, c);
+  c = mfma_f32(a.z, b.z, c);
+  return mfma_f32(a.w, b.w, c);
+}
+
+// 16 bytes (or their zero-padded tail) of a row of `d` elements from element t
+template <typename T, bool VEC>
+__device__ __forceinline__ uint4 row16(const T* row, int t, int d) {
+  constexpr int E = 16 / sizeof(T);
+  if constexpr (VEC) {
+    const uint4 v = *reinterpret_cast<const uint4*>(row + min(t, d - E));
+    return t < d ? v : make_uint4(0, 0, 0, 0);
+  } else {
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const T x = row[min(t + e, d - 1)];
+      uint32_t bits;
+      if constexpr (sizeof(T) == 4) bits = __float_as_uint(x);
+      else bits = x;
+      if (t + e >= d) bits = 0;
+      if constexpr (sizeof(T) == 4) w[e] = bits;
+      else w[e / 2] |= bits << (16 * (e & 1));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ f32x4_t mma16(uint4 a, uint4 b, f32x4_t c) {
+  if constexpr (sizeof(T) == 4)
+    return mfma_f32x4(__builtin_bit_cast(float4, a), __builtin_bit_cast(float4, b), c);
+  else
+    return mfma_bf16(a, b, c);
+}
+
+// v as two bf16 terms, hi in the low half
+__device__ __forceinline__ uint32_t split_bf16(float v) {
+  const __bf16 hi = static_cast<__bf16>(v);
+  const __bf16 lo = static_cast<__bf16>(v - static_cast<float>(hi));
+  return static_cast<uint32_t>(__builtin_bit_cast(uint16_t, hi)) |
+         static_cast<uint32_t>(__builtin_bit_cast(uint16_t, lo)) << 16;
+}
+
+struct GradDims {
+  int QB, upq_log2;        // queries of a tile, log2 of its 16-item units a query
+  int TI, TIP;             // items of a tile, floats of an LDS row of s
+  int n0, ns;              // the slab's first item, its items (a multiple of TI)
+  int qsplits;             // query ranges: blockIdx.y
+  int group;               // hidden units 16 JTG group .. of dW1, dW2
+  long m;                  // B Pq
+};
+
+// Per-workgroup sums in the workspace.
+struct GradParts {
+  uint32_t* ds;            // [Px][B Pq][ns]
+  float* da_q;             // [ns / 16][B][P]
+  float* da_x;             // [qsplits][ns][P]
+  float* dW1;              // [workgroups][H][P]
+  float* dW2;              // [workgroups][P][H]
+  float* db1;              // [workgroups][H]
+};
+
+template <int PV>
+constexpr int op_tiles() { return PV / 16; }   // 1 KB blocks of prepared weights per 16 hidden units and matrix
+
+// floats of LDS; weights: the four prepared operand matrices, us: the units' u
+template <int PV>
+size_t grad_lds(int JT, bool weights, bool us, const GradDims& dm) {
+  return (weights ? 4ul * JT * op_tiles<PV>() * 256 : 0) + 16ul * JT + dm.QB * PV + dm.TI * (PV + 4) +
+         static_cast<size_t>(dm.QB) * PV * dm.TIP + (us ? 256ul * kWaves * JT : 0) + kWaves * 2 * 256 + PV + 256;
+}
+
+// prepared operands of 16x16x4 f32 MFMAs, 64 lanes x 4 floats a block:
+// W1 and W2T (A operands with K = p), W2 and W1T (K = j), see k_mol_f32
+template <typename T, int PV>
+__device__ __forceinline__ float prepared(const T* W1, const T* W2, int P, int H, int which, int jt, int m, int lane,
+                                          int e) {
+  constexpr int RUN = PV / 4;
+  const int c = lane & 15, g = lane >> 4;
+  if (which < 2) {
+    const int j = 16 * jt + c, p = RUN * g + 4 * m + e;
+    if (j >= H || p >= P) return 0.f;
+    return which == 0 ? to_f32(W1[j * P + p]) : to_f32(W2[p * H + j]);
+  }
+  const int p = RUN * (c >> 2) + 4 * m + (c & 3), j = 16 * jt + 4 * g + e;
+  if (j >= H || p >= P) return 0.f;
+  return which == 2 ? to_f32(W2[p * H + j]) : to_f32(W1[j * P + p]);
+}
+
+}  // namespace
+
+// The four prepared matrices in the workspace, for MLPs too wide for LDS.
+template <typename T, int PV>
+__global__ __launch_bounds__(256) void k_grad_weights(DevProb pr, int JT, float* __restrict__ out) {
+  const int i = blockIdx.x * 256 + threadIdx.x, per = JT * op_tiles<PV>() * 256;
+  if (i >= 4 * per) return;
+  const int which = i / per, r = i - which * per, e = r & 3, lane = (r >> 2) & 63, blk = r >> 8;
+  out[i] = prepared<T, PV>(static_cast<const T*>(pr.W1), static_cast<const T*>(pr.W2), pr.P, pr.H, which,
+                           blk / op_tiles<PV>(), blk % op_tiles<PV>(), lane, e);
+}
+
+template <typename T, int PV, bool VEC>
+__global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims dm, const float* __restrict__ dphi,
+                                                            const float* __restrict__ wglob,
+                                                            float* __restrict__ uglob, GradParts out) {
+  constexpr int RUN = PV / 4, PT = PV / 16, E = 16 / sizeof(T), KCH = 4 * E, JTG = group_tiles<PV>();
+  extern __shared__ __attribute__((aligned(16))) float smf[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  const int P = pr.P, H = pr.H, d = pr.d, N = pr.N, JT = (H + 15) / 16;
+  const int QB = dm.QB, TI = dm.TI, TIP = dm.TIP;
+  const int wsize = JT * PT * 256;
+  float* sW = smf;                                                     // prepared weights, or nothing
+  float* sB1 = sW + (wglob ? 0 : 4 * wsize);
+  float* sC = sB1 + 16 * JT;                                           // a_q + b2, -inf past P
+  float* sAx = sC + QB * PV;
+  float* sS = sAx + TI * (PV + 4);
+  float* sU = sS + QB * PV * TIP + (wave * JT) * 256 + lane * 4;       // the lane's u, 16 bytes a block
+  float* sT0 = sS + QB * PV * TIP + (uglob ? 0 : 256 * kWaves * JT);
+  const long wg = static_cast<long>(blockIdx.y) * gridDim.x + blockIdx.x;
+  float4* gU = reinterpret_cast<float4*>(uglob) + (wg * kWaves + wave) * JT * 64 + lane;   // the same, where LDS has no room
+  float* sT = sT0 + wave * 512;                                        // du and h of 16 hidden units, [16][16 items] each
+  uint32_t* sOff = reinterpret_cast<uint32_t*>(sT0 + kWaves * 512);    // ds offset of p
+  int* sRow = reinterpret_cast<int*>(sOff + PV);                       // s row of each query vector (QB P_q <= 256)
+  const float4* w1 = reinterpret_cast<const float4*>(wglob ? wglob : sW) + lane;
+  const float4* w2t = w1 + wsize / 4;
+  const float4* w2 = w2t + wsize / 4;
+  const float4* w1t = w2 + wsize / 4;
+  const T* X = static_cast<const T*>(pr.X);
+  const T* Q = static_cast<const T*>(pr.Q);
+
+  if (!wglob)
+    for (int i = tid; i < 4 * wsize; i += kThreads) {
+      const int which = i / wsize, r = i - which * wsize, blk = r >> 8;
+      sW[i] = prepared<T, PV>(static_cast<const T*>(pr.W1), static_cast<const T*>(pr.W2), P, H, which, blk / PT,
+                              blk % PT, (r >> 2) & 63, r & 3);
+    }
+  for (int i = tid; i < 16 * JT; i += kThreads) sB1[i] = i < H ? pr.b1[i] : 0.f;
+  for (int i = tid; i < QB * PV * TIP; i += kThreads) sS[i] = 0.f;
+  for (int i = tid; i < PV; i += kThreads)
+    sOff[i] = i < P ? static_cast<uint32_t>((i % pr.Px * dm.m + i / pr.Px) * dm.ns) : 0xFFFFFFFFu;
+  for (int i = tid; i < (QB * pr.Pq + 31) / 32 * 32; i += kThreads)
+    sRow[i] = i < QB * pr.Pq ? (i / pr.Pq * PV + i % pr.Pq * pr.Px) * TIP : -1;
+  const int i0 = blockIdx.x * TI;                                      // the tile's first item of the slab
+  auto item_of = [&](int i) { return min(dm.n0 + i0 + i, N - 1); };
+  for (int i = tid; i < TI * (PV + 4); i += kThreads) {
+    const int n = i / (PV + 4), p = i - n * (PV + 4);
+    sAx[i] = p < P ? pr.a_x[static_cast<long>(item_of(n)) * P + p] : 0.f;
+  }
+
+  const int q = wave >> dm.upq_log2, it = 16 * (wave & ((1 << dm.upq_log2) - 1)) + c;
+  const int slot = i0 + it;                                            // of the slab
+  const bool has_item = dm.n0 + slot < N;
+  f32x4_t aw1[JTG][PT] = {}, aw2[JTG][PT] = {};
+  float ab1[JTG] = {}, dax[RUN] = {};
+  const int nqb = (pr.B + QB - 1) / QB;
+  const int qb0 = static_cast<int>(static_cast<long>(nqb) * blockIdx.y / dm.qsplits);
+  const int qb1 = static_cast<int>(static_cast<long>(nqb) * (blockIdx.y + 1) / dm.qsplits);
+  for (int qb = qb0; qb < qb1; ++qb) {
+    const int b0 = qb * QB, nq = min(QB, pr.B - b0);
+    __syncthreads();                                                   // the previous tile's units are done
+    for (int i = tid; i < QB * PV; i += kThreads) {
+      const int p = i % PV, b = min(b0 + i / PV, pr.B - 1);
+      sC[i] = p < P ? pr.a_q[static_cast<long>(b) * P + p] + pr.b2[p] : -__builtin_inff();
+    }
+    const int b = b0 + q;
+    const bool live = q < nq && has_item;
+    const float gr = live ? dphi[static_cast<long>(b) * N + dm.n0 + slot] : 0.f;
+    // 1. dot products: jobs of (item component, 32 items, 32 vector rows)
+    const int nvec = nq * pr.Pq, nrt = (nvec + 31) / 32, nct = TI / 32;
+    for (int job = wave; job < pr.Px * nrt * nct; job += kWaves) {
+      const int ct = job % nct, jr = job / nct, px = jr / nrt, rt = jr - px * nrt;
+      const T* qv = Q + static_cast<long>(b0) * pr.Pq * d;
+      const T* q0 = qv + static_cast<long>(min(32 * rt + c, nvec - 1)) * d;
+      const T* q1 = qv + static_cast<long>(min(32 * rt + 16 + c, nvec - 1)) * d;
+      const T* Xp = X + static_cast<long>(px) * N * d;
+      const T* x0 = Xp + static_cast<long>(item_of(32 * ct + c)) * d;
+      const T* x1 = Xp + static_cast<long>(item_of(32 * ct + 16 + c)) * d;
+      f32x4_t acc[2][2] = {};
+      for (int k0 = 0; k0 < d; k0 += KCH) {
+        const int t = k0 + g * E;
+        const uint4 xa = row16<T, VEC>(x0, t, d), xb = row16<T, VEC>(x1, t, d);
+        const uint4 qa = row16<T, VEC>(q0, t, d), qc = row16<T, VEC>(q1, t, d);
+        acc[0][0] = mma16<T>(qa, xa, acc[0][0]);
+        acc[0][1] = mma16<T>(qa, xb, acc[0][1]);
+        acc[1][0] = mma16<T>(qc, xa, acc[1][0]);
+        acc[1][1] = mma16<T>(qc, xb, acc[1][1]);
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int v = 32 * rt + 16 * r + 4 * g;
+        const int4 row = *reinterpret_cast<const int4*>(sRow + v);
+        const int ro[4] = {row.x, row.y, row.z, row.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (v + i < nvec) {
+            float* dst = sS + ro[i] + px * TIP + 32 * ct + c;
+            dst[0] = acc[r][0][i];
+            dst[16] = acc[r][1][i];
+          }
+      }
+    }
+    __syncthreads();
+
+    // 2. the wave's unit (queries past the batch: g = 0 on the last tile's s)
+    float dl[RUN];
+    f32x4_t ds[PT];
+    float4 sv[PT];                                                     // s[16 pt + c][4 g ..]: K = items
+    {
+      float s[RUN];
+      const float* src = sS + (q * PV + RUN * g) * TIP + it;
+#pragma unroll
+      for (int mu = 0; mu < RUN; ++mu) s[mu] = src[mu * TIP];
+#pragma unroll
+      for (int pt = 0; pt < PT; ++pt)
+        sv[pt] = *reinterpret_cast<const float4*>(sS + (q * PV + 16 * pt + c) * TIP + it - c + 4 * g);
+      f32x4_t l[PT];
+      const float* ax = sAx + it * (PV + 4) + RUN * g;
+#pragma unroll
+      for (int pt = 0; pt < PT; ++pt) {
+        const float4 cq = *reinterpret_cast<const float4*>(sC + q * PV + RUN * g + 4 * pt);
+        const float4 a = *reinterpret_cast<const float4*>(ax + 4 * pt);
+        l[pt] = f32x4_t{cq.x + a.x, cq.y + a.y, cq.z + a.z, cq.w + a.w};
+      }
+      for (int jt = 0; jt < JT; ++jt) {
+        const float4 bj = *reinterpret_cast<const float4*>(sB1 + 16 * jt + 4 * g);
+        f32x4_t u = f32x4_t{bj.x, bj.y, bj.z, bj.w};
+#pragma unroll
+        for (int m = 0; m < PT; ++m)
+          u = mfma_f32x4(w1[(jt * PT + m) * 64], float4{s[4 * m], s[4 * m + 1], s[4 * m + 2], s[4 * m + 3]}, u);
+        if (uglob) gU[jt * 64] = float4{u[0], u[1], u[2], u[3]};
+        else *reinterpret_cast<float4*>(sU + jt * 256) = float4{u[0], u[1], u[2], u[3]};
+        float h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          h[i] = u[i] * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u[i]));
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt)
+          l[pt] = mfma_f32x4(w2[(jt * PT + pt) * 64], float4{h[0], h[1], h[2], h[3]}, l[pt]);
+      }
+      float mx = l[0][0];
+#pragma unroll
+      for (int mu = 0; mu < RUN; ++mu) mx = fmaxf(mx, l[mu / 4][mu % 4]);
+      mx = max_groups(mx);
+      float den = 0.f, num = 0.f;
+#pragma unroll
+      for (int mu = 0; mu < RUN; ++mu) {
+        const float w = __builtin_amdgcn_exp2f(kLog2e * (l[mu / 4][mu % 4] - mx));   // 0 past P
+        l[mu / 4][mu % 4] = w;
+        den += w;
+        num = fmaf(w, s[mu], num);
+      }
+      const float rden = 1.f / sum_groups(den), phi = sum_groups(num) * rden, gw = gr * rden;
+#pragma unroll
+      for (int mu = 0; mu < RUN; ++mu) {
+        const float gpi = gw * l[mu / 4][mu % 4];
+        ds[mu / 4][mu % 4] = gpi;
+        dl[mu] = gpi * (s[mu] - phi);
+        dax[mu] += dl[mu];
+      }
+    }
+    // dl in the place of the unit's s, read back with K = items
+    {
+      float* dst = sS + (q * PV + RUN * g) * TIP + it;
+#pragma unroll
+      for (int mu = 0; mu < RUN; ++mu) dst[mu * TIP] = dl[mu];
+    }
+    wave_lds_sync();
+    float4 dv[PT];
+    float rowsum = 0.f;                                                // sum over the items, p = 16 g' + c of lane group g'
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt) {
+      dv[pt] = *reinterpret_cast<const float4*>(sS + (q * PV + 16 * pt + c) * TIP + it - c + 4 * g);
+      const float t = sum_groups((dv[pt].x + dv[pt].y) + (dv[pt].z + dv[pt].w));
+      if (g == pt) rowsum = t;
+    }
+    if (dm.group == 0 && q < nq && 16 * g + c < P && g < PT)
+      out.da_q[(static_cast<long>((i0 >> 4) + (wave & ((1 << dm.upq_log2) - 1))) * pr.B + b) * P + 16 * g + c] = rowsum;
+
+    for (int jg = 0; jg < JT; jg += JTG) {
+      const bool mine = jg == dm.group * JTG;                          // accumulates dW1, dW2
+#pragma unroll
+      for (int jj = 0; jj < JTG; ++jj) {
+        const int jt = jg + jj;
+        if (jt >= JT) break;
+        f32x4_t dh = {};
+#pragma unroll
+        for (int m = 0; m < PT; ++m)
+          dh = mfma_f32x4(w2t[(jt * PT + m) * 64], float4{dl[4 * m], dl[4 * m + 1], dl[4 * m + 2], dl[4 * m + 3]}, dh);
+        float4 u;
+        if (uglob) u = gU[jt * 64];
+        else u = *reinterpret_cast<const float4*>(sU + jt * 256);
+        const float uu[4] = {u.x, u.y, u.z, u.w};
+        float du[4], h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float sig = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * uu[i]));
+          h[i] = uu[i] * sig;
+          du[i] = dh[i] * fmaf(h[i], 1.f - sig, sig);                  // sig (1 + u (1 - sig))
+        }
+        if (dm.group == 0) {
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt)
+            ds[pt] = mfma_f32x4(w1t[(jt * PT + pt) * 64], float4{du[0], du[1], du[2], du[3]}, ds[pt]);
+        }
+        if (mine) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sT[(4 * g + i) * 16 + c] = du[i];
+            sT[256 + (4 * g + i) * 16 + c] = h[i];
+          }
+          wave_lds_sync();
+          const float4 duv = *reinterpret_cast<const float4*>(sT + c * 16 + 4 * g);
+          const float4 hv = *reinterpret_cast<const float4*>(sT + 256 + c * 16 + 4 * g);
+          ab1[jj] += (duv.x + duv.y) + (duv.z + duv.w);
+#pragma unroll
+          for (int pt = 0; pt < PT; ++pt) {
+            aw1[jj][pt] = mfma_f32x4(duv, sv[pt], aw1[jj][pt]);
+            aw2[jj][pt] = mfma_f32x4(dv[pt], hv, aw2[jj][pt]);
+          }
+          wave_lds_sync();
+        }
+      }
+    }
+    if (dm.group == 0 && q < nq) {
+      // pairs past the corpus end are stored as zeros (g = 0)
+      const long base = static_cast<long>(b) * pr.Pq * dm.ns + slot;
+#pragma unroll
+      for (int mu = 0; mu < RUN; ++mu) {
+        const uint32_t off = sOff[RUN * g + mu];
+        const float v = ds[mu / 4][mu % 4];
+        if (RUN * g + mu < P) out.ds[base + off] = sizeof(T) == 4 ? __float_as_uint(v) : split_bf16(v);
+      }
+    }
+  }
+
+  // the workgroup's sums: waves in turn, in LDS, in the place of the rest
+  float* acc = smf;                                                    // [2][JTG][PT][64][4], then [JTG][16], then [TI][PV]
+  for (int w = 0; w < kWaves; ++w) {
+    __syncthreads();
+    if (wave == w) {
+#pragma unroll
+      for (int jj = 0; jj < JTG; ++jj) {
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) {
+          f32x4_t* a = reinterpret_cast<f32x4_t*>(acc) + (jj * PT + pt) * 64 + lane;
+          f32x4_t* b = a + JTG * PT * 64;
+          *a = w ? *a + aw1[jj][pt] : aw1[jj][pt];
+          *b = w ? *b + aw2[jj][pt] : aw2[jj][pt];
+        }
+        const float t = sum_groups(ab1[jj]);
+        float* o = acc + 2 * JTG * PT * 256 + 16 * jj + c;
+        if (g == 0) *o = w ? *o + t : t;
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < JTG * PT * 256; i += kThreads) {
+    // block (jj, pt), lane l, register r: row 4 (l / 16) + r, column l % 16
+    const int r = i & 3, l = (i >> 2) & 63, blk = i >> 8, jj = blk / PT, pt = blk - jj * PT;
+    const int row = 4 * (l >> 4) + r, colm = l & 15, jb = 16 * (dm.group * JTG + jj);
+    const int j1 = jb + row, p1 = 16 * pt + colm, j2 = jb + colm, p2 = 16 * pt + row;
+    if (j1 < H && p1 < P) out.dW1[(wg * H + j1) * P + p1] = acc[i];
+    if (j2 < H && p2 < P) out.dW2[(wg * P + p2) * H + j2] = acc[JTG * PT * 256 + i];
+  }
+  for (int i = tid; i < 16 * JTG; i += kThreads) {
+    const int j = 16 * dm.group * JTG + i;
+    if (j < H) out.db1[wg * H + j] = acc[2 * JTG * PT * 256 + i];
+  }
+  if (dm.group) return;
+  // da_x: the waves of a tile's queries in turn
+  for (int w = 0; w < QB; ++w) {
+    __syncthreads();
+    if (q == w) {
+#pragma unroll
+      for (int mu = 0; mu < RUN; ++mu) {
+        float* o = acc + it * (PV + 1) + RUN * g + mu;
+        *o = w ? *o + dax[mu] : dax[mu];
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < TI * P; i += kThreads) {
+    const int n = i / P, p = i - n * P;
+    out.da_x[(static_cast<long>(blockIdx.y) * dm.ns + i0 + n) * P + p] = acc[n * (PV + 1) + p];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// [batch][rows][d] -> [batch][d][ld], zero from `rows` to `ld`; in_stride: elements a batch.
+template <typename T>
+__global__ __launch_bounds__(256) void k_transpose(const T* __restrict__ in, long in_stride, long row0, int rows,
+                                                   int d, int ld, T* __restrict__ out) {
+  __shared__ T tile[32][33];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const long r0 = static_cast<long>(blockIdx.x) * 32;
+  const int t0 = blockIdx.y * 32;
+  const T* src = in + blockIdx.z * in_stride + row0 * d;
+  T* dst = out + blockIdx.z * static_cast<long>(d) * ld;
+  for (int k = y; k < 32; k += 8) {
+    T v = 0;
+    if (r0 + k < rows && t0 + x < d) v = src[(r0 + k) * d + t0 + x];
+    tile[k][x] = v;
+  }
+  __syncthreads();
+  for (int k = y; k < 32; k += 8)
+    if (t0 + k < d && r0 + x < ld) dst[static_cast<long>(t0 + k) * ld + r0 + x] = tile[x][k];
+}
+
+// Products with ds on matrix cores: out[m][t] = sum_k A[m][k] Bt[t][k].
+// COLS false (dQ): m = (b, pq), k = (px, item): A rows run along k.
+// COLS true (dX): one px a batch, m = item, k = (b, pq): A columns run along m.
+// A wave has 32 rows and 64 columns; K chunks of `KCH` are split over
+// blockIdx.z's ranges, whose sums are separate parts.
+struct GemmDims {
+  int m, d;
+  long lda;                // elements of a row of ds
+  long a_px;               // elements between item components of ds
+  int k_px, kvalid;        // K of one px (padded), valid ones (COLS)
+  int npx;                 // px of the K loop (dQ) or of the batch (dX)
+  long b_px;               // elements between px of Bt (0: the same)
+  int ldb;
+  int splits;
+  int add;                 // to the parts of the slab before
+  long out_px, out_split;  // floats between px (dX), between splits
+};
+template <typename T, bool COLS>
+__global__ __launch_bounds__(256) void k_grad_gemm(GemmDims gd, const uint32_t* __restrict__ ds,
+                                                   const T* __restrict__ Bt, float* __restrict__ out) {
+  constexpr int E = 16 / sizeof(T), KCH = 4 * E, RB = 2, CB = 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int m0 = (blockIdx.x * 4 + wave) * 16 * RB, t0 = blockIdx.y * 16 * CB;
+  if (m0 >= gd.m) return;
+  const int split = blockIdx.z % gd.splits, px0 = COLS ? blockIdx.z / gd.splits : 0;
+  const int per = gd.k_px / KCH, chunks = COLS ? per : per * gd.npx;
+  const int k0 = static_cast<int>(static_cast<long>(chunks) * split / gd.splits);
+  const int k1 = static_cast<int>(static_cast<long>(chunks) * (split + 1) / gd.splits);
+  f32x4_t acc[RB][CB] = {};
+  int row[RB], col[CB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) row[r] = min(m0 + 16 * r + c, gd.m - 1);
+#pragma unroll
+  for (int t = 0; t < CB; ++t) col[t] = min(t0 + 16 * t + c, gd.d - 1);
+  for (int ch = k0; ch < k1; ++ch) {
+    const int px = COLS ? px0 : ch / per, k = (COLS ? ch : ch - px * per) * KCH + g * E;
+    const uint32_t* A = ds + px * gd.a_px;
+    const T* B = Bt + px * gd.b_px + k;
+    uint32_t a[RB][E];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      if constexpr (COLS) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const uint32_t v = A[min(k + e, gd.kvalid - 1) * gd.lda + row[r]];
+          a[r][e] = k + e < gd.kvalid ? v : 0;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+          const uint4 v = *reinterpret_cast<const uint4*>(A + row[r] * gd.lda + k + e);
+          a[r][e] = v.x;
+          a[r][e + 1] = v.y;
+          a[r][e + 2] = v.z;
+          a[r][e + 3] = v.w;
+        }
+      }
+    }
+    uint4 bv[CB];
+#pragma unroll
+    for (int t = 0; t < CB; ++t) bv[t] = *reinterpret_cast<const uint4*>(B + static_cast<long>(col[t]) * gd.ldb);
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      if constexpr (sizeof(T) == 4) {
+        const uint4 av = make_uint4(a[r][0], a[r][1], a[r][2], a[r][3]);
+#pragma unroll
+        for (int t = 0; t < CB; ++t) acc[r][t] = mma16<T>(av, bv[t], acc[r][t]);
+      } else {
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          hi[e] = __builtin_amdgcn_perm(a[r][2 * e + 1], a[r][2 * e], 0x05040100u);
+          lo[e] = __builtin_amdgcn_perm(a[r][2 * e + 1], a[r][2 * e], 0x07060302u);
+        }
+        const uint4 ah = make_uint4(hi[0], hi[1], hi[2], hi[3]), al = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+#pragma unroll
+        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(al, bv[t], acc[r][t]);
+#pragma unroll
+        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(ah, bv[t], acc[r][t]);
+      }
+    }
+  }
+  float* dst = out + px0 * gd.out_px + split * gd.out_split;
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int t = 0; t < CB; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int m = m0 + 16 * r + 4 * g + i, x = t0 + 16 * t + c;
+        if (m < gd.m && x < gd.d) {
+          float* o = dst + static_cast<long>(m) * gd.d + x;
+          *o = gd.add ? *o + acc[r][t][i] : acc[r][t][i];
+        }
+      }
+}
+
+// ---------------------------------------------------------------------------
+// Sums of partial results: out[o] = sum over s < S of in[s * stride + o], as
+// float32 (added to what an earlier slab left in acc) and, where wanted, in the
+// output's type.  Column groups of 64, four runs of s in a block.
+struct SumJob {
+  const float* in;
+  long L, stride;          // columns, floats between parts
+  int S;
+  int blocks;              // of 64 columns
+  float* acc;              // NULL, or float32 sums kept between slabs
+  int add;
+  void* out;               // NULL, or the output: o of batch o / batch_in goes to batch_out floats a batch
+  int bf16;
+  long in_len, out_len;    // elements of a batch (a px of dX): in the parts, in the output
+  long out_at;             // first element within a batch
+};
+constexpr int kSumJobs = 8;
+struct SumArgs {
+  int n;
+  int first[kSumJobs + 1];
+  SumJob job[kSumJobs];
+};
+
+__global__ __launch_bounds__(256) void k_sum_parts(SumArgs a) {
+  __shared__ float sh[4][64];
+  int j = 0;
+  while (j + 1 < a.n && a.first[j + 1] <= static_cast<int>(blockIdx.x)) ++j;
+  const SumJob& s = a.job[j];
+  const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
+  const long o = (static_cast<long>(blockIdx.x) - a.first[j]) * 64 + lane;
+  float v = 0.f;
+  if (o < s.L) {
+    const int k0 = static_cast<int>(static_cast<long>(s.S) * run / 4), k1 = static_cast<int>(static_cast<long>(s.S) * (run + 1) / 4);
+#pragma unroll 8
+    for (int k = k0; k < k1; ++k) v += s.in[k * s.stride + o];
+  }
+  sh[run][lane] = v;
+  __syncthreads();
+  if (run || o >= s.L) return;
+  v = (sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane]);
+  if (s.add) v += s.acc[o];
+  if (s.acc) s.acc[o] = v;
+  if (s.out) {
+    const long bt = o / s.in_len, at = bt * s.out_len + s.out_at + (o - bt * s.in_len);
+    if (s.bf16)
+      static_cast<bf16_t*>(s.out)[at] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+    else
+      static_cast<float*>(s.out)[at] = v;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+namespace {
+
+struct GradPlan {
+  GradDims dm;
+  int JT, groups, slab, slabs;
+  bool wlds, ulds;                      // prepared weights and the units' u in LDS
+  size_t lds;
+  int sp_q, sp_x, ldq;                  // K splits of dQ and dX, row length of Q transposed
+  size_t off_w, off_u, off_ds, off_xt, off_qt, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_pq, off_px, off_acc, bytes;
+  long a_daq, a_dw1, a_dw2, a_db1;      // floats into the accumulators
+  int wgs;
+};
+
+// parts of a product of `waves` waves a part, at least `chunks_min` K chunks each
+int split_of(long waves, long chunks, long chunks_min) {
+  return static_cast<int>(std::max<long>(1, std::min({(2048 + waves - 1) / waves, chunks / chunks_min, 64l})));
+}
+
+template <typename T, int PV>
+GradPlan plan_grad(const DevProb& pr) {
+  GradPlan f{};
+  f.JT = (pr.H + 15) / 16;
+  f.groups = (f.JT + group_tiles<PV>() - 1) / group_tiles<PV>();
+  GradDims& dm = f.dm;
+  dm.QB = pr.B >= 4 ? 4 : pr.B >= 2 ? 2 : 1;
+  dm.upq_log2 = dm.QB == 4 ? 1 : dm.QB == 2 ? 2 : 3;
+  dm.TI = kPairs / dm.QB;
+  dm.TIP = dm.TI + 4;
+  dm.m = static_cast<long>(pr.B) * pr.Pq;
+  // LDS has room for both up to P H = 4096; u is the less to read from the caches
+  constexpr size_t most = 160 * 1024 / 4;
+  f.ulds = grad_lds<PV>(f.JT, true, true, dm) <= most;
+  f.wlds = grad_lds<PV>(f.JT, true, f.ulds, dm) <= most;
+  if (!f.wlds) f.ulds = grad_lds<PV>(f.JT, false, true, dm) <= most;
+  f.lds = grad_lds<PV>(f.JT, f.wlds, f.ulds, dm) * 4;
+  // the final sums take the same place: JTG blocks of dW1, dW2 and db1, then [TI][PV + 1] of da_x
+  f.lds = std::max<size_t>(f.lds, 4 * (2ul * group_tiles<PV>() * (PV / 16) * 256 + 16 * group_tiles<PV>()));
+  f.lds = std::max<size_t>(f.lds, 4ul * dm.TI * (PV + 1));
+  const long per_item = 4l * pr.Px * dm.m;
+  const long tiles = (static_cast<long>(pr.N) + dm.TI - 1) / dm.TI;
+  const long fit = std::max<long>(1, static_cast<long>(kSlabBytes) / (per_item * dm.TI));
+  f.slabs = static_cast<int>((tiles + fit - 1) / fit);
+  f.slab = static_cast<int>((tiles + f.slabs - 1) / f.slabs * dm.TI);
+  f.slabs = static_cast<int>((static_cast<long>(pr.N) + f.slab - 1) / f.slab);
+  dm.ns = f.slab;
+  const int st = f.slab / dm.TI, nqb = (pr.B + dm.QB - 1) / dm.QB;
+  dm.qsplits = std::max(1, std::min(nqb, 256 / st));
+  f.wgs = st * dm.qsplits;
+  constexpr int KCH = 64 / sizeof(T);
+  f.ldq = static_cast<int>((dm.m + 31) / 32 * 32);
+  const long cg = (pr.d + 63) / 64;
+  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * f.slab / KCH, 8);
+  f.sp_x = split_of((f.slab + 31l) / 32 * cg * pr.Px, f.ldq / KCH, 8);
+  auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+  size_t at = 0;
+  const size_t P = pr.P, H = pr.H;
+  f.off_w = at;   at = up(at + (f.wlds ? 0 : 16ul * f.JT * (PV / 16) * 256));
+  f.off_u = at;   at = up(at + (f.ulds ? 0 : 1024ul * f.wgs * kWaves * f.JT));
+  f.off_ds = at;  at = up(at + 4ul * pr.Px * dm.m * f.slab);
+  f.off_xt = at;  at = up(at + sizeof(T) * pr.Px * pr.d * static_cast<size_t>(f.slab));
+  f.off_qt = at;  at = up(at + sizeof(T) * pr.d * static_cast<size_t>(f.ldq));
+  f.off_daq = at; at = up(at + 4ul * (f.slab / 16) * pr.B * P);
+  f.off_dax = at; at = up(at + 4ul * dm.qsplits * f.slab * P);
+  f.off_dw1 = at; at = up(at + 4ul * f.wgs * H * P);
+  f.off_dw2 = at; at = up(at + 4ul * f.wgs * H * P);
+  f.off_db1 = at; at = up(at + 4ul * f.wgs * H);
+  f.off_pq = at;  at = up(at + 4ul * f.sp_q * dm.m * pr.d);
+  f.off_px = at;  at = up(at + 4ul * f.sp_x * pr.Px * static_cast<size_t>(f.slab) * pr.d);
+  f.a_daq = 0;
+  f.a_dw1 = f.a_daq + static_cast<long>(pr.B) * P;
+  f.a_dw2 = f.a_dw1 + static_cast<long>(H * P);
+  f.a_db1 = f.a_dw2 + static_cast<long>(H * P);
+  f.off_acc = at; at = up(at + 4ul * (f.a_db1 + H));
+  f.bytes = at;
+  return f;
+}
+
+struct SumList {
+  SumArgs a{};
+  hipStream_t st;
+  void add(const SumJob& j) {
+    a.job[a.n] = j;
+    a.job[a.n].blocks = static_cast<int>((j.L + 63) / 64);
+    a.first[a.n + 1] = a.first[a.n] + a.job[a.n].blocks;
+    ++a.n;
+  }
+  hipError_t run() {
+    if (a.n) hipLaunchKernelGGL(k_sum_parts, dim3(a.first[a.n]), dim3(256), 0, st, a);
+    a.n = 0;
+    return hipGetLastError();
+  }
+};
+
+template <typename T, int PV>
+hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads& o, char* ws, hipStream_t st) {
+  const GradPlan f = plan_grad<T, PV>(pr);
+  const int bf = sizeof(T) == 2;
+  GradDims dm = f.dm;
+  auto F = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
+  GradParts parts{reinterpret_cast<uint32_t*>(ws + f.off_ds), F(f.off_daq), F(f.off_dax), F(f.off_dw1), F(f.off_dw2),
+                  F(f.off_db1)};
+  T* xt = reinterpret_cast<T*>(ws + f.off_xt);
+  T* qt = reinterpret_cast<T*>(ws + f.off_qt);
+  float* acc = F(f.off_acc);
+  const float* wglob = nullptr;
+  if (!f.wlds) {
+    wglob = F(f.off_w);
+    hipLaunchKernelGGL((k_grad_weights<T, PV>), dim3(4 * f.JT * (PV / 16)), dim3(256), 0, st, pr, f.JT, F(f.off_w));
+  }
+  const bool vec = (pr.d * sizeof(T)) % 16 == 0 &&
+                   ((reinterpret_cast<uintptr_t>(pr.Q) | reinterpret_cast<uintptr_t>(pr.X)) & 15) == 0;
+  auto kern = vec ? &k_score_grad<T, PV, true> : &k_score_grad<T, PV, false>;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                     static_cast<int>(f.lds));
+  if (e != hipSuccess) return e;
+  const int dt = (pr.d + 31) / 32, cg = (pr.d + 63) / 64;
+  if (o.dX)
+    hipLaunchKernelGGL(k_transpose<T>, dim3((f.ldq + 31) / 32, dt, 1), dim3(256), 0, st, static_cast<const T*>(pr.Q), 0l,
+                       0l, static_cast<int>(dm.m), pr.d, f.ldq, qt);
+  SumList sums;
+  sums.st = st;
+  for (int sl = 0; sl < f.slabs; ++sl) {
+    const bool last = sl + 1 == f.slabs;
+    dm.n0 = sl * f.slab;
+    const int items = std::min(f.slab, pr.N - dm.n0);
+    for (int grp = 0; grp < f.groups; ++grp) {
+      dm.group = grp;
+      if (grp && !o.dW1 && !o.dW2 && !o.db1) break;
+      hipLaunchKernelGGL(kern, dim3(f.slab / dm.TI, dm.qsplits), dim3(kThreads), f.lds, st, pr, dm, dphi, wglob,
+                         f.ulds ? nullptr : F(f.off_u), parts);
+    }
+    const long P = pr.P, H = pr.H, BP = pr.B * P;
+    if (o.dQ) {
+      hipLaunchKernelGGL(k_transpose<T>, dim3(f.slab / 32, dt, pr.Px), dim3(256), 0, st, static_cast<const T*>(pr.X),
+                         static_cast<long>(pr.N) * pr.d, static_cast<long>(dm.n0), items, pr.d, f.slab, xt);
+      GemmDims gd{static_cast<int>(dm.m), pr.d, f.slab, dm.m * f.slab, f.slab, f.slab, pr.Px,
+                  static_cast<long>(pr.d) * f.slab, f.slab, f.sp_q, sl > 0, 0, dm.m * pr.d};
+      hipLaunchKernelGGL((k_grad_gemm<T, false>), dim3(static_cast<unsigned>((dm.m + 127) / 128), cg, f.sp_q), dim3(256),
+                         0, st, gd, parts.ds, xt, F(f.off_pq));
+      if (last)
+        sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, 0, nullptr, 0, o.dQ, bf, dm.m * pr.d, dm.m * pr.d, 0});
+    }
+    if (o.dX) {
+      const long per_px = static_cast<long>(items) * pr.d;
+      GemmDims gd{items, pr.d, f.slab, dm.m * f.slab, f.ldq, static_cast<int>(dm.m), pr.Px, 0, f.ldq, f.sp_x, 0, per_px,
+                  per_px * pr.Px};
+      hipLaunchKernelGGL((k_grad_gemm<T, true>), dim3((items + 127) / 128, cg, f.sp_x * pr.Px), dim3(256), 0, st, gd,
+                         parts.ds, qt, F(f.off_px));
+      sums.add({F(f.off_px), per_px * pr.Px, per_px * pr.Px, f.sp_x, 0, nullptr, 0, o.dX, bf, per_px,
+                static_cast<long>(pr.N) * pr.d, static_cast<long>(dm.n0) * pr.d});
+    }
+    if (o.da_q || o.db2)
+      sums.add({parts.da_q, BP, BP, f.slab / 16, 0, acc + f.a_daq, sl > 0, last ? o.da_q : nullptr, 0, BP, BP, 0});
+    if (o.da_x)
+      sums.add({parts.da_x, items * P, f.slab * P, dm.qsplits, 0, nullptr, 0, o.da_x, 0, items * P, items * P,
+                static_cast<long>(dm.n0) * P});
+    if (o.dW1)
+      sums.add({parts.dW1, H * P, H * P, f.wgs, 0, acc + f.a_dw1, sl > 0, last ? o.dW1 : nullptr, bf, H * P, H * P, 0});
+    if (o.dW2)
+      sums.add({parts.dW2, H * P, H * P, f.wgs, 0, acc + f.a_dw2, sl > 0, last ? o.dW2 : nullptr, bf, H * P, H * P, 0});
+    if (o.db1) sums.add({parts.db1, H, H, f.wgs, 0, acc + f.a_db1, sl > 0, last ? o.db1 : nullptr, 0, H, H, 0});
+    if ((e = sums.run()) != hipSuccess) return e;
+  }
+  if (o.db2) {
+    sums.add({acc + f.a_daq, pr.P, pr.P, pr.B, 0, nullptr, 0, o.db2, 0, pr.P, pr.P, 0});
+    if ((e = sums.run()) != hipSuccess) return e;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t score_grad_bytes(const DevProb& pr) {
+  if (pr.dtype == MOL_BF16)
+    return (pr.P <= 16 ? plan_grad<bf16_t, 16>(pr) : pr.P <= 32 ? plan_grad<bf16_t, 32>(pr) : plan_grad<bf16_t, 64>(pr)).bytes;
+  return (pr.P <= 16 ? plan_grad<float, 16>(pr) : pr.P <= 32 ? plan_grad<float, 32>(pr) : plan_grad<float, 64>(pr)).bytes;
+}
+
+hipError_t launch_score_grad(const DevProb& pr, const float* dphi, const mol_score_grads& o, void* ws, hipStream_t st) {
+  auto f = pr.dtype == MOL_BF16
+               ? (pr.P <= 16 ? &run_grad<bf16_t, 16> : pr.P <= 32 ? &run_grad<bf16_t, 32> : &run_grad<bf16_t, 64>)
+               : (pr.P <= 16 ? &run_grad<float, 16> : pr.P <= 32 ? &run_grad<float, 32> : &run_grad<float, 64>);
+  return f(pr, dphi, o, static_cast<char*>(ws), st);
+}
+
+}  // namespace mol

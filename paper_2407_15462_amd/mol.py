@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import torch
 
@@ -19,16 +19,22 @@ LIB_PATH = os.path.join(_HERE, "libmol.so")
 MOL_OK, MOL_EINVAL, MOL_EUNSUPPORTED, MOL_EWORKSPACE, MOL_EHIP = range(5)
 MOL_F32, MOL_BF16 = 0, 1
 (MOL_OP_SCORE, MOL_OP_TOPK_EXACT, MOL_OP_TOPK_PER_EMBD, MOL_OP_RERANK, MOL_OP_TOPK_MAXDOT,
- MOL_OP_TOPK_BOUNDED, MOL_OP_TOPK_TWO_PASS) = range(7)
+ MOL_OP_TOPK_BOUNDED, MOL_OP_TOPK_TWO_PASS, MOL_OP_SCORE_GRAD) = range(8)
 MOL_TWO_PASS_MIN, MOL_TWO_PASS_KTH = 0, 1
 MOL_FLAG_F32_GATING = 1
 MOL_FLAG_BF16X2_GATING = 2
+MOL_STATE_F32, MOL_STATE_E4M3 = 0, 1
+MOL_STATE_BLOCK = 256
 
 EXPORTS = ("mol_workspace_size", "mol_score", "mol_topk_exact", "mol_topk_exact_noalloc", "mol_topk_exact_bounded",
            "mol_topk_two_pass", "mol_topk_maxdot", "mol_topk_per_embd",
            "mol_rerank", "mol_avg_embed", "mol_gap_bound", "mol_gap_bound_combined",
+           "mol_embed_lookup", "mol_embed_grad_workspace", "mol_embed_grad",
+           "mol_softmax_loss_workspace", "mol_softmax_loss", "mol_score_grad", "mol_adamw_step",
            "mol_timing_enable", "mol_timing_read",
            "mol_status_str", "mol_last_error")
+
+_DTYPES = {torch.float32: MOL_F32, torch.bfloat16: MOL_BF16}
 
 
 class MolError(RuntimeError):
@@ -49,6 +55,24 @@ class MolProblemC(ctypes.Structure):
                 ("W2", ctypes.c_void_p), ("b2", ctypes.c_void_p), ("flags", ctypes.c_uint32)]
 
 
+class MolScoreGradsC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dQ", "dX", "da_q", "da_x", "dW1", "db1", "dW2", "db2")]
+
+
+class MolAdamwTensorC(ctypes.Structure):
+    _fields_ = ([("n", ctypes.c_int64)] +
+                [(n, ctypes.c_void_p) for n in ("p", "g", "m", "v", "m_scale", "v_scale", "p_out", "m_out", "v_out",
+                                                "m_scale_out", "v_scale_out", "copy_out")] +
+                [("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("state", ctypes.c_int32),
+                 ("weight_decay", ctypes.c_float), ("rng_offset", ctypes.c_uint64)])
+
+
+class MolAdamwC(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int32), ("seed", ctypes.c_uint32),
+                ("grad_scale", ctypes.c_void_p), ("lr_ptr", ctypes.c_void_p), ("step_ptr", ctypes.c_void_p)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -62,7 +86,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                            "`python -m paper_2407_15462_amd.build` (there is no fallback)")
     lib = ctypes.CDLL(path)
     P = ctypes.POINTER(MolProblemC)
-    vp, i32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+    vp, i32, sz, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float
     sig = {
         "mol_workspace_size": [P, ctypes.c_int, i32, i32, i32, ctypes.POINTER(sz)],
         "mol_score": [P, i32, i32, vp, vp],
@@ -76,6 +100,13 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "mol_avg_embed": [P, vp, vp, vp],
         "mol_gap_bound": [i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp],
         "mol_gap_bound_combined": [i32, i32, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp],
+        "mol_embed_lookup": [vp, i32, i32, i32, i32, vp, i32, f32, vp, i32, vp],
+        "mol_embed_grad_workspace": [i32, i32, i32, i32, ctypes.POINTER(sz)],
+        "mol_embed_grad": [vp, i32, i32, i32, i32, vp, i32, f32, i32, vp, i32, vp, sz, vp],
+        "mol_softmax_loss_workspace": [i32, i32, ctypes.POINTER(sz)],
+        "mol_softmax_loss": [i32, i32, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp],
+        "mol_score_grad": [P, vp, ctypes.POINTER(MolScoreGradsC), vp, sz, vp],
+        "mol_adamw_step": [ctypes.POINTER(MolAdamwC), vp, i32, vp],
         "mol_timing_enable": [ctypes.c_int],
         "mol_timing_read": [ctypes.c_int, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)],
     }
@@ -214,6 +245,54 @@ def mol_gap_bound_combined(B: int, P: int, m: int, dots, ids, kprime: int, avg_i
                                          _stream(stream)))
 
 
+def _dtype(t) -> int:
+    dt = t if isinstance(t, torch.dtype) else t.dtype
+    if dt not in _DTYPES:
+        raise ValueError(f"unsupported dtype {dt}: torch.float32 or torch.bfloat16")
+    return _DTYPES[dt]
+
+
+def mol_embed_lookup(table, ids, scale: float, out, stream=None) -> None:
+    C, V, d = table.shape
+    _check(load().mol_embed_lookup(_ptr(table), _dtype(table), C, V, d, _ptr(ids), ids.numel(), scale, _ptr(out),
+                                   _dtype(out), _stream(stream)))
+
+
+def mol_embed_grad_workspace(C: int, V: int, d: int, T: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().mol_embed_grad_workspace(C, V, d, T, ctypes.byref(out)))
+    return out.value
+
+
+def mol_embed_grad(grad, ids, scale: float, accumulate: bool, table_grad, ws, stream=None) -> None:
+    C, V, d = table_grad.shape
+    _check(load().mol_embed_grad(_ptr(grad), _dtype(grad), C, V, d, _ptr(ids), ids.numel(), scale, int(accumulate),
+                                 _ptr(table_grad), _dtype(table_grad), _ptr(ws), ws.numel() if ws is not None else 0,
+                                 _stream(stream)))
+
+
+def mol_softmax_loss_workspace(B: int, N: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().mol_softmax_loss_workspace(B, N, ctypes.byref(out)))
+    return out.value
+
+
+def mol_softmax_loss(phi, target, ids, inv_temp: float, row_weight, loss, dphi, ws, stream=None) -> None:
+    B, N = phi.shape
+    _check(load().mol_softmax_loss(B, N, _ptr(phi), _ptr(target), _ptr(ids), inv_temp, _ptr(row_weight), _ptr(loss),
+                                   _ptr(dphi), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream)))
+
+
+def mol_score_grad(prob: Problem, dphi, grads: Dict[str, Optional[torch.Tensor]], ws, stream=None) -> None:
+    c = MolScoreGradsC(**{n: _ptr(t) for n, t in grads.items()})
+    _check(load().mol_score_grad(prob.ref, _ptr(dphi), ctypes.byref(c), _ptr(ws), ws.numel() if ws is not None else 0,
+                                 _stream(stream)))
+
+
+def mol_adamw_step(opt: MolAdamwC, tensors, n_tensors: int, stream=None) -> None:
+    _check(load().mol_adamw_step(ctypes.byref(opt), tensors, n_tensors, _stream(stream)))
+
+
 def mol_timing_enable(on: bool) -> None:
     _check(load().mol_timing_enable(1 if on else 0))
 
@@ -334,3 +413,247 @@ def avg_embed(prob: Problem, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
 def averaged_problem(prob: Problem, q_avg: torch.Tensor, x_avg: torch.Tensor) -> Problem:
     """The P = 1 problem TopKAvg runs on (Q = q', X = x')."""
     return Problem(q_avg.view(prob.B, 1, prob.d), x_avg.view(1, prob.N, prob.d))
+
+
+# ------------------------------------------------------- learning the similarity
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _operand(t: torch.Tensor, name: str, shape, dtypes, device) -> None:
+    """Checks what the C ABI cannot see: shape, element type, device and layout."""
+    _need(isinstance(t, torch.Tensor), f"{name} must be a tensor")
+    _need(tuple(t.shape) == tuple(shape), f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
+    _need(t.dtype in dtypes, f"{name} has dtype {t.dtype}, needs {' or '.join(str(d) for d in dtypes)}")
+    _need(t.device == device, f"{name} is on {t.device}, needs {device}")
+    _need(t.is_contiguous(), f"{name} must be contiguous")
+
+
+_FLOATS = (torch.float32, torch.bfloat16)
+
+
+class _On:
+    """The device of the operands, current for the call, and with ``stream``
+    that stream too, so that what the call allocates belongs to it."""
+
+    def __init__(self, device: torch.device, stream):
+        _need(device.type == "cuda", f"the operands are on {device}, not on a GPU")
+        self.stream = stream
+        self.device = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+        self.on = None
+
+    def __enter__(self):
+        if self.device is not None:
+            self.device.__enter__()
+        if self.stream is not None:
+            s = self.stream
+            self.on = torch.cuda.stream(s if hasattr(s, "cuda_stream") else torch.cuda.ExternalStream(int(s)))
+            self.on.__enter__()
+
+    def __exit__(self, *exc):
+        if self.on is not None:
+            self.on.__exit__(*exc)
+        if self.device is not None:
+            self.device.__exit__(*exc)
+
+
+def _workspace(n: int, ws, device) -> Optional[torch.Tensor]:
+    if ws is not None:
+        _need(ws.dtype == torch.uint8 and ws.device == device and ws.is_contiguous(),
+              f"the workspace must be a contiguous uint8 tensor on {device}")
+        return ws
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dtype=None, out=None, stream=None):
+    """Rows of C tables by id, scaled: out[c][t] = scale table[c][ids[t]].
+
+    table [C][V][d] float32 or bfloat16, ids int32 [T] -> [C][T][d] in
+    ``dtype`` (the table's by default).  An id outside [0, V) gives a zero row.
+    """
+    _need(isinstance(table, torch.Tensor) and table.dim() == 3, "table must be a tensor [C][V][d]")
+    _need(isinstance(ids, torch.Tensor) and ids.dim() == 1, "ids must be a tensor [T]")
+    C, V, d = table.shape
+    dtype = (table.dtype if out is None else out.dtype) if dtype is None else dtype
+    _need(dtype in _FLOATS, f"unsupported output dtype {dtype}")
+    _operand(table, "table", table.shape, _FLOATS, table.device)
+    _operand(ids, "ids", ids.shape, (torch.int32,), table.device)
+    with _On(table.device, stream):
+        if out is None:
+            out = torch.empty((C, ids.numel(), d), dtype=dtype, device=table.device)
+        else:
+            _operand(out, "out", (C, ids.numel(), d), (dtype,), table.device)
+        mol_embed_lookup(table, ids, scale, out, stream)
+    return out
+
+
+def embed_grad_workspace(grad: torch.Tensor, V: int) -> torch.Tensor:
+    """The workspace of embed_grad for a gradient [C][T][d] of tables of V rows."""
+    C, T, d = grad.shape
+    return torch.empty(max(mol_embed_grad_workspace(C, V, d, T), 1), dtype=torch.uint8, device=grad.device)
+
+
+def embed_grad(grad: torch.Tensor, ids: torch.Tensor, V: int, scale: float = 1.0, dtype=torch.float32, out=None,
+               accumulate: bool = False, ws=None, stream=None):
+    """Gradient of embed_lookup for its tables: the rows of grad [C][T][d]
+    summed by id into [C][V][d], times ``scale``.
+
+    ``accumulate`` adds to the rows of ``out`` that have tokens and leaves the
+    others as they are; otherwise every row is written.
+    """
+    _need(isinstance(grad, torch.Tensor) and grad.dim() == 3, "grad must be a tensor [C][T][d]")
+    C, T, d = grad.shape
+    _operand(grad, "grad", grad.shape, _FLOATS, grad.device)
+    _operand(ids, "ids", (T,), (torch.int32,), grad.device)
+    _need(out is not None or not accumulate, "accumulate needs out")
+    dtype = dtype if out is None else out.dtype
+    _need(dtype in _FLOATS, f"unsupported output dtype {dtype}")
+    n = mol_embed_grad_workspace(C, V, d, T)
+    with _On(grad.device, stream):
+        ws = _workspace(n, ws, grad.device)
+        if out is None:
+            out = torch.empty((C, V, d), dtype=dtype, device=grad.device)
+        else:
+            _operand(out, "out", (C, V, d), (dtype,), grad.device)
+        mol_embed_grad(grad, ids, scale, accumulate, out, ws, stream)
+    return out
+
+
+def softmax_loss(phi: torch.Tensor, target: torch.Tensor, ids: Optional[torch.Tensor] = None, inv_temp: float = 1.0,
+                 row_weight: Optional[torch.Tensor] = None, dphi: Optional[torch.Tensor] = None, ws=None, stream=None):
+    """Sampled-softmax loss of score rows phi [B][N] with the positives'
+    columns target int32 [B], and its gradient: (loss [B], dphi [B][N]).
+
+    ids int32 [N]: the columns' items; a column with a negative id, or with the
+    positive's id in another place than the positive's, is left out.  dphi is
+    the gradient of sum_b row_weight[b] loss[b] (weights of 1 by default) and
+    may be written over phi.
+    """
+    _need(isinstance(phi, torch.Tensor) and phi.dim() == 2, "phi must be a tensor [B][N]")
+    B, N = phi.shape
+    dev = phi.device
+    _operand(phi, "phi", (B, N), (torch.float32,), dev)
+    _operand(target, "target", (B,), (torch.int32,), dev)
+    if ids is not None:
+        _operand(ids, "ids", (N,), (torch.int32,), dev)
+    if row_weight is not None:
+        _operand(row_weight, "row_weight", (B,), (torch.float32,), dev)
+    if dphi is not None:
+        _operand(dphi, "dphi", (B, N), (torch.float32,), dev)
+    n = mol_softmax_loss_workspace(B, N)
+    with _On(dev, stream):
+        ws = _workspace(n, ws, dev)
+        loss = torch.empty((B,), dtype=torch.float32, device=dev)
+        if dphi is None:
+            dphi = torch.empty((B, N), dtype=torch.float32, device=dev)
+        mol_softmax_loss(phi, target, ids, inv_temp, row_weight, loss, dphi, ws, stream)
+    return loss, dphi
+
+
+_GRADS = ("dQ", "dX", "da_q", "da_x", "dW1", "db1", "dW2", "db2")
+
+
+def score_grad(prob: Problem, dphi: torch.Tensor, ws=None, stream=None, only: Optional[Sequence[str]] = None):
+    """Gradients of score(prob) for the problem's tensors, given dphi [B][N]:
+    a dict of dQ, dX, da_q, da_x, dW1, db1, dW2 and db2 (or those in ``only``),
+    each of its tensor's shape and type."""
+    _operand(dphi, "dphi", (prob.B, prob.N), (torch.float32,), prob.device)
+    names = _GRADS if only is None else tuple(only)
+    _need(all(n in _GRADS for n in names), f"unknown gradient in {names}: {', '.join(_GRADS)}")
+    _need(all(t is not None for t in prob.tensors), "the problem lacks a gating tensor")
+    n = mol_workspace_size(prob, MOL_OP_SCORE_GRAD)
+    with _On(prob.device, stream):
+        ws = _workspace(n, ws, prob.device)
+        out = {g: torch.empty_like(t) for g, t in zip(_GRADS, prob.tensors) if g in names}
+        mol_score_grad(prob, dphi, out, ws, stream)
+    return out
+
+
+class AdamwTensors:
+    """The tensors of an AdamW step and their states, laid out once for the
+    library (and kept alive by this object).
+
+    p, g: lists of float32 or bfloat16 tensors; m, v: float32, or 8-bit
+    (float8_e4m3fn codes, with m_scale and v_scale float32 [ceil(n / 256)]).
+    weight_decay: one number, or one a tensor.  out: None (in place), or a
+    dict of lists "p", "m", "v" (and "m_scale", "v_scale") to write the new
+    state to, and "copy": bfloat16 copies of the new parameters, whole or for
+    some tensors (None for the others); any may be missing or None.  Tensors
+    keep their place in the stream of random numbers that rounds 8-bit states
+    by their order: each starts at a multiple of 256.
+    """
+
+    def __init__(self, p: List[torch.Tensor], g: List[torch.Tensor], m: List[torch.Tensor], v: List[torch.Tensor],
+                 m_scale: Optional[List[torch.Tensor]] = None, v_scale: Optional[List[torch.Tensor]] = None,
+                 weight_decay=0.0, out: Optional[dict] = None):
+        n = len(p)
+        lists = {"g": g, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale}
+        out = {k: x for k, x in (out or {}).items() if x is not None}
+        unknown = set(out) - {"p", "m", "v", "m_scale", "v_scale", "copy"}
+        _need(not unknown, f"unknown outputs {sorted(unknown)}")
+        for name, x in list(lists.items()) + list(out.items()):
+            _need(x is None or len(x) == n, f"{name} has not the {n} entries of p")
+        decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        _need(len(decay) == n, f"weight_decay has not the {n} entries of p")
+        self.n, self.device = n, p[0].device if n else torch.device("cuda")
+        self.c = (MolAdamwTensorC * max(n, 1))()
+        self.tensors = (p, g, m, v, m_scale, v_scale, out)
+        offset = 0
+        for i in range(n):
+            _need(isinstance(p[i], torch.Tensor), "p must hold tensors")
+            shape, blocks = p[i].shape, (p[i].numel() + MOL_STATE_BLOCK - 1) // MOL_STATE_BLOCK
+            _operand(p[i], f"p[{i}]", shape, _FLOATS, self.device)
+            _operand(g[i], f"g[{i}]", shape, _FLOATS, self.device)
+            eight = isinstance(m[i], torch.Tensor) and m[i].dtype == torch.float8_e4m3fn
+            state = torch.float8_e4m3fn if eight else torch.float32
+            e = self.c[i]
+            e.n, e.p, e.g, e.rng_offset, e.weight_decay = p[i].numel(), _ptr(p[i]), _ptr(g[i]), offset, decay[i]
+            e.param_dtype, e.grad_dtype = _dtype(p[i]), _dtype(g[i])
+            e.state = MOL_STATE_E4M3 if eight else MOL_STATE_F32
+            if "p" in out:
+                _operand(out["p"][i], f"out p[{i}]", shape, (p[i].dtype,), self.device)
+            e.p_out = _ptr(out["p"][i]) if "p" in out else e.p
+            if out.get("copy") is not None and out["copy"][i] is not None:
+                _operand(out["copy"][i], f"out copy[{i}]", shape, (torch.bfloat16,), self.device)
+                e.copy_out = _ptr(out["copy"][i])
+            for name, x in (("m", m), ("v", v)):
+                _operand(x[i], f"{name}[{i}]", shape, (state,), self.device)
+                if name in out:
+                    _operand(out[name][i], f"out {name}[{i}]", shape, (state,), self.device)
+                setattr(e, name, _ptr(x[i]))
+                setattr(e, name + "_out", _ptr(out[name][i]) if name in out else _ptr(x[i]))
+                if not eight:
+                    continue
+                scale, key = lists[name + "_scale"], name + "_scale"
+                _need(scale is not None, f"8-bit states need {key}")
+                _operand(scale[i], f"{key}[{i}]", (blocks,), (torch.float32,), self.device)
+                if key in out:
+                    _operand(out[key][i], f"out {key}[{i}]", (blocks,), (torch.float32,), self.device)
+                _need((key in out) == (name in out), f"outputs {name} and {key} go together")
+                setattr(e, key, _ptr(scale[i]))
+                setattr(e, key + "_out", _ptr(out[key][i]) if key in out else _ptr(scale[i]))
+            offset += blocks * MOL_STATE_BLOCK
+
+
+def adamw_step(tensors: AdamwTensors, lr=1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step=1,
+               seed: int = 0, grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
+    """One AdamW step over all of ``tensors``.
+
+    lr and step (from 1) are numbers, or one-element tensors on the GPU
+    (float32, int32) that the kernel reads, for graphs that are replayed;
+    grad_scale: None, or one float32 on the GPU that multiplies every gradient.
+    """
+    if tensors.n == 0:
+        return
+    for name, t, dt in (("lr", lr, torch.float32), ("step", step, torch.int32), ("grad_scale", grad_scale, torch.float32)):
+        if isinstance(t, torch.Tensor):
+            _need(t.numel() == 1, f"{name} must have one element")
+            _operand(t, name, t.shape, (dt,), tensors.device)
+        else:
+            _need(name != "grad_scale" or t is None, "grad_scale must be a tensor")
+    on_lr, on_step = isinstance(lr, torch.Tensor), isinstance(step, torch.Tensor)
+    opt = MolAdamwC(0.0 if on_lr else lr, beta1, beta2, eps, 1 if on_step else step, seed & 0xFFFFFFFF, _ptr(grad_scale),
+                    _ptr(lr) if on_lr else None, _ptr(step) if on_step else None)
+    with _On(tensors.device, stream):
+        mol_adamw_step(opt, tensors.c, tensors.n, stream)
