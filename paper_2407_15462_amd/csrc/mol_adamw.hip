@@ -104,15 +104,13 @@ __device__ __forceinline__ void store_f32(void* base, long i, long n, bool vec, 
 }
 __device__ __forceinline__ void store_bf16(void* base, long i, long n, bool vec, const float (&x)[4]) {
   bf16_t* p = static_cast<bf16_t*>(base) + i;
-  uint32_t w[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) w[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x[e]));
+  const uint2 w = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
   if (vec && i + 4 <= n) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+    *reinterpret_cast<uint2*>(p) = w;
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (i + e < n) p[e] = static_cast<bf16_t>(w[e]);
+      if (i + e < n) p[e] = static_cast<bf16_t>((e < 2 ? w.x : w.y) >> (16 * (e & 1)));
   }
 }
 __device__ __forceinline__ void store_codes(void* base, long i, long n, bool vec, uint32_t c) {
@@ -126,21 +124,21 @@ __device__ __forceinline__ void store_codes(void* base, long i, long n, bool vec
   }
 }
 
-// largest of a wave, in all lanes; a NaN anywhere gives NaN
-__device__ __forceinline__ float wave_top(float v, bool nan) {
-  v = max_groups(row16_max(v));
-  return __any(nan) ? __builtin_nanf("") : v;
+// largest magnitude of a wave from each lane's, as bits (ordered as the numbers
+// are, NaN above all), in all lanes
+template <int ROR>
+__device__ __forceinline__ uint32_t ror_bits(uint32_t v) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x120 + ROR, 0xf, 0xf, true));
 }
-
-// e4m3 code of |y| <= 448, rounded up with the chance r16 / 2^16 of what is cut off
-__device__ __forceinline__ uint32_t encode(float y, uint32_t r16, bool nonzero) {
-  const float a = fabsf(y);
-  const int32_t normal = static_cast<int32_t>((__float_as_uint(a) + (r16 << 4)) >> 20) - (120 << 3);
-  const int32_t small = static_cast<int32_t>(fmaf(a, 512.f, static_cast<float>(r16) * 0x1p-16f));
-  int32_t c = a < 0x1p-6f ? small : normal;
-  c = min(c, 0x7E);
-  if (nonzero) c = max(c, 1);
-  return static_cast<uint32_t>(c) | (__float_as_uint(y) >> 24 & 0x80u);
+__device__ __forceinline__ float wave_top(uint32_t v) {
+  v = max(v, ror_bits<8>(v));
+  v = max(v, ror_bits<4>(v));
+  v = max(v, ror_bits<2>(v));
+  v = max(v, ror_bits<1>(v));
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __uint_as_float(max(b[0], b[1]));
 }
 
 // the four values of a word of codes
@@ -152,18 +150,24 @@ __device__ __forceinline__ void decode(uint32_t c, float scale, float (&x)[4]) {
   x[3] = hi[1] * scale;
 }
 
-// codes of a block's four values a lane, and its scale (448 / top as a float32
-// division, which overflows for a top below 2^-119: such a block is stored as zeros)
-__device__ __forceinline__ uint32_t encode4(const float (&x)[4], const uint32_t (&r)[4], bool positive, float top,
-                                            float& scale) {
-  scale = top * (1.f / 448.f);
-  const float inv = top > 0x1p-119f ? 448.f / top : 0.f;      // (false for NaN)
-  if (!(top > 0x1p-119f) && top == top) scale = 0.f;
-  if (__builtin_isinf(top)) scale = __builtin_nanf("");
-  uint32_t c = 0;
+// codes of a block's four values a lane, and its scale (448 / top overflows
+// for a top below 2^-119: such a block is stored as zeros).  The conversion adds the top bits of r below the last bit that it keeps
+// and cuts the rest off: up with the chance r16 / 2^16 of what is cut off, also
+// among the subnormal codes.
+template <bool POSITIVE>
+__device__ __forceinline__ uint32_t encode4(const float (&x)[4], const uint32_t (&r)[4], float top, float& scale) {
+  const bool some = top > 0x1p-119f && top <= 3.4e38f;        // (false for NaN)
+  scale = some ? top * (1.f / 448.f) : top <= 0x1p-119f ? 0.f : __builtin_nanf("");
+  const float rt = __builtin_amdgcn_rcpf(top), q = 448.f * rt, inv = fmaf(fmaf(-q, top, 448.f), rt, q);   // 448 / top
+  float y[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) c |= encode(x[e] * inv, r[e], positive && x[e] > 0.f) << (8 * e);
-  return inv > 0.f ? c : 0;
+  for (int e = 0; e < 4; ++e)
+    y[e] = __builtin_amdgcn_fmed3f(x[e] * inv, POSITIVE ? (x[e] > 0.f ? 0x1p-9f : 0.f) : -448.f, 448.f);
+  int c = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], r[0], 0, 0);
+  c = __builtin_amdgcn_cvt_sr_fp8_f32(y[1], r[1], c, 1);
+  c = __builtin_amdgcn_cvt_sr_fp8_f32(y[2], r[2], c, 2);
+  c = __builtin_amdgcn_cvt_sr_fp8_f32(y[3], r[3], c, 3);
+  return some ? static_cast<uint32_t>(c) : 0;
 }
 
 struct Rates {
@@ -206,22 +210,25 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwDesc& 
       decode(mc[k], ms[k], mk);
       decode(vc[k], vs[k], vk);
     }
-    bool nan_m = false, nan_v = false;
-    float top_m = 0.f, top_v = 0.f;
+    uint32_t top_m = 0, top_v = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float gg = g[k][e] * gs;
       const float m0 = E8 ? mk[e] : m[E8 ? 0 : k][e], v0 = E8 ? vk[e] * vk[e] : v[E8 ? 0 : k][e];
       mk[e] = a.beta1 * m0 + a.one_beta1 * gg;
       vk[e] = a.beta2 * v0 + a.one_beta2 * gg * gg;
-      root[e] = E8 ? sqrtf(vk[e]) : __builtin_amdgcn_sqrtf(vk[e]);   // (rounded once where it is stored)
+      if constexpr (E8) {
+        // the root is stored: the instruction's last bit put right by one step
+        const float y = __builtin_amdgcn_rsqf(fmaxf(vk[e], 0x1p-126f)), r = vk[e] * y;
+        root[e] = fmaf(fmaf(-r, r, vk[e]), 0.5f * y, r);
+      } else {
+        root[e] = __builtin_amdgcn_sqrtf(vk[e]);
+      }
       const float x = rt.step_size * mk[e] * __builtin_amdgcn_rcpf(fmaf(root[e], rt.root, a.eps));
       p[k][e] = p[k][e] * keep - x;
       if constexpr (E8) {
-        top_m = fmaxf(top_m, fabsf(mk[e]));
-        top_v = fmaxf(top_v, root[e]);
-        nan_m = nan_m || mk[e] != mk[e];
-        nan_v = nan_v || root[e] != root[e];
+        top_m = max(top_m, __float_as_uint(mk[e]) & 0x7FFFFFFFu);
+        top_v = max(top_v, __float_as_uint(root[e]) & 0x7FFFFFFFu);
       }
     }
     if constexpr (sizeof(TP) == 4)
@@ -236,12 +243,12 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwDesc& 
         // the element's place, 64 bits: the high word moves the seed
         const uint64_t at = (static_cast<uint64_t>(t.rng_hi) << 32 | t.rng_lo) + static_cast<uint64_t>(i + e);
         const uint32_t h = mix32(static_cast<uint32_t>(at) ^ rt.mixed ^ static_cast<uint32_t>(at >> 32) * 0x85EBCA6Bu);
-        rm[e] = h & 0xFFFFu;
-        rv[e] = h >> 16;
+        rm[e] = h << 16;
+        rv[e] = h & 0xFFFF0000u;
       }
       float sm, sv;
-      const uint32_t cm = encode4(mk, rm, false, wave_top(top_m, nan_m), sm);
-      const uint32_t cv = encode4(root, rv, true, wave_top(top_v, nan_v), sv);
+      const uint32_t cm = encode4<false>(mk, rm, wave_top(top_m), sm);
+      const uint32_t cv = encode4<true>(root, rv, wave_top(top_v), sv);
       store_codes(t.m_out, i, t.n, vec, cm);
       store_codes(t.v_out, i, t.n, vec, cv);
       if (lane == 0) {
