@@ -4,10 +4,10 @@
 // Column i is kept unless its id is negative or it repeats the positive's id.
 //
 // Bound by memory: a row is read once and written once.  A workgroup holds a
-// whole row of up to kRegs values a thread in registers (64, 256 or 1024
-// threads: rows of up to 2048, 8192 or 32,768 columns, and the columns past
-// that, up to an eighth of them, read again); which of them are kept is one bit
-// each.  Longer rows are cut into parts, whose maxima and sums a first launch
+// whole row in registers, kRegs values a thread (64, 256 or 1024 threads: rows
+// of up to 2176, 8704 or 34,816 columns), in few enough of them that two
+// workgroups of 1024 share a CU and one's loads run under the other's stores.
+// Longer rows are cut into parts, whose maxima and sums a first launch
 // leaves in the workspace and a second one joins, reading the row again (from
 // the last-level cache where the batch's scores fit it).  Rows start at any
 // element, so that loads are 4 bytes a lane, kRegs of them in flight.
@@ -20,7 +20,7 @@ namespace mol {
 
 namespace {
 
-constexpr int kRegs = 32;
+constexpr int kRegs = 34;
 constexpr float kLog2E = 1.4426950408889634f, kLog2ELo = 1.925963033500e-8f, kLn2 = 0.6931471805599453f;
 
 // e^x, x <= 0: 2^t with t = x log2(e) in two parts, since float32's rounding of
@@ -31,6 +31,9 @@ __device__ __forceinline__ float exp_neg(float x) {
   const float e = __builtin_amdgcn_exp2f(t);
   return e == 0.f ? 0.f : fmaf(e, r * kLn2, e);   // (0 for x = -inf, whose r is NaN)
 }
+
+// e^{z - m}; 0 for z = -inf, also where the whole row is (its sum is then 0, its loss NaN)
+__device__ __forceinline__ float weight(float z, float m) { return z == -__builtin_inff() ? 0.f : exp_neg(z - m); }
 
 __device__ __forceinline__ float wave_max(float v) {
   for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
@@ -102,9 +105,10 @@ __device__ __forceinline__ bool kept(const LossArgs& a, const Row& r, int i) {
 
 }  // namespace
 
-// One workgroup a row.
+// One workgroup a row.  A left-out column is held as -inf: its exponential is 0,
+// and a gradient whose exponential is 0 is written as 0 whatever the row's sum is.
 template <int NT>
-__global__ __launch_bounds__(NT) void k_softmax_loss(LossArgs a) {
+__global__ __launch_bounds__(NT, NT == 1024 ? 8 : 4) void k_softmax_loss(LossArgs a) {
   __shared__ float sh[NT / 64];
   const int b = blockIdx.x, tid = threadIdx.x;
   const long at = static_cast<long>(b) * a.N;
@@ -118,52 +122,43 @@ __global__ __launch_bounds__(NT) void k_softmax_loss(LossArgs a) {
     return;
   }
   const float zt = a.inv_temp * phi[r.t];
-  const int regs = min((a.N + NT - 1) / NT, kRegs);        // registers in use
-  float z[kRegs];
-  uint32_t keep = 0;
+  // columns k NT + tid for the k < full, and one of the rest
+  const int full = a.N / NT, il = full * NT + tid;
+  const bool rest = il < a.N;
+  float z[kRegs], zl = -__builtin_inff();
 #pragma unroll
-  for (int k = 0; k < kRegs; ++k) {
-    const int i = k * NT + tid;
-    z[k] = -__builtin_inff();
-    if (k < regs && i < a.N) {
-      z[k] = phi[i];
-      keep |= static_cast<uint32_t>(kept(a, r, i)) << k;
-    }
-  }
+  for (int k = 0; k < kRegs; ++k)
+    if (k < full) z[k] = phi[k * NT + tid];
+  if (rest) zl = phi[il];
   float m = -__builtin_inff();
-  bool nan = false;                                        // fmaxf passes over NaN
 #pragma unroll
-  for (int k = 0; k < kRegs; ++k) {
-    z[k] = (keep >> k) & 1 ? a.inv_temp * z[k] : -__builtin_inff();
-    m = fmaxf(m, z[k]);
-    nan = nan || z[k] != z[k];
-  }
-  for (int i = kRegs * NT + tid; i < a.N; i += NT)
-    if (kept(a, r, i)) {
-      const float v = a.inv_temp * phi[i];
-      m = fmaxf(m, v);
-      nan = nan || v != v;
+  for (int k = 0; k < kRegs; ++k)
+    if (k < full) {
+      z[k] = kept(a, r, k * NT + tid) ? a.inv_temp * z[k] : -__builtin_inff();
+      m = fmaxf(m, z[k]);
     }
-  m = block_max<NT>(m, sh);
-  float s = nan ? __builtin_nanf("") : 0.f;
-#pragma unroll
-  for (int k = 0; k < kRegs; ++k) {
-    z[k] = (keep >> k) & 1 ? exp_neg(z[k] - m) : 0.f;
-    s += z[k];
+  if (rest) {
+    zl = kept(a, r, il) ? a.inv_temp * zl : -__builtin_inff();
+    m = fmaxf(m, zl);
   }
-  for (int i = kRegs * NT + tid; i < a.N; i += NT)
-    if (kept(a, r, i)) s += exp_neg(a.inv_temp * phi[i] - m);
+  m = block_max<NT>(m, sh);
+  zl = weight(zl, m);
+  float s = zl;                                            // (a NaN, which the maximum passes over, shows here)
+#pragma unroll
+  for (int k = 0; k < kRegs; ++k)
+    if (k < full) {
+      z[k] = weight(z[k], m);
+      s += z[k];
+    }
   s = block_sum<NT>(s, sh);
   if (a.loss && tid == 0) a.loss[b] = logf(s) + (m - zt);
   if (!out) return;
   const float w = (a.row_weight ? a.row_weight[b] : 1.f) * a.inv_temp, q = 1.f / s;
+  auto grad = [&](int i, float e) { return i == r.t ? w * (e * q - 1.f) : e == 0.f ? 0.f : w * (e * q); };
 #pragma unroll
-  for (int k = 0; k < kRegs; ++k) {
-    const int i = k * NT + tid;
-    if (k < regs && i < a.N) out[i] = (keep >> k) & 1 ? w * (z[k] * q - (i == r.t ? 1.f : 0.f)) : 0.f;
-  }
-  for (int i = kRegs * NT + tid; i < a.N; i += NT)
-    out[i] = kept(a, r, i) ? w * (exp_neg(a.inv_temp * phi[i] - m) * q - (i == r.t ? 1.f : 0.f)) : 0.f;
+  for (int k = 0; k < kRegs; ++k)
+    if (k < full) out[k * NT + tid] = grad(k * NT + tid, z[k]);
+  if (rest) out[il] = grad(il, zl);
 }
 
 // Long rows, first launch: maximum and sum of part blockIdx.x of row blockIdx.y.
@@ -192,7 +187,7 @@ __global__ __launch_bounds__(256) void k_softmax_part(LossArgs a) {
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (v[u] != -__builtin_inff()) s += exp_neg(v[u] - m);   // (NaN is not passed over)
+      s += weight(v[u], m);                                     // (NaN is not passed over)
   }
   const float all = block_max<256>(m, sh);
   // (a part of nothing but -inf has the sum 0)
@@ -224,7 +219,7 @@ __global__ __launch_bounds__(256) void k_softmax_join(LossArgs a) {
   m = block_max<256>(m, sh);
   for (int k = tid; k < a.parts; k += 256) {
     const float pm = part[2 * k], ps = part[2 * k + 1];
-    s += pm == -__builtin_inff() && ps == 0.f ? (m == pm ? __builtin_nanf("") : 0.f) : ps * exp_neg(pm - m);
+    s += pm == -__builtin_inff() && ps == 0.f ? 0.f : ps * exp_neg(pm - m);
   }
   s = block_sum<256>(s, sh);
   if (a.loss && blockIdx.x == 0 && tid == 0) a.loss[b] = logf(s) + (m - a.ws[2l * a.B * a.parts + b]);
@@ -246,8 +241,9 @@ __global__ __launch_bounds__(256) void k_softmax_join(LossArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const long i = base + u * 256 + tid;
-      if (i < i1)
-        a.dphi[at + i] = (keep >> u) & 1 ? w * (exp_neg(a.inv_temp * v[u] - m) * q - (i == r.t ? 1.f : 0.f)) : 0.f;
+      if (i >= i1) continue;
+      const float e = (keep >> u) & 1 ? weight(a.inv_temp * v[u], m) : 0.f;
+      a.dphi[at + i] = i == r.t ? w * (e * q - 1.f) : e == 0.f ? 0.f : w * (e * q);
     }
   }
 }
@@ -258,8 +254,7 @@ namespace {
 // A row's parts: none where one workgroup holds it; else parts of about 8192
 // columns, fewer and longer ones where the batch fills the card anyway.
 int loss_parts(int B, int N) {
-  constexpr long held = 1024l * kRegs;
-  if (N <= held + held / 8) return 1;
+  if (N <= 1024 * kRegs) return 1;
   const long most = (N + 8191l) / 8192, want = (1024l + B - 1) / B;
   return static_cast<int>(std::max<long>(2, std::min(most, want)));
 }
