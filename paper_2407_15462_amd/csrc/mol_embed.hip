@@ -32,11 +32,12 @@ namespace mol {
 namespace {
 
 constexpr int kSortOne = 4096;        // tokens sorted by one workgroup
-constexpr int kSortThreads = 512;     // of a block of the radix passes
+constexpr int kSortThreads = 256;     // of a block of the radix passes
 constexpr int kSortWaves = kSortThreads / 64;
+constexpr int kSortU = 8;             // loads in flight
 constexpr int kMaxBits = 11;          // digit of a radix pass
-constexpr int kSortBlock = 4096;      // tokens a block takes at least
-constexpr int kSortBlocks = 128;      // blocks at most
+constexpr int kSortBlock = kSortThreads * kSortU;   // tokens a block takes at least
+constexpr int kSortBlocks = 128;      // blocks at most (a row of counts is a multiple of 4)
 
 template <typename T>
 struct Elem;
@@ -185,21 +186,32 @@ __global__ __launch_bounds__(1024) void k_sort_one(const int32_t* __restrict__ i
   for (int i = tid; i < T; i += 1024) out[i] = pairs[cur][i];
 }
 
-// counts[block][bin] of the digit at `shift`; in: NULL for the ids themselves
+// a token's (key, place); in: NULL for the ids themselves
+__device__ __forceinline__ uint2 token(const int32_t* __restrict__ ids, const uint2* __restrict__ in, long i, int V) {
+  return in ? in[i] : make_uint2(key_of(ids[i], V), static_cast<uint32_t>(i));
+}
+
+// counts[bin][block] of the digit at `shift`, rows of nbp (zero past the blocks)
 __global__ __launch_bounds__(kSortThreads) void k_sort_hist(const int32_t* __restrict__ ids,
                                                             const uint2* __restrict__ in, long T, int V, int per,
-                                                            int shift, int bits, uint32_t* __restrict__ counts) {
+                                                            int shift, int bits, int nbp,
+                                                            uint32_t* __restrict__ counts) {
   __shared__ uint32_t hist[1 << kMaxBits];
   const int bins = 1 << bits;
   for (int i = threadIdx.x; i < bins; i += kSortThreads) hist[i] = 0;
   __syncthreads();
   const long i0 = static_cast<long>(blockIdx.x) * per, i1 = min(T, i0 + per);
-  for (long i = i0 + threadIdx.x; i < i1; i += kSortThreads) {
-    const uint32_t k = in ? in[i].x : key_of(ids[i], V);
-    atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
+  for (long b = i0 + threadIdx.x; b < i1; b += kSortThreads * kSortU) {
+    uint32_t k[kSortU];
+#pragma unroll
+    for (int u = 0; u < kSortU; ++u) k[u] = token(ids, in, min(b + u * kSortThreads, i1 - 1), V).x;
+#pragma unroll
+    for (int u = 0; u < kSortU; ++u)
+      if (b + u * kSortThreads < i1) atomicAdd(&hist[(k[u] >> shift) & (bins - 1)], 1u);
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < bins; i += kSortThreads) counts[static_cast<long>(blockIdx.x) * bins + i] = hist[i];
+  // (the grid has nbp blocks: those past the tokens count nothing)
+  for (int i = threadIdx.x; i < bins; i += kSortThreads) counts[static_cast<long>(i) * nbp + blockIdx.x] = hist[i];
 }
 
 // Stable scatter of one pass: wave w of block j takes the w-th part of the
@@ -207,36 +219,46 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_hist(const int32_t* __res
 // digits below, of the blocks before and of the waves before.
 __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(const int32_t* __restrict__ ids,
                                                                const uint2* __restrict__ in, long T, int V, int per,
-                                                               int shift, int bits,
+                                                               int shift, int bits, int nbp,
                                                                const uint32_t* __restrict__ counts,
                                                                uint2* __restrict__ out) {
   __shared__ uint32_t hist[kSortWaves][1 << kMaxBits];
   __shared__ uint32_t carry[kSortWaves];
   constexpr int PT = (1 << kMaxBits) / kSortThreads;   // bins a thread, at most
   const int bins = 1 << bits, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int nb = gridDim.x, mine = blockIdx.x;
+  const int mine = blockIdx.x;
   for (int i = tid; i < bins * kSortWaves; i += kSortThreads) hist[i / bins][i & (bins - 1)] = 0;
+  const long i0 = min(T, static_cast<long>(mine) * per + static_cast<long>(w) * (per / kSortWaves));
+  const long i1 = min(T, i0 + per / kSortWaves);
+  uint2 tok[kSortU];                                   // the wave's next tokens
+  auto fetch = [&](long b) {
+#pragma unroll
+    for (int u = 0; u < kSortU; ++u) tok[u] = token(ids, in, min(b + u * 64 + lane, T - 1), V);
+  };
+  fetch(i0);
   __syncthreads();
-  const long i0 = static_cast<long>(mine) * per + static_cast<long>(w) * (per / kSortWaves);
-  const long i1 = min(min(T, i0 + per / kSortWaves), T);
-  for (long i = i0 + lane; i < i1; i += 64) {
-    const uint32_t k = in ? in[i].x : key_of(ids[i], V);
-    atomicAdd(&hist[w][(k >> shift) & (bins - 1)], 1u);
+  for (long b = i0; b < i1; b += 64 * kSortU) {
+    if (b > i0) fetch(b);
+#pragma unroll
+    for (int u = 0; u < kSortU; ++u)
+      if (b + u * 64 + lane < i1) atomicAdd(&hist[w][(tok[u].x >> shift) & (bins - 1)], 1u);
   }
-  // totals of every bin and those of the blocks before: thread tid has bins tid + 512 k
+  // totals of every bin and those of the blocks before: thread tid has bins tid + 256 k
   uint32_t tot[PT] = {}, before[PT] = {};
 #pragma unroll
   for (int k = 0; k < PT; ++k) {
     const int b = tid + k * kSortThreads;
     if (b < bins) {
+      const uint4* row = reinterpret_cast<const uint4*>(counts + static_cast<long>(b) * nbp);
 #pragma unroll 8
-      for (int j = 0; j < nb; ++j) {
-        const uint32_t n = counts[static_cast<long>(j) * bins + b];
-        tot[k] += n;
-        before[k] += j < mine ? n : 0;
+      for (int j = 0; j < nbp; j += 4) {
+        const uint4 n = row[j >> 2];
+        tot[k] += (n.x + n.y) + (n.z + n.w);
+        before[k] += (j < mine ? n.x : 0) + (j + 1 < mine ? n.y : 0) + (j + 2 < mine ? n.z : 0) + (j + 3 < mine ? n.w : 0);
       }
     }
   }
+  if (i1 - i0 > 64 * kSortU) fetch(i0);
   __syncthreads();
   uint32_t run = 0;                                    // tokens of the bins of earlier rounds
 #pragma unroll
@@ -261,18 +283,20 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(const int32_t* __
     }
     __syncthreads();
   }
-  for (long b = i0; b < i1; b += 64) {
-    const bool live = b + lane < i1;
-    uint2 p = make_uint2(0, 0);
-    if (live) p = in ? in[b + lane] : make_uint2(key_of(ids[b + lane], V), static_cast<uint32_t>(b + lane));
-    const uint32_t digit = (p.x >> shift) & (bins - 1);
-    const uint64_t m = same_digit(digit, bits, __ballot(live));
-    const int rank = __popcll(m & ((1ull << lane) - 1));
-    const uint32_t at = hist[w][digit] + rank;
-    __builtin_amdgcn_wave_barrier();
-    if (live && rank == 0) hist[w][digit] += __popcll(m);
-    __builtin_amdgcn_wave_barrier();
-    if (live) out[at] = p;
+  for (long b = i0; b < i1; b += 64 * kSortU) {
+    if (b > i0) fetch(b);
+#pragma unroll
+    for (int u = 0; u < kSortU; ++u) {
+      const bool live = b + u * 64 + lane < i1;
+      const uint32_t digit = (tok[u].x >> shift) & (bins - 1);
+      const uint64_t m = same_digit(digit, bits, __ballot(live));
+      const int rank = __popcll(m & ((1ull << lane) - 1));
+      const uint32_t at = hist[w][digit] + rank;
+      __builtin_amdgcn_wave_barrier();
+      if (live && rank == 0) hist[w][digit] += __popcll(m);
+      __builtin_amdgcn_wave_barrier();
+      if (live) out[at] = tok[u];
+    }
   }
 }
 
@@ -491,7 +515,7 @@ int key_bits(int V) {
 
 int sort_per(long T) {
   const long per = std::max<long>(kSortBlock, (T + kSortBlocks - 1) / kSortBlocks);
-  return static_cast<int>((per + kSortThreads - 1) / kSortThreads * kSortThreads);
+  return static_cast<int>((per + kSortBlock - 1) / kSortBlock * kSortBlock);
 }
 
 // Tokens of a team: the most that still gives every CU two workgroups (fewer
@@ -568,14 +592,15 @@ static hipError_t launch_sort(const int32_t* ids, long T, int V, uint2* a, uint2
     return hipGetLastError();
   }
   const int passes = (bits + kMaxBits - 1) / kMaxBits, each = (bits + passes - 1) / passes;
-  const int per = sort_per(T), nb = static_cast<int>((T + per - 1) / per);
+  const int per = sort_per(T), nb = static_cast<int>((T + per - 1) / per), nbp = (nb + 3) / 4 * 4;
   // the last pass ends in `a`
   const uint2* in = nullptr;
   for (int p = 0; p < passes; ++p) {
     uint2* to = (passes - p) % 2 ? a : b;
-    hipLaunchKernelGGL(k_sort_hist, dim3(nb), dim3(kSortThreads), 0, st, ids, in, T, V, per, p * each, each, counts);
-    hipLaunchKernelGGL(k_sort_scatter, dim3(nb), dim3(kSortThreads), 0, st, ids, in, T, V, per, p * each, each, counts,
-                       to);
+    hipLaunchKernelGGL(k_sort_hist, dim3(nbp), dim3(kSortThreads), 0, st, ids, in, T, V, per, p * each, each, nbp,
+                       counts);
+    hipLaunchKernelGGL(k_sort_scatter, dim3(nb), dim3(kSortThreads), 0, st, ids, in, T, V, per, p * each, each, nbp,
+                       counts, to);
     in = to;
   }
   return hipGetLastError();

@@ -7,6 +7,7 @@ outputs and workspace with torch and call them.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, List, Optional, Sequence, Tuple
@@ -139,7 +140,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())   # (a Stream object costs 5 us)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -423,6 +424,9 @@ def _need(ok: bool, what: str) -> None:
 
 def _operand(t: torch.Tensor, name: str, shape, dtypes, device) -> None:
     """Checks what the C ABI cannot see: shape, element type, device and layout."""
+    if (isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == shape and t.device == device and
+            t.is_contiguous()):
+        return
     _need(isinstance(t, torch.Tensor), f"{name} must be a tensor")
     _need(tuple(t.shape) == tuple(shape), f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
     _need(t.dtype in dtypes, f"{name} has dtype {t.dtype}, needs {' or '.join(str(d) for d in dtypes)}")
@@ -431,38 +435,31 @@ def _operand(t: torch.Tensor, name: str, shape, dtypes, device) -> None:
 
 
 _FLOATS = (torch.float32, torch.bfloat16)
+_HERE_NOW = contextlib.nullcontext()
 
 
-class _On:
-    """The device of the operands, current for the call, and with ``stream``
+def _on(device: torch.device, stream):
+    """A context in which the operands' device is current, and with ``stream``
     that stream too, so that what the call allocates belongs to it."""
-
-    def __init__(self, device: torch.device, stream):
-        _need(device.type == "cuda", f"the operands are on {device}, not on a GPU")
-        self.stream = stream
-        self.device = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-        self.on = None
-
-    def __enter__(self):
-        if self.device is not None:
-            self.device.__enter__()
-        if self.stream is not None:
-            s = self.stream
-            self.on = torch.cuda.stream(s if hasattr(s, "cuda_stream") else torch.cuda.ExternalStream(int(s)))
-            self.on.__enter__()
-
-    def __exit__(self, *exc):
-        if self.on is not None:
-            self.on.__exit__(*exc)
-        if self.device is not None:
-            self.device.__exit__(*exc)
+    if device.type != "cuda":
+        raise ValueError(f"the operands are on {device}, not on a GPU")
+    if stream is None and device.index == torch.cuda.current_device():
+        return _HERE_NOW
+    stack = contextlib.ExitStack()
+    stack.enter_context(torch.cuda.device(device))
+    if stream is not None:
+        s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+        stack.enter_context(torch.cuda.stream(s))
+    return stack
 
 
-def _workspace(n: int, ws, device) -> Optional[torch.Tensor]:
+def _workspace(size, ws, device) -> Optional[torch.Tensor]:
+    """The caller's workspace, or one of size() bytes (None for none)."""
     if ws is not None:
-        _need(ws.dtype == torch.uint8 and ws.device == device and ws.is_contiguous(),
-              f"the workspace must be a contiguous uint8 tensor on {device}")
+        if ws.dtype != torch.uint8 or ws.device != device or not ws.is_contiguous():
+            raise ValueError(f"the workspace must be a contiguous uint8 tensor on {device}")
         return ws
+    n = size()
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
@@ -476,10 +473,11 @@ def embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dty
     _need(isinstance(ids, torch.Tensor) and ids.dim() == 1, "ids must be a tensor [T]")
     C, V, d = table.shape
     dtype = (table.dtype if out is None else out.dtype) if dtype is None else dtype
-    _need(dtype in _FLOATS, f"unsupported output dtype {dtype}")
+    if dtype not in _FLOATS:
+        raise ValueError(f"unsupported output dtype {dtype}")
     _operand(table, "table", table.shape, _FLOATS, table.device)
     _operand(ids, "ids", ids.shape, (torch.int32,), table.device)
-    with _On(table.device, stream):
+    with _on(table.device, stream):
         if out is None:
             out = torch.empty((C, ids.numel(), d), dtype=dtype, device=table.device)
         else:
@@ -508,10 +506,10 @@ def embed_grad(grad: torch.Tensor, ids: torch.Tensor, V: int, scale: float = 1.0
     _operand(ids, "ids", (T,), (torch.int32,), grad.device)
     _need(out is not None or not accumulate, "accumulate needs out")
     dtype = dtype if out is None else out.dtype
-    _need(dtype in _FLOATS, f"unsupported output dtype {dtype}")
-    n = mol_embed_grad_workspace(C, V, d, T)
-    with _On(grad.device, stream):
-        ws = _workspace(n, ws, grad.device)
+    if dtype not in _FLOATS:
+        raise ValueError(f"unsupported output dtype {dtype}")
+    with _on(grad.device, stream):
+        ws = _workspace(lambda: mol_embed_grad_workspace(C, V, d, T), ws, grad.device)
         if out is None:
             out = torch.empty((C, V, d), dtype=dtype, device=grad.device)
         else:
@@ -541,9 +539,8 @@ def softmax_loss(phi: torch.Tensor, target: torch.Tensor, ids: Optional[torch.Te
         _operand(row_weight, "row_weight", (B,), (torch.float32,), dev)
     if dphi is not None:
         _operand(dphi, "dphi", (B, N), (torch.float32,), dev)
-    n = mol_softmax_loss_workspace(B, N)
-    with _On(dev, stream):
-        ws = _workspace(n, ws, dev)
+    with _on(dev, stream):
+        ws = _workspace(lambda: mol_softmax_loss_workspace(B, N), ws, dev)
         loss = torch.empty((B,), dtype=torch.float32, device=dev)
         if dphi is None:
             dphi = torch.empty((B, N), dtype=torch.float32, device=dev)
@@ -560,11 +557,11 @@ def score_grad(prob: Problem, dphi: torch.Tensor, ws=None, stream=None, only: Op
     each of its tensor's shape and type."""
     _operand(dphi, "dphi", (prob.B, prob.N), (torch.float32,), prob.device)
     names = _GRADS if only is None else tuple(only)
-    _need(all(n in _GRADS for n in names), f"unknown gradient in {names}: {', '.join(_GRADS)}")
+    if not all(n in _GRADS for n in names):
+        raise ValueError(f"unknown gradient in {names}: {', '.join(_GRADS)}")
     _need(all(t is not None for t in prob.tensors), "the problem lacks a gating tensor")
-    n = mol_workspace_size(prob, MOL_OP_SCORE_GRAD)
-    with _On(prob.device, stream):
-        ws = _workspace(n, ws, prob.device)
+    with _on(prob.device, stream):
+        ws = _workspace(lambda: mol_workspace_size(prob, MOL_OP_SCORE_GRAD), ws, prob.device)
         out = {g: torch.empty_like(t) for g, t in zip(_GRADS, prob.tensors) if g in names}
         mol_score_grad(prob, dphi, out, ws, stream)
     return out
@@ -655,5 +652,5 @@ def adamw_step(tensors: AdamwTensors, lr=1e-3, beta1: float = 0.9, beta2: float 
     on_lr, on_step = isinstance(lr, torch.Tensor), isinstance(step, torch.Tensor)
     opt = MolAdamwC(0.0 if on_lr else lr, beta1, beta2, eps, 1 if on_step else step, seed & 0xFFFFFFFF, _ptr(grad_scale),
                     _ptr(lr) if on_lr else None, _ptr(step) if on_step else None)
-    with _On(tensors.device, stream):
+    with _on(tensors.device, stream):
         mol_adamw_step(opt, tensors.c, tensors.n, stream)
