@@ -30,11 +30,12 @@
 // What bounds it: the f32 matrix rate, 12 P H flop a pair (157 TFLOP/s).
 #include <algorithm>
 
-#include "mol_tile.h"
+#include "mol_grad.h"
 
 namespace mol {
 
 using namespace tile;
+using namespace grad;
 
 namespace {
 
@@ -439,16 +440,18 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims
 }
 
 // ---------------------------------------------------------------------------
-// [batch][rows][d] -> [batch][d][ld], zero from `rows` to `ld`; in_stride: elements a batch.
+// blockIdx.z < Px: item component blockIdx.z of X (none without xt); Px: Q.
 template <typename T>
-__global__ __launch_bounds__(256) void k_transpose(const T* __restrict__ in, long in_stride, long row0, int rows,
-                                                   int d, int ld, T* __restrict__ out) {
+__global__ __launch_bounds__(256) void k_transpose(DevProb pr, long m, int ldq, T* __restrict__ qt, int n0, int items,
+                                                   int ns, T* __restrict__ xt) {
   __shared__ T tile[32][33];
+  const bool is_q = static_cast<int>(blockIdx.z) == pr.Px;
+  const long rows = is_q ? m : items, r0 = static_cast<long>(blockIdx.x) * 32;
+  const int d = pr.d, ld = is_q ? ldq : ns, t0 = blockIdx.y * 32;
+  T* dst = is_q ? qt : xt ? xt + blockIdx.z * static_cast<long>(d) * ns : nullptr;
+  if (!dst || r0 >= ld) return;                                        // (the whole workgroup)
+  const T* src = is_q ? static_cast<const T*>(pr.Q) : static_cast<const T*>(pr.X) + (blockIdx.z * static_cast<long>(pr.N) + n0) * d;
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-  const long r0 = static_cast<long>(blockIdx.x) * 32;
-  const int t0 = blockIdx.y * 32;
-  const T* src = in + blockIdx.z * in_stride + row0 * d;
-  T* dst = out + blockIdx.z * static_cast<long>(d) * ld;
   for (int k = y; k < 32; k += 8) {
     T v = 0;
     if (r0 + k < rows && t0 + x < d) v = src[(r0 + k) * d + t0 + x];
@@ -557,45 +560,30 @@ __global__ __launch_bounds__(256) void k_grad_gemm(GemmDims gd, const uint32_t* 
 }
 
 // ---------------------------------------------------------------------------
-// Sums of partial results: out[o] = sum over s < S of in[s * stride + o], as
-// float32 (added to what an earlier slab left in acc) and, where wanted, in the
-// output's type.  Column groups of 64, four runs of s in a block.
-struct SumJob {
-  const float* in;
-  long L, stride;          // columns, floats between parts
-  int S;
-  int blocks;              // of 64 columns
-  float* acc;              // NULL, or float32 sums kept between slabs
-  int add;
-  void* out;               // NULL, or the output: o of batch o / batch_in goes to batch_out floats a batch
-  int bf16;
-  long in_len, out_len;    // elements of a batch (a px of dX): in the parts, in the output
-  long out_at;             // first element within a batch
-};
-constexpr int kSumJobs = 8;
-struct SumArgs {
-  int n;
-  int first[kSumJobs + 1];
-  SumJob job[kSumJobs];
-};
-
+// Sums of partial results (SumJob).  Few parts: a column a thread, 256 a
+// block; many: 64 columns and four runs of parts a block.
 __global__ __launch_bounds__(256) void k_sum_parts(SumArgs a) {
   __shared__ float sh[4][64];
   int j = 0;
   while (j + 1 < a.n && a.first[j + 1] <= static_cast<int>(blockIdx.x)) ++j;
   const SumJob& s = a.job[j];
   const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
-  const long o = (static_cast<long>(blockIdx.x) - a.first[j]) * 64 + lane;
+  const long blk = static_cast<long>(blockIdx.x) - a.first[j];
+  const long o = s.wide ? blk * 256 + threadIdx.x : blk * 64 + lane;
   float v = 0.f;
+  const int k0 = s.wide ? 0 : static_cast<int>(static_cast<long>(s.S) * run / 4);
+  const int k1 = s.wide ? s.S : static_cast<int>(static_cast<long>(s.S) * (run + 1) / 4);
   if (o < s.L) {
-    const int k0 = static_cast<int>(static_cast<long>(s.S) * run / 4), k1 = static_cast<int>(static_cast<long>(s.S) * (run + 1) / 4);
 #pragma unroll 8
     for (int k = k0; k < k1; ++k) v += s.in[k * s.stride + o];
   }
-  sh[run][lane] = v;
-  __syncthreads();
-  if (run || o >= s.L) return;
-  v = (sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane]);
+  if (!s.wide) {
+    sh[run][lane] = v;
+    __syncthreads();
+    if (run) return;
+    v = (sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane]);
+  }
+  if (o >= s.L) return;
   if (s.add) v += s.acc[o];
   if (s.acc) s.acc[o] = v;
   if (s.out) {
@@ -606,6 +594,36 @@ __global__ __launch_bounds__(256) void k_sum_parts(SumArgs a) {
       static_cast<float*>(s.out)[at] = v;
   }
 }
+
+namespace grad {
+
+void SumList::add(const SumJob& j) {
+  SumJob& s = a.job[a.n] = j;
+  s.wide = j.S <= 16 && j.L >= 4096;
+  s.blocks = static_cast<int>(s.wide ? (j.L + 255) / 256 : (j.L + 63) / 64);
+  a.first[a.n + 1] = a.first[a.n] + s.blocks;
+  ++a.n;
+}
+
+hipError_t SumList::run() {
+  if (a.n) hipLaunchKernelGGL(k_sum_parts, dim3(a.first[a.n]), dim3(256), 0, st, a);
+  a.n = 0;
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_transposes(const DevProb& pr, long m, int ldq, T* qt, int n0, int items, int ns, T* xt,
+                             hipStream_t st) {
+  if (!qt && !xt) return hipSuccess;
+  const long rows = std::max<long>(qt ? ldq : 0, xt ? ns : 0);
+  hipLaunchKernelGGL(k_transpose<T>, dim3(static_cast<unsigned>((rows + 31) / 32), (pr.d + 31) / 32, pr.Px + (qt ? 1 : 0)),
+                     dim3(256), 0, st, pr, m, ldq, qt, n0, items, ns, xt);
+  return hipGetLastError();
+}
+template hipError_t launch_transposes<bf16_t>(const DevProb&, long, int, bf16_t*, int, int, int, bf16_t*, hipStream_t);
+template hipError_t launch_transposes<float>(const DevProb&, long, int, float*, int, int, int, float*, hipStream_t);
+
+}  // namespace grad
 
 // ---------------------------------------------------------------------------
 // Host side.
@@ -621,11 +639,6 @@ struct GradPlan {
   long a_daq, a_dw1, a_dw2, a_db1;      // floats into the accumulators
   int wgs;
 };
-
-// parts of a product of `waves` waves a part, at least `chunks_min` K chunks each
-int split_of(long waves, long chunks, long chunks_min) {
-  return static_cast<int>(std::max<long>(1, std::min({(2048 + waves - 1) / waves, chunks / chunks_min, 64l})));
-}
 
 template <typename T, int PV>
 GradPlan plan_grad(const DevProb& pr) {
@@ -686,22 +699,6 @@ GradPlan plan_grad(const DevProb& pr) {
   return f;
 }
 
-struct SumList {
-  SumArgs a{};
-  hipStream_t st;
-  void add(const SumJob& j) {
-    a.job[a.n] = j;
-    a.job[a.n].blocks = static_cast<int>((j.L + 63) / 64);
-    a.first[a.n + 1] = a.first[a.n] + a.job[a.n].blocks;
-    ++a.n;
-  }
-  hipError_t run() {
-    if (a.n) hipLaunchKernelGGL(k_sum_parts, dim3(a.first[a.n]), dim3(256), 0, st, a);
-    a.n = 0;
-    return hipGetLastError();
-  }
-};
-
 template <typename T, int PV>
 hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads& o, char* ws, hipStream_t st) {
   const GradPlan f = plan_grad<T, PV>(pr);
@@ -724,16 +721,15 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
                                      static_cast<int>(f.lds));
   if (e != hipSuccess) return e;
-  const int dt = (pr.d + 31) / 32, cg = (pr.d + 63) / 64;
-  if (o.dX)
-    hipLaunchKernelGGL(k_transpose<T>, dim3((f.ldq + 31) / 32, dt, 1), dim3(256), 0, st, static_cast<const T*>(pr.Q), 0l,
-                       0l, static_cast<int>(dm.m), pr.d, f.ldq, qt);
-  SumList sums;
-  sums.st = st;
+  const int cg = (pr.d + 63) / 64;
+  SumList sums(st);
   for (int sl = 0; sl < f.slabs; ++sl) {
     const bool last = sl + 1 == f.slabs;
     dm.n0 = sl * f.slab;
     const int items = std::min(f.slab, pr.N - dm.n0);
+    if ((e = launch_transposes<T>(pr, dm.m, f.ldq, o.dX && sl == 0 ? qt : nullptr, dm.n0, items, f.slab, o.dQ ? xt : nullptr,
+                                  st)) != hipSuccess)
+      return e;
     for (int grp = 0; grp < f.groups; ++grp) {
       dm.group = grp;
       if (grp && !o.dW1 && !o.dW2 && !o.db1) break;
@@ -742,14 +738,12 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
     }
     const long P = pr.P, H = pr.H, BP = pr.B * P;
     if (o.dQ) {
-      hipLaunchKernelGGL(k_transpose<T>, dim3(f.slab / 32, dt, pr.Px), dim3(256), 0, st, static_cast<const T*>(pr.X),
-                         static_cast<long>(pr.N) * pr.d, static_cast<long>(dm.n0), items, pr.d, f.slab, xt);
       GemmDims gd{static_cast<int>(dm.m), pr.d, f.slab, dm.m * f.slab, f.slab, f.slab, pr.Px,
                   static_cast<long>(pr.d) * f.slab, f.slab, f.sp_q, sl > 0, 0, dm.m * pr.d};
       hipLaunchKernelGGL((k_grad_gemm<T, false>), dim3(static_cast<unsigned>((dm.m + 127) / 128), cg, f.sp_q), dim3(256),
                          0, st, gd, parts.ds, xt, F(f.off_pq));
       if (last)
-        sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, 0, nullptr, 0, o.dQ, bf, dm.m * pr.d, dm.m * pr.d, 0});
+        sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, nullptr, 0, o.dQ, bf, dm.m * pr.d, dm.m * pr.d, 0});
     }
     if (o.dX) {
       const long per_px = static_cast<long>(items) * pr.d;
@@ -757,23 +751,23 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
                   per_px * pr.Px};
       hipLaunchKernelGGL((k_grad_gemm<T, true>), dim3((items + 127) / 128, cg, f.sp_x * pr.Px), dim3(256), 0, st, gd,
                          parts.ds, qt, F(f.off_px));
-      sums.add({F(f.off_px), per_px * pr.Px, per_px * pr.Px, f.sp_x, 0, nullptr, 0, o.dX, bf, per_px,
+      sums.add({F(f.off_px), per_px * pr.Px, per_px * pr.Px, f.sp_x, nullptr, 0, o.dX, bf, per_px,
                 static_cast<long>(pr.N) * pr.d, static_cast<long>(dm.n0) * pr.d});
     }
     if (o.da_q || o.db2)
-      sums.add({parts.da_q, BP, BP, f.slab / 16, 0, acc + f.a_daq, sl > 0, last ? o.da_q : nullptr, 0, BP, BP, 0});
+      sums.add({parts.da_q, BP, BP, f.slab / 16, acc + f.a_daq, sl > 0, last ? o.da_q : nullptr, 0, BP, BP, 0});
     if (o.da_x)
-      sums.add({parts.da_x, items * P, f.slab * P, dm.qsplits, 0, nullptr, 0, o.da_x, 0, items * P, items * P,
+      sums.add({parts.da_x, items * P, f.slab * P, dm.qsplits, nullptr, 0, o.da_x, 0, items * P, items * P,
                 static_cast<long>(dm.n0) * P});
     if (o.dW1)
-      sums.add({parts.dW1, H * P, H * P, f.wgs, 0, acc + f.a_dw1, sl > 0, last ? o.dW1 : nullptr, bf, H * P, H * P, 0});
+      sums.add({parts.dW1, H * P, H * P, f.wgs, acc + f.a_dw1, sl > 0, last ? o.dW1 : nullptr, bf, H * P, H * P, 0});
     if (o.dW2)
-      sums.add({parts.dW2, H * P, H * P, f.wgs, 0, acc + f.a_dw2, sl > 0, last ? o.dW2 : nullptr, bf, H * P, H * P, 0});
-    if (o.db1) sums.add({parts.db1, H, H, f.wgs, 0, acc + f.a_db1, sl > 0, last ? o.db1 : nullptr, 0, H, H, 0});
+      sums.add({parts.dW2, H * P, H * P, f.wgs, acc + f.a_dw2, sl > 0, last ? o.dW2 : nullptr, bf, H * P, H * P, 0});
+    if (o.db1) sums.add({parts.db1, H, H, f.wgs, acc + f.a_db1, sl > 0, last ? o.db1 : nullptr, 0, H, H, 0});
     if ((e = sums.run()) != hipSuccess) return e;
   }
   if (o.db2) {
-    sums.add({acc + f.a_daq, pr.P, pr.P, pr.B, 0, nullptr, 0, o.db2, 0, pr.P, pr.P, 0});
+    sums.add({acc + f.a_daq, pr.P, pr.P, pr.B, nullptr, 0, o.db2, 0, pr.P, pr.P, 0});
     if ((e = sums.run()) != hipSuccess) return e;
   }
   return hipGetLastError();
@@ -782,12 +776,14 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
 }  // namespace
 
 size_t score_grad_bytes(const DevProb& pr) {
+  if (bf16_supported(pr)) return bf16_bytes(pr);
   if (pr.dtype == MOL_BF16)
     return (pr.P <= 16 ? plan_grad<bf16_t, 16>(pr) : pr.P <= 32 ? plan_grad<bf16_t, 32>(pr) : plan_grad<bf16_t, 64>(pr)).bytes;
   return (pr.P <= 16 ? plan_grad<float, 16>(pr) : pr.P <= 32 ? plan_grad<float, 32>(pr) : plan_grad<float, 64>(pr)).bytes;
 }
 
 hipError_t launch_score_grad(const DevProb& pr, const float* dphi, const mol_score_grads& o, void* ws, hipStream_t st) {
+  if (bf16_supported(pr)) return launch_bf16(pr, dphi, o, static_cast<char*>(ws), st);
   auto f = pr.dtype == MOL_BF16
                ? (pr.P <= 16 ? &run_grad<bf16_t, 16> : pr.P <= 32 ? &run_grad<bf16_t, 32> : &run_grad<bf16_t, 64>)
                : (pr.P <= 16 ? &run_grad<float, 16> : pr.P <= 32 ? &run_grad<float, 32> : &run_grad<float, 64>);

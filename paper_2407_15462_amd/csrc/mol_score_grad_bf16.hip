@@ -1,0 +1,844 @@
+// Gradient of the MoL scores for bf16 problems of up to 8 x 8 components and
+// 64 hidden units, on bf16 matrix instructions (mol_score_grad.hip has the
+// formulas and every other shape).
+//
+// Precision.  W1 and W2 are bf16, exact.  What meets them on the way to the
+// float32 outputs (s, h and dl) is split into three bf16 terms, 8 + 8 + 8 bits by
+// truncation: exact, so that a product is as good as a float32 one at three
+// bf16 MFMAs (of 8 times the f32 rate).  du for ds, and both factors of dW1 and
+// dW2, which end in bf16, take two terms (16 bits; the products of two second terms are left out).
+//
+// A wave takes units of 16 items of one query, independent of the other waves.
+// Lane (c = lane % 16, g = lane / 16) holds item c's slots (g, mu), mu < RUN,
+// of components pq = NPQ g + mu / PXP, px = mu % PXP: the dot products come out
+// of the MFMA in that layout (row 4 g + i of A is query component NPQ g + i, i
+// < NPQ; the other rows repeat it), and nothing is exchanged between lanes
+// up to the sums over items.  u^T = W1 s and dh^T = W2^T dl have K = the slots (K slot 8 g + e of
+// block m is (g, 8 m + e)), l^T += W2 h and ds^T += W1^T du have K = hidden
+// units (K slot 8 g + e of block m is j = 32 m + 16 (e / 4) + 4 g + e % 4, where
+// the accumulators of u and dh have them), and their output row 4 g + i of
+// tile pt is the lane's own slot (g, 4 pt + i).  W1 and W2 sit in LDS once,
+// as [j][slot] and [slot][j]; the transposed operands are read by the
+// transposing LDS read.  dW1 = sum du s^T and dW2 = sum dl h^T have K = items: the four
+// factors are written item by item (two terms each) and read transposed too.
+// dW1, dW2, db1 and da_x stay in registers over all of the wave's units.
+//
+// ds goes to the workspace as two bf16 terms, by blocks of 16 items, [px][item
+// block][b pq][16 first terms, 16 second terms]: 64-byte rows that both products read
+// whole.  dQ = sum ds X reads rows (K = items); dX = sum ds Q (K = b pq) takes them through LDS
+// and the transposing read.
+#include <algorithm>
+
+#include "mol_grad.h"
+
+namespace mol {
+
+using namespace tile;
+
+namespace {
+
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr size_t kSlabBytes = size_t(256) << 20;   // of ds
+constexpr int kAhead = 2;                          // blocks of 32 of d loaded ahead
+constexpr int kJT = 4;                             // hidden tiles of 16
+constexpr int kH = 16 * kJT;
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+// the transposing read: each group of 16 lanes reads 4 rows of 16 elements (8
+// bytes a lane, rows lane / 4) and gets column lane, its 4 rows in order
+__device__ __forceinline__ uint2 read_tr(const void* lds) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                       (lds_s16x4_t*)(__attribute__((address_space(3))) const void*)lds));
+}
+
+// high halves of a and b: their first bf16 terms by truncation
+__device__ __forceinline__ uint32_t high_halves(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ float rest(float a) { return a - __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
+
+// eight values as bf16 terms, two values a word
+template <int TERMS>
+struct Terms {
+  uint4 t[TERMS];
+};
+template <int TERMS>
+__device__ __forceinline__ Terms<TERMS> split(const float (&x)[8]) {
+  Terms<TERMS> o;
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = x[e];
+#pragma unroll
+  for (int k = 0; k < TERMS; ++k) {
+    o.t[k] = make_uint4(high_halves(v[0], v[1]), high_halves(v[2], v[3]), high_halves(v[4], v[5]), high_halves(v[6], v[7]));
+    if (k + 1 < TERMS)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = rest(v[e]);
+  }
+  return o;
+}
+template <int TERMS>
+__device__ __forceinline__ f32x4_t mfma_terms(uint4 a, const Terms<TERMS>& b, f32x4_t c) {
+#pragma unroll
+  for (int k = TERMS - 1; k >= 0; --k) c = mfma_bf16(a, b.t[k], c);   // small terms first
+  return c;
+}
+
+// Elements t .. t + 7 of a row of `d` at base + off bytes, of which base is the
+// same for the whole wave; past the row's end zeros (ZERO) or other elements of it
+template <bool VEC, bool ZERO>
+__device__ __forceinline__ uint4 row16(const bf16_t* base, uint32_t off, int t, int d) {
+  const char* p = reinterpret_cast<const char*>(base);
+  if constexpr (VEC) {                                                // (d is a multiple of 8)
+    const uint4 v = *reinterpret_cast<const uint4*>(p + (off + 2u * min(t, d - 8)));
+    return !ZERO || t < d ? v : make_uint4(0, 0, 0, 0);
+  } else {
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t x = *reinterpret_cast<const bf16_t*>(p + (off + 2u * min(t + e, d - 1)));
+      w[e / 2] |= (!ZERO || t + e < d ? x : 0u) << (16 * (e & 1));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+// A lane's offset, unknown to the compiler from here on: it would otherwise keep
+// the 64-bit sums of every base and offset in registers over the whole loop.
+__device__ __forceinline__ uint32_t fresh(uint32_t off) {
+  asm volatile("" : "+v"(off));
+  return off;
+}
+template <typename T>
+__device__ __forceinline__ const T& at32(const T* base, uint32_t bytes) {
+  return *reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + bytes);
+}
+
+// x[slot] summed over the 16 lanes of a row, lane c with the sum of slot c mod
+// RUN: at each step a lane passes on one half of its slots and keeps the
+// other, so that 16 slots take 15 additions and not 64
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int HALF, int CTRL, int LEN>
+__device__ __forceinline__ void fold(float (&v)[LEN], bool upper) {
+#pragma unroll
+  for (int i = 0; i < HALF; ++i) {
+    const float keep = upper ? v[i + HALF] : v[i], pass = upper ? v[i] : v[i + HALF];
+    v[i] = keep + dpp<CTRL>(pass);
+  }
+}
+template <int RUN>
+__device__ __forceinline__ float sum_items(const float (&x)[RUN], int c) {
+  constexpr int kRor8 = 0x128, kHalfMirror = 0x141, kReverse4 = 0x1B, kSwap2 = 0xB1;   // lane c ^ 8, c ^ 7, c ^ 3, c ^ 1
+  float v[RUN];
+#pragma unroll
+  for (int i = 0; i < RUN; ++i) v[i] = x[i];
+  if constexpr (RUN >= 16) fold<8, kRor8>(v, c & 8);
+  if constexpr (RUN >= 8) fold<4, kHalfMirror>(v, c & 4);
+  fold<2, kReverse4>(v, c & 2);
+  fold<1, kSwap2>(v, c & 1);
+  float t = v[0];
+  if constexpr (RUN < 16) t += dpp<kRor8>(t);
+  if constexpr (RUN < 8) t += dpp<0x124>(t);                           // (rotated by 4)
+  return t;
+}
+
+struct Bf16Dims {
+  int QB;            // waves that share 16 items: queries a step
+  int n0, ns, items; // the slab's first item, its padded length (a multiple of 32) and its items
+  int nb;            // its blocks of 16
+  int qsplits;       // query ranges
+  long m;            // B Pq
+};
+struct Bf16Parts {
+  uint32_t* ds;      // [Px][nb][m][16]
+  float* da_q;       // [nb][B][P]
+  float* da_x;       // [qsplits][ns][P]
+  float* dW1;        // [workgroups][H][P]
+  float* dW2;        // [workgroups][P][H]
+  float* db1;        // [workgroups][H]
+};
+
+// LDS bytes of a wave: s or dl, h and du by tiles of 16 slots or hidden units
+// (16 items x 32 bytes, first and second terms), k in the place of du
+template <int RUN>
+constexpr int wave_bytes() { return 1024 * (2 * (RUN / 4) + 2 * kJT); }
+// rows of W1 [j][slot] and W2 [slot][j]: 16 bytes past them spread the banks
+template <int RUN>
+constexpr int w1_row() { return 8 * RUN + 16; }
+constexpr int kW2Row = 2 * kH + 16;
+template <int RUN>
+constexpr int weight_bytes() { return kH * w1_row<RUN>() + 4 * RUN * kW2Row; }
+template <int RUN>
+constexpr int lds_bytes() { return weight_bytes<RUN>() + 4 * (kH + 4 * RUN) + kWaves * wave_bytes<RUN>(); }
+static_assert(lds_bytes<4>() >= 4 * kWaves * 16 * 16 && lds_bytes<16>() >= 4 * kWaves * 16 * 64, "the sums of da_x fit");
+
+}  // namespace
+
+// VEC: rows of Q and X allow 16-byte reads
+template <int NPQ, int PXP, bool VEC>
+__global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf16Dims dm,
+                                                                 const float* __restrict__ dphi, Bf16Parts out) {
+  constexpr int RUN = NPQ * PXP, SLOTS = 4 * RUN, PT = RUN / 4, KB = RUN > 8 ? RUN / 8 : 1;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smb[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane & 15, g = lane >> 4;
+  const int P = pr.P, H = pr.H, d = pr.d, N = pr.N, Pq = pr.Pq, Px = pr.Px, JT2 = (H + 31) / 32;
+  unsigned char* sW1 = smb;
+  unsigned char* sW2 = sW1 + kH * w1_row<RUN>();
+  float* sB1 = reinterpret_cast<float*>(sW2 + SLOTS * kW2Row);
+  float* sB2 = sB1 + kH;                                              // -inf in the slots of no component
+  unsigned char* mine = reinterpret_cast<unsigned char*>(sB2 + SLOTS) + wave * wave_bytes<RUN>();
+  unsigned char* sS = mine;                                           // s by tiles: first terms, second terms
+  unsigned char* sD = sS + 1024 * PT;                                 // dl
+  unsigned char* sH = sD + 1024 * PT;                                 // h
+  unsigned char* sU = sH + 1024 * kJT;                                // k (float32, as the lanes have it), then du
+  auto component = [&](int slot) {                                    // p of a slot, -1 for none
+    const int pq = NPQ * (slot / RUN) + slot % RUN / PXP, px = slot % PXP;
+    return pq < Pq && px < Px ? pq * Px + px : -1;
+  };
+  {
+    const bf16_t* W1 = static_cast<const bf16_t*>(pr.W1);
+    const bf16_t* W2 = static_cast<const bf16_t*>(pr.W2);
+    for (int i = tid; i < kH * SLOTS; i += kThreads) {
+      const int j = i / SLOTS, sl = i - j * SLOTS, p = component(sl);
+      const bool in = j < H && p >= 0;
+      *reinterpret_cast<bf16_t*>(sW1 + j * w1_row<RUN>() + 2 * sl) = in ? W1[j * P + p] : 0;
+      *reinterpret_cast<bf16_t*>(sW2 + sl * kW2Row + 2 * j) = in ? W2[p * H + j] : 0;
+    }
+    for (int i = tid; i < kH; i += kThreads) sB1[i] = i < H ? pr.b1[i] : 0.f;
+    for (int i = tid; i < SLOTS; i += kThreads) sB2[i] = component(i) >= 0 ? pr.b2[component(i)] : -__builtin_inff();
+  }
+  __syncthreads();
+
+  const int q = wave % dm.QB, blk = blockIdx.x * (kWaves / dm.QB) + wave / dm.QB;   // the wave's query of a step, its block
+  const bool has_blk = blk < dm.nb;
+  const int slot = 16 * min(blk, dm.nb - 1) + c;                                    // its item of the slab
+  const bool has_item = has_blk && slot < dm.items;
+  const int n = min(dm.n0 + slot, N - 1);
+  const bool whole = Px == PXP && Pq == 4 * NPQ && ((reinterpret_cast<uintptr_t>(pr.a_q) | reinterpret_cast<uintptr_t>(pr.a_x)) & 15) == 0;
+  const int row_pq = min(NPQ * (c >> 2) + min(c & 3, NPQ - 1), Pq - 1);             // the component of A row c
+  // offsets of a lane in 32 bits (the launcher sees to it), from bases that are the wave's
+  const bf16_t* X = static_cast<const bf16_t*>(pr.X);
+  const long x_px = static_cast<long>(N) * d;
+  const uint32_t x_off = 2u * static_cast<uint32_t>(n) * d, q_off = 2u * row_pq * d, ax_off = 4u * static_cast<uint32_t>(n) * P;
+  // where the lane's slots lie in a tile array: 8 bytes (16 of RUN > 4), halves of a row swapped from item 8 on
+  auto place = [&](int sl) { return (sl >> 4) * 1024 + c * 32 + ((((sl >> 3) & 1) ^ (c >> 3)) << 4) + ((sl & 4) << 1); };
+  // the transposing read of a tile: rows 4 g .. of items
+  const int tr = (4 * g + (c >> 2)) * 32 + ((((c & 3) >> 1) ^ (g >> 1)) << 4) + ((c & 1) << 3);
+
+  // the wave's part of the workgroup's dW1 (waves 0 to 3) or dW2: hidden tiles j0 .., slot tiles pt0 ..
+  constexpr int JW = PT == 4 ? 2 : 1, PW = PT == 1 ? 1 : 2;
+  const int sub = wave & 3, j0 = PT == 4 ? 2 * (sub >> 1) : sub, pt0 = PT == 4 ? 2 * (sub & 1) : 0;
+  const bool second = wave >= 4;
+  f32x4_t aw[JW][PW] = {}, ab1[kJT] = {};
+  float dax[RUN] = {};
+  // Operands of a unit's dot products for the first kAhead blocks of 32 of d, loaded a step ahead
+  constexpr int AHEAD = VEC ? kAhead : 0;
+  uint4 qf[AHEAD + 1], xf[AHEAD + 1][PXP];
+  float gr = 0.f, gr_next = 0.f;
+  auto fetch = [&](int b) {
+    const bf16_t* Q = static_cast<const bf16_t*>(pr.Q) + static_cast<long>(b) * Pq * d;
+    gr_next = at32(dphi + static_cast<long>(b) * N, fresh(4u * n));
+    const uint32_t qo = fresh(q_off), xo = fresh(x_off);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int t = 32 * k + 8 * g;
+      qf[k] = row16<VEC, true>(Q, qo, t, d);
+      const bf16_t* Xp = X;
+#pragma unroll
+      for (int px = 0; px < PXP; ++px, Xp += px < Px ? x_px : 0) xf[k][px] = row16<VEC, false>(Xp, xo, t, d);
+    }
+  };
+  const int steps = (pr.B + dm.QB - 1) / dm.QB;
+  const int st0 = static_cast<int>(static_cast<long>(steps) * blockIdx.y / dm.qsplits);
+  const int st1 = static_cast<int>(static_cast<long>(steps) * (blockIdx.y + 1) / dm.qsplits);
+  if (has_blk && st0 * dm.QB + q < pr.B) fetch(st0 * dm.QB + q);
+  for (int st = st0; st < st1; ++st) {
+    const int b = st * dm.QB + q;
+    const bool busy = has_blk && b < pr.B;                            // (the same for the whole wave)
+    if (busy) {
+    gr = has_item ? gr_next : 0.f;
+    // a_q and a_x, for l
+    f32x4_t l[PT], lx[PT];
+    {
+      const float* aq = pr.a_q + static_cast<long>(b) * P;
+      const uint32_t ao = fresh(ax_off), go = fresh(4u * RUN * g);
+#pragma unroll
+      for (int pt = 0; pt < PT; ++pt) {
+        if (whole) {
+          l[pt] = at32(reinterpret_cast<const f32x4_t*>(aq), go + 16u * pt);
+          lx[pt] = at32(reinterpret_cast<const f32x4_t*>(pr.a_x), ao + go + 16u * pt);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int mu = 4 * pt + i, p = min(NPQ * g + mu / PXP, Pq - 1) * Px + min(mu % PXP, Px - 1);
+            l[pt][i] = at32(aq, 4u * p);
+            lx[pt][i] = at32(pr.a_x, ao + 4u * p);
+          }
+        }
+      }
+    }
+    // s: one MFMA row tile of query components against the 16 items, each item component
+    float s[RUN];
+    {
+      f32x4_t acc[PXP] = {};
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+        for (int px = 0; px < PXP; ++px) acc[px] = mfma_bf16(qf[k], xf[k][px], acc[px]);
+      const bf16_t* Q = static_cast<const bf16_t*>(pr.Q) + static_cast<long>(b) * Pq * d;
+      const uint32_t qo = fresh(q_off), xo = fresh(x_off);
+      for (int k0 = 32 * AHEAD; k0 < d; k0 += 32) {
+        const int t = k0 + 8 * g;
+        const uint4 qv = row16<VEC, true>(Q, qo, t, d);               // (zeros past d meet X's own, finite, elements)
+        const bf16_t* Xp = X;
+#pragma unroll
+        for (int px = 0; px < PXP; ++px, Xp += px < Px ? x_px : 0)
+          acc[px] = mfma_bf16(qv, row16<VEC, false>(Xp, xo, t, d), acc[px]);
+      }
+#pragma unroll
+      for (int px = 0; px < PXP; ++px)
+#pragma unroll
+        for (int i = 0; i < NPQ; ++i) s[i * PXP + px] = acc[px][i];
+    }
+    // forward
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt) l[pt] = l[pt] + lx[pt] + *reinterpret_cast<const f32x4_t*>(sB2 + RUN * g + 4 * pt);
+    Terms<3> a[KB];
+    auto slots8 = [&](const float (&x)[RUN], int m) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = 8 * m + e < RUN ? x[(8 * m + e) % RUN] : 0.f;
+      return split<3>(v);
+    };
+    auto store_slots = [&](unsigned char* to) {                       // two terms, item by item
+#pragma unroll
+      for (int m = 0; m < KB; ++m)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          unsigned char* at = to + place(RUN * g + 8 * m) + 512 * k;
+          if constexpr (RUN >= 8)
+            *reinterpret_cast<uint4*>(at) = a[m].t[k];
+          else
+            *reinterpret_cast<uint2*>(at) = make_uint2(a[m].t[k].x, a[m].t[k].y);
+        }
+    };
+#pragma unroll
+    for (int m = 0; m < KB; ++m) a[m] = slots8(s, m);
+    store_slots(sS);
+#pragma unroll
+    for (int j2 = 0; j2 < kJT / 2; ++j2) {
+      if (j2 >= JT2) break;
+      float h[8];
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const int jt = 2 * j2 + hf;
+        const float4 bj = *reinterpret_cast<const float4*>(sB1 + 16 * jt + 4 * g);
+        f32x4_t u = f32x4_t{bj.x, bj.y, bj.z, bj.w};
+#pragma unroll
+        for (int m = 0; m < KB; ++m) {
+          uint4 w;
+          const unsigned char* at = sW1 + (16 * jt + c) * w1_row<RUN>() + 2 * (RUN * g + 8 * m);
+          if constexpr (RUN >= 8) {
+            w = *reinterpret_cast<const uint4*>(at);
+          } else {
+            const uint2 w2 = *reinterpret_cast<const uint2*>(at);
+            w = make_uint4(w2.x, w2.y, 0, 0);
+          }
+          u = mfma_terms<3>(w, a[m], u);
+        }
+        float4 k;
+        float kk[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float sig = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u[i]));
+          h[4 * hf + i] = u[i] * sig;
+          kk[i] = fmaf(h[4 * hf + i], 1.f - sig, sig);                // sig (1 + u (1 - sig))
+        }
+        k = float4{kk[0], kk[1], kk[2], kk[3]};
+        *reinterpret_cast<float4*>(sU + 1024 * jt + 16 * lane) = k;
+      }
+      const Terms<3> ht = split<3>(h);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        *reinterpret_cast<uint2*>(sH + 1024 * (2 * j2) + 512 * k + place(4 * g)) = make_uint2(ht.t[k].x, ht.t[k].y);
+        *reinterpret_cast<uint2*>(sH + 1024 * (2 * j2 + 1) + 512 * k + place(4 * g)) = make_uint2(ht.t[k].z, ht.t[k].w);
+      }
+#pragma unroll
+      for (int pt = 0; pt < PT; ++pt) {
+        // row c of tile pt: slot RUN (c / 4) + 4 pt + c % 4
+        const unsigned char* at = sW2 + (RUN * (c >> 2) + 4 * pt + (c & 3)) * kW2Row + 2 * (32 * j2 + 4 * g);
+        const uint2 w0 = *reinterpret_cast<const uint2*>(at), w1 = *reinterpret_cast<const uint2*>(at + 32);
+        l[pt] = mfma_terms<3>(make_uint4(w0.x, w0.y, w1.x, w1.y), ht, l[pt]);
+      }
+    }
+    // softmax, dl
+    float dl[RUN];
+    f32x4_t ds[PT];
+    {
+      float mx = l[0][0];
+#pragma unroll
+      for (int mu = 0; mu < RUN; ++mu) mx = fmaxf(mx, l[mu / 4][mu % 4]);
+      mx = max_groups(mx);
+      float den = 0.f, num = 0.f;
+#pragma unroll
+      for (int mu = 0; mu < RUN; ++mu) {
+        const float w = __builtin_amdgcn_exp2f(kLog2e * (l[mu / 4][mu % 4] - mx));   // 0 in the slots of no component
+        l[mu / 4][mu % 4] = w;
+        den += w;
+        num = fmaf(w, s[mu], num);
+      }
+      const float rden = 1.f / sum_groups(den), phi = sum_groups(num) * rden, gw = gr * rden;
+#pragma unroll
+      for (int mu = 0; mu < RUN; ++mu) {
+        const float gpi = gw * l[mu / 4][mu % 4];
+        ds[mu / 4][mu % 4] = gpi;
+        dl[mu] = gpi * (s[mu] - phi);
+        dax[mu] += dl[mu];
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < KB; ++m) a[m] = slots8(dl, m);
+    store_slots(sD);
+    // the next unit's operands, behind which there is still the way back
+    if (st + 1 < st1 && b + dm.QB < pr.B) fetch(b + dm.QB);
+    // da_q: sums over the 16 items, lane c of the group gets slot c's (c mod RUN)
+    {
+      const float t = sum_items<RUN>(dl, c);
+      const int pq = NPQ * g + c / PXP, px = c % PXP;
+      if (c < RUN && pq < Pq && px < Px) out.da_q[(static_cast<long>(blk) * pr.B + b) * P + pq * Px + px] = t;
+    }
+    // back through the MLP
+#pragma unroll
+    for (int j2 = 0; j2 < kJT / 2; ++j2) {
+      if (j2 >= JT2) break;
+      float du[8];
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const int jt = 2 * j2 + hf;
+        f32x4_t dh = {};
+#pragma unroll
+        for (int m = 0; m < KB; ++m) {
+          // A row j = 16 jt + c, K = slots RUN g + 8 m + e: columns of W2's rows
+          const unsigned char* at = sW2 + (RUN * g + 8 * m + (c >> 2)) * kW2Row + 2 * (16 * jt + 4 * (c & 3));
+          const uint2 w0 = read_tr(at);
+          const uint2 w1 = RUN >= 8 ? read_tr(at + 4 * kW2Row) : make_uint2(0, 0);
+          dh = mfma_terms<3>(make_uint4(w0.x, w0.y, w1.x, w1.y), a[m], dh);
+        }
+        const float4 k = *reinterpret_cast<const float4*>(sU + 1024 * jt + 16 * lane);
+        const float kk[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          du[4 * hf + i] = dh[i] * kk[i];
+          ab1[jt][i] += du[4 * hf + i];
+        }
+      }
+      const Terms<2> dt = split<2>(du);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {                                   // (in the place of k, which the wave has read)
+        *reinterpret_cast<uint2*>(sU + 1024 * (2 * j2) + 512 * k + place(4 * g)) = make_uint2(dt.t[k].x, dt.t[k].y);
+        *reinterpret_cast<uint2*>(sU + 1024 * (2 * j2 + 1) + 512 * k + place(4 * g)) = make_uint2(dt.t[k].z, dt.t[k].w);
+      }
+#pragma unroll
+      for (int pt = 0; pt < PT; ++pt) {
+        // A row slot RUN (c / 4) + 4 pt + c % 4, K = j: columns of W1's rows
+        const unsigned char* at = sW1 + (32 * j2 + 4 * g + (c >> 2)) * w1_row<RUN>() + 2 * (RUN * (c & 3) + 4 * pt);
+        const uint2 w0 = read_tr(at), w1 = read_tr(at + 16 * w1_row<RUN>());
+        ds[pt] = mfma_terms<2>(make_uint4(w0.x, w0.y, w1.x, w1.y), dt, ds[pt]);
+      }
+    }
+    // ds as two terms; lanes of a pair of items exchange them, the even one takes the first terms of both
+    {
+      const uint32_t pick = c & 1 ? 0x03020706u : 0x05040100u;        // (own word low in the permute)
+      uint32_t* to = out.ds + (static_cast<long>(blk) * dm.m + static_cast<long>(b) * Pq) * 16;
+      const uint32_t to_off = fresh(4u * (16 * NPQ * g + ((c & 1) << 3) + (c >> 1)));
+      const long px_step = static_cast<long>(dm.nb) * dm.m * 16;
+#pragma unroll
+      for (int px = 0; px < PXP; ++px, to += px_step)
+#pragma unroll
+      for (int i = 0; i < NPQ; ++i) {
+        const int mu = i * PXP + px;
+        const float v = ds[mu / 4][mu % 4];
+        const uint32_t hi = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+        const uint32_t lo = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v - __uint_as_float(hi << 16)));
+        const uint32_t own = hi | lo << 16;
+        const uint32_t other = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(own), 0xB1, 0xf, 0xf, true));   // quad_perm 1,0,3,2
+        // even: (own low, other low); odd: (other high, own high)
+        const uint32_t w = __builtin_amdgcn_perm(other, own, pick);
+        if (NPQ * g + i < Pq && px < Px) const_cast<uint32_t&>(at32(to, to_off + 64u * i)) = w;
+      }
+    }
+    } else {
+      // no unit: factors of zeros
+      for (int i = lane; i < wave_bytes<RUN>() / 16; i += 64) reinterpret_cast<uint4*>(mine)[i] = make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
+    // dW1 += du s^T, dW2^T += h dl^T over the eight units' items, two units a K block:
+    // slots 8 g + e are items 4 g + e % 4 of the one and the other
+    if (j0 < 2 * JT2) {
+      const unsigned char* u0 = reinterpret_cast<unsigned char*>(sB2 + SLOTS) + tr;
+      const unsigned char* pj = u0 + 1024 * (2 * PT + (second ? 0 : kJT) + j0);      // h or du
+      const unsigned char* pp = u0 + 1024 * ((second ? PT : 0) + pt0);               // dl or s
+#pragma unroll 1
+      for (int u = 0; u < kWaves; u += 2, pj += 2 * wave_bytes<RUN>(), pp += 2 * wave_bytes<RUN>()) {
+        uint4 fj[JW][2], fp[PW][2];
+        auto pair = [&](const unsigned char* at) {
+          const uint2 x = read_tr(at), y = read_tr(at + wave_bytes<RUN>());
+          return make_uint4(x.x, x.y, y.x, y.y);
+        };
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+          for (int j = 0; j < JW; ++j) fj[j][k] = pair(pj + 1024 * j + 512 * k);
+#pragma unroll
+          for (int i = 0; i < PW; ++i) fp[i][k] = pair(pp + 1024 * i + 512 * k);
+        }
+#pragma unroll
+        for (int k = 2; k >= 0; --k)                                  // small products first
+#pragma unroll
+          for (int j = 0; j < JW; ++j)
+#pragma unroll
+            for (int i = 0; i < PW; ++i) aw[j][i] = mfma_bf16(fj[j][k == 2], fp[i][k == 1], aw[j][i]);
+      }
+    }
+    __syncthreads();                                                  // read before the next units write
+  }
+
+  // the workgroup's sums
+  const long wg = static_cast<long>(blockIdx.y) * gridDim.x + blockIdx.x;
+#pragma unroll
+  for (int j = 0; j < JW; ++j)
+#pragma unroll
+    for (int i = 0; i < PW; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        // rows: hidden units, 4 g + r of a tile; columns: slots, c (of dW2 too, as its transpose)
+        const int jj = 16 * (j0 + j) + 4 * g + r, p = component(16 * (pt0 + i) + c);
+        if (jj < H && p >= 0) {
+          if (second) out.dW2[(wg * P + p) * H + jj] = aw[j][i][r];
+          else out.dW1[(wg * H + jj) * P + p] = aw[j][i][r];
+        }
+      }
+  float* acc = reinterpret_cast<float*>(smb);                         // (in the place of everything in LDS)
+#pragma unroll
+  for (int jt = 0; jt < kJT; ++jt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float t = ab1[jt][i];
+      t += row_ror<8>(t);
+      t += row_ror<4>(t);
+      t += row_ror<2>(t);
+      t += row_ror<1>(t);
+      if (c == 0) acc[wave * kH + 16 * jt + 4 * g + i] = t;
+    }
+  __syncthreads();
+  for (int i = tid; i < H; i += kThreads) {
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) t += acc[w * kH + i];
+    out.db1[wg * H + i] = t;
+  }
+  __syncthreads();
+  // da_x: the waves of a block's queries in turn
+  float* sx = acc + wave / dm.QB * (16 * SLOTS);                      // [blocks][16 items][slots]
+  for (int w = 0; w < dm.QB; ++w) {
+    __syncthreads();
+    if (q == w) {
+#pragma unroll
+      for (int mu = 0; mu < RUN; ++mu) {
+        float* o = sx + c * SLOTS + ((RUN * g + mu) ^ c);             // (spread over the banks)
+        *o = w ? *o + dax[mu] : dax[mu];
+      }
+    }
+  }
+  __syncthreads();
+  const int nblk = min(kWaves / dm.QB, dm.nb - static_cast<int>(blockIdx.x) * (kWaves / dm.QB));
+  for (int i = tid; i < nblk * 16 * SLOTS; i += kThreads) {
+    const int it = i / SLOTS, sl = i - it * SLOTS, p = component(sl);
+    if (p >= 0)
+      out.da_x[(static_cast<long>(blockIdx.y) * dm.ns + 16 * blockIdx.x * (kWaves / dm.QB) + it) * P + p] =
+          acc[it * SLOTS + (sl ^ (it & 15))];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// dQ and dX on matrix cores from ds: 32 rows and 64 columns a wave, K split.
+struct GemmBf16 {
+  int m, nb, d, npx;
+  int splits, add;
+  int items;         // dX: rows that exist
+};
+
+// dQ[m][t] = sum over px and items of ds X
+__global__ __launch_bounds__(256) void k_grad_dq_bf16(GemmBf16 gd, const uint32_t* __restrict__ ds,
+                                                      const bf16_t* __restrict__ xt, float* __restrict__ out) {
+  constexpr int RB = 2, CB = 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int m0 = (blockIdx.x * 4 + wave) * 16 * RB, t0 = blockIdx.y * 16 * CB;
+  if (m0 >= gd.m) return;
+  const int per = gd.nb / 2, chunks = per * gd.npx, ns = 16 * gd.nb;  // a chunk: two blocks of items
+  const int k0 = static_cast<int>(static_cast<long>(chunks) * blockIdx.z / gd.splits);
+  const int k1 = static_cast<int>(static_cast<long>(chunks) * (blockIdx.z + 1) / gd.splits);
+  f32x4_t acc[RB][CB] = {};
+  // items 8 g .. 8 g + 7 of a chunk: half g % 2 of block g / 2's row
+  const uint32_t* a[RB];
+  const bf16_t* bt[CB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+    a[r] = ds + (static_cast<long>(g >> 1) * gd.m + min(m0 + 16 * r + c, gd.m - 1)) * 16 + 4 * (g & 1);
+#pragma unroll
+  for (int t = 0; t < CB; ++t) bt[t] = xt + static_cast<long>(min(t0 + 16 * t + c, gd.d - 1)) * ns + 8 * g;
+  const long a_step = 32l * gd.m, x_px = static_cast<long>(gd.d) * ns;
+  uint4 hi[RB], lo[RB], bv[CB];
+  auto fetch = [&](int ch) {
+    const int px = ch / per, k = ch - px * per;
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      const uint32_t* p = a[r] + ch * a_step;                         // (px by px, the blocks follow each other)
+      hi[r] = *reinterpret_cast<const uint4*>(p);
+      lo[r] = *reinterpret_cast<const uint4*>(p + 8);
+    }
+#pragma unroll
+    for (int t = 0; t < CB; ++t) bv[t] = *reinterpret_cast<const uint4*>(bt[t] + px * x_px + 32 * k);
+  };
+  if (k0 < k1) fetch(k0);
+  for (int ch = k0; ch < k1; ++ch) {
+    uint4 h[RB], l[RB], b[CB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      h[r] = hi[r];
+      l[r] = lo[r];
+    }
+#pragma unroll
+    for (int t = 0; t < CB; ++t) b[t] = bv[t];
+    if (ch + 1 < k1) fetch(ch + 1);
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(h[r], b[t], mfma_bf16(l[r], b[t], acc[r][t]));
+  }
+  float* dst = out + static_cast<long>(blockIdx.z) * gd.m * gd.d;
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int t = 0; t < CB; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int m = m0 + 16 * r + 4 * g + i, x = t0 + 16 * t + c;
+        if (m < gd.m && x < gd.d) {
+          float* o = dst + static_cast<long>(m) * gd.d + x;
+          *o = gd.add ? *o + acc[r][t][i] : acc[r][t][i];
+        }
+      }
+}
+
+// dX[px][n][t] = sum over (b, pq) of ds Q: rows of ds of a block of items, 32
+// at a time, through the wave's LDS and the transposing read
+__global__ __launch_bounds__(256) void k_grad_dx_bf16(GemmBf16 gd, const uint32_t* __restrict__ ds,
+                                                      const bf16_t* __restrict__ qt, int ldq, float* __restrict__ out) {
+  constexpr int RB = 2, CB = 4;
+  __shared__ __attribute__((aligned(16))) uint4 sh[4][RB * 128];      // [block][32 rows][64 bytes] a wave
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int blk0 = (blockIdx.x * 4 + wave) * RB, t0 = blockIdx.y * 16 * CB;
+  if (blk0 >= gd.nb) return;                                          // (no workgroup barrier below)
+  const int px = blockIdx.z / gd.splits, split = blockIdx.z - px * gd.splits;
+  const int chunks = (gd.m + 31) / 32;
+  const int k0 = static_cast<int>(static_cast<long>(chunks) * split / gd.splits);
+  const int k1 = static_cast<int>(static_cast<long>(chunks) * (split + 1) / gd.splits);
+  f32x4_t acc[RB][CB] = {};
+  const uint4* a[RB];
+  const bf16_t* bt[CB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+    a[r] = reinterpret_cast<const uint4*>(ds + (static_cast<long>(px) * gd.nb + min(blk0 + r, gd.nb - 1)) * gd.m * 16);
+#pragma unroll
+  for (int t = 0; t < CB; ++t) bt[t] = qt + static_cast<long>(min(t0 + 16 * t + c, gd.d - 1)) * ldq + 8 * g;
+  uint4 av[RB][2], bv[CB];
+  const long last = static_cast<long>(gd.m) * 4 - 1;                  // 16-byte pieces of a block's rows
+  auto fetch = [&](int ch) {
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const long at = ch * 128l + e * 64 + lane;
+        const uint4 v = a[r][min(at, last)];
+        av[r][e] = at <= last ? v : make_uint4(0, 0, 0, 0);           // (rows past b pq: Q's are zero too)
+      }
+#pragma unroll
+    for (int t = 0; t < CB; ++t) bv[t] = *reinterpret_cast<const uint4*>(bt[t] + 32 * ch);
+  };
+  const unsigned char* mine = reinterpret_cast<const unsigned char*>(sh[wave]);
+  // K slots 8 g + e: rows 8 g + e
+  const int tr = (8 * g + (c >> 2)) * 64 + 8 * (c & 3);
+  if (k0 < k1) fetch(k0);
+  for (int ch = k0; ch < k1; ++ch) {
+    uint4 b[CB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      sh[wave][r * 128 + lane] = av[r][0];
+      sh[wave][r * 128 + 64 + lane] = av[r][1];
+    }
+#pragma unroll
+    for (int t = 0; t < CB; ++t) b[t] = bv[t];
+    wave_lds_sync();
+    if (ch + 1 < k1) fetch(ch + 1);
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      const unsigned char* p = mine + r * 2048 + tr;
+      const uint2 h0 = read_tr(p), h1 = read_tr(p + 256), l0 = read_tr(p + 32), l1 = read_tr(p + 288);
+      const uint4 h = make_uint4(h0.x, h0.y, h1.x, h1.y), l = make_uint4(l0.x, l0.y, l1.x, l1.y);
+#pragma unroll
+      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(h, b[t], mfma_bf16(l, b[t], acc[r][t]));
+    }
+    wave_lds_sync();
+  }
+  const long per_px = static_cast<long>(gd.items) * gd.d;
+  float* dst = out + (static_cast<long>(split) * gd.npx + px) * per_px;
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int t = 0; t < CB; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int m = 16 * (blk0 + r) + 4 * g + i, x = t0 + 16 * t + c;
+        if (m < gd.items && x < gd.d) dst[static_cast<long>(m) * gd.d + x] = acc[r][t][i];
+      }
+}
+
+// ---------------------------------------------------------------------------
+namespace grad {
+
+namespace {
+
+struct Bf16Plan {
+  Bf16Dims dm;
+  int slab, slabs, wgx, wgs;
+  int sp_q, sp_x, ldq;
+  size_t off_ds, off_xt, off_qt, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_pq, off_px, off_acc, bytes;
+  long a_dw1, a_dw2, a_db1;
+};
+
+Bf16Plan plan(const DevProb& pr) {
+  Bf16Plan f{};
+  Bf16Dims& dm = f.dm;
+  dm.QB = pr.B >= 8 ? 8 : pr.B >= 4 ? 4 : pr.B >= 2 ? 2 : 1;
+  dm.m = static_cast<long>(pr.B) * pr.Pq;
+  const long blocks = (pr.N + 31l) / 32;                              // slabs of whole pairs of 16 items
+  const long fit = std::max<long>(1, static_cast<long>(kSlabBytes) / (128l * pr.Px * dm.m));
+  f.slabs = static_cast<int>((blocks + fit - 1) / fit);
+  f.slab = static_cast<int>((blocks + f.slabs - 1) / f.slabs * 32);
+  f.slabs = static_cast<int>((static_cast<long>(pr.N) + f.slab - 1) / f.slab);
+  dm.ns = f.slab;
+  dm.nb = f.slab / 16;
+  const int steps = (pr.B + dm.QB - 1) / dm.QB, per = kWaves / dm.QB;
+  f.wgx = (dm.nb + per - 1) / per;
+  dm.qsplits = std::max(1, std::min(steps, 256 / f.wgx));
+  f.wgs = f.wgx * dm.qsplits;
+  f.ldq = static_cast<int>((dm.m + 31) / 32 * 32);
+  const long cg = (pr.d + 63) / 64;
+  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * dm.nb / 2, 8);
+  f.sp_x = split_of(static_cast<long>(dm.nb) / 2 * cg * pr.Px, f.ldq / 32, 8);
+  auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+  size_t at = 0;
+  const size_t P = pr.P, H = pr.H;
+  f.off_ds = at;  at = up(at + 4ul * pr.Px * dm.m * f.slab);
+  f.off_xt = at;  at = up(at + 2ul * pr.Px * pr.d * f.slab);
+  f.off_qt = at;  at = up(at + 2ul * pr.d * f.ldq);
+  f.off_daq = at; at = up(at + 4ul * dm.nb * pr.B * P);
+  f.off_dax = at; at = up(at + 4ul * dm.qsplits * f.slab * P);
+  f.off_dw1 = at; at = up(at + 4ul * f.wgs * H * P);
+  f.off_dw2 = at; at = up(at + 4ul * f.wgs * H * P);
+  f.off_db1 = at; at = up(at + 4ul * f.wgs * H);
+  f.off_pq = at;  at = up(at + 4ul * f.sp_q * dm.m * pr.d);
+  f.off_px = at;  at = up(at + 4ul * f.sp_x * pr.Px * f.slab * pr.d);
+  f.a_dw1 = static_cast<long>(pr.B) * P;
+  f.a_dw2 = f.a_dw1 + static_cast<long>(H * P);
+  f.a_db1 = f.a_dw2 + static_cast<long>(H * P);
+  f.off_acc = at; at = up(at + 4ul * (f.a_db1 + H));
+  f.bytes = at;
+  return f;
+}
+
+template <int NPQ, int PXP>
+hipError_t launch_pairs(const DevProb& pr, const Bf16Plan& f, const Bf16Dims& dm, const float* dphi,
+                        const Bf16Parts& parts, hipStream_t st) {
+  const bool vec = pr.d % 8 == 0 && ((reinterpret_cast<uintptr_t>(pr.Q) | reinterpret_cast<uintptr_t>(pr.X)) & 15) == 0;
+  auto kern = vec ? &k_score_grad_bf16<NPQ, PXP, true> : &k_score_grad_bf16<NPQ, PXP, false>;
+  constexpr int lds = lds_bytes<NPQ * PXP>();
+  static_assert(lds <= 160 * 1024, "LDS");
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kern, dim3(f.wgx, dm.qsplits), dim3(kThreads), lds, st, pr, dm, dphi, parts);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+bool bf16_supported(const DevProb& pr) {
+  // (a lane's offsets from its wave's bases in 32 bits)
+  return pr.dtype == MOL_BF16 && pr.Pq <= 8 && pr.Px <= 8 && pr.H <= kH && static_cast<long>(pr.N) * pr.d < (1l << 31) &&
+         static_cast<long>(pr.N) * pr.P < (1l << 30);
+}
+
+size_t bf16_bytes(const DevProb& pr) { return plan(pr).bytes; }
+
+hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_grads& o, char* ws, hipStream_t st) {
+  const Bf16Plan f = plan(pr);
+  Bf16Dims dm = f.dm;
+  auto F = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
+  const Bf16Parts parts{reinterpret_cast<uint32_t*>(ws + f.off_ds), F(f.off_daq), F(f.off_dax), F(f.off_dw1),
+                        F(f.off_dw2), F(f.off_db1)};
+  bf16_t* xt = reinterpret_cast<bf16_t*>(ws + f.off_xt);
+  bf16_t* qt = reinterpret_cast<bf16_t*>(ws + f.off_qt);
+  float* acc = F(f.off_acc);
+  auto pairs = pr.Pq <= 4 && pr.Px <= 4 ? &launch_pairs<1, 4> : pr.Px <= 4 ? &launch_pairs<2, 4> : &launch_pairs<2, 8>;
+  const int cg = (pr.d + 63) / 64;
+  const long P = pr.P, H = pr.H, BP = pr.B * P;
+  SumList sums(st);
+  for (int sl = 0; sl < f.slabs; ++sl) {
+    const bool last = sl + 1 == f.slabs;
+    dm.n0 = sl * f.slab;
+    dm.items = std::min(f.slab, pr.N - dm.n0);
+    hipError_t e = launch_transposes<bf16_t>(pr, dm.m, f.ldq, o.dX && sl == 0 ? qt : nullptr, dm.n0, dm.items, dm.ns,
+                                             o.dQ ? xt : nullptr, st);
+    if (e != hipSuccess) return e;
+    if ((e = pairs(pr, f, dm, dphi, parts, st)) != hipSuccess) return e;
+    if (o.dQ) {
+      const GemmBf16 gd{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_q, sl > 0, dm.items};
+      hipLaunchKernelGGL(k_grad_dq_bf16, dim3(static_cast<unsigned>((dm.m + 127) / 128), cg, f.sp_q), dim3(256), 0, st, gd,
+                         parts.ds, xt, F(f.off_pq));
+      if (last)
+        sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, nullptr, 0, o.dQ, 1, dm.m * pr.d, dm.m * pr.d, 0});
+    }
+    if (o.dX) {
+      const long per_px = static_cast<long>(dm.items) * pr.d;
+      const GemmBf16 gd{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_x, 0, dm.items};
+      hipLaunchKernelGGL(k_grad_dx_bf16, dim3((dm.nb + 7) / 8, cg, f.sp_x * pr.Px), dim3(256), 0, st, gd, parts.ds, qt,
+                         f.ldq, F(f.off_px));
+      sums.add({F(f.off_px), per_px * pr.Px, per_px * pr.Px, f.sp_x, nullptr, 0, o.dX, 1, per_px,
+                static_cast<long>(pr.N) * pr.d, static_cast<long>(dm.n0) * pr.d});
+    }
+    if (o.da_q || o.db2)
+      sums.add({parts.da_q, BP, BP, dm.nb, acc, sl > 0, last ? o.da_q : nullptr, 0, BP, BP, 0});
+    if (o.da_x)
+      sums.add({parts.da_x, dm.items * P, f.slab * P, dm.qsplits, nullptr, 0, o.da_x, 0, dm.items * P, dm.items * P,
+                static_cast<long>(dm.n0) * P});
+    if (o.dW1)
+      sums.add({parts.dW1, H * P, H * P, f.wgs, acc + f.a_dw1, sl > 0, last ? o.dW1 : nullptr, 1, H * P, H * P, 0});
+    if (o.dW2)
+      sums.add({parts.dW2, H * P, H * P, f.wgs, acc + f.a_dw2, sl > 0, last ? o.dW2 : nullptr, 1, H * P, H * P, 0});
+    if (o.db1) sums.add({parts.db1, H, H, f.wgs, acc + f.a_db1, sl > 0, last ? o.db1 : nullptr, 0, H, H, 0});
+    if ((e = sums.run()) != hipSuccess) return e;
+  }
+  if (o.db2) sums.add({acc, P, P, pr.B, nullptr, 0, o.db2, 0, P, P, 0});
+  return sums.run();
+}
+
+}  // namespace grad
+
+}  // namespace mol
