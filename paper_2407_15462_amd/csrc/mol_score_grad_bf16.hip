@@ -87,19 +87,19 @@ __device__ __forceinline__ f32x4_t mfma_terms(uint4 a, const Terms<TERMS>& b, f3
 }
 
 // Elements t .. t + 7 of a row of `d` at base + off bytes, of which base is the
-// same for the whole wave; past the row's end zeros (ZERO) or other elements of it
-template <bool VEC, bool ZERO>
-__device__ __forceinline__ uint4 row16(const bf16_t* base, uint32_t off, int t, int d) {
+// same for the whole wave; past the row's end zeros, or other elements of it
+template <bool VEC>
+__device__ __forceinline__ uint4 row16_of(const bf16_t* base, uint32_t off, int t, int d, bool zero) {
   const char* p = reinterpret_cast<const char*>(base);
   if constexpr (VEC) {                                                // (d is a multiple of 8)
     const uint4 v = *reinterpret_cast<const uint4*>(p + (off + 2u * min(t, d - 8)));
-    return !ZERO || t < d ? v : make_uint4(0, 0, 0, 0);
+    return !zero || t < d ? v : make_uint4(0, 0, 0, 0);
   } else {
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const uint32_t x = *reinterpret_cast<const bf16_t*>(p + (off + 2u * min(t + e, d - 1)));
-      w[e / 2] |= (!ZERO || t + e < d ? x : 0u) << (16 * (e & 1));
+      w[e / 2] |= (!zero || t + e < d ? x : 0u) << (16 * (e & 1));
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
@@ -166,20 +166,20 @@ struct Bf16Parts {
 // (16 items x 32 bytes, first and second terms), k in the place of du
 template <int RUN>
 constexpr int wave_bytes() { return 1024 * (2 * (RUN / 4) + 2 * kJT); }
-// rows of W1 [j][slot] and W2 [slot][j]: 16 bytes past them spread the banks
+// W1 [j][slot] and W2 [slot][j], rows without padding
 template <int RUN>
-constexpr int w1_row() { return 8 * RUN + 16; }
-constexpr int kW2Row = 2 * kH + 16;
+constexpr int weight_bytes() { return 2 * kH * 4 * RUN * 2; }
 template <int RUN>
-constexpr int weight_bytes() { return kH * w1_row<RUN>() + 4 * RUN * kW2Row; }
-template <int RUN>
-constexpr int lds_bytes() { return weight_bytes<RUN>() + 4 * (kH + 4 * RUN) + kWaves * wave_bytes<RUN>(); }
+constexpr int lds_bytes() { return weight_bytes<RUN>() + kWaves * wave_bytes<RUN>(); }
+// Bytes of the items' rows in LDS, [px][d / 8, whole K blocks][16 items][16 bytes]
+inline int x_bytes(int pxp, int d) { return pxp * ((d + 31) / 32 * 4) * 256; }
 static_assert(lds_bytes<4>() >= 4 * kWaves * 16 * 16 && lds_bytes<16>() >= 4 * kWaves * 16 * 64, "the sums of da_x fit");
 
 }  // namespace
 
-// VEC: rows of Q and X allow 16-byte reads
-template <int NPQ, int PXP, bool VEC>
+// XL: the workgroup's waves share 16 items, whose rows lie in LDS.  FULL: P_q = 4
+// NPQ, P_x = PXP, and every row allows 16-byte reads (H a multiple of 4).
+template <int NPQ, int PXP, bool XL, bool FULL>
 __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf16Dims dm,
                                                                  const float* __restrict__ dphi, Bf16Parts out) {
   constexpr int RUN = NPQ * PXP, SLOTS = 4 * RUN, PT = RUN / 4, KB = RUN > 8 ? RUN / 8 : 1;
@@ -187,45 +187,60 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g = lane >> 4;
-  const int P = pr.P, H = pr.H, d = pr.d, N = pr.N, Pq = pr.Pq, Px = pr.Px, JT2 = (H + 31) / 32;
+  const int P = pr.P, H = pr.H, d = pr.d, N = pr.N, JT2 = (H + 31) / 32, nch = (d + 31) / 32 * 4;
+  const int Pq = FULL ? 4 * NPQ : pr.Pq, Px = FULL ? PXP : pr.Px;
   unsigned char* sW1 = smb;
-  unsigned char* sW2 = sW1 + kH * w1_row<RUN>();
-  float* sB1 = reinterpret_cast<float*>(sW2 + SLOTS * kW2Row);
-  float* sB2 = sB1 + kH;                                              // -inf in the slots of no component
-  unsigned char* mine = reinterpret_cast<unsigned char*>(sB2 + SLOTS) + wave * wave_bytes<RUN>();
+  unsigned char* sW2 = sW1 + 2 * kH * SLOTS;
+  unsigned char* waves = sW2 + 2 * kH * SLOTS;
+  unsigned char* mine = waves + wave * wave_bytes<RUN>();
   unsigned char* sS = mine;                                           // s by tiles: first terms, second terms
   unsigned char* sD = sS + 1024 * PT;                                 // dl
   unsigned char* sH = sD + 1024 * PT;                                 // h
   unsigned char* sU = sH + 1024 * kJT;                                // k (float32, as the lanes have it), then du
+  uint4* sX = reinterpret_cast<uint4*>(waves + kWaves * wave_bytes<RUN>());
   auto component = [&](int slot) {                                    // p of a slot, -1 for none
     const int pq = NPQ * (slot / RUN) + slot % RUN / PXP, px = slot % PXP;
     return pq < Pq && px < Px ? pq * Px + px : -1;
   };
-  {
-    const bf16_t* W1 = static_cast<const bf16_t*>(pr.W1);
-    const bf16_t* W2 = static_cast<const bf16_t*>(pr.W2);
-    for (int i = tid; i < kH * SLOTS; i += kThreads) {
-      const int j = i / SLOTS, sl = i - j * SLOTS, p = component(sl);
-      const bool in = j < H && p >= 0;
-      *reinterpret_cast<bf16_t*>(sW1 + j * w1_row<RUN>() + 2 * sl) = in ? W1[j * P + p] : 0;
-      *reinterpret_cast<bf16_t*>(sW2 + sl * kW2Row + 2 * j) = in ? W2[p * H + j] : 0;
-    }
-    for (int i = tid; i < kH; i += kThreads) sB1[i] = i < H ? pr.b1[i] : 0.f;
-    for (int i = tid; i < SLOTS; i += kThreads) sB2[i] = component(i) >= 0 ? pr.b2[component(i)] : -__builtin_inff();
-  }
-  __syncthreads();
+  // byte of an element of W1 (row j) and W2 (row a slot): the 8-byte pieces of a
+  // row are rotated by two for each row, so that rows meet different banks
+  auto w1_at = [](int j, int sl) { return j * (2 * SLOTS) + ((2 * sl + 16 * j) & (2 * SLOTS - 1)); };
+  auto w2_at = [](int sl, int j) { return sl * (2 * kH) + ((2 * j + 16 * sl) & (2 * kH - 1)); };
+  const bool vec = FULL || (d % 8 == 0 && ((reinterpret_cast<uintptr_t>(pr.Q) | reinterpret_cast<uintptr_t>(pr.X)) & 15) == 0);
+  auto row16 = [&](const bf16_t* base, uint32_t off, int t, bool zero) {
+    return vec ? row16_of<true>(base, off, t, d, zero) : row16_of<false>(base, off, t, d, zero);
+  };
 
   const int q = wave % dm.QB, blk = blockIdx.x * (kWaves / dm.QB) + wave / dm.QB;   // the wave's query of a step, its block
   const bool has_blk = blk < dm.nb;
   const int slot = 16 * min(blk, dm.nb - 1) + c;                                    // its item of the slab
   const bool has_item = has_blk && slot < dm.items;
   const int n = min(dm.n0 + slot, N - 1);
-  const bool whole = Px == PXP && Pq == 4 * NPQ && ((reinterpret_cast<uintptr_t>(pr.a_q) | reinterpret_cast<uintptr_t>(pr.a_x)) & 15) == 0;
   const int row_pq = min(NPQ * (c >> 2) + min(c & 3, NPQ - 1), Pq - 1);             // the component of A row c
   // offsets of a lane in 32 bits (the launcher sees to it), from bases that are the wave's
   const bf16_t* X = static_cast<const bf16_t*>(pr.X);
   const long x_px = static_cast<long>(N) * d;
   const uint32_t x_off = 2u * static_cast<uint32_t>(n) * d, q_off = 2u * row_pq * d, ax_off = 4u * static_cast<uint32_t>(n) * P;
+  {
+    const bf16_t* W1 = static_cast<const bf16_t*>(pr.W1);
+    const bf16_t* W2 = static_cast<const bf16_t*>(pr.W2);
+    for (int i = tid; i < kH * SLOTS; i += kThreads) {
+      const int j = i / SLOTS, sl = i - j * SLOTS, p = component(sl);
+      const bool in = j < H && p >= 0;
+      *reinterpret_cast<bf16_t*>(sW1 + w1_at(j, sl)) = in ? W1[j * P + p] : 0;
+      *reinterpret_cast<bf16_t*>(sW2 + w2_at(sl, j)) = in ? W2[p * H + j] : 0;
+    }
+    if constexpr (XL) {
+      // (zeros past d would do no good here: Q has them)
+      for (int i = tid; i < PXP * nch * 16; i += kThreads) {
+        const int it = i & 15, ch = (i >> 4) % nch, px = (i >> 4) / nch;
+        const int item = min(dm.n0 + 16 * static_cast<int>(blockIdx.x) + it, N - 1);
+        sX[i] = row16(X + min(px, Px - 1) * x_px, 2u * static_cast<uint32_t>(item) * d, 8 * ch, false);
+      }
+    }
+  }
+  __syncthreads();
+
   // where the lane's slots lie in a tile array: 8 bytes (16 of RUN > 4), halves of a row swapped from item 8 on
   auto place = [&](int sl) { return (sl >> 4) * 1024 + c * 32 + ((((sl >> 3) & 1) ^ (c >> 3)) << 4) + ((sl & 4) << 1); };
   // the transposing read of a tile: rows 4 g .. of items
@@ -237,22 +252,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
   const bool second = wave >= 4;
   f32x4_t aw[JW][PW] = {}, ab1[kJT] = {};
   float dax[RUN] = {};
-  // Operands of a unit's dot products for the first kAhead blocks of 32 of d, loaded a step ahead
-  constexpr int AHEAD = VEC ? kAhead : 0;
-  uint4 qf[AHEAD + 1], xf[AHEAD + 1][PXP];
+  // what a unit reads from its query's rows, loaded a step ahead
+  uint4 qf[kAhead];
   float gr = 0.f, gr_next = 0.f;
   auto fetch = [&](int b) {
     const bf16_t* Q = static_cast<const bf16_t*>(pr.Q) + static_cast<long>(b) * Pq * d;
     gr_next = at32(dphi + static_cast<long>(b) * N, fresh(4u * n));
-    const uint32_t qo = fresh(q_off), xo = fresh(x_off);
+    const uint32_t qo = fresh(q_off);
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      const int t = 32 * k + 8 * g;
-      qf[k] = row16<VEC, true>(Q, qo, t, d);
-      const bf16_t* Xp = X;
-#pragma unroll
-      for (int px = 0; px < PXP; ++px, Xp += px < Px ? x_px : 0) xf[k][px] = row16<VEC, false>(Xp, xo, t, d);
-    }
+    for (int k = 0; k < kAhead; ++k) qf[k] = row16(Q, qo, 32 * k + 8 * g, true);
   };
   const int steps = (pr.B + dm.QB - 1) / dm.QB;
   const int st0 = static_cast<int>(static_cast<long>(steps) * blockIdx.y / dm.qsplits);
@@ -263,22 +271,25 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
     const bool busy = has_blk && b < pr.B;                            // (the same for the whole wave)
     if (busy) {
     gr = has_item ? gr_next : 0.f;
-    // a_q and a_x, for l
-    f32x4_t l[PT], lx[PT];
+    // a_q, a_x and b2, for l
+    f32x4_t l[PT], lx[PT], b2[PT];
     {
       const float* aq = pr.a_q + static_cast<long>(b) * P;
       const uint32_t ao = fresh(ax_off), go = fresh(4u * RUN * g);
 #pragma unroll
       for (int pt = 0; pt < PT; ++pt) {
-        if (whole) {
+        if constexpr (FULL) {
           l[pt] = at32(reinterpret_cast<const f32x4_t*>(aq), go + 16u * pt);
           lx[pt] = at32(reinterpret_cast<const f32x4_t*>(pr.a_x), ao + go + 16u * pt);
+          b2[pt] = at32(reinterpret_cast<const f32x4_t*>(pr.b2), go + 16u * pt);
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int mu = 4 * pt + i, p = min(NPQ * g + mu / PXP, Pq - 1) * Px + min(mu % PXP, Px - 1);
             l[pt][i] = at32(aq, 4u * p);
             lx[pt][i] = at32(pr.a_x, ao + 4u * p);
+            const float v = at32(pr.b2, 4u * p);
+            b2[pt][i] = NPQ * g + mu / PXP < Pq && mu % PXP < Px ? v : -__builtin_inff();   // no component
           }
         }
       }
@@ -287,28 +298,49 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
     float s[RUN];
     {
       f32x4_t acc[PXP] = {};
-#pragma unroll
-      for (int k = 0; k < AHEAD; ++k)
-#pragma unroll
-        for (int px = 0; px < PXP; ++px) acc[px] = mfma_bf16(qf[k], xf[k][px], acc[px]);
       const bf16_t* Q = static_cast<const bf16_t*>(pr.Q) + static_cast<long>(b) * Pq * d;
       const uint32_t qo = fresh(q_off), xo = fresh(x_off);
-      for (int k0 = 32 * AHEAD; k0 < d; k0 += 32) {
-        const int t = k0 + 8 * g;
-        const uint4 qv = row16<VEC, true>(Q, qo, t, d);               // (zeros past d meet X's own, finite, elements)
+      auto block = [&](int k, uint4 qv) {                             // (zeros of Q past d meet X's own, finite, elements)
+        uint4 xv[PXP];
         const bf16_t* Xp = X;
 #pragma unroll
         for (int px = 0; px < PXP; ++px, Xp += px < Px ? x_px : 0)
-          acc[px] = mfma_bf16(qv, row16<VEC, false>(Xp, xo, t, d), acc[px]);
-      }
+          xv[px] = XL ? sX[(px * nch + 4 * k + g) * 16 + c] : row16(Xp, xo, 32 * k + 8 * g, false);
+#pragma unroll
+        for (int px = 0; px < PXP; ++px) acc[px] = mfma_bf16(qv, xv[px], acc[px]);
+      };
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (32 * k < d) block(k, qf[k]);
+      for (int k = kAhead; 32 * k < d; ++k) block(k, row16(Q, qo, 32 * k + 8 * g, true));
 #pragma unroll
       for (int px = 0; px < PXP; ++px)
 #pragma unroll
         for (int i = 0; i < NPQ; ++i) s[i * PXP + px] = acc[px][i];
     }
     // forward
+    // (b1 and b2 come from the caches each time: LDS and registers are full)
+    f32x4_t b1[kJT];
+    {
+      const uint32_t go = fresh(16u * g);
 #pragma unroll
-    for (int pt = 0; pt < PT; ++pt) l[pt] = l[pt] + lx[pt] + *reinterpret_cast<const f32x4_t*>(sB2 + RUN * g + 4 * pt);
+      for (int jt = 0; jt < kJT; ++jt) {
+        if constexpr (FULL) {
+          const f32x4_t v = at32(reinterpret_cast<const f32x4_t*>(pr.b1), min(go + 64u * jt, 4u * H - 16u));
+          b1[jt] = 16 * jt + 4 * g < H ? v : f32x4_t{0.f, 0.f, 0.f, 0.f};
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float v = at32(pr.b1, min(go + 64u * jt + 4u * i, 4u * H - 4u));
+            b1[jt][i] = 16 * jt + 4 * g + i < H ? v : 0.f;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int pt = 0; pt < PT; ++pt) {
+      l[pt] = l[pt] + lx[pt] + b2[pt];
+    }
     Terms<3> a[KB];
     auto slots8 = [&](const float (&x)[RUN], int m) {
       float v[8];
@@ -338,12 +370,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         const int jt = 2 * j2 + hf;
-        const float4 bj = *reinterpret_cast<const float4*>(sB1 + 16 * jt + 4 * g);
-        f32x4_t u = f32x4_t{bj.x, bj.y, bj.z, bj.w};
+        f32x4_t u = b1[jt];
 #pragma unroll
         for (int m = 0; m < KB; ++m) {
           uint4 w;
-          const unsigned char* at = sW1 + (16 * jt + c) * w1_row<RUN>() + 2 * (RUN * g + 8 * m);
+          const unsigned char* at = sW1 + w1_at(16 * jt + c, RUN * g + 8 * m);
           if constexpr (RUN >= 8) {
             w = *reinterpret_cast<const uint4*>(at);
           } else {
@@ -372,8 +403,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
 #pragma unroll
       for (int pt = 0; pt < PT; ++pt) {
         // row c of tile pt: slot RUN (c / 4) + 4 pt + c % 4
-        const unsigned char* at = sW2 + (RUN * (c >> 2) + 4 * pt + (c & 3)) * kW2Row + 2 * (32 * j2 + 4 * g);
-        const uint2 w0 = *reinterpret_cast<const uint2*>(at), w1 = *reinterpret_cast<const uint2*>(at + 32);
+        const int sl = RUN * (c >> 2) + 4 * pt + (c & 3);
+        const uint2 w0 = *reinterpret_cast<const uint2*>(sW2 + w2_at(sl, 32 * j2 + 4 * g));
+        const uint2 w1 = *reinterpret_cast<const uint2*>(sW2 + w2_at(sl, 32 * j2 + 16 + 4 * g));
         l[pt] = mfma_terms<3>(make_uint4(w0.x, w0.y, w1.x, w1.y), ht, l[pt]);
       }
     }
@@ -425,9 +457,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
 #pragma unroll
         for (int m = 0; m < KB; ++m) {
           // A row j = 16 jt + c, K = slots RUN g + 8 m + e: columns of W2's rows
-          const unsigned char* at = sW2 + (RUN * g + 8 * m + (c >> 2)) * kW2Row + 2 * (16 * jt + 4 * (c & 3));
-          const uint2 w0 = read_tr(at);
-          const uint2 w1 = RUN >= 8 ? read_tr(at + 4 * kW2Row) : make_uint2(0, 0);
+          const int sl = RUN * g + 8 * m + (c >> 2), j = 16 * jt + 4 * (c & 3);
+          const uint2 w0 = read_tr(sW2 + w2_at(sl, j));
+          const uint2 w1 = RUN >= 8 ? read_tr(sW2 + w2_at(sl + 4, j)) : make_uint2(0, 0);
           dh = mfma_terms<3>(make_uint4(w0.x, w0.y, w1.x, w1.y), a[m], dh);
         }
         const float4 k = *reinterpret_cast<const float4*>(sU + 1024 * jt + 16 * lane);
@@ -447,8 +479,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
 #pragma unroll
       for (int pt = 0; pt < PT; ++pt) {
         // A row slot RUN (c / 4) + 4 pt + c % 4, K = j: columns of W1's rows
-        const unsigned char* at = sW1 + (32 * j2 + 4 * g + (c >> 2)) * w1_row<RUN>() + 2 * (RUN * (c & 3) + 4 * pt);
-        const uint2 w0 = read_tr(at), w1 = read_tr(at + 16 * w1_row<RUN>());
+        const int j = 32 * j2 + 4 * g + (c >> 2), sl = RUN * (c & 3) + 4 * pt;
+        const uint2 w0 = read_tr(sW1 + w1_at(j, sl)), w1 = read_tr(sW1 + w1_at(j + 16, sl));
         ds[pt] = mfma_terms<2>(make_uint4(w0.x, w0.y, w1.x, w1.y), dt, ds[pt]);
       }
     }
@@ -470,18 +502,19 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
         const uint32_t other = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(own), 0xB1, 0xf, 0xf, true));   // quad_perm 1,0,3,2
         // even: (own low, other low); odd: (other high, own high)
         const uint32_t w = __builtin_amdgcn_perm(other, own, pick);
-        if (NPQ * g + i < Pq && px < Px) const_cast<uint32_t&>(at32(to, to_off + 64u * i)) = w;
+        if (FULL || (NPQ * g + i < Pq && px < Px)) const_cast<uint32_t&>(at32(to, to_off + 64u * i)) = w;
       }
     }
     } else {
       // no unit: factors of zeros
       for (int i = lane; i < wave_bytes<RUN>() / 16; i += 64) reinterpret_cast<uint4*>(mine)[i] = make_uint4(0, 0, 0, 0);
     }
-    __syncthreads();
+    // (these barriers wait for LDS alone: the stores of ds and the next operands stay in flight)
+    ring_barrier<63>();
     // dW1 += du s^T, dW2^T += h dl^T over the eight units' items, two units a K block:
     // slots 8 g + e are items 4 g + e % 4 of the one and the other
     if (j0 < 2 * JT2) {
-      const unsigned char* u0 = reinterpret_cast<unsigned char*>(sB2 + SLOTS) + tr;
+      const unsigned char* u0 = waves + tr;
       const unsigned char* pj = u0 + 1024 * (2 * PT + (second ? 0 : kJT) + j0);      // h or du
       const unsigned char* pp = u0 + 1024 * ((second ? PT : 0) + pt0);               // dl or s
 #pragma unroll 1
@@ -506,7 +539,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
             for (int i = 0; i < PW; ++i) aw[j][i] = mfma_bf16(fj[j][k == 2], fp[i][k == 1], aw[j][i]);
       }
     }
-    __syncthreads();                                                  // read before the next units write
+    ring_barrier<63>();                                               // read before the next units write
   }
 
   // the workgroup's sums
@@ -767,10 +800,16 @@ Bf16Plan plan(const DevProb& pr) {
 template <int NPQ, int PXP>
 hipError_t launch_pairs(const DevProb& pr, const Bf16Plan& f, const Bf16Dims& dm, const float* dphi,
                         const Bf16Parts& parts, hipStream_t st) {
-  const bool vec = pr.d % 8 == 0 && ((reinterpret_cast<uintptr_t>(pr.Q) | reinterpret_cast<uintptr_t>(pr.X)) & 15) == 0;
-  auto kern = vec ? &k_score_grad_bf16<NPQ, PXP, true> : &k_score_grad_bf16<NPQ, PXP, false>;
-  constexpr int lds = lds_bytes<NPQ * PXP>();
-  static_assert(lds <= 160 * 1024, "LDS");
+  auto aligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
+  const bool full = pr.Pq == 4 * NPQ && pr.Px == PXP && pr.d % 8 == 0 && aligned(pr.Q) && aligned(pr.X) && aligned(pr.a_q) &&
+                    aligned(pr.a_x) && aligned(pr.b1) && aligned(pr.b2) && pr.H % 4 == 0;
+  // the items' rows in LDS where the workgroup has one block of items and there is room
+  constexpr int base = lds_bytes<NPQ * PXP>();
+  static_assert(base <= 160 * 1024, "LDS");
+  const bool xl = dm.QB == kWaves && base + x_bytes(PXP, pr.d) <= 160 * 1024;
+  const int lds = base + (xl ? x_bytes(PXP, pr.d) : 0);
+  auto kern = xl ? (full ? &k_score_grad_bf16<NPQ, PXP, true, true> : &k_score_grad_bf16<NPQ, PXP, true, false>)
+                 : (full ? &k_score_grad_bf16<NPQ, PXP, false, true> : &k_score_grad_bf16<NPQ, PXP, false, false>);
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(kern, dim3(f.wgx, dm.qsplits), dim3(kThreads), lds, st, pr, dm, dphi, parts);
