@@ -47,6 +47,11 @@ bool bf16_supported(const DevProb& pr);
 size_t bf16_bytes(const DevProb& pr);
 hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_grads& o, char* ws, hipStream_t st);
 
+// Elements of a row of X or Q transposed: whole K blocks of 32, and 64 more, so that
+// the rows that a load takes together (powers of two apart otherwise) are not
+// all in the same channels of the L2 cache.
+inline int padded_row(long n) { return static_cast<int>((n + 31) / 32 * 32 + 64); }
+
 // K splits of a product of `waves` waves a part with `chunks` K chunks, `least` of them a part
 inline int split_of(long waves, long chunks, long least) {
   const long want = (2048 + waves - 1) / waves, most = chunks / least;

@@ -476,7 +476,6 @@ struct GemmDims {
   long b_px;               // elements between px of Bt (0: the same)
   int ldb;
   int splits;
-  int add;                 // to the parts of the slab before
   long out_px, out_split;  // floats between px (dX), between splits
 };
 template <typename T, bool COLS>
@@ -552,10 +551,7 @@ __global__ __launch_bounds__(256) void k_grad_gemm(GemmDims gd, const uint32_t* 
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int m = m0 + 16 * r + 4 * g + i, x = t0 + 16 * t + c;
-        if (m < gd.m && x < gd.d) {
-          float* o = dst + static_cast<long>(m) * gd.d + x;
-          *o = gd.add ? *o + acc[r][t][i] : acc[r][t][i];
-        }
+        if (m < gd.m && x < gd.d) dst[static_cast<long>(m) * gd.d + x] = acc[r][t][i];
       }
 }
 
@@ -634,9 +630,9 @@ struct GradPlan {
   int JT, groups, slab, slabs;
   bool wlds, ulds;                      // prepared weights and the units' u in LDS
   size_t lds;
-  int sp_q, sp_x, ldq;                  // K splits of dQ and dX, row length of Q transposed
+  int sp_q, sp_x, ldq, ldx;             // K splits of dQ and dX, row lengths of Q and X transposed
   size_t off_w, off_u, off_ds, off_xt, off_qt, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_pq, off_px, off_acc, bytes;
-  long a_daq, a_dw1, a_dw2, a_db1;      // floats into the accumulators
+  long a_daq, a_dw1, a_dw2, a_db1, a_dq;   // floats into the sums over slabs
   int wgs;
 };
 
@@ -671,17 +667,18 @@ GradPlan plan_grad(const DevProb& pr) {
   dm.qsplits = std::max(1, std::min(nqb, 256 / st));
   f.wgs = st * dm.qsplits;
   constexpr int KCH = 64 / sizeof(T);
-  f.ldq = static_cast<int>((dm.m + 31) / 32 * 32);
+  f.ldq = padded_row(dm.m);
+  f.ldx = padded_row(f.slab);
   const long cg = (pr.d + 63) / 64;
   f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * f.slab / KCH, 8);
-  f.sp_x = split_of((f.slab + 31l) / 32 * cg * pr.Px, f.ldq / KCH, 8);
+  f.sp_x = split_of((f.slab + 31l) / 32 * cg * pr.Px, (dm.m + 31) / 32 * 32 / KCH, 8);
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   size_t at = 0;
   const size_t P = pr.P, H = pr.H;
   f.off_w = at;   at = up(at + (f.wlds ? 0 : 16ul * f.JT * (PV / 16) * 256));
   f.off_u = at;   at = up(at + (f.ulds ? 0 : 1024ul * f.wgs * kWaves * f.JT));
   f.off_ds = at;  at = up(at + 4ul * pr.Px * dm.m * f.slab);
-  f.off_xt = at;  at = up(at + sizeof(T) * pr.Px * pr.d * static_cast<size_t>(f.slab));
+  f.off_xt = at;  at = up(at + sizeof(T) * pr.Px * pr.d * static_cast<size_t>(f.ldx));
   f.off_qt = at;  at = up(at + sizeof(T) * pr.d * static_cast<size_t>(f.ldq));
   f.off_daq = at; at = up(at + 4ul * (f.slab / 16) * pr.B * P);
   f.off_dax = at; at = up(at + 4ul * dm.qsplits * f.slab * P);
@@ -694,7 +691,8 @@ GradPlan plan_grad(const DevProb& pr) {
   f.a_dw1 = f.a_daq + static_cast<long>(pr.B) * P;
   f.a_dw2 = f.a_dw1 + static_cast<long>(H * P);
   f.a_db1 = f.a_dw2 + static_cast<long>(H * P);
-  f.off_acc = at; at = up(at + 4ul * (f.a_db1 + H));
+  f.a_dq = f.a_db1 + static_cast<long>(H);
+  f.off_acc = at; at = up(at + 4ul * (f.a_dq + (f.slabs > 1 ? dm.m * pr.d : 0)));
   f.bytes = at;
   return f;
 }
@@ -727,7 +725,7 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
     const bool last = sl + 1 == f.slabs;
     dm.n0 = sl * f.slab;
     const int items = std::min(f.slab, pr.N - dm.n0);
-    if ((e = launch_transposes<T>(pr, dm.m, f.ldq, o.dX && sl == 0 ? qt : nullptr, dm.n0, items, f.slab, o.dQ ? xt : nullptr,
+    if ((e = launch_transposes<T>(pr, dm.m, f.ldq, o.dX && sl == 0 ? qt : nullptr, dm.n0, items, f.ldx, o.dQ ? xt : nullptr,
                                   st)) != hipSuccess)
       return e;
     for (int grp = 0; grp < f.groups; ++grp) {
@@ -739,15 +737,15 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
     const long P = pr.P, H = pr.H, BP = pr.B * P;
     if (o.dQ) {
       GemmDims gd{static_cast<int>(dm.m), pr.d, f.slab, dm.m * f.slab, f.slab, f.slab, pr.Px,
-                  static_cast<long>(pr.d) * f.slab, f.slab, f.sp_q, sl > 0, 0, dm.m * pr.d};
+                  static_cast<long>(pr.d) * f.ldx, f.ldx, f.sp_q, 0, dm.m * pr.d};
       hipLaunchKernelGGL((k_grad_gemm<T, false>), dim3(static_cast<unsigned>((dm.m + 127) / 128), cg, f.sp_q), dim3(256),
                          0, st, gd, parts.ds, xt, F(f.off_pq));
-      if (last)
-        sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, nullptr, 0, o.dQ, bf, dm.m * pr.d, dm.m * pr.d, 0});
+      sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, f.slabs > 1 ? acc + f.a_dq : nullptr, sl > 0,
+                last ? o.dQ : nullptr, bf, dm.m * pr.d, dm.m * pr.d, 0});
     }
     if (o.dX) {
       const long per_px = static_cast<long>(items) * pr.d;
-      GemmDims gd{items, pr.d, f.slab, dm.m * f.slab, f.ldq, static_cast<int>(dm.m), pr.Px, 0, f.ldq, f.sp_x, 0, per_px,
+      GemmDims gd{items, pr.d, f.slab, dm.m * f.slab, static_cast<int>((dm.m + 31) / 32 * 32), static_cast<int>(dm.m), pr.Px, 0, f.ldq, f.sp_x, per_px,
                   per_px * pr.Px};
       hipLaunchKernelGGL((k_grad_gemm<T, true>), dim3((items + 127) / 128, cg, f.sp_x * pr.Px), dim3(256), 0, st, gd,
                          parts.ds, qt, F(f.off_px));

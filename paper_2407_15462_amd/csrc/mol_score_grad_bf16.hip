@@ -177,9 +177,10 @@ static_assert(lds_bytes<4>() >= 4 * kWaves * 16 * 16 && lds_bytes<16>() >= 4 * k
 
 }  // namespace
 
-// XL: the workgroup's waves share 16 items, whose rows lie in LDS.  FULL: P_q = 4
-// NPQ, P_x = PXP, and every row allows 16-byte reads (H a multiple of 4).
-template <int NPQ, int PXP, bool XL, bool FULL>
+// XL: the workgroup's waves share 16 items, whose rows lie in LDS.  FULL 1 or 2: P_q = 4
+// NPQ, P_x = PXP, every row allows 16-byte reads (H a multiple of 4) and H is
+// at most 32 or 64: no branches in a unit, which leaves its order to the compiler.
+template <int NPQ, int PXP, bool XL, int FULL>
 __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf16Dims dm,
                                                                  const float* __restrict__ dphi, Bf16Parts out) {
   constexpr int RUN = NPQ * PXP, SLOTS = 4 * RUN, PT = RUN / 4, KB = RUN > 8 ? RUN / 8 : 1;
@@ -187,7 +188,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g = lane >> 4;
-  const int P = pr.P, H = pr.H, d = pr.d, N = pr.N, JT2 = (H + 31) / 32, nch = (d + 31) / 32 * 4;
+  const int P = pr.P, H = pr.H, d = pr.d, N = pr.N, JT2 = FULL ? FULL : (H + 31) / 32, nch = (d + 31) / 32 * 4;
   const int Pq = FULL ? 4 * NPQ : pr.Pq, Px = FULL ? PXP : pr.Px;
   unsigned char* sW1 = smb;
   unsigned char* sW2 = sW1 + 2 * kH * SLOTS;
@@ -603,8 +604,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
 // dQ and dX on matrix cores from ds: 32 rows and 64 columns a wave, K split.
 struct GemmBf16 {
   int m, nb, d, npx;
-  int splits, add;
+  int splits;
   int items;         // dX: rows that exist
+  int ldb;           // elements of a row of X or Q transposed
 };
 
 // dQ[m][t] = sum over px and items of ds X
@@ -614,46 +616,55 @@ __global__ __launch_bounds__(256) void k_grad_dq_bf16(GemmBf16 gd, const uint32_
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
   const int m0 = (blockIdx.x * 4 + wave) * 16 * RB, t0 = blockIdx.y * 16 * CB;
   if (m0 >= gd.m) return;
-  const int per = gd.nb / 2, chunks = per * gd.npx, ns = 16 * gd.nb;  // a chunk: two blocks of items
+  const int per = gd.nb / 2, chunks = per * gd.npx;  // a chunk: two blocks of items
   const int k0 = static_cast<int>(static_cast<long>(chunks) * blockIdx.z / gd.splits);
   const int k1 = static_cast<int>(static_cast<long>(chunks) * (blockIdx.z + 1) / gd.splits);
   f32x4_t acc[RB][CB] = {};
-  // items 8 g .. 8 g + 7 of a chunk: half g % 2 of block g / 2's row
+  // Lane (c, g) reads piece g of row c of both blocks, rows of 64 bytes, whole;
+  // the halves of the wave are then swapped to first terms (items 8 g .. of the
+  // chunk) and second terms.
   const uint32_t* a[RB];
   const bf16_t* bt[CB];
 #pragma unroll
-  for (int r = 0; r < RB; ++r)
-    a[r] = ds + (static_cast<long>(g >> 1) * gd.m + min(m0 + 16 * r + c, gd.m - 1)) * 16 + 4 * (g & 1);
+  for (int r = 0; r < RB; ++r) a[r] = ds + static_cast<long>(min(m0 + 16 * r + c, gd.m - 1)) * 16 + 4 * g;
 #pragma unroll
-  for (int t = 0; t < CB; ++t) bt[t] = xt + static_cast<long>(min(t0 + 16 * t + c, gd.d - 1)) * ns + 8 * g;
-  const long a_step = 32l * gd.m, x_px = static_cast<long>(gd.d) * ns;
-  uint4 hi[RB], lo[RB], bv[CB];
-  auto fetch = [&](int ch) {
-    const int px = ch / per, k = ch - px * per;
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-      const uint32_t* p = a[r] + ch * a_step;                         // (px by px, the blocks follow each other)
-      hi[r] = *reinterpret_cast<const uint4*>(p);
-      lo[r] = *reinterpret_cast<const uint4*>(p + 8);
-    }
-#pragma unroll
-    for (int t = 0; t < CB; ++t) bv[t] = *reinterpret_cast<const uint4*>(bt[t] + px * x_px + 32 * k);
+  for (int t = 0; t < CB; ++t) bt[t] = xt + static_cast<long>(min(t0 + 16 * t + c, gd.d - 1)) * gd.ldb + 8 * g;
+  const long a_blk = 16l * gd.m, x_px = static_cast<long>(gd.d) * gd.ldb;
+  struct Chunk {
+    uint4 a[RB][2], b[CB];
   };
-  if (k0 < k1) fetch(k0);
-  for (int ch = k0; ch < k1; ++ch) {
-    uint4 h[RB], l[RB], b[CB];
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-      h[r] = hi[r];
-      l[r] = lo[r];
-    }
-#pragma unroll
-    for (int t = 0; t < CB; ++t) b[t] = bv[t];
-    if (ch + 1 < k1) fetch(ch + 1);
+  auto fetch = [&](Chunk& v, int ch) {                                // (px by px, the blocks follow each other)
+    const int px = ch / per, k = ch - px * per;
 #pragma unroll
     for (int r = 0; r < RB; ++r)
 #pragma unroll
-      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(h[r], b[t], mfma_bf16(l[r], b[t], acc[r][t]));
+      for (int e = 0; e < 2; ++e) v.a[r][e] = *reinterpret_cast<const uint4*>(a[r] + (2l * ch + e) * a_blk);
+#pragma unroll
+    for (int t = 0; t < CB; ++t) v.b[t] = *reinterpret_cast<const uint4*>(bt[t] + px * x_px + 32 * k);
+  };
+  auto use = [&](const Chunk& v) {
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      const uint4 x = v.a[r][0], y = v.a[r][1];
+      const auto p0 = __builtin_amdgcn_permlane32_swap(x.x, y.x, false, false);
+      const auto p1 = __builtin_amdgcn_permlane32_swap(x.y, y.y, false, false);
+      const auto p2 = __builtin_amdgcn_permlane32_swap(x.z, y.z, false, false);
+      const auto p3 = __builtin_amdgcn_permlane32_swap(x.w, y.w, false, false);
+      const uint4 h = make_uint4(p0[0], p1[0], p2[0], p3[0]), l = make_uint4(p0[1], p1[1], p2[1], p3[1]);
+#pragma unroll
+      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(l, v.b[t], acc[r][t]);
+#pragma unroll
+      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(h, v.b[t], acc[r][t]);
+    }
+  };
+  // (two sets of registers in turn: copies of one would wait for its loads)
+  Chunk v0, v1;
+  if (k0 < k1) fetch(v0, k0);
+  for (int ch = k0; ch < k1; ch += 2) {
+    fetch(v1, min(ch + 1, k1 - 1));
+    use(v0);
+    fetch(v0, min(ch + 2, k1 - 1));
+    if (ch + 1 < k1) use(v1);
   }
   float* dst = out + static_cast<long>(blockIdx.z) * gd.m * gd.d;
 #pragma unroll
@@ -663,17 +674,14 @@ __global__ __launch_bounds__(256) void k_grad_dq_bf16(GemmBf16 gd, const uint32_
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int m = m0 + 16 * r + 4 * g + i, x = t0 + 16 * t + c;
-        if (m < gd.m && x < gd.d) {
-          float* o = dst + static_cast<long>(m) * gd.d + x;
-          *o = gd.add ? *o + acc[r][t][i] : acc[r][t][i];
-        }
+        if (m < gd.m && x < gd.d) dst[static_cast<long>(m) * gd.d + x] = acc[r][t][i];
       }
 }
 
 // dX[px][n][t] = sum over (b, pq) of ds Q: rows of ds of a block of items, 32
 // at a time, through the wave's LDS and the transposing read
 __global__ __launch_bounds__(256) void k_grad_dx_bf16(GemmBf16 gd, const uint32_t* __restrict__ ds,
-                                                      const bf16_t* __restrict__ qt, int ldq, float* __restrict__ out) {
+                                                      const bf16_t* __restrict__ qt, float* __restrict__ out) {
   constexpr int RB = 2, CB = 4;
   __shared__ __attribute__((aligned(16))) uint4 sh[4][RB * 128];      // [block][32 rows][64 bytes] a wave
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
@@ -690,45 +698,48 @@ __global__ __launch_bounds__(256) void k_grad_dx_bf16(GemmBf16 gd, const uint32_
   for (int r = 0; r < RB; ++r)
     a[r] = reinterpret_cast<const uint4*>(ds + (static_cast<long>(px) * gd.nb + min(blk0 + r, gd.nb - 1)) * gd.m * 16);
 #pragma unroll
-  for (int t = 0; t < CB; ++t) bt[t] = qt + static_cast<long>(min(t0 + 16 * t + c, gd.d - 1)) * ldq + 8 * g;
-  uint4 av[RB][2], bv[CB];
+  for (int t = 0; t < CB; ++t) bt[t] = qt + static_cast<long>(min(t0 + 16 * t + c, gd.d - 1)) * gd.ldb + 8 * g;
+  struct Chunk {
+    uint4 a[RB][2], b[CB];
+  };
   const long last = static_cast<long>(gd.m) * 4 - 1;                  // 16-byte pieces of a block's rows
-  auto fetch = [&](int ch) {
+  auto fetch = [&](Chunk& v, int ch) {
 #pragma unroll
     for (int r = 0; r < RB; ++r)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const long at = ch * 128l + e * 64 + lane;
-        const uint4 v = a[r][min(at, last)];
-        av[r][e] = at <= last ? v : make_uint4(0, 0, 0, 0);           // (rows past b pq: Q's are zero too)
-      }
+      for (int e = 0; e < 2; ++e) v.a[r][e] = a[r][min(ch * 128l + e * 64 + lane, last)];
 #pragma unroll
-    for (int t = 0; t < CB; ++t) bv[t] = *reinterpret_cast<const uint4*>(bt[t] + 32 * ch);
+    for (int t = 0; t < CB; ++t) v.b[t] = *reinterpret_cast<const uint4*>(bt[t] + 32 * ch);
   };
   const unsigned char* mine = reinterpret_cast<const unsigned char*>(sh[wave]);
   // K slots 8 g + e: rows 8 g + e
   const int tr = (8 * g + (c >> 2)) * 64 + 8 * (c & 3);
-  if (k0 < k1) fetch(k0);
-  for (int ch = k0; ch < k1; ++ch) {
-    uint4 b[CB];
+  auto use = [&](const Chunk& v, int ch) {
 #pragma unroll
-    for (int r = 0; r < RB; ++r) {
-      sh[wave][r * 128 + lane] = av[r][0];
-      sh[wave][r * 128 + 64 + lane] = av[r][1];
-    }
+    for (int r = 0; r < RB; ++r)
 #pragma unroll
-    for (int t = 0; t < CB; ++t) b[t] = bv[t];
+      for (int e = 0; e < 2; ++e)                                     // (rows past b pq: zeros, as Q's are)
+        sh[wave][r * 128 + e * 64 + lane] = ch * 128l + e * 64 + lane <= last ? v.a[r][e] : make_uint4(0, 0, 0, 0);
     wave_lds_sync();
-    if (ch + 1 < k1) fetch(ch + 1);
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
       const unsigned char* p = mine + r * 2048 + tr;
       const uint2 h0 = read_tr(p), h1 = read_tr(p + 256), l0 = read_tr(p + 32), l1 = read_tr(p + 288);
       const uint4 h = make_uint4(h0.x, h0.y, h1.x, h1.y), l = make_uint4(l0.x, l0.y, l1.x, l1.y);
 #pragma unroll
-      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(h, b[t], mfma_bf16(l, b[t], acc[r][t]));
+      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(l, v.b[t], acc[r][t]);
+#pragma unroll
+      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(h, v.b[t], acc[r][t]);
     }
     wave_lds_sync();
+  };
+  Chunk v0, v1;
+  if (k0 < k1) fetch(v0, k0);
+  for (int ch = k0; ch < k1; ch += 2) {
+    fetch(v1, min(ch + 1, k1 - 1));
+    use(v0, ch);
+    fetch(v0, min(ch + 2, k1 - 1));
+    if (ch + 1 < k1) use(v1, ch + 1);
   }
   const long per_px = static_cast<long>(gd.items) * gd.d;
   float* dst = out + (static_cast<long>(split) * gd.npx + px) * per_px;
@@ -751,9 +762,9 @@ namespace {
 struct Bf16Plan {
   Bf16Dims dm;
   int slab, slabs, wgx, wgs;
-  int sp_q, sp_x, ldq;
+  int sp_q, sp_x, ldq, ldx;
   size_t off_ds, off_xt, off_qt, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_pq, off_px, off_acc, bytes;
-  long a_dw1, a_dw2, a_db1;
+  long a_dw1, a_dw2, a_db1, a_dq;       // floats into the sums over slabs
 };
 
 Bf16Plan plan(const DevProb& pr) {
@@ -772,15 +783,16 @@ Bf16Plan plan(const DevProb& pr) {
   f.wgx = (dm.nb + per - 1) / per;
   dm.qsplits = std::max(1, std::min(steps, 256 / f.wgx));
   f.wgs = f.wgx * dm.qsplits;
-  f.ldq = static_cast<int>((dm.m + 31) / 32 * 32);
+  f.ldq = padded_row(dm.m);
+  f.ldx = padded_row(f.slab);
   const long cg = (pr.d + 63) / 64;
   f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * dm.nb / 2, 8);
-  f.sp_x = split_of(static_cast<long>(dm.nb) / 2 * cg * pr.Px, f.ldq / 32, 8);
+  f.sp_x = split_of(static_cast<long>(dm.nb) / 2 * cg * pr.Px, (dm.m + 31) / 32, 8);
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   size_t at = 0;
   const size_t P = pr.P, H = pr.H;
   f.off_ds = at;  at = up(at + 4ul * pr.Px * dm.m * f.slab);
-  f.off_xt = at;  at = up(at + 2ul * pr.Px * pr.d * f.slab);
+  f.off_xt = at;  at = up(at + 2ul * pr.Px * pr.d * f.ldx);
   f.off_qt = at;  at = up(at + 2ul * pr.d * f.ldq);
   f.off_daq = at; at = up(at + 4ul * dm.nb * pr.B * P);
   f.off_dax = at; at = up(at + 4ul * dm.qsplits * f.slab * P);
@@ -792,7 +804,8 @@ Bf16Plan plan(const DevProb& pr) {
   f.a_dw1 = static_cast<long>(pr.B) * P;
   f.a_dw2 = f.a_dw1 + static_cast<long>(H * P);
   f.a_db1 = f.a_dw2 + static_cast<long>(H * P);
-  f.off_acc = at; at = up(at + 4ul * (f.a_db1 + H));
+  f.a_dq = f.a_db1 + static_cast<long>(H);
+  f.off_acc = at; at = up(at + 4ul * (f.a_dq + (f.slabs > 1 ? dm.m * pr.d : 0)));
   f.bytes = at;
   return f;
 }
@@ -808,8 +821,13 @@ hipError_t launch_pairs(const DevProb& pr, const Bf16Plan& f, const Bf16Dims& dm
   static_assert(base <= 160 * 1024, "LDS");
   const bool xl = dm.QB == kWaves && base + x_bytes(PXP, pr.d) <= 160 * 1024;
   const int lds = base + (xl ? x_bytes(PXP, pr.d) : 0);
-  auto kern = xl ? (full ? &k_score_grad_bf16<NPQ, PXP, true, true> : &k_score_grad_bf16<NPQ, PXP, true, false>)
-                 : (full ? &k_score_grad_bf16<NPQ, PXP, false, true> : &k_score_grad_bf16<NPQ, PXP, false, false>);
+  const int form = !full ? 0 : pr.H <= 32 ? 1 : 2;
+  auto kern = xl ? (form == 2   ? &k_score_grad_bf16<NPQ, PXP, true, 2>
+                    : form == 1 ? &k_score_grad_bf16<NPQ, PXP, true, 1>
+                                : &k_score_grad_bf16<NPQ, PXP, true, 0>)
+                 : (form == 2   ? &k_score_grad_bf16<NPQ, PXP, false, 2>
+                    : form == 1 ? &k_score_grad_bf16<NPQ, PXP, false, 1>
+                                : &k_score_grad_bf16<NPQ, PXP, false, 0>);
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(kern, dim3(f.wgx, dm.qsplits), dim3(kThreads), lds, st, pr, dm, dphi, parts);
@@ -843,22 +861,22 @@ hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_gra
     const bool last = sl + 1 == f.slabs;
     dm.n0 = sl * f.slab;
     dm.items = std::min(f.slab, pr.N - dm.n0);
-    hipError_t e = launch_transposes<bf16_t>(pr, dm.m, f.ldq, o.dX && sl == 0 ? qt : nullptr, dm.n0, dm.items, dm.ns,
+    hipError_t e = launch_transposes<bf16_t>(pr, dm.m, f.ldq, o.dX && sl == 0 ? qt : nullptr, dm.n0, dm.items, f.ldx,
                                              o.dQ ? xt : nullptr, st);
     if (e != hipSuccess) return e;
     if ((e = pairs(pr, f, dm, dphi, parts, st)) != hipSuccess) return e;
     if (o.dQ) {
-      const GemmBf16 gd{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_q, sl > 0, dm.items};
+      const GemmBf16 gd{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_q, dm.items, f.ldx};
       hipLaunchKernelGGL(k_grad_dq_bf16, dim3(static_cast<unsigned>((dm.m + 127) / 128), cg, f.sp_q), dim3(256), 0, st, gd,
                          parts.ds, xt, F(f.off_pq));
-      if (last)
-        sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, nullptr, 0, o.dQ, 1, dm.m * pr.d, dm.m * pr.d, 0});
+      sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, f.slabs > 1 ? acc + f.a_dq : nullptr, sl > 0,
+                last ? o.dQ : nullptr, 1, dm.m * pr.d, dm.m * pr.d, 0});
     }
     if (o.dX) {
       const long per_px = static_cast<long>(dm.items) * pr.d;
-      const GemmBf16 gd{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_x, 0, dm.items};
+      const GemmBf16 gd{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_x, dm.items, f.ldq};
       hipLaunchKernelGGL(k_grad_dx_bf16, dim3((dm.nb + 7) / 8, cg, f.sp_x * pr.Px), dim3(256), 0, st, gd, parts.ds, qt,
-                         f.ldq, F(f.off_px));
+                         F(f.off_px));
       sums.add({F(f.off_px), per_px * pr.Px, per_px * pr.Px, f.sp_x, nullptr, 0, o.dX, 1, per_px,
                 static_cast<long>(pr.N) * pr.d, static_cast<long>(dm.n0) * pr.d});
     }
