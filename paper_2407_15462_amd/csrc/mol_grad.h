@@ -21,7 +21,7 @@ struct SumJob {
   long in_len, out_len, out_at;
   int wide, blocks;        // (set by the launcher) 256 columns a block, blocks
 };
-constexpr int kSumJobs = 8;
+constexpr int kSumJobs = 8;   // one an output
 struct SumArgs {
   int n;
   int first[kSumJobs + 1];
@@ -46,6 +46,12 @@ hipError_t launch_transposes(const DevProb& pr, long m, int ldq, T* qt, int n0, 
 bool bf16_supported(const DevProb& pr);
 size_t bf16_bytes(const DevProb& pr);
 hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_grads& o, char* ws, hipStream_t st);
+
+// dQ and dX from ds in one launch or in two.  Together they fill the card where
+// there is little of it (34 MB of ds: 18 us against 12 + 12); apart the second finds
+// part of what the first read in the last-level cache (268 MB: 77 + 60 us against 259).
+constexpr int kProductQ = 1, kProductX = 2;
+inline bool products_together(size_t ds_bytes) { return ds_bytes <= (size_t(64) << 20); }
 
 // Elements of a row of X or Q transposed: whole K blocks of 32, and 64 more, so that
 // the rows that a load takes together (powers of two apart otherwise) are not

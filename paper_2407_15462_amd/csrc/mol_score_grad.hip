@@ -110,6 +110,7 @@ struct GradParts {
   float* dW1;              // [workgroups][H][P]
   float* dW2;              // [workgroups][P][H]
   float* db1;              // [workgroups][H]
+  float* db2;              // [workgroups][P]
 };
 
 template <int PV>
@@ -230,7 +231,28 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims
       const T* x0 = Xp + static_cast<long>(item_of(32 * ct + c)) * d;
       const T* x1 = Xp + static_cast<long>(item_of(32 * ct + 16 + c)) * d;
       f32x4_t acc[2][2] = {};
-      for (int k0 = 0; k0 < d; k0 += KCH) {
+      int k0 = 0;
+      if constexpr (PV < 64) {
+        // (registers for four chunks in flight)
+        for (; k0 + 4 * KCH <= d; k0 += 4 * KCH) {
+          uint4 x[4][2], y[4][2];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int t = k0 + e * KCH + g * E;
+            x[e][0] = row16<T, VEC>(x0, t, d);
+            x[e][1] = row16<T, VEC>(x1, t, d);
+            y[e][0] = row16<T, VEC>(q0, t, d);
+            y[e][1] = row16<T, VEC>(q1, t, d);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) acc[r][h] = mma16<T>(y[e][r], x[e][h], acc[r][h]);
+        }
+      }
+      for (; k0 < d; k0 += KCH) {
         const int t = k0 + g * E;
         const uint4 xa = row16<T, VEC>(x0, t, d), xb = row16<T, VEC>(x1, t, d);
         const uint4 qa = row16<T, VEC>(q0, t, d), qc = row16<T, VEC>(q1, t, d);
@@ -421,6 +443,25 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims
     if (j < H) out.db1[wg * H + j] = acc[2 * JTG * PT * 256 + i];
   }
   if (dm.group) return;
+  // db2: da_x summed over the items, then over the waves
+#pragma unroll
+  for (int mu = 0; mu < RUN; ++mu) {
+    float t = dax[mu];
+    t += row_ror<8>(t);
+    t += row_ror<4>(t);
+    t += row_ror<2>(t);
+    t += row_ror<1>(t);
+    if (c == mu % 16) ab1[0] = t;                                      // (RUN <= 16: lane c keeps component c)
+  }
+  __syncthreads();
+  if (c < RUN) acc[wave * PV + RUN * g + c] = ab1[0];
+  __syncthreads();
+  for (int i = tid; i < P; i += kThreads) {
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) t += acc[w * PV + i];
+    out.db2[wg * P + i] = t;
+  }
   // da_x: the waves of a tile's queries in turn
   for (int w = 0; w < QB; ++w) {
     __syncthreads();
@@ -465,8 +506,8 @@ __global__ __launch_bounds__(256) void k_transpose(DevProb pr, long m, int ldq, 
 // Products with ds on matrix cores: out[m][t] = sum_k A[m][k] Bt[t][k].
 // COLS false (dQ): m = (b, pq), k = (px, item): A rows run along k.
 // COLS true (dX): one px a batch, m = item, k = (b, pq): A columns run along m.
-// A wave has 32 rows and 64 columns; K chunks of `KCH` are split over
-// blockIdx.z's ranges, whose sums are separate parts.
+// A wave has 32 rows and 64 columns; K chunks of `KCH` are split into ranges, z % splits,
+// whose sums are separate parts.
 struct GemmDims {
   int m, d;
   long lda;                // elements of a row of ds
@@ -479,13 +520,13 @@ struct GemmDims {
   long out_px, out_split;  // floats between px (dX), between splits
 };
 template <typename T, bool COLS>
-__global__ __launch_bounds__(256) void k_grad_gemm(GemmDims gd, const uint32_t* __restrict__ ds,
-                                                   const T* __restrict__ Bt, float* __restrict__ out) {
+__device__ __forceinline__ void product_tile(const GemmDims& gd, int z, const uint32_t* __restrict__ ds,
+                                             const T* __restrict__ Bt, float* __restrict__ out) {
   constexpr int E = 16 / sizeof(T), KCH = 4 * E, RB = 2, CB = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
   const int m0 = (blockIdx.x * 4 + wave) * 16 * RB, t0 = blockIdx.y * 16 * CB;
   if (m0 >= gd.m) return;
-  const int split = blockIdx.z % gd.splits, px0 = COLS ? blockIdx.z / gd.splits : 0;
+  const int split = z % gd.splits, px0 = COLS ? z / gd.splits : 0;
   const int per = gd.k_px / KCH, chunks = COLS ? per : per * gd.npx;
   const int k0 = static_cast<int>(static_cast<long>(chunks) * split / gd.splits);
   const int k1 = static_cast<int>(static_cast<long>(chunks) * (split + 1) / gd.splits);
@@ -553,6 +594,18 @@ __global__ __launch_bounds__(256) void k_grad_gemm(GemmDims gd, const uint32_t* 
         const int m = m0 + 16 * r + 4 * g + i, x = t0 + 16 * t + c;
         if (m < gd.m && x < gd.d) dst[static_cast<long>(m) * gd.d + x] = acc[r][t][i];
       }
+}
+
+// ---------------------------------------------------------------------------
+// Both products, side by side (blockIdx.z < zq for dQ), or one.
+template <typename T, int WHAT>
+__global__ __launch_bounds__(256) void k_grad_products(GemmDims q, GemmDims x, int zq, const uint32_t* __restrict__ ds,
+                                                       const T* __restrict__ xt, const T* __restrict__ qt,
+                                                       float* __restrict__ out_q, float* __restrict__ out_x) {
+  if constexpr (WHAT & kProductQ)
+    if (static_cast<int>(blockIdx.z) < zq) product_tile<T, false>(q, blockIdx.z, ds, xt, out_q);
+  if constexpr (WHAT & kProductX)
+    if (static_cast<int>(blockIdx.z) >= zq) product_tile<T, true>(x, blockIdx.z - zq, ds, qt, out_x);
 }
 
 // ---------------------------------------------------------------------------
@@ -631,8 +684,8 @@ struct GradPlan {
   bool wlds, ulds;                      // prepared weights and the units' u in LDS
   size_t lds;
   int sp_q, sp_x, ldq, ldx;             // K splits of dQ and dX, row lengths of Q and X transposed
-  size_t off_w, off_u, off_ds, off_xt, off_qt, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_pq, off_px, off_acc, bytes;
-  long a_daq, a_dw1, a_dw2, a_db1, a_dq;   // floats into the sums over slabs
+  size_t off_w, off_u, off_ds, off_xt, off_qt, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_db2, off_pq, off_px, off_acc, bytes;
+  long a_daq, a_dw1, a_dw2, a_db1, a_db2, a_dq;   // floats into the sums over slabs
   int wgs;
 };
 
@@ -670,8 +723,8 @@ GradPlan plan_grad(const DevProb& pr) {
   f.ldq = padded_row(dm.m);
   f.ldx = padded_row(f.slab);
   const long cg = (pr.d + 63) / 64;
-  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * f.slab / KCH, 8);
-  f.sp_x = split_of((f.slab + 31l) / 32 * cg * pr.Px, (dm.m + 31) / 32 * 32 / KCH, 8);
+  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * f.slab / KCH, 2);
+  f.sp_x = split_of((f.slab + 31l) / 32 * cg * pr.Px, (dm.m + 31) / 32 * 32 / KCH, 2);
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   size_t at = 0;
   const size_t P = pr.P, H = pr.H;
@@ -685,13 +738,15 @@ GradPlan plan_grad(const DevProb& pr) {
   f.off_dw1 = at; at = up(at + 4ul * f.wgs * H * P);
   f.off_dw2 = at; at = up(at + 4ul * f.wgs * H * P);
   f.off_db1 = at; at = up(at + 4ul * f.wgs * H);
+  f.off_db2 = at; at = up(at + 4ul * f.wgs * P);
   f.off_pq = at;  at = up(at + 4ul * f.sp_q * dm.m * pr.d);
   f.off_px = at;  at = up(at + 4ul * f.sp_x * pr.Px * static_cast<size_t>(f.slab) * pr.d);
   f.a_daq = 0;
   f.a_dw1 = f.a_daq + static_cast<long>(pr.B) * P;
   f.a_dw2 = f.a_dw1 + static_cast<long>(H * P);
   f.a_db1 = f.a_dw2 + static_cast<long>(H * P);
-  f.a_dq = f.a_db1 + static_cast<long>(H);
+  f.a_db2 = f.a_db1 + static_cast<long>(H);
+  f.a_dq = f.a_db2 + static_cast<long>(P);
   f.off_acc = at; at = up(at + 4ul * (f.a_dq + (f.slabs > 1 ? dm.m * pr.d : 0)));
   f.bytes = at;
   return f;
@@ -704,7 +759,7 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
   GradDims dm = f.dm;
   auto F = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
   GradParts parts{reinterpret_cast<uint32_t*>(ws + f.off_ds), F(f.off_daq), F(f.off_dax), F(f.off_dw1), F(f.off_dw2),
-                  F(f.off_db1)};
+                  F(f.off_db1), F(f.off_db2)};
   T* xt = reinterpret_cast<T*>(ws + f.off_xt);
   T* qt = reinterpret_cast<T*>(ws + f.off_qt);
   float* acc = F(f.off_acc);
@@ -735,24 +790,33 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
                          f.ulds ? nullptr : F(f.off_u), parts);
     }
     const long P = pr.P, H = pr.H, BP = pr.B * P;
-    if (o.dQ) {
-      GemmDims gd{static_cast<int>(dm.m), pr.d, f.slab, dm.m * f.slab, f.slab, f.slab, pr.Px,
-                  static_cast<long>(pr.d) * f.ldx, f.ldx, f.sp_q, 0, dm.m * pr.d};
-      hipLaunchKernelGGL((k_grad_gemm<T, false>), dim3(static_cast<unsigned>((dm.m + 127) / 128), cg, f.sp_q), dim3(256),
-                         0, st, gd, parts.ds, xt, F(f.off_pq));
+    const long per_px = static_cast<long>(items) * pr.d;
+    if (o.dQ || o.dX) {
+      const int m = static_cast<int>(dm.m);
+      const GemmDims gq{m, pr.d, f.slab, dm.m * f.slab, f.slab, f.slab, pr.Px, static_cast<long>(pr.d) * f.ldx, f.ldx,
+                        f.sp_q, 0, dm.m * pr.d};
+      const GemmDims gx{items, pr.d, f.slab, dm.m * f.slab, (m + 31) / 32 * 32, m, pr.Px, 0, f.ldq, f.sp_x, per_px,
+                        per_px * pr.Px};
+      auto launch = [&](auto kern, int zq, int zx) {
+        const unsigned x = std::max(zq ? (m + 127) / 128 : 0, zx ? (items + 127) / 128 : 0);
+        hipLaunchKernelGGL(kern, dim3(x, cg, zq + zx), dim3(256), 0, st, gq, gx, zq, parts.ds, xt, qt, F(f.off_pq),
+                           F(f.off_px));
+      };
+      const int zq = o.dQ ? f.sp_q : 0, zx = o.dX ? f.sp_x * pr.Px : 0;
+      if (zq && zx && products_together(4ul * pr.Px * dm.m * f.slab)) {
+        launch(&k_grad_products<T, kProductQ | kProductX>, zq, zx);
+      } else {
+        if (zq) launch(&k_grad_products<T, kProductQ>, zq, 0);
+        if (zx) launch(&k_grad_products<T, kProductX>, 0, zx);
+      }
+    }
+    if (o.dQ)
       sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, f.slabs > 1 ? acc + f.a_dq : nullptr, sl > 0,
                 last ? o.dQ : nullptr, bf, dm.m * pr.d, dm.m * pr.d, 0});
-    }
-    if (o.dX) {
-      const long per_px = static_cast<long>(items) * pr.d;
-      GemmDims gd{items, pr.d, f.slab, dm.m * f.slab, static_cast<int>((dm.m + 31) / 32 * 32), static_cast<int>(dm.m), pr.Px, 0, f.ldq, f.sp_x, per_px,
-                  per_px * pr.Px};
-      hipLaunchKernelGGL((k_grad_gemm<T, true>), dim3((items + 127) / 128, cg, f.sp_x * pr.Px), dim3(256), 0, st, gd,
-                         parts.ds, qt, F(f.off_px));
+    if (o.dX)
       sums.add({F(f.off_px), per_px * pr.Px, per_px * pr.Px, f.sp_x, nullptr, 0, o.dX, bf, per_px,
                 static_cast<long>(pr.N) * pr.d, static_cast<long>(dm.n0) * pr.d});
-    }
-    if (o.da_q || o.db2)
+    if (o.da_q)
       sums.add({parts.da_q, BP, BP, f.slab / 16, acc + f.a_daq, sl > 0, last ? o.da_q : nullptr, 0, BP, BP, 0});
     if (o.da_x)
       sums.add({parts.da_x, items * P, f.slab * P, dm.qsplits, nullptr, 0, o.da_x, 0, items * P, items * P,
@@ -762,13 +826,10 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
     if (o.dW2)
       sums.add({parts.dW2, H * P, H * P, f.wgs, acc + f.a_dw2, sl > 0, last ? o.dW2 : nullptr, bf, H * P, H * P, 0});
     if (o.db1) sums.add({parts.db1, H, H, f.wgs, acc + f.a_db1, sl > 0, last ? o.db1 : nullptr, 0, H, H, 0});
+    if (o.db2) sums.add({parts.db2, P, P, f.wgs, acc + f.a_db2, sl > 0, last ? o.db2 : nullptr, 0, P, P, 0});
     if ((e = sums.run()) != hipSuccess) return e;
   }
-  if (o.db2) {
-    sums.add({acc + f.a_daq, pr.P, pr.P, pr.B, nullptr, 0, o.db2, 0, pr.P, pr.P, 0});
-    if ((e = sums.run()) != hipSuccess) return e;
-  }
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace

@@ -160,6 +160,7 @@ struct Bf16Parts {
   float* dW1;        // [workgroups][H][P]
   float* dW2;        // [workgroups][P][H]
   float* db1;        // [workgroups][H]
+  float* db2;        // [workgroups][P]
 };
 
 // LDS bytes of a wave: s or dl, h and du by tiles of 16 slots or hidden units
@@ -570,12 +571,25 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
       t += row_ror<1>(t);
       if (c == 0) acc[wave * kH + 16 * jt + 4 * g + i] = t;
     }
+  // (db2: da_x summed over the items)
+  float* acc2 = acc + kWaves * kH;
+  {
+    const float t = sum_items<RUN>(dax, c);
+    if (c < RUN) acc2[wave * SLOTS + RUN * g + c] = t;
+  }
   __syncthreads();
   for (int i = tid; i < H; i += kThreads) {
     float t = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) t += acc[w * kH + i];
     out.db1[wg * H + i] = t;
+  }
+  for (int i = tid; i < SLOTS; i += kThreads) {
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) t += acc2[w * SLOTS + i];
+    const int p = component(i);
+    if (p >= 0) out.db2[wg * P + p] = t;
   }
   __syncthreads();
   // da_x: the waves of a block's queries in turn
@@ -609,16 +623,16 @@ struct GemmBf16 {
   int ldb;           // elements of a row of X or Q transposed
 };
 
-// dQ[m][t] = sum over px and items of ds X
-__global__ __launch_bounds__(256) void k_grad_dq_bf16(GemmBf16 gd, const uint32_t* __restrict__ ds,
-                                                      const bf16_t* __restrict__ xt, float* __restrict__ out) {
+// dQ[m][t] = sum over px and items of ds X; z: the split
+__device__ __forceinline__ void dq_tile(const GemmBf16& gd, int z, const uint32_t* __restrict__ ds,
+                                        const bf16_t* __restrict__ xt, float* __restrict__ out) {
   constexpr int RB = 2, CB = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
   const int m0 = (blockIdx.x * 4 + wave) * 16 * RB, t0 = blockIdx.y * 16 * CB;
   if (m0 >= gd.m) return;
   const int per = gd.nb / 2, chunks = per * gd.npx;  // a chunk: two blocks of items
-  const int k0 = static_cast<int>(static_cast<long>(chunks) * blockIdx.z / gd.splits);
-  const int k1 = static_cast<int>(static_cast<long>(chunks) * (blockIdx.z + 1) / gd.splits);
+  const int k0 = static_cast<int>(static_cast<long>(chunks) * z / gd.splits);
+  const int k1 = static_cast<int>(static_cast<long>(chunks) * (z + 1) / gd.splits);
   f32x4_t acc[RB][CB] = {};
   // Lane (c, g) reads piece g of row c of both blocks, rows of 64 bytes, whole;
   // the halves of the wave are then swapped to first terms (items 8 g .. of the
@@ -666,7 +680,7 @@ __global__ __launch_bounds__(256) void k_grad_dq_bf16(GemmBf16 gd, const uint32_
     fetch(v0, min(ch + 2, k1 - 1));
     if (ch + 1 < k1) use(v1);
   }
-  float* dst = out + static_cast<long>(blockIdx.z) * gd.m * gd.d;
+  float* dst = out + static_cast<long>(z) * gd.m * gd.d;
 #pragma unroll
   for (int r = 0; r < RB; ++r)
 #pragma unroll
@@ -680,14 +694,14 @@ __global__ __launch_bounds__(256) void k_grad_dq_bf16(GemmBf16 gd, const uint32_
 
 // dX[px][n][t] = sum over (b, pq) of ds Q: rows of ds of a block of items, 32
 // at a time, through the wave's LDS and the transposing read
-__global__ __launch_bounds__(256) void k_grad_dx_bf16(GemmBf16 gd, const uint32_t* __restrict__ ds,
-                                                      const bf16_t* __restrict__ qt, float* __restrict__ out) {
+// (z: px and split; sh: [block][32 rows][64 bytes] a wave)
+__device__ __forceinline__ void dx_tile(const GemmBf16& gd, int z, const uint32_t* __restrict__ ds,
+                                        const bf16_t* __restrict__ qt, float* __restrict__ out, uint4 (*sh)[256]) {
   constexpr int RB = 2, CB = 4;
-  __shared__ __attribute__((aligned(16))) uint4 sh[4][RB * 128];      // [block][32 rows][64 bytes] a wave
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
   const int blk0 = (blockIdx.x * 4 + wave) * RB, t0 = blockIdx.y * 16 * CB;
   if (blk0 >= gd.nb) return;                                          // (no workgroup barrier below)
-  const int px = blockIdx.z / gd.splits, split = blockIdx.z - px * gd.splits;
+  const int px = z / gd.splits, split = z - px * gd.splits;
   const int chunks = (gd.m + 31) / 32;
   const int k0 = static_cast<int>(static_cast<long>(chunks) * split / gd.splits);
   const int k1 = static_cast<int>(static_cast<long>(chunks) * (split + 1) / gd.splits);
@@ -754,6 +768,21 @@ __global__ __launch_bounds__(256) void k_grad_dx_bf16(GemmBf16 gd, const uint32_
       }
 }
 
+// Both products, side by side (blockIdx.z < zq for dQ), or one.
+template <int WHAT>
+__global__ __launch_bounds__(256) void k_grad_products_bf16(GemmBf16 q, GemmBf16 x, int zq,
+                                                            const uint32_t* __restrict__ ds,
+                                                            const bf16_t* __restrict__ xt,
+                                                            const bf16_t* __restrict__ qt, float* __restrict__ out_q,
+                                                            float* __restrict__ out_x) {
+  if constexpr (WHAT & grad::kProductQ)
+    if (static_cast<int>(blockIdx.z) < zq) dq_tile(q, blockIdx.z, ds, xt, out_q);
+  if constexpr (WHAT & grad::kProductX) {
+    __shared__ __attribute__((aligned(16))) uint4 sh[4][256];
+    if (static_cast<int>(blockIdx.z) >= zq) dx_tile(x, blockIdx.z - zq, ds, qt, out_x, sh);
+  }
+}
+
 // ---------------------------------------------------------------------------
 namespace grad {
 
@@ -763,8 +792,8 @@ struct Bf16Plan {
   Bf16Dims dm;
   int slab, slabs, wgx, wgs;
   int sp_q, sp_x, ldq, ldx;
-  size_t off_ds, off_xt, off_qt, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_pq, off_px, off_acc, bytes;
-  long a_dw1, a_dw2, a_db1, a_dq;       // floats into the sums over slabs
+  size_t off_ds, off_xt, off_qt, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_db2, off_pq, off_px, off_acc, bytes;
+  long a_dw1, a_dw2, a_db1, a_db2, a_dq;       // floats into the sums over slabs
 };
 
 Bf16Plan plan(const DevProb& pr) {
@@ -786,8 +815,8 @@ Bf16Plan plan(const DevProb& pr) {
   f.ldq = padded_row(dm.m);
   f.ldx = padded_row(f.slab);
   const long cg = (pr.d + 63) / 64;
-  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * dm.nb / 2, 8);
-  f.sp_x = split_of(static_cast<long>(dm.nb) / 2 * cg * pr.Px, (dm.m + 31) / 32, 8);
+  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * dm.nb / 2, 2);
+  f.sp_x = split_of(static_cast<long>(dm.nb) / 2 * cg * pr.Px, (dm.m + 31) / 32, 2);
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   size_t at = 0;
   const size_t P = pr.P, H = pr.H;
@@ -799,12 +828,14 @@ Bf16Plan plan(const DevProb& pr) {
   f.off_dw1 = at; at = up(at + 4ul * f.wgs * H * P);
   f.off_dw2 = at; at = up(at + 4ul * f.wgs * H * P);
   f.off_db1 = at; at = up(at + 4ul * f.wgs * H);
+  f.off_db2 = at; at = up(at + 4ul * f.wgs * P);
   f.off_pq = at;  at = up(at + 4ul * f.sp_q * dm.m * pr.d);
   f.off_px = at;  at = up(at + 4ul * f.sp_x * pr.Px * f.slab * pr.d);
   f.a_dw1 = static_cast<long>(pr.B) * P;
   f.a_dw2 = f.a_dw1 + static_cast<long>(H * P);
   f.a_db1 = f.a_dw2 + static_cast<long>(H * P);
-  f.a_dq = f.a_db1 + static_cast<long>(H);
+  f.a_db2 = f.a_db1 + static_cast<long>(H);
+  f.a_dq = f.a_db2 + static_cast<long>(P);
   f.off_acc = at; at = up(at + 4ul * (f.a_dq + (f.slabs > 1 ? dm.m * pr.d : 0)));
   f.bytes = at;
   return f;
@@ -849,7 +880,7 @@ hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_gra
   Bf16Dims dm = f.dm;
   auto F = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
   const Bf16Parts parts{reinterpret_cast<uint32_t*>(ws + f.off_ds), F(f.off_daq), F(f.off_dax), F(f.off_dw1),
-                        F(f.off_dw2), F(f.off_db1)};
+                        F(f.off_dw2), F(f.off_db1), F(f.off_db2)};
   bf16_t* xt = reinterpret_cast<bf16_t*>(ws + f.off_xt);
   bf16_t* qt = reinterpret_cast<bf16_t*>(ws + f.off_qt);
   float* acc = F(f.off_acc);
@@ -865,22 +896,30 @@ hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_gra
                                              o.dQ ? xt : nullptr, st);
     if (e != hipSuccess) return e;
     if ((e = pairs(pr, f, dm, dphi, parts, st)) != hipSuccess) return e;
-    if (o.dQ) {
-      const GemmBf16 gd{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_q, dm.items, f.ldx};
-      hipLaunchKernelGGL(k_grad_dq_bf16, dim3(static_cast<unsigned>((dm.m + 127) / 128), cg, f.sp_q), dim3(256), 0, st, gd,
-                         parts.ds, xt, F(f.off_pq));
+    const long per_px = static_cast<long>(dm.items) * pr.d;
+    if (o.dQ || o.dX) {
+      const GemmBf16 gq{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_q, dm.items, f.ldx};
+      const GemmBf16 gx{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_x, dm.items, f.ldq};
+      auto launch = [&](auto kern, int zq, int zx) {
+        const unsigned x = std::max<long>(zq ? (dm.m + 127) / 128 : 0, zx ? (dm.nb + 7) / 8 : 0);
+        hipLaunchKernelGGL(kern, dim3(x, cg, zq + zx), dim3(256), 0, st, gq, gx, zq, parts.ds, xt, qt, F(f.off_pq),
+                           F(f.off_px));
+      };
+      const int zq = o.dQ ? f.sp_q : 0, zx = o.dX ? f.sp_x * pr.Px : 0;
+      if (zq && zx && products_together(4ul * pr.Px * dm.m * f.slab)) {
+        launch(&k_grad_products_bf16<kProductQ | kProductX>, zq, zx);
+      } else {
+        if (zq) launch(&k_grad_products_bf16<kProductQ>, zq, 0);
+        if (zx) launch(&k_grad_products_bf16<kProductX>, 0, zx);
+      }
+    }
+    if (o.dQ)
       sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, f.slabs > 1 ? acc + f.a_dq : nullptr, sl > 0,
                 last ? o.dQ : nullptr, 1, dm.m * pr.d, dm.m * pr.d, 0});
-    }
-    if (o.dX) {
-      const long per_px = static_cast<long>(dm.items) * pr.d;
-      const GemmBf16 gd{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_x, dm.items, f.ldq};
-      hipLaunchKernelGGL(k_grad_dx_bf16, dim3((dm.nb + 7) / 8, cg, f.sp_x * pr.Px), dim3(256), 0, st, gd, parts.ds, qt,
-                         F(f.off_px));
+    if (o.dX)
       sums.add({F(f.off_px), per_px * pr.Px, per_px * pr.Px, f.sp_x, nullptr, 0, o.dX, 1, per_px,
                 static_cast<long>(pr.N) * pr.d, static_cast<long>(dm.n0) * pr.d});
-    }
-    if (o.da_q || o.db2)
+    if (o.da_q)
       sums.add({parts.da_q, BP, BP, dm.nb, acc, sl > 0, last ? o.da_q : nullptr, 0, BP, BP, 0});
     if (o.da_x)
       sums.add({parts.da_x, dm.items * P, f.slab * P, dm.qsplits, nullptr, 0, o.da_x, 0, dm.items * P, dm.items * P,
@@ -890,10 +929,10 @@ hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_gra
     if (o.dW2)
       sums.add({parts.dW2, H * P, H * P, f.wgs, acc + f.a_dw2, sl > 0, last ? o.dW2 : nullptr, 1, H * P, H * P, 0});
     if (o.db1) sums.add({parts.db1, H, H, f.wgs, acc + f.a_db1, sl > 0, last ? o.db1 : nullptr, 0, H, H, 0});
+    if (o.db2) sums.add({parts.db2, P, P, f.wgs, acc + f.a_db2, sl > 0, last ? o.db2 : nullptr, 0, P, P, 0});
     if ((e = sums.run()) != hipSuccess) return e;
   }
-  if (o.db2) sums.add({acc, P, P, pr.B, nullptr, 0, o.db2, 0, P, P, 0});
-  return sums.run();
+  return hipSuccess;
 }
 
 }  // namespace grad
