@@ -35,7 +35,7 @@ constexpr int kSortOne = 4096;        // tokens sorted by one workgroup
 constexpr int kSortThreads = 256;     // of a block of the radix passes
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSortU = 8;             // loads in flight
-constexpr int kMaxBits = 11;          // digit of a radix pass
+constexpr int kMinBits = 8, kMaxBits = 11;   // digit of a radix pass
 constexpr int kSortBlock = kSortThreads * kSortU;   // tokens a block takes at least
 constexpr int kSortBlocks = 128;      // blocks at most (a row of counts is a multiple of 4)
 
@@ -62,10 +62,12 @@ struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Pack {
   T v[N];
 };
 
-// lanes of the wave (of `live`) whose low `bits` bits of `digit` equal this lane's
-__device__ __forceinline__ uint64_t same_digit(uint32_t digit, int bits, uint64_t live) {
+// lanes of the wave (of `live`) whose low BITS bits of `digit` equal this lane's
+template <int BITS>
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, uint64_t live) {
   uint64_t m = live;
-  for (int b = 0; b < bits; ++b) {
+#pragma unroll
+  for (int b = 0; b < BITS; ++b) {
     const bool on = (digit >> b) & 1;
     const uint64_t x = __ballot(on);
     m &= on ? x : ~x;
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(1024) void k_sort_one(const int32_t* __restrict__ i
       const bool live = b + lane < i1;
       const uint2 p = live ? pairs[cur][b + lane] : make_uint2(0, 0);
       const uint32_t digit = (p.x >> shift) & 255;
-      const uint64_t m = same_digit(digit, 8, __ballot(live));
+      const uint64_t m = same_digit<8>(digit, __ballot(live));
       const int rank = __popcll(m & ((1ull << lane) - 1));
       const uint32_t at = hist[w][digit] + rank;
       __builtin_amdgcn_wave_barrier();
@@ -217,17 +219,17 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_hist(const int32_t* __res
 // Stable scatter of one pass: wave w of block j takes the w-th part of the
 // block's tokens, in order, and its tokens of a digit follow those of the
 // digits below, of the blocks before and of the waves before.
+template <int BITS>
 __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(const int32_t* __restrict__ ids,
                                                                const uint2* __restrict__ in, long T, int V, int per,
-                                                               int shift, int bits, int nbp,
+                                                               int shift, int nbp,
                                                                const uint32_t* __restrict__ counts,
                                                                uint2* __restrict__ out) {
-  __shared__ uint32_t hist[kSortWaves][1 << kMaxBits];
+  constexpr int bins = 1 << BITS, PT = bins / kSortThreads, UN = 16 / PT;   // thread tid has bins PT tid ..
+  __shared__ uint32_t hist[kSortWaves][bins];
   __shared__ uint32_t carry[kSortWaves];
-  constexpr int PT = (1 << kMaxBits) / kSortThreads;   // bins a thread, at most
-  const int bins = 1 << bits, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int mine = blockIdx.x;
-  for (int i = tid; i < bins * kSortWaves; i += kSortThreads) hist[i / bins][i & (bins - 1)] = 0;
   const long i0 = min(T, static_cast<long>(mine) * per + static_cast<long>(w) * (per / kSortWaves));
   const long i1 = min(T, i0 + per / kSortWaves);
   uint2 tok[kSortU];                                   // the wave's next tokens
@@ -236,6 +238,25 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(const int32_t* __
     for (int u = 0; u < kSortU; ++u) tok[u] = token(ids, in, min(b + u * 64 + lane, T - 1), V);
   };
   fetch(i0);
+  // totals of every bin and those of the blocks before
+  uint32_t tot[PT] = {}, before[PT] = {};
+#pragma unroll UN
+  for (int j = 0; j < nbp; j += 4)
+#pragma unroll
+    for (int k = 0; k < PT; ++k) {
+      const uint4 n = *reinterpret_cast<const uint4*>(counts + static_cast<long>(PT * tid + k) * nbp + j);
+      tot[k] += (n.x + n.y) + (n.z + n.w);
+      before[k] += (j < mine ? n.x : 0) + (j + 1 < mine ? n.y : 0) + (j + 2 < mine ? n.z : 0) + (j + 3 < mine ? n.w : 0);
+    }
+#pragma unroll
+  for (int k = 0; k < PT; ++k)
+#pragma unroll
+    for (int j = 0; j < kSortWaves; ++j) hist[j][PT * tid + k] = 0;
+  uint32_t sum = 0;
+#pragma unroll
+  for (int k = 0; k < PT; ++k) sum += tot[k];
+  const uint32_t incl = wave_scan(sum, lane);
+  if (lane == 63) carry[w] = incl;
   __syncthreads();
   for (long b = i0; b < i1; b += 64 * kSortU) {
     if (b > i0) fetch(b);
@@ -243,53 +264,30 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(const int32_t* __
     for (int u = 0; u < kSortU; ++u)
       if (b + u * 64 + lane < i1) atomicAdd(&hist[w][(tok[u].x >> shift) & (bins - 1)], 1u);
   }
-  // totals of every bin and those of the blocks before: thread tid has bins tid + 256 k
-  uint32_t tot[PT] = {}, before[PT] = {};
-#pragma unroll
-  for (int k = 0; k < PT; ++k) {
-    const int b = tid + k * kSortThreads;
-    if (b < bins) {
-      const uint4* row = reinterpret_cast<const uint4*>(counts + static_cast<long>(b) * nbp);
-#pragma unroll 8
-      for (int j = 0; j < nbp; j += 4) {
-        const uint4 n = row[j >> 2];
-        tot[k] += (n.x + n.y) + (n.z + n.w);
-        before[k] += (j < mine ? n.x : 0) + (j + 1 < mine ? n.y : 0) + (j + 2 < mine ? n.z : 0) + (j + 3 < mine ? n.w : 0);
-      }
-    }
-  }
   if (i1 - i0 > 64 * kSortU) fetch(i0);
+  uint32_t start = incl - sum;
+#pragma unroll
+  for (int j = 0; j < kSortWaves; ++j) start += j < w ? carry[j] : 0;
   __syncthreads();
-  uint32_t run = 0;                                    // tokens of the bins of earlier rounds
 #pragma unroll
   for (int k = 0; k < PT; ++k) {
-    if (k * kSortThreads >= bins) break;
-    const uint32_t incl = wave_scan(tot[k], lane);
-    if (lane == 63) carry[w] = incl;
-    __syncthreads();
-    uint32_t at = run + incl - tot[k] + before[k], all = 0;
+    uint32_t at = start + before[k];
+    start += tot[k];
+#pragma unroll
     for (int j = 0; j < kSortWaves; ++j) {
-      if (j < w) at += carry[j];
-      all += carry[j];
+      const uint32_t n = hist[j][PT * tid + k];
+      hist[j][PT * tid + k] = at;
+      at += n;
     }
-    run += all;
-    const int b = tid + k * kSortThreads;
-    if (b < bins) {
-      for (int j = 0; j < kSortWaves; ++j) {
-        const uint32_t n = hist[j][b];
-        hist[j][b] = at;
-        at += n;
-      }
-    }
-    __syncthreads();
   }
+  __syncthreads();
   for (long b = i0; b < i1; b += 64 * kSortU) {
     if (b > i0) fetch(b);
 #pragma unroll
     for (int u = 0; u < kSortU; ++u) {
       const bool live = b + u * 64 + lane < i1;
       const uint32_t digit = (tok[u].x >> shift) & (bins - 1);
-      const uint64_t m = same_digit(digit, bits, __ballot(live));
+      const uint64_t m = same_digit<BITS>(digit, __ballot(live));
       const int rank = __popcll(m & ((1ull << lane) - 1));
       const uint32_t at = hist[w][digit] + rank;
       __builtin_amdgcn_wave_barrier();
@@ -591,16 +589,17 @@ static hipError_t launch_sort(const int32_t* ids, long T, int V, uint2* a, uint2
     hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(1024), 0, st, ids, static_cast<int>(T), V, bits, a);
     return hipGetLastError();
   }
-  const int passes = (bits + kMaxBits - 1) / kMaxBits, each = (bits + passes - 1) / passes;
+  const int passes = (bits + kMaxBits - 1) / kMaxBits, each = std::max(kMinBits, (bits + passes - 1) / passes);
   const int per = sort_per(T), nb = static_cast<int>((T + per - 1) / per), nbp = (nb + 3) / 4 * 4;
+  auto scatter = each == 8 ? &k_sort_scatter<8> : each == 9 ? &k_sort_scatter<9> : each == 10 ? &k_sort_scatter<10>
+                                                                                              : &k_sort_scatter<11>;
   // the last pass ends in `a`
   const uint2* in = nullptr;
   for (int p = 0; p < passes; ++p) {
     uint2* to = (passes - p) % 2 ? a : b;
     hipLaunchKernelGGL(k_sort_hist, dim3(nbp), dim3(kSortThreads), 0, st, ids, in, T, V, per, p * each, each, nbp,
                        counts);
-    hipLaunchKernelGGL(k_sort_scatter, dim3(nb), dim3(kSortThreads), 0, st, ids, in, T, V, per, p * each, each, nbp,
-                       counts, to);
+    hipLaunchKernelGGL(scatter, dim3(nb), dim3(kSortThreads), 0, st, ids, in, T, V, per, p * each, nbp, counts, to);
     in = to;
   }
   return hipGetLastError();

@@ -551,20 +551,31 @@ def softmax_loss(phi: torch.Tensor, target: torch.Tensor, ids: Optional[torch.Te
 _GRADS = ("dQ", "dX", "da_q", "da_x", "dW1", "db1", "dW2", "db2")
 
 
-def score_grad(prob: Problem, dphi: torch.Tensor, ws=None, stream=None, only: Optional[Sequence[str]] = None):
+def score_grad(prob: Problem, dphi: torch.Tensor, ws=None, stream=None, only: Optional[Sequence[str]] = None,
+               out: Optional[dict] = None):
     """Gradients of score(prob) for the problem's tensors, given dphi [B][N]:
     a dict of dQ, dX, da_q, da_x, dW1, db1, dW2 and db2 (or those in ``only``),
-    each of its tensor's shape and type."""
+    each of its tensor's shape and type.  out: tensors to write some of them to."""
     _operand(dphi, "dphi", (prob.B, prob.N), (torch.float32,), prob.device)
     names = _GRADS if only is None else tuple(only)
     if not all(n in _GRADS for n in names):
         raise ValueError(f"unknown gradient in {names}: {', '.join(_GRADS)}")
     _need(all(t is not None for t in prob.tensors), "the problem lacks a gating tensor")
+    if out is not None and not set(out) <= set(names):
+        raise ValueError(f"out holds {sorted(out)}, gradients are {', '.join(names)}")
     with _on(prob.device, stream):
         ws = _workspace(lambda: mol_workspace_size(prob, MOL_OP_SCORE_GRAD), ws, prob.device)
-        out = {g: torch.empty_like(t) for g, t in zip(_GRADS, prob.tensors) if g in names}
-        mol_score_grad(prob, dphi, out, ws, stream)
-    return out
+        got = {}
+        for g, t in zip(_GRADS, prob.tensors):
+            if g not in names:
+                continue
+            if out is not None and g in out:
+                _operand(out[g], g, t.shape, (t.dtype,), prob.device)
+                got[g] = out[g]
+            else:
+                got[g] = torch.empty_like(t)
+        mol_score_grad(prob, dphi, got, ws, stream)
+    return got
 
 
 class AdamwTensors:
@@ -654,3 +665,81 @@ def adamw_step(tensors: AdamwTensors, lr=1e-3, beta1: float = 0.9, beta2: float 
                     _ptr(lr) if on_lr else None, _ptr(step) if on_step else None)
     with _on(tensors.device, stream):
         mol_adamw_step(opt, tensors.c, tensors.n, stream)
+
+
+class Learner:
+    """One model in training by the sampled-softmax objective: embedding tables
+    and gating parameters, their bfloat16 copies that the kernels score with,
+    gradients and AdamW states, all laid out once.
+
+    queries [Vq][Pq][d] and items [Px][V][d]: the component embeddings' float32
+    masters; a_q [Vq][P], a_x [V][P]: the gating logits of every query and item;
+    W1 [H][P], b1 [H], W2 [P][H], b2 [P]: the gating MLP, all float32 (they are
+    updated in place).  weight_decay is for the embeddings and W1, W2.
+    states_8bit: AdamW states of the two embedding tables in 8 bits.
+
+    The copy of the items' table is laid out as a corpus: ``problem`` gives the
+    retrieval problem of the model as it is.
+    """
+
+    def __init__(self, queries, items, a_q, a_x, W1, b1, W2, b2, weight_decay: float = 0.0, states_8bit: bool = False,
+                 seed: int = 0):
+        Vq, Pq, d = queries.shape
+        Px, V, _ = items.shape
+        P, dev = Pq * Px, queries.device
+        H = W1.shape[0]
+        for name, t, shape in (("items", items, (Px, V, d)), ("a_q", a_q, (Vq, P)), ("a_x", a_x, (V, P)), ("W1", W1, (H, P)),
+                               ("b1", b1, (H,)), ("W2", W2, (P, H)), ("b2", b2, (P,)), ("queries", queries, (Vq, Pq, d))):
+            _operand(t, name, shape, (torch.float32,), dev)
+        self.master = dict(queries=queries, items=items, a_q=a_q, a_x=a_x, W1=W1, b1=b1, W2=W2, b2=b2)
+        self.copy = {n: self.master[n].bfloat16() for n in ("queries", "items", "W1", "W2")}
+        self.grad = {n: torch.empty_like(t, dtype=torch.bfloat16 if n in ("W1", "W2") else torch.float32)
+                     for n, t in self.master.items()}
+        eight = {n: states_8bit and n in ("queries", "items") for n in self.master}
+        state = lambda n, t: torch.zeros_like(t, dtype=torch.float8_e4m3fn if eight[n] else torch.float32)  # noqa: E731
+        scale = lambda n, t: (torch.zeros((t.numel() + MOL_STATE_BLOCK - 1) // MOL_STATE_BLOCK, device=dev)  # noqa: E731
+                              if eight[n] else None)
+        m, v = ({n: state(n, t) for n, t in self.master.items()} for _ in range(2))
+        ms, vs = ([scale(n, t) for n, t in self.master.items()] for _ in range(2))
+        self.tensors = AdamwTensors(
+            list(self.master.values()), list(self.grad.values()), list(m.values()), list(v.values()), ms, vs,
+            weight_decay=[weight_decay if n in self.copy else 0.0 for n in self.master],
+            out=dict(copy=[self.copy.get(n) for n in self.master]))
+        self.state = dict(m=m, v=v)
+        self.steps = torch.zeros(1, dtype=torch.int32, device=dev)   # on the GPU, so that a captured step counts on
+        self.seed = seed
+        self.shape = (Vq, V, Pq, Px, P, d)
+
+    def step(self, query_ids: torch.Tensor, item_ids: torch.Tensor, target: torch.Tensor, lr: torch.Tensor,
+             inv_temp: float = 20.0) -> torch.Tensor:
+        """One optimisation step on B queries and N sampled items: query_ids int32
+        [B], item_ids int32 [N] (negative: an empty slot), target int32 [B]: the
+        column of each query's positive; lr: one float32 on the GPU.  Returns the
+        losses [B] from before the step.  Allocates with torch and launches on the
+        current stream only: it can be captured into a graph."""
+        Vq, V, Pq, Px, P, d = self.shape
+        B, N = query_ids.numel(), item_ids.numel()
+        M, C, G = self.master, self.copy, self.grad
+        queries = C["queries"].view(1, Vq, Pq * d)
+        prob = Problem(embed_lookup(queries, query_ids).view(B, Pq, d), embed_lookup(C["items"], item_ids),
+                       embed_lookup(M["a_q"].view(1, Vq, P), query_ids).view(B, P),
+                       embed_lookup(M["a_x"].view(1, V, P), item_ids).view(N, P), C["W1"], M["b1"], C["W2"], M["b2"])
+        phi = score(prob)
+        weight = torch.full((B,), 1.0 / B, device=phi.device)
+        loss, dphi = softmax_loss(phi, target, item_ids, inv_temp, weight, dphi=phi)
+        g = score_grad(prob, dphi, out=dict(dW1=G["W1"], db1=G["b1"], dW2=G["W2"], db2=G["b2"]))
+        embed_grad(g["dQ"].view(1, B, Pq * d), query_ids, Vq, out=G["queries"].view(1, Vq, Pq * d))
+        embed_grad(g["dX"], item_ids, V, out=G["items"])
+        embed_grad(g["da_q"].view(1, B, P), query_ids, Vq, out=G["a_q"].view(1, Vq, P))
+        embed_grad(g["da_x"].view(1, N, P), item_ids, V, out=G["a_x"].view(1, V, P))
+        self.steps.add_(1)
+        adamw_step(self.tensors, lr=lr, step=self.steps, seed=self.seed)
+        return loss
+
+    def problem(self, query_ids: torch.Tensor, flags: int = 0) -> Problem:
+        """The retrieval problem of these queries against all items."""
+        Vq, V, Pq, Px, P, d = self.shape
+        B = query_ids.numel()
+        return Problem(embed_lookup(self.copy["queries"].view(1, Vq, Pq * d), query_ids).view(B, Pq, d), self.copy["items"],
+                       embed_lookup(self.master["a_q"].view(1, Vq, P), query_ids).view(B, P), self.master["a_x"],
+                       self.copy["W1"], self.master["b1"], self.copy["W2"], self.master["b2"], flags)
