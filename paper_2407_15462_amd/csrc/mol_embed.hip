@@ -624,7 +624,7 @@ static hipError_t grad_t(const void* grad, int C, int V, int d, const int32_t* i
   a.accumulate = accumulate;
   // zero rows: blocks of about 64 KB, as many rows as their bitmap holds at most
   a.zrows = static_cast<int>(std::max<long>(1, std::min<long>({65536l / (static_cast<long>(d) * static_cast<long>(sizeof(TO))), 8192l, static_cast<long>(V)})));
-  a.zblocks = accumulate ? 0 : (V + a.zrows - 1) / a.zrows;
+  a.zblocks = accumulate ? 0 : static_cast<int>((V + a.zrows - 1l) / a.zrows);
   const long blocks = static_cast<long>(a.spans) * a.slices * C + static_cast<long>(a.zblocks) * C;
   if (blocks > 0) {
     auto kern = ve == 1 ? &k_embed_grad<TI, TO, 1> : &k_embed_grad<TI, TO, VE>;

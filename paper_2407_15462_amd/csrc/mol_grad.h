@@ -19,12 +19,12 @@ struct SumJob {
   void* out;               // NULL, or the output
   int bf16;
   long in_len, out_len, out_at;
-  int wide, blocks;        // (set by the launcher) 256 columns a block, blocks
+  int wide;                // (set by the launcher) 256 columns a block
 };
 constexpr int kSumJobs = 8;   // one an output
 struct SumArgs {
   int n;
-  int first[kSumJobs + 1];
+  long first[kSumJobs + 1];    // first block of each job
   SumJob job[kSumJobs];
 };
 struct SumList {

@@ -613,34 +613,35 @@ __global__ __launch_bounds__(256) void k_grad_products(GemmDims q, GemmDims x, i
 // block; many: 64 columns and four runs of parts a block.
 __global__ __launch_bounds__(256) void k_sum_parts(SumArgs a) {
   __shared__ float sh[4][64];
-  int j = 0;
-  while (j + 1 < a.n && a.first[j + 1] <= static_cast<int>(blockIdx.x)) ++j;
-  const SumJob& s = a.job[j];
   const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
-  const long blk = static_cast<long>(blockIdx.x) - a.first[j];
-  const long o = s.wide ? blk * 256 + threadIdx.x : blk * 64 + lane;
-  float v = 0.f;
-  const int k0 = s.wide ? 0 : static_cast<int>(static_cast<long>(s.S) * run / 4);
-  const int k1 = s.wide ? s.S : static_cast<int>(static_cast<long>(s.S) * (run + 1) / 4);
-  if (o < s.L) {
+  for (long blk0 = blockIdx.x; blk0 < a.first[a.n]; blk0 += gridDim.x) {
+    int j = 0;
+    while (j + 1 < a.n && a.first[j + 1] <= blk0) ++j;
+    const SumJob& s = a.job[j];
+    const long blk = blk0 - a.first[j], o = s.wide ? blk * 256 + threadIdx.x : blk * 64 + lane;
+    float v = 0.f;
+    const int k0 = s.wide ? 0 : static_cast<int>(static_cast<long>(s.S) * run / 4);
+    const int k1 = s.wide ? s.S : static_cast<int>(static_cast<long>(s.S) * (run + 1) / 4);
+    if (o < s.L) {
 #pragma unroll 8
-    for (int k = k0; k < k1; ++k) v += s.in[k * s.stride + o];
-  }
-  if (!s.wide) {
-    sh[run][lane] = v;
-    __syncthreads();
-    if (run) return;
-    v = (sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane]);
-  }
-  if (o >= s.L) return;
-  if (s.add) v += s.acc[o];
-  if (s.acc) s.acc[o] = v;
-  if (s.out) {
-    const long bt = o / s.in_len, at = bt * s.out_len + s.out_at + (o - bt * s.in_len);
-    if (s.bf16)
-      static_cast<bf16_t*>(s.out)[at] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
-    else
-      static_cast<float*>(s.out)[at] = v;
+      for (int k = k0; k < k1; ++k) v += s.in[k * s.stride + o];
+    }
+    if (!s.wide) {
+      sh[run][lane] = v;
+      __syncthreads();
+      v = (sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane]);
+      __syncthreads();
+    }
+    if (o >= s.L || (run && !s.wide)) continue;
+    if (s.add) v += s.acc[o];
+    if (s.acc) s.acc[o] = v;
+    if (s.out) {
+      const long bt = o / s.in_len, at = bt * s.out_len + s.out_at + (o - bt * s.in_len);
+      if (s.bf16)
+        static_cast<bf16_t*>(s.out)[at] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+      else
+        static_cast<float*>(s.out)[at] = v;
+    }
   }
 }
 
@@ -649,13 +650,14 @@ namespace grad {
 void SumList::add(const SumJob& j) {
   SumJob& s = a.job[a.n] = j;
   s.wide = j.S <= 16 && j.L >= 4096;
-  s.blocks = static_cast<int>(s.wide ? (j.L + 255) / 256 : (j.L + 63) / 64);
-  a.first[a.n + 1] = a.first[a.n] + s.blocks;
+  a.first[a.n + 1] = a.first[a.n] + (s.wide ? (j.L + 255) / 256 : (j.L + 63) / 64);
   ++a.n;
 }
 
 hipError_t SumList::run() {
-  if (a.n) hipLaunchKernelGGL(k_sum_parts, dim3(a.first[a.n]), dim3(256), 0, st, a);
+  // (a grid holds 2^32 threads)
+  const unsigned blocks = static_cast<unsigned>(std::min<long>(a.first[a.n], 1l << 22));
+  if (a.n) hipLaunchKernelGGL(k_sum_parts, dim3(blocks), dim3(256), 0, st, a);
   a.n = 0;
   return hipGetLastError();
 }

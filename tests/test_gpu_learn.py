@@ -115,6 +115,27 @@ def test_embed_grad_is_the_transpose_of_lookup():
     assert abs((up - down) / 2 - dot) <= size * 505 * lh.U
 
 
+def test_rows_past_32_bits():
+    """Tables whose rows lie beyond 2^32 bytes and 2^32 elements from their start."""
+    V, d = (1 << 30) + 7, 4
+    table = torch.zeros(1, V, d, dtype=BF16, device="cuda")
+    far = torch.tensor([V - 1, 0, 1 << 29, V - 3, V, -1, V - 1], dtype=torch.int32, device="cuda")
+    rows = torch.arange(1, 29, device="cuda").view(7, 4).to(BF16)
+    live = [0, 1, 2, 3]
+    table[0, far[live].long()] = rows[live]
+    got = mol.embed_lookup(table, far, 2.0)
+    want = rows * 2
+    want[[4, 5]] = 0
+    want[6] = want[0]
+    assert torch.equal(got[0], want)
+    table.fill_(9.0)
+    mol.embed_grad(rows.view(1, 7, 4), far, V, out=table)
+    sums = rows.float()
+    sums[0] += sums[6]
+    assert torch.equal(table[0, far[live].long()], sums[live].to(BF16))
+    assert int((table != 0).sum()) == 16
+
+
 # ------------------------------------------------------------------ loss
 def loss_case(B, N, gen, with_ids):
     phi = torch.randn(B, N, generator=gen).clamp_(-3, 3)
