@@ -189,7 +189,7 @@ def test_binding_refuses_what_the_library_cannot_see():
 # ---------------------------------------------------------------- the compiled kernels
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not available")
 def test_no_mfma_result_read_early(tmp_path):
-    sources = ["mol_score_grad.hip"]
+    sources = ["mol_score_grad.hip", "mol_score_grad_bf16.hip"]
     with cf.ThreadPoolExecutor() as ex:
         listings = dict(zip(sources, ex.map(lambda s: _asm(s, str(tmp_path)), sources)))
     bad = {s: early_reads(a, need=8) for s, a in listings.items()}
