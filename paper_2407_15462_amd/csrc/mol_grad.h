@@ -19,7 +19,7 @@ struct SumJob {
   void* out;               // NULL, or the output
   int bf16;
   long in_len, out_len, out_at;
-  int wide;                // (set by the launcher) 256 columns a block
+  int cols_log2;           // (set by the launcher) columns of a block: 256, 64 or 16
 };
 constexpr int kSumJobs = 8;   // one an output
 struct SumArgs {
@@ -58,11 +58,50 @@ inline bool products_together(size_t ds_bytes) { return ds_bytes <= (size_t(64) 
 // all in the same channels of the L2 cache.
 inline int padded_row(long n) { return static_cast<int>((n + 31) / 32 * 32 + 64); }
 
-// K splits of a product of `waves` waves a part with `chunks` K chunks, `least` of them a part
+// K splits of a product of `waves` waves a part with `chunks` K chunks: 2048 waves
+// in all at most, with two chunks a split up to 64 splits (a short product is a chain of
+// latencies) and `least` beyond (each split is a part to write and to add).
 inline int split_of(long waves, long chunks, long least) {
-  const long want = (2048 + waves - 1) / waves, most = chunks / least;
+  const long want = 2048 / waves;
+  long most = chunks / 2 < 64 ? chunks / 2 : 64;
+  if (chunks / least > most) most = chunks / least;
   const long n = want < most ? want : most;
-  return static_cast<int>(n < 1 ? 1 : n > 64 ? 64 : n);
+  return static_cast<int>(n < 1 ? 1 : n);
+}
+
+// Stores a wave's tile of a product: element (4 g + i, c) of each 16x16 block, rows
+// from m0 to m and columns from t0 to d, as a part's float32 or as the output's type.
+template <typename T, int RB, int CB>
+__device__ __forceinline__ void put_tile(void* out, long base, int m0, int m, int t0, int d, int direct,
+                                         const tile::f32x4_t (&acc)[RB][CB]) {
+  const int c = threadIdx.x & 15, g = threadIdx.x / 16 % 4;
+  auto each = [&](auto put) {
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+      for (int t = 0; t < CB; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = m0 + 16 * r + 4 * g + i, x = t0 + 16 * t + c;
+          if (row < m && x < d) put(base + static_cast<long>(row) * d + x, acc[r][t][i]);
+        }
+  };
+  if (sizeof(T) == 2 && direct)
+    each([&](long at, float v) { static_cast<bf16_t*>(out)[at] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v)); });
+  else
+    each([&](long at, float v) { static_cast<float*>(out)[at] = v; });
+}
+
+// A product's tiles of 32 rows and 64 columns, a wave each: `rows` by `cols` of them
+// and z (splits, and item components of dX).  Waves are numbered through, so that
+// four of any of them make a workgroup.
+struct Tiles {
+  int rows, cols, z;
+  __host__ __device__ long count() const { return static_cast<long>(rows) * cols * z; }
+};
+__device__ __forceinline__ int3 tile_of(const Tiles& t, uint32_t unit) {
+  const uint32_t rest = unit / static_cast<uint32_t>(t.rows), z = rest / static_cast<uint32_t>(t.cols);
+  return make_int3(unit - rest * t.rows, rest - z * t.cols, z);
 }
 
 }  // namespace grad

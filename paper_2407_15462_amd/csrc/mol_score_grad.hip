@@ -517,15 +517,17 @@ struct GemmDims {
   long b_px;               // elements between px of Bt (0: the same)
   int ldb;
   int splits;
-  long out_px, out_split;  // floats between px (dX), between splits
+  long out_px, out_split;  // elements between px (dX), between splits
+  int direct;              // one split: out is the output itself
+  Tiles tiles;
 };
 template <typename T, bool COLS>
-__device__ __forceinline__ void product_tile(const GemmDims& gd, int z, const uint32_t* __restrict__ ds,
-                                             const T* __restrict__ Bt, float* __restrict__ out) {
+__device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, const uint32_t* __restrict__ ds,
+                                             const T* __restrict__ Bt, void* __restrict__ out) {
   constexpr int E = 16 / sizeof(T), KCH = 4 * E, RB = 2, CB = 4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-  const int m0 = (blockIdx.x * 4 + wave) * 16 * RB, t0 = blockIdx.y * 16 * CB;
-  if (m0 >= gd.m) return;
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int3 at = tile_of(gd.tiles, unit);
+  const int m0 = at.x * 16 * RB, t0 = at.y * 16 * CB, z = at.z;
   const int split = z % gd.splits, px0 = COLS ? z / gd.splits : 0;
   const int per = gd.k_px / KCH, chunks = COLS ? per : per * gd.npx;
   const int k0 = static_cast<int>(static_cast<long>(chunks) * split / gd.splits);
@@ -536,103 +538,112 @@ __device__ __forceinline__ void product_tile(const GemmDims& gd, int z, const ui
   for (int r = 0; r < RB; ++r) row[r] = min(m0 + 16 * r + c, gd.m - 1);
 #pragma unroll
   for (int t = 0; t < CB; ++t) col[t] = min(t0 + 16 * t + c, gd.d - 1);
-  for (int ch = k0; ch < k1; ++ch) {
+  struct Chunk {
+    uint32_t a[RB][E];
+    uint4 b[CB];
+  };
+  auto fetch = [&](Chunk& v, int ch) {
     const int px = COLS ? px0 : ch / per, k = (COLS ? ch : ch - px * per) * KCH + g * E;
     const uint32_t* A = ds + px * gd.a_px;
     const T* B = Bt + px * gd.b_px + k;
-    uint32_t a[RB][E];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
       if constexpr (COLS) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const uint32_t v = A[min(k + e, gd.kvalid - 1) * gd.lda + row[r]];
-          a[r][e] = k + e < gd.kvalid ? v : 0;
-        }
+        for (int e = 0; e < E; ++e) v.a[r][e] = A[min(k + e, gd.kvalid - 1) * gd.lda + row[r]];
       } else {
 #pragma unroll
         for (int e = 0; e < E; e += 4) {
-          const uint4 v = *reinterpret_cast<const uint4*>(A + row[r] * gd.lda + k + e);
-          a[r][e] = v.x;
-          a[r][e + 1] = v.y;
-          a[r][e + 2] = v.z;
-          a[r][e + 3] = v.w;
+          const uint4 x = *reinterpret_cast<const uint4*>(A + row[r] * gd.lda + k + e);
+          v.a[r][e] = x.x;
+          v.a[r][e + 1] = x.y;
+          v.a[r][e + 2] = x.z;
+          v.a[r][e + 3] = x.w;
         }
       }
     }
-    uint4 bv[CB];
 #pragma unroll
-    for (int t = 0; t < CB; ++t) bv[t] = *reinterpret_cast<const uint4*>(B + static_cast<long>(col[t]) * gd.ldb);
+    for (int t = 0; t < CB; ++t) v.b[t] = *reinterpret_cast<const uint4*>(B + static_cast<long>(col[t]) * gd.ldb);
+  };
+  auto use = [&](const Chunk& v, int ch) {
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-      if constexpr (sizeof(T) == 4) {
-        const uint4 av = make_uint4(a[r][0], a[r][1], a[r][2], a[r][3]);
+      uint32_t a[E];
 #pragma unroll
-        for (int t = 0; t < CB; ++t) acc[r][t] = mma16<T>(av, bv[t], acc[r][t]);
+      for (int e = 0; e < E; ++e) a[e] = !COLS || ch * KCH + g * E + e < gd.kvalid ? v.a[r][e] : 0;
+      if constexpr (sizeof(T) == 4) {
+        const uint4 av = make_uint4(a[0], a[1], a[2], a[3]);
+#pragma unroll
+        for (int t = 0; t < CB; ++t) acc[r][t] = mma16<T>(av, v.b[t], acc[r][t]);
       } else {
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          hi[e] = __builtin_amdgcn_perm(a[r][2 * e + 1], a[r][2 * e], 0x05040100u);
-          lo[e] = __builtin_amdgcn_perm(a[r][2 * e + 1], a[r][2 * e], 0x07060302u);
+          hi[e] = __builtin_amdgcn_perm(a[2 * e + 1], a[2 * e], 0x05040100u);
+          lo[e] = __builtin_amdgcn_perm(a[2 * e + 1], a[2 * e], 0x07060302u);
         }
         const uint4 ah = make_uint4(hi[0], hi[1], hi[2], hi[3]), al = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 #pragma unroll
-        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(al, bv[t], acc[r][t]);
+        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(al, v.b[t], acc[r][t]);
 #pragma unroll
-        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(ah, bv[t], acc[r][t]);
+        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(ah, v.b[t], acc[r][t]);
       }
     }
+  };
+  // (two sets of registers in turn: copies of one would wait for its loads)
+  Chunk v0, v1;
+  if (k0 < k1) fetch(v0, k0);
+  for (int ch = k0; ch < k1; ch += 2) {
+    fetch(v1, min(ch + 1, k1 - 1));
+    use(v0, ch);
+    fetch(v0, min(ch + 2, k1 - 1));
+    if (ch + 1 < k1) use(v1, ch + 1);
   }
-  float* dst = out + px0 * gd.out_px + split * gd.out_split;
-#pragma unroll
-  for (int r = 0; r < RB; ++r)
-#pragma unroll
-    for (int t = 0; t < CB; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int m = m0 + 16 * r + 4 * g + i, x = t0 + 16 * t + c;
-        if (m < gd.m && x < gd.d) dst[static_cast<long>(m) * gd.d + x] = acc[r][t][i];
-      }
+  put_tile<T>(out, px0 * gd.out_px + split * gd.out_split, m0, gd.m, t0, gd.d, gd.direct, acc);
 }
 
 // ---------------------------------------------------------------------------
-// Both products, side by side (blockIdx.z < zq for dQ), or one.
+// Both products, side by side (the first tiles are dQ's), or one.
 template <typename T, int WHAT>
-__global__ __launch_bounds__(256) void k_grad_products(GemmDims q, GemmDims x, int zq, const uint32_t* __restrict__ ds,
+__global__ __launch_bounds__(256) void k_grad_products(GemmDims q, GemmDims x, const uint32_t* __restrict__ ds,
                                                        const T* __restrict__ xt, const T* __restrict__ qt,
-                                                       float* __restrict__ out_q, float* __restrict__ out_x) {
+                                                       void* __restrict__ out_q, void* __restrict__ out_x) {
+  const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t nq = WHAT & kProductQ ? static_cast<uint32_t>(q.tiles.count()) : 0;
   if constexpr (WHAT & kProductQ)
-    if (static_cast<int>(blockIdx.z) < zq) product_tile<T, false>(q, blockIdx.z, ds, xt, out_q);
+    if (unit < nq) product_tile<T, false>(q, unit, ds, xt, out_q);
   if constexpr (WHAT & kProductX)
-    if (static_cast<int>(blockIdx.z) >= zq) product_tile<T, true>(x, blockIdx.z - zq, ds, qt, out_x);
+    if (unit >= nq && unit - nq < static_cast<uint32_t>(x.tiles.count())) product_tile<T, true>(x, unit - nq, ds, qt, out_x);
 }
 
 // ---------------------------------------------------------------------------
-// Sums of partial results (SumJob).  Few parts: a column a thread, 256 a
-// block; many: 64 columns and four runs of parts a block.
+// Sums of partial results (SumJob).  A block has 256, 64 or 16 columns, and
+// one, 4 or 16 runs of the parts of each: the more parts there are, the fewer columns.
 __global__ __launch_bounds__(256) void k_sum_parts(SumArgs a) {
-  __shared__ float sh[4][64];
-  const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
+  __shared__ float sh[256];
   for (long blk0 = blockIdx.x; blk0 < a.first[a.n]; blk0 += gridDim.x) {
     int j = 0;
     while (j + 1 < a.n && a.first[j + 1] <= blk0) ++j;
     const SumJob& s = a.job[j];
-    const long blk = blk0 - a.first[j], o = s.wide ? blk * 256 + threadIdx.x : blk * 64 + lane;
+    const int cols = 1 << s.cols_log2, runs = 256 >> s.cols_log2;
+    const int lane = threadIdx.x & (cols - 1), run = threadIdx.x >> s.cols_log2;
+    const long o = (blk0 - a.first[j]) * cols + lane;
     float v = 0.f;
-    const int k0 = s.wide ? 0 : static_cast<int>(static_cast<long>(s.S) * run / 4);
-    const int k1 = s.wide ? s.S : static_cast<int>(static_cast<long>(s.S) * (run + 1) / 4);
+    const int k0 = static_cast<int>(static_cast<long>(s.S) * run / runs);
+    const int k1 = static_cast<int>(static_cast<long>(s.S) * (run + 1) / runs);
     if (o < s.L) {
 #pragma unroll 8
       for (int k = k0; k < k1; ++k) v += s.in[k * s.stride + o];
     }
-    if (!s.wide) {
-      sh[run][lane] = v;
+    if (runs > 1) {
+      sh[threadIdx.x] = v;
       __syncthreads();
-      v = (sh[0][lane] + sh[1][lane]) + (sh[2][lane] + sh[3][lane]);
+      v = 0.f;
+      if (run == 0)
+        for (int k = 0; k < runs; ++k) v += sh[k * cols + lane];
       __syncthreads();
     }
-    if (o >= s.L || (run && !s.wide)) continue;
+    if (o >= s.L || run) continue;
     if (s.add) v += s.acc[o];
     if (s.acc) s.acc[o] = v;
     if (s.out) {
@@ -649,8 +660,8 @@ namespace grad {
 
 void SumList::add(const SumJob& j) {
   SumJob& s = a.job[a.n] = j;
-  s.wide = j.S <= 16 && j.L >= 4096;
-  a.first[a.n + 1] = a.first[a.n] + (s.wide ? (j.L + 255) / 256 : (j.L + 63) / 64);
+  s.cols_log2 = j.S <= 16 && j.L >= 4096 ? 8 : j.S <= 64 ? 6 : 4;
+  a.first[a.n + 1] = a.first[a.n] + ((j.L + (1l << s.cols_log2) - 1) >> s.cols_log2);
   ++a.n;
 }
 
@@ -721,12 +732,12 @@ GradPlan plan_grad(const DevProb& pr) {
   const int st = f.slab / dm.TI, nqb = (pr.B + dm.QB - 1) / dm.QB;
   dm.qsplits = std::max(1, std::min(nqb, 256 / st));
   f.wgs = st * dm.qsplits;
-  constexpr int KCH = 64 / sizeof(T);
+  constexpr int KCH = 64 / sizeof(T), kLeast = 128 / KCH;   // 128 items or query vectors
   f.ldq = padded_row(dm.m);
   f.ldx = padded_row(f.slab);
   const long cg = (pr.d + 63) / 64;
-  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * f.slab / KCH, 2);
-  f.sp_x = split_of((f.slab + 31l) / 32 * cg * pr.Px, (dm.m + 31) / 32 * 32 / KCH, 2);
+  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * f.slab / KCH, kLeast);
+  f.sp_x = split_of((f.slab + 31l) / 32 * cg * pr.Px, (dm.m + 31) / 32 * 32 / KCH, kLeast);
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   size_t at = 0;
   const size_t P = pr.P, H = pr.H;
@@ -742,7 +753,7 @@ GradPlan plan_grad(const DevProb& pr) {
   f.off_db1 = at; at = up(at + 4ul * f.wgs * H);
   f.off_db2 = at; at = up(at + 4ul * f.wgs * P);
   f.off_pq = at;  at = up(at + 4ul * f.sp_q * dm.m * pr.d);
-  f.off_px = at;  at = up(at + 4ul * f.sp_x * pr.Px * static_cast<size_t>(f.slab) * pr.d);
+  f.off_px = at;  at = up(at + (f.sp_x > 1 ? 4ul * f.sp_x * pr.Px * static_cast<size_t>(f.slab) * pr.d : 0));
   f.a_daq = 0;
   f.a_dw1 = f.a_daq + static_cast<long>(pr.B) * P;
   f.a_dw2 = f.a_dw1 + static_cast<long>(H * P);
@@ -776,7 +787,7 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
                                      static_cast<int>(f.lds));
   if (e != hipSuccess) return e;
-  const int cg = (pr.d + 63) / 64;
+  const int cg = (pr.d + 63) / 64;   // column tiles
   SumList sums(st);
   for (int sl = 0; sl < f.slabs; ++sl) {
     const bool last = sl + 1 == f.slabs;
@@ -795,27 +806,31 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
     const long per_px = static_cast<long>(items) * pr.d;
     if (o.dQ || o.dX) {
       const int m = static_cast<int>(dm.m);
+      // a product of one split (of dQ: and one slab) is stored as the output's type
+      const bool dir_q = f.sp_q == 1 && f.slabs == 1, dir_x = f.sp_x == 1;
       const GemmDims gq{m, pr.d, f.slab, dm.m * f.slab, f.slab, f.slab, pr.Px, static_cast<long>(pr.d) * f.ldx, f.ldx,
-                        f.sp_q, 0, dm.m * pr.d};
-      const GemmDims gx{items, pr.d, f.slab, dm.m * f.slab, (m + 31) / 32 * 32, m, pr.Px, 0, f.ldq, f.sp_x, per_px,
-                        per_px * pr.Px};
-      auto launch = [&](auto kern, int zq, int zx) {
-        const unsigned x = std::max(zq ? (m + 127) / 128 : 0, zx ? (items + 127) / 128 : 0);
-        hipLaunchKernelGGL(kern, dim3(x, cg, zq + zx), dim3(256), 0, st, gq, gx, zq, parts.ds, xt, qt, F(f.off_pq),
-                           F(f.off_px));
+                        f.sp_q, 0, dm.m * pr.d, dir_q, Tiles{(m + 31) / 32, cg, f.sp_q}};
+      const GemmDims gx{items, pr.d, f.slab, dm.m * f.slab, (m + 31) / 32 * 32, m, pr.Px, 0, f.ldq, f.sp_x,
+                        dir_x ? static_cast<long>(pr.N) * pr.d : per_px, per_px * pr.Px, dir_x,
+                        Tiles{(items + 31) / 32, cg, f.sp_x * pr.Px}};
+      void* to_q = dir_q ? o.dQ : F(f.off_pq);
+      void* to_x = dir_x ? static_cast<T*>(o.dX) + static_cast<long>(dm.n0) * pr.d : static_cast<void*>(F(f.off_px));
+      auto launch = [&](auto kern, bool q, bool x) {
+        const long units = (q ? gq.tiles.count() : 0) + (x ? gx.tiles.count() : 0);
+        hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, st, gq, gx, parts.ds, xt, qt,
+                           to_q, to_x);
       };
-      const int zq = o.dQ ? f.sp_q : 0, zx = o.dX ? f.sp_x * pr.Px : 0;
-      if (zq && zx && products_together(4ul * pr.Px * dm.m * f.slab)) {
-        launch(&k_grad_products<T, kProductQ | kProductX>, zq, zx);
+      if (o.dQ && o.dX && products_together(4ul * pr.Px * dm.m * f.slab)) {
+        launch(&k_grad_products<T, kProductQ | kProductX>, true, true);
       } else {
-        if (zq) launch(&k_grad_products<T, kProductQ>, zq, 0);
-        if (zx) launch(&k_grad_products<T, kProductX>, 0, zx);
+        if (o.dQ) launch(&k_grad_products<T, kProductQ>, true, false);
+        if (o.dX) launch(&k_grad_products<T, kProductX>, false, true);
       }
     }
-    if (o.dQ)
+    if (o.dQ && (f.sp_q > 1 || f.slabs > 1))
       sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, f.slabs > 1 ? acc + f.a_dq : nullptr, sl > 0,
                 last ? o.dQ : nullptr, bf, dm.m * pr.d, dm.m * pr.d, 0});
-    if (o.dX)
+    if (o.dX && f.sp_x > 1)
       sums.add({F(f.off_px), per_px * pr.Px, per_px * pr.Px, f.sp_x, nullptr, 0, o.dX, bf, per_px,
                 static_cast<long>(pr.N) * pr.d, static_cast<long>(dm.n0) * pr.d});
     if (o.da_q)

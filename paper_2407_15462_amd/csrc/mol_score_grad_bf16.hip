@@ -621,15 +621,18 @@ struct GemmBf16 {
   int splits;
   int items;         // dX: rows that exist
   int ldb;           // elements of a row of X or Q transposed
+  int direct;        // one split: out is the output itself
+  long out_px;       // dX: elements between item components of out
+  grad::Tiles tiles;
 };
 
 // dQ[m][t] = sum over px and items of ds X; z: the split
-__device__ __forceinline__ void dq_tile(const GemmBf16& gd, int z, const uint32_t* __restrict__ ds,
-                                        const bf16_t* __restrict__ xt, float* __restrict__ out) {
+__device__ __forceinline__ void dq_tile(const GemmBf16& gd, uint32_t unit, const uint32_t* __restrict__ ds,
+                                        const bf16_t* __restrict__ xt, void* __restrict__ out) {
   constexpr int RB = 2, CB = 4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-  const int m0 = (blockIdx.x * 4 + wave) * 16 * RB, t0 = blockIdx.y * 16 * CB;
-  if (m0 >= gd.m) return;
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int3 at = grad::tile_of(gd.tiles, unit);
+  const int m0 = at.x * 16 * RB, t0 = at.y * 16 * CB, z = at.z;
   const int per = gd.nb / 2, chunks = per * gd.npx;  // a chunk: two blocks of items
   const int k0 = static_cast<int>(static_cast<long>(chunks) * z / gd.splits);
   const int k1 = static_cast<int>(static_cast<long>(chunks) * (z + 1) / gd.splits);
@@ -680,27 +683,18 @@ __device__ __forceinline__ void dq_tile(const GemmBf16& gd, int z, const uint32_
     fetch(v0, min(ch + 2, k1 - 1));
     if (ch + 1 < k1) use(v1);
   }
-  float* dst = out + static_cast<long>(z) * gd.m * gd.d;
-#pragma unroll
-  for (int r = 0; r < RB; ++r)
-#pragma unroll
-    for (int t = 0; t < CB; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int m = m0 + 16 * r + 4 * g + i, x = t0 + 16 * t + c;
-        if (m < gd.m && x < gd.d) dst[static_cast<long>(m) * gd.d + x] = acc[r][t][i];
-      }
+  grad::put_tile<bf16_t>(out, static_cast<long>(z) * gd.m * gd.d, m0, gd.m, t0, gd.d, gd.direct, acc);
 }
 
 // dX[px][n][t] = sum over (b, pq) of ds Q: rows of ds of a block of items, 32
 // at a time, through the wave's LDS and the transposing read
 // (z: px and split; sh: [block][32 rows][64 bytes] a wave)
-__device__ __forceinline__ void dx_tile(const GemmBf16& gd, int z, const uint32_t* __restrict__ ds,
-                                        const bf16_t* __restrict__ qt, float* __restrict__ out, uint4 (*sh)[256]) {
+__device__ __forceinline__ void dx_tile(const GemmBf16& gd, uint32_t unit, const uint32_t* __restrict__ ds,
+                                        const bf16_t* __restrict__ qt, void* __restrict__ out, uint4 (*sh)[256]) {
   constexpr int RB = 2, CB = 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-  const int blk0 = (blockIdx.x * 4 + wave) * RB, t0 = blockIdx.y * 16 * CB;
-  if (blk0 >= gd.nb) return;                                          // (no workgroup barrier below)
+  const int3 at = grad::tile_of(gd.tiles, unit);                            // (no workgroup barrier below)
+  const int blk0 = at.x * RB, t0 = at.y * 16 * CB, z = at.z;
   const int px = z / gd.splits, split = z - px * gd.splits;
   const int chunks = (gd.m + 31) / 32;
   const int k0 = static_cast<int>(static_cast<long>(chunks) * split / gd.splits);
@@ -755,31 +749,23 @@ __device__ __forceinline__ void dx_tile(const GemmBf16& gd, int z, const uint32_
     fetch(v0, min(ch + 2, k1 - 1));
     if (ch + 1 < k1) use(v1, ch + 1);
   }
-  const long per_px = static_cast<long>(gd.items) * gd.d;
-  float* dst = out + (static_cast<long>(split) * gd.npx + px) * per_px;
-#pragma unroll
-  for (int r = 0; r < RB; ++r)
-#pragma unroll
-    for (int t = 0; t < CB; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int m = 16 * (blk0 + r) + 4 * g + i, x = t0 + 16 * t + c;
-        if (m < gd.items && x < gd.d) dst[static_cast<long>(m) * gd.d + x] = acc[r][t][i];
-      }
+  grad::put_tile<bf16_t>(out, (static_cast<long>(split) * gd.npx + px) * gd.out_px, 16 * blk0, gd.items, t0, gd.d, gd.direct,
+                         acc);
 }
 
-// Both products, side by side (blockIdx.z < zq for dQ), or one.
+// Both products, side by side (the first tiles are dQ's), or one.
 template <int WHAT>
-__global__ __launch_bounds__(256) void k_grad_products_bf16(GemmBf16 q, GemmBf16 x, int zq,
-                                                            const uint32_t* __restrict__ ds,
+__global__ __launch_bounds__(256) void k_grad_products_bf16(GemmBf16 q, GemmBf16 x, const uint32_t* __restrict__ ds,
                                                             const bf16_t* __restrict__ xt,
-                                                            const bf16_t* __restrict__ qt, float* __restrict__ out_q,
-                                                            float* __restrict__ out_x) {
+                                                            const bf16_t* __restrict__ qt, void* __restrict__ out_q,
+                                                            void* __restrict__ out_x) {
+  const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t nq = WHAT & grad::kProductQ ? static_cast<uint32_t>(q.tiles.count()) : 0;
   if constexpr (WHAT & grad::kProductQ)
-    if (static_cast<int>(blockIdx.z) < zq) dq_tile(q, blockIdx.z, ds, xt, out_q);
+    if (unit < nq) dq_tile(q, unit, ds, xt, out_q);
   if constexpr (WHAT & grad::kProductX) {
     __shared__ __attribute__((aligned(16))) uint4 sh[4][256];
-    if (static_cast<int>(blockIdx.z) >= zq) dx_tile(x, blockIdx.z - zq, ds, qt, out_x, sh);
+    if (unit >= nq && unit - nq < static_cast<uint32_t>(x.tiles.count())) dx_tile(x, unit - nq, ds, qt, out_x, sh);
   }
 }
 
@@ -815,8 +801,8 @@ Bf16Plan plan(const DevProb& pr) {
   f.ldq = padded_row(dm.m);
   f.ldx = padded_row(f.slab);
   const long cg = (pr.d + 63) / 64;
-  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * dm.nb / 2, 2);
-  f.sp_x = split_of(static_cast<long>(dm.nb) / 2 * cg * pr.Px, (dm.m + 31) / 32, 2);
+  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * dm.nb / 2, 4);
+  f.sp_x = split_of(static_cast<long>(dm.nb) / 2 * cg * pr.Px, (dm.m + 31) / 32, 4);
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   size_t at = 0;
   const size_t P = pr.P, H = pr.H;
@@ -830,7 +816,7 @@ Bf16Plan plan(const DevProb& pr) {
   f.off_db1 = at; at = up(at + 4ul * f.wgs * H);
   f.off_db2 = at; at = up(at + 4ul * f.wgs * P);
   f.off_pq = at;  at = up(at + 4ul * f.sp_q * dm.m * pr.d);
-  f.off_px = at;  at = up(at + 4ul * f.sp_x * pr.Px * f.slab * pr.d);
+  f.off_px = at;  at = up(at + (f.sp_x > 1 ? 4ul * f.sp_x * pr.Px * f.slab * pr.d : 0));
   f.a_dw1 = static_cast<long>(pr.B) * P;
   f.a_dw2 = f.a_dw1 + static_cast<long>(H * P);
   f.a_db1 = f.a_dw2 + static_cast<long>(H * P);
@@ -898,25 +884,30 @@ hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_gra
     if ((e = pairs(pr, f, dm, dphi, parts, st)) != hipSuccess) return e;
     const long per_px = static_cast<long>(dm.items) * pr.d;
     if (o.dQ || o.dX) {
-      const GemmBf16 gq{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_q, dm.items, f.ldx};
-      const GemmBf16 gx{static_cast<int>(dm.m), dm.nb, pr.d, pr.Px, f.sp_x, dm.items, f.ldq};
-      auto launch = [&](auto kern, int zq, int zx) {
-        const unsigned x = std::max<long>(zq ? (dm.m + 127) / 128 : 0, zx ? (dm.nb + 7) / 8 : 0);
-        hipLaunchKernelGGL(kern, dim3(x, cg, zq + zx), dim3(256), 0, st, gq, gx, zq, parts.ds, xt, qt, F(f.off_pq),
-                           F(f.off_px));
+      // a product of one split (of dQ: and one slab) is stored as bf16
+      const bool dir_q = f.sp_q == 1 && f.slabs == 1, dir_x = f.sp_x == 1;
+      const int m = static_cast<int>(dm.m);
+      const GemmBf16 gq{m, dm.nb, pr.d, pr.Px, f.sp_q, dm.items, f.ldx, dir_q, 0, Tiles{(m + 31) / 32, cg, f.sp_q}};
+      const GemmBf16 gx{m, dm.nb, pr.d, pr.Px, f.sp_x, dm.items, f.ldq, dir_x,
+                        dir_x ? static_cast<long>(pr.N) * pr.d : per_px, Tiles{(dm.nb + 1) / 2, cg, f.sp_x * pr.Px}};
+      void* to_q = dir_q ? o.dQ : F(f.off_pq);
+      void* to_x = dir_x ? static_cast<bf16_t*>(o.dX) + static_cast<long>(dm.n0) * pr.d : static_cast<void*>(F(f.off_px));
+      auto launch = [&](auto kern, bool q, bool x) {
+        const long units = (q ? gq.tiles.count() : 0) + (x ? gx.tiles.count() : 0);
+        hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, st, gq, gx, parts.ds, xt, qt,
+                           to_q, to_x);
       };
-      const int zq = o.dQ ? f.sp_q : 0, zx = o.dX ? f.sp_x * pr.Px : 0;
-      if (zq && zx && products_together(4ul * pr.Px * dm.m * f.slab)) {
-        launch(&k_grad_products_bf16<kProductQ | kProductX>, zq, zx);
+      if (o.dQ && o.dX && products_together(4ul * pr.Px * dm.m * f.slab)) {
+        launch(&k_grad_products_bf16<kProductQ | kProductX>, true, true);
       } else {
-        if (zq) launch(&k_grad_products_bf16<kProductQ>, zq, 0);
-        if (zx) launch(&k_grad_products_bf16<kProductX>, 0, zx);
+        if (o.dQ) launch(&k_grad_products_bf16<kProductQ>, true, false);
+        if (o.dX) launch(&k_grad_products_bf16<kProductX>, false, true);
       }
     }
-    if (o.dQ)
+    if (o.dQ && (f.sp_q > 1 || f.slabs > 1))
       sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, f.slabs > 1 ? acc + f.a_dq : nullptr, sl > 0,
                 last ? o.dQ : nullptr, 1, dm.m * pr.d, dm.m * pr.d, 0});
-    if (o.dX)
+    if (o.dX && f.sp_x > 1)
       sums.add({F(f.off_px), per_px * pr.Px, per_px * pr.Px, f.sp_x, nullptr, 0, o.dX, 1, per_px,
                 static_cast<long>(pr.N) * pr.d, static_cast<long>(dm.n0) * pr.d});
     if (o.da_q)
