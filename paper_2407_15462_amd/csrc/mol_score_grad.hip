@@ -409,25 +409,31 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims
     }
   }
 
-  // the workgroup's sums: waves in turn, in LDS, in the place of the rest
+  // the workgroup's sums in LDS, in the place of the rest: in round r wave w adds
+  // its eighth (w + r) % 8, so that every wave has work in each
   float* acc = smf;                                                    // [2][JTG][PT][64][4], then [JTG][16], then [TI][PV]
-  for (int w = 0; w < kWaves; ++w) {
+#pragma unroll 1
+  for (int r = 0; r < kWaves; ++r) {
+    const int part = (wave + r) & (kWaves - 1);
     __syncthreads();
-    if (wave == w) {
 #pragma unroll
-      for (int jj = 0; jj < JTG; ++jj) {
+    for (int jj = 0; jj < JTG; ++jj)
 #pragma unroll
-        for (int pt = 0; pt < PT; ++pt) {
+      for (int pt = 0; pt < PT; ++pt)
+        if (part == (jj * PT + pt) % kWaves) {
           f32x4_t* a = reinterpret_cast<f32x4_t*>(acc) + (jj * PT + pt) * 64 + lane;
           f32x4_t* b = a + JTG * PT * 64;
-          *a = w ? *a + aw1[jj][pt] : aw1[jj][pt];
-          *b = w ? *b + aw2[jj][pt] : aw2[jj][pt];
+          const f32x4_t a0 = *a, b0 = *b;
+          *a = r ? a0 + aw1[jj][pt] : aw1[jj][pt];
+          *b = r ? b0 + aw2[jj][pt] : aw2[jj][pt];
         }
+#pragma unroll
+    for (int jj = 0; jj < JTG; ++jj)
+      if (part == jj % kWaves) {
         const float t = sum_groups(ab1[jj]);
         float* o = acc + 2 * JTG * PT * 256 + 16 * jj + c;
-        if (g == 0) *o = w ? *o + t : t;
+        if (g == 0) *o = r ? *o + t : t;
       }
-    }
   }
   __syncthreads();
   for (int i = tid; i < JTG * PT * 256; i += kThreads) {
