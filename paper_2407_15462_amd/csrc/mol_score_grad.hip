@@ -183,12 +183,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims
   const T* X = static_cast<const T*>(pr.X);
   const T* Q = static_cast<const T*>(pr.Q);
 
-  if (!wglob)
-    for (int i = tid; i < 4 * wsize; i += kThreads) {
-      const int which = i / wsize, r = i - which * wsize, blk = r >> 8;
-      sW[i] = prepared<T, PV>(static_cast<const T*>(pr.W1), static_cast<const T*>(pr.W2), P, H, which, blk / PT,
-                              blk % PT, (r >> 2) & 63, r & 3);
-    }
+  if (!wglob) {
+#pragma unroll
+    for (int which = 0; which < 4; ++which)
+      for (int i = tid; i < wsize; i += kThreads) {
+        const int blk = i >> 8;
+        sW[which * wsize + i] = prepared<T, PV>(static_cast<const T*>(pr.W1), static_cast<const T*>(pr.W2), P, H, which,
+                                                blk / PT, blk % PT, (i >> 2) & 63, i & 3);
+      }
+  }
   for (int i = tid; i < 16 * JT; i += kThreads) sB1[i] = i < H ? pr.b1[i] : 0.f;
   for (int i = tid; i < QB * PV * TIP; i += kThreads) sS[i] = 0.f;
   for (int i = tid; i < PV; i += kThreads)
@@ -412,6 +415,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims
   // the workgroup's sums in LDS, in the place of the rest: in round r wave w adds
   // its eighth (w + r) % 8, so that every wave has work in each
   float* acc = smf;                                                    // [2][JTG][PT][64][4], then [JTG][16], then [TI][PV]
+#pragma unroll
+  for (int jj = 0; jj < JTG; ++jj) ab1[jj] = sum_groups(ab1[jj]);
 #pragma unroll 1
   for (int r = 0; r < kWaves; ++r) {
     const int part = (wave + r) & (kWaves - 1);
@@ -430,9 +435,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims
 #pragma unroll
     for (int jj = 0; jj < JTG; ++jj)
       if (part == jj % kWaves) {
-        const float t = sum_groups(ab1[jj]);
         float* o = acc + 2 * JTG * PT * 256 + 16 * jj + c;
-        if (g == 0) *o = r ? *o + t : t;
+        if (g == 0) *o = r ? *o + ab1[jj] : ab1[jj];
       }
   }
   __syncthreads();
