@@ -169,6 +169,7 @@ class Problem:
         self.B, self.N, self.Pq, self.Px, self.d, self.H = B, N, Pq, Px, d, H
         self.P = Pq * Px
         self.device = Q.device
+        self.checked = False                   # sizes and types, which only gradients look at
 
     @classmethod
     def from_inputs(cls, inp, flags: int = 0) -> "Problem":
@@ -443,7 +444,7 @@ def _on(device: torch.device, stream):
     that stream too, so that what the call allocates belongs to it."""
     if device.type != "cuda":
         raise ValueError(f"the operands are on {device}, not on a GPU")
-    if stream is None and device.index == torch.cuda.current_device():
+    if stream is None and device.index == torch._C._cuda_getDevice():   # (a GPU tensor exists: no set-up to wait for)
         return _HERE_NOW
     stack = contextlib.ExitStack()
     stack.enter_context(torch.cuda.device(device))
@@ -548,6 +549,19 @@ def softmax_loss(phi: torch.Tensor, target: torch.Tensor, ids: Optional[torch.Te
     return loss, dphi
 
 
+def _check_problem(prob: Problem) -> None:
+    """What the gradients rely on: every tensor of the sizes, type and device that Q, X and W1 imply."""
+    B, N, P, d, H, e = prob.B, prob.N, prob.P, prob.d, prob.H, prob.tensors[0].dtype
+    f32 = torch.float32
+    for name, t, n, dt in zip(("Q", "X", "a_q", "a_x", "W1", "b1", "W2", "b2"), prob.tensors,
+                              (B * prob.Pq * d, prob.Px * N * d, B * P, N * P, H * P, H, P * H, P),
+                              (e, e, f32, f32, e, f32, e, f32)):
+        _need(t.numel() == n, f"{name} has {t.numel()} elements, needs {n}")
+        _need(t.dtype == dt, f"{name} has dtype {t.dtype}, needs {dt}")
+        _need(t.device == prob.device, f"{name} is on {t.device}, needs {prob.device}")
+    prob.checked = True
+
+
 _GRADS = ("dQ", "dX", "da_q", "da_x", "dW1", "db1", "dW2", "db2")
 
 
@@ -561,6 +575,8 @@ def score_grad(prob: Problem, dphi: torch.Tensor, ws=None, stream=None, only: Op
     if not all(n in _GRADS for n in names):
         raise ValueError(f"unknown gradient in {names}: {', '.join(_GRADS)}")
     _need(all(t is not None for t in prob.tensors), "the problem lacks a gating tensor")
+    if not prob.checked:
+        _check_problem(prob)
     if out is not None and not set(out) <= set(names):
         raise ValueError(f"out holds {sorted(out)}, gradients are {', '.join(names)}")
     with _on(prob.device, stream):
@@ -604,43 +620,42 @@ class AdamwTensors:
             _need(x is None or len(x) == n, f"{name} has not the {n} entries of p")
         decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
         _need(len(decay) == n, f"weight_decay has not the {n} entries of p")
+        _need(all(isinstance(t, torch.Tensor) for t in p), "p must hold tensors")
         self.n, self.device = n, p[0].device if n else torch.device("cuda")
         self.c = (MolAdamwTensorC * max(n, 1))()
         self.tensors = (p, g, m, v, m_scale, v_scale, out)
+        dev, index = self.device, p[0].get_device() if n else 0
+
+        def at(t, name, i, shape, dtypes):             # (a plan of many tensors is made of thousands of these checks)
+            if not (isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == shape and t.get_device() == index and
+                    t.is_contiguous()):
+                _operand(t, f"{name}[{i}]", shape, dtypes, dev)
+            return t.data_ptr()
+
+        def new(name, i, shape, dtypes, old):          # where an output goes: in place unless out has it
+            return at(out[name][i], "out " + name, i, shape, dtypes) if name in out else old
+
+        f32, e4m3, bf16, copies = (torch.float32,), (torch.float8_e4m3fn,), (torch.bfloat16,), out.get("copy")
         offset = 0
-        for i in range(n):
-            _need(isinstance(p[i], torch.Tensor), "p must hold tensors")
-            shape, blocks = p[i].shape, (p[i].numel() + MOL_STATE_BLOCK - 1) // MOL_STATE_BLOCK
-            _operand(p[i], f"p[{i}]", shape, _FLOATS, self.device)
-            _operand(g[i], f"g[{i}]", shape, _FLOATS, self.device)
+        for i, t in enumerate(p):
+            shape, count = t.shape, t.numel()
+            blocks = (count + MOL_STATE_BLOCK - 1) // MOL_STATE_BLOCK
             eight = isinstance(m[i], torch.Tensor) and m[i].dtype == torch.float8_e4m3fn
-            state = torch.float8_e4m3fn if eight else torch.float32
-            e = self.c[i]
-            e.n, e.p, e.g, e.rng_offset, e.weight_decay = p[i].numel(), _ptr(p[i]), _ptr(g[i]), offset, decay[i]
-            e.param_dtype, e.grad_dtype = _dtype(p[i]), _dtype(g[i])
-            e.state = MOL_STATE_E4M3 if eight else MOL_STATE_F32
-            if "p" in out:
-                _operand(out["p"][i], f"out p[{i}]", shape, (p[i].dtype,), self.device)
-            e.p_out = _ptr(out["p"][i]) if "p" in out else e.p
-            if out.get("copy") is not None and out["copy"][i] is not None:
-                _operand(out["copy"][i], f"out copy[{i}]", shape, (torch.bfloat16,), self.device)
-                e.copy_out = _ptr(out["copy"][i])
-            for name, x in (("m", m), ("v", v)):
-                _operand(x[i], f"{name}[{i}]", shape, (state,), self.device)
-                if name in out:
-                    _operand(out[name][i], f"out {name}[{i}]", shape, (state,), self.device)
-                setattr(e, name, _ptr(x[i]))
-                setattr(e, name + "_out", _ptr(out[name][i]) if name in out else _ptr(x[i]))
-                if not eight:
-                    continue
-                scale, key = lists[name + "_scale"], name + "_scale"
-                _need(scale is not None, f"8-bit states need {key}")
-                _operand(scale[i], f"{key}[{i}]", (blocks,), (torch.float32,), self.device)
-                if key in out:
-                    _operand(out[key][i], f"out {key}[{i}]", (blocks,), (torch.float32,), self.device)
-                _need((key in out) == (name in out), f"outputs {name} and {key} go together")
-                setattr(e, key, _ptr(scale[i]))
-                setattr(e, key + "_out", _ptr(out[key][i]) if key in out else _ptr(scale[i]))
+            state = e4m3 if eight else f32
+            pp, gp = at(t, "p", i, shape, _FLOATS), at(g[i], "g", i, shape, _FLOATS)
+            mp, vp = at(m[i], "m", i, shape, state), at(v[i], "v", i, shape, state)
+            ms = vs = mso = vso = None
+            if eight:
+                _need(m_scale is not None and v_scale is not None, "8-bit states need m_scale and v_scale")
+                _need(("m" in out) == ("m_scale" in out) and ("v" in out) == ("v_scale" in out),
+                      "outputs m and m_scale, v and v_scale go together")
+                ms, vs = at(m_scale[i], "m_scale", i, (blocks,), f32), at(v_scale[i], "v_scale", i, (blocks,), f32)
+                mso, vso = new("m_scale", i, (blocks,), f32, ms), new("v_scale", i, (blocks,), f32, vs)
+            self.c[i] = MolAdamwTensorC(
+                count, pp, gp, mp, vp, ms, vs, new("p", i, shape, (t.dtype,), pp), new("m", i, shape, state, mp),
+                new("v", i, shape, state, vp), mso, vso,
+                None if copies is None or copies[i] is None else at(copies[i], "out copy", i, shape, bf16),
+                _DTYPES[t.dtype], _DTYPES[g[i].dtype], MOL_STATE_E4M3 if eight else MOL_STATE_F32, decay[i], offset)
             offset += blocks * MOL_STATE_BLOCK
 
 
@@ -710,13 +725,21 @@ class Learner:
         self.seed = seed
         self.shape = (Vq, V, Pq, Px, P, d)
 
-    def step(self, query_ids: torch.Tensor, item_ids: torch.Tensor, target: torch.Tensor, lr: torch.Tensor,
+    def step(self, query_ids: torch.Tensor, item_ids: torch.Tensor, target: torch.Tensor, lr,
              inv_temp: float = 20.0) -> torch.Tensor:
         """One optimisation step on B queries and N sampled items: query_ids int32
         [B], item_ids int32 [N] (negative: an empty slot), target int32 [B]: the
-        column of each query's positive; lr: one float32 on the GPU.  Returns the
-        losses [B] from before the step.  Allocates with torch and launches on the
-        current stream only: it can be captured into a graph."""
+        column of each query's positive; lr: a number, or one float32 on the GPU
+        (which a captured step reads when it runs).  Returns the losses [B] from
+        before the step.  Allocates with torch and launches on the current stream
+        only: it can be captured into a graph."""
+        if isinstance(lr, torch.Tensor):
+            _need(lr.numel() == 1, "lr must have one element")
+            _operand(lr, "lr", lr.shape, (torch.float32,), self.steps.device)   # (before anything is changed)
+        with _on(self.steps.device, None):
+            return self._step(query_ids, item_ids, target, lr, inv_temp)
+
+    def _step(self, query_ids, item_ids, target, lr, inv_temp) -> torch.Tensor:
         Vq, V, Pq, Px, P, d = self.shape
         B, N = query_ids.numel(), item_ids.numel()
         M, C, G = self.master, self.copy, self.grad

@@ -186,6 +186,22 @@ def test_binding_refuses_what_the_library_cannot_see():
             pytest.fail(f"call {k} was taken")
 
 
+def test_score_grad_refuses_a_problem_of_other_sizes():
+    B, N, Pq, Px, d, H = 3, 5, 2, 2, 8, 6
+    good = dict(Q=torch.zeros(B, Pq, d), X=torch.zeros(Px, N, d), a_q=torch.zeros(B, Pq * Px), a_x=torch.zeros(N, Pq * Px),
+                W1=torch.zeros(H, Pq * Px), b1=torch.zeros(H), W2=torch.zeros(Pq * Px, H), b2=torch.zeros(Pq * Px))
+    dphi = torch.zeros(B, N)
+    for name, t in (("X", torch.zeros(Px, N, d + 8)), ("a_q", torch.zeros(B, 3)), ("a_x", torch.zeros(N - 1, 4)),
+                    ("b1", torch.zeros(H + 1)), ("W2", torch.zeros(4, H - 1)), ("b2", torch.zeros(3)),
+                    ("a_x", torch.zeros(N, 4, dtype=torch.bfloat16)), ("W1", torch.zeros(H, 4, dtype=torch.bfloat16)),
+                    ("b2", None)):
+        prob = mol.Problem(**dict(good, **{name: t}))
+        with pytest.raises(ValueError):
+            mol.score_grad(prob, dphi)
+    with pytest.raises(ValueError, match="not on a GPU"):
+        mol.score_grad(mol.Problem(**good), dphi)
+
+
 # ---------------------------------------------------------------- the compiled kernels
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not available")
 def test_no_mfma_result_read_early(tmp_path):
