@@ -25,7 +25,7 @@
 //    k_grad_gemm forms dQ = sum ds X and dX = sum ds Q on matrix cores from it,
 //    with X and Q transposed once.
 // 3. k_sum_parts adds the partial sums in a fixed order.
-// Items are taken in slabs, so that ds stays within kSlabBytes.
+// Items are taken in slabs, so that ds and what else grows with them stay within kSlabBytes.
 //
 // What bounds it: the f32 matrix rate, 12 P H flop a pair (157 TFLOP/s).
 #include <algorithm>
@@ -40,7 +40,7 @@ using namespace grad;
 namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves, kPairs = 16 * kWaves;
-constexpr size_t kSlabBytes = size_t(256) << 20;   // of ds
+constexpr size_t kSlabBytes = size_t(256) << 20;   // of a slab's ds, X transposed and partial sums
 
 template <int PV>
 constexpr int group_tiles() { return PV == 64 ? 4 : 8; }   // JTG
@@ -732,7 +732,9 @@ GradPlan plan_grad(const DevProb& pr) {
   // the final sums take the same place: JTG blocks of dW1, dW2 and db1, then [TI][PV + 1] of da_x
   f.lds = std::max<size_t>(f.lds, 4 * (2ul * group_tiles<PV>() * (PV / 16) * 256 + 16 * group_tiles<PV>()));
   f.lds = std::max<size_t>(f.lds, 4ul * dm.TI * (PV + 1));
-  const long per_item = 4l * pr.Px * dm.m;
+  // of ds and X transposed, and of what a tile's workgroup leaves: dW1, dW2 and u
+  const long per_item = pr.Px * (4l * dm.m + static_cast<long>(sizeof(T)) * pr.d) +
+                        (8l * pr.H * pr.P + (f.ulds ? 0 : 1024l * kWaves * f.JT)) / dm.TI;
   const long tiles = (static_cast<long>(pr.N) + dm.TI - 1) / dm.TI;
   const long fit = std::max<long>(1, static_cast<long>(kSlabBytes) / (per_item * dm.TI));
   f.slabs = static_cast<int>((tiles + fit - 1) / fit);

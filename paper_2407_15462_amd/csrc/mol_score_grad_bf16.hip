@@ -38,7 +38,7 @@ using namespace tile;
 namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
-constexpr size_t kSlabBytes = size_t(256) << 20;   // of ds
+constexpr size_t kSlabBytes = size_t(256) << 20;   // of a slab's ds, X transposed and partial sums
 constexpr int kAhead = 2;                          // blocks of 32 of d loaded ahead
 constexpr int kJT = 4;                             // hidden tiles of 16
 constexpr int kH = 16 * kJT;
@@ -788,7 +788,9 @@ Bf16Plan plan(const DevProb& pr) {
   dm.QB = pr.B >= 8 ? 8 : pr.B >= 4 ? 4 : pr.B >= 2 ? 2 : 1;
   dm.m = static_cast<long>(pr.B) * pr.Pq;
   const long blocks = (pr.N + 31l) / 32;                              // slabs of whole pairs of 16 items
-  const long fit = std::max<long>(1, static_cast<long>(kSlabBytes) / (128l * pr.Px * dm.m));
+  // of ds and X transposed, and of a workgroup's dW1 and dW2
+  const long per_item = pr.Px * (4l * dm.m + 2l * pr.d) + 8l * pr.H * pr.P * dm.QB / (16 * kWaves);
+  const long fit = std::max<long>(1, static_cast<long>(kSlabBytes) / (32 * per_item));
   f.slabs = static_cast<int>((blocks + fit - 1) / fit);
   f.slab = static_cast<int>((blocks + f.slabs - 1) / f.slabs * 32);
   f.slabs = static_cast<int>((static_cast<long>(pr.N) + f.slab - 1) / f.slab);

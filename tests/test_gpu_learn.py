@@ -275,6 +275,30 @@ def test_score_grad_in_slabs():
         assert rel < (2.0 ** -8 if got[name].dtype == BF16 else 1e-5), (name, rel)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_score_grad_in_slabs_of_few_queries(dtype):
+    """Where X transposed is what fills a slab: B P_q of 6, rows of 1024 elements, two to four slabs."""
+    B, N, Pq, Px, d, H, part = 3, 200003, 2, 1, 1024, 16, 20000
+    log(f"[score_grad] B={B} N={N} P={Pq}x{Px} d={d} H={H} {NAME[dtype]}")
+    inputs, dphi = lh.mol_inputs(B, N, Pq, Px, d, H, dtype, seed=8, device="cuda")
+    got = mol.score_grad(mol.Problem(*inputs), dphi)
+    Q, X, a_q, a_x, W1, b1, W2, b2 = inputs
+    want = [torch.zeros_like(t, dtype=torch.float64) for t in inputs]
+    for n0 in range(0, N, part):
+        leaves = [t.double().clone().requires_grad_() for t in (Q, X[:, n0:n0 + part], a_q, a_x[n0:n0 + part], W1, b1, W2, b2)]
+        q, x, aq, ax, w1, c1, w2, c2 = leaves
+        s = torch.matmul(q.reshape(B * Pq, d), x[0].t()).view(B, Pq, -1).transpose(1, 2)
+        lg = torch.nn.functional.silu(s @ w1.t() + c1) @ w2.t() + c2 + aq[:, None] + ax[None]
+        phi = (torch.softmax(lg, -1) * s).sum(-1)
+        for k, gr in enumerate(torch.autograd.grad(phi, leaves, dphi[:, n0:n0 + part].double())):
+            (want[k][:, n0:n0 + part] if k == 1 else want[k][n0:n0 + part] if k == 3 else want[k]).add_(gr)
+    for name, w in zip(("dQ", "dX", "da_q", "da_x", "dW1", "db1", "dW2", "db2"), want):
+        rel = float((got[name].double() - w).norm() / w.norm())
+        # a bf16 rounding: 2^-8 / sqrt(3) at most; in float32 a pair's terms take about ten roundings (6e-7) and the
+        # sums, of 2000 terms in a chain at most, sqrt(2000) 2^-24 = 2.7e-6 more
+        assert rel < (2.0 ** -8 if got[name].dtype == BF16 else 1e-5), (name, rel)
+
+
 def test_score_grad_against_differences_of_the_oracle():
     inputs, dphi = lh.mol_inputs(4, 30, 4, 2, 24, 16, F32, seed=21)
     got = mol.score_grad(mol.Problem(*(t.cuda() for t in inputs)), dphi.cuda())

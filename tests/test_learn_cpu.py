@@ -119,6 +119,18 @@ def test_score_grad_workspace_is_bounded(B, N, Pq, Px, d, H):
     assert out.value < (256 << 20) + 4 * B * Pq * (40 * d + 64 * 32 + 3 * Px) + 16 * N * Px * d + (1 << 30)
 
 
+@pytest.mark.parametrize("B,N,Pq,Px,d,H", [(1, 1 << 28, 1, 1, 64, 256), (1, 1 << 27, 1, 1, 1024, 8), (1, 1 << 25, 1, 8, 256, 64),
+                                           (2, 1 << 24, 1, 64, 8, 256), (3, 1 << 28, 2, 2, 16, 16), (65535, 1 << 20, 8, 8, 64, 64)])
+@pytest.mark.parametrize("dtype", [mol.MOL_BF16, mol.MOL_F32])
+def test_score_grad_workspace_does_not_grow_with_the_corpus(B, N, Pq, Px, d, H, dtype):
+    """A few slabs' worth of buffers, and the sums of what the queries have, whatever the number of items."""
+    out = ctypes.c_size_t(0)
+    c = mol.MolProblemC(B, N, Pq, Px, d, H, dtype, *([FAKE] * 8))
+    assert mol.load().mol_workspace_size(ctypes.byref(c), mol.MOL_OP_SCORE_GRAD, 0, 0, 0, ctypes.byref(out)) == mol.MOL_OK
+    per_query = 4 * Pq * (d * 3 + 64) + 8 * Pq * Px
+    assert out.value < (1 << 30) + B * per_query + 64 * H * Pq * Px * 4 * 256
+
+
 def _tensor(**kw):
     t = mol.MolAdamwTensorC(100, *([FAKE] * 11), None, mol.MOL_F32, mol.MOL_BF16, mol.MOL_STATE_E4M3, 0.1, 0)
     for k, v in kw.items():
