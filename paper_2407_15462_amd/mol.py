@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 from typing import Dict, List, Optional, Sequence, Tuple
 
@@ -273,6 +274,7 @@ def mol_embed_grad(grad, ids, scale: float, accumulate: bool, table_grad, ws, st
                                  _stream(stream)))
 
 
+@functools.lru_cache(maxsize=256)              # (a call of its own costs a tenth of a small loss)
 def mol_softmax_loss_workspace(B: int, N: int) -> int:
     out = ctypes.c_size_t(0)
     _check(load().mol_softmax_loss_workspace(B, N, ctypes.byref(out)))
@@ -424,18 +426,19 @@ def _need(ok: bool, what: str) -> None:
 
 
 def _operand(t: torch.Tensor, name: str, shape, dtypes, device) -> None:
-    """Checks what the C ABI cannot see: shape, element type, device and layout."""
-    if (isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == shape and t.device == device and
-            t.is_contiguous()):
+    """Checks what the C ABI cannot see: shape (unless None), element type, device and layout."""
+    if (isinstance(t, torch.Tensor) and t.dtype in dtypes and (shape is None or t.shape == shape) and
+            t.device == device and t.is_contiguous()):
         return
     _need(isinstance(t, torch.Tensor), f"{name} must be a tensor")
-    _need(tuple(t.shape) == tuple(shape), f"{name} has shape {tuple(t.shape)}, needs {tuple(shape)}")
+    _need(shape is None or tuple(t.shape) == tuple(shape), f"{name} has shape {tuple(t.shape)}, needs {shape and tuple(shape)}")
     _need(t.dtype in dtypes, f"{name} has dtype {t.dtype}, needs {' or '.join(str(d) for d in dtypes)}")
     _need(t.device == device, f"{name} is on {t.device}, needs {device}")
     _need(t.is_contiguous(), f"{name} must be contiguous")
 
 
 _FLOATS = (torch.float32, torch.bfloat16)
+_F32, _INT32 = (torch.float32,), (torch.int32,)
 _HERE_NOW = contextlib.nullcontext()
 
 
@@ -472,18 +475,19 @@ def embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dty
     """
     _need(isinstance(table, torch.Tensor) and table.dim() == 3, "table must be a tensor [C][V][d]")
     _need(isinstance(ids, torch.Tensor) and ids.dim() == 1, "ids must be a tensor [T]")
-    C, V, d = table.shape
+    dev, (C, V, d), (T,) = table.device, table.shape, ids.shape
     dtype = (table.dtype if out is None else out.dtype) if dtype is None else dtype
     if dtype not in _FLOATS:
         raise ValueError(f"unsupported output dtype {dtype}")
-    _operand(table, "table", table.shape, _FLOATS, table.device)
-    _operand(ids, "ids", ids.shape, (torch.int32,), table.device)
-    with _on(table.device, stream):
+    _operand(table, "table", None, _FLOATS, dev)
+    _operand(ids, "ids", None, _INT32, dev)
+    with _on(dev, stream):
         if out is None:
-            out = torch.empty((C, ids.numel(), d), dtype=dtype, device=table.device)
+            out = table.new_empty((C, T, d), dtype=dtype)
         else:
-            _operand(out, "out", (C, ids.numel(), d), (dtype,), table.device)
-        mol_embed_lookup(table, ids, scale, out, stream)
+            _operand(out, "out", (C, T, d), (dtype,), dev)
+        _check(load().mol_embed_lookup(table.data_ptr(), _DTYPES[table.dtype], C, V, d, ids.data_ptr(), T, scale,
+                                       out.data_ptr(), _DTYPES[dtype], _stream(stream)))
     return out
 
 
@@ -503,18 +507,19 @@ def embed_grad(grad: torch.Tensor, ids: torch.Tensor, V: int, scale: float = 1.0
     """
     _need(isinstance(grad, torch.Tensor) and grad.dim() == 3, "grad must be a tensor [C][T][d]")
     C, T, d = grad.shape
-    _operand(grad, "grad", grad.shape, _FLOATS, grad.device)
-    _operand(ids, "ids", (T,), (torch.int32,), grad.device)
+    dev = grad.device
+    _operand(grad, "grad", None, _FLOATS, dev)
+    _operand(ids, "ids", (T,), _INT32, dev)
     _need(out is not None or not accumulate, "accumulate needs out")
     dtype = dtype if out is None else out.dtype
     if dtype not in _FLOATS:
         raise ValueError(f"unsupported output dtype {dtype}")
-    with _on(grad.device, stream):
-        ws = _workspace(lambda: mol_embed_grad_workspace(C, V, d, T), ws, grad.device)
+    with _on(dev, stream):
+        ws = _workspace(lambda: mol_embed_grad_workspace(C, V, d, T), ws, dev)
         if out is None:
-            out = torch.empty((C, V, d), dtype=dtype, device=grad.device)
+            out = grad.new_empty((C, V, d), dtype=dtype)
         else:
-            _operand(out, "out", (C, V, d), (dtype,), grad.device)
+            _operand(out, "out", (C, V, d), (dtype,), dev)
         mol_embed_grad(grad, ids, scale, accumulate, out, ws, stream)
     return out
 
@@ -532,20 +537,23 @@ def softmax_loss(phi: torch.Tensor, target: torch.Tensor, ids: Optional[torch.Te
     _need(isinstance(phi, torch.Tensor) and phi.dim() == 2, "phi must be a tensor [B][N]")
     B, N = phi.shape
     dev = phi.device
-    _operand(phi, "phi", (B, N), (torch.float32,), dev)
-    _operand(target, "target", (B,), (torch.int32,), dev)
+    _operand(phi, "phi", None, _F32, dev)
+    _operand(target, "target", (B,), _INT32, dev)
     if ids is not None:
-        _operand(ids, "ids", (N,), (torch.int32,), dev)
+        _operand(ids, "ids", (N,), _INT32, dev)
     if row_weight is not None:
-        _operand(row_weight, "row_weight", (B,), (torch.float32,), dev)
+        _operand(row_weight, "row_weight", (B,), _F32, dev)
     if dphi is not None:
-        _operand(dphi, "dphi", (B, N), (torch.float32,), dev)
+        _operand(dphi, "dphi", (B, N), _F32, dev)
     with _on(dev, stream):
         ws = _workspace(lambda: mol_softmax_loss_workspace(B, N), ws, dev)
-        loss = torch.empty((B,), dtype=torch.float32, device=dev)
+        loss = phi.new_empty((B,))
         if dphi is None:
-            dphi = torch.empty((B, N), dtype=torch.float32, device=dev)
-        mol_softmax_loss(phi, target, ids, inv_temp, row_weight, loss, dphi, ws, stream)
+            dphi = phi.new_empty((B, N))
+        _check(load().mol_softmax_loss(
+            B, N, phi.data_ptr(), target.data_ptr(), None if ids is None else ids.data_ptr(), inv_temp,
+            None if row_weight is None else row_weight.data_ptr(), loss.data_ptr(), dphi.data_ptr(),
+            None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream(stream)))
     return loss, dphi
 
 
@@ -553,6 +561,7 @@ def _check_problem(prob: Problem) -> None:
     """What the gradients rely on: every tensor of the sizes, type and device that Q, X and W1 imply."""
     B, N, P, d, H, e = prob.B, prob.N, prob.P, prob.d, prob.H, prob.tensors[0].dtype
     f32 = torch.float32
+    _need(all(t is not None for t in prob.tensors), "the problem lacks a gating tensor")
     for name, t, n, dt in zip(("Q", "X", "a_q", "a_x", "W1", "b1", "W2", "b2"), prob.tensors,
                               (B * prob.Pq * d, prob.Px * N * d, B * P, N * P, H * P, H, P * H, P),
                               (e, e, f32, f32, e, f32, e, f32)):
@@ -572,16 +581,15 @@ def score_grad(prob: Problem, dphi: torch.Tensor, ws=None, stream=None, only: Op
     each of its tensor's shape and type.  out: tensors to write some of them to."""
     _operand(dphi, "dphi", (prob.B, prob.N), (torch.float32,), prob.device)
     names = _GRADS if only is None else tuple(only)
-    if not all(n in _GRADS for n in names):
+    if only is not None and not all(n in _GRADS for n in names):
         raise ValueError(f"unknown gradient in {names}: {', '.join(_GRADS)}")
-    _need(all(t is not None for t in prob.tensors), "the problem lacks a gating tensor")
     if not prob.checked:
         _check_problem(prob)
     if out is not None and not set(out) <= set(names):
         raise ValueError(f"out holds {sorted(out)}, gradients are {', '.join(names)}")
     with _on(prob.device, stream):
         ws = _workspace(lambda: mol_workspace_size(prob, MOL_OP_SCORE_GRAD), ws, prob.device)
-        got = {}
+        got, c = {}, MolScoreGradsC()
         for g, t in zip(_GRADS, prob.tensors):
             if g not in names:
                 continue
@@ -590,7 +598,9 @@ def score_grad(prob: Problem, dphi: torch.Tensor, ws=None, stream=None, only: Op
                 got[g] = out[g]
             else:
                 got[g] = torch.empty_like(t)
-        mol_score_grad(prob, dphi, got, ws, stream)
+            setattr(c, g, got[g].data_ptr())
+        _check(load().mol_score_grad(prob.ref, dphi.data_ptr(), ctypes.byref(c), None if ws is None else ws.data_ptr(),
+                                     0 if ws is None else ws.numel(), _stream(stream)))
     return got
 
 
