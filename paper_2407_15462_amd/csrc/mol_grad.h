@@ -58,11 +58,11 @@ inline bool products_together(size_t ds_bytes) { return ds_bytes <= (size_t(64) 
 // all in the same channels of the L2 cache.
 inline int padded_row(long n) { return static_cast<int>((n + 31) / 32 * 32 + 64); }
 
-// K splits of a product of `waves` waves a part with `chunks` K chunks: 2048 waves
-// in all at most, with two chunks a split up to 64 splits (a short product is a chain of
+// K splits of a product of `waves` waves a part with `chunks` K chunks: about 2048
+// waves in all, with two chunks a split up to 64 splits (a short product is a chain of
 // latencies) and `least` beyond (each split is a part to write and to add).
 inline int split_of(long waves, long chunks, long least) {
-  const long want = 2048 / waves;
+  const long want = (2048 + waves / 2) / waves;
   long most = chunks / 2 < 64 ? chunks / 2 : 64;
   if (chunks / least > most) most = chunks / least;
   const long n = want < most ? want : most;

@@ -40,7 +40,9 @@ using namespace grad;
 namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves, kPairs = 16 * kWaves;
-constexpr size_t kSlabBytes = size_t(256) << 20;   // of a slab's ds, X transposed and partial sums
+// Of a slab's ds, X transposed and partial sums: a million pairs of 64 components, whose
+// ds alone is 268 MB (in bf16 at 1024 x 2048 pairs: two such slabs 848 us, three of 187 MB 930 us).
+constexpr size_t kSlabBytes = size_t(288) << 20;
 
 template <int PV>
 constexpr int group_tiles() { return PV == 64 ? 4 : 8; }   // JTG
@@ -670,7 +672,7 @@ namespace grad {
 
 void SumList::add(const SumJob& j) {
   SumJob& s = a.job[a.n] = j;
-  s.cols_log2 = j.S <= 16 && j.L >= 4096 ? 8 : j.S <= 64 ? 6 : 4;
+  s.cols_log2 = j.S <= 16 && j.L >= 4096 ? 8 : j.S <= 128 ? 6 : 4;
   a.first[a.n + 1] = a.first[a.n] + ((j.L + (1l << s.cols_log2) - 1) >> s.cols_log2);
   ++a.n;
 }

@@ -38,7 +38,9 @@ using namespace tile;
 namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
-constexpr size_t kSlabBytes = size_t(256) << 20;   // of a slab's ds, X transposed and partial sums
+// Of a slab's ds, X transposed and partial sums: a million pairs of 64 components, whose
+// ds alone is 268 MB (in bf16 at 1024 x 2048 pairs: two such slabs 848 us, three of 187 MB 930 us).
+constexpr size_t kSlabBytes = size_t(288) << 20;
 constexpr int kAhead = 2;                          // blocks of 32 of d loaded ahead
 constexpr int kJT = 4;                             // hidden tiles of 16
 constexpr int kH = 16 * kJT;
