@@ -38,7 +38,7 @@ using namespace tile;
 namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
-// Of a slab's ds, X transposed and partial sums: a million pairs of 64 components, whose
+// Of a slab's ds and partial sums: a million pairs of 64 components, whose
 // ds alone is 268 MB (in bf16 at 1024 x 2048 pairs: two such slabs 848 us, three of 187 MB 930 us).
 constexpr size_t kSlabBytes = size_t(288) << 20;
 constexpr int kAhead = 2;                          // blocks of 32 of d loaded ahead
@@ -618,19 +618,62 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
 
 // ---------------------------------------------------------------------------
 // dQ and dX on matrix cores from ds: 32 rows and 64 columns a wave, K split.
+// The rows of X and Q are the products' K: a chunk of 32 of them, 64 columns wide,
+// goes through the wave's LDS and the transposing read.
 struct GemmBf16 {
   int m, nb, d, npx;
   int splits;
-  int items;         // dX: rows that exist
-  int ldb;           // elements of a row of X or Q transposed
+  int items;         // of the slab: rows of X (dQ), rows of the output (dX)
+  long x_px;         // dQ: elements between item components of X
   int direct;        // one split: out is the output itself
   long out_px;       // dX: elements between item components of out
   grad::Tiles tiles;
 };
+constexpr int kRowB = 9;                             // 16-byte words of an LDS row of 64 columns (144 bytes: spread over the banks)
+constexpr int kTileB = 32 * kRowB, kTileA = 256;     // of a wave's chunk of X or Q, and of ds
+
+// Lane l of a wave has piece l % 8 (8 columns) of rows l / 8 + 8 j of a chunk.
+template <bool VEC>
+struct RowTile {
+  int rows, d, row, col;
+  __device__ __forceinline__ RowTile(int rows_, int d_, int t0) : rows(rows_), d(d_) {
+    const int lane = threadIdx.x & 63;
+    row = lane >> 3;
+    col = min(t0 + 8 * (lane & 7), VEC ? d - 8 : d - 1);   // (past d: others, for products that are not stored)
+  }
+  __device__ __forceinline__ void fetch(uint4 (&v)[4], const bf16_t* base, int k0) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bf16_t* p = base + static_cast<uint32_t>(min(k0 + 8 * j + row, rows - 1) * d + col);   // (N d < 2^31)
+      if constexpr (VEC) {
+        v[j] = *reinterpret_cast<const uint4*>(p);
+      } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w[e] = p[min(2 * e, d - 1 - col)] | static_cast<uint32_t>(p[min(2 * e + 1, d - 1 - col)]) << 16;
+        v[j] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+  // (rows past the end: zeros, as ds is there)
+  __device__ __forceinline__ void put(const uint4 (&v)[4], uint4* sh, int k0) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      sh[(8 * j + row) * kRowB + (threadIdx.x & 7)] = k0 + 8 * j + row < rows ? v[j] : make_uint4(0, 0, 0, 0);
+  }
+};
+// column 16 t + c of the chunk, K slots 8 g ..
+__device__ __forceinline__ uint4 column_of(const uint4* sh, int t, int c, int g) {
+  const unsigned char* p = reinterpret_cast<const unsigned char*>(sh) + (8 * g + (c >> 2)) * (16 * kRowB) + 8 * (c & 3) + 32 * t;
+  const uint2 a = read_tr(p), b = read_tr(p + 4 * 16 * kRowB);
+  return make_uint4(a.x, a.y, b.x, b.y);
+}
 
 // dQ[m][t] = sum over px and items of ds X; z: the split
+template <bool VEC>
 __device__ __forceinline__ void dq_tile(const GemmBf16& gd, uint32_t unit, const uint32_t* __restrict__ ds,
-                                        const bf16_t* __restrict__ xt, void* __restrict__ out) {
+                                        const bf16_t* __restrict__ X, void* __restrict__ out, uint4* sh) {
   constexpr int RB = 2, CB = 4;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int3 at = grad::tile_of(gd.tiles, unit);
@@ -643,12 +686,10 @@ __device__ __forceinline__ void dq_tile(const GemmBf16& gd, uint32_t unit, const
   // the halves of the wave are then swapped to first terms (items 8 g .. of the
   // chunk) and second terms.
   const uint32_t* a[RB];
-  const bf16_t* bt[CB];
 #pragma unroll
   for (int r = 0; r < RB; ++r) a[r] = ds + static_cast<long>(min(m0 + 16 * r + c, gd.m - 1)) * 16 + 4 * g;
-#pragma unroll
-  for (int t = 0; t < CB; ++t) bt[t] = xt + static_cast<long>(min(t0 + 16 * t + c, gd.d - 1)) * gd.ldb + 8 * g;
-  const long a_blk = 16l * gd.m, x_px = static_cast<long>(gd.d) * gd.ldb;
+  const RowTile<VEC> rows(gd.items, gd.d, t0);
+  const long a_blk = 16l * gd.m;
   struct Chunk {
     uint4 a[RB][2], b[CB];
   };
@@ -658,10 +699,14 @@ __device__ __forceinline__ void dq_tile(const GemmBf16& gd, uint32_t unit, const
     for (int r = 0; r < RB; ++r)
 #pragma unroll
       for (int e = 0; e < 2; ++e) v.a[r][e] = *reinterpret_cast<const uint4*>(a[r] + (2l * ch + e) * a_blk);
-#pragma unroll
-    for (int t = 0; t < CB; ++t) v.b[t] = *reinterpret_cast<const uint4*>(bt[t] + px * x_px + 32 * k);
+    rows.fetch(v.b, X + px * gd.x_px, 32 * k);
   };
-  auto use = [&](const Chunk& v) {
+  auto use = [&](const Chunk& v, int ch) {
+    rows.put(v.b, sh, 32 * (ch % per));
+    wave_lds_sync();
+    uint4 bv[CB];
+#pragma unroll
+    for (int t = 0; t < CB; ++t) bv[t] = column_of(sh, t, c, g);
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
       const uint4 x = v.a[r][0], y = v.a[r][1];
@@ -671,31 +716,33 @@ __device__ __forceinline__ void dq_tile(const GemmBf16& gd, uint32_t unit, const
       const auto p3 = __builtin_amdgcn_permlane32_swap(x.w, y.w, false, false);
       const uint4 h = make_uint4(p0[0], p1[0], p2[0], p3[0]), l = make_uint4(p0[1], p1[1], p2[1], p3[1]);
 #pragma unroll
-      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(l, v.b[t], acc[r][t]);
+      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(l, bv[t], acc[r][t]);
 #pragma unroll
-      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(h, v.b[t], acc[r][t]);
+      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(h, bv[t], acc[r][t]);
     }
+    wave_lds_sync();
   };
   // (two sets of registers in turn: copies of one would wait for its loads)
   Chunk v0, v1;
   if (k0 < k1) fetch(v0, k0);
   for (int ch = k0; ch < k1; ch += 2) {
     fetch(v1, min(ch + 1, k1 - 1));
-    use(v0);
+    use(v0, ch);
     fetch(v0, min(ch + 2, k1 - 1));
-    if (ch + 1 < k1) use(v1);
+    if (ch + 1 < k1) use(v1, ch + 1);
   }
   grad::put_tile<bf16_t>(out, static_cast<long>(z) * gd.m * gd.d, m0, gd.m, t0, gd.d, gd.direct, acc);
 }
 
 // dX[px][n][t] = sum over (b, pq) of ds Q: rows of ds of a block of items, 32
-// at a time, through the wave's LDS and the transposing read
-// (z: px and split; sh: [block][32 rows][64 bytes] a wave)
+// at a time, through the wave's LDS and the transposing read as well
+// (z: px and split; sh: [block][32 rows][64 bytes], then the rows of Q)
+template <bool VEC>
 __device__ __forceinline__ void dx_tile(const GemmBf16& gd, uint32_t unit, const uint32_t* __restrict__ ds,
-                                        const bf16_t* __restrict__ qt, void* __restrict__ out, uint4 (*sh)[256]) {
+                                        const bf16_t* __restrict__ Q, void* __restrict__ out, uint4* sh) {
   constexpr int RB = 2, CB = 4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-  const int3 at = grad::tile_of(gd.tiles, unit);                            // (no workgroup barrier below)
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int3 at = grad::tile_of(gd.tiles, unit);                      // (no workgroup barrier below)
   const int blk0 = at.x * RB, t0 = at.y * 16 * CB, z = at.z;
   const int px = z / gd.splits, split = z - px * gd.splits;
   const int chunks = (gd.m + 31) / 32;
@@ -703,12 +750,10 @@ __device__ __forceinline__ void dx_tile(const GemmBf16& gd, uint32_t unit, const
   const int k1 = static_cast<int>(static_cast<long>(chunks) * (split + 1) / gd.splits);
   f32x4_t acc[RB][CB] = {};
   const uint4* a[RB];
-  const bf16_t* bt[CB];
 #pragma unroll
   for (int r = 0; r < RB; ++r)
     a[r] = reinterpret_cast<const uint4*>(ds + (static_cast<long>(px) * gd.nb + min(blk0 + r, gd.nb - 1)) * gd.m * 16);
-#pragma unroll
-  for (int t = 0; t < CB; ++t) bt[t] = qt + static_cast<long>(min(t0 + 16 * t + c, gd.d - 1)) * gd.ldb + 8 * g;
+  const RowTile<VEC> rows(gd.m, gd.d, t0);
   struct Chunk {
     uint4 a[RB][2], b[CB];
   };
@@ -718,28 +763,30 @@ __device__ __forceinline__ void dx_tile(const GemmBf16& gd, uint32_t unit, const
     for (int r = 0; r < RB; ++r)
 #pragma unroll
       for (int e = 0; e < 2; ++e) v.a[r][e] = a[r][min(ch * 128l + e * 64 + lane, last)];
-#pragma unroll
-    for (int t = 0; t < CB; ++t) v.b[t] = *reinterpret_cast<const uint4*>(bt[t] + 32 * ch);
+    rows.fetch(v.b, Q, 32 * ch);
   };
-  const unsigned char* mine = reinterpret_cast<const unsigned char*>(sh[wave]);
   // K slots 8 g + e: rows 8 g + e
-  const int tr = (8 * g + (c >> 2)) * 64 + 8 * (c & 3);
+  const unsigned char* mine = reinterpret_cast<const unsigned char*>(sh) + (8 * g + (c >> 2)) * 64 + 8 * (c & 3);
   auto use = [&](const Chunk& v, int ch) {
 #pragma unroll
     for (int r = 0; r < RB; ++r)
 #pragma unroll
       for (int e = 0; e < 2; ++e)                                     // (rows past b pq: zeros, as Q's are)
-        sh[wave][r * 128 + e * 64 + lane] = ch * 128l + e * 64 + lane <= last ? v.a[r][e] : make_uint4(0, 0, 0, 0);
+        sh[r * 128 + e * 64 + lane] = ch * 128l + e * 64 + lane <= last ? v.a[r][e] : make_uint4(0, 0, 0, 0);
+    rows.put(v.b, sh + kTileA, 32 * ch);
     wave_lds_sync();
+    uint4 bv[CB];
+#pragma unroll
+    for (int t = 0; t < CB; ++t) bv[t] = column_of(sh + kTileA, t, c, g);
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-      const unsigned char* p = mine + r * 2048 + tr;
+      const unsigned char* p = mine + r * 2048;
       const uint2 h0 = read_tr(p), h1 = read_tr(p + 256), l0 = read_tr(p + 32), l1 = read_tr(p + 288);
       const uint4 h = make_uint4(h0.x, h0.y, h1.x, h1.y), l = make_uint4(l0.x, l0.y, l1.x, l1.y);
 #pragma unroll
-      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(l, v.b[t], acc[r][t]);
+      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(l, bv[t], acc[r][t]);
 #pragma unroll
-      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(h, v.b[t], acc[r][t]);
+      for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(h, bv[t], acc[r][t]);
     }
     wave_lds_sync();
   };
@@ -756,19 +803,20 @@ __device__ __forceinline__ void dx_tile(const GemmBf16& gd, uint32_t unit, const
 }
 
 // Both products, side by side (the first tiles are dQ's), or one.
-template <int WHAT>
+// VEC: rows of X and Q of whole 16-byte words.
+template <int WHAT, bool VEC>
 __global__ __launch_bounds__(256) void k_grad_products_bf16(GemmBf16 q, GemmBf16 x, const uint32_t* __restrict__ ds,
-                                                            const bf16_t* __restrict__ xt,
-                                                            const bf16_t* __restrict__ qt, void* __restrict__ out_q,
-                                                            void* __restrict__ out_x) {
-  const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+                                                            const bf16_t* __restrict__ X, const bf16_t* __restrict__ Q,
+                                                            void* __restrict__ out_q, void* __restrict__ out_x) {
+  constexpr int words = kTileB + (WHAT & grad::kProductX ? kTileA : 0);
+  __shared__ __attribute__((aligned(16))) uint4 sh[4][words];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t unit = blockIdx.x * 4 + wave;
   const uint32_t nq = WHAT & grad::kProductQ ? static_cast<uint32_t>(q.tiles.count()) : 0;
   if constexpr (WHAT & grad::kProductQ)
-    if (unit < nq) dq_tile(q, unit, ds, xt, out_q);
-  if constexpr (WHAT & grad::kProductX) {
-    __shared__ __attribute__((aligned(16))) uint4 sh[4][256];
-    if (unit >= nq && unit - nq < static_cast<uint32_t>(x.tiles.count())) dx_tile(x, unit - nq, ds, qt, out_x, sh);
-  }
+    if (unit < nq) dq_tile<VEC>(q, unit, ds, X, out_q, sh[wave]);
+  if constexpr (WHAT & grad::kProductX)
+    if (unit >= nq && unit - nq < static_cast<uint32_t>(x.tiles.count())) dx_tile<VEC>(x, unit - nq, ds, Q, out_x, sh[wave]);
 }
 
 // ---------------------------------------------------------------------------
@@ -779,8 +827,8 @@ namespace {
 struct Bf16Plan {
   Bf16Dims dm;
   int slab, slabs, wgx, wgs;
-  int sp_q, sp_x, ldq, ldx;
-  size_t off_ds, off_xt, off_qt, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_db2, off_pq, off_px, off_acc, bytes;
+  int sp_q, sp_x;
+  size_t off_ds, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_db2, off_pq, off_px, off_acc, bytes;
   long a_dw1, a_dw2, a_db1, a_db2, a_dq;       // floats into the sums over slabs
 };
 
@@ -790,8 +838,8 @@ Bf16Plan plan(const DevProb& pr) {
   dm.QB = pr.B >= 8 ? 8 : pr.B >= 4 ? 4 : pr.B >= 2 ? 2 : 1;
   dm.m = static_cast<long>(pr.B) * pr.Pq;
   const long blocks = (pr.N + 31l) / 32;                              // slabs of whole pairs of 16 items
-  // of ds and X transposed, and of a workgroup's dW1 and dW2
-  const long per_item = pr.Px * (4l * dm.m + 2l * pr.d) + 8l * pr.H * pr.P * dm.QB / (16 * kWaves);
+  // of ds, and of a workgroup's dW1 and dW2
+  const long per_item = 4l * pr.Px * dm.m + 8l * pr.H * pr.P * dm.QB / (16 * kWaves);
   const long fit = std::max<long>(1, static_cast<long>(kSlabBytes) / (32 * per_item));
   f.slabs = static_cast<int>((blocks + fit - 1) / fit);
   f.slab = static_cast<int>((blocks + f.slabs - 1) / f.slabs * 32);
@@ -802,8 +850,6 @@ Bf16Plan plan(const DevProb& pr) {
   f.wgx = (dm.nb + per - 1) / per;
   dm.qsplits = std::max(1, std::min(steps, 256 / f.wgx));
   f.wgs = f.wgx * dm.qsplits;
-  f.ldq = padded_row(dm.m);
-  f.ldx = padded_row(f.slab);
   const long cg = (pr.d + 63) / 64;
   f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * dm.nb / 2, 4);
   f.sp_x = split_of(static_cast<long>(dm.nb) / 2 * cg * pr.Px, (dm.m + 31) / 32, 4);
@@ -811,8 +857,6 @@ Bf16Plan plan(const DevProb& pr) {
   size_t at = 0;
   const size_t P = pr.P, H = pr.H;
   f.off_ds = at;  at = up(at + 4ul * pr.Px * dm.m * f.slab);
-  f.off_xt = at;  at = up(at + 2ul * pr.Px * pr.d * f.ldx);
-  f.off_qt = at;  at = up(at + 2ul * pr.d * f.ldq);
   f.off_daq = at; at = up(at + 4ul * dm.nb * pr.B * P);
   f.off_dax = at; at = up(at + 4ul * dm.qsplits * f.slab * P);
   f.off_dw1 = at; at = up(at + 4ul * f.wgs * H * P);
@@ -871,8 +915,6 @@ hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_gra
   auto F = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
   const Bf16Parts parts{reinterpret_cast<uint32_t*>(ws + f.off_ds), F(f.off_daq), F(f.off_dax), F(f.off_dw1),
                         F(f.off_dw2), F(f.off_db1), F(f.off_db2)};
-  bf16_t* xt = reinterpret_cast<bf16_t*>(ws + f.off_xt);
-  bf16_t* qt = reinterpret_cast<bf16_t*>(ws + f.off_qt);
   float* acc = F(f.off_acc);
   auto pairs = pr.Pq <= 4 && pr.Px <= 4 ? &launch_pairs<1, 4> : pr.Px <= 4 ? &launch_pairs<2, 4> : &launch_pairs<2, 8>;
   const int cg = (pr.d + 63) / 64;
@@ -882,30 +924,31 @@ hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_gra
     const bool last = sl + 1 == f.slabs;
     dm.n0 = sl * f.slab;
     dm.items = std::min(f.slab, pr.N - dm.n0);
-    hipError_t e = launch_transposes<bf16_t>(pr, dm.m, f.ldq, o.dX && sl == 0 ? qt : nullptr, dm.n0, dm.items, f.ldx,
-                                             o.dQ ? xt : nullptr, st);
-    if (e != hipSuccess) return e;
+    hipError_t e;
     if ((e = pairs(pr, f, dm, dphi, parts, st)) != hipSuccess) return e;
     const long per_px = static_cast<long>(dm.items) * pr.d;
     if (o.dQ || o.dX) {
       // a product of one split (of dQ: and one slab) is stored as bf16
       const bool dir_q = f.sp_q == 1 && f.slabs == 1, dir_x = f.sp_x == 1;
       const int m = static_cast<int>(dm.m);
-      const GemmBf16 gq{m, dm.nb, pr.d, pr.Px, f.sp_q, dm.items, f.ldx, dir_q, 0, Tiles{(m + 31) / 32, cg, f.sp_q}};
-      const GemmBf16 gx{m, dm.nb, pr.d, pr.Px, f.sp_x, dm.items, f.ldq, dir_x,
+      const GemmBf16 gq{m, dm.nb, pr.d, pr.Px, f.sp_q, dm.items, static_cast<long>(pr.N) * pr.d, dir_q, 0, Tiles{(m + 31) / 32, cg, f.sp_q}};
+      const GemmBf16 gx{m, dm.nb, pr.d, pr.Px, f.sp_x, dm.items, 0, dir_x,
                         dir_x ? static_cast<long>(pr.N) * pr.d : per_px, Tiles{(dm.nb + 1) / 2, cg, f.sp_x * pr.Px}};
       void* to_q = dir_q ? o.dQ : F(f.off_pq);
       void* to_x = dir_x ? static_cast<bf16_t*>(o.dX) + static_cast<long>(dm.n0) * pr.d : static_cast<void*>(F(f.off_px));
+      const bf16_t* X = static_cast<const bf16_t*>(pr.X) + static_cast<long>(dm.n0) * pr.d;
+      const bf16_t* Q = static_cast<const bf16_t*>(pr.Q);
+      const bool vec = pr.d % 8 == 0 && ((reinterpret_cast<uintptr_t>(pr.X) | reinterpret_cast<uintptr_t>(pr.Q)) & 15) == 0;
       auto launch = [&](auto kern, bool q, bool x) {
         const long units = (q ? gq.tiles.count() : 0) + (x ? gx.tiles.count() : 0);
-        hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, st, gq, gx, parts.ds, xt, qt,
-                           to_q, to_x);
+        hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, st, gq, gx, parts.ds, X, Q, to_q,
+                           to_x);
       };
       if (o.dQ && o.dX && products_together(4ul * pr.Px * dm.m * f.slab)) {
-        launch(&k_grad_products_bf16<kProductQ | kProductX>, true, true);
+        launch(vec ? &k_grad_products_bf16<kProductQ | kProductX, true> : &k_grad_products_bf16<kProductQ | kProductX, false>, true, true);
       } else {
-        if (o.dQ) launch(&k_grad_products_bf16<kProductQ>, true, false);
-        if (o.dX) launch(&k_grad_products_bf16<kProductX>, false, true);
+        if (o.dQ) launch(vec ? &k_grad_products_bf16<kProductQ, true> : &k_grad_products_bf16<kProductQ, false>, true, false);
+        if (o.dX) launch(vec ? &k_grad_products_bf16<kProductX, true> : &k_grad_products_bf16<kProductX, false>, false, true);
       }
     }
     if (o.dQ && (f.sp_q > 1 || f.slabs > 1))
