@@ -35,13 +35,6 @@ struct SumList {
   hipError_t run();
 };
 
-// Q [m][d] -> qt [d][ldq] (rows from m to ldq zero) where qt is not NULL, and items
-// [n0, n0 + items) of X [Px][N][d] -> xt [Px][d][ns] (zero from items to ns)
-// where xt is not NULL, one launch.
-template <typename T>
-hipError_t launch_transposes(const DevProb& pr, long m, int ldq, T* qt, int n0, int items, int ns, T* xt,
-                             hipStream_t st);
-
 // The bf16 form on 16-bit matrix instructions (mol_score_grad_bf16.hip).
 bool bf16_supported(const DevProb& pr);
 size_t bf16_bytes(const DevProb& pr);
@@ -52,11 +45,6 @@ hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_gra
 // part of what the first read in the last-level cache (268 MB: 77 + 60 us against 259).
 constexpr int kProductQ = 1, kProductX = 2;
 inline bool products_together(size_t ds_bytes) { return ds_bytes <= (size_t(64) << 20); }
-
-// Elements of a row of X or Q transposed: whole K blocks of 32, and 64 more, so that
-// the rows that a load takes together (powers of two apart otherwise) are not
-// all in the same channels of the L2 cache.
-inline int padded_row(long n) { return static_cast<int>((n + 31) / 32 * 32 + 64); }
 
 // K splits of a product of `waves` waves a part with `chunks` K chunks: about 2048
 // waves in all, with two chunks a split up to 64 splits (a short product is a chain of
@@ -102,6 +90,58 @@ struct Tiles {
 __device__ __forceinline__ int3 tile_of(const Tiles& t, uint32_t unit) {
   const uint32_t rest = unit / static_cast<uint32_t>(t.rows), z = rest / static_cast<uint32_t>(t.cols);
   return make_int3(unit - rest * t.rows, rest - z * t.cols, z);
+}
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+// The transposing read: each group of 16 lanes reads 4 rows of 16 elements (8
+// bytes a lane, rows lane / 4) and gets column lane, its 4 rows in order
+__device__ __forceinline__ uint2 read_tr(const void* lds) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                       (lds_s16x4_t*)(__attribute__((address_space(3))) const void*)lds));
+}
+
+// Rows of X or Q as the K of a bf16 product: a chunk of 32 of them, 64 columns wide.
+constexpr int kRowB = 9;                             // 16-byte words of an LDS row of 64 columns (144 bytes: spread over the banks)
+constexpr int kTileB = 32 * kRowB;                   // of a wave's chunk of X or Q
+
+// Lane l of a wave has piece l % 8 (8 columns) of rows l / 8 + 8 j of a chunk.
+template <bool VEC>
+struct RowTile {
+  int rows, d, row, col;
+  __device__ __forceinline__ RowTile(int rows_, int d_, int t0) : rows(rows_), d(d_) {
+    const int lane = threadIdx.x & 63;
+    row = lane >> 3;
+    col = min(t0 + 8 * (lane & 7), VEC ? d - 8 : d - 1);   // (past d: others, for products that are not stored)
+  }
+  __device__ __forceinline__ void fetch(uint4 (&v)[4], const bf16_t* base, int k0) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bf16_t* p = base + (static_cast<uint64_t>(min(k0 + 8 * j + row, rows - 1)) * static_cast<uint32_t>(d) + col);
+      if constexpr (VEC) {
+        v[j] = *reinterpret_cast<const uint4*>(p);
+      } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w[e] = p[min(2 * e, d - 1 - col)] | static_cast<uint32_t>(p[min(2 * e + 1, d - 1 - col)]) << 16;
+        v[j] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+  // (rows past the end: zeros, as ds is there)
+  __device__ __forceinline__ void put(const uint4 (&v)[4], uint4* sh, int k0) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      sh[(8 * j + row) * kRowB + (threadIdx.x & 7)] = k0 + 8 * j + row < rows ? v[j] : make_uint4(0, 0, 0, 0);
+  }
+};
+// column 16 t + c of the chunk, K slots 8 g ..
+__device__ __forceinline__ uint4 column_of(const uint4* sh, int t, int c, int g) {
+  const unsigned char* p = reinterpret_cast<const unsigned char*>(sh) + (8 * g + (c >> 2)) * (16 * kRowB) + 8 * (c & 3) + 32 * t;
+  const uint2 a = read_tr(p), b = read_tr(p + 4 * 16 * kRowB);
+  return make_uint4(a.x, a.y, b.x, b.y);
 }
 
 }  // namespace grad

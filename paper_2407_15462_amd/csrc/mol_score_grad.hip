@@ -22,8 +22,8 @@
 //    does da_x.  The workgroup's sums go to the workspace.
 // 2. ds goes there too, [Px][B Pq][items], as float32 or, for bf16 problems, as
 //    two bf16 terms (16 significant bits, more than dQ and dX keep), and
-//    k_grad_gemm forms dQ = sum ds X and dX = sum ds Q on matrix cores from it,
-//    with X and Q transposed once.
+//    k_grad_products forms dQ = sum ds X and dX = sum ds Q on matrix cores from it,
+//    with rows of X and Q as K, as they lie.
 // 3. k_sum_parts adds the partial sums in a fixed order.
 // Items are taken in slabs, so that ds and what else grows with them stay within kSlabBytes.
 //
@@ -40,7 +40,7 @@ using namespace grad;
 namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves, kPairs = 16 * kWaves;
-// Of a slab's ds, X transposed and partial sums: a million pairs of 64 components, whose
+// Of a slab's ds and partial sums: a million pairs of 64 components, whose
 // ds alone is 268 MB (in bf16 at 1024 x 2048 pairs: two such slabs 848 us, three of 187 MB 930 us).
 constexpr size_t kSlabBytes = size_t(288) << 20;
 
@@ -493,28 +493,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims
 }
 
 // ---------------------------------------------------------------------------
-// blockIdx.z < Px: item component blockIdx.z of X (none without xt); Px: Q.
-template <typename T>
-__global__ __launch_bounds__(256) void k_transpose(DevProb pr, long m, int ldq, T* __restrict__ qt, int n0, int items,
-                                                   int ns, T* __restrict__ xt) {
-  __shared__ T tile[32][33];
-  const bool is_q = static_cast<int>(blockIdx.z) == pr.Px;
-  const long rows = is_q ? m : items, r0 = static_cast<long>(blockIdx.x) * 32;
-  const int d = pr.d, ld = is_q ? ldq : ns, t0 = blockIdx.y * 32;
-  T* dst = is_q ? qt : xt ? xt + blockIdx.z * static_cast<long>(d) * ns : nullptr;
-  if (!dst || r0 >= ld) return;                                        // (the whole workgroup)
-  const T* src = is_q ? static_cast<const T*>(pr.Q) : static_cast<const T*>(pr.X) + (blockIdx.z * static_cast<long>(pr.N) + n0) * d;
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-  for (int k = y; k < 32; k += 8) {
-    T v = 0;
-    if (r0 + k < rows && t0 + x < d) v = src[(r0 + k) * d + t0 + x];
-    tile[k][x] = v;
-  }
-  __syncthreads();
-  for (int k = y; k < 32; k += 8)
-    if (t0 + k < d && r0 + x < ld) dst[static_cast<long>(t0 + k) * ld + r0 + x] = tile[x][k];
-}
-
 // Products with ds on matrix cores: out[m][t] = sum_k A[m][k] Bt[t][k].
 // COLS false (dQ): m = (b, pq), k = (px, item): A rows run along k.
 // COLS true (dX): one px a batch, m = item, k = (b, pq): A columns run along m.
@@ -524,18 +502,17 @@ struct GemmDims {
   int m, d;
   long lda;                // elements of a row of ds
   long a_px;               // elements between item components of ds
-  int k_px, kvalid;        // K of one px (padded), valid ones (COLS)
+  int k_px, kvalid;        // K of one px (padded), rows of X or Q that exist
   int npx;                 // px of the K loop (dQ) or of the batch (dX)
-  long b_px;               // elements between px of Bt (0: the same)
-  int ldb;
+  long b_px;               // elements between px of X (dQ)
   int splits;
   long out_px, out_split;  // elements between px (dX), between splits
   int direct;              // one split: out is the output itself
   Tiles tiles;
 };
-template <typename T, bool COLS>
+template <typename T, bool COLS, bool VEC>
 __device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, const uint32_t* __restrict__ ds,
-                                             const T* __restrict__ Bt, void* __restrict__ out) {
+                                             const T* __restrict__ rows, void* __restrict__ out, uint4* sh) {
   constexpr int E = 16 / sizeof(T), KCH = 4 * E, RB = 2, CB = 4;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int3 at = tile_of(gd.tiles, unit);
@@ -550,14 +527,14 @@ __device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, 
   for (int r = 0; r < RB; ++r) row[r] = min(m0 + 16 * r + c, gd.m - 1);
 #pragma unroll
   for (int t = 0; t < CB; ++t) col[t] = min(t0 + 16 * t + c, gd.d - 1);
+  const RowTile<VEC> rt(gd.kvalid, gd.d, t0);
   struct Chunk {
     uint32_t a[RB][E];
     uint4 b[CB];
   };
   auto fetch = [&](Chunk& v, int ch) {
-    const int px = COLS ? px0 : ch / per, k = (COLS ? ch : ch - px * per) * KCH + g * E;
+    const int px = COLS ? px0 : ch / per, kc = (COLS ? ch : ch - px * per) * KCH, k = kc + g * E;
     const uint32_t* A = ds + px * gd.a_px;
-    const T* B = Bt + px * gd.b_px + k;
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
       if constexpr (COLS) {
@@ -574,19 +551,44 @@ __device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, 
         }
       }
     }
+    const T* B = COLS ? rows : rows + px * gd.b_px;
+    if constexpr (sizeof(T) == 2) {
+      rt.fetch(v.b, B, kc);
+    } else {
+      // (four rows of 16 columns a load)
+      uint32_t w[CB][4];
 #pragma unroll
-    for (int t = 0; t < CB; ++t) v.b[t] = *reinterpret_cast<const uint4*>(B + static_cast<long>(col[t]) * gd.ldb);
+      for (int e = 0; e < 4; ++e) {
+        const float* p = B + static_cast<long>(min(k + e, gd.kvalid - 1)) * gd.d;
+#pragma unroll
+        for (int t = 0; t < CB; ++t) w[t][e] = __float_as_uint(p[col[t]]);
+      }
+#pragma unroll
+      for (int t = 0; t < CB; ++t) v.b[t] = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
+    }
   };
   auto use = [&](const Chunk& v, int ch) {
+    const int kc = (COLS ? ch : ch % per) * KCH, left = gd.kvalid - kc - g * E;   // rows past the end: zeros, as ds is there
+    uint4 bv[CB];
+    if constexpr (sizeof(T) == 2) {
+      rt.put(v.b, sh, kc);
+      wave_lds_sync();
+#pragma unroll
+      for (int t = 0; t < CB; ++t) bv[t] = column_of(sh, t, c, g);
+    } else {
+#pragma unroll
+      for (int t = 0; t < CB; ++t)
+        bv[t] = make_uint4(left > 0 ? v.b[t].x : 0, left > 1 ? v.b[t].y : 0, left > 2 ? v.b[t].z : 0, left > 3 ? v.b[t].w : 0);
+    }
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
       uint32_t a[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) a[e] = !COLS || ch * KCH + g * E + e < gd.kvalid ? v.a[r][e] : 0;
+      for (int e = 0; e < E; ++e) a[e] = !COLS || e < left ? v.a[r][e] : 0;
       if constexpr (sizeof(T) == 4) {
         const uint4 av = make_uint4(a[0], a[1], a[2], a[3]);
 #pragma unroll
-        for (int t = 0; t < CB; ++t) acc[r][t] = mma16<T>(av, v.b[t], acc[r][t]);
+        for (int t = 0; t < CB; ++t) acc[r][t] = mma16<T>(av, bv[t], acc[r][t]);
       } else {
         uint32_t hi[4], lo[4];
 #pragma unroll
@@ -596,11 +598,12 @@ __device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, 
         }
         const uint4 ah = make_uint4(hi[0], hi[1], hi[2], hi[3]), al = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 #pragma unroll
-        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(al, v.b[t], acc[r][t]);
+        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(al, bv[t], acc[r][t]);
 #pragma unroll
-        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(ah, v.b[t], acc[r][t]);
+        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(ah, bv[t], acc[r][t]);
       }
     }
+    if constexpr (sizeof(T) == 2) wave_lds_sync();                     // read before the next chunk is written
   };
   // (two sets of registers in turn: copies of one would wait for its loads)
   Chunk v0, v1;
@@ -616,16 +619,20 @@ __device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, 
 
 // ---------------------------------------------------------------------------
 // Both products, side by side (the first tiles are dQ's), or one.
-template <typename T, int WHAT>
+// VEC: rows of X and Q of whole 16-byte words (bf16).
+template <typename T, int WHAT, bool VEC>
 __global__ __launch_bounds__(256) void k_grad_products(GemmDims q, GemmDims x, const uint32_t* __restrict__ ds,
-                                                       const T* __restrict__ xt, const T* __restrict__ qt,
+                                                       const T* __restrict__ X, const T* __restrict__ Q,
                                                        void* __restrict__ out_q, void* __restrict__ out_x) {
-  const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ __attribute__((aligned(16))) uint4 sh[4][sizeof(T) == 2 ? kTileB : 1];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t unit = blockIdx.x * 4 + wave;
   const uint32_t nq = WHAT & kProductQ ? static_cast<uint32_t>(q.tiles.count()) : 0;
   if constexpr (WHAT & kProductQ)
-    if (unit < nq) product_tile<T, false>(q, unit, ds, xt, out_q);
+    if (unit < nq) product_tile<T, false, VEC>(q, unit, ds, X, out_q, sh[wave]);
   if constexpr (WHAT & kProductX)
-    if (unit >= nq && unit - nq < static_cast<uint32_t>(x.tiles.count())) product_tile<T, true>(x, unit - nq, ds, qt, out_x);
+    if (unit >= nq && unit - nq < static_cast<uint32_t>(x.tiles.count()))
+      product_tile<T, true, VEC>(x, unit - nq, ds, Q, out_x, sh[wave]);
 }
 
 // ---------------------------------------------------------------------------
@@ -685,18 +692,6 @@ hipError_t SumList::run() {
   return hipGetLastError();
 }
 
-template <typename T>
-hipError_t launch_transposes(const DevProb& pr, long m, int ldq, T* qt, int n0, int items, int ns, T* xt,
-                             hipStream_t st) {
-  if (!qt && !xt) return hipSuccess;
-  const long rows = std::max<long>(qt ? ldq : 0, xt ? ns : 0);
-  hipLaunchKernelGGL(k_transpose<T>, dim3(static_cast<unsigned>((rows + 31) / 32), (pr.d + 31) / 32, pr.Px + (qt ? 1 : 0)),
-                     dim3(256), 0, st, pr, m, ldq, qt, n0, items, ns, xt);
-  return hipGetLastError();
-}
-template hipError_t launch_transposes<bf16_t>(const DevProb&, long, int, bf16_t*, int, int, int, bf16_t*, hipStream_t);
-template hipError_t launch_transposes<float>(const DevProb&, long, int, float*, int, int, int, float*, hipStream_t);
-
 }  // namespace grad
 
 // ---------------------------------------------------------------------------
@@ -708,8 +703,8 @@ struct GradPlan {
   int JT, groups, slab, slabs;
   bool wlds, ulds;                      // prepared weights and the units' u in LDS
   size_t lds;
-  int sp_q, sp_x, ldq, ldx;             // K splits of dQ and dX, row lengths of Q and X transposed
-  size_t off_w, off_u, off_ds, off_xt, off_qt, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_db2, off_pq, off_px, off_acc, bytes;
+  int sp_q, sp_x;                       // K splits of dQ and dX
+  size_t off_w, off_u, off_ds, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_db2, off_pq, off_px, off_acc, bytes;
   long a_daq, a_dw1, a_dw2, a_db1, a_db2, a_dq;   // floats into the sums over slabs
   int wgs;
 };
@@ -734,9 +729,8 @@ GradPlan plan_grad(const DevProb& pr) {
   // the final sums take the same place: JTG blocks of dW1, dW2 and db1, then [TI][PV + 1] of da_x
   f.lds = std::max<size_t>(f.lds, 4 * (2ul * group_tiles<PV>() * (PV / 16) * 256 + 16 * group_tiles<PV>()));
   f.lds = std::max<size_t>(f.lds, 4ul * dm.TI * (PV + 1));
-  // of ds and X transposed, and of what a tile's workgroup leaves: dW1, dW2 and u
-  const long per_item = pr.Px * (4l * dm.m + static_cast<long>(sizeof(T)) * pr.d) +
-                        (8l * pr.H * pr.P + (f.ulds ? 0 : 1024l * kWaves * f.JT)) / dm.TI;
+  // of ds, and of what a tile's workgroup leaves: dW1, dW2 and u
+  const long per_item = 4l * pr.Px * dm.m + (8l * pr.H * pr.P + (f.ulds ? 0 : 1024l * kWaves * f.JT)) / dm.TI;
   const long tiles = (static_cast<long>(pr.N) + dm.TI - 1) / dm.TI;
   const long fit = std::max<long>(1, static_cast<long>(kSlabBytes) / (per_item * dm.TI));
   f.slabs = static_cast<int>((tiles + fit - 1) / fit);
@@ -747,8 +741,6 @@ GradPlan plan_grad(const DevProb& pr) {
   dm.qsplits = std::max(1, std::min(nqb, 256 / st));
   f.wgs = st * dm.qsplits;
   constexpr int KCH = 64 / sizeof(T), kLeast = 128 / KCH;   // 128 items or query vectors
-  f.ldq = padded_row(dm.m);
-  f.ldx = padded_row(f.slab);
   const long cg = (pr.d + 63) / 64;
   f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * f.slab / KCH, kLeast);
   f.sp_x = split_of((f.slab + 31l) / 32 * cg * pr.Px, (dm.m + 31) / 32 * 32 / KCH, kLeast);
@@ -758,8 +750,6 @@ GradPlan plan_grad(const DevProb& pr) {
   f.off_w = at;   at = up(at + (f.wlds ? 0 : 16ul * f.JT * (PV / 16) * 256));
   f.off_u = at;   at = up(at + (f.ulds ? 0 : 1024ul * f.wgs * kWaves * f.JT));
   f.off_ds = at;  at = up(at + 4ul * pr.Px * dm.m * f.slab);
-  f.off_xt = at;  at = up(at + sizeof(T) * pr.Px * pr.d * static_cast<size_t>(f.ldx));
-  f.off_qt = at;  at = up(at + sizeof(T) * pr.d * static_cast<size_t>(f.ldq));
   f.off_daq = at; at = up(at + 4ul * (f.slab / 16) * pr.B * P);
   f.off_dax = at; at = up(at + 4ul * dm.qsplits * f.slab * P);
   f.off_dw1 = at; at = up(at + 4ul * f.wgs * H * P);
@@ -787,8 +777,6 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
   auto F = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
   GradParts parts{reinterpret_cast<uint32_t*>(ws + f.off_ds), F(f.off_daq), F(f.off_dax), F(f.off_dw1), F(f.off_dw2),
                   F(f.off_db1), F(f.off_db2)};
-  T* xt = reinterpret_cast<T*>(ws + f.off_xt);
-  T* qt = reinterpret_cast<T*>(ws + f.off_qt);
   float* acc = F(f.off_acc);
   const float* wglob = nullptr;
   if (!f.wlds) {
@@ -797,6 +785,8 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
   }
   const bool vec = (pr.d * sizeof(T)) % 16 == 0 &&
                    ((reinterpret_cast<uintptr_t>(pr.Q) | reinterpret_cast<uintptr_t>(pr.X)) & 15) == 0;
+  const T* X = static_cast<const T*>(pr.X);
+  const T* Q = static_cast<const T*>(pr.Q);
   auto kern = vec ? &k_score_grad<T, PV, true> : &k_score_grad<T, PV, false>;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
                                      static_cast<int>(f.lds));
@@ -807,9 +797,6 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
     const bool last = sl + 1 == f.slabs;
     dm.n0 = sl * f.slab;
     const int items = std::min(f.slab, pr.N - dm.n0);
-    if ((e = launch_transposes<T>(pr, dm.m, f.ldq, o.dX && sl == 0 ? qt : nullptr, dm.n0, items, f.ldx, o.dQ ? xt : nullptr,
-                                  st)) != hipSuccess)
-      return e;
     for (int grp = 0; grp < f.groups; ++grp) {
       dm.group = grp;
       if (grp && !o.dW1 && !o.dW2 && !o.db1) break;
@@ -822,23 +809,22 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
       const int m = static_cast<int>(dm.m);
       // a product of one split (of dQ: and one slab) is stored as the output's type
       const bool dir_q = f.sp_q == 1 && f.slabs == 1, dir_x = f.sp_x == 1;
-      const GemmDims gq{m, pr.d, f.slab, dm.m * f.slab, f.slab, f.slab, pr.Px, static_cast<long>(pr.d) * f.ldx, f.ldx,
-                        f.sp_q, 0, dm.m * pr.d, dir_q, Tiles{(m + 31) / 32, cg, f.sp_q}};
-      const GemmDims gx{items, pr.d, f.slab, dm.m * f.slab, (m + 31) / 32 * 32, m, pr.Px, 0, f.ldq, f.sp_x,
+      const GemmDims gq{m, pr.d, f.slab, dm.m * f.slab, f.slab, items, pr.Px, static_cast<long>(pr.N) * pr.d, f.sp_q, 0, dm.m * pr.d, dir_q, Tiles{(m + 31) / 32, cg, f.sp_q}};
+      const GemmDims gx{items, pr.d, f.slab, dm.m * f.slab, (m + 31) / 32 * 32, m, pr.Px, 0, f.sp_x,
                         dir_x ? static_cast<long>(pr.N) * pr.d : per_px, per_px * pr.Px, dir_x,
                         Tiles{(items + 31) / 32, cg, f.sp_x * pr.Px}};
       void* to_q = dir_q ? o.dQ : F(f.off_pq);
       void* to_x = dir_x ? static_cast<T*>(o.dX) + static_cast<long>(dm.n0) * pr.d : static_cast<void*>(F(f.off_px));
       auto launch = [&](auto kern, bool q, bool x) {
         const long units = (q ? gq.tiles.count() : 0) + (x ? gx.tiles.count() : 0);
-        hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, st, gq, gx, parts.ds, xt, qt,
-                           to_q, to_x);
+        hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, st, gq, gx, parts.ds,
+                           X + static_cast<long>(dm.n0) * pr.d, Q, to_q, to_x);
       };
       if (o.dQ && o.dX && products_together(4ul * pr.Px * dm.m * f.slab)) {
-        launch(&k_grad_products<T, kProductQ | kProductX>, true, true);
+        launch(vec || !bf ? &k_grad_products<T, kProductQ | kProductX, true> : &k_grad_products<T, kProductQ | kProductX, sizeof(T) != 2>, true, true);
       } else {
-        if (o.dQ) launch(&k_grad_products<T, kProductQ>, true, false);
-        if (o.dX) launch(&k_grad_products<T, kProductX>, false, true);
+        if (o.dQ) launch(vec || !bf ? &k_grad_products<T, kProductQ, true> : &k_grad_products<T, kProductQ, sizeof(T) != 2>, true, false);
+        if (o.dX) launch(vec || !bf ? &k_grad_products<T, kProductX, true> : &k_grad_products<T, kProductX, sizeof(T) != 2>, false, true);
       }
     }
     if (o.dQ && (f.sp_q > 1 || f.slabs > 1))

@@ -34,6 +34,7 @@
 namespace mol {
 
 using namespace tile;
+using namespace grad;
 
 namespace {
 
@@ -44,16 +45,6 @@ constexpr size_t kSlabBytes = size_t(288) << 20;
 constexpr int kAhead = 2;                          // blocks of 32 of d loaded ahead
 constexpr int kJT = 4;                             // hidden tiles of 16
 constexpr int kH = 16 * kJT;
-
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
-
-// the transposing read: each group of 16 lanes reads 4 rows of 16 elements (8
-// bytes a lane, rows lane / 4) and gets column lane, its 4 rows in order
-__device__ __forceinline__ uint2 read_tr(const void* lds) {
-  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                       (lds_s16x4_t*)(__attribute__((address_space(3))) const void*)lds));
-}
 
 // high halves of a and b: their first bf16 terms by truncation
 __device__ __forceinline__ uint32_t high_halves(float a, float b) {
@@ -627,48 +618,9 @@ struct GemmBf16 {
   long x_px;         // dQ: elements between item components of X
   int direct;        // one split: out is the output itself
   long out_px;       // dX: elements between item components of out
-  grad::Tiles tiles;
+  Tiles tiles;
 };
-constexpr int kRowB = 9;                             // 16-byte words of an LDS row of 64 columns (144 bytes: spread over the banks)
-constexpr int kTileB = 32 * kRowB, kTileA = 256;     // of a wave's chunk of X or Q, and of ds
-
-// Lane l of a wave has piece l % 8 (8 columns) of rows l / 8 + 8 j of a chunk.
-template <bool VEC>
-struct RowTile {
-  int rows, d, row, col;
-  __device__ __forceinline__ RowTile(int rows_, int d_, int t0) : rows(rows_), d(d_) {
-    const int lane = threadIdx.x & 63;
-    row = lane >> 3;
-    col = min(t0 + 8 * (lane & 7), VEC ? d - 8 : d - 1);   // (past d: others, for products that are not stored)
-  }
-  __device__ __forceinline__ void fetch(uint4 (&v)[4], const bf16_t* base, int k0) const {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bf16_t* p = base + static_cast<uint32_t>(min(k0 + 8 * j + row, rows - 1) * d + col);   // (N d < 2^31)
-      if constexpr (VEC) {
-        v[j] = *reinterpret_cast<const uint4*>(p);
-      } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          w[e] = p[min(2 * e, d - 1 - col)] | static_cast<uint32_t>(p[min(2 * e + 1, d - 1 - col)]) << 16;
-        v[j] = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    }
-  }
-  // (rows past the end: zeros, as ds is there)
-  __device__ __forceinline__ void put(const uint4 (&v)[4], uint4* sh, int k0) const {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      sh[(8 * j + row) * kRowB + (threadIdx.x & 7)] = k0 + 8 * j + row < rows ? v[j] : make_uint4(0, 0, 0, 0);
-  }
-};
-// column 16 t + c of the chunk, K slots 8 g ..
-__device__ __forceinline__ uint4 column_of(const uint4* sh, int t, int c, int g) {
-  const unsigned char* p = reinterpret_cast<const unsigned char*>(sh) + (8 * g + (c >> 2)) * (16 * kRowB) + 8 * (c & 3) + 32 * t;
-  const uint2 a = read_tr(p), b = read_tr(p + 4 * 16 * kRowB);
-  return make_uint4(a.x, a.y, b.x, b.y);
-}
+constexpr int kTileA = 256;                          // 16-byte words of a wave's chunk of ds
 
 // dQ[m][t] = sum over px and items of ds X; z: the split
 template <bool VEC>
@@ -676,7 +628,7 @@ __device__ __forceinline__ void dq_tile(const GemmBf16& gd, uint32_t unit, const
                                         const bf16_t* __restrict__ X, void* __restrict__ out, uint4* sh) {
   constexpr int RB = 2, CB = 4;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int3 at = grad::tile_of(gd.tiles, unit);
+  const int3 at = tile_of(gd.tiles, unit);
   const int m0 = at.x * 16 * RB, t0 = at.y * 16 * CB, z = at.z;
   const int per = gd.nb / 2, chunks = per * gd.npx;  // a chunk: two blocks of items
   const int k0 = static_cast<int>(static_cast<long>(chunks) * z / gd.splits);
@@ -731,7 +683,7 @@ __device__ __forceinline__ void dq_tile(const GemmBf16& gd, uint32_t unit, const
     fetch(v0, min(ch + 2, k1 - 1));
     if (ch + 1 < k1) use(v1, ch + 1);
   }
-  grad::put_tile<bf16_t>(out, static_cast<long>(z) * gd.m * gd.d, m0, gd.m, t0, gd.d, gd.direct, acc);
+  put_tile<bf16_t>(out, static_cast<long>(z) * gd.m * gd.d, m0, gd.m, t0, gd.d, gd.direct, acc);
 }
 
 // dX[px][n][t] = sum over (b, pq) of ds Q: rows of ds of a block of items, 32
@@ -742,7 +694,7 @@ __device__ __forceinline__ void dx_tile(const GemmBf16& gd, uint32_t unit, const
                                         const bf16_t* __restrict__ Q, void* __restrict__ out, uint4* sh) {
   constexpr int RB = 2, CB = 4;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  const int3 at = grad::tile_of(gd.tiles, unit);                      // (no workgroup barrier below)
+  const int3 at = tile_of(gd.tiles, unit);                      // (no workgroup barrier below)
   const int blk0 = at.x * RB, t0 = at.y * 16 * CB, z = at.z;
   const int px = z / gd.splits, split = z - px * gd.splits;
   const int chunks = (gd.m + 31) / 32;
@@ -798,7 +750,7 @@ __device__ __forceinline__ void dx_tile(const GemmBf16& gd, uint32_t unit, const
     fetch(v0, min(ch + 2, k1 - 1));
     if (ch + 1 < k1) use(v1, ch + 1);
   }
-  grad::put_tile<bf16_t>(out, (static_cast<long>(split) * gd.npx + px) * gd.out_px, 16 * blk0, gd.items, t0, gd.d, gd.direct,
+  put_tile<bf16_t>(out, (static_cast<long>(split) * gd.npx + px) * gd.out_px, 16 * blk0, gd.items, t0, gd.d, gd.direct,
                          acc);
 }
 
@@ -808,14 +760,14 @@ template <int WHAT, bool VEC>
 __global__ __launch_bounds__(256) void k_grad_products_bf16(GemmBf16 q, GemmBf16 x, const uint32_t* __restrict__ ds,
                                                             const bf16_t* __restrict__ X, const bf16_t* __restrict__ Q,
                                                             void* __restrict__ out_q, void* __restrict__ out_x) {
-  constexpr int words = kTileB + (WHAT & grad::kProductX ? kTileA : 0);
+  constexpr int words = kTileB + (WHAT & kProductX ? kTileA : 0);
   __shared__ __attribute__((aligned(16))) uint4 sh[4][words];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t unit = blockIdx.x * 4 + wave;
-  const uint32_t nq = WHAT & grad::kProductQ ? static_cast<uint32_t>(q.tiles.count()) : 0;
-  if constexpr (WHAT & grad::kProductQ)
+  const uint32_t nq = WHAT & kProductQ ? static_cast<uint32_t>(q.tiles.count()) : 0;
+  if constexpr (WHAT & kProductQ)
     if (unit < nq) dq_tile<VEC>(q, unit, ds, X, out_q, sh[wave]);
-  if constexpr (WHAT & grad::kProductX)
+  if constexpr (WHAT & kProductX)
     if (unit >= nq && unit - nq < static_cast<uint32_t>(x.tiles.count())) dx_tile<VEC>(x, unit - nq, ds, Q, out_x, sh[wave]);
 }
 

@@ -276,8 +276,8 @@ def test_score_grad_in_slabs():
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
-def test_score_grad_in_slabs_of_few_queries(dtype):
-    """Where X transposed is what fills a slab: B P_q of 6, rows of 1024 elements, two to four slabs."""
+def test_score_grad_of_few_queries_and_many_items(dtype):
+    """Sums of dQ and the weights over 200,003 items with B P_q of 6: many splits of a short product."""
     B, N, Pq, Px, d, H, part = 3, 200003, 2, 1, 1024, 16, 20000
     log(f"[score_grad] B={B} N={N} P={Pq}x{Px} d={d} H={H} {NAME[dtype]}")
     inputs, dphi = lh.mol_inputs(B, N, Pq, Px, d, H, dtype, seed=8, device="cuda")
