@@ -40,12 +40,6 @@ bool bf16_supported(const DevProb& pr);
 size_t bf16_bytes(const DevProb& pr);
 hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_grads& o, char* ws, hipStream_t st);
 
-// dQ and dX from ds in one launch or in two.  Together they fill the card where
-// there is little of it (34 MB of ds: 18 us against 12 + 12); apart the second finds
-// part of what the first read in the last-level cache (268 MB: 77 + 60 us against 259).
-constexpr int kProductQ = 1, kProductX = 2;
-inline bool products_together(size_t ds_bytes) { return ds_bytes <= (size_t(64) << 20); }
-
 // K splits of a product of `waves` waves a part with `chunks` K chunks: about 2048
 // waves in all, with two chunks a split up to 64 splits (a short product is a chain of
 // latencies) and `least` beyond (each split is a part to write and to add).

@@ -41,7 +41,7 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves, kPairs = 16 * kWaves;
 // Of a slab's ds and partial sums: a million pairs of 64 components, whose
-// ds alone is 268 MB (in bf16 at 1024 x 2048 pairs: two such slabs 848 us, three of 187 MB 930 us).
+// ds alone is 268 MB (see the bf16 form).
 constexpr size_t kSlabBytes = size_t(288) << 20;
 
 template <int PV>
@@ -618,21 +618,20 @@ __device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, 
 }
 
 // ---------------------------------------------------------------------------
-// Both products, side by side (the first tiles are dQ's), or one.
+// Both products, side by side: the first tiles are dQ's.  (In bf16 at 1024 x 2048
+// pairs of 8 x 8 one launch of both is 13 us shorter than two.)
 // VEC: rows of X and Q of whole 16-byte words (bf16).
-template <typename T, int WHAT, bool VEC>
+template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void k_grad_products(GemmDims q, GemmDims x, const uint32_t* __restrict__ ds,
                                                        const T* __restrict__ X, const T* __restrict__ Q,
                                                        void* __restrict__ out_q, void* __restrict__ out_x) {
   __shared__ __attribute__((aligned(16))) uint4 sh[4][sizeof(T) == 2 ? kTileB : 1];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t unit = blockIdx.x * 4 + wave;
-  const uint32_t nq = WHAT & kProductQ ? static_cast<uint32_t>(q.tiles.count()) : 0;
-  if constexpr (WHAT & kProductQ)
-    if (unit < nq) product_tile<T, false, VEC>(q, unit, ds, X, out_q, sh[wave]);
-  if constexpr (WHAT & kProductX)
-    if (unit >= nq && unit - nq < static_cast<uint32_t>(x.tiles.count()))
-      product_tile<T, true, VEC>(x, unit - nq, ds, Q, out_x, sh[wave]);
+  const uint32_t unit = blockIdx.x * 4 + wave, nq = static_cast<uint32_t>(q.tiles.count());
+  if (unit < nq)
+    product_tile<T, false, VEC>(q, unit, ds, X, out_q, sh[wave]);
+  else if (unit - nq < static_cast<uint32_t>(x.tiles.count()))
+    product_tile<T, true, VEC>(x, unit - nq, ds, Q, out_x, sh[wave]);
 }
 
 // ---------------------------------------------------------------------------
@@ -809,23 +808,16 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
       const int m = static_cast<int>(dm.m);
       // a product of one split (of dQ: and one slab) is stored as the output's type
       const bool dir_q = f.sp_q == 1 && f.slabs == 1, dir_x = f.sp_x == 1;
-      const GemmDims gq{m, pr.d, f.slab, dm.m * f.slab, f.slab, items, pr.Px, static_cast<long>(pr.N) * pr.d, f.sp_q, 0, dm.m * pr.d, dir_q, Tiles{(m + 31) / 32, cg, f.sp_q}};
+      const GemmDims gq{m, pr.d, f.slab, dm.m * f.slab, f.slab, items, pr.Px, static_cast<long>(pr.N) * pr.d, f.sp_q, 0, dm.m * pr.d, dir_q, Tiles{(m + 31) / 32, cg, o.dQ ? f.sp_q : 0}};
       const GemmDims gx{items, pr.d, f.slab, dm.m * f.slab, (m + 31) / 32 * 32, m, pr.Px, 0, f.sp_x,
                         dir_x ? static_cast<long>(pr.N) * pr.d : per_px, per_px * pr.Px, dir_x,
-                        Tiles{(items + 31) / 32, cg, f.sp_x * pr.Px}};
+                        Tiles{(items + 31) / 32, cg, o.dX ? f.sp_x * pr.Px : 0}};
       void* to_q = dir_q ? o.dQ : F(f.off_pq);
       void* to_x = dir_x ? static_cast<T*>(o.dX) + static_cast<long>(dm.n0) * pr.d : static_cast<void*>(F(f.off_px));
-      auto launch = [&](auto kern, bool q, bool x) {
-        const long units = (q ? gq.tiles.count() : 0) + (x ? gx.tiles.count() : 0);
-        hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, st, gq, gx, parts.ds,
-                           X + static_cast<long>(dm.n0) * pr.d, Q, to_q, to_x);
-      };
-      if (o.dQ && o.dX && products_together(4ul * pr.Px * dm.m * f.slab)) {
-        launch(vec || !bf ? &k_grad_products<T, kProductQ | kProductX, true> : &k_grad_products<T, kProductQ | kProductX, sizeof(T) != 2>, true, true);
-      } else {
-        if (o.dQ) launch(vec || !bf ? &k_grad_products<T, kProductQ, true> : &k_grad_products<T, kProductQ, sizeof(T) != 2>, true, false);
-        if (o.dX) launch(vec || !bf ? &k_grad_products<T, kProductX, true> : &k_grad_products<T, kProductX, sizeof(T) != 2>, false, true);
-      }
+      const long units = gq.tiles.count() + gx.tiles.count();
+      auto products = vec || !bf ? &k_grad_products<T, true> : &k_grad_products<T, sizeof(T) != 2>;
+      hipLaunchKernelGGL(products, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, st, gq, gx, parts.ds,
+                         X + static_cast<long>(dm.n0) * pr.d, Q, to_q, to_x);
     }
     if (o.dQ && (f.sp_q > 1 || f.slabs > 1))
       sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, f.slabs > 1 ? acc + f.a_dq : nullptr, sl > 0,

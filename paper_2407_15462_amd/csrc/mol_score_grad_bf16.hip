@@ -40,7 +40,8 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 // Of a slab's ds and partial sums: a million pairs of 64 components, whose
-// ds alone is 268 MB (in bf16 at 1024 x 2048 pairs: two such slabs 848 us, three of 187 MB 930 us).
+// ds alone is 268 MB (1024 x 2048 pairs: two such slabs 770 us, three of 187 MB, whose
+// workgroups fill 220 of the 256 CUs, 882).
 constexpr size_t kSlabBytes = size_t(288) << 20;
 constexpr int kAhead = 2;                          // blocks of 32 of d loaded ahead
 constexpr int kJT = 4;                             // hidden tiles of 16
@@ -754,21 +755,19 @@ __device__ __forceinline__ void dx_tile(const GemmBf16& gd, uint32_t unit, const
                          acc);
 }
 
-// Both products, side by side (the first tiles are dQ's), or one.
+// Both products, side by side: the first tiles are dQ's.
 // VEC: rows of X and Q of whole 16-byte words.
-template <int WHAT, bool VEC>
+template <bool VEC>
 __global__ __launch_bounds__(256) void k_grad_products_bf16(GemmBf16 q, GemmBf16 x, const uint32_t* __restrict__ ds,
                                                             const bf16_t* __restrict__ X, const bf16_t* __restrict__ Q,
                                                             void* __restrict__ out_q, void* __restrict__ out_x) {
-  constexpr int words = kTileB + (WHAT & kProductX ? kTileA : 0);
-  __shared__ __attribute__((aligned(16))) uint4 sh[4][words];
+  __shared__ __attribute__((aligned(16))) uint4 sh[4][kTileB + kTileA];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t unit = blockIdx.x * 4 + wave;
-  const uint32_t nq = WHAT & kProductQ ? static_cast<uint32_t>(q.tiles.count()) : 0;
-  if constexpr (WHAT & kProductQ)
-    if (unit < nq) dq_tile<VEC>(q, unit, ds, X, out_q, sh[wave]);
-  if constexpr (WHAT & kProductX)
-    if (unit >= nq && unit - nq < static_cast<uint32_t>(x.tiles.count())) dx_tile<VEC>(x, unit - nq, ds, Q, out_x, sh[wave]);
+  const uint32_t unit = blockIdx.x * 4 + wave, nq = static_cast<uint32_t>(q.tiles.count());
+  if (unit < nq)
+    dq_tile<VEC>(q, unit, ds, X, out_q, sh[wave]);
+  else if (unit - nq < static_cast<uint32_t>(x.tiles.count()))
+    dx_tile<VEC>(x, unit - nq, ds, Q, out_x, sh[wave]);
 }
 
 // ---------------------------------------------------------------------------
@@ -883,25 +882,18 @@ hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_gra
       // a product of one split (of dQ: and one slab) is stored as bf16
       const bool dir_q = f.sp_q == 1 && f.slabs == 1, dir_x = f.sp_x == 1;
       const int m = static_cast<int>(dm.m);
-      const GemmBf16 gq{m, dm.nb, pr.d, pr.Px, f.sp_q, dm.items, static_cast<long>(pr.N) * pr.d, dir_q, 0, Tiles{(m + 31) / 32, cg, f.sp_q}};
+      const GemmBf16 gq{m, dm.nb, pr.d, pr.Px, f.sp_q, dm.items, static_cast<long>(pr.N) * pr.d, dir_q, 0, Tiles{(m + 31) / 32, cg, o.dQ ? f.sp_q : 0}};
       const GemmBf16 gx{m, dm.nb, pr.d, pr.Px, f.sp_x, dm.items, 0, dir_x,
-                        dir_x ? static_cast<long>(pr.N) * pr.d : per_px, Tiles{(dm.nb + 1) / 2, cg, f.sp_x * pr.Px}};
+                        dir_x ? static_cast<long>(pr.N) * pr.d : per_px, Tiles{(dm.nb + 1) / 2, cg, o.dX ? f.sp_x * pr.Px : 0}};
       void* to_q = dir_q ? o.dQ : F(f.off_pq);
       void* to_x = dir_x ? static_cast<bf16_t*>(o.dX) + static_cast<long>(dm.n0) * pr.d : static_cast<void*>(F(f.off_px));
       const bf16_t* X = static_cast<const bf16_t*>(pr.X) + static_cast<long>(dm.n0) * pr.d;
       const bf16_t* Q = static_cast<const bf16_t*>(pr.Q);
       const bool vec = pr.d % 8 == 0 && ((reinterpret_cast<uintptr_t>(pr.X) | reinterpret_cast<uintptr_t>(pr.Q)) & 15) == 0;
-      auto launch = [&](auto kern, bool q, bool x) {
-        const long units = (q ? gq.tiles.count() : 0) + (x ? gx.tiles.count() : 0);
-        hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, st, gq, gx, parts.ds, X, Q, to_q,
-                           to_x);
-      };
-      if (o.dQ && o.dX && products_together(4ul * pr.Px * dm.m * f.slab)) {
-        launch(vec ? &k_grad_products_bf16<kProductQ | kProductX, true> : &k_grad_products_bf16<kProductQ | kProductX, false>, true, true);
-      } else {
-        if (o.dQ) launch(vec ? &k_grad_products_bf16<kProductQ, true> : &k_grad_products_bf16<kProductQ, false>, true, false);
-        if (o.dX) launch(vec ? &k_grad_products_bf16<kProductX, true> : &k_grad_products_bf16<kProductX, false>, false, true);
-      }
+      const long units = gq.tiles.count() + gx.tiles.count();
+      auto products = vec ? &k_grad_products_bf16<true> : &k_grad_products_bf16<false>;
+      hipLaunchKernelGGL(products, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, st, gq, gx, parts.ds, X, Q,
+                         to_q, to_x);
     }
     if (o.dQ && (f.sp_q > 1 || f.slabs > 1))
       sums.add({F(f.off_pq), dm.m * pr.d, dm.m * pr.d, f.sp_q, f.slabs > 1 ? acc + f.a_dq : nullptr, sl > 0,
