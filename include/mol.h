@@ -378,11 +378,12 @@ int mol_softmax_loss(int32_t B, int32_t N, const float *phi,
  *   du   = dh sig (1 + u (1 - sig))    dW1 = sum du s^T,        db1 = sum du
  *   ds   = g pi + W1^T du              dQ = sum ds X,           dX = sum ds Q
  * Each output has its tensor's shape and type, and any may be NULL.  Every
- * element is written.  The gating chain runs in float32 for float32 problems
- * and in float32 or better than float32's rounding allows to tell for bf16
- * ones whatever the flags say; sums are float32, rounded once to bf16 at the
- * end.  Needs every problem pointer and
- * mol_workspace_size(MOL_OP_SCORE_GRAD) bytes of workspace. */
+ * element is written.  The gating chain has float32's precision whatever the
+ * problem's type and flags; sums are float32, rounded once to bf16 at the end
+ * where the output is bf16.  Outputs overlap neither the inputs nor each other.
+ * Needs every problem pointer and mol_workspace_size(MOL_OP_SCORE_GRAD) bytes
+ * of workspace (256-byte aligned), which stay bounded as the corpus grows:
+ * items are taken in slabs. */
 typedef struct mol_score_grads {
   void *dQ;      /* [B][Pq][d]  dtype   */
   void *dX;      /* [Px][N][d]  dtype   */

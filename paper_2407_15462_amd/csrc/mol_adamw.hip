@@ -4,9 +4,11 @@
 //   p' = p (1 - lr wd) - lr (m' / bc1) / (sqrt(v' / bc2) + eps).
 //
 // Bound by memory: every buffer is read or written once (28 bytes an element in
-// float32, 16 with 8-bit states, bf16 gradients and a bf16 copy).  A launch takes up to kMaxTensors tensors,
-// described in its arguments; workgroups have chunks of kChunk elements, found by
-// a search over the tensors' first chunks.  A wave has 256 elements, one block
+// float32, 16 with 8-bit states, bf16 gradients and a bf16 copy): 3 M elements of
+// 24 float32 tensors in 16 us (5.2 TB/s), 173 M with 8-bit states in 520 us (5.3 TB/s,
+// a copy runs at 4.6).  A launch takes up to kMaxTensors tensors, described in
+// its arguments; workgroups have chunks of kChunk elements, found by a search
+// over the tensors' first chunks.  A wave has 256 elements, one block
 // of an 8-bit state, at a time, four a lane: the block's largest magnitude is a
 // reduction in registers, and the loads of its kChunk / 1024 blocks are issued together.
 //

@@ -97,7 +97,7 @@ __device__ __forceinline__ uint2 read_tr(const void* lds) {
 }
 
 // Rows of X or Q as the K of a bf16 product: a chunk of 32 of them, 64 columns wide.
-constexpr int kRowB = 9;                             // 16-byte words of an LDS row of 64 columns (144 bytes: spread over the banks)
+constexpr int kRowB = 9;                             // 16-byte words of an LDS row of 64 columns (and one: other banks)
 constexpr int kTileB = 32 * kRowB;                   // of a wave's chunk of X or Q
 
 // Lane l of a wave has piece l % 8 (8 columns) of rows l / 8 + 8 j of a chunk.
@@ -133,7 +133,8 @@ struct RowTile {
 };
 // column 16 t + c of the chunk, K slots 8 g ..
 __device__ __forceinline__ uint4 column_of(const uint4* sh, int t, int c, int g) {
-  const unsigned char* p = reinterpret_cast<const unsigned char*>(sh) + (8 * g + (c >> 2)) * (16 * kRowB) + 8 * (c & 3) + 32 * t;
+  const unsigned char* p =
+      reinterpret_cast<const unsigned char*>(sh) + (8 * g + (c >> 2)) * (16 * kRowB) + 8 * (c & 3) + 32 * t;
   const uint2 a = read_tr(p), b = read_tr(p + 4 * 16 * kRowB);
   return make_uint4(a.x, a.y, b.x, b.y);
 }

@@ -11,6 +11,8 @@
 // leaves in the workspace and a second one joins, reading the row again (from
 // the last-level cache where the batch's scores fit it).  Rows start at any
 // element, so that loads are 4 bytes a lane, kRegs of them in flight.
+// Measured: 1024 rows of 32,771 take 70 us (3.8 TB/s; a copy of as much 59),
+// 128 rows of 128 5 us, of a call's 10.
 // Maximum, sum and loss are float32.
 #include <algorithm>
 

@@ -27,7 +27,12 @@
 // 3. k_sum_parts adds the partial sums in a fixed order.
 // Items are taken in slabs, so that ds and what else grows with them stay within kSlabBytes.
 //
-// What bounds it: the f32 matrix rate, 12 P H flop a pair (157 TFLOP/s).
+// What bounds it: the f32 matrix rate, 12 P H + 2 P d flop a pair, and for few pairs
+// the latencies of a workgroup's one or two tiles (weights, dot products, the
+// chain and back, the sums: 55 us at P = H = 64).  Measured in float32: 32 x 129
+// pairs of 4 x 4, H = 32 16 + 6 + 5 us (pairs, products, sums), 26 a call; 200 x 4000 of
+// them 175 + 58 + 14 (pairs at 48 TFLOP/s, a large product at 144); 8 x 6112 of
+// 8 x 8, H = 64 70 + 23 + 8.
 #include <algorithm>
 
 #include "mol_grad.h"
@@ -808,7 +813,8 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
       const int m = static_cast<int>(dm.m);
       // a product of one split (of dQ: and one slab) is stored as the output's type
       const bool dir_q = f.sp_q == 1 && f.slabs == 1, dir_x = f.sp_x == 1;
-      const GemmDims gq{m, pr.d, f.slab, dm.m * f.slab, f.slab, items, pr.Px, static_cast<long>(pr.N) * pr.d, f.sp_q, 0, dm.m * pr.d, dir_q, Tiles{(m + 31) / 32, cg, o.dQ ? f.sp_q : 0}};
+      const GemmDims gq{m, pr.d, f.slab, dm.m * f.slab, f.slab, items, pr.Px, static_cast<long>(pr.N) * pr.d, f.sp_q, 0,
+                        dm.m * pr.d, dir_q, Tiles{(m + 31) / 32, cg, o.dQ ? f.sp_q : 0}};
       const GemmDims gx{items, pr.d, f.slab, dm.m * f.slab, (m + 31) / 32 * 32, m, pr.Px, 0, f.sp_x,
                         dir_x ? static_cast<long>(pr.N) * pr.d : per_px, per_px * pr.Px, dir_x,
                         Tiles{(items + 31) / 32, cg, o.dX ? f.sp_x * pr.Px : 0}};

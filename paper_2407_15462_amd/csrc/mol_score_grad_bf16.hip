@@ -27,6 +27,14 @@
 // block][b pq][16 first terms, 16 second terms]: 64-byte rows that both products read
 // whole.  dQ = sum ds X reads rows (K = items); dX = sum ds Q (K = b pq) takes them through LDS
 // and the transposing read.
+//
+// Measured, 1024 x 2048 pairs of 8 x 8, d = H = 64, in two slabs: 760 us a call,
+// 203 TFLOP/s; a slab's pairs 295 us, products 101 (5.3 TB/s of ds), sums 18.  128 x 1031
+// of 8 x 8, d = 32: 64 + 18 + 10.  The pairs are bound by issue and latency: a unit
+// is 914 vector, 49 transcendental, 124 matrix and 121 LDS instructions, its
+// 256 registers leave two waves a SIMD, and these issue vector instructions 40 % of
+// the time.  The general form, on f32 matrix instructions, takes 435 us for half as
+// many pairs.
 #include <algorithm>
 
 #include "mol_grad.h"
@@ -495,7 +503,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
         const uint32_t hi = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
         const uint32_t lo = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v - __uint_as_float(hi << 16)));
         const uint32_t own = hi | lo << 16;
-        const uint32_t other = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(own), 0xB1, 0xf, 0xf, true));   // quad_perm 1,0,3,2
+        const uint32_t other =                                         // quad_perm 1,0,3,2
+            static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(own), 0xB1, 0xf, 0xf, true));
         // even: (own low, other low); odd: (other high, own high)
         const uint32_t w = __builtin_amdgcn_perm(other, own, pick);
         if (FULL || (NPQ * g + i < Pq && px < Px)) const_cast<uint32_t&>(at32(to, to_off + 64u * i)) = w;
@@ -882,7 +891,8 @@ hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_gra
       // a product of one split (of dQ: and one slab) is stored as bf16
       const bool dir_q = f.sp_q == 1 && f.slabs == 1, dir_x = f.sp_x == 1;
       const int m = static_cast<int>(dm.m);
-      const GemmBf16 gq{m, dm.nb, pr.d, pr.Px, f.sp_q, dm.items, static_cast<long>(pr.N) * pr.d, dir_q, 0, Tiles{(m + 31) / 32, cg, o.dQ ? f.sp_q : 0}};
+      const GemmBf16 gq{m, dm.nb, pr.d, pr.Px, f.sp_q, dm.items, static_cast<long>(pr.N) * pr.d, dir_q, 0,
+                        Tiles{(m + 31) / 32, cg, o.dQ ? f.sp_q : 0}};
       const GemmBf16 gx{m, dm.nb, pr.d, pr.Px, f.sp_x, dm.items, 0, dir_x,
                         dir_x ? static_cast<long>(pr.N) * pr.d : per_px, Tiles{(dm.nb + 1) / 2, cg, o.dX ? f.sp_x * pr.Px : 0}};
       void* to_q = dir_q ? o.dQ : F(f.off_pq);
