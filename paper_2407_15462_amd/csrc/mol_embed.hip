@@ -6,10 +6,9 @@
 // from each of 8 float32 tables to bf16: 61 us, 6.6 TB/s, where a copy runs at 4.6).
 //
 // Gradient: table_grad[c][v][:] = scale sum_{t: ids[t] = v} grad[c][t][:].
-//  1. The tokens are sorted by id, stably: least-significant-digit radix
-//     passes over (id, t) pairs, of 8 bits in one workgroup's LDS for up to
-//     kSortOne tokens, else of up to 11 bits, a histogram and a scatter
-//     launch each.  Empty slots sort behind every row (key V).
+//  1. The tokens are sorted by id, stably: up to kSortRank of them by counting,
+//     else in least-significant-digit radix passes over (id, t) pairs, of up to
+//     11 bits, a histogram and a scatter launch each.  Empty slots sort behind every row (key V).
 //  2. Each workgroup takes a span of sorted tokens and a column slice of a
 //     table.  Teams of LPR lanes (16 bytes a lane) walk K tokens each, with
 //     four rows in flight, and keep the running sum of the current id in
@@ -29,7 +28,8 @@
 // 8 x 32 onto 674,044 rows 35, 139 (5.2 TB/s, nine tenths of it zero rows) and 5.
 // The sort's passes are chains of latencies (6 us a histogram, 11 a scatter).
 // Sorted chunks of 4096 merged by rank took 53 us against 35 at 65,536 tokens, and
-// rows cleared beside the sort slowed it by what the sums gained.
+// rows cleared beside the sort slowed it by what the sums gained.  Spans that end
+// where runs do, with nothing to join, took 12 us against 6 + 4 at 1024 tokens of 512.
 #include <algorithm>
 
 #include "mol_kernels.h"
@@ -38,7 +38,9 @@ namespace mol {
 
 namespace {
 
-constexpr int kSortOne = 4096;        // tokens sorted by one workgroup
+// Tokens at most that are sorted by counting (1024: 3.7 us, 4096: 6.8, 8192: 12.4,
+// 16,384: 38; the radix passes take 21 from 8193 on, one workgroup's took 6.8 at 1024).
+constexpr int kSortRank = 8192;
 constexpr int kSortThreads = 256;     // of a block of the radix passes
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSortU = 8;             // loads in flight
@@ -144,55 +146,59 @@ __global__ __launch_bounds__(256) void k_embed_lookup(const TI* __restrict__ tab
 }
 
 // ---------------------------------------------------------------------------
-// Sorting.  One workgroup: all 8-bit passes in LDS.
-__global__ __launch_bounds__(1024) void k_sort_one(const int32_t* __restrict__ ids, int T, int V, int bits,
+// Sorting few tokens: a token's place is the number of those before it in the
+// order of (key, token), counted against all keys in LDS.  A workgroup has 16
+// tokens, and lane (c = lane % 16, q = lane / 16) of wave w counts every 16th
+// four keys, from 4 w + q on, for token c.
+__global__ __launch_bounds__(256) void k_sort_rank(const int32_t* __restrict__ ids, int T, int V,
                                                    uint2* __restrict__ out) {
-  constexpr int NW = 16, PER = kSortOne / NW;
-  __shared__ uint2 pairs[2][kSortOne];
-  __shared__ uint32_t hist[NW][256];
-  __shared__ uint32_t carry[4];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  for (int i = tid; i < T; i += 1024) pairs[0][i] = make_uint2(key_of(ids[i], V), i);
-  int cur = 0;
-  for (int shift = 0; shift < bits; shift += 8, cur ^= 1) {
-    for (int i = tid; i < NW * 256; i += 1024) hist[i >> 8][i & 255] = 0;
-    __syncthreads();
-    const int i0 = w * PER, i1 = min(T, i0 + PER);
-    for (int i = i0 + lane; i < i1; i += 64) atomicAdd(&hist[w][(pairs[cur][i].x >> shift) & 255], 1u);
-    __syncthreads();
-    // exclusive starts: digits first, waves of a digit in order
-    uint32_t sum = 0, incl = 0;
-    if (tid < 256) {
-      for (int k = 0; k < NW; ++k) sum += hist[k][tid];
-      incl = wave_scan(sum, lane);
-      if (lane == 63) carry[w] = incl;
+  extern __shared__ __attribute__((aligned(16))) uint32_t keys[];   // 64 ceil(T / 64), then [16][16] counts
+  const int tid = threadIdx.x, c = tid & 15, part = tid >> 4;
+  const int Tp = (T + 63) / 64 * 64, i0 = blockIdx.x * 16;
+  for (int b = tid; b < Tp; b += 256 * kSortU) {
+    int32_t id[kSortU];
+#pragma unroll
+    for (int u = 0; u < kSortU; ++u) id[u] = ids[min(b + 256 * u, T - 1)];
+#pragma unroll
+    for (int u = 0; u < kSortU; ++u) {
+      const int i = b + 256 * u;
+      if (i < Tp) keys[i] = i < T ? key_of(id[u], V) : 0xFFFFFFFFu;
     }
-    __syncthreads();
-    if (tid < 256) {
-      uint32_t at = incl - sum;
-      for (int k = 0; k < w; ++k) at += carry[k];
-      for (int k = 0; k < NW; ++k) {
-        const uint32_t n = hist[k][tid];
-        hist[k][tid] = at;
-        at += n;
-      }
-    }
-    __syncthreads();
-    for (int b = i0; b < i1; b += 64) {
-      const bool live = b + lane < i1;
-      const uint2 p = live ? pairs[cur][b + lane] : make_uint2(0, 0);
-      const uint32_t digit = (p.x >> shift) & 255;
-      const uint64_t m = same_digit<8>(digit, __ballot(live));
-      const int rank = __popcll(m & ((1ull << lane) - 1));
-      const uint32_t at = hist[w][digit] + rank;
-      __builtin_amdgcn_wave_barrier();
-      if (live && rank == 0) hist[w][digit] += __popcll(m);   // (a wave's LDS operations complete in order)
-      __builtin_amdgcn_wave_barrier();
-      if (live) pairs[cur ^ 1][at] = p;
-    }
-    __syncthreads();
   }
-  for (int i = tid; i < T; i += 1024) out[i] = pairs[cur][i];
+  __syncthreads();
+  const uint32_t mine = keys[min(i0 + c, T - 1)];
+  // keys of tokens before the workgroup's count where they are mine or less, of those
+  // behind it where they are less; its own 16 (four fours) by place
+  const uint4* four = reinterpret_cast<const uint4*>(keys);
+  const int own = i0 / 4, all = Tp / 4;
+  uint32_t n = 0;
+  int m = part;
+#pragma unroll 4
+  for (; m < own; m += 16) {
+    const uint4 k = four[m];
+    n += (k.x <= mine) + (k.y <= mine) + (k.z <= mine) + (k.w <= mine);
+  }
+  if (m < own + 4) {
+    const uint4 k = four[m];
+    const int before = i0 + c - 4 * m;                                // of the four
+    n += (before > 0 ? k.x <= mine : k.x < mine) + (before > 1 ? k.y <= mine : k.y < mine) +
+         (before > 2 ? k.z <= mine : k.z < mine) + (before > 3 ? k.w <= mine : k.w < mine);
+    m += 16;
+  }
+#pragma unroll 4
+  for (; m < all; m += 16) {
+    const uint4 k = four[m];
+    n += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
+  }
+  uint32_t* counts = keys + Tp;
+  counts[part * 16 + c] = n;
+  __syncthreads();
+  if (tid < 16 && i0 + tid < T) {
+    uint32_t at = 0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) at += counts[k * 16 + tid];
+    out[at] = make_uint2(mine, i0 + tid);
+  }
 }
 
 // a token's (key, place); in: NULL for the ids themselves
@@ -562,8 +568,8 @@ size_t embed_grad_bytes(int C, int V, int d, long T, size_t off[4]) {
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   size_t at = 0;
   off[0] = at; at = up(at + 8ul * T);                      // sorted pairs
-  off[1] = at; if (T > kSortOne) at = up(at + 8ul * T);    // the other side of the passes
-  off[2] = at; if (T > kSortOne) at = up(at + 4ul * kSortBlocks * (1 << kMaxBits));
+  off[1] = at; if (T > kSortRank) at = up(at + 8ul * T);    // the other side of the passes
+  off[2] = at; if (T > kSortRank) at = up(at + 4ul * kSortBlocks * (1 << kMaxBits));
   off[3] = at;
   size_t spans = 0;
   for (int VE : {1, 4, 8}) spans = std::max<size_t>(spans, grad_args(C, V, d, T, VE).spans);
@@ -592,11 +598,13 @@ hipError_t launch_embed_lookup(const void* table, int table_dtype, int C, int V,
 }
 
 static hipError_t launch_sort(const int32_t* ids, long T, int V, uint2* a, uint2* b, uint32_t* counts, hipStream_t st) {
-  const int bits = key_bits(V);
-  if (T <= kSortOne) {
-    hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(1024), 0, st, ids, static_cast<int>(T), V, bits, a);
+  if (T <= kSortRank) {
+    const size_t lds = ((T + 63) / 64 * 64 + 256) * 4;                // (33 KB at most)
+    hipLaunchKernelGGL(k_sort_rank, dim3(static_cast<unsigned>((T + 15) / 16)), dim3(256), lds, st, ids,
+                       static_cast<int>(T), V, a);
     return hipGetLastError();
   }
+  const int bits = key_bits(V);
   const int passes = (bits + kMaxBits - 1) / kMaxBits, each = std::max(kMinBits, (bits + passes - 1) / passes);
   const int per = sort_per(T), nb = static_cast<int>((T + per - 1) / per), nbp = (nb + 3) / 4 * 4;
   auto scatter = each == 8 ? &k_sort_scatter<8> : each == 9 ? &k_sort_scatter<9> : each == 10 ? &k_sort_scatter<10>

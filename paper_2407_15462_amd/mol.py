@@ -520,7 +520,9 @@ def embed_grad(grad: torch.Tensor, ids: torch.Tensor, V: int, scale: float = 1.0
             out = grad.new_empty((C, V, d), dtype=dtype)
         else:
             _operand(out, "out", (C, V, d), (dtype,), dev)
-        mol_embed_grad(grad, ids, scale, accumulate, out, ws, stream)
+        _check(load().mol_embed_grad(grad.data_ptr(), _DTYPES[grad.dtype], C, V, d, ids.data_ptr(), T, scale,
+                                     int(accumulate), out.data_ptr(), _DTYPES[dtype], None if ws is None else ws.data_ptr(),
+                                     0 if ws is None else ws.numel(), _stream(stream)))
     return out
 
 

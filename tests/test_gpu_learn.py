@@ -62,7 +62,8 @@ def test_lookup_of_no_ids():
 # ------------------------------------------------------------------ gradient of the lookup
 @pytest.mark.parametrize("C,V,d,T", [(1, 1, 1, 1), (1, 3, 5, 40), (2, 50, 33, 64), (4, 1000, 64, 300), (1, 9, 1024, 130),
                                      (2, 300, 96, 4096), (1, 5000, 32, 4097), (8, 2000, 32, 9000), (1, 70000, 8, 30000),
-                                     (2, 3000, 16, 16384), (1, 999, 8, 16385), (1, 500, 4, 65537),
+                                     (2, 3000, 16, 16384), (1, 999, 8, 16385), (1, 500, 4, 65537), (1, 9, 4, 15), (1, 9, 4, 17),
+                                     (2, 5, 8, 65), (1, 1, 4, 1000), (1, 300, 16, 8192), (2, 77, 8, 8193),
                                      (1, 1 << 21, 4, 6000), (1, 40, 64, 50000), (1, 3, 1000, 777), (1, 2, 65536, 9)])
 @pytest.mark.parametrize("ti,to", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
 def test_embed_grad(C, V, d, T, ti, to):
