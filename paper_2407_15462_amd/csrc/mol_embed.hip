@@ -23,14 +23,15 @@
 // floats, the same bits every time.  Bound by memory: grad is read once and
 // table_grad written once; a row that a million tokens share costs no more than
 // a million rows (its span sums run side by side).
-// Measured: 262,144 tokens of 4 x 128 bf16 onto 24,186 float32 rows take 35 us
+// Measured: 262,144 tokens of 4 x 128 bf16 onto 24,186 float32 rows take 29 us
 // for the sort, 68 for the sums (4.7 TB/s) and 8 for the join, 117 a call; 65,536 of
-// 8 x 32 onto 674,044 rows 35, 139 (5.2 TB/s, nine tenths of it zero rows) and 5.
-// The sort's passes are chains of latencies (6 us a histogram, 11 a scatter).
-// Sorted chunks of 4096 merged by rank took 53 us against 35 at 65,536 tokens, and
+// 8 x 32 onto 674,044 rows 30, 139 (5.2 TB/s, nine tenths of it zero rows) and 5.
+// The sort's passes are chains of latencies (5 us a histogram, 9 a scatter).
+// Sorted chunks of 4096 merged by rank took 53 us against 31 at 65,536 tokens, and
 // rows cleared beside the sort slowed it by what the sums gained.  Spans that end
 // where runs do, with nothing to join, took 12 us against 6 + 4 at 1024 tokens of 512.
 #include <algorithm>
+#include <type_traits>
 
 #include "mol_kernels.h"
 
@@ -46,7 +47,7 @@ constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSortU = 8;             // loads in flight
 constexpr int kMinBits = 8, kMaxBits = 11;   // digit of a radix pass
 constexpr int kSortBlock = kSortThreads * kSortU;   // tokens a block takes at least
-constexpr int kSortBlocks = 128;      // blocks at most (a row of counts is a multiple of 4)
+constexpr int kSortBlocks = 128;      // blocks at most
 
 template <typename T>
 struct Elem;
@@ -206,11 +207,10 @@ __device__ __forceinline__ uint2 token(const int32_t* __restrict__ ids, const ui
   return in ? in[i] : make_uint2(key_of(ids[i], V), static_cast<uint32_t>(i));
 }
 
-// counts[bin][block] of the digit at `shift`, rows of nbp (zero past the blocks)
+// counts[block][bin] of the digit at `shift`
 __global__ __launch_bounds__(kSortThreads) void k_sort_hist(const int32_t* __restrict__ ids,
                                                             const uint2* __restrict__ in, long T, int V, int per,
-                                                            int shift, int bits, int nbp,
-                                                            uint32_t* __restrict__ counts) {
+                                                            int shift, int bits, uint32_t* __restrict__ counts) {
   __shared__ uint32_t hist[1 << kMaxBits];
   const int bins = 1 << bits;
   for (int i = threadIdx.x; i < bins; i += kSortThreads) hist[i] = 0;
@@ -225,8 +225,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_hist(const int32_t* __res
       if (b + u * kSortThreads < i1) atomicAdd(&hist[(k[u] >> shift) & (bins - 1)], 1u);
   }
   __syncthreads();
-  // (the grid has nbp blocks: those past the tokens count nothing)
-  for (int i = threadIdx.x; i < bins; i += kSortThreads) counts[static_cast<long>(i) * nbp + blockIdx.x] = hist[i];
+  for (int i = threadIdx.x; i < bins; i += kSortThreads) counts[static_cast<long>(blockIdx.x) * bins + i] = hist[i];
 }
 
 // Stable scatter of one pass: wave w of block j takes the w-th part of the
@@ -235,11 +234,14 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_hist(const int32_t* __res
 template <int BITS>
 __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(const int32_t* __restrict__ ids,
                                                                const uint2* __restrict__ in, long T, int V, int per,
-                                                               int shift, int nbp,
+                                                               int shift, int nb,
                                                                const uint32_t* __restrict__ counts,
                                                                uint2* __restrict__ out) {
-  constexpr int bins = 1 << BITS, PT = bins / kSortThreads, UN = 16 / PT;   // thread tid has bins PT tid ..
+  constexpr int bins = 1 << BITS, PT = bins / kSortThreads;          // thread tid has bins PT tid ..
+  // a wave adds the counts of 256 bins (and of 256 more), four a lane, over a part of the blocks
+  constexpr int kGroups = bins / 256, kParts = kGroups < kSortWaves ? kSortWaves / kGroups : 1;
   __shared__ uint32_t hist[kSortWaves][bins];
+  __shared__ __attribute__((aligned(16))) uint32_t sums[2][kParts][bins];
   __shared__ uint32_t carry[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int mine = blockIdx.x;
@@ -252,14 +254,38 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_scatter(const int32_t* __
   };
   fetch(i0);
   // totals of every bin and those of the blocks before
+#pragma unroll
+  for (int grp = w / kParts; grp < kGroups; grp += kSortWaves / kParts) {
+    const int part = w % kParts, j0 = nb * part / kParts, j1 = nb * (part + 1) / kParts;
+    uint4 t = make_uint4(0, 0, 0, 0), f = t;
+    auto add = [&](auto width) {
+      constexpr int U = decltype(width)::value;
+      for (int j = j0; j < j1; j += U) {
+        uint4 n[U];                                                    // (other XCDs' counts: a trip past L2)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          n[u] = *reinterpret_cast<const uint4*>(counts + static_cast<long>(min(j + u, j1 - 1)) * bins + grp * 256 + 4 * lane);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const uint32_t in_t = j + u < j1 ? 0xFFFFFFFFu : 0u, in_f = j + u < min(j1, mine) ? 0xFFFFFFFFu : 0u;
+          t = make_uint4(t.x + (n[u].x & in_t), t.y + (n[u].y & in_t), t.z + (n[u].z & in_t), t.w + (n[u].w & in_t));
+          f = make_uint4(f.x + (n[u].x & in_f), f.y + (n[u].y & in_f), f.z + (n[u].z & in_f), f.w + (n[u].w & in_f));
+        }
+      }
+    };
+    if (j1 - j0 <= 4) add(std::integral_constant<int, 4>());
+    else add(std::integral_constant<int, 32>());
+    *reinterpret_cast<uint4*>(&sums[0][part][grp * 256 + 4 * lane]) = t;
+    *reinterpret_cast<uint4*>(&sums[1][part][grp * 256 + 4 * lane]) = f;
+  }
+  __syncthreads();
   uint32_t tot[PT] = {}, before[PT] = {};
-#pragma unroll UN
-  for (int j = 0; j < nbp; j += 4)
+#pragma unroll
+  for (int part = 0; part < kParts; ++part)
 #pragma unroll
     for (int k = 0; k < PT; ++k) {
-      const uint4 n = *reinterpret_cast<const uint4*>(counts + static_cast<long>(PT * tid + k) * nbp + j);
-      tot[k] += (n.x + n.y) + (n.z + n.w);
-      before[k] += (j < mine ? n.x : 0) + (j + 1 < mine ? n.y : 0) + (j + 2 < mine ? n.z : 0) + (j + 3 < mine ? n.w : 0);
+      tot[k] += sums[0][part][PT * tid + k];
+      before[k] += sums[1][part][PT * tid + k];
     }
 #pragma unroll
   for (int k = 0; k < PT; ++k)
@@ -606,16 +632,15 @@ static hipError_t launch_sort(const int32_t* ids, long T, int V, uint2* a, uint2
   }
   const int bits = key_bits(V);
   const int passes = (bits + kMaxBits - 1) / kMaxBits, each = std::max(kMinBits, (bits + passes - 1) / passes);
-  const int per = sort_per(T), nb = static_cast<int>((T + per - 1) / per), nbp = (nb + 3) / 4 * 4;
+  const int per = sort_per(T), nb = static_cast<int>((T + per - 1) / per);
   auto scatter = each == 8 ? &k_sort_scatter<8> : each == 9 ? &k_sort_scatter<9> : each == 10 ? &k_sort_scatter<10>
                                                                                               : &k_sort_scatter<11>;
   // the last pass ends in `a`
   const uint2* in = nullptr;
   for (int p = 0; p < passes; ++p) {
     uint2* to = (passes - p) % 2 ? a : b;
-    hipLaunchKernelGGL(k_sort_hist, dim3(nbp), dim3(kSortThreads), 0, st, ids, in, T, V, per, p * each, each, nbp,
-                       counts);
-    hipLaunchKernelGGL(scatter, dim3(nb), dim3(kSortThreads), 0, st, ids, in, T, V, per, p * each, nbp, counts, to);
+    hipLaunchKernelGGL(k_sort_hist, dim3(nb), dim3(kSortThreads), 0, st, ids, in, T, V, per, p * each, each, counts);
+    hipLaunchKernelGGL(scatter, dim3(nb), dim3(kSortThreads), 0, st, ids, in, T, V, per, p * each, nb, counts, to);
     in = to;
   }
   return hipGetLastError();
