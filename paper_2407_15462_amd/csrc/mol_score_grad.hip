@@ -45,6 +45,7 @@ using namespace grad;
 namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves, kPairs = 16 * kWaves;
+constexpr int kSumFloats = kWaves * 2 * 4 * 256;     // of the waves' sums in LDS: four blocks of two matrices
 // Of a slab's ds and partial sums: a million pairs of 64 components, whose
 // ds alone is 268 MB (see the bf16 form).
 constexpr size_t kSlabBytes = size_t(288) << 20;
@@ -419,45 +420,49 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims
     }
   }
 
-  // the workgroup's sums in LDS, in the place of the rest: in round r wave w adds
-  // its eighth (w + r) % 8, so that every wave has work in each
-  float* acc = smf;                                                    // [2][JTG][PT][64][4], then [JTG][16], then [TI][PV]
-#pragma unroll
-  for (int jj = 0; jj < JTG; ++jj) ab1[jj] = sum_groups(ab1[jj]);
-#pragma unroll 1
-  for (int r = 0; r < kWaves; ++r) {
-    const int part = (wave + r) & (kWaves - 1);
-    __syncthreads();
-#pragma unroll
-    for (int jj = 0; jj < JTG; ++jj)
-#pragma unroll
-      for (int pt = 0; pt < PT; ++pt)
-        if (part == (jj * PT + pt) % kWaves) {
-          f32x4_t* a = reinterpret_cast<f32x4_t*>(acc) + (jj * PT + pt) * 64 + lane;
-          f32x4_t* b = a + JTG * PT * 64;
-          const f32x4_t a0 = *a, b0 = *b;
-          *a = r ? a0 + aw1[jj][pt] : aw1[jj][pt];
-          *b = r ? b0 + aw2[jj][pt] : aw2[jj][pt];
-        }
-#pragma unroll
-    for (int jj = 0; jj < JTG; ++jj)
-      if (part == jj % kWaves) {
-        float* o = acc + 2 * JTG * PT * 256 + 16 * jj + c;
-        if (g == 0) *o = r ? *o + ab1[jj] : ab1[jj];
-      }
-  }
+  // the workgroup's sums, in the place of the rest: four blocks of dW1 and of dW2 of
+  // every wave at a time ([wave][2][4][64][4]), added and stored by four elements a thread
+  float* acc = smf;
+  float* acc1 = smf + kSumFloats;                                      // [wave][JTG][16] of db1
+  const int live_tiles = min(JTG, JT - dm.group * JTG);
   __syncthreads();
-  for (int i = tid; i < JTG * PT * 256; i += kThreads) {
-    // block (jj, pt), lane l, register r: row 4 (l / 16) + r, column l % 16
-    const int r = i & 3, l = (i >> 2) & 63, blk = i >> 8, jj = blk / PT, pt = blk - jj * PT;
-    const int row = 4 * (l >> 4) + r, colm = l & 15, jb = 16 * (dm.group * JTG + jj);
-    const int j1 = jb + row, p1 = 16 * pt + colm, j2 = jb + colm, p2 = 16 * pt + row;
-    if (j1 < H && p1 < P) out.dW1[(wg * H + j1) * P + p1] = acc[i];
-    if (j2 < H && p2 < P) out.dW2[(wg * P + p2) * H + j2] = acc[JTG * PT * 256 + i];
+#pragma unroll
+  for (int jj = 0; jj < JTG; ++jj) {
+    const float t = sum_groups(ab1[jj]);
+    if (g == 0) acc1[(wave * JTG + jj) * 16 + c] = t;
+  }
+#pragma unroll
+  for (int b0 = 0; b0 < JTG * PT; b0 += 4) {
+    if (b0 >= live_tiles * PT) break;
+    if (b0) __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      f32x4_t* to = reinterpret_cast<f32x4_t*>(acc) + (wave * 8 + k) * 64 + lane;
+      to[0] = aw1[(b0 + k) / PT][(b0 + k) % PT];
+      to[256] = aw2[(b0 + k) / PT][(b0 + k) % PT];
+    }
+    __syncthreads();
+    f32x4_t t = {};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) t += reinterpret_cast<const f32x4_t*>(acc)[w * 512 + tid];
+    // (block (jj, pt) of matrix `which`; element r of lane l: row 4 (l / 16) + r, column l % 16)
+    const int which = tid >> 8, blk = b0 + ((tid >> 6) & 3), jj = blk / PT, pt = blk - jj * PT;
+    const int row = 4 * g, jb = 16 * (dm.group * JTG + jj);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int j = which ? jb + c : jb + row + r, p = which ? 16 * pt + row + r : 16 * pt + c;
+      if (j < H && p < P) {
+        if (which) out.dW2[(wg * P + p) * H + j] = t[r];
+        else out.dW1[(wg * H + j) * P + p] = t[r];
+      }
+    }
   }
   for (int i = tid; i < 16 * JTG; i += kThreads) {
     const int j = 16 * dm.group * JTG + i;
-    if (j < H) out.db1[wg * H + j] = acc[2 * JTG * PT * 256 + i];
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) t += acc1[w * JTG * 16 + i];
+    if (j < H) out.db1[wg * H + j] = t;
   }
   if (dm.group) return;
   // db2: da_x summed over the items, then over the waves
@@ -730,8 +735,8 @@ GradPlan plan_grad(const DevProb& pr) {
   f.wlds = grad_lds<PV>(f.JT, true, f.ulds, dm) <= most;
   if (!f.wlds) f.ulds = grad_lds<PV>(f.JT, false, true, dm) <= most;
   f.lds = grad_lds<PV>(f.JT, f.wlds, f.ulds, dm) * 4;
-  // the final sums take the same place: JTG blocks of dW1, dW2 and db1, then [TI][PV + 1] of da_x
-  f.lds = std::max<size_t>(f.lds, 4 * (2ul * group_tiles<PV>() * (PV / 16) * 256 + 16 * group_tiles<PV>()));
+  // the final sums take the same place: dW1 and dW2 by four blocks, db1, then [TI][PV + 1] of da_x
+  f.lds = std::max<size_t>(f.lds, 4 * (kSumFloats + 16ul * kWaves * group_tiles<PV>()));
   f.lds = std::max<size_t>(f.lds, 4ul * dm.TI * (PV + 1));
   // of ds, and of what a tile's workgroup leaves: dW1, dW2 and u
   const long per_item = 4l * pr.Px * dm.m + (8l * pr.H * pr.P + (f.ulds ? 0 : 1024l * kWaves * f.JT)) / dm.TI;
