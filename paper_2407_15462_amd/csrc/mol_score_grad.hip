@@ -231,58 +231,61 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims
     const int b = b0 + q;
     const bool live = q < nq && has_item;
     const float gr = live ? dphi[static_cast<long>(b) * N + dm.n0 + slot] : 0.f;
-    // 1. dot products: jobs of (item component, 32 items, 32 vector rows)
-    const int nvec = nq * pr.Pq, nrt = (nvec + 31) / 32, nct = TI / 32;
+    // 1. dot products: jobs of (item component, 16 R items, 16 R vector rows)
+    constexpr int R = PV == 16 ? 1 : 2;                                // (few components: as many jobs as waves)
+    const int nvec = nq * pr.Pq, nrt = (nvec + 16 * R - 1) / (16 * R), nct = TI / (16 * R);
     for (int job = wave; job < pr.Px * nrt * nct; job += kWaves) {
       const int ct = job % nct, jr = job / nct, px = jr / nrt, rt = jr - px * nrt;
-      const T* qv = Q + static_cast<long>(b0) * pr.Pq * d;
-      const T* q0 = qv + static_cast<long>(min(32 * rt + c, nvec - 1)) * d;
-      const T* q1 = qv + static_cast<long>(min(32 * rt + 16 + c, nvec - 1)) * d;
-      const T* Xp = X + static_cast<long>(px) * N * d;
-      const T* x0 = Xp + static_cast<long>(item_of(32 * ct + c)) * d;
-      const T* x1 = Xp + static_cast<long>(item_of(32 * ct + 16 + c)) * d;
-      f32x4_t acc[2][2] = {};
+      const T *qr[R], *xr[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        qr[r] = Q + (static_cast<long>(b0) * pr.Pq + min(16 * (R * rt + r) + c, nvec - 1)) * d;
+        xr[r] = X + (static_cast<long>(px) * N + item_of(16 * (R * ct + r) + c)) * d;
+      }
+      f32x4_t acc[R][R] = {};
       int k0 = 0;
       if constexpr (PV < 64) {
         // (registers for four chunks in flight)
         for (; k0 + 4 * KCH <= d; k0 += 4 * KCH) {
-          uint4 x[4][2], y[4][2];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int t = k0 + e * KCH + g * E;
-            x[e][0] = row16<T, VEC>(x0, t, d);
-            x[e][1] = row16<T, VEC>(x1, t, d);
-            y[e][0] = row16<T, VEC>(q0, t, d);
-            y[e][1] = row16<T, VEC>(q1, t, d);
-          }
+          uint4 x[4][R], y[4][R];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
+            for (int r = 0; r < R; ++r) {
+              x[e][r] = row16<T, VEC>(xr[r], k0 + e * KCH + g * E, d);
+              y[e][r] = row16<T, VEC>(qr[r], k0 + e * KCH + g * E, d);
+            }
 #pragma unroll
-              for (int h = 0; h < 2; ++h) acc[r][h] = mma16<T>(y[e][r], x[e][h], acc[r][h]);
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+              for (int h = 0; h < R; ++h) acc[r][h] = mma16<T>(y[e][r], x[e][h], acc[r][h]);
         }
       }
       for (; k0 < d; k0 += KCH) {
-        const int t = k0 + g * E;
-        const uint4 xa = row16<T, VEC>(x0, t, d), xb = row16<T, VEC>(x1, t, d);
-        const uint4 qa = row16<T, VEC>(q0, t, d), qc = row16<T, VEC>(q1, t, d);
-        acc[0][0] = mma16<T>(qa, xa, acc[0][0]);
-        acc[0][1] = mma16<T>(qa, xb, acc[0][1]);
-        acc[1][0] = mma16<T>(qc, xa, acc[1][0]);
-        acc[1][1] = mma16<T>(qc, xb, acc[1][1]);
+        uint4 x[R], y[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          x[r] = row16<T, VEC>(xr[r], k0 + g * E, d);
+          y[r] = row16<T, VEC>(qr[r], k0 + g * E, d);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int h = 0; h < R; ++h) acc[r][h] = mma16<T>(y[r], x[h], acc[r][h]);
       }
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int v = 32 * rt + 16 * r + 4 * g;
+      for (int r = 0; r < R; ++r) {
+        const int v = 16 * (R * rt + r) + 4 * g;
         const int4 row = *reinterpret_cast<const int4*>(sRow + v);
         const int ro[4] = {row.x, row.y, row.z, row.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (v + i < nvec) {
-            float* dst = sS + ro[i] + px * TIP + 32 * ct + c;
-            dst[0] = acc[r][0][i];
-            dst[16] = acc[r][1][i];
+            float* dst = sS + ro[i] + px * TIP + 16 * R * ct + c;
+#pragma unroll
+            for (int h = 0; h < R; ++h) dst[16 * h] = acc[r][h][i];
           }
       }
     }
