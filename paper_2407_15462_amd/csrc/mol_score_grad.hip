@@ -29,10 +29,10 @@
 //
 // What bounds it: the f32 matrix rate, 12 P H + 2 P d flop a pair, and for few pairs
 // the latencies of a workgroup's one or two tiles (weights, dot products, the
-// chain and back, the sums: 55 us at P = H = 64).  Measured in float32: 32 x 129
-// pairs of 4 x 4, H = 32 16 + 6 + 5 us (pairs, products, sums), 26 a call; 200 x 4000 of
-// them 175 + 58 + 14 (pairs at 48 TFLOP/s, a large product at 144); 8 x 6112 of
-// 8 x 8, H = 64 70 + 23 + 8.
+// chain and back, the sums: 50 us at P = H = 64).  Measured in float32: 32 x 129
+// pairs of 4 x 4, H = 32 13 + 6 + 5 us (pairs, products, sums), 24 a call; 200 x 4000 of
+// them 131 + 58 + 14 (pairs at 50 TFLOP/s, a large product at 144); 8 x 6112 of
+// 8 x 8, H = 64 69 + 23 + 8.
 #include <algorithm>
 
 #include "mol_grad.h"
@@ -50,8 +50,13 @@ constexpr int kSumFloats = kWaves * 2 * 4 * 256;     // of the waves' sums in LD
 // ds alone is 268 MB (see the bf16 form).
 constexpr size_t kSlabBytes = size_t(288) << 20;
 
+// JTG, blocks of 16 hidden units whose sums a workgroup keeps.  Up to 64 units of up to 16
+// components leave registers for a second workgroup on the CU (launch bounds of four waves
+// a SIMD): one's dot products run beside the other's chain (200 x 4000: 161 -> 131 us).
 template <int PV>
-constexpr int group_tiles() { return PV == 64 ? 4 : 8; }   // JTG
+constexpr int group_tiles(bool few) { return PV == 64 || (PV == 16 && few) ? 4 : 8; }
+template <int PV, int JTG>
+constexpr int wgs_per_cu() { return PV == 16 && JTG == 4 ? 2 : 1; }
 
 __device__ __forceinline__ f32x4_t mfma_f32(float a, float b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -160,11 +165,11 @@ __global__ __launch_bounds__(256) void k_grad_weights(DevProb pr, int JT, float*
                            blk / op_tiles<PV>(), blk % op_tiles<PV>(), lane, e);
 }
 
-template <typename T, int PV, bool VEC>
-__global__ __launch_bounds__(kThreads, 2) void k_score_grad(DevProb pr, GradDims dm, const float* __restrict__ dphi,
+template <typename T, int PV, bool VEC, int JTG>
+__global__ __launch_bounds__(kThreads, (2 * wgs_per_cu<PV, JTG>())) void k_score_grad(DevProb pr, GradDims dm, const float* __restrict__ dphi,
                                                             const float* __restrict__ wglob,
                                                             float* __restrict__ uglob, GradParts out) {
-  constexpr int RUN = PV / 4, PT = PV / 16, E = 16 / sizeof(T), KCH = 4 * E, JTG = group_tiles<PV>();
+  constexpr int RUN = PV / 4, PT = PV / 16, E = 16 / sizeof(T), KCH = 4 * E;
   extern __shared__ __attribute__((aligned(16))) float smf[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -712,7 +717,7 @@ namespace {
 
 struct GradPlan {
   GradDims dm;
-  int JT, groups, slab, slabs;
+  int JT, jtg, groups, slab, slabs;
   bool wlds, ulds;                      // prepared weights and the units' u in LDS
   size_t lds;
   int sp_q, sp_x;                       // K splits of dQ and dX
@@ -725,7 +730,8 @@ template <typename T, int PV>
 GradPlan plan_grad(const DevProb& pr) {
   GradPlan f{};
   f.JT = (pr.H + 15) / 16;
-  f.groups = (f.JT + group_tiles<PV>() - 1) / group_tiles<PV>();
+  f.jtg = group_tiles<PV>(f.JT <= 4);
+  f.groups = (f.JT + f.jtg - 1) / f.jtg;
   GradDims& dm = f.dm;
   dm.QB = pr.B >= 4 ? 4 : pr.B >= 2 ? 2 : 1;
   dm.upq_log2 = dm.QB == 4 ? 1 : dm.QB == 2 ? 2 : 3;
@@ -739,7 +745,7 @@ GradPlan plan_grad(const DevProb& pr) {
   if (!f.wlds) f.ulds = grad_lds<PV>(f.JT, false, true, dm) <= most;
   f.lds = grad_lds<PV>(f.JT, f.wlds, f.ulds, dm) * 4;
   // the final sums take the same place: dW1 and dW2 by four blocks, db1, then [TI][PV + 1] of da_x
-  f.lds = std::max<size_t>(f.lds, 4 * (kSumFloats + 16ul * kWaves * group_tiles<PV>()));
+  f.lds = std::max<size_t>(f.lds, 4 * (kSumFloats + 16ul * kWaves * f.jtg));
   f.lds = std::max<size_t>(f.lds, 4ul * dm.TI * (PV + 1));
   // of ds, and of what a tile's workgroup leaves: dW1, dW2 and u
   const long per_item = 4l * pr.Px * dm.m + (8l * pr.H * pr.P + (f.ulds ? 0 : 1024l * kWaves * f.JT)) / dm.TI;
@@ -750,7 +756,8 @@ GradPlan plan_grad(const DevProb& pr) {
   f.slabs = static_cast<int>((static_cast<long>(pr.N) + f.slab - 1) / f.slab);
   dm.ns = f.slab;
   const int st = f.slab / dm.TI, nqb = (pr.B + dm.QB - 1) / dm.QB;
-  dm.qsplits = std::max(1, std::min(nqb, 256 / st));
+  const int cus = PV == 16 && f.jtg == 4 && f.lds <= 80 * 1024 ? 512 : 256;   // workgroups that run at once
+  dm.qsplits = std::max(1, std::min(nqb, cus / st));
   f.wgs = st * dm.qsplits;
   constexpr int KCH = 64 / sizeof(T), kLeast = 128 / KCH;   // 128 items or query vectors
   const long cg = (pr.d + 63) / 64;
@@ -799,7 +806,9 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
                    ((reinterpret_cast<uintptr_t>(pr.Q) | reinterpret_cast<uintptr_t>(pr.X)) & 15) == 0;
   const T* X = static_cast<const T*>(pr.X);
   const T* Q = static_cast<const T*>(pr.Q);
-  auto kern = vec ? &k_score_grad<T, PV, true> : &k_score_grad<T, PV, false>;
+  constexpr int few = group_tiles<PV>(true), many = group_tiles<PV>(false);
+  auto kern = f.jtg == few ? (vec ? &k_score_grad<T, PV, true, few> : &k_score_grad<T, PV, false, few>)
+                           : (vec ? &k_score_grad<T, PV, true, many> : &k_score_grad<T, PV, false, many>);
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
                                      static_cast<int>(f.lds));
   if (e != hipSuccess) return e;
