@@ -153,6 +153,7 @@ struct Bf16Dims {
   int n0, ns, items; // the slab's first item, its padded length (a multiple of 32) and its items
   int nb;            // its blocks of 16
   int qsplits;       // query ranges
+  int kl;            // blocks of 32 of d that the items' rows have in LDS
   long m;            // B Pq
 };
 struct Bf16Parts {
@@ -174,13 +175,13 @@ template <int RUN>
 constexpr int weight_bytes() { return 2 * kH * 4 * RUN * 2; }
 template <int RUN>
 constexpr int lds_bytes() { return weight_bytes<RUN>() + kWaves * wave_bytes<RUN>(); }
-// Bytes of the items' rows in LDS, [px][d / 8, whole K blocks][16 items][16 bytes]
-inline int x_bytes(int pxp, int d) { return pxp * ((d + 31) / 32 * 4) * 256; }
+// Bytes of a block of 32 of the items' rows in LDS, [px][4][16 items][16 bytes]
+constexpr int x_bytes(int pxp) { return pxp * 1024; }
 static_assert(lds_bytes<4>() >= 4 * kWaves * 16 * 16 && lds_bytes<16>() >= 4 * kWaves * 16 * 64, "the sums of da_x fit");
 
 }  // namespace
 
-// XL: the workgroup's waves share 16 items, whose rows lie in LDS.  FULL 1 or 2: P_q = 4
+// XL: the workgroup's waves share 16 items, whose rows lie in LDS, as far as there is room.  FULL 1 or 2: P_q = 4
 // NPQ, P_x = PXP, every row allows 16-byte reads (H a multiple of 4) and H is
 // at most 32 or 64: no branches in a unit, which leaves its order to the compiler.
 template <int NPQ, int PXP, bool XL, int FULL>
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g = lane >> 4;
-  const int P = pr.P, H = pr.H, d = pr.d, N = pr.N, JT2 = FULL ? FULL : (H + 31) / 32, nch = (d + 31) / 32 * 4;
+  const int P = pr.P, H = pr.H, d = pr.d, N = pr.N, JT2 = FULL ? FULL : (H + 31) / 32, nch = 4 * dm.kl;
   const int Pq = FULL ? 4 * NPQ : pr.Pq, Px = FULL ? PXP : pr.Px;
   unsigned char* sW1 = smb;
   unsigned char* sW2 = sW1 + 2 * kH * SLOTS;
@@ -304,19 +305,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
       f32x4_t acc[PXP] = {};
       const bf16_t* Q = static_cast<const bf16_t*>(pr.Q) + static_cast<long>(b) * Pq * d;
       const uint32_t qo = fresh(q_off), xo = fresh(x_off);
-      auto block = [&](int k, uint4 qv) {                             // (zeros of Q past d meet X's own, finite, elements)
+      auto block = [&](int k, uint4 qv, bool lds) {                   // (zeros of Q past d meet X's own, finite, elements)
         uint4 xv[PXP];
         const bf16_t* Xp = X;
 #pragma unroll
         for (int px = 0; px < PXP; ++px, Xp += px < Px ? x_px : 0)
-          xv[px] = XL ? sX[(px * nch + 4 * k + g) * 16 + c] : row16(Xp, xo, 32 * k + 8 * g, false);
+          xv[px] = lds ? sX[(px * nch + 4 * k + g) * 16 + c] : row16(Xp, xo, 32 * k + 8 * g, false);
 #pragma unroll
         for (int px = 0; px < PXP; ++px) acc[px] = mfma_bf16(qv, xv[px], acc[px]);
       };
 #pragma unroll
       for (int k = 0; k < kAhead; ++k)
-        if (32 * k < d) block(k, qf[k]);
-      for (int k = kAhead; 32 * k < d; ++k) block(k, row16(Q, qo, 32 * k + 8 * g, true));
+        if (32 * k < d) block(k, qf[k], XL);
+      int k = kAhead;
+      if constexpr (XL)
+        for (; k < dm.kl; ++k) block(k, row16(Q, qo, 32 * k + 8 * g, true), true);
+      for (; 32 * k < d; ++k) block(k, row16(Q, qo, 32 * k + 8 * g, true), false);
 #pragma unroll
       for (int px = 0; px < PXP; ++px)
 #pragma unroll
@@ -836,16 +840,18 @@ Bf16Plan plan(const DevProb& pr) {
 }
 
 template <int NPQ, int PXP>
-hipError_t launch_pairs(const DevProb& pr, const Bf16Plan& f, const Bf16Dims& dm, const float* dphi,
+hipError_t launch_pairs(const DevProb& pr, const Bf16Plan& f, Bf16Dims dm, const float* dphi,
                         const Bf16Parts& parts, hipStream_t st) {
   auto aligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
   const bool full = pr.Pq == 4 * NPQ && pr.Px == PXP && pr.d % 8 == 0 && aligned(pr.Q) && aligned(pr.X) && aligned(pr.a_q) &&
                     aligned(pr.a_x) && aligned(pr.b1) && aligned(pr.b2) && pr.H % 4 == 0;
-  // the items' rows in LDS where the workgroup has one block of items and there is room
-  constexpr int base = lds_bytes<NPQ * PXP>();
-  static_assert(base <= 160 * 1024, "LDS");
-  const bool xl = dm.QB == kWaves && base + x_bytes(PXP, pr.d) <= 160 * 1024;
-  const int lds = base + (xl ? x_bytes(PXP, pr.d) : 0);
+  // the items' rows in LDS where the workgroup has one block of items: whole, or the first
+  // blocks of 32 that there is room for (the loaded-ahead ones at least)
+  constexpr int base = lds_bytes<NPQ * PXP>(), room = (160 * 1024 - base) / x_bytes(PXP);
+  static_assert(room >= kAhead, "LDS");
+  const bool xl = dm.QB == kWaves;
+  dm.kl = xl ? std::min((pr.d + 31) / 32, room) : 0;
+  const int lds = base + dm.kl * x_bytes(PXP);
   const int form = !full ? 0 : pr.H <= 32 ? 1 : 2;
   auto kern = xl ? (form == 2   ? &k_score_grad_bf16<NPQ, PXP, true, 2>
                     : form == 1 ? &k_score_grad_bf16<NPQ, PXP, true, 1>
