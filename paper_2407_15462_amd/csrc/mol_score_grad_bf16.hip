@@ -1,5 +1,5 @@
-// Gradient of the MoL scores for bf16 problems of up to 8 x 8 components and
-// 64 hidden units, on bf16 matrix instructions (mol_score_grad.hip has the
+// Gradient of the MoL scores for bf16 problems of up to 8 x 8 components and 64
+// hidden units, or 8 x 4 and 128, on bf16 matrix instructions (mol_score_grad.hip has the
 // formulas and every other shape).
 //
 // Precision.  W1 and W2 are bf16, exact.  What meets them on the way to the
@@ -52,7 +52,7 @@ constexpr int kWaves = 8, kThreads = 64 * kWaves;
 // workgroups fill 220 of the 256 CUs, 882).
 constexpr size_t kSlabBytes = size_t(288) << 20;
 constexpr int kAhead = 2;                          // blocks of 32 of d loaded ahead
-constexpr int kJT = 4;                             // hidden tiles of 16
+constexpr int kJT = 4;                             // hidden tiles of 16 that LDS holds h and du of
 constexpr int kH = 16 * kJT;
 
 // high halves of a and b: their first bf16 terms by truncation
@@ -171,23 +171,26 @@ struct Bf16Parts {
 template <int RUN>
 constexpr int wave_bytes() { return 1024 * (2 * (RUN / 4) + 2 * kJT); }
 // W1 [j][slot] and W2 [slot][j], rows without padding
-template <int RUN>
-constexpr int weight_bytes() { return 2 * kH * 4 * RUN * 2; }
-template <int RUN>
-constexpr int lds_bytes() { return weight_bytes<RUN>() + kWaves * wave_bytes<RUN>(); }
+template <int RUN, int HALVES>
+constexpr int weight_bytes() { return 2 * HALVES * kH * 4 * RUN * 2; }
+template <int RUN, int HALVES>
+constexpr int lds_bytes() { return weight_bytes<RUN, HALVES>() + kWaves * wave_bytes<RUN>(); }
 // Bytes of a block of 32 of the items' rows in LDS, [px][4][16 items][16 bytes]
 constexpr int x_bytes(int pxp) { return pxp * 1024; }
-static_assert(lds_bytes<4>() >= 4 * kWaves * 16 * 16 && lds_bytes<16>() >= 4 * kWaves * 16 * 64, "the sums of da_x fit");
+static_assert(lds_bytes<4, 1>() >= 4 * kWaves * 16 * 16 && lds_bytes<16, 1>() >= 4 * kWaves * 16 * 64, "the sums of da_x fit");
 
 }  // namespace
 
 // XL: the workgroup's waves share 16 items, whose rows lie in LDS, as far as there is room.  FULL 1 or 2: P_q = 4
 // NPQ, P_x = PXP, every row allows 16-byte reads (H a multiple of 4) and H is
-// at most 32 or 64: no branches in a unit, which leaves its order to the compiler.
-template <int NPQ, int PXP, bool XL, int FULL>
+// at most 32 FULL: no branches in a unit, which leaves its order to the compiler.
+// HALVES 2: 65 to 128 hidden units.  u stays in registers on the way forward, and the way
+// back takes 64 of them at a time: h and du of those to LDS, and their part of dW1 and dW2
+// (512 x 2000 pairs of 8 x 4, d = H = 128: 339 us, 831 in the general form).
+template <int NPQ, int PXP, bool XL, int FULL, int HALVES>
 __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf16Dims dm,
                                                                  const float* __restrict__ dphi, Bf16Parts out) {
-  constexpr int RUN = NPQ * PXP, SLOTS = 4 * RUN, PT = RUN / 4, KB = RUN > 8 ? RUN / 8 : 1;
+  constexpr int RUN = NPQ * PXP, SLOTS = 4 * RUN, PT = RUN / 4, KB = RUN > 8 ? RUN / 8 : 1, HU = HALVES * kH;
   extern __shared__ __attribute__((aligned(16))) unsigned char smb[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -195,8 +198,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
   const int P = pr.P, H = pr.H, d = pr.d, N = pr.N, JT2 = FULL ? FULL : (H + 31) / 32, nch = 4 * dm.kl;
   const int Pq = FULL ? 4 * NPQ : pr.Pq, Px = FULL ? PXP : pr.Px;
   unsigned char* sW1 = smb;
-  unsigned char* sW2 = sW1 + 2 * kH * SLOTS;
-  unsigned char* waves = sW2 + 2 * kH * SLOTS;
+  unsigned char* sW2 = sW1 + 2 * HU * SLOTS;
+  unsigned char* waves = sW2 + 2 * HU * SLOTS;
   unsigned char* mine = waves + wave * wave_bytes<RUN>();
   unsigned char* sS = mine;                                           // s by tiles: first terms, second terms
   unsigned char* sD = sS + 1024 * PT;                                 // dl
@@ -210,7 +213,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
   // byte of an element of W1 (row j) and W2 (row a slot): the 8-byte pieces of a
   // row are rotated by two for each row, so that rows meet different banks
   auto w1_at = [](int j, int sl) { return j * (2 * SLOTS) + ((2 * sl + 16 * j) & (2 * SLOTS - 1)); };
-  auto w2_at = [](int sl, int j) { return sl * (2 * kH) + ((2 * j + 16 * sl) & (2 * kH - 1)); };
+  auto w2_at = [](int sl, int j) { return sl * (2 * HU) + ((2 * j + 16 * sl) & (2 * HU - 1)); };
   const bool vec = FULL || (d % 8 == 0 && ((reinterpret_cast<uintptr_t>(pr.Q) | reinterpret_cast<uintptr_t>(pr.X)) & 15) == 0);
   auto row16 = [&](const bf16_t* base, uint32_t off, int t, bool zero) {
     return vec ? row16_of<true>(base, off, t, d, zero) : row16_of<false>(base, off, t, d, zero);
@@ -229,7 +232,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
   {
     const bf16_t* W1 = static_cast<const bf16_t*>(pr.W1);
     const bf16_t* W2 = static_cast<const bf16_t*>(pr.W2);
-    for (int i = tid; i < kH * SLOTS; i += kThreads) {
+    for (int i = tid; i < HU * SLOTS; i += kThreads) {
       const int j = i / SLOTS, sl = i - j * SLOTS, p = component(sl);
       const bool in = j < H && p >= 0;
       *reinterpret_cast<bf16_t*>(sW1 + w1_at(j, sl)) = in ? W1[j * P + p] : 0;
@@ -255,7 +258,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
   constexpr int JW = PT == 4 ? 2 : 1, PW = PT == 1 ? 1 : 2;
   const int sub = wave & 3, j0 = PT == 4 ? 2 * (sub >> 1) : sub, pt0 = PT == 4 ? 2 * (sub & 1) : 0;
   const bool second = wave >= 4;
-  f32x4_t aw[JW][PW] = {}, ab1[kJT] = {};
+  f32x4_t aw[HALVES][JW][PW] = {}, ab1[HALVES * kJT] = {};
   float dax[RUN] = {};
   // what a unit reads from its query's rows, loaded a step ahead
   uint4 qf[kAhead];
@@ -274,6 +277,115 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
   for (int st = st0; st < st1; ++st) {
     const int b = st * dm.QB + q;
     const bool busy = has_blk && b < pr.B;                            // (the same for the whole wave)
+    Terms<3> a[KB];                                                   // of s, then of dl
+    f32x4_t ds[PT], ur[HALVES == 2 ? 2 * kJT : 1];
+    // back through 64 hidden units of the MLP
+    auto back = [&](int half) {
+#pragma unroll
+      for (int l2 = 0; l2 < kJT / 2; ++l2) {
+        const int j2 = half * (kJT / 2) + l2;
+        if (j2 >= JT2) break;
+        float du[8], h[8];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const int jt = 2 * j2 + hf;
+          f32x4_t dh = {};
+#pragma unroll
+          for (int m = 0; m < KB; ++m) {
+            // A row j = 16 jt + c, K = slots RUN g + 8 m + e: columns of W2's rows
+            const int sl = RUN * g + 8 * m + (c >> 2), j = 16 * jt + 4 * (c & 3);
+            const uint2 w0 = read_tr(sW2 + w2_at(sl, j));
+            const uint2 w1 = RUN >= 8 ? read_tr(sW2 + w2_at(sl + 4, j)) : make_uint2(0, 0);
+            dh = mfma_terms<3>(make_uint4(w0.x, w0.y, w1.x, w1.y), a[m], dh);
+          }
+          float kk[4];
+          if constexpr (HALVES == 1) {
+            const float4 k = *reinterpret_cast<const float4*>(sU + 1024 * jt + 16 * lane);
+            kk[0] = k.x, kk[1] = k.y, kk[2] = k.z, kk[3] = k.w;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float u = ur[jt][i], sig = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u));
+              h[4 * hf + i] = u * sig;
+              kk[i] = fmaf(h[4 * hf + i], 1.f - sig, sig);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            du[4 * hf + i] = dh[i] * kk[i];
+            ab1[jt][i] += du[4 * hf + i];
+          }
+        }
+        auto store_hidden = [&](unsigned char* to, const Terms<2>& x) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            *reinterpret_cast<uint2*>(to + 1024 * (2 * l2) + 512 * k + place(4 * g)) = make_uint2(x.t[k].x, x.t[k].y);
+            *reinterpret_cast<uint2*>(to + 1024 * (2 * l2 + 1) + 512 * k + place(4 * g)) = make_uint2(x.t[k].z, x.t[k].w);
+          }
+        };
+        const Terms<2> dt = split<2>(du);
+        store_hidden(sU, dt);                                         // (in the place of k, which the wave has read)
+        if constexpr (HALVES == 2) store_hidden(sH, split<2>(h));
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) {
+          // A row slot RUN (c / 4) + 4 pt + c % 4, K = j: columns of W1's rows
+          const int j = 32 * j2 + 4 * g + (c >> 2), sl = RUN * (c & 3) + 4 * pt;
+          const uint2 w0 = read_tr(sW1 + w1_at(j, sl)), w1 = read_tr(sW1 + w1_at(j + 16, sl));
+          ds[pt] = mfma_terms<2>(make_uint4(w0.x, w0.y, w1.x, w1.y), dt, ds[pt]);
+        }
+      }
+    };
+    // ds as two terms; lanes of a pair of items exchange them, the even one takes the first terms of both
+    auto store_ds = [&] {
+      const uint32_t pick = c & 1 ? 0x03020706u : 0x05040100u;        // (own word low in the permute)
+      uint32_t* to = out.ds + (static_cast<long>(blk) * dm.m + static_cast<long>(b) * Pq) * 16;
+      const uint32_t to_off = fresh(4u * (16 * NPQ * g + ((c & 1) << 3) + (c >> 1)));
+      const long px_step = static_cast<long>(dm.nb) * dm.m * 16;
+#pragma unroll
+      for (int px = 0; px < PXP; ++px, to += px_step)
+#pragma unroll
+      for (int i = 0; i < NPQ; ++i) {
+        const int mu = i * PXP + px;
+        const float v = ds[mu / 4][mu % 4];
+        const uint32_t hi = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+        const uint32_t lo = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v - __uint_as_float(hi << 16)));
+        const uint32_t own = hi | lo << 16;
+        const uint32_t other =                                         // quad_perm 1,0,3,2
+            static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(own), 0xB1, 0xf, 0xf, true));
+        // even: (own low, other low); odd: (other high, own high)
+        const uint32_t w = __builtin_amdgcn_perm(other, own, pick);
+        if (FULL || (NPQ * g + i < Pq && px < Px)) const_cast<uint32_t&>(at32(to, to_off + 64u * i)) = w;
+      }
+    };
+    // dW1 += du s^T, dW2^T += h dl^T over the eight units' items, two units a K block:
+    // slots 8 g + e are items 4 g + e % 4 of the one and the other
+    auto sum_weights = [&](int half) {
+      if (half * kJT + j0 >= 2 * JT2) return;
+      const unsigned char* u0 = waves + tr;
+      const unsigned char* pj = u0 + 1024 * (2 * PT + (second ? 0 : kJT) + j0);      // h or du
+      const unsigned char* pp = u0 + 1024 * ((second ? PT : 0) + pt0);               // dl or s
+#pragma unroll 1
+      for (int u = 0; u < kWaves; u += 2, pj += 2 * wave_bytes<RUN>(), pp += 2 * wave_bytes<RUN>()) {
+        uint4 fj[JW][2], fp[PW][2];
+        auto pair = [&](const unsigned char* at) {
+          const uint2 x = read_tr(at), y = read_tr(at + wave_bytes<RUN>());
+          return make_uint4(x.x, x.y, y.x, y.y);
+        };
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+          for (int j = 0; j < JW; ++j) fj[j][k] = pair(pj + 1024 * j + 512 * k);
+#pragma unroll
+          for (int i = 0; i < PW; ++i) fp[i][k] = pair(pp + 1024 * i + 512 * k);
+        }
+#pragma unroll
+        for (int k = 2; k >= 0; --k)                                  // small products first
+#pragma unroll
+          for (int j = 0; j < JW; ++j)
+#pragma unroll
+            for (int i = 0; i < PW; ++i) aw[half][j][i] = mfma_bf16(fj[j][k == 2], fp[i][k == 1], aw[half][j][i]);
+      }
+    };
     if (busy) {
     gr = has_item ? gr_next : 0.f;
     // a_q, a_x and b2, for l
@@ -328,11 +440,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
     }
     // forward
     // (b1 and b2 come from the caches each time: LDS and registers are full)
-    f32x4_t b1[kJT];
+    f32x4_t b1[HALVES * kJT];
     {
       const uint32_t go = fresh(16u * g);
 #pragma unroll
-      for (int jt = 0; jt < kJT; ++jt) {
+      for (int jt = 0; jt < HALVES * kJT; ++jt) {
         if constexpr (FULL) {
           const f32x4_t v = at32(reinterpret_cast<const f32x4_t*>(pr.b1), min(go + 64u * jt, 4u * H - 16u));
           b1[jt] = 16 * jt + 4 * g < H ? v : f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -349,7 +461,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
     for (int pt = 0; pt < PT; ++pt) {
       l[pt] = l[pt] + lx[pt] + b2[pt];
     }
-    Terms<3> a[KB];
     auto slots8 = [&](const float (&x)[RUN], int m) {
       float v[8];
 #pragma unroll
@@ -372,7 +483,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
     for (int m = 0; m < KB; ++m) a[m] = slots8(s, m);
     store_slots(sS);
 #pragma unroll
-    for (int j2 = 0; j2 < kJT / 2; ++j2) {
+    for (int j2 = 0; j2 < HALVES * kJT / 2; ++j2) {
       if (j2 >= JT2) break;
       float h[8];
 #pragma unroll
@@ -391,7 +502,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
           }
           u = mfma_terms<3>(w, a[m], u);
         }
-        float4 k;
+        if constexpr (HALVES == 2) ur[jt] = u;
         float kk[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -399,14 +510,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
           h[4 * hf + i] = u[i] * sig;
           kk[i] = fmaf(h[4 * hf + i], 1.f - sig, sig);                // sig (1 + u (1 - sig))
         }
-        k = float4{kk[0], kk[1], kk[2], kk[3]};
-        *reinterpret_cast<float4*>(sU + 1024 * jt + 16 * lane) = k;
+        if constexpr (HALVES == 1) *reinterpret_cast<float4*>(sU + 1024 * jt + 16 * lane) = float4{kk[0], kk[1], kk[2], kk[3]};
       }
       const Terms<3> ht = split<3>(h);
+      if constexpr (HALVES == 1) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        *reinterpret_cast<uint2*>(sH + 1024 * (2 * j2) + 512 * k + place(4 * g)) = make_uint2(ht.t[k].x, ht.t[k].y);
-        *reinterpret_cast<uint2*>(sH + 1024 * (2 * j2 + 1) + 512 * k + place(4 * g)) = make_uint2(ht.t[k].z, ht.t[k].w);
+        for (int k = 0; k < 2; ++k) {
+          *reinterpret_cast<uint2*>(sH + 1024 * (2 * j2) + 512 * k + place(4 * g)) = make_uint2(ht.t[k].x, ht.t[k].y);
+          *reinterpret_cast<uint2*>(sH + 1024 * (2 * j2 + 1) + 512 * k + place(4 * g)) = make_uint2(ht.t[k].z, ht.t[k].w);
+        }
       }
 #pragma unroll
       for (int pt = 0; pt < PT; ++pt) {
@@ -419,7 +531,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
     }
     // softmax, dl
     float dl[RUN];
-    f32x4_t ds[PT];
     {
       float mx = l[0][0];
 #pragma unroll
@@ -453,122 +564,47 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
       const int pq = NPQ * g + c / PXP, px = c % PXP;
       if (c < RUN && pq < Pq && px < Px) out.da_q[(static_cast<long>(blk) * pr.B + b) * P + pq * Px + px] = t;
     }
-    // back through the MLP
-#pragma unroll
-    for (int j2 = 0; j2 < kJT / 2; ++j2) {
-      if (j2 >= JT2) break;
-      float du[8];
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const int jt = 2 * j2 + hf;
-        f32x4_t dh = {};
-#pragma unroll
-        for (int m = 0; m < KB; ++m) {
-          // A row j = 16 jt + c, K = slots RUN g + 8 m + e: columns of W2's rows
-          const int sl = RUN * g + 8 * m + (c >> 2), j = 16 * jt + 4 * (c & 3);
-          const uint2 w0 = read_tr(sW2 + w2_at(sl, j));
-          const uint2 w1 = RUN >= 8 ? read_tr(sW2 + w2_at(sl + 4, j)) : make_uint2(0, 0);
-          dh = mfma_terms<3>(make_uint4(w0.x, w0.y, w1.x, w1.y), a[m], dh);
-        }
-        const float4 k = *reinterpret_cast<const float4*>(sU + 1024 * jt + 16 * lane);
-        const float kk[4] = {k.x, k.y, k.z, k.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          du[4 * hf + i] = dh[i] * kk[i];
-          ab1[jt][i] += du[4 * hf + i];
-        }
-      }
-      const Terms<2> dt = split<2>(du);
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {                                   // (in the place of k, which the wave has read)
-        *reinterpret_cast<uint2*>(sU + 1024 * (2 * j2) + 512 * k + place(4 * g)) = make_uint2(dt.t[k].x, dt.t[k].y);
-        *reinterpret_cast<uint2*>(sU + 1024 * (2 * j2 + 1) + 512 * k + place(4 * g)) = make_uint2(dt.t[k].z, dt.t[k].w);
-      }
-#pragma unroll
-      for (int pt = 0; pt < PT; ++pt) {
-        // A row slot RUN (c / 4) + 4 pt + c % 4, K = j: columns of W1's rows
-        const int j = 32 * j2 + 4 * g + (c >> 2), sl = RUN * (c & 3) + 4 * pt;
-        const uint2 w0 = read_tr(sW1 + w1_at(j, sl)), w1 = read_tr(sW1 + w1_at(j + 16, sl));
-        ds[pt] = mfma_terms<2>(make_uint4(w0.x, w0.y, w1.x, w1.y), dt, ds[pt]);
-      }
-    }
-    // ds as two terms; lanes of a pair of items exchange them, the even one takes the first terms of both
-    {
-      const uint32_t pick = c & 1 ? 0x03020706u : 0x05040100u;        // (own word low in the permute)
-      uint32_t* to = out.ds + (static_cast<long>(blk) * dm.m + static_cast<long>(b) * Pq) * 16;
-      const uint32_t to_off = fresh(4u * (16 * NPQ * g + ((c & 1) << 3) + (c >> 1)));
-      const long px_step = static_cast<long>(dm.nb) * dm.m * 16;
-#pragma unroll
-      for (int px = 0; px < PXP; ++px, to += px_step)
-#pragma unroll
-      for (int i = 0; i < NPQ; ++i) {
-        const int mu = i * PXP + px;
-        const float v = ds[mu / 4][mu % 4];
-        const uint32_t hi = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
-        const uint32_t lo = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v - __uint_as_float(hi << 16)));
-        const uint32_t own = hi | lo << 16;
-        const uint32_t other =                                         // quad_perm 1,0,3,2
-            static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(own), 0xB1, 0xf, 0xf, true));
-        // even: (own low, other low); odd: (other high, own high)
-        const uint32_t w = __builtin_amdgcn_perm(other, own, pick);
-        if (FULL || (NPQ * g + i < Pq && px < Px)) const_cast<uint32_t&>(at32(to, to_off + 64u * i)) = w;
-      }
-    }
+    back(0);
+    if constexpr (HALVES == 1) store_ds();
     } else {
       // no unit: factors of zeros
       for (int i = lane; i < wave_bytes<RUN>() / 16; i += 64) reinterpret_cast<uint4*>(mine)[i] = make_uint4(0, 0, 0, 0);
     }
     // (these barriers wait for LDS alone: the stores of ds and the next operands stay in flight)
     ring_barrier<63>();
-    // dW1 += du s^T, dW2^T += h dl^T over the eight units' items, two units a K block:
-    // slots 8 g + e are items 4 g + e % 4 of the one and the other
-    if (j0 < 2 * JT2) {
-      const unsigned char* u0 = waves + tr;
-      const unsigned char* pj = u0 + 1024 * (2 * PT + (second ? 0 : kJT) + j0);      // h or du
-      const unsigned char* pp = u0 + 1024 * ((second ? PT : 0) + pt0);               // dl or s
-#pragma unroll 1
-      for (int u = 0; u < kWaves; u += 2, pj += 2 * wave_bytes<RUN>(), pp += 2 * wave_bytes<RUN>()) {
-        uint4 fj[JW][2], fp[PW][2];
-        auto pair = [&](const unsigned char* at) {
-          const uint2 x = read_tr(at), y = read_tr(at + wave_bytes<RUN>());
-          return make_uint4(x.x, x.y, y.x, y.y);
-        };
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-#pragma unroll
-          for (int j = 0; j < JW; ++j) fj[j][k] = pair(pj + 1024 * j + 512 * k);
-#pragma unroll
-          for (int i = 0; i < PW; ++i) fp[i][k] = pair(pp + 1024 * i + 512 * k);
-        }
-#pragma unroll
-        for (int k = 2; k >= 0; --k)                                  // small products first
-#pragma unroll
-          for (int j = 0; j < JW; ++j)
-#pragma unroll
-            for (int i = 0; i < PW; ++i) aw[j][i] = mfma_bf16(fj[j][k == 2], fp[i][k == 1], aw[j][i]);
+    sum_weights(0);
+    ring_barrier<63>();                                               // read before the next units, or halves, write
+    if constexpr (HALVES == 2) {
+      if (busy) {
+        back(1);
+        store_ds();
       }
+      ring_barrier<63>();
+      sum_weights(1);
+      ring_barrier<63>();
     }
-    ring_barrier<63>();                                               // read before the next units write
   }
 
   // the workgroup's sums
   const long wg = static_cast<long>(blockIdx.y) * gridDim.x + blockIdx.x;
 #pragma unroll
-  for (int j = 0; j < JW; ++j)
+  for (int half = 0; half < HALVES; ++half)
 #pragma unroll
-    for (int i = 0; i < PW; ++i)
+    for (int j = 0; j < JW; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        // rows: hidden units, 4 g + r of a tile; columns: slots, c (of dW2 too, as its transpose)
-        const int jj = 16 * (j0 + j) + 4 * g + r, p = component(16 * (pt0 + i) + c);
-        if (jj < H && p >= 0) {
-          if (second) out.dW2[(wg * P + p) * H + jj] = aw[j][i][r];
-          else out.dW1[(wg * H + jj) * P + p] = aw[j][i][r];
+      for (int i = 0; i < PW; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          // rows: hidden units, 4 g + r of a tile; columns: slots, c (of dW2 too, as its transpose)
+          const int jj = kH * half + 16 * (j0 + j) + 4 * g + r, p = component(16 * (pt0 + i) + c);
+          if (jj < H && p >= 0) {
+            if (second) out.dW2[(wg * P + p) * H + jj] = aw[half][j][i][r];
+            else out.dW1[(wg * H + jj) * P + p] = aw[half][j][i][r];
+          }
         }
-      }
   float* acc = reinterpret_cast<float*>(smb);                         // (in the place of everything in LDS)
 #pragma unroll
-  for (int jt = 0; jt < kJT; ++jt)
+  for (int jt = 0; jt < HALVES * kJT; ++jt)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float t = ab1[jt][i];
@@ -576,10 +612,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
       t += row_ror<4>(t);
       t += row_ror<2>(t);
       t += row_ror<1>(t);
-      if (c == 0) acc[wave * kH + 16 * jt + 4 * g + i] = t;
+      if (c == 0) acc[wave * HU + 16 * jt + 4 * g + i] = t;
     }
   // (db2: da_x summed over the items)
-  float* acc2 = acc + kWaves * kH;
+  float* acc2 = acc + kWaves * HU;
   {
     const float t = sum_items<RUN>(dax, c);
     if (c < RUN) acc2[wave * SLOTS + RUN * g + c] = t;
@@ -588,7 +624,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
   for (int i = tid; i < H; i += kThreads) {
     float t = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) t += acc[w * kH + i];
+    for (int w = 0; w < kWaves; ++w) t += acc[w * HU + i];
     out.db1[wg * H + i] = t;
   }
   for (int i = tid; i < SLOTS; i += kThreads) {
@@ -839,7 +875,7 @@ Bf16Plan plan(const DevProb& pr) {
   return f;
 }
 
-template <int NPQ, int PXP>
+template <int NPQ, int PXP, int HALVES>
 hipError_t launch_pairs(const DevProb& pr, const Bf16Plan& f, Bf16Dims dm, const float* dphi,
                         const Bf16Parts& parts, hipStream_t st) {
   auto aligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
@@ -847,18 +883,17 @@ hipError_t launch_pairs(const DevProb& pr, const Bf16Plan& f, Bf16Dims dm, const
                     aligned(pr.a_x) && aligned(pr.b1) && aligned(pr.b2) && pr.H % 4 == 0;
   // the items' rows in LDS where the workgroup has one block of items: whole, or the first
   // blocks of 32 that there is room for (the loaded-ahead ones at least)
-  constexpr int base = lds_bytes<NPQ * PXP>(), room = (160 * 1024 - base) / x_bytes(PXP);
+  constexpr int base = lds_bytes<NPQ * PXP, HALVES>(), room = (160 * 1024 - base) / x_bytes(PXP);
   static_assert(room >= kAhead, "LDS");
   const bool xl = dm.QB == kWaves;
   dm.kl = xl ? std::min((pr.d + 31) / 32, room) : 0;
   const int lds = base + dm.kl * x_bytes(PXP);
-  const int form = !full ? 0 : pr.H <= 32 ? 1 : 2;
-  auto kern = xl ? (form == 2   ? &k_score_grad_bf16<NPQ, PXP, true, 2>
-                    : form == 1 ? &k_score_grad_bf16<NPQ, PXP, true, 1>
-                                : &k_score_grad_bf16<NPQ, PXP, true, 0>)
-                 : (form == 2   ? &k_score_grad_bf16<NPQ, PXP, false, 2>
-                    : form == 1 ? &k_score_grad_bf16<NPQ, PXP, false, 1>
-                                : &k_score_grad_bf16<NPQ, PXP, false, 0>);
+  constexpr int all = 2 * HALVES;
+  auto kern = xl ? &k_score_grad_bf16<NPQ, PXP, true, 0, HALVES> : &k_score_grad_bf16<NPQ, PXP, false, 0, HALVES>;
+  if (full && HALVES == 1 && pr.H <= 32)
+    kern = xl ? &k_score_grad_bf16<NPQ, PXP, true, 1, 1> : &k_score_grad_bf16<NPQ, PXP, false, 1, 1>;
+  else if (full)
+    kern = xl ? &k_score_grad_bf16<NPQ, PXP, true, all, HALVES> : &k_score_grad_bf16<NPQ, PXP, false, all, HALVES>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(kern, dim3(f.wgx, dm.qsplits), dim3(kThreads), lds, st, pr, dm, dphi, parts);
@@ -869,7 +904,7 @@ hipError_t launch_pairs(const DevProb& pr, const Bf16Plan& f, Bf16Dims dm, const
 
 bool bf16_supported(const DevProb& pr) {
   // (a lane's offsets from its wave's bases in 32 bits)
-  return pr.dtype == MOL_BF16 && pr.Pq <= 8 && pr.Px <= 8 && pr.H <= kH && static_cast<long>(pr.N) * pr.d < (1l << 31) &&
+  return pr.dtype == MOL_BF16 && pr.Pq <= 8 && (pr.H <= kH ? pr.Px <= 8 : pr.H <= 2 * kH && pr.Px <= 4) && static_cast<long>(pr.N) * pr.d < (1l << 31) &&
          static_cast<long>(pr.N) * pr.P < (1l << 30);
 }
 
@@ -882,7 +917,9 @@ hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_gra
   const Bf16Parts parts{reinterpret_cast<uint32_t*>(ws + f.off_ds), F(f.off_daq), F(f.off_dax), F(f.off_dw1),
                         F(f.off_dw2), F(f.off_db1), F(f.off_db2)};
   float* acc = F(f.off_acc);
-  auto pairs = pr.Pq <= 4 && pr.Px <= 4 ? &launch_pairs<1, 4> : pr.Px <= 4 ? &launch_pairs<2, 4> : &launch_pairs<2, 8>;
+  auto pairs = pr.H > kH ? (pr.Pq <= 4 ? &launch_pairs<1, 4, 2> : &launch_pairs<2, 4, 2>)
+               : pr.Px > 4 ? &launch_pairs<2, 8, 1>
+                           : (pr.Pq <= 4 ? &launch_pairs<1, 4, 1> : &launch_pairs<2, 4, 1>);
   const int cg = (pr.d + 63) / 64;
   const long P = pr.P, H = pr.H, BP = pr.B * P;
   SumList sums(st);

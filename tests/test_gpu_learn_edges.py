@@ -44,7 +44,8 @@ def off_by_one(t):
 
 # ------------------------------------------------------------------ buffers' ends
 SHAPES = [(1, 1, 1, 1, 1, 1), (3, 21, 2, 3, 9, 7), (7, 50, 5, 3, 33, 24), (9, 70, 8, 8, 31, 64), (5, 37, 8, 8, 64, 64),
-          (2, 19, 3, 7, 40, 100), (33, 129, 4, 4, 24, 32), (9, 40, 4, 4, 768, 64), (8, 33, 8, 8, 200, 64), (10, 20, 8, 4, 777, 33)]
+          (2, 19, 3, 7, 40, 100), (33, 129, 4, 4, 24, 32), (9, 40, 4, 4, 768, 64), (8, 33, 8, 8, 200, 64), (10, 20, 8, 4, 777, 33),
+          (9, 41, 8, 4, 128, 128), (17, 50, 3, 2, 20, 70), (4, 33, 4, 4, 64, 96), (1, 40, 5, 4, 33, 127)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
