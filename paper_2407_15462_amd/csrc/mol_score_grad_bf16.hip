@@ -28,14 +28,15 @@
 // whole.  dQ = sum ds X reads rows (K = items); dX = sum ds Q (K = b pq) takes them through LDS
 // and the transposing read.
 //
-// Measured, 1024 x 2048 pairs of 8 x 8, d = H = 64, in two slabs: 760 us a call,
-// 203 TFLOP/s; a slab's pairs 295 us, products 101 (5.3 TB/s of ds), sums 18.  128 x 1031
+// Measured, 1024 x 2048 pairs of 8 x 8, d = H = 64, in two slabs: 755 us a call,
+// 205 TFLOP/s; a slab's pairs 295 us, products 101 (5.3 TB/s of ds), sums 18.  128 x 1031
 // of 8 x 8, d = 32: 64 + 18 + 10.  The pairs are bound by issue and latency: a unit
 // is 914 vector, 49 transcendental, 124 matrix and 121 LDS instructions, its
 // 256 registers leave two waves a SIMD, and these issue vector instructions 40 % of
 // the time.  The general form, on f32 matrix instructions, takes 435 us for half as
 // many pairs.
 #include <algorithm>
+#include <type_traits>
 
 #include "mol_grad.h"
 
@@ -181,13 +182,13 @@ static_assert(lds_bytes<4, 1>() >= 4 * kWaves * 16 * 16 && lds_bytes<16, 1>() >=
 
 }  // namespace
 
-// XL: the workgroup's waves share 16 items, whose rows lie in LDS, as far as there is room.  FULL 1 or 2: P_q = 4
+// XL: the workgroup's waves share 16 items, whose rows lie in LDS (2: as far as there is room).  FULL 1 or 2: P_q = 4
 // NPQ, P_x = PXP, every row allows 16-byte reads (H a multiple of 4) and H is
 // at most 32 FULL: no branches in a unit, which leaves its order to the compiler.
 // HALVES 2: 65 to 128 hidden units.  u stays in registers on the way forward, and the way
 // back takes 64 of them at a time: h and du of those to LDS, and their part of dW1 and dW2
 // (512 x 2000 pairs of 8 x 4, d = H = 128: 339 us, 831 in the general form).
-template <int NPQ, int PXP, bool XL, int FULL, int HALVES>
+template <int NPQ, int PXP, int XL, int FULL, int HALVES>
 __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf16Dims dm,
                                                                  const float* __restrict__ dphi, Bf16Parts out) {
   constexpr int RUN = NPQ * PXP, SLOTS = 4 * RUN, PT = RUN / 4, KB = RUN > 8 ? RUN / 8 : 1, HU = HALVES * kH;
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, g = lane >> 4;
-  const int P = pr.P, H = pr.H, d = pr.d, N = pr.N, JT2 = FULL ? FULL : (H + 31) / 32, nch = 4 * dm.kl;
+  const int P = pr.P, H = pr.H, d = pr.d, N = pr.N, JT2 = FULL ? FULL : (H + 31) / 32, nch = 4 * (XL == 2 ? dm.kl : (d + 31) / 32);
   const int Pq = FULL ? 4 * NPQ : pr.Pq, Px = FULL ? PXP : pr.Px;
   unsigned char* sW1 = smb;
   unsigned char* sW2 = sW1 + 2 * HU * SLOTS;
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
       *reinterpret_cast<bf16_t*>(sW1 + w1_at(j, sl)) = in ? W1[j * P + p] : 0;
       *reinterpret_cast<bf16_t*>(sW2 + w2_at(sl, j)) = in ? W2[p * H + j] : 0;
     }
-    if constexpr (XL) {
+    if constexpr (XL != 0) {
       // (zeros past d would do no good here: Q has them)
       for (int i = tid; i < PXP * nch * 16; i += kThreads) {
         const int it = i & 15, ch = (i >> 4) % nch, px = (i >> 4) / nch;
@@ -279,114 +280,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
     const bool busy = has_blk && b < pr.B;                            // (the same for the whole wave)
     Terms<3> a[KB];                                                   // of s, then of dl
     f32x4_t ds[PT], ur[HALVES == 2 ? 2 * kJT : 1];
-    // back through 64 hidden units of the MLP
-    auto back = [&](int half) {
+    // (not indented: the way forward, before the first half; the way back, a half; ds, after the last)
 #pragma unroll
-      for (int l2 = 0; l2 < kJT / 2; ++l2) {
-        const int j2 = half * (kJT / 2) + l2;
-        if (j2 >= JT2) break;
-        float du[8], h[8];
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          const int jt = 2 * j2 + hf;
-          f32x4_t dh = {};
-#pragma unroll
-          for (int m = 0; m < KB; ++m) {
-            // A row j = 16 jt + c, K = slots RUN g + 8 m + e: columns of W2's rows
-            const int sl = RUN * g + 8 * m + (c >> 2), j = 16 * jt + 4 * (c & 3);
-            const uint2 w0 = read_tr(sW2 + w2_at(sl, j));
-            const uint2 w1 = RUN >= 8 ? read_tr(sW2 + w2_at(sl + 4, j)) : make_uint2(0, 0);
-            dh = mfma_terms<3>(make_uint4(w0.x, w0.y, w1.x, w1.y), a[m], dh);
-          }
-          float kk[4];
-          if constexpr (HALVES == 1) {
-            const float4 k = *reinterpret_cast<const float4*>(sU + 1024 * jt + 16 * lane);
-            kk[0] = k.x, kk[1] = k.y, kk[2] = k.z, kk[3] = k.w;
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float u = ur[jt][i], sig = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u));
-              h[4 * hf + i] = u * sig;
-              kk[i] = fmaf(h[4 * hf + i], 1.f - sig, sig);
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            du[4 * hf + i] = dh[i] * kk[i];
-            ab1[jt][i] += du[4 * hf + i];
-          }
-        }
-        auto store_hidden = [&](unsigned char* to, const Terms<2>& x) {
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            *reinterpret_cast<uint2*>(to + 1024 * (2 * l2) + 512 * k + place(4 * g)) = make_uint2(x.t[k].x, x.t[k].y);
-            *reinterpret_cast<uint2*>(to + 1024 * (2 * l2 + 1) + 512 * k + place(4 * g)) = make_uint2(x.t[k].z, x.t[k].w);
-          }
-        };
-        const Terms<2> dt = split<2>(du);
-        store_hidden(sU, dt);                                         // (in the place of k, which the wave has read)
-        if constexpr (HALVES == 2) store_hidden(sH, split<2>(h));
-#pragma unroll
-        for (int pt = 0; pt < PT; ++pt) {
-          // A row slot RUN (c / 4) + 4 pt + c % 4, K = j: columns of W1's rows
-          const int j = 32 * j2 + 4 * g + (c >> 2), sl = RUN * (c & 3) + 4 * pt;
-          const uint2 w0 = read_tr(sW1 + w1_at(j, sl)), w1 = read_tr(sW1 + w1_at(j + 16, sl));
-          ds[pt] = mfma_terms<2>(make_uint4(w0.x, w0.y, w1.x, w1.y), dt, ds[pt]);
-        }
-      }
-    };
-    // ds as two terms; lanes of a pair of items exchange them, the even one takes the first terms of both
-    auto store_ds = [&] {
-      const uint32_t pick = c & 1 ? 0x03020706u : 0x05040100u;        // (own word low in the permute)
-      uint32_t* to = out.ds + (static_cast<long>(blk) * dm.m + static_cast<long>(b) * Pq) * 16;
-      const uint32_t to_off = fresh(4u * (16 * NPQ * g + ((c & 1) << 3) + (c >> 1)));
-      const long px_step = static_cast<long>(dm.nb) * dm.m * 16;
-#pragma unroll
-      for (int px = 0; px < PXP; ++px, to += px_step)
-#pragma unroll
-      for (int i = 0; i < NPQ; ++i) {
-        const int mu = i * PXP + px;
-        const float v = ds[mu / 4][mu % 4];
-        const uint32_t hi = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
-        const uint32_t lo = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v - __uint_as_float(hi << 16)));
-        const uint32_t own = hi | lo << 16;
-        const uint32_t other =                                         // quad_perm 1,0,3,2
-            static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(own), 0xB1, 0xf, 0xf, true));
-        // even: (own low, other low); odd: (other high, own high)
-        const uint32_t w = __builtin_amdgcn_perm(other, own, pick);
-        if (FULL || (NPQ * g + i < Pq && px < Px)) const_cast<uint32_t&>(at32(to, to_off + 64u * i)) = w;
-      }
-    };
-    // dW1 += du s^T, dW2^T += h dl^T over the eight units' items, two units a K block:
-    // slots 8 g + e are items 4 g + e % 4 of the one and the other
-    auto sum_weights = [&](int half) {
-      if (half * kJT + j0 >= 2 * JT2) return;
-      const unsigned char* u0 = waves + tr;
-      const unsigned char* pj = u0 + 1024 * (2 * PT + (second ? 0 : kJT) + j0);      // h or du
-      const unsigned char* pp = u0 + 1024 * ((second ? PT : 0) + pt0);               // dl or s
-#pragma unroll 1
-      for (int u = 0; u < kWaves; u += 2, pj += 2 * wave_bytes<RUN>(), pp += 2 * wave_bytes<RUN>()) {
-        uint4 fj[JW][2], fp[PW][2];
-        auto pair = [&](const unsigned char* at) {
-          const uint2 x = read_tr(at), y = read_tr(at + wave_bytes<RUN>());
-          return make_uint4(x.x, x.y, y.x, y.y);
-        };
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-#pragma unroll
-          for (int j = 0; j < JW; ++j) fj[j][k] = pair(pj + 1024 * j + 512 * k);
-#pragma unroll
-          for (int i = 0; i < PW; ++i) fp[i][k] = pair(pp + 1024 * i + 512 * k);
-        }
-#pragma unroll
-        for (int k = 2; k >= 0; --k)                                  // small products first
-#pragma unroll
-          for (int j = 0; j < JW; ++j)
-#pragma unroll
-            for (int i = 0; i < PW; ++i) aw[half][j][i] = mfma_bf16(fj[j][k == 2], fp[i][k == 1], aw[half][j][i]);
-      }
-    };
+    for (int half = 0; half < HALVES; ++half) {
     if (busy) {
+    if (half == 0) {
     gr = has_item ? gr_next : 0.f;
     // a_q, a_x and b2, for l
     f32x4_t l[PT], lx[PT], b2[PT];
@@ -428,11 +326,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
       };
 #pragma unroll
       for (int k = 0; k < kAhead; ++k)
-        if (32 * k < d) block(k, qf[k], XL);
+        if (32 * k < d) block(k, qf[k], XL != 0);
       int k = kAhead;
-      if constexpr (XL)
+      if constexpr (XL == 2)
         for (; k < dm.kl; ++k) block(k, row16(Q, qo, 32 * k + 8 * g, true), true);
-      for (; 32 * k < d; ++k) block(k, row16(Q, qo, 32 * k + 8 * g, true), false);
+      for (; 32 * k < d; ++k) block(k, row16(Q, qo, 32 * k + 8 * g, true), XL == 1);
 #pragma unroll
       for (int px = 0; px < PXP; ++px)
 #pragma unroll
@@ -564,24 +462,118 @@ __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf1
       const int pq = NPQ * g + c / PXP, px = c % PXP;
       if (c < RUN && pq < Pq && px < Px) out.da_q[(static_cast<long>(blk) * pr.B + b) * P + pq * Px + px] = t;
     }
-    back(0);
-    if constexpr (HALVES == 1) store_ds();
-    } else {
+    }
+    // back through 64 hidden units of the MLP
+#pragma unroll
+      for (int l2 = 0; l2 < kJT / 2; ++l2) {
+        const int j2 = half * (kJT / 2) + l2;
+        if (j2 >= JT2) break;
+        float du[8], h[8];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const int jt = 2 * j2 + hf;
+          f32x4_t dh = {};
+#pragma unroll
+          for (int m = 0; m < KB; ++m) {
+            // A row j = 16 jt + c, K = slots RUN g + 8 m + e: columns of W2's rows
+            const int sl = RUN * g + 8 * m + (c >> 2), j = 16 * jt + 4 * (c & 3);
+            const uint2 w0 = read_tr(sW2 + w2_at(sl, j));
+            const uint2 w1 = RUN >= 8 ? read_tr(sW2 + w2_at(sl + 4, j)) : make_uint2(0, 0);
+            dh = mfma_terms<3>(make_uint4(w0.x, w0.y, w1.x, w1.y), a[m], dh);
+          }
+          float kk[4];
+          if constexpr (HALVES == 1) {
+            const float4 k = *reinterpret_cast<const float4*>(sU + 1024 * jt + 16 * lane);
+            kk[0] = k.x, kk[1] = k.y, kk[2] = k.z, kk[3] = k.w;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float u = ur[jt][i], sig = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * u));
+              h[4 * hf + i] = u * sig;
+              kk[i] = fmaf(h[4 * hf + i], 1.f - sig, sig);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            du[4 * hf + i] = dh[i] * kk[i];
+            ab1[jt][i] += du[4 * hf + i];
+          }
+        }
+        auto store_hidden = [&](unsigned char* to, const Terms<2>& x) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            *reinterpret_cast<uint2*>(to + 1024 * (2 * l2) + 512 * k + place(4 * g)) = make_uint2(x.t[k].x, x.t[k].y);
+            *reinterpret_cast<uint2*>(to + 1024 * (2 * l2 + 1) + 512 * k + place(4 * g)) = make_uint2(x.t[k].z, x.t[k].w);
+          }
+        };
+        const Terms<2> dt = split<2>(du);
+        store_hidden(sU, dt);                                         // (in the place of k, which the wave has read)
+        if constexpr (HALVES == 2) store_hidden(sH, split<2>(h));
+#pragma unroll
+        for (int pt = 0; pt < PT; ++pt) {
+          // A row slot RUN (c / 4) + 4 pt + c % 4, K = j: columns of W1's rows
+          const int j = 32 * j2 + 4 * g + (c >> 2), sl = RUN * (c & 3) + 4 * pt;
+          const uint2 w0 = read_tr(sW1 + w1_at(j, sl)), w1 = read_tr(sW1 + w1_at(j + 16, sl));
+          ds[pt] = mfma_terms<2>(make_uint4(w0.x, w0.y, w1.x, w1.y), dt, ds[pt]);
+        }
+      }
+    // ds as two terms; lanes of a pair of items exchange them, the even one takes the first terms of both
+    if (half + 1 == HALVES) {
+      const uint32_t pick = c & 1 ? 0x03020706u : 0x05040100u;        // (own word low in the permute)
+      uint32_t* to = out.ds + (static_cast<long>(blk) * dm.m + static_cast<long>(b) * Pq) * 16;
+      const uint32_t to_off = fresh(4u * (16 * NPQ * g + ((c & 1) << 3) + (c >> 1)));
+      const long px_step = static_cast<long>(dm.nb) * dm.m * 16;
+#pragma unroll
+      for (int px = 0; px < PXP; ++px, to += px_step)
+#pragma unroll
+      for (int i = 0; i < NPQ; ++i) {
+        const int mu = i * PXP + px;
+        const float v = ds[mu / 4][mu % 4];
+        const uint32_t hi = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+        const uint32_t lo = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v - __uint_as_float(hi << 16)));
+        const uint32_t own = hi | lo << 16;
+        const uint32_t other =                                         // quad_perm 1,0,3,2
+            static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(own), 0xB1, 0xf, 0xf, true));
+        // even: (own low, other low); odd: (other high, own high)
+        const uint32_t w = __builtin_amdgcn_perm(other, own, pick);
+        if (FULL || (NPQ * g + i < Pq && px < Px)) const_cast<uint32_t&>(at32(to, to_off + 64u * i)) = w;
+      }
+    }
+    } else if (half == 0) {
       // no unit: factors of zeros
       for (int i = lane; i < wave_bytes<RUN>() / 16; i += 64) reinterpret_cast<uint4*>(mine)[i] = make_uint4(0, 0, 0, 0);
     }
     // (these barriers wait for LDS alone: the stores of ds and the next operands stay in flight)
     ring_barrier<63>();
-    sum_weights(0);
-    ring_barrier<63>();                                               // read before the next units, or halves, write
-    if constexpr (HALVES == 2) {
-      if (busy) {
-        back(1);
-        store_ds();
+    // dW1 += du s^T, dW2^T += h dl^T over the eight units' items, two units a K block:
+    // slots 8 g + e are items 4 g + e % 4 of the one and the other
+    if (half * kJT + j0 < 2 * JT2) {
+      const unsigned char* u0 = waves + tr;
+      const unsigned char* pj = u0 + 1024 * (2 * PT + (second ? 0 : kJT) + j0);      // h or du
+      const unsigned char* pp = u0 + 1024 * ((second ? PT : 0) + pt0);               // dl or s
+#pragma unroll 1
+      for (int u = 0; u < kWaves; u += 2, pj += 2 * wave_bytes<RUN>(), pp += 2 * wave_bytes<RUN>()) {
+        uint4 fj[JW][2], fp[PW][2];
+        auto pair = [&](const unsigned char* at) {
+          const uint2 x = read_tr(at), y = read_tr(at + wave_bytes<RUN>());
+          return make_uint4(x.x, x.y, y.x, y.y);
+        };
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+          for (int j = 0; j < JW; ++j) fj[j][k] = pair(pj + 1024 * j + 512 * k);
+#pragma unroll
+          for (int i = 0; i < PW; ++i) fp[i][k] = pair(pp + 1024 * i + 512 * k);
+        }
+#pragma unroll
+        for (int k = 2; k >= 0; --k)                                  // small products first
+#pragma unroll
+          for (int j = 0; j < JW; ++j)
+#pragma unroll
+            for (int i = 0; i < PW; ++i) aw[half][j][i] = mfma_bf16(fj[j][k == 2], fp[i][k == 1], aw[half][j][i]);
       }
-      ring_barrier<63>();
-      sum_weights(1);
-      ring_barrier<63>();
+    }
+    ring_barrier<63>();                                               // read before the next units, or halves, write
     }
   }
 
@@ -885,15 +877,16 @@ hipError_t launch_pairs(const DevProb& pr, const Bf16Plan& f, Bf16Dims dm, const
   // blocks of 32 that there is room for (the loaded-ahead ones at least)
   constexpr int base = lds_bytes<NPQ * PXP, HALVES>(), room = (160 * 1024 - base) / x_bytes(PXP);
   static_assert(room >= kAhead, "LDS");
-  const bool xl = dm.QB == kWaves;
-  dm.kl = xl ? std::min((pr.d + 31) / 32, room) : 0;
+  const int blocks = (pr.d + 31) / 32;
+  dm.kl = dm.QB == kWaves ? std::min(blocks, room) : 0;
   const int lds = base + dm.kl * x_bytes(PXP);
-  constexpr int all = 2 * HALVES;
-  auto kern = xl ? &k_score_grad_bf16<NPQ, PXP, true, 0, HALVES> : &k_score_grad_bf16<NPQ, PXP, false, 0, HALVES>;
-  if (full && HALVES == 1 && pr.H <= 32)
-    kern = xl ? &k_score_grad_bf16<NPQ, PXP, true, 1, 1> : &k_score_grad_bf16<NPQ, PXP, false, 1, 1>;
-  else if (full)
-    kern = xl ? &k_score_grad_bf16<NPQ, PXP, true, all, HALVES> : &k_score_grad_bf16<NPQ, PXP, false, all, HALVES>;
+  auto of = [&](auto xl) {
+    constexpr int XL = decltype(xl)::value, all = 2 * HALVES;
+    return full ? (HALVES == 1 && pr.H <= 32 ? &k_score_grad_bf16<NPQ, PXP, XL, 1, 1> : &k_score_grad_bf16<NPQ, PXP, XL, all, HALVES>)
+                : &k_score_grad_bf16<NPQ, PXP, XL, 0, HALVES>;
+  };
+  auto kern = dm.kl == 0 ? of(std::integral_constant<int, 0>())
+              : dm.kl == blocks ? of(std::integral_constant<int, 1>()) : of(std::integral_constant<int, 2>());
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(kern, dim3(f.wgx, dm.qsplits), dim3(kThreads), lds, st, pr, dm, dphi, parts);
