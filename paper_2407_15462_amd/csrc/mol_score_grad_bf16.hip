@@ -29,8 +29,8 @@
 // and the transposing read.
 //
 // Measured, 1024 x 2048 pairs of 8 x 8, d = H = 64, in two slabs: 755 us a call,
-// 205 TFLOP/s; a slab's pairs 295 us, products 101 (5.3 TB/s of ds), sums 18.  128 x 1031
-// of 8 x 8, d = 32: 64 + 18 + 10.  The pairs are bound by issue and latency: a unit
+// 205 TFLOP/s; a slab's pairs 275 us, products 87 (6.2 TB/s of ds), sums 16.  128 x 1031
+// of 8 x 8, d = 32: 61 + 17 + 9.  The pairs are bound by issue and latency: a unit
 // is 914 vector, 49 transcendental, 124 matrix and 121 LDS instructions, its
 // 256 registers leave two waves a SIMD, and these issue vector instructions 40 % of
 // the time.  The general form, on f32 matrix instructions, takes 435 us for half as
