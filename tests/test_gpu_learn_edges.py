@@ -188,6 +188,27 @@ def test_score_grad_of_a_corpus_past_32_bits(N):
     assert bool(torch.isfinite(got["dQ"]).all())
 
 
+@pytest.mark.parametrize("dtype,H", [(F32, 20), (BF16, 20), (BF16, 100)])
+def test_score_grad_of_the_most_queries(dtype, H):
+    """65,535 queries, slabs of the fewest items: a query's gradients are those it has among few, a sum's parts add up."""
+    B, N, Pq, Px, d = 65535, 70, 8, 4, 24
+    log(f"[edges] score_grad B={B} N={N} H={H} {dtype}")
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    randn = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    P = Pq * Px
+    Q, X = (0.3 * randn(B, Pq, d)).to(dtype), (0.3 * randn(Px, N, d)).to(dtype)
+    a_q, a_x, b1, b2 = randn(B, P), randn(N, P), randn(H), randn(P)
+    W1, W2 = (0.3 * randn(H, P)).to(dtype), (0.3 * randn(P, H)).to(dtype)
+    dphi = randn(B, N)
+    dphi[4:-4] = 0                                       # (so that the sums over queries are those of eight)
+    got = mol.score_grad(mol.Problem(Q, X, a_q, a_x, W1, b1, W2, b2), dphi)
+    rows = [0, 1, 2, 3, B - 4, B - 3, B - 2, B - 1]
+    want, bound = lh.score_grads([t.cpu() for t in (Q[rows], X, a_q[rows], a_x, W1, b1, W2, b2)], dphi[rows].cpu())
+    for n in NAMES:
+        lh.within(got[n][rows] if n in ("dQ", "da_q") else got[n], want[n], bound[n], n)
+    assert int((got["dQ"][4:-4] != 0).sum()) == 0 and int((got["da_q"][4:-4] != 0).sum()) == 0
+
+
 def test_softmax_loss_past_32_bits():
     """Score rows that begin past 2^32 elements."""
     B, N = 61000, 70417
@@ -233,3 +254,53 @@ def test_adamw_past_32_bits():
         assert torch.equal(a[-tail:], b)
     assert torch.equal(ms[-4:], sms) and torch.equal(vs[-4:], svs)
     assert int((p[:4096] != 0).sum()) == 0
+
+
+# ------------------------------------------------------------------ graphs
+def test_two_graphs_share_a_workspace():
+    """Two captured sequences that use one workspace, replayed in turn with eager work and new inputs between them:
+    the bits of eager calls."""
+    B, N, Pq, Px, d, H, V = 24, 9000, 4, 4, 32, 32, 500
+    inputs, dphi = lh.mol_inputs(B, N, Pq, Px, d, H, BF16, seed=2, device="cuda")
+    prob = mol.Problem(*inputs)
+    gen = torch.Generator().manual_seed(7)
+    ids = torch.randint(-1, V, (N,), generator=gen).int().cuda()
+    phi = torch.randn(3, 50000, generator=gen).cuda()
+    target = torch.tensor([1, 40000, 7], dtype=torch.int32, device="cuda")
+    sizes = (mol.mol_workspace_size(prob, mol.MOL_OP_SCORE_GRAD), mol.mol_embed_grad_workspace(Px, V, d, N),
+             mol.mol_softmax_loss_workspace(3, 50000))
+    ws = torch.empty(max(sizes), dtype=torch.uint8, device="cuda")
+
+    def first():
+        g = mol.score_grad(prob, dphi, ws=ws)
+        return list(g.values()) + [mol.embed_grad(g["dX"], ids, V, ws=ws)]
+
+    def second():
+        return list(mol.softmax_loss(phi, target, inv_temp=3.0, ws=ws)) + [mol.embed_grad(prob.tensors[1], ids, V, 2.0, ws=ws)]
+
+    graphs = []
+    for run in (first, second):
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            run()
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = run()
+        graphs.append((graph, out, run))
+    for turn in range(3):
+        dphi.mul_(1.5)
+        phi.add_(0.25)
+        ids.copy_(ids.roll(11))
+        for graph, out, run in graphs:
+            for t in out:
+                t.zero_()
+            ws.fill_(0xFF)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            held = [t.clone() for t in out]
+            for got, want in zip(held, run()):
+                assert torch.equal(got, want), turn
