@@ -51,6 +51,39 @@ inline int split_of(long waves, long chunks, long least) {
   return static_cast<int>(n < 1 ? 1 : n);
 }
 
+// high halves of a and b: their first bf16 terms by truncation
+__device__ __forceinline__ uint32_t high_halves(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ float rest(float a) { return a - __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
+
+// eight values as bf16 terms, two values a word
+template <int TERMS>
+struct Terms {
+  uint4 t[TERMS];
+};
+template <int TERMS>
+__device__ __forceinline__ Terms<TERMS> split(const float (&x)[8]) {
+  Terms<TERMS> o;
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = x[e];
+#pragma unroll
+  for (int k = 0; k < TERMS; ++k) {
+    o.t[k] = make_uint4(high_halves(v[0], v[1]), high_halves(v[2], v[3]), high_halves(v[4], v[5]), high_halves(v[6], v[7]));
+    if (k + 1 < TERMS)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = rest(v[e]);
+  }
+  return o;
+}
+template <int TERMS>
+__device__ __forceinline__ tile::f32x4_t mfma_terms(uint4 a, const Terms<TERMS>& b, tile::f32x4_t c) {
+#pragma unroll
+  for (int k = TERMS - 1; k >= 0; --k) c = tile::mfma_bf16(a, b.t[k], c);   // small terms first
+  return c;
+}
+
 // Stores a wave's tile of a product: element (4 g + i, c) of each 16x16 block, rows
 // from m0 to m and columns from t0 to d, as a part's float32 or as the output's type.
 template <typename T, int RB, int CB>

@@ -1,5 +1,6 @@
 // Gradient of the MoL scores (Eq. 1 / Eq. 2 with the gating MLP of Appendix
-// A.3) for every input, any supported shape and both storage types.
+// A.3) for every input, any supported shape and both storage types, in float32
+// throughout: bf16 outputs are rounded once, at the end.
 //
 // With g = dphi, per pair (query, item):
 //   dl_p = g pi_p (s_p - phi)             dh = W2^T dl
@@ -20,10 +21,9 @@
 //    whole walk (JTG blocks of 16 hidden units; a wider MLP takes a launch for
 //    every JTG blocks, of which only the first writes ds, da_q and da_x), as
 //    does da_x.  The workgroup's sums go to the workspace.
-// 2. ds goes there too, [Px][B Pq][items], as float32 or, for bf16 problems, as
-//    two bf16 terms (16 significant bits, more than dQ and dX keep), and
-//    k_grad_products forms dQ = sum ds X and dX = sum ds Q on matrix cores from it,
-//    with rows of X and Q as K, as they lie.
+// 2. ds goes there too, [Px][B Pq][items], as float32, and k_grad_products forms
+//    dQ = sum ds X and dX = sum ds Q on matrix cores from it, with rows of X and Q as
+//    K, as they lie (bf16 problems: ds in three bf16 terms, which are exact).
 // 3. k_sum_parts adds the partial sums in a fixed order.
 // Items are taken in slabs, so that ds and what else grows with them stay within kSlabBytes.
 //
@@ -98,14 +98,6 @@ __device__ __forceinline__ f32x4_t mma16(uint4 a, uint4 b, f32x4_t c) {
     return mfma_bf16(a, b, c);
 }
 
-// v as two bf16 terms, hi in the low half
-__device__ __forceinline__ uint32_t split_bf16(float v) {
-  const __bf16 hi = static_cast<__bf16>(v);
-  const __bf16 lo = static_cast<__bf16>(v - static_cast<float>(hi));
-  return static_cast<uint32_t>(__builtin_bit_cast(uint16_t, hi)) |
-         static_cast<uint32_t>(__builtin_bit_cast(uint16_t, lo)) << 16;
-}
-
 struct GradDims {
   int QB, upq_log2;        // queries of a tile, log2 of its 16-item units a query
   int TI, TIP;             // items of a tile, floats of an LDS row of s
@@ -117,7 +109,7 @@ struct GradDims {
 
 // Per-workgroup sums in the workspace.
 struct GradParts {
-  uint32_t* ds;            // [Px][B Pq][ns]
+  float* ds;               // [Px][B Pq][ns]
   float* da_q;             // [ns / 16][B][P]
   float* da_x;             // [qsplits][ns][P]
   float* dW1;              // [workgroups][H][P]
@@ -423,7 +415,7 @@ __global__ __launch_bounds__(kThreads, (2 * wgs_per_cu<PV, JTG>())) void k_score
       for (int mu = 0; mu < RUN; ++mu) {
         const uint32_t off = sOff[RUN * g + mu];
         const float v = ds[mu / 4][mu % 4];
-        if (RUN * g + mu < P) out.ds[base + off] = sizeof(T) == 4 ? __float_as_uint(v) : split_bf16(v);
+        if (RUN * g + mu < P) out.ds[base + off] = v;
       }
     }
   }
@@ -529,7 +521,7 @@ struct GemmDims {
   Tiles tiles;
 };
 template <typename T, bool COLS, bool VEC>
-__device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, const uint32_t* __restrict__ ds,
+__device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, const float* __restrict__ ds,
                                              const T* __restrict__ rows, void* __restrict__ out, uint4* sh) {
   constexpr int E = 16 / sizeof(T), KCH = 4 * E, RB = 2, CB = 4;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -547,12 +539,12 @@ __device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, 
   for (int t = 0; t < CB; ++t) col[t] = min(t0 + 16 * t + c, gd.d - 1);
   const RowTile<VEC> rt(gd.kvalid, gd.d, t0);
   struct Chunk {
-    uint32_t a[RB][E];
+    float a[RB][E];
     uint4 b[CB];
   };
   auto fetch = [&](Chunk& v, int ch) {
     const int px = COLS ? px0 : ch / per, kc = (COLS ? ch : ch - px * per) * KCH, k = kc + g * E;
-    const uint32_t* A = ds + px * gd.a_px;
+    const float* A = ds + px * gd.a_px;
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
       if constexpr (COLS) {
@@ -561,7 +553,7 @@ __device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, 
       } else {
 #pragma unroll
         for (int e = 0; e < E; e += 4) {
-          const uint4 x = *reinterpret_cast<const uint4*>(A + row[r] * gd.lda + k + e);
+          const float4 x = *reinterpret_cast<const float4*>(A + row[r] * gd.lda + k + e);
           v.a[r][e] = x.x;
           v.a[r][e + 1] = x.y;
           v.a[r][e + 2] = x.z;
@@ -600,25 +592,19 @@ __device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, 
     }
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
-      uint32_t a[E];
+      float a[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) a[e] = !COLS || e < left ? v.a[r][e] : 0;
+      for (int e = 0; e < E; ++e) a[e] = !COLS || e < left ? v.a[r][e] : 0.f;
       if constexpr (sizeof(T) == 4) {
-        const uint4 av = make_uint4(a[0], a[1], a[2], a[3]);
 #pragma unroll
-        for (int t = 0; t < CB; ++t) acc[r][t] = mma16<T>(av, bv[t], acc[r][t]);
+        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_f32x4(float4{a[0], a[1], a[2], a[3]}, __builtin_bit_cast(float4, bv[t]), acc[r][t]);
       } else {
-        uint32_t hi[4], lo[4];
+        // exact, in three terms; small products first
+        const Terms<3> at = grad::split<3>(a);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          hi[e] = __builtin_amdgcn_perm(a[2 * e + 1], a[2 * e], 0x05040100u);
-          lo[e] = __builtin_amdgcn_perm(a[2 * e + 1], a[2 * e], 0x07060302u);
-        }
-        const uint4 ah = make_uint4(hi[0], hi[1], hi[2], hi[3]), al = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        for (int k = 2; k >= 0; --k)
 #pragma unroll
-        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(al, bv[t], acc[r][t]);
-#pragma unroll
-        for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(ah, bv[t], acc[r][t]);
+          for (int t = 0; t < CB; ++t) acc[r][t] = mfma_bf16(at.t[k], bv[t], acc[r][t]);
       }
     }
     if constexpr (sizeof(T) == 2) wave_lds_sync();                     // read before the next chunk is written
@@ -640,7 +626,7 @@ __device__ __forceinline__ void product_tile(const GemmDims& gd, uint32_t unit, 
 // pairs of 8 x 8 one launch of both is 13 us shorter than two.)
 // VEC: rows of X and Q of whole 16-byte words (bf16).
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void k_grad_products(GemmDims q, GemmDims x, const uint32_t* __restrict__ ds,
+__global__ __launch_bounds__(256) void k_grad_products(GemmDims q, GemmDims x, const float* __restrict__ ds,
                                                        const T* __restrict__ X, const T* __restrict__ Q,
                                                        void* __restrict__ out_q, void* __restrict__ out_x) {
   __shared__ __attribute__((aligned(16))) uint4 sh[4][sizeof(T) == 2 ? kTileB : 1];
@@ -794,7 +780,7 @@ hipError_t run_grad(const DevProb& pr, const float* dphi, const mol_score_grads&
   const int bf = sizeof(T) == 2;
   GradDims dm = f.dm;
   auto F = [&](size_t off) { return reinterpret_cast<float*>(ws + off); };
-  GradParts parts{reinterpret_cast<uint32_t*>(ws + f.off_ds), F(f.off_daq), F(f.off_dax), F(f.off_dw1), F(f.off_dw2),
+  GradParts parts{F(f.off_ds), F(f.off_daq), F(f.off_dax), F(f.off_dw1), F(f.off_dw2),
                   F(f.off_db1), F(f.off_db2)};
   float* acc = F(f.off_acc);
   const float* wglob = nullptr;

@@ -5,8 +5,15 @@
 // Precision.  W1 and W2 are bf16, exact.  What meets them on the way to the
 // float32 outputs (s, h and dl) is split into three bf16 terms, 8 + 8 + 8 bits by
 // truncation: exact, so that a product is as good as a float32 one at three
-// bf16 MFMAs (of 8 times the f32 rate).  du for ds, and both factors of dW1 and
-// dW2, which end in bf16, take two terms (16 bits; the products of two second terms are left out).
+// bf16 MFMAs (of 8 times the f32 rate).  Three values that only bf16 outputs are
+// made of take two terms, 16 bits: du on its way to ds, ds itself, and both factors
+// of dW1 and dW2 (the products of two second terms are left out).  An output's error
+// against 64 bits stays that of its own rounding to 8 bits (128 x 1031 of 8 x 8: dQ
+// 1.656e-3 in the norm, as from float32 operations), but one element in 80 to 230 of dQ, dX, dW1
+// and dW2 rounds to the other neighbour; and a sum whose terms cancel to less than
+// 2^-8 of their size keeps fewer than 8 bits.  A third term of ds would be half as much
+// again to write and read, one of the factors has no room in LDS.  MOL_FLAG_F32_GATING takes
+// the general form, which has none of these roundings.
 //
 // A wave takes units of 16 items of one query, independent of the other waves.
 // Lane (c = lane % 16, g = lane / 16) holds item c's slots (g, mu), mu < RUN,
@@ -55,39 +62,6 @@ constexpr size_t kSlabBytes = size_t(288) << 20;
 constexpr int kAhead = 2;                          // blocks of 32 of d loaded ahead
 constexpr int kJT = 4;                             // hidden tiles of 16 that LDS holds h and du of
 constexpr int kH = 16 * kJT;
-
-// high halves of a and b: their first bf16 terms by truncation
-__device__ __forceinline__ uint32_t high_halves(float a, float b) {
-  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-}
-__device__ __forceinline__ float rest(float a) { return a - __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
-
-// eight values as bf16 terms, two values a word
-template <int TERMS>
-struct Terms {
-  uint4 t[TERMS];
-};
-template <int TERMS>
-__device__ __forceinline__ Terms<TERMS> split(const float (&x)[8]) {
-  Terms<TERMS> o;
-  float v[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = x[e];
-#pragma unroll
-  for (int k = 0; k < TERMS; ++k) {
-    o.t[k] = make_uint4(high_halves(v[0], v[1]), high_halves(v[2], v[3]), high_halves(v[4], v[5]), high_halves(v[6], v[7]));
-    if (k + 1 < TERMS)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = rest(v[e]);
-  }
-  return o;
-}
-template <int TERMS>
-__device__ __forceinline__ f32x4_t mfma_terms(uint4 a, const Terms<TERMS>& b, f32x4_t c) {
-#pragma unroll
-  for (int k = TERMS - 1; k >= 0; --k) c = mfma_bf16(a, b.t[k], c);   // small terms first
-  return c;
-}
 
 // Elements t .. t + 7 of a row of `d` at base + off bytes, of which base is the
 // same for the whole wave; past the row's end zeros, or other elements of it
@@ -896,8 +870,8 @@ hipError_t launch_pairs(const DevProb& pr, const Bf16Plan& f, Bf16Dims dm, const
 }  // namespace
 
 bool bf16_supported(const DevProb& pr) {
-  // (a lane's offsets from its wave's bases in 32 bits)
-  return pr.dtype == MOL_BF16 && pr.Pq <= 8 && (pr.H <= kH ? pr.Px <= 8 : pr.H <= 2 * kH && pr.Px <= 4) && static_cast<long>(pr.N) * pr.d < (1l << 31) &&
+  // (a lane's offsets from its wave's bases in 32 bits; a problem that asks for float32 gets it throughout)
+  return pr.dtype == MOL_BF16 && !(pr.flags & MOL_FLAG_F32_GATING) && pr.Pq <= 8 && (pr.H <= kH ? pr.Px <= 8 : pr.H <= 2 * kH && pr.Px <= 4) && static_cast<long>(pr.N) * pr.d < (1l << 31) &&
          static_cast<long>(pr.N) * pr.P < (1l << 30);
 }
 
