@@ -623,9 +623,12 @@ class AdamwTensors:
     def __init__(self, p: List[torch.Tensor], g: List[torch.Tensor], m: List[torch.Tensor], v: List[torch.Tensor],
                  m_scale: Optional[List[torch.Tensor]] = None, v_scale: Optional[List[torch.Tensor]] = None,
                  weight_decay=0.0, out: Optional[dict] = None):
+        # (lists of its own: the descriptors hold addresses, which the caller's lists may let go of)
+        p, g, m, v = tuple(p), tuple(g), tuple(m), tuple(v)
+        m_scale, v_scale = (None if x is None else tuple(x) for x in (m_scale, v_scale))
+        out = {k: tuple(x) for k, x in (out or {}).items() if x is not None}
         n = len(p)
         lists = {"g": g, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale}
-        out = {k: x for k, x in (out or {}).items() if x is not None}
         unknown = set(out) - {"p", "m", "v", "m_scale", "v_scale", "copy"}
         _need(not unknown, f"unknown outputs {sorted(unknown)}")
         for name, x in list(lists.items()) + list(out.items()):
