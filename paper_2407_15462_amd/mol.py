@@ -710,6 +710,10 @@ class Learner:
 
     The copy of the items' table is laid out as a corpus: ``problem`` gives the
     retrieval problem of the model as it is.
+
+    To save a learner: ``master``, ``state`` (m and v, and of 8-bit states
+    m_scale and v_scale, by tensor) and ``steps``.  One made of the saved masters,
+    whose state and steps the saved ones are copied into, goes on bit for bit.
     """
 
     def __init__(self, queries, items, a_q, a_x, W1, b1, W2, b2, weight_decay: float = 0.0, states_8bit: bool = False,
@@ -736,6 +740,9 @@ class Learner:
             weight_decay=[weight_decay if n in self.copy else 0.0 for n in self.master],
             out=dict(copy=[self.copy.get(n) for n in self.master]))
         self.state = dict(m=m, v=v)
+        if any(eight.values()):
+            for k, x in (("m_scale", ms), ("v_scale", vs)):
+                self.state[k] = {n: t for n, t in zip(self.master, x) if t is not None}
         self.steps = torch.zeros(1, dtype=torch.int32, device=dev)   # on the GPU, so that a captured step counts on
         self.seed = seed
         self.shape = (Vq, V, Pq, Px, P, d)
