@@ -532,7 +532,8 @@ def softmax_loss(phi: torch.Tensor, target: torch.Tensor, ids: Optional[torch.Te
     columns target int32 [B], and its gradient: (loss [B], dphi [B][N]).
 
     ids int32 [N]: the columns' items; a column with a negative id, or with the
-    positive's id in another place than the positive's, is left out.  dphi is
+    positive's id in another place than the positive's, is left out (an id past
+    the tables, an empty slot to embed_lookup, is not: make it negative).  dphi is
     the gradient of sum_b row_weight[b] loss[b] (weights of 1 by default) and
     may be written over phi.
     """
@@ -750,8 +751,9 @@ class Learner:
     def step(self, query_ids: torch.Tensor, item_ids: torch.Tensor, target: torch.Tensor, lr,
              inv_temp: float = 20.0) -> torch.Tensor:
         """One optimisation step on B queries and N sampled items: query_ids int32
-        [B], item_ids int32 [N] (negative: an empty slot), target int32 [B]: the
-        column of each query's positive; lr: a number, or one float32 on the GPU
+        [B] (outside the table: a row of zeros, which adds to no gradient), item_ids
+        int32 [N] (outside the table: an empty slot, no candidate), target int32 [B]:
+        the column of each query's positive; lr: a number, or one float32 on the GPU
         (which a captured step reads when it runs).  Returns the losses [B] from
         before the step.  Allocates with torch and launches on the current stream
         only: it can be captured into a graph."""
@@ -766,6 +768,7 @@ class Learner:
         B, N = query_ids.numel(), item_ids.numel()
         M, C, G = self.master, self.copy, self.grad
         queries = C["queries"].view(1, Vq, Pq * d)
+        item_ids = item_ids.masked_fill(item_ids >= V, -1)       # (the loss takes negative ids alone for empty slots)
         prob = Problem(embed_lookup(queries, query_ids).view(B, Pq, d), embed_lookup(C["items"], item_ids),
                        embed_lookup(M["a_q"].view(1, Vq, P), query_ids).view(B, P),
                        embed_lookup(M["a_x"].view(1, V, P), item_ids).view(N, P), C["W1"], M["b1"], C["W2"], M["b2"])

@@ -40,3 +40,36 @@ def test_a_saved_learner_goes_on_bit_for_bit(states_8bit):
         assert torch.equal(whole.step(*ids[k], lr), again.step(*ids[k], lr)), k
     assert same(whole, again)
     assert ("m_scale" in whole.state) == ("v_scale" in whole.state) == states_8bit
+
+
+def test_an_item_id_past_the_table_is_an_empty_slot():
+    """In all of a step, as in the lookup: not a negative of score 0, and no positive."""
+    Vq, V, B, N = 40, 200, 16, 64
+    lr = torch.tensor([0.01], device="cuda")
+    q, items, target = (x.cuda() for x in batch(Vq, V, B, N, seed=1))
+    target[3] = 9
+    got = []
+    for empty in (-1, V, 2 ** 31 - 1):
+        learner, _ = make(Vq, V, 4, 4, 32, 32, seed=2)
+        ids = items.clone()
+        ids[9] = ids[40] = empty                          # a positive among them, and a negative
+        got.append((learner.step(q, ids, target, lr), learner))
+        assert float(got[-1][0][3]) == 0.0, "the positive of query 3 is an empty slot"
+        assert ids[9] == empty, "the caller's ids were written"
+    for loss, learner in got[1:]:
+        assert torch.equal(loss, got[0][0]) and same(learner, got[0][1])
+
+
+def test_a_query_id_past_the_table_adds_to_no_gradient():
+    Vq, V, B, N = 40, 200, 16, 64
+    lr = torch.tensor([0.01], device="cuda")
+    q, items, target = (x.cuda() for x in batch(Vq, V, B, N, seed=1))
+    learners = []
+    for empty, at in ((-1, 11), (Vq, 11), (-1, 20)):      # (whatever its positive is)
+        learner, _ = make(Vq, V, 4, 4, 32, 32, seed=2)
+        ids, t = q.clone(), target.clone()
+        ids[2], t[2] = empty, at
+        loss = learner.step(ids, items, t, lr)
+        assert bool(torch.isfinite(loss).all())
+        learners.append(learner)
+    assert same(learners[0], learners[1]) and same(learners[0], learners[2])
