@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import numbers
 import os
 from typing import Dict, List, Optional, Sequence, Tuple
 
@@ -438,6 +439,7 @@ def _operand(t: torch.Tensor, name: str, shape, dtypes, device) -> None:
 
 
 _FLOATS = (torch.float32, torch.bfloat16)
+_F32_MAX = torch.finfo(torch.float32).max
 _F32, _INT32 = (torch.float32,), (torch.int32,)
 _HERE_NOW = contextlib.nullcontext()
 
@@ -757,9 +759,13 @@ class Learner:
         (which a captured step reads when it runs).  Returns the losses [B] from
         before the step.  Allocates with torch and launches on the current stream
         only: it can be captured into a graph."""
+        # (what AdamW and the loss would refuse, before anything is changed)
         if isinstance(lr, torch.Tensor):
             _need(lr.numel() == 1, "lr must have one element")
-            _operand(lr, "lr", lr.shape, (torch.float32,), self.steps.device)   # (before anything is changed)
+            _operand(lr, "lr", lr.shape, (torch.float32,), self.steps.device)
+        else:
+            _need(isinstance(lr, numbers.Real) and 0 <= lr <= _F32_MAX, f"lr = {lr!r} is not a rate: a number from 0 to {_F32_MAX:g}")
+        _need(query_ids.numel() > 0 and item_ids.numel() > 0, "a step needs a query and an item")
         with _on(self.steps.device, None):
             return self._step(query_ids, item_ids, target, lr, inv_temp)
 

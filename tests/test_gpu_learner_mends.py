@@ -73,3 +73,31 @@ def test_a_query_id_past_the_table_adds_to_no_gradient():
         assert bool(torch.isfinite(loss).all())
         learners.append(learner)
     assert same(learners[0], learners[1]) and same(learners[0], learners[2])
+
+
+# ---------------------------------------------------------------- refusals
+def everything(learner):
+    return [bits(t).clone() for d in (learner.master, learner.copy, learner.grad, *learner.state.values()) for t in d.values()] + \
+        [learner.steps.clone()]
+
+
+@pytest.mark.parametrize("bad", [dict(lr=-0.01), dict(lr=float("nan")), dict(lr=float("inf")), dict(lr=1e39), dict(lr=None),
+                                 dict(lr="0.1"), dict(inv_temp=0.0), dict(inv_temp=float("inf")), dict(target="short"),
+                                 dict(target="wide"), dict(items="wide"), dict(items="none"), dict(queries="none")])
+def test_a_refused_step_changes_nothing(bad):
+    Vq, V, B, N = 40, 200, 16, 64
+    learner, _ = make(Vq, V, 4, 4, 32, 32, seed=2)
+    q, items, target = (x.cuda() for x in batch(Vq, V, B, N, seed=1))
+    learner.step(q, items, target, 0.01)
+    before = everything(learner)
+    kw = dict(lr=0.01, inv_temp=20.0)
+    kw.update({k: x for k, x in bad.items() if k in kw})
+    if "target" in bad:
+        target = target[:-1] if bad["target"] == "short" else target.long()
+    if "items" in bad:
+        items = items.long() if bad["items"] == "wide" else items[:0]
+    if bad.get("queries") == "none":
+        q, target = q[:0], target[:0]
+    with pytest.raises((ValueError, mol.MolError)):
+        learner.step(q, items, target, **kw)
+    assert all(torch.equal(a, b) for a, b in zip(before, everything(learner)))
