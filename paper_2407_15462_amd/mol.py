@@ -583,7 +583,9 @@ def score_grad(prob: Problem, dphi: torch.Tensor, ws=None, stream=None, only: Op
                out: Optional[dict] = None):
     """Gradients of score(prob) for the problem's tensors, given dphi [B][N]:
     a dict of dQ, dX, da_q, da_x, dW1, db1, dW2 and db2 (or those in ``only``),
-    each of its tensor's shape and type.  out: tensors to write some of them to."""
+    each of its tensor's shape and type.  out: tensors to write some of them to.
+    Problems with MOL_FLAG_F32_GATING: float32 throughout; bf16 ones without it keep
+    16 bits of what dQ, dX, dW1 and dW2 are summed from."""
     _operand(dphi, "dphi", (prob.B, prob.N), (torch.float32,), prob.device)
     names = _GRADS if only is None else tuple(only)
     if only is not None and not all(n in _GRADS for n in names):
@@ -709,7 +711,13 @@ class Learner:
     masters; a_q [Vq][P], a_x [V][P]: the gating logits of every query and item;
     W1 [H][P], b1 [H], W2 [P][H], b2 [P]: the gating MLP, all float32 (they are
     updated in place).  weight_decay is for the embeddings and W1, W2.
-    states_8bit: AdamW states of the two embedding tables in 8 bits.
+    states_8bit: AdamW states of the two embedding tables in 8 bits.  flags: the
+    precision of the gating MLP in a step's scores (MOL_FLAG_*); float32 by default,
+    since training moves its weights out of the range that the others are meant for
+    (1024 x 2048 pairs of 8 x 8: 430 us of a step's 1560; 0 takes 90, with weights of RMS
+    up to 0.3, MOL_FLAG_BF16X2_GATING 130, up to 1).  grad_flags: the same for the
+    gradients, whose chain has no such range; MOL_FLAG_F32_GATING keeps float32 up to
+    their rounding to bf16 (see score_grad).
 
     The copy of the items' table is laid out as a corpus: ``problem`` gives the
     retrieval problem of the model as it is.
@@ -720,7 +728,7 @@ class Learner:
     """
 
     def __init__(self, queries, items, a_q, a_x, W1, b1, W2, b2, weight_decay: float = 0.0, states_8bit: bool = False,
-                 seed: int = 0):
+                 seed: int = 0, flags: int = MOL_FLAG_F32_GATING, grad_flags: int = 0):
         Vq, Pq, d = queries.shape
         Px, V, _ = items.shape
         P, dev = Pq * Px, queries.device
@@ -747,7 +755,7 @@ class Learner:
             for k, x in (("m_scale", ms), ("v_scale", vs)):
                 self.state[k] = {n: t for n, t in zip(self.master, x) if t is not None}
         self.steps = torch.zeros(1, dtype=torch.int32, device=dev)   # on the GPU, so that a captured step counts on
-        self.seed = seed
+        self.seed, self.flags, self.grad_flags = seed, flags, grad_flags
         self.shape = (Vq, V, Pq, Px, P, d)
 
     def step(self, query_ids: torch.Tensor, item_ids: torch.Tensor, target: torch.Tensor, lr,
@@ -775,13 +783,13 @@ class Learner:
         M, C, G = self.master, self.copy, self.grad
         queries = C["queries"].view(1, Vq, Pq * d)
         item_ids = item_ids.masked_fill(item_ids >= V, -1)       # (the loss takes negative ids alone for empty slots)
-        prob = Problem(embed_lookup(queries, query_ids).view(B, Pq, d), embed_lookup(C["items"], item_ids),
-                       embed_lookup(M["a_q"].view(1, Vq, P), query_ids).view(B, P),
-                       embed_lookup(M["a_x"].view(1, V, P), item_ids).view(N, P), C["W1"], M["b1"], C["W2"], M["b2"])
-        phi = score(prob)
+        tensors = (embed_lookup(queries, query_ids).view(B, Pq, d), embed_lookup(C["items"], item_ids),
+                   embed_lookup(M["a_q"].view(1, Vq, P), query_ids).view(B, P),
+                   embed_lookup(M["a_x"].view(1, V, P), item_ids).view(N, P), C["W1"], M["b1"], C["W2"], M["b2"])
+        phi = score(Problem(*tensors, flags=self.flags))
         weight = torch.full((B,), 1.0 / B, device=phi.device)
         loss, dphi = softmax_loss(phi, target, item_ids, inv_temp, weight, dphi=phi)
-        g = score_grad(prob, dphi, out=dict(dW1=G["W1"], db1=G["b1"], dW2=G["W2"], db2=G["b2"]))
+        g = score_grad(Problem(*tensors, flags=self.grad_flags), dphi, out=dict(dW1=G["W1"], db1=G["b1"], dW2=G["W2"], db2=G["b2"]))
         embed_grad(g["dQ"].view(1, B, Pq * d), query_ids, Vq, out=G["queries"].view(1, Vq, Pq * d))
         embed_grad(g["dX"], item_ids, V, out=G["items"])
         embed_grad(g["da_q"].view(1, B, P), query_ids, Vq, out=G["a_q"].view(1, Vq, P))
@@ -791,7 +799,8 @@ class Learner:
         return loss
 
     def problem(self, query_ids: torch.Tensor, flags: int = 0) -> Problem:
-        """The retrieval problem of these queries against all items."""
+        """The retrieval problem of these queries against all items.  flags: 0 is
+        meant for gating weights of RMS up to 0.3 (see MOL_FLAG_*)."""
         Vq, V, Pq, Px, P, d = self.shape
         B = query_ids.numel()
         return Problem(embed_lookup(self.copy["queries"].view(1, Vq, Pq * d), query_ids).view(B, Pq, d), self.copy["items"],

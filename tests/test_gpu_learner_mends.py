@@ -101,3 +101,41 @@ def test_a_refused_step_changes_nothing(bad):
     with pytest.raises((ValueError, mol.MolError)):
         learner.step(q, items, target, **kw)
     assert all(torch.equal(a, b) for a, b in zip(before, everything(learner)))
+
+
+# ---------------------------------------------------------------- precision of the gating MLP
+@pytest.mark.parametrize("std", [0.5, 2.0])
+@pytest.mark.parametrize("Vq,V,Pq,Px,d,H,B,N", [(50, 300, 8, 8, 64, 64, 40, 120), (20, 90, 4, 4, 24, 32, 9, 33)])
+def test_a_step_with_large_gating_weights_follows_float64(Vq, V, Pq, Px, d, H, B, N, std):
+    """Weights that have left the range of the float16 chain (RMS 0.3): the losses and gradients keep the precision of small ones."""
+    log(f"[learner] Vq={Vq} V={V} {Pq}x{Px} d={d} H={H} B={B} N={N} weights of {std}")
+    _, t = make(Vq, V, Pq, Px, d, H, seed=1)
+    t["W1"], t["W2"] = t["W1"] * (std / 0.1), t["W2"] * (std / 0.1)
+    learner = mol.Learner(*(t[n].cuda().contiguous() for n in NAMES))
+    p = {n: learner.master[n].double().cpu() for n in NAMES}
+    copies = {n: learner.copy[n].cpu() for n in learner.copy}
+    state = {n: (torch.zeros_like(p[n]), torch.zeros_like(p[n])) for n in NAMES}
+    ids = batch(Vq, V, B, N, seed=1)
+    loss, g = step64(p, copies, state, ids, 0.01, 20.0, 0.0, 1)
+    got = learner.step(*(x.cuda() for x in ids), 0.01)
+    # scores within 1e-4 (the library's stated precision), z and the loss 20 times that, twice
+    assert float((got.double().cpu() - loss).abs().max()) < 4e-3
+    for n in NAMES:
+        rel = float((learner.grad[n].double().cpu() - g[n]).norm() / g[n].norm())
+        assert rel < 4e-3 + 2.0 ** -8 + 1e-4, (n, rel)
+
+
+def test_the_gating_of_a_step_is_the_callers_choice():
+    ids = tuple(x.cuda() for x in batch(50, 300, 40, 120, seed=4))
+    losses, grads = {}, {}
+    for name, kw in (("default", {}), ("f32", dict(flags=mol.MOL_FLAG_F32_GATING)), ("f16", dict(flags=0)),
+                     ("all f32", dict(grad_flags=mol.MOL_FLAG_F32_GATING))):
+        learner, _ = make(50, 300, 8, 8, 64, 64, seed=6, **kw)
+        losses[name] = learner.step(*ids, 0.01)
+        grads[name] = learner.grad["W1"].clone()
+    assert torch.equal(losses["default"], losses["f32"]) and torch.equal(losses["default"], losses["all f32"])
+    assert not torch.equal(losses["default"], losses["f16"]) and not torch.equal(grads["default"], grads["all f32"])
+    # both gradients a rounding to bf16 away from the same values, and those float32's errors apart
+    assert float((grads["default"] - grads["all f32"]).float().norm() / grads["default"].float().norm()) < 2.0 ** -8
+    with pytest.raises(mol.MolError):
+        make(50, 300, 8, 8, 64, 64, seed=6, flags=4)[0].step(*ids, 0.01)
