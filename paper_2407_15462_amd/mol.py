@@ -256,6 +256,12 @@ def _dtype(t) -> int:
     return _DTYPES[dt]
 
 
+def _sizes(*sizes: int) -> None:
+    """The library's sizes are int32: ctypes would cut others off to it."""
+    if max(sizes) >= 1 << 31 or min(sizes) < -(1 << 31):
+        raise ValueError(f"sizes {sizes}: the library takes up to 2^31 - 1")
+
+
 def mol_embed_lookup(table, ids, scale: float, out, stream=None) -> None:
     C, V, d = table.shape
     _check(load().mol_embed_lookup(_ptr(table), _dtype(table), C, V, d, _ptr(ids), ids.numel(), scale, _ptr(out),
@@ -263,6 +269,7 @@ def mol_embed_lookup(table, ids, scale: float, out, stream=None) -> None:
 
 
 def mol_embed_grad_workspace(C: int, V: int, d: int, T: int) -> int:
+    _sizes(C, V, d, T)
     out = ctypes.c_size_t(0)
     _check(load().mol_embed_grad_workspace(C, V, d, T, ctypes.byref(out)))
     return out.value
@@ -284,6 +291,7 @@ def mol_softmax_loss_workspace(B: int, N: int) -> int:
 
 def mol_softmax_loss(phi, target, ids, inv_temp: float, row_weight, loss, dphi, ws, stream=None) -> None:
     B, N = phi.shape
+    _sizes(B, N)
     _check(load().mol_softmax_loss(B, N, _ptr(phi), _ptr(target), _ptr(ids), inv_temp, _ptr(row_weight), _ptr(loss),
                                    _ptr(dphi), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream)))
 
@@ -483,6 +491,7 @@ def embed_lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dty
         raise ValueError(f"unsupported output dtype {dtype}")
     _operand(table, "table", None, _FLOATS, dev)
     _operand(ids, "ids", None, _INT32, dev)
+    _sizes(C, V, d, T)
     with _on(dev, stream):
         if out is None:
             out = table.new_empty((C, T, d), dtype=dtype)
@@ -512,6 +521,7 @@ def embed_grad(grad: torch.Tensor, ids: torch.Tensor, V: int, scale: float = 1.0
     dev = grad.device
     _operand(grad, "grad", None, _FLOATS, dev)
     _operand(ids, "ids", (T,), _INT32, dev)
+    _sizes(C, V, d, T)
     _need(out is not None or not accumulate, "accumulate needs out")
     dtype = dtype if out is None else out.dtype
     if dtype not in _FLOATS:
@@ -550,6 +560,7 @@ def softmax_loss(phi: torch.Tensor, target: torch.Tensor, ids: Optional[torch.Te
         _operand(row_weight, "row_weight", (B,), _F32, dev)
     if dphi is not None:
         _operand(dphi, "dphi", (B, N), _F32, dev)
+    _sizes(B, N)
     with _on(dev, stream):
         ws = _workspace(lambda: mol_softmax_loss_workspace(B, N), ws, dev)
         loss = phi.new_empty((B,))
@@ -566,6 +577,7 @@ def _check_problem(prob: Problem) -> None:
     """What the gradients rely on: every tensor of the sizes, type and device that Q, X and W1 imply."""
     B, N, P, d, H, e = prob.B, prob.N, prob.P, prob.d, prob.H, prob.tensors[0].dtype
     f32 = torch.float32
+    _sizes(B, N, P, d, H)
     _need(all(t is not None for t in prob.tensors), "the problem lacks a gating tensor")
     for name, t, n, dt in zip(("Q", "X", "a_q", "a_x", "W1", "b1", "W2", "b2"), prob.tensors,
                               (B * prob.Pq * d, prob.Px * N * d, B * P, N * P, H * P, H, P * H, P),
@@ -696,6 +708,7 @@ def adamw_step(tensors: AdamwTensors, lr=1e-3, beta1: float = 0.9, beta2: float 
         else:
             _need(name != "grad_scale" or t is None, "grad_scale must be a tensor")
     on_lr, on_step = isinstance(lr, torch.Tensor), isinstance(step, torch.Tensor)
+    _need(on_step or step < 1 << 31, f"step = {step} is not below 2^31")
     opt = MolAdamwC(0.0 if on_lr else lr, beta1, beta2, eps, 1 if on_step else step, seed & 0xFFFFFFFF, _ptr(grad_scale),
                     _ptr(lr) if on_lr else None, _ptr(step) if on_step else None)
     with _on(tensors.device, stream):

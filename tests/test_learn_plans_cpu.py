@@ -31,3 +31,35 @@ def test_adamw_plan_keeps_its_tensors_when_the_lists_change():
     del plan
     gc.collect()
     assert all(r() is None for r in held.values())
+
+
+# ---------------------------------------------------------------- sizes that the C ABI has no room for
+def meta(*shape, dtype=torch.float32):
+    return torch.empty(*shape, dtype=dtype, device="meta")
+
+
+I32, LONG = torch.int32, (1 << 31) + 5
+SIZES = [
+    ("table of 2^31 + 5 rows", lambda: mol.embed_lookup(meta(1, LONG, 4), meta(3, dtype=I32))),
+    ("2^31 + 5 ids", lambda: mol.embed_lookup(meta(1, 7, 4), meta(LONG, dtype=I32))),
+    ("2^32 + 5 ids", lambda: mol.embed_lookup(meta(1, 7, 4), meta((1 << 32) + 5, dtype=I32))),
+    ("rows of 2^32 + 8", lambda: mol.embed_lookup(meta(1, 7, (1 << 32) + 8), meta(3, dtype=I32))),
+    ("2^32 + 1 tables", lambda: mol.embed_lookup(meta((1 << 32) + 1, 1, 1), meta(3, dtype=I32))),
+    ("gradient onto 2^32 + 5 rows", lambda: mol.embed_grad(meta(1, 3, 4), meta(3, dtype=I32), (1 << 32) + 5)),
+    ("gradient of 2^32 + 5 tokens", lambda: mol.embed_grad(meta(1, (1 << 32) + 5, 4), meta((1 << 32) + 5, dtype=I32), 7)),
+    ("its workspace", lambda: mol.embed_grad_workspace(meta(1, 3, 4), (1 << 32) + 5)),
+    ("loss of 2^32 + 5 columns", lambda: mol.softmax_loss(meta(1, (1 << 32) + 5), meta(1, dtype=I32))),
+    ("loss of 2^32 + 1 rows", lambda: mol.softmax_loss(meta((1 << 32) + 1, 3), meta((1 << 32) + 1, dtype=I32))),
+    ("scores of 2^32 + 5 items", lambda: mol.score_grad(
+        mol.Problem(meta(1, 1, 4), meta(1, (1 << 32) + 5, 4), meta(1, 1), meta((1 << 32) + 5, 1), meta(1, 1), meta(1), meta(1, 1), meta(1)),
+        meta(1, (1 << 32) + 5))),
+    ("step 2^32 + 1", lambda: mol.adamw_step(mol.AdamwTensors([torch.zeros(3)], [torch.zeros(3)], [torch.zeros(3)], [torch.zeros(3)]),
+                                             step=(1 << 32) + 1)),
+]
+
+
+@pytest.mark.parametrize("what,call", SIZES, ids=[s[0] for s in SIZES])
+def test_sizes_past_32_bits_are_refused(what, call):
+    """They would be cut off to other sizes on their way into the library."""
+    with pytest.raises(ValueError, match="2\\^31"):
+        call()
