@@ -12,7 +12,7 @@ import ctypes
 import functools
 import numbers
 import os
-from typing import Dict, List, Optional, Sequence, Tuple
+from typing import List, Optional, Sequence, Tuple
 
 import torch
 
@@ -249,23 +249,10 @@ def mol_gap_bound_combined(B: int, P: int, m: int, dots, ids, kprime: int, avg_i
                                          _stream(stream)))
 
 
-def _dtype(t) -> int:
-    dt = t if isinstance(t, torch.dtype) else t.dtype
-    if dt not in _DTYPES:
-        raise ValueError(f"unsupported dtype {dt}: torch.float32 or torch.bfloat16")
-    return _DTYPES[dt]
-
-
 def _sizes(*sizes: int) -> None:
     """The library's sizes are int32: ctypes would cut others off to it."""
     if max(sizes) >= 1 << 31 or min(sizes) < -(1 << 31):
         raise ValueError(f"sizes {sizes}: the library takes up to 2^31 - 1")
-
-
-def mol_embed_lookup(table, ids, scale: float, out, stream=None) -> None:
-    C, V, d = table.shape
-    _check(load().mol_embed_lookup(_ptr(table), _dtype(table), C, V, d, _ptr(ids), ids.numel(), scale, _ptr(out),
-                                   _dtype(out), _stream(stream)))
 
 
 def mol_embed_grad_workspace(C: int, V: int, d: int, T: int) -> int:
@@ -273,13 +260,6 @@ def mol_embed_grad_workspace(C: int, V: int, d: int, T: int) -> int:
     out = ctypes.c_size_t(0)
     _check(load().mol_embed_grad_workspace(C, V, d, T, ctypes.byref(out)))
     return out.value
-
-
-def mol_embed_grad(grad, ids, scale: float, accumulate: bool, table_grad, ws, stream=None) -> None:
-    C, V, d = table_grad.shape
-    _check(load().mol_embed_grad(_ptr(grad), _dtype(grad), C, V, d, _ptr(ids), ids.numel(), scale, int(accumulate),
-                                 _ptr(table_grad), _dtype(table_grad), _ptr(ws), ws.numel() if ws is not None else 0,
-                                 _stream(stream)))
 
 
 @functools.lru_cache(maxsize=256)              # (a call of its own costs a tenth of a small loss)
@@ -294,12 +274,6 @@ def mol_softmax_loss(phi, target, ids, inv_temp: float, row_weight, loss, dphi, 
     _sizes(B, N)
     _check(load().mol_softmax_loss(B, N, _ptr(phi), _ptr(target), _ptr(ids), inv_temp, _ptr(row_weight), _ptr(loss),
                                    _ptr(dphi), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream)))
-
-
-def mol_score_grad(prob: Problem, dphi, grads: Dict[str, Optional[torch.Tensor]], ws, stream=None) -> None:
-    c = MolScoreGradsC(**{n: _ptr(t) for n, t in grads.items()})
-    _check(load().mol_score_grad(prob.ref, _ptr(dphi), ctypes.byref(c), _ptr(ws), ws.numel() if ws is not None else 0,
-                                 _stream(stream)))
 
 
 def mol_adamw_step(opt: MolAdamwC, tensors, n_tensors: int, stream=None) -> None:
