@@ -411,7 +411,8 @@ int mol_score_grad(const mol_problem *prob, const float *dphi,
  *   m' = beta1 m + (1 - beta1) g',   v' = beta2 v + (1 - beta2) g'^2
  *   p' = p (1 - lr weight_decay)
  *        - lr (m' / (1 - beta1^step)) / (sqrt(v' / (1 - beta2^step)) + eps)
- * in float32, from the new states before they are rounded.
+ * in float32, from the new states before they are rounded.  lr and weight_decay
+ * are from 0 to FLT_MAX, eps from FLT_MIN to FLT_MAX.
  *
  * A tensor's states are float32 (MOL_STATE_F32) or 8-bit (MOL_STATE_E4M3):
  * m and sqrt(v) as e4m3 codes with one float32 scale per run of

@@ -1374,8 +1374,10 @@ int mol_adamw_step(const mol_adamw* opt, const mol_adamw_tensor* tensors, int32_
   if (n_tensors > 0 && !tensors) return fail(MOL_EINVAL, "tensors is NULL");
   if (!(opt->beta1 >= 0 && opt->beta1 < 1 && opt->beta2 >= 0 && opt->beta2 < 1))
     return fail(MOL_EINVAL, "beta1 = %g, beta2 = %g: need 0 <= beta < 1", opt->beta1, opt->beta2);
-  if (!(opt->eps > 0)) return fail(MOL_EINVAL, "eps = %g is not positive", opt->eps);
-  if (!opt->lr_ptr && !(opt->lr >= 0)) return fail(MOL_EINVAL, "lr = %g is negative", opt->lr);
+  // (as float32, which the step is taken in; of a smaller eps the hardware's reciprocal is infinite)
+  if (!(opt->eps >= FLT_MIN && opt->eps <= FLT_MAX))
+    return fail(MOL_EINVAL, "eps = %g outside [%g, %g]", opt->eps, FLT_MIN, FLT_MAX);
+  if (!opt->lr_ptr && !(opt->lr >= 0 && opt->lr <= FLT_MAX)) return fail(MOL_EINVAL, "lr = %g outside [0, %g]", opt->lr, FLT_MAX);
   if (!opt->step_ptr && opt->step < 1) return fail(MOL_EINVAL, "step = %d: steps count from 1", opt->step);
   for (int32_t i = 0; i < n_tensors; ++i) {
     const mol_adamw_tensor& t = tensors[i];
@@ -1384,7 +1386,8 @@ int mol_adamw_step(const mol_adamw* opt, const mol_adamw_tensor* tensors, int32_
     if ((rc = check_dtype(t.param_dtype, "param_dtype")) || (rc = check_dtype(t.grad_dtype, "grad_dtype"))) return rc;
     if (t.state != MOL_STATE_F32 && t.state != MOL_STATE_E4M3)
       return fail(MOL_EUNSUPPORTED, "tensor %d: state = %d is not MOL_STATE_F32 or MOL_STATE_E4M3", i, t.state);
-    if (!(t.weight_decay >= 0)) return fail(MOL_EINVAL, "tensor %d: weight_decay = %g is negative", i, t.weight_decay);
+    if (!(t.weight_decay >= 0 && t.weight_decay <= FLT_MAX))
+      return fail(MOL_EINVAL, "tensor %d: weight_decay = %g outside [0, %g]", i, t.weight_decay, FLT_MAX);
     if (t.n == 0) continue;
     if (!t.p || !t.g || !t.m || !t.v || !t.p_out || !t.m_out || !t.v_out)
       return fail(MOL_EINVAL, "tensor %d: a pointer (p, g, m, v, p_out, m_out, v_out) is NULL", i);

@@ -63,3 +63,25 @@ def test_sizes_past_32_bits_are_refused(what, call):
     """They would be cut off to other sizes on their way into the library."""
     with pytest.raises(ValueError, match="2\\^31"):
         call()
+
+
+# ---------------------------------------------------------------- rates that float32 does not hold
+@pytest.mark.parametrize("bad", [dict(eps=1e-46), dict(eps=1e-40), dict(eps=1e39), dict(eps=float("inf")), dict(lr=1e39),
+                                 dict(lr=float("inf")), dict(decay=float("inf"))])
+def test_adamw_refuses_rates_outside_float32(bad):
+    """The step is taken in float32: there eps = 1e-46 is 0, and parameters that have had no gradient become 0 / 0."""
+    a = dict(lr=1e-3, eps=1e-8, decay=0.0)
+    a.update(bad)
+    opt = mol.MolAdamwC(a["lr"], 0.9, 0.999, a["eps"], 1, 0, None, None, None)
+    t = (mol.MolAdamwTensorC * 1)(mol.MolAdamwTensorC(0, *([None] * 12), 0, 0, 0, a["decay"], 0))
+    assert mol.load().mol_adamw_step(mol.ctypes.byref(opt), t, 1, None) == mol.MOL_EINVAL
+    assert mol.load().mol_last_error()
+
+
+@pytest.mark.parametrize("good", [dict(eps=1.2e-38), dict(eps=3e38), dict(lr=0.0), dict(lr=3e38)])
+def test_adamw_takes_rates_of_float32(good):
+    a = dict(lr=1e-3, eps=1e-8)
+    a.update(good)
+    opt = mol.MolAdamwC(a["lr"], 0.9, 0.999, a["eps"], 1, 0, None, None, None)
+    t = (mol.MolAdamwTensorC * 1)(mol.MolAdamwTensorC(0, *([None] * 12), 0, 0, 0, 0.0, 0))
+    assert mol.load().mol_adamw_step(mol.ctypes.byref(opt), t, 1, None) == mol.MOL_OK
