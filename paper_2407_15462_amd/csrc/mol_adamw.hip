@@ -172,6 +172,23 @@ __device__ __forceinline__ uint32_t encode4(const float (&x)[4], const uint32_t 
   return some ? static_cast<uint32_t>(c) : 0;
 }
 
+// sqrt(v) of v >= 0.  The hardware's root takes numbers below 2^-126 for 0, and a
+// gradient of 1e-19 leaves a v of 1e-41: small ones are taken 2^64 times as large.
+// EXACT (the root is stored): the last bit put right by one step from the reciprocal root.
+template <bool EXACT>
+__device__ __forceinline__ float root_of(float v) {
+  const bool small = v < 0x1p-96f;
+  const float x = small ? v * 0x1p64f : v;
+  float r;
+  if constexpr (EXACT) {
+    const float y = __builtin_amdgcn_rsqf(fmaxf(x, 0x1p-126f)), t = x * y;
+    r = fmaf(fmaf(-t, t, x), 0.5f * y, t);
+  } else {
+    r = __builtin_amdgcn_sqrtf(x);
+  }
+  return small ? r * 0x1p-32f : r;
+}
+
 struct Rates {
   float decay_lr, step_size, root;
   uint32_t mixed;
@@ -219,13 +236,7 @@ __device__ __forceinline__ void step_chunk(const AdamwArgs& a, const AdamwDesc& 
       const float m0 = E8 ? mk[e] : m[E8 ? 0 : k][e], v0 = E8 ? vk[e] * vk[e] : v[E8 ? 0 : k][e];
       mk[e] = a.beta1 * m0 + a.one_beta1 * gg;
       vk[e] = a.beta2 * v0 + a.one_beta2 * gg * gg;
-      if constexpr (E8) {
-        // the root is stored: the instruction's last bit put right by one step
-        const float y = __builtin_amdgcn_rsqf(fmaxf(vk[e], 0x1p-126f)), r = vk[e] * y;
-        root[e] = fmaf(fmaf(-r, r, vk[e]), 0.5f * y, r);
-      } else {
-        root[e] = __builtin_amdgcn_sqrtf(vk[e]);
-      }
+      root[e] = root_of<E8>(vk[e]);
       const float x = rt.step_size * mk[e] * __builtin_amdgcn_rcpf(fmaf(root[e], rt.root, a.eps));
       p[k][e] = p[k][e] * keep - x;
       if constexpr (E8) {

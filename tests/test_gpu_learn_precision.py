@@ -54,3 +54,29 @@ def test_score_grad_in_float32_is_one_rounding_off(B, N, Pq, Px, d, H):
     for n in NAMES:
         half = lh.HALF[got[n].dtype]
         lh.within(got[n], want[n], bound[n] + half * (1 + 2 * half) * want[n].abs(), n)
+
+
+# ------------------------------------------------------------------ AdamW
+@pytest.mark.parametrize("g0", [3e-20, 1e-19, 1e-18, 1e-17, 1e-15, 1e-3])
+@pytest.mark.parametrize("eight", [False, True], ids=["f32states", "e4m3states"])
+def test_adamw_of_the_smallest_second_moments(g0, eight):
+    """Second moments below 2^-126 (gradients below 3e-18) keep their root: with a small eps the step is lr, not m / eps.
+    v = 0.001 g g has three roundings and what underflow adds, 2^-150; its root half of that, and the step 16 more."""
+    n, eps, b1, b2 = 700, 1e-30, 0.9, 0.999
+    gen = torch.Generator().manual_seed(5)
+    p = torch.randn(n, generator=gen)
+    g = g0 * (1 + torch.rand(n, generator=gen)) * torch.where(torch.rand(n, generator=gen) < 0.5, -1.0, 1.0)
+    zeros = lambda: torch.zeros(n, dtype=torch.float8_e4m3fn if eight else torch.float32, device="cuda")  # noqa: E731
+    got, m, v = p.cuda(), zeros(), zeros()
+    scales = [[torch.zeros(3, device="cuda")] for _ in range(2)] if eight else [None, None]
+    mol.adamw_step(mol.AdamwTensors([got], [g.cuda()], [m], [v], *scales), lr=0.5, eps=eps)
+    want, wm, wv = lh.adamw(p, g, torch.zeros(n), torch.zeros(n), 0.5, b1, b2, eps, 0.0, 1)
+    rel = 2.0 ** -150 / wv + 20 * lh.U
+    lh.within(got, want, (p.double() - want).abs() * rel + 2 * lh.U * (p.double().abs() + 0.5), "p")
+    if eight:
+        top = torch.stack([x.abs().max() for x in wv.sqrt().split(256)])
+        lh.within(scales[1][0], top / 448, top * (2.0 ** -150 / wv.min() + 12 * lh.U), "scale of v")
+        back = v.float().double().cpu() * scales[1][0].double().cpu().repeat_interleave(256)[:n]
+        assert bool(((back / wv.sqrt() - 1).abs() <= 0.126).all()), "codes: a neighbour's distance is an eighth at most"
+    else:
+        lh.within(v, wv, wv * 4 * lh.U + 2.0 ** -150, "v")
