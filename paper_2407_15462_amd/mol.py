@@ -682,7 +682,8 @@ def adamw_step(tensors: AdamwTensors, lr=1e-3, beta1: float = 0.9, beta2: float 
         else:
             _need(name != "grad_scale" or t is None, "grad_scale must be a tensor")
     on_lr, on_step = isinstance(lr, torch.Tensor), isinstance(step, torch.Tensor)
-    _need(on_step or step < 1 << 31, f"step = {step} is not below 2^31")
+    if not on_step and step >= 1 << 31:
+        raise ValueError(f"step = {step} is not below 2^31")
     opt = MolAdamwC(0.0 if on_lr else lr, beta1, beta2, eps, 1 if on_step else step, seed & 0xFFFFFFFF, _ptr(grad_scale),
                     _ptr(lr) if on_lr else None, _ptr(step) if on_step else None)
     with _on(tensors.device, stream):
@@ -758,8 +759,8 @@ class Learner:
         if isinstance(lr, torch.Tensor):
             _need(lr.numel() == 1, "lr must have one element")
             _operand(lr, "lr", lr.shape, (torch.float32,), self.steps.device)
-        else:
-            _need(isinstance(lr, numbers.Real) and 0 <= lr <= _F32_MAX, f"lr = {lr!r} is not a rate: a number from 0 to {_F32_MAX:g}")
+        elif not isinstance(lr, numbers.Real) or not 0 <= lr <= _F32_MAX:
+            raise ValueError(f"lr = {lr!r} is not a rate: a number from 0 to {_F32_MAX:g}")
         _need(query_ids.numel() > 0 and item_ids.numel() > 0, "a step needs a query and an item")
         with _on(self.steps.device, None):
             return self._step(query_ids, item_ids, target, lr, inv_temp)
