@@ -152,6 +152,8 @@ typedef struct mol_problem {
  * library gives them; the least they take is in the message of
  * MOL_EWORKSPACE.  The rows are the same (mol_rerank's within the precision of
  * the gating MLP: without room for its dot products it scores in float32).
+ * mol_score_grad has one form; the size given for B and N is enough for every
+ * problem of the same shape, type and flags with no more queries or items.
  * Returns MOL_OK or the validation error the entry point would return. */
 int mol_workspace_size(const mol_problem *prob, int op, int32_t k,
                        int32_t kprime, int32_t C, size_t *bytes);
@@ -343,7 +345,8 @@ int mol_embed_lookup(const void *table, int32_t table_dtype, int32_t C,
  * others are neither read nor written (T == 0: nothing is).  The tokens are
  * sorted by id, stably, and each row is summed in float32, in an order that
  * only ids and the sizes fix, and rounded once.  Needs
- * mol_embed_grad_workspace bytes of workspace (256-byte aligned). */
+ * mol_embed_grad_workspace bytes of workspace (256-byte aligned); those for T
+ * tokens are enough for fewer. */
 int mol_embed_grad_workspace(int32_t C, int32_t V, int32_t d, int32_t T,
                              size_t *bytes);
 int mol_embed_grad(const void *grad, int32_t grad_dtype, int32_t C, int32_t V,
@@ -364,7 +367,8 @@ int mol_embed_grad(const void *grad, int32_t grad_dtype, int32_t C, int32_t V,
  * 0.  The tables' length is not known here: an id past it, an empty slot to
  * mol_embed_lookup, is made negative by the caller.  row_weight float32 [B] is the gradient of the total for loss[b] (NULL:
  * 1 each); it does not scale loss.  loss may be NULL, and dphi may be NULL
- * or phi itself.  Maximum, sum and loss are float32. */
+ * or phi itself.  Maximum, sum and loss are float32.  The workspace for B
+ * rows of N columns is enough for fewer of either. */
 int mol_softmax_loss_workspace(int32_t B, int32_t N, size_t *bytes);
 int mol_softmax_loss(int32_t B, int32_t N, const float *phi,
                      const int32_t *target, const int32_t *ids, float inv_temp,

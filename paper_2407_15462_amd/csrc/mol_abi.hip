@@ -1106,7 +1106,7 @@ int mol_workspace_size(const mol_problem* prob, int op, int32_t k, int32_t kprim
       return MOL_OK;
     case MOL_OP_SCORE_GRAD:
       if ((rc = check_problem(prob, true))) return rc;
-      *bytes = score_grad_bytes(dev_prob(prob));
+      *bytes = score_grad_most(dev_prob(prob));
       return MOL_OK;
     default:
       return fail(MOL_EINVAL, "unknown op %d", op);
@@ -1307,8 +1307,7 @@ int mol_embed_grad_workspace(int32_t C, int32_t V, int32_t d, int32_t T, size_t*
   int rc;
   if ((rc = check_rows(C, V, d, T))) return rc;
   if (!bytes) return fail(MOL_EINVAL, "bytes is NULL");
-  size_t off[4];
-  *bytes = embed_grad_bytes(C, V, d, T, off);
+  *bytes = embed_grad_most(C, V, d, T);
   return MOL_OK;
 }
 
@@ -1339,7 +1338,7 @@ int mol_softmax_loss_workspace(int32_t B, int32_t N, size_t* bytes) {
   int rc;
   if ((rc = check_loss(B, N))) return rc;
   if (!bytes) return fail(MOL_EINVAL, "bytes is NULL");
-  *bytes = softmax_loss_bytes(B, N);
+  *bytes = softmax_loss_most(B, N);
   return MOL_OK;
 }
 

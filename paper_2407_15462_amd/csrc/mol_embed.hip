@@ -592,17 +592,34 @@ GradArgs grad_args(int C, int V, int d, long T, int VE) {
 
 }  // namespace
 
-size_t embed_grad_bytes(int C, int V, int d, long T, size_t off[4]) {
+static size_t grad_layout(int C, int d, long T, size_t spans, size_t off[4]) {
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   size_t at = 0;
   off[0] = at; at = up(at + 8ul * T);                      // sorted pairs
   off[1] = at; if (T > kSortRank) at = up(at + 8ul * T);    // the other side of the passes
   off[2] = at; if (T > kSortRank) at = up(at + 4ul * kSortBlocks * (1 << kMaxBits));
   off[3] = at;
-  size_t spans = 0;
-  for (int VE : {1, 4, 8}) spans = std::max<size_t>(spans, grad_args(C, V, d, T, VE).spans);
   if (spans > 1) at = up(at + 8ul * spans * C * d);
   return at;
+}
+
+size_t embed_grad_bytes(int C, int V, int d, long T, size_t off[4]) {
+  size_t spans = 0;
+  for (int VE : {1, 4, 8}) spans = std::max<size_t>(spans, grad_args(C, V, d, T, VE).spans);
+  return grad_layout(C, d, T, spans, off);
+}
+
+// Spans of up to T tokens: teams of 32 tokens make the most of the longest list, and
+// fewer tokens a team (4 at least) are taken up to 512 workgroups, which at most doubles them.
+size_t embed_grad_most(int C, int V, int d, long T) {
+  size_t spans = 0, off[4];
+  for (int VE : {1, 4, 8}) {
+    const GradArgs a = grad_args(C, V, d, T, VE);
+    const long teams = 256 >> a.lpr_log2, per_span = static_cast<long>(a.slices) * C;
+    const long few = std::min((T + 4 * teams - 1) / (4 * teams), 2 * ((511 + per_span) / per_span));
+    spans = std::max<size_t>(spans, std::max((T + 32 * teams - 1) / (32 * teams), few));
+  }
+  return grad_layout(C, d, T, spans, off);
 }
 
 template <typename TI, typename TO>

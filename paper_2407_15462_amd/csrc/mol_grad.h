@@ -1,6 +1,8 @@
 // Pieces shared by the two forms of the score gradient.
 #pragma once
 
+#include <algorithm>
+
 #include "mol_tile.h"
 
 namespace mol {
@@ -37,18 +39,23 @@ struct SumList {
 
 // The bf16 form on 16-bit matrix instructions (mol_score_grad_bf16.hip).
 bool bf16_supported(const DevProb& pr);
-size_t bf16_bytes(const DevProb& pr);
+size_t bf16_bytes(const DevProb& pr);      // of a call
+size_t bf16_most(const DevProb& pr);       // of every call with the same shape and no more queries or items; 0: none takes this form
 hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_grads& o, char* ws, hipStream_t st);
 
 // K splits of a product of `waves` waves a part with `chunks` K chunks: about 2048
 // waves in all, with two chunks a split up to 64 splits (a short product is a chain of
 // latencies) and `least` beyond (each split is a part to write and to add).
+inline long most_splits(long chunks, long least) { return std::max(std::min(chunks / 2, 64l), chunks / least); }
 inline int split_of(long waves, long chunks, long least) {
   const long want = (2048 + waves / 2) / waves;
-  long most = chunks / 2 < 64 ? chunks / 2 : 64;
-  if (chunks / least > most) most = chunks / least;
-  const long n = want < most ? want : most;
-  return static_cast<int>(n < 1 ? 1 : n);
+  return static_cast<int>(std::max(1l, std::min(want, most_splits(chunks, least))));
+}
+// Bytes of the parts of such a product of `out` bytes: two splits or more leave at
+// most 2730 tiles of 32 x 64 floats (n splits of w waves, n w <= 2048 + w / 2 and 2 w <= n w).
+inline size_t most_parts(size_t out, long chunks, long least) {
+  const long n = most_splits(chunks, least);
+  return n < 2 ? 0 : std::min<size_t>(2730ul * 8192, n * out);
 }
 
 // high halves of a and b: their first bf16 terms by truncation

@@ -232,19 +232,22 @@ namespace mol {
 // Embedding rows by id and the gradient of their tables (mol_embed.hip).
 hipError_t launch_embed_lookup(const void* table, int table_dtype, int C, int V, int d, const int32_t* ids, int T,
                                float scale, void* out, int out_dtype, hipStream_t st);
-// workspace of the gradient: bytes, and where its parts begin
+// workspace of the gradient: bytes, and where its parts begin; most: of up to T tokens
 size_t embed_grad_bytes(int C, int V, int d, long T, size_t off[4]);
+size_t embed_grad_most(int C, int V, int d, long T);
 hipError_t launch_embed_grad(const void* grad, int grad_dtype, int C, int V, int d, const int32_t* ids, int T,
                              float scale, int accumulate, void* out, int out_dtype, void* ws, hipStream_t st);
 
-// Sampled-softmax loss and gradient (mol_loss.hip); ws: softmax_loss_bytes
+// Sampled-softmax loss and gradient (mol_loss.hip); ws: softmax_loss_bytes; most: of up to B rows of up to N
 size_t softmax_loss_bytes(int B, int N);
+size_t softmax_loss_most(int B, int N);
 hipError_t launch_softmax_loss(int B, int N, const float* phi, const int32_t* target, const int32_t* ids,
                                float inv_temp, const float* row_weight, float* loss, float* dphi, void* ws,
                                hipStream_t st);
 
-// Gradient of the scores for every input (mol_score_grad.hip); ws: score_grad_bytes
+// Gradient of the scores for every input (mol_score_grad.hip); ws: score_grad_bytes; most: of up to B queries and N items
 size_t score_grad_bytes(const DevProb& pr);
+size_t score_grad_most(const DevProb& pr);
 hipError_t launch_score_grad(const DevProb& pr, const float* dphi, const mol_score_grads& o, void* ws, hipStream_t st);
 
 // AdamW over many tensors (mol_adamw.hip); arguments checked

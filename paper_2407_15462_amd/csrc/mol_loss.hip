@@ -268,6 +268,14 @@ size_t softmax_loss_bytes(int B, int N) {
   return parts == 1 ? 0 : (4ul * B * (2ul * parts + 1) + 255) / 256 * 256;
 }
 
+// the most of up to B rows of up to N columns: rows of ceil(1024 / B) parts, of which B times
+// as many pass 1024 by up to B - 1, two at least and one for 8192 columns at most
+size_t softmax_loss_most(int B, int N) {
+  if (N <= 1024 * kRegs) return 0;
+  const size_t b = B, parts = std::max(2 * b, std::min(b * ((N + 8191ul) / 8192), 1023 + b));
+  return (4 * (2 * parts + b) + 255) / 256 * 256;
+}
+
 hipError_t launch_softmax_loss(int B, int N, const float* phi, const int32_t* target, const int32_t* ids,
                                float inv_temp, const float* row_weight, float* loss, float* dphi, void* ws,
                                hipStream_t st) {

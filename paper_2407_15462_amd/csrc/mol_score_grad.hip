@@ -710,20 +710,24 @@ struct GradPlan {
   size_t off_w, off_u, off_ds, off_daq, off_dax, off_dw1, off_dw2, off_db1, off_db2, off_pq, off_px, off_acc, bytes;
   long a_daq, a_dw1, a_dw2, a_db1, a_db2, a_dq;   // floats into the sums over slabs
   int wgs;
+  int cus;                              // workgroups that run at once
+  size_t wg_bytes;                      // of a workgroup's sums, and of u where LDS has no room
 };
 
-template <typename T, int PV>
-GradPlan plan_grad(const DevProb& pr) {
+int queries_of(long B) { return B >= 4 ? 4 : B >= 2 ? 2 : 1; }
+
+// What a plan owes to the shape and to QB, the queries of a tile.
+template <int PV>
+GradPlan plan_shape(const DevProb& pr, int QB) {
   GradPlan f{};
   f.JT = (pr.H + 15) / 16;
   f.jtg = group_tiles<PV>(f.JT <= 4);
   f.groups = (f.JT + f.jtg - 1) / f.jtg;
   GradDims& dm = f.dm;
-  dm.QB = pr.B >= 4 ? 4 : pr.B >= 2 ? 2 : 1;
+  dm.QB = QB;
   dm.upq_log2 = dm.QB == 4 ? 1 : dm.QB == 2 ? 2 : 3;
   dm.TI = kPairs / dm.QB;
   dm.TIP = dm.TI + 4;
-  dm.m = static_cast<long>(pr.B) * pr.Pq;
   // LDS has room for both up to P H = 4096; u is the less to read from the caches
   constexpr size_t most = 160 * 1024 / 4;
   f.ulds = grad_lds<PV>(f.JT, true, true, dm) <= most;
@@ -733,22 +737,37 @@ GradPlan plan_grad(const DevProb& pr) {
   // the final sums take the same place: dW1 and dW2 by four blocks, db1, then [TI][PV + 1] of da_x
   f.lds = std::max<size_t>(f.lds, 4 * (kSumFloats + 16ul * kWaves * f.jtg));
   f.lds = std::max<size_t>(f.lds, 4ul * dm.TI * (PV + 1));
-  // of ds, and of what a tile's workgroup leaves: dW1, dW2 and u
-  const long per_item = 4l * pr.Px * dm.m + (8l * pr.H * pr.P + (f.ulds ? 0 : 1024l * kWaves * f.JT)) / dm.TI;
+  f.cus = PV == 16 && f.jtg == 4 && f.lds <= 80 * 1024 ? 512 : 256;
+  f.wg_bytes = 4ul * (2ul * pr.H * pr.P + pr.H + pr.P) + (f.ulds ? 0 : 1024ul * kWaves * f.JT);
+  return f;
+}
+// bytes of an item of a slab: ds, da_x, and what a tile's workgroup leaves (its sums and u)
+size_t item_bytes(const DevProb& pr, const GradPlan& f, long B) {
+  return 4ul * pr.P * (B + 1) + (f.wg_bytes + f.dm.TI - 1) / f.dm.TI;
+}
+// least chunks of a long product's split: 128 items or query vectors
+template <typename T>
+constexpr int kChunk = 64 / sizeof(T);
+template <typename T>
+constexpr int kLeast = 128 / kChunk<T>;
+
+template <typename T, int PV>
+GradPlan plan_grad(const DevProb& pr) {
+  GradPlan f = plan_shape<PV>(pr, queries_of(pr.B));
+  GradDims& dm = f.dm;
+  dm.m = static_cast<long>(pr.B) * pr.Pq;
   const long tiles = (static_cast<long>(pr.N) + dm.TI - 1) / dm.TI;
-  const long fit = std::max<long>(1, static_cast<long>(kSlabBytes) / (per_item * dm.TI));
+  const long fit = std::max<long>(1, static_cast<long>(kSlabBytes / (item_bytes(pr, f, pr.B) * dm.TI)));
   f.slabs = static_cast<int>((tiles + fit - 1) / fit);
   f.slab = static_cast<int>((tiles + f.slabs - 1) / f.slabs * dm.TI);
   f.slabs = static_cast<int>((static_cast<long>(pr.N) + f.slab - 1) / f.slab);
   dm.ns = f.slab;
   const int st = f.slab / dm.TI, nqb = (pr.B + dm.QB - 1) / dm.QB;
-  const int cus = PV == 16 && f.jtg == 4 && f.lds <= 80 * 1024 ? 512 : 256;   // workgroups that run at once
-  dm.qsplits = std::max(1, std::min(nqb, cus / st));
+  dm.qsplits = std::max(1, std::min(nqb, f.cus / st));
   f.wgs = st * dm.qsplits;
-  constexpr int KCH = 64 / sizeof(T), kLeast = 128 / KCH;   // 128 items or query vectors
   const long cg = (pr.d + 63) / 64;
-  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * f.slab / KCH, kLeast);
-  f.sp_x = split_of((f.slab + 31l) / 32 * cg * pr.Px, (dm.m + 31) / 32 * 32 / KCH, kLeast);
+  f.sp_q = split_of((dm.m + 31) / 32 * cg, static_cast<long>(pr.Px) * f.slab / kChunk<T>, kLeast<T>);
+  f.sp_x = split_of((f.slab + 31l) / 32 * cg * pr.Px, (dm.m + 31) / 32 * 32 / kChunk<T>, kLeast<T>);
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   size_t at = 0;
   const size_t P = pr.P, H = pr.H;
@@ -772,6 +791,29 @@ GradPlan plan_grad(const DevProb& pr) {
   f.off_acc = at; at = up(at + 4ul * (f.a_dq + (f.slabs > 1 ? dm.m * pr.d : 0)));
   f.bytes = at;
   return f;
+}
+
+// The most that plan_grad takes of the same shape with no more queries or items: each
+// term bounds a part of the workspace by what grows with B and N alone, for the batches of each QB.
+template <typename T, int PV>
+size_t most_grad(const DevProb& pr) {
+  size_t most = 0;
+  for (int QB = 1; QB <= queries_of(pr.B); QB *= 2) {
+    const GradPlan f = plan_shape<PV>(pr, QB);
+    const size_t B = std::min<long>(pr.B, QB == 4 ? pr.B : 2 * QB - 1), m = B * pr.Pq, P = pr.P, TI = f.dm.TI;
+    const size_t tiles = (pr.N + TI - 1) / TI, items = tiles * TI, item = item_bytes(pr, f, B);
+    // ds, da_x of one range of queries and the workgroups' sums; da_q is a sixteenth of ds
+    const size_t slab = std::min(item * items, std::max(kSlabBytes, TI * item));
+    // more ranges of queries: f.cus workgroups at most
+    const size_t nqb = (B + QB - 1) / QB;
+    const size_t ranges = f.wg_bytes * std::min<size_t>(f.cus, nqb * tiles) + 4 * P * std::min(f.cus * TI, nqb * items);
+    const size_t q = 4 * m * pr.d, chunks = (m + 31) / 32 * 32 / kChunk<T>;
+    const size_t products = std::max(q, most_parts(q, pr.Px * items / kChunk<T>, kLeast<T>)) +
+                            most_parts(4 * pr.Px * items * pr.d, chunks, kLeast<T>);
+    const size_t weights = f.wlds ? 0 : 16ul * f.JT * (PV / 16) * 256;
+    most = std::max(most, weights + slab + slab / 16 + ranges + products + 4 * B * P + f.wg_bytes + q + 16 * 256);
+  }
+  return (most + 255) / 256 * 256;
 }
 
 template <typename T, int PV>
@@ -857,6 +899,15 @@ size_t score_grad_bytes(const DevProb& pr) {
   if (pr.dtype == MOL_BF16)
     return (pr.P <= 16 ? plan_grad<bf16_t, 16>(pr) : pr.P <= 32 ? plan_grad<bf16_t, 32>(pr) : plan_grad<bf16_t, 64>(pr)).bytes;
   return (pr.P <= 16 ? plan_grad<float, 16>(pr) : pr.P <= 32 ? plan_grad<float, 32>(pr) : plan_grad<float, 64>(pr)).bytes;
+}
+
+size_t score_grad_most(const DevProb& pr) {
+  if (bf16_supported(pr)) return bf16_most(pr);
+  const size_t general =
+      pr.dtype == MOL_BF16
+          ? (pr.P <= 16 ? most_grad<bf16_t, 16>(pr) : pr.P <= 32 ? most_grad<bf16_t, 32>(pr) : most_grad<bf16_t, 64>(pr))
+          : (pr.P <= 16 ? most_grad<float, 16>(pr) : pr.P <= 32 ? most_grad<float, 32>(pr) : most_grad<float, 64>(pr));
+  return std::max(general, bf16_most(pr));   // (a shorter corpus may take the bf16 form)
 }
 
 hipError_t launch_score_grad(const DevProb& pr, const float* dphi, const mol_score_grads& o, void* ws, hipStream_t st) {

@@ -798,15 +798,20 @@ struct Bf16Plan {
   long a_dw1, a_dw2, a_db1, a_db2, a_dq;       // floats into the sums over slabs
 };
 
+// waves that share 16 items, and the bytes of an item of a slab: ds, da_x and what the workgroups leave
+int queries_of(long B) { return B >= 8 ? 8 : B >= 4 ? 4 : B >= 2 ? 2 : 1; }
+size_t wg_bytes(const DevProb& pr) { return 4ul * (2ul * pr.H * pr.P + pr.H + pr.P); }
+size_t item_bytes(const DevProb& pr, long B, int QB) {
+  return 4ul * pr.P * (B + 1) + (wg_bytes(pr) * QB + 16 * kWaves - 1) / (16 * kWaves);
+}
+
 Bf16Plan plan(const DevProb& pr) {
   Bf16Plan f{};
   Bf16Dims& dm = f.dm;
-  dm.QB = pr.B >= 8 ? 8 : pr.B >= 4 ? 4 : pr.B >= 2 ? 2 : 1;
+  dm.QB = queries_of(pr.B);
   dm.m = static_cast<long>(pr.B) * pr.Pq;
   const long blocks = (pr.N + 31l) / 32;                              // slabs of whole pairs of 16 items
-  // of ds, and of a workgroup's dW1 and dW2
-  const long per_item = 4l * pr.Px * dm.m + 8l * pr.H * pr.P * dm.QB / (16 * kWaves);
-  const long fit = std::max<long>(1, static_cast<long>(kSlabBytes) / (32 * per_item));
+  const long fit = std::max<long>(1, static_cast<long>(kSlabBytes / (32 * item_bytes(pr, pr.B, dm.QB))));
   f.slabs = static_cast<int>((blocks + fit - 1) / fit);
   f.slab = static_cast<int>((blocks + f.slabs - 1) / f.slabs * 32);
   f.slabs = static_cast<int>((static_cast<long>(pr.N) + f.slab - 1) / f.slab);
@@ -869,13 +874,37 @@ hipError_t launch_pairs(const DevProb& pr, const Bf16Plan& f, Bf16Dims dm, const
 
 }  // namespace
 
+// (a problem that asks for float32 gets it throughout)
+static bool bf16_shape(const DevProb& pr) {
+  return pr.dtype == MOL_BF16 && !(pr.flags & MOL_FLAG_F32_GATING) && pr.Pq <= 8 &&
+         (pr.H <= kH ? pr.Px <= 8 : pr.H <= 2 * kH && pr.Px <= 4);
+}
 bool bf16_supported(const DevProb& pr) {
-  // (a lane's offsets from its wave's bases in 32 bits; a problem that asks for float32 gets it throughout)
-  return pr.dtype == MOL_BF16 && !(pr.flags & MOL_FLAG_F32_GATING) && pr.Pq <= 8 && (pr.H <= kH ? pr.Px <= 8 : pr.H <= 2 * kH && pr.Px <= 4) && static_cast<long>(pr.N) * pr.d < (1l << 31) &&
-         static_cast<long>(pr.N) * pr.P < (1l << 30);
+  // (a lane's offsets from its wave's bases in 32 bits)
+  return bf16_shape(pr) && static_cast<long>(pr.N) * pr.d < (1l << 31) && static_cast<long>(pr.N) * pr.P < (1l << 30);
 }
 
 size_t bf16_bytes(const DevProb& pr) { return plan(pr).bytes; }
+
+// Each term bounds a part of plan()'s workspace by what grows with B and N alone, for
+// the batches of each QB: slabs, splits and ranges of the queries fall as well as rise with them.
+size_t bf16_most(const DevProb& pr) {
+  if (!bf16_shape(pr)) return 0;
+  size_t most = 0;
+  for (int QB = 1; QB <= queries_of(pr.B); QB *= 2) {
+    const size_t B = std::min<long>(pr.B, QB == 8 ? pr.B : 2 * QB - 1), m = B * pr.Pq, P = pr.P;
+    const size_t items = (pr.N + 31ul) / 32 * 32, item = item_bytes(pr, B, QB), wg = wg_bytes(pr);
+    // ds, da_x of one range of queries and the workgroups' sums; da_q is a sixteenth of ds
+    const size_t slab = std::min(item * items, std::max(kSlabBytes, 32 * item)) + wg;
+    // more ranges of queries: 256 workgroups at most
+    const size_t steps = (B + QB - 1) / QB, wgs = std::min<size_t>(256, steps * (items * QB / (16 * kWaves) + 1));
+    const size_t ranges = wg * wgs + 4 * P * std::min<size_t>(256ul * 16 * kWaves / QB, steps * items);
+    const size_t q = 4 * m * pr.d;
+    const size_t products = std::max(q, most_parts(q, pr.Px * items / 32, 4)) + most_parts(4 * pr.Px * items * pr.d, (m + 31) / 32, 4);
+    most = std::max(most, slab + slab / 16 + ranges + products + 4 * B * P + wg + q + 16 * 256);
+  }
+  return (most + 255) / 256 * 256;
+}
 
 hipError_t launch_bf16(const DevProb& pr, const float* dphi, const mol_score_grads& o, char* ws, hipStream_t st) {
   const Bf16Plan f = plan(pr);
