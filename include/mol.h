@@ -382,7 +382,8 @@ int mol_softmax_loss(int32_t B, int32_t N, const float *phi,
  *   dh   = W2^T dl                     dW2 = sum dl SiLU(u)^T,  db2 = sum dl
  *   du   = dh sig (1 + u (1 - sig))    dW1 = sum du s^T,        db1 = sum du
  *   ds   = g pi + W1^T du              dQ = sum ds X,           dX = sum ds Q
- * Each output has its tensor's shape and type, and any may be NULL.  Every
+ * Each output has its tensor's shape and type, and any may be NULL (without
+ * dQ and dX their products are saved, without the others little).  Every
  * element is written.  Outputs overlap neither the inputs nor each other.
  *
  * Precision.  float32 problems, and bf16 ones with MOL_FLAG_F32_GATING: float32

@@ -6,7 +6,7 @@
 // Bound by memory: every buffer is read or written once (28 bytes an element in
 // float32, 16 with 8-bit states, bf16 gradients and a bf16 copy): 3 M elements of
 // 24 float32 tensors in 16 us (5.2 TB/s), 173 M with 8-bit states in 520 us (5.3 TB/s,
-// a copy runs at 4.6).  A launch takes up to kMaxTensors tensors, described in
+// a copy runs at 4.6); with step and rate on the GPU 17 and 524.  A launch takes up to kMaxTensors tensors, described in
 // its arguments; workgroups have chunks of kChunk elements, found by a search
 // over the tensors' first chunks.  A wave has 256 elements, one block
 // of an 8-bit state, at a time, four a lane: the block's largest magnitude is a
@@ -58,6 +58,9 @@ struct AdamwArgs {
 };
 static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
 
+// A 32-bit mix: shifts and multipliers that C. Wellons published in 2018, from a search
+// for the least bias of two multiplications.  The other odd factors spread the step
+// (2^32 over the golden ratio) and the place's high word (from A. Appleby's public-domain hash, 2011).
 __host__ __device__ inline uint32_t mix32(uint32_t x) {
   x = (x ^ (x >> 16)) * 0x7FEB352Du;
   x = (x ^ (x >> 15)) * 0x846CA68Bu;

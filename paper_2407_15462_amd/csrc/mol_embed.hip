@@ -20,12 +20,16 @@
 //     in LDS), so that every row is written once and nothing is cleared first.
 //  3. The few runs that cross spans are joined from the workspace.
 // Every sum is formed in an order that ids and sizes fix: no atomics on
-// floats, the same bits every time.  Bound by memory: grad is read once and
-// table_grad written once; a row that a million tokens share costs no more than
-// a million rows (its span sums run side by side).
+// floats, the same bits every time.  Bound by memory where rows have few tokens: grad is
+// read once and table_grad written once.
 // Measured: 262,144 tokens of 4 x 128 bf16 onto 24,186 float32 rows take 29 us
-// for the sort, 68 for the sums (4.7 TB/s) and 8 for the join, 117 a call; 65,536 of
+// for the sort, 68 for the sums (4.7 TB/s) and 8 for the join, 112 a call; 65,536 of
 // 8 x 32 onto 674,044 rows 30, 139 (5.2 TB/s, nine tenths of it zero rows) and 5.
+// Many tokens a row cost more than as many rows, in two chains of latencies: the workgroup
+// that looks for a block of zero rows reads every token of them, 256 a step, and the join
+// walks the spans of a run one by one.  262,144 tokens onto 1000 rows of 8: 338 us (34 with
+// accumulate, which has no zero rows), of 128: 73 (38); a million of 64 bf16 on a single row: 1674 (539),
+// spread over 1000 rows 387 (76), over a million 201 (194).
 // The sort's passes are chains of latencies (5 us a histogram, 9 a scatter).
 // Sorted chunks of 4096 merged by rank took 53 us against 31 at 65,536 tokens, and
 // rows cleared beside the sort slowed it by what the sums gained.  Spans that end

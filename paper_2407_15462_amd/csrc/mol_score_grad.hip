@@ -30,9 +30,11 @@
 // What bounds it: the f32 matrix rate, 12 P H + 2 P d flop a pair, and for few pairs
 // the latencies of a workgroup's one or two tiles (weights, dot products, the
 // chain and back, the sums: 50 us at P = H = 64).  Measured in float32: 32 x 129
-// pairs of 4 x 4, H = 32 13 + 6 + 5 us (pairs, products, sums), 24 a call; 200 x 4000 of
-// them 131 + 58 + 14 (pairs at 50 TFLOP/s, a large product at 144); 8 x 6112 of
-// 8 x 8, H = 64 69 + 23 + 8.
+// pairs of 4 x 4, H = 32 13 + 7 + 5 us (pairs, products, sums), 24 a call; 200 x 4000 of
+// them 121 + 54 + 15 (pairs at 54 TFLOP/s, a large product at 144); 8 x 6112 of
+// 8 x 8, H = 64 66 + 22 + 8.  In bf16: 128 x 1000 of 16 x 4, H = 64 112 + 24 + 11; 128 x 1000 of
+// 8 x 8, H = 256, whose four groups of hidden units repeat the chain, 4 x 345 + 24 + 19;
+// 1024 x 2048 of 8 x 8, H = 64 in two slabs of 698 + 111 + 19.
 #include <algorithm>
 
 #include "mol_grad.h"

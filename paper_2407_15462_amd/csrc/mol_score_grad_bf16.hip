@@ -35,13 +35,13 @@
 // whole.  dQ = sum ds X reads rows (K = items); dX = sum ds Q (K = b pq) takes them through LDS
 // and the transposing read.
 //
-// Measured, 1024 x 2048 pairs of 8 x 8, d = H = 64, in two slabs: 755 us a call,
-// 205 TFLOP/s; a slab's pairs 275 us, products 87 (6.2 TB/s of ds), sums 16.  128 x 1031
-// of 8 x 8, d = 32: 61 + 17 + 9.  The pairs are bound by issue and latency: a unit
+// Measured, 1024 x 2048 pairs of 8 x 8, d = H = 64, in two slabs: 763 us a call,
+// 203 TFLOP/s; under the profiler, a tenth slower, a slab's pairs take 283 to 312 us,
+// products 95 to 107 (5.4 TB/s of ds), sums 17 to 20.  128 x 1031 of 8 x 8, d = 32: 63 + 18 + 9.  The pairs are bound by issue and latency: a unit
 // is 914 vector, 49 transcendental, 124 matrix and 121 LDS instructions, its
 // 256 registers leave two waves a SIMD, and these issue vector instructions 40 % of
-// the time.  The general form, on f32 matrix instructions, takes 435 us for half as
-// many pairs.
+// the time.  The general form, on f32 matrix instructions, takes 698 us for a slab's
+// pairs.
 #include <algorithm>
 #include <type_traits>
 
@@ -161,7 +161,7 @@ static_assert(lds_bytes<4, 1>() >= 4 * kWaves * 16 * 16 && lds_bytes<16, 1>() >=
 // at most 32 FULL: no branches in a unit, which leaves its order to the compiler.
 // HALVES 2: 65 to 128 hidden units.  u stays in registers on the way forward, and the way
 // back takes 64 of them at a time: h and du of those to LDS, and their part of dW1 and dW2
-// (512 x 2000 pairs of 8 x 4, d = H = 128: 339 us, 831 in the general form).
+// (512 x 2000 pairs of 8 x 4, d = H = 128: 331 us; a call 410, 865 in the general form).
 template <int NPQ, int PXP, int XL, int FULL, int HALVES>
 __global__ __launch_bounds__(kThreads, 2) void k_score_grad_bf16(DevProb pr, Bf16Dims dm,
                                                                  const float* __restrict__ dphi, Bf16Parts out) {

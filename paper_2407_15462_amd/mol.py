@@ -609,6 +609,9 @@ class AdamwTensors:
     some tensors (None for the others); any may be missing or None.  Tensors
     keep their place in the stream of random numbers that rounds 8-bit states
     by their order: each starts at a multiple of 256.
+
+    Making a plan takes about 11 us a tensor on the host (24 tensors: 270 us,
+    their step 17), so that it is for tensors that stay where they are.
     """
 
     def __init__(self, p: List[torch.Tensor], g: List[torch.Tensor], m: List[torch.Tensor], v: List[torch.Tensor],
@@ -698,11 +701,13 @@ class Learner:
     queries [Vq][Pq][d] and items [Px][V][d]: the component embeddings' float32
     masters; a_q [Vq][P], a_x [V][P]: the gating logits of every query and item;
     W1 [H][P], b1 [H], W2 [P][H], b2 [P]: the gating MLP, all float32 (they are
-    updated in place).  weight_decay is for the embeddings and W1, W2.
+    updated in place).  weight_decay is for the embeddings and W1, W2.  The rows
+    are learned and served as they are: Eq. 2's L2 normalisation of the components is
+    not part of a step, so that it is a model of unnormalised dot products.
     states_8bit: AdamW states of the two embedding tables in 8 bits.  flags: the
     precision of the gating MLP in a step's scores (MOL_FLAG_*); float32 by default,
     since training moves its weights out of the range that the others are meant for
-    (1024 x 2048 pairs of 8 x 8: 430 us of a step's 1560; 0 takes 90, with weights of RMS
+    (1024 x 2048 pairs of 8 x 8: 430 us of a step's 1580; 0 takes 90, with weights of RMS
     up to 0.3, MOL_FLAG_BF16X2_GATING 130, up to 1).  grad_flags: the same for the
     gradients, whose chain has no such range; MOL_FLAG_F32_GATING keeps float32 up to
     their rounding to bf16 (see score_grad).
