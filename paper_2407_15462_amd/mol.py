@@ -264,6 +264,7 @@ def mol_embed_grad_workspace(C: int, V: int, d: int, T: int) -> int:
 
 @functools.lru_cache(maxsize=256)              # (a call of its own costs a tenth of a small loss)
 def mol_softmax_loss_workspace(B: int, N: int) -> int:
+    _sizes(B, N)
     out = ctypes.c_size_t(0)
     _check(load().mol_softmax_loss_workspace(B, N, ctypes.byref(out)))
     return out.value
@@ -716,8 +717,8 @@ class Learner:
     retrieval problem of the model as it is.
 
     To save a learner: ``master``, ``state`` (m and v, and of 8-bit states
-    m_scale and v_scale, by tensor) and ``steps``.  One made of the saved masters,
-    whose state and steps the saved ones are copied into, goes on bit for bit.
+    m_scale and v_scale, by tensor) and ``steps``.  One made of the saved masters with
+    the same options, whose state and steps the saved ones are copied into, goes on bit for bit.
     """
 
     def __init__(self, queries, items, a_q, a_x, W1, b1, W2, b2, weight_decay: float = 0.0, states_8bit: bool = False,

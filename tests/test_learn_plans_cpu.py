@@ -49,6 +49,7 @@ SIZES = [
     ("gradient of 2^32 + 5 tokens", lambda: mol.embed_grad(meta(1, (1 << 32) + 5, 4), meta((1 << 32) + 5, dtype=I32), 7)),
     ("its workspace", lambda: mol.embed_grad_workspace(meta(1, 3, 4), (1 << 32) + 5)),
     ("loss of 2^32 + 5 columns", lambda: mol.softmax_loss(meta(1, (1 << 32) + 5), meta(1, dtype=I32))),
+    ("its workspace, of 2^32 + 5 columns", lambda: mol.mol_softmax_loss_workspace(1, (1 << 32) + 5)),
     ("loss of 2^32 + 1 rows", lambda: mol.softmax_loss(meta((1 << 32) + 1, 3), meta((1 << 32) + 1, dtype=I32))),
     ("scores of 2^32 + 5 items", lambda: mol.score_grad(
         mol.Problem(meta(1, 1, 4), meta(1, (1 << 32) + 5, 4), meta(1, 1), meta((1 << 32) + 5, 1), meta(1, 1), meta(1), meta(1, 1), meta(1)),
