@@ -365,9 +365,9 @@ int mol_embed_grad(const void *grad, int32_t grad_dtype, int32_t C, int32_t V,
  * query's positive: i != t and ids[i] == ids[t].  A row whose target is
  * outside [0, N), or whose target's id is negative, has loss 0 and gradient
  * 0.  The tables' length is not known here: an id past it, an empty slot to
- * mol_embed_lookup, is made negative by the caller.  row_weight float32 [B] is the gradient of the total for loss[b] (NULL:
- * 1 each); it does not scale loss.  loss may be NULL, and dphi may be NULL
- * or phi itself.  Maximum, sum and loss are float32.  The workspace for B
+ * mol_embed_lookup, is made negative by the caller.  row_weight float32 [B] is
+ * the gradient of the total for loss[b] (NULL: 1 each); it does not scale loss.
+ * loss may be NULL, and dphi may be NULL or phi itself.  Maximum, sum and loss are float32.  The workspace for B
  * rows of N columns is enough for fewer of either. */
 int mol_softmax_loss_workspace(int32_t B, int32_t N, size_t *bytes);
 int mol_softmax_loss(int32_t B, int32_t N, const float *phi,

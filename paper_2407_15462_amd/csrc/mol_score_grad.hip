@@ -747,7 +747,7 @@ GradPlan plan_shape(const DevProb& pr, int QB) {
 size_t item_bytes(const DevProb& pr, const GradPlan& f, long B) {
   return 4ul * pr.P * (B + 1) + (f.wg_bytes + f.dm.TI - 1) / f.dm.TI;
 }
-// least chunks of a long product's split: 128 items or query vectors
+// K of a product's chunk, and the least chunks of a long product's split: 128 items or query vectors
 template <typename T>
 constexpr int kChunk = 64 / sizeof(T);
 template <typename T>
