@@ -95,6 +95,8 @@ typedef enum {
 #define MOL_MAX_C 16384   /* candidates per query handed to mol_rerank       */
 #define MOL_MAX_ROW 65536 /* elements of an embedding table's row            */
 #define MOL_MAX_TABLES 64 /* component tables per embedding call             */
+#define MOL_MAX_NORM 16384 /* elements of a row that is normalised            */
+#define MOL_MAX_TOKENS (1 << 30) /* tokens, and histories, of a gated scan    */
 
 /* One retrieval problem: shapes, storage type and device pointers (the
  * notation table of Section 2; gating parameters per Appendix A.3).
@@ -464,6 +466,107 @@ typedef struct mol_adamw {
 } mol_adamw;
 int mol_adamw_step(const mol_adamw *opt, const mol_adamw_tensor *tensors,
                    int32_t n_tensors, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Between embedding rows and scores: a query formed from a user's history,
+ * rows and components normalised, dropout in training.  Reductions, states
+ * and statistics are float32, outputs are rounded once, and all of it is
+ * deterministic.  Tensors need the alignment of their elements only. */
+
+/* Layer norm of every row of x [T][d]:
+ *   y = (x - mean) / sqrt(var + eps) * gamma + beta
+ * with the row's mean and (biased) variance, formed about the mean; gamma and
+ * beta float32 [d], NULL for 1 and 0.  eps from FLT_MIN to FLT_MAX, d up to
+ * MOL_MAX_NORM.  y may be x itself where their types are the same.  T == 0 is
+ * a no-op. */
+int mol_layer_norm(const void *x, int32_t x_dtype, int64_t T, int32_t d,
+                   const float *gamma, const float *beta, float eps, void *y,
+                   int32_t y_dtype, void *stream);
+
+/* Gradient of mol_layer_norm, with xhat = (x - mean) / sqrt(var + eps) formed
+ * again from x and w = dy gamma:
+ *   dx = (w - mean(w) - xhat mean(w xhat)) / sqrt(var + eps)
+ *   dgamma = sum over rows of dy xhat,  dbeta = sum over rows of dy
+ * dgamma and dbeta float32 [d], or both NULL (and then no workspace).  dx may
+ * be dy or x where the types are the same.  T == 0 gives zero sums.  Needs
+ * mol_layer_norm_grad_workspace bytes (256-byte aligned), which serve
+ * every call of no more rows and no more elements a row. */
+int mol_layer_norm_grad_workspace(int64_t T, int32_t d, size_t *bytes);
+int mol_layer_norm_grad(const void *dy, int32_t dy_dtype, const void *x,
+                        int32_t x_dtype, int64_t T, int32_t d,
+                        const float *gamma, float eps, void *dx,
+                        int32_t dx_dtype, float *dgamma, float *dbeta,
+                        void *ws, size_t ws_bytes, void *stream);
+
+/* L2 normalisation of every row of x [T][d], Eq. 2's of a component:
+ *   y = x / max(|x|, eps),   |x| = sqrt(sum x^2)
+ * right for every finite row, also where its squares leave float32's range.
+ * eps from FLT_MIN to 1.  A row of zeros stays one.  y may be x itself. */
+int mol_normalize(const void *x, int32_t x_dtype, int64_t T, int32_t d,
+                  float eps, void *y, int32_t y_dtype, void *stream);
+
+/* Gradient of mol_normalize:  dx = (dy - y <y, dy>) / |x|, and dy / eps for
+ * rows with |x| <= eps.  dx may be dy or x where the types are the same. */
+int mol_normalize_grad(const void *dy, int32_t dy_dtype, const void *x,
+                       int32_t x_dtype, int64_t T, int32_t d, float eps,
+                       void *dx, int32_t dx_dtype, void *stream);
+
+/* Dropout of n elements:
+ *   y_i = residual_i + (kept_i ? x_i / (1 - p) : 0)
+ * p is taken as the nearest multiple of 2^-16, t / 65536 (below 1).  The mask
+ * is never stored: element i, j = offset + i, is kept if half j mod 8 (16 bits;
+ * the low half of word 0 first) of the four words that Philox 4x32 with 10
+ * rounds gives for the counter (j / 8 in two words, step, 0) and the key seed
+ * is at least t.  So the same call on dy, without residual, is the gradient,
+ * and tensors with places of their own (offset, a multiple of 8) have masks of
+ * their own under one seed.  step_ptr: NULL, or device memory read in place of
+ * step, so that a captured graph drops other elements each time.  residual
+ * (y_dtype) may be NULL; y may be x or residual where the types are the same.
+ * A dropped element is 0 whatever x holds.  n == 0 is a no-op. */
+int mol_dropout(const void *x, int32_t x_dtype, int64_t n, double p,
+                uint64_t seed, uint64_t offset, uint32_t step,
+                const int32_t *step_ptr, const void *residual, void *y,
+                int32_t y_dtype, void *stream);
+
+/* A gated linear recurrence over B histories of packed tokens; history b's are
+ * offsets[b] .. offsets[b + 1] - 1, and for each of d channels
+ *   f_t = 1 / (1 + exp(-gate_t)),   h_t = f_t h_{t-1} + (1 - f_t) x_t
+ * from the state h0[b] (float32 [B][d]; NULL: zeros).  gate and x [T][d]
+ * (x_dtype), h [T][d] (h_dtype), last float32 [B][d] or NULL: the states behind
+ * the last tokens, h0's for histories without tokens; it may be h0 itself.
+ * offsets int32 [B + 1] on the device, not decreasing, within [0, T] (others are
+ * clamped to it), or NULL: one history of all T tokens, B = 1.  Rows in front
+ * of offsets[0] and from offsets[B] on belong to no history: their h is left
+ * as it is.  States are float32 throughout.  Needs mol_gated_scan_workspace bytes
+ * (256-byte aligned), which serve every scan and gradient of no more tokens,
+ * channels and histories.  d up to MOL_MAX_ROW, T and B up to MOL_MAX_TOKENS. */
+int mol_gated_scan_workspace(int32_t T, int32_t d, int32_t B, size_t *bytes);
+int mol_gated_scan(const void *gate, const void *x, int32_t x_dtype, int32_t T,
+                   int32_t d, const int32_t *offsets, int32_t B,
+                   const float *h0, void *h, int32_t h_dtype, float *last,
+                   void *ws, size_t ws_bytes, void *stream);
+
+/* Gradient of mol_gated_scan, from dh [T][d] (h_dtype; NULL: zeros) and dlast
+ * float32 [B][d] (NULL: zeros; not both), with D_t the gradient for h_t in all:
+ *   D_t = dh_t + f_{t+1} D_{t+1}   (at a history's last token dh_t + dlast)
+ *   dx_t = (1 - f_t) D_t,   dgate_t = f_t (1 - f_t) (h_{t-1} - x_t) D_t
+ *   dh0 = f_0 D_0                  (dlast for histories without tokens)
+ * h: as mol_gated_scan wrote it, rounded to its type.  dgate and dx x_dtype [T][d],
+ * zero in rows of no history; dh0 float32 [B][d] or NULL, and may be dlast
+ * itself.  Workspace: mol_gated_scan_workspace. */
+int mol_gated_scan_grad(const void *gate, const void *x, int32_t x_dtype,
+                        const void *h, const void *dh, int32_t h_dtype,
+                        int32_t T, int32_t d, const int32_t *offsets,
+                        int32_t B, const float *h0, const float *dlast,
+                        void *dgate, void *dx, float *dh0, void *ws,
+                        size_t ws_bytes, void *stream);
+
+/* One more token of each of B histories, as they are served: gate and x
+ * [B][d], state float32 [B][d] -> state_out (may be state itself) and, unless
+ * NULL, h [B][d] in h_dtype.  B == 0 is a no-op. */
+int mol_gated_step(const void *gate, const void *x, int32_t x_dtype, int32_t B,
+                   int32_t d, const float *state, float *state_out, void *h,
+                   int32_t h_dtype, void *stream);
 
 /* Kernel timing, a diagnostic for throughput measurements.
  * mol_timing_enable(1) makes every later call record a pair of HIP events on

@@ -1397,6 +1397,159 @@ int mol_adamw_step(const mol_adamw* opt, const mol_adamw_tensor* tensors, int32_
   return MOL_OK;
 }
 
+// ---------------------------------------------------------------------------
+// Between embedding rows and scores.
+
+static int check_norm(int64_t T, int32_t d, float eps, float eps_most) {
+  if (T < 0 || d < 1) return fail(MOL_EINVAL, "need T >= 0 and d >= 1 (T=%lld d=%d)", static_cast<long long>(T), d);
+  if (d > MOL_MAX_NORM) return fail(MOL_EUNSUPPORTED, "d = %d exceeds %d", d, MOL_MAX_NORM);
+  if (T >= 1ll << 40) return fail(MOL_EUNSUPPORTED, "T = %lld rows pass 2^40", static_cast<long long>(T));
+  if (!(eps >= FLT_MIN && eps <= eps_most)) return fail(MOL_EINVAL, "eps = %g outside [%g, %g]", eps, FLT_MIN, eps_most);
+  return MOL_OK;
+}
+
+int mol_layer_norm(const void* x, int32_t x_dtype, int64_t T, int32_t d, const float* gamma, const float* beta, float eps,
+                   void* y, int32_t y_dtype, void* stream) {
+  int rc;
+  if ((rc = check_norm(T, d, eps, FLT_MAX))) return rc;
+  if ((rc = check_dtype(x_dtype, "x_dtype")) || (rc = check_dtype(y_dtype, "y_dtype"))) return rc;
+  if (T == 0) return MOL_OK;
+  if (!x || !y) return fail(MOL_EINVAL, "x or y is NULL");
+  MOL_TRY_HIP(launch_norm(0, x, x_dtype, T, d, gamma, beta, eps, y, y_dtype, static_cast<hipStream_t>(stream)), "layer norm");
+  return MOL_OK;
+}
+
+int mol_layer_norm_grad_workspace(int64_t T, int32_t d, size_t* bytes) {
+  int rc;
+  if ((rc = check_norm(T, d, 1.f, 1.f))) return rc;
+  if (!bytes) return fail(MOL_EINVAL, "bytes is NULL");
+  *bytes = norm_grad_bytes(T, d);
+  return MOL_OK;
+}
+
+int mol_layer_norm_grad(const void* dy, int32_t dy_dtype, const void* x, int32_t x_dtype, int64_t T, int32_t d,
+                        const float* gamma, float eps, void* dx, int32_t dx_dtype, float* dgamma, float* dbeta, void* ws,
+                        size_t ws_bytes, void* stream) {
+  int rc;
+  if ((rc = check_norm(T, d, eps, FLT_MAX))) return rc;
+  if ((rc = check_dtype(dy_dtype, "dy_dtype")) || (rc = check_dtype(x_dtype, "x_dtype")) ||
+      (rc = check_dtype(dx_dtype, "dx_dtype")))
+    return rc;
+  if (!dgamma != !dbeta) return fail(MOL_EINVAL, "dgamma and dbeta go together");
+  if (T == 0 && !dgamma) return MOL_OK;
+  if (T > 0 && (!dy || !x || !dx)) return fail(MOL_EINVAL, "dy, x or dx is NULL");
+  if (dgamma && (rc = check_ws(ws, ws_bytes, norm_grad_bytes(T, d)))) return rc;
+  MOL_TRY_HIP(launch_norm_grad(0, dy, dy_dtype, x, x_dtype, T, d, gamma, eps, dx, dx_dtype, dgamma, dbeta, ws,
+                               static_cast<hipStream_t>(stream)),
+              "layer norm gradient");
+  return MOL_OK;
+}
+
+int mol_normalize(const void* x, int32_t x_dtype, int64_t T, int32_t d, float eps, void* y, int32_t y_dtype, void* stream) {
+  int rc;
+  if ((rc = check_norm(T, d, eps, 1.f))) return rc;
+  if ((rc = check_dtype(x_dtype, "x_dtype")) || (rc = check_dtype(y_dtype, "y_dtype"))) return rc;
+  if (T == 0) return MOL_OK;
+  if (!x || !y) return fail(MOL_EINVAL, "x or y is NULL");
+  MOL_TRY_HIP(launch_norm(1, x, x_dtype, T, d, nullptr, nullptr, eps, y, y_dtype, static_cast<hipStream_t>(stream)), "normalize");
+  return MOL_OK;
+}
+
+int mol_normalize_grad(const void* dy, int32_t dy_dtype, const void* x, int32_t x_dtype, int64_t T, int32_t d, float eps,
+                       void* dx, int32_t dx_dtype, void* stream) {
+  int rc;
+  if ((rc = check_norm(T, d, eps, 1.f))) return rc;
+  if ((rc = check_dtype(dy_dtype, "dy_dtype")) || (rc = check_dtype(x_dtype, "x_dtype")) ||
+      (rc = check_dtype(dx_dtype, "dx_dtype")))
+    return rc;
+  if (T == 0) return MOL_OK;
+  if (!dy || !x || !dx) return fail(MOL_EINVAL, "dy, x or dx is NULL");
+  MOL_TRY_HIP(launch_norm_grad(1, dy, dy_dtype, x, x_dtype, T, d, nullptr, eps, dx, dx_dtype, nullptr, nullptr, nullptr,
+                               static_cast<hipStream_t>(stream)),
+              "normalize gradient");
+  return MOL_OK;
+}
+
+int mol_dropout(const void* x, int32_t x_dtype, int64_t n, double p, uint64_t seed, uint64_t offset, uint32_t step,
+                const int32_t* step_ptr, const void* residual, void* y, int32_t y_dtype, void* stream) {
+  int rc;
+  if (n < 0 || n >= 1ll << 40) return fail(MOL_EINVAL, "n = %lld outside [0, 2^40)", static_cast<long long>(n));
+  if (!(p >= 0 && p < 1) || dropout_threshold(p) > 65535)
+    return fail(MOL_EINVAL, "p = %g: need 0 <= p, and p < 1 as a multiple of 2^-16", p);
+  if (offset % 8) return fail(MOL_EINVAL, "offset = %llu is not a multiple of 8", static_cast<unsigned long long>(offset));
+  if ((rc = check_dtype(x_dtype, "x_dtype")) || (rc = check_dtype(y_dtype, "y_dtype"))) return rc;
+  if (n == 0) return MOL_OK;
+  if (!x || !y) return fail(MOL_EINVAL, "x or y is NULL");
+  MOL_TRY_HIP(launch_dropout(x, x_dtype, n, dropout_threshold(p), seed, offset, step, step_ptr, residual, y, y_dtype,
+                             static_cast<hipStream_t>(stream)),
+              "dropout");
+  return MOL_OK;
+}
+
+static int check_scan(int32_t T, int32_t d, int32_t B) {
+  if (T < 0 || d < 1 || B < 1) return fail(MOL_EINVAL, "need T >= 0, d >= 1 and B >= 1 (T=%d d=%d B=%d)", T, d, B);
+  if (d > MOL_MAX_ROW) return fail(MOL_EUNSUPPORTED, "d = %d exceeds %d", d, MOL_MAX_ROW);
+  if (T > MOL_MAX_TOKENS || B > MOL_MAX_TOKENS)
+    return fail(MOL_EUNSUPPORTED, "T = %d tokens or B = %d histories exceed %d", T, B, MOL_MAX_TOKENS);
+  // (a grid holds 2^32 threads)
+  if (gated_scan_blocks(T, d) >= 1l << 23) return fail(MOL_EUNSUPPORTED, "T = %d tokens of d = %d are too many", T, d);
+  return MOL_OK;
+}
+
+int mol_gated_scan_workspace(int32_t T, int32_t d, int32_t B, size_t* bytes) {
+  int rc;
+  if ((rc = check_scan(T, d, B))) return rc;
+  if (!bytes) return fail(MOL_EINVAL, "bytes is NULL");
+  *bytes = gated_scan_bytes(T, d);
+  return MOL_OK;
+}
+
+int mol_gated_scan(const void* gate, const void* x, int32_t x_dtype, int32_t T, int32_t d, const int32_t* offsets, int32_t B,
+                   const float* h0, void* h, int32_t h_dtype, float* last, void* ws, size_t ws_bytes, void* stream) {
+  int rc;
+  if ((rc = check_scan(T, d, B))) return rc;
+  if ((rc = check_dtype(x_dtype, "x_dtype")) || (rc = check_dtype(h_dtype, "h_dtype"))) return rc;
+  if (!offsets && B != 1) return fail(MOL_EINVAL, "offsets is NULL with B = %d histories", B);
+  if (T > 0 && (!gate || !x || !h)) return fail(MOL_EINVAL, "gate, x or h is NULL");
+  if ((rc = check_ws(ws, ws_bytes, gated_scan_bytes(T, d)))) return rc;
+  if (T == 0 && !last) return MOL_OK;
+  MOL_TRY_HIP(launch_gated_scan(gate, x, x_dtype, T, d, offsets, B, h0, h, h_dtype, last, ws, static_cast<hipStream_t>(stream)),
+              "gated scan");
+  return MOL_OK;
+}
+
+int mol_gated_scan_grad(const void* gate, const void* x, int32_t x_dtype, const void* h, const void* dh, int32_t h_dtype,
+                        int32_t T, int32_t d, const int32_t* offsets, int32_t B, const float* h0, const float* dlast,
+                        void* dgate, void* dx, float* dh0, void* ws, size_t ws_bytes, void* stream) {
+  int rc;
+  if ((rc = check_scan(T, d, B))) return rc;
+  if ((rc = check_dtype(x_dtype, "x_dtype")) || (rc = check_dtype(h_dtype, "h_dtype"))) return rc;
+  if (!offsets && B != 1) return fail(MOL_EINVAL, "offsets is NULL with B = %d histories", B);
+  if (!dh && !dlast) return fail(MOL_EINVAL, "dh and dlast are both NULL");
+  if (T > 0 && (!gate || !x || !h || !dgate || !dx)) return fail(MOL_EINVAL, "gate, x, h, dgate or dx is NULL");
+  if ((rc = check_ws(ws, ws_bytes, gated_scan_bytes(T, d)))) return rc;
+  if (T == 0 && !dh0) return MOL_OK;
+  MOL_TRY_HIP(launch_gated_scan_grad(gate, x, x_dtype, h, dh, h_dtype, T, d, offsets, B, h0, dlast, dgate, dx, dh0, ws,
+                                     static_cast<hipStream_t>(stream)),
+              "gated scan gradient");
+  return MOL_OK;
+}
+
+int mol_gated_step(const void* gate, const void* x, int32_t x_dtype, int32_t B, int32_t d, const float* state,
+                   float* state_out, void* h, int32_t h_dtype, void* stream) {
+  int rc;
+  if (B < 0 || d < 1) return fail(MOL_EINVAL, "need B >= 0 and d >= 1 (B=%d d=%d)", B, d);
+  if (d > MOL_MAX_ROW) return fail(MOL_EUNSUPPORTED, "d = %d exceeds %d", d, MOL_MAX_ROW);
+  const int64_t n = static_cast<int64_t>(B) * d;
+  if (n >= 1ll << 33) return fail(MOL_EUNSUPPORTED, "B d = %lld elements pass 2^33", static_cast<long long>(n));
+  if ((rc = check_dtype(x_dtype, "x_dtype")) || (rc = check_dtype(h_dtype, "h_dtype"))) return rc;
+  if (B == 0) return MOL_OK;
+  if (!gate || !x || !state || !state_out) return fail(MOL_EINVAL, "gate, x, state or state_out is NULL");
+  MOL_TRY_HIP(launch_gated_step(gate, x, x_dtype, n, state, state_out, h, h_dtype, static_cast<hipStream_t>(stream)),
+              "gated step");
+  return MOL_OK;
+}
+
 int mol_timing_enable(int on) {
   TimingLog& t = timing_log();
   std::lock_guard<std::mutex> g(t.mu);

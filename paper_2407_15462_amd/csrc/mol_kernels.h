@@ -253,4 +253,31 @@ hipError_t launch_score_grad(const DevProb& pr, const float* dphi, const mol_sco
 // AdamW over many tensors (mol_adamw.hip); arguments checked
 hipError_t launch_adamw(const mol_adamw& opt, const mol_adamw_tensor* tensors, int n_tensors, hipStream_t st);
 
+// Layer norm and L2 normalisation (length) of rows, and their gradients (mol_rows.hip); dgamma, dbeta: NULL or both;
+// ws: norm_grad_bytes, where they are wanted
+hipError_t launch_norm(int length, const void* x, int x_dtype, long T, int d, const float* gamma, const float* beta, float eps,
+                       void* y, int y_dtype, hipStream_t st);
+size_t norm_grad_bytes(long T, int d);
+hipError_t launch_norm_grad(int length, const void* dy, int dy_dtype, const void* x, int x_dtype, long T, int d,
+                            const float* gamma, float eps, void* dx, int dx_dtype, float* dgamma, float* dbeta, void* ws,
+                            hipStream_t st);
+
+// Dropout (mol_dropout.hip); threshold: of 65,536 chances those that drop an element
+uint32_t dropout_threshold(double p);
+hipError_t launch_dropout(const void* x, int x_dtype, int64_t n, uint32_t threshold, uint64_t seed, uint64_t offset,
+                          uint32_t step, const int32_t* step_ptr, const void* residual, void* y, int y_dtype,
+                          hipStream_t st);
+
+// The gated recurrence over histories, its gradient and one token of it (mol_scan.hip); ws: gated_scan_bytes;
+// blocks: the most workgroups of a launch
+size_t gated_scan_bytes(int T, int d);
+long gated_scan_blocks(int T, int d);
+hipError_t launch_gated_scan(const void* gate, const void* x, int x_dtype, int T, int d, const int32_t* offsets, int B,
+                             const float* h0, void* h, int h_dtype, float* last, void* ws, hipStream_t st);
+hipError_t launch_gated_scan_grad(const void* gate, const void* x, int x_dtype, const void* h, const void* dh, int h_dtype,
+                                  int T, int d, const int32_t* offsets, int B, const float* h0, const float* dlast,
+                                  void* dgate, void* dx, float* dh0, void* ws, hipStream_t st);
+hipError_t launch_gated_step(const void* gate, const void* x, int x_dtype, int64_t n, const float* state, float* state_out,
+                             void* h, int h_dtype, hipStream_t st);
+
 }  // namespace mol

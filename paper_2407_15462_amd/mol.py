@@ -34,6 +34,8 @@ EXPORTS = ("mol_workspace_size", "mol_score", "mol_topk_exact", "mol_topk_exact_
            "mol_rerank", "mol_avg_embed", "mol_gap_bound", "mol_gap_bound_combined",
            "mol_embed_lookup", "mol_embed_grad_workspace", "mol_embed_grad",
            "mol_softmax_loss_workspace", "mol_softmax_loss", "mol_score_grad", "mol_adamw_step",
+           "mol_layer_norm", "mol_layer_norm_grad_workspace", "mol_layer_norm_grad", "mol_normalize", "mol_normalize_grad",
+           "mol_dropout", "mol_gated_scan_workspace", "mol_gated_scan", "mol_gated_scan_grad", "mol_gated_step",
            "mol_timing_enable", "mol_timing_read",
            "mol_status_str", "mol_last_error")
 
@@ -90,6 +92,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib = ctypes.CDLL(path)
     P = ctypes.POINTER(MolProblemC)
     vp, i32, sz, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float
+    i64, u64 = ctypes.c_int64, ctypes.c_uint64
     sig = {
         "mol_workspace_size": [P, ctypes.c_int, i32, i32, i32, ctypes.POINTER(sz)],
         "mol_score": [P, i32, i32, vp, vp],
@@ -110,6 +113,16 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "mol_softmax_loss": [i32, i32, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp],
         "mol_score_grad": [P, vp, ctypes.POINTER(MolScoreGradsC), vp, sz, vp],
         "mol_adamw_step": [ctypes.POINTER(MolAdamwC), vp, i32, vp],
+        "mol_layer_norm": [vp, i32, i64, i32, vp, vp, f32, vp, i32, vp],
+        "mol_layer_norm_grad_workspace": [i64, i32, ctypes.POINTER(sz)],
+        "mol_layer_norm_grad": [vp, i32, vp, i32, i64, i32, vp, f32, vp, i32, vp, vp, vp, sz, vp],
+        "mol_normalize": [vp, i32, i64, i32, f32, vp, i32, vp],
+        "mol_normalize_grad": [vp, i32, vp, i32, i64, i32, f32, vp, i32, vp],
+        "mol_dropout": [vp, i32, i64, ctypes.c_double, u64, u64, ctypes.c_uint32, vp, vp, vp, i32, vp],
+        "mol_gated_scan_workspace": [i32, i32, i32, ctypes.POINTER(sz)],
+        "mol_gated_scan": [vp, vp, i32, i32, i32, vp, i32, vp, vp, i32, vp, vp, sz, vp],
+        "mol_gated_scan_grad": [vp, vp, i32, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp],
+        "mol_gated_step": [vp, vp, i32, i32, i32, vp, vp, vp, i32, vp],
         "mol_timing_enable": [ctypes.c_int],
         "mol_timing_read": [ctypes.c_int, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)],
     }
@@ -275,6 +288,22 @@ def mol_softmax_loss(phi, target, ids, inv_temp: float, row_weight, loss, dphi, 
     _sizes(B, N)
     _check(load().mol_softmax_loss(B, N, _ptr(phi), _ptr(target), _ptr(ids), inv_temp, _ptr(row_weight), _ptr(loss),
                                    _ptr(dphi), _ptr(ws), ws.numel() if ws is not None else 0, _stream(stream)))
+
+
+@functools.lru_cache(maxsize=256)
+def mol_layer_norm_grad_workspace(T: int, d: int) -> int:
+    _sizes(d)
+    out = ctypes.c_size_t(0)
+    _check(load().mol_layer_norm_grad_workspace(T, d, ctypes.byref(out)))
+    return out.value
+
+
+@functools.lru_cache(maxsize=256)
+def mol_gated_scan_workspace(T: int, d: int, B: int) -> int:
+    _sizes(T, d, B)
+    out = ctypes.c_size_t(0)
+    _check(load().mol_gated_scan_workspace(T, d, B, ctypes.byref(out)))
+    return out.value
 
 
 def mol_adamw_step(opt: MolAdamwC, tensors, n_tensors: int, stream=None) -> None:
@@ -692,6 +721,221 @@ def adamw_step(tensors: AdamwTensors, lr=1e-3, beta1: float = 0.9, beta2: float 
                     _ptr(lr) if on_lr else None, _ptr(step) if on_step else None)
     with _on(tensors.device, stream):
         mol_adamw_step(opt, tensors.c, tensors.n, stream)
+
+
+# --------------------------------------------- between embedding rows and scores
+def _row_tensor(x: torch.Tensor, name: str) -> Tuple[int, int]:
+    """(rows, elements of a row) of a float tensor [..., d]."""
+    _need(isinstance(x, torch.Tensor) and x.dim() >= 1 and x.shape[-1] > 0, f"{name} must be a tensor [..., d]")
+    _operand(x, name, None, _FLOATS, x.device)
+    d = x.shape[-1]
+    _sizes(d)
+    return x.numel() // d, d
+
+
+def _output(out: Optional[torch.Tensor], like: torch.Tensor, dtype, name: str = "out", shape=None) -> torch.Tensor:
+    """The caller's tensor, or a new one of ``dtype`` (like's by default)."""
+    shape = like.shape if shape is None else shape
+    if out is None:
+        dtype = like.dtype if dtype is None else dtype
+        if dtype not in _FLOATS:
+            raise ValueError(f"unsupported output dtype {dtype}")
+        return like.new_empty(shape, dtype=dtype)
+    _operand(out, name, shape, _FLOATS if dtype is None else (dtype,), like.device)
+    return out
+
+
+def _at(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: float = 1e-5,
+               dtype=None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Layer norm of the rows of x [..., d]: (x - mean) / sqrt(var + eps) gamma + beta, in ``dtype`` (x's by default).
+
+    gamma, beta: float32 [d] (1 and 0 by default).  out may be x."""
+    T, d = _row_tensor(x, "x")
+    dev = x.device
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        if t is not None:
+            _operand(t, name, (d,), _F32, dev)
+    with _on(dev, stream):
+        out = _output(out, x, dtype)
+        _check(load().mol_layer_norm(x.data_ptr(), _DTYPES[x.dtype], T, d, _at(gamma), _at(beta), eps, out.data_ptr(),
+                                     _DTYPES[out.dtype], _stream(stream)))
+    return out
+
+
+def layer_norm_grad_workspace(x: torch.Tensor) -> torch.Tensor:
+    """The workspace of layer_norm_grad for rows x [..., d]."""
+    d = x.shape[-1]
+    return torch.empty(max(mol_layer_norm_grad_workspace(x.numel() // d, d), 1), dtype=torch.uint8, device=x.device)
+
+
+def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, eps: float = 1e-5, dtype=None,
+                    weights: bool = True, out: Optional[torch.Tensor] = None, ws=None, stream=None):
+    """Gradient of layer_norm, given dy [..., d] and the x that went in: (dx, dgamma, dbeta).
+
+    dx in ``dtype`` (x's by default), and into ``out`` if given (which may be dy or x); dgamma and dbeta float32 [d],
+    or None without ``weights``."""
+    T, d = _row_tensor(x, "x")
+    dev = x.device
+    _operand(dy, "dy", x.shape, _FLOATS, dev)
+    if gamma is not None:
+        _operand(gamma, "gamma", (d,), _F32, dev)
+    with _on(dev, stream):
+        out = _output(out, x, dtype)
+        dgamma = dbeta = None
+        if weights:
+            ws = _workspace(lambda: mol_layer_norm_grad_workspace(T, d), ws, dev)
+            dgamma, dbeta = x.new_empty((2, d), dtype=torch.float32).unbind(0)
+        _check(load().mol_layer_norm_grad(
+            dy.data_ptr(), _DTYPES[dy.dtype], x.data_ptr(), _DTYPES[x.dtype], T, d, _at(gamma), eps, out.data_ptr(),
+            _DTYPES[out.dtype], _at(dgamma), _at(dbeta), _at(ws) if weights else None,
+            ws.numel() if weights and ws is not None else 0, _stream(stream)))
+    return out, dgamma, dbeta
+
+
+def normalize(x: torch.Tensor, eps: float = 1e-12, dtype=None, out: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
+    """The rows of x [..., d] to length one (Eq. 2's components): x / max(|x|, eps), in ``dtype`` (x's by default).
+    out may be x."""
+    T, d = _row_tensor(x, "x")
+    with _on(x.device, stream):
+        out = _output(out, x, dtype)
+        _check(load().mol_normalize(x.data_ptr(), _DTYPES[x.dtype], T, d, eps, out.data_ptr(), _DTYPES[out.dtype],
+                                    _stream(stream)))
+    return out
+
+
+def normalize_grad(dy: torch.Tensor, x: torch.Tensor, eps: float = 1e-12, dtype=None, out: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """Gradient of normalize, given dy [..., d] and the x that went in, in ``dtype`` (x's by default).  out may be dy or x."""
+    T, d = _row_tensor(x, "x")
+    _operand(dy, "dy", x.shape, _FLOATS, x.device)
+    with _on(x.device, stream):
+        out = _output(out, x, dtype)
+        _check(load().mol_normalize_grad(dy.data_ptr(), _DTYPES[dy.dtype], x.data_ptr(), _DTYPES[x.dtype], T, d, eps,
+                                         out.data_ptr(), _DTYPES[out.dtype], _stream(stream)))
+    return out
+
+
+def dropout(x: torch.Tensor, p: float, seed: int, step=0, offset: int = 0, residual: Optional[torch.Tensor] = None,
+            dtype=None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Dropout: residual + x / (1 - p) where an element is kept, in ``dtype`` (residual's, else x's, by default).
+
+    p is taken as the nearest multiple of 2^-16.  The mask comes from (seed, step, offset + the element's index) and is
+    not stored: the gradient for x is the same call on dy, without residual.  step: a number in [0, 2^32), or one
+    int32 on the GPU that the kernel reads, for graphs that are replayed.  offset: a multiple of 8; tensors of one
+    step that are to have masks of their own need ranges of their own.  out may be x or residual."""
+    _need(isinstance(x, torch.Tensor), "x must be a tensor")
+    dev = x.device
+    _operand(x, "x", None, _FLOATS, dev)
+    if residual is not None:
+        _operand(residual, "residual", x.shape, _FLOATS, dev)
+    on_step = isinstance(step, torch.Tensor)
+    if on_step:
+        _need(step.numel() == 1, "step must have one element")
+        _operand(step, "step", step.shape, _INT32, dev)
+    elif not 0 <= step < 1 << 32:
+        raise ValueError(f"step = {step} outside [0, 2^32)")
+    if not 0 <= offset < 1 << 63:
+        raise ValueError(f"offset = {offset} outside [0, 2^63)")
+    with _on(dev, stream):
+        out = _output(out, x, residual.dtype if out is None and dtype is None and residual is not None else dtype)
+        _need(residual is None or residual.dtype == out.dtype, "residual must have the output's dtype")
+        _check(load().mol_dropout(x.data_ptr(), _DTYPES[x.dtype], x.numel(), p, seed & 0xFFFFFFFFFFFFFFFF, offset,
+                                  0 if on_step else step, step.data_ptr() if on_step else None, _at(residual),
+                                  out.data_ptr(), _DTYPES[out.dtype], _stream(stream)))
+    return out
+
+
+def gated_scan_workspace(x: torch.Tensor, B: int) -> torch.Tensor:
+    """The workspace of gated_scan and gated_scan_grad for tokens x [T][d] of B histories."""
+    T, d = x.shape
+    return torch.empty(max(mol_gated_scan_workspace(T, d, B), 1), dtype=torch.uint8, device=x.device)
+
+
+def _histories(gate, x, offsets, h0):
+    """(T, d, B) of a scan's operands."""
+    _need(isinstance(x, torch.Tensor) and x.dim() == 2, "x must be a tensor [T][d]")
+    dev, (T, d) = x.device, x.shape
+    _operand(x, "x", None, _FLOATS, dev)
+    _operand(gate, "gate", x.shape, (x.dtype,), dev)
+    B = 1
+    if offsets is not None:
+        _need(isinstance(offsets, torch.Tensor) and offsets.dim() == 1 and offsets.numel() > 1, "offsets must be a tensor [B + 1]")
+        _operand(offsets, "offsets", None, _INT32, dev)
+        B = offsets.numel() - 1
+    if h0 is not None:
+        _operand(h0, "h0", (B, d), _F32, dev)
+    _sizes(T, d, B)
+    return T, d, B
+
+
+def gated_scan(gate: torch.Tensor, x: torch.Tensor, offsets: Optional[torch.Tensor] = None,
+               h0: Optional[torch.Tensor] = None, dtype=None, out: Optional[torch.Tensor] = None,
+               last: Optional[torch.Tensor] = None, ws=None, stream=None):
+    """h_t = f_t h_{t-1} + (1 - f_t) x_t, f = sigmoid(gate), over the tokens of every history: (h [T][d], last [B][d]).
+
+    gate, x: [T][d] packed tokens; offsets: int32 [B + 1], history b's tokens are offsets[b] .. offsets[b + 1] - 1
+    (None: one history of all tokens); h0: float32 [B][d], the states before them (zeros by default).  h in ``dtype``
+    (x's by default), last in float32, and may be written to ``out`` and ``last``; last may be h0.  Rows of no history
+    are not written in h."""
+    T, d, B = _histories(gate, x, offsets, h0)
+    dev = x.device
+    with _on(dev, stream):
+        ws = _workspace(lambda: mol_gated_scan_workspace(T, d, B), ws, dev)
+        out = _output(out, x, dtype)
+        last = _output(last, x, torch.float32, "last", (B, d))
+        _check(load().mol_gated_scan(gate.data_ptr(), x.data_ptr(), _DTYPES[x.dtype], T, d, _at(offsets), B, _at(h0),
+                                     out.data_ptr(), _DTYPES[out.dtype], last.data_ptr(), _at(ws),
+                                     0 if ws is None else ws.numel(), _stream(stream)))
+    return out, last
+
+
+def gated_scan_grad(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor, dh: Optional[torch.Tensor] = None,
+                    offsets: Optional[torch.Tensor] = None, h0: Optional[torch.Tensor] = None,
+                    dlast: Optional[torch.Tensor] = None, ws=None, stream=None):
+    """Gradient of gated_scan, given its output h and the gradients dh [T][d] for h (of h's type) and dlast float32
+    [B][d] for last (either may be None): (dgate, dx, dh0), of x's type and float32; dh0 is None without h0.
+    Rows of no history have gradients of zero."""
+    T, d, B = _histories(gate, x, offsets, h0)
+    dev = x.device
+    _operand(h, "h", x.shape, _FLOATS, dev)
+    if dh is not None:
+        _operand(dh, "dh", x.shape, (h.dtype,), dev)
+    if dlast is not None:
+        _operand(dlast, "dlast", (B, d), _F32, dev)
+    with _on(dev, stream):
+        ws = _workspace(lambda: mol_gated_scan_workspace(T, d, B), ws, dev)
+        dgate, dx = torch.empty_like(x), torch.empty_like(x)
+        dh0 = None if h0 is None else torch.empty_like(h0)
+        _check(load().mol_gated_scan_grad(
+            gate.data_ptr(), x.data_ptr(), _DTYPES[x.dtype], h.data_ptr(), _at(dh), _DTYPES[h.dtype], T, d, _at(offsets), B,
+            _at(h0), _at(dlast), dgate.data_ptr(), dx.data_ptr(), _at(dh0), _at(ws), 0 if ws is None else ws.numel(),
+            _stream(stream)))
+    return dgate, dx, dh0
+
+
+def gated_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, new: Optional[torch.Tensor] = None, dtype=None,
+               out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """One more token of every history: gate, x [B][d] and the states float32 [B][d], which are updated in place (or
+    written to ``new``).  Returns the new states in ``dtype`` (x's by default)."""
+    _need(isinstance(x, torch.Tensor) and x.dim() == 2, "x must be a tensor [B][d]")
+    dev, (B, d) = x.device, x.shape
+    _operand(x, "x", None, _FLOATS, dev)
+    _operand(gate, "gate", x.shape, (x.dtype,), dev)
+    _operand(state, "state", x.shape, _F32, dev)
+    if new is not None:
+        _operand(new, "new", x.shape, _F32, dev)
+    _sizes(B, d)
+    with _on(dev, stream):
+        out = _output(out, x, dtype)
+        _check(load().mol_gated_step(gate.data_ptr(), x.data_ptr(), _DTYPES[x.dtype], B, d, state.data_ptr(),
+                                     (state if new is None else new).data_ptr(), out.data_ptr(), _DTYPES[out.dtype],
+                                     _stream(stream)))
+    return out
 
 
 class Learner:
