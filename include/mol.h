@@ -533,7 +533,7 @@ int mol_dropout(const void *x, int32_t x_dtype, int64_t n, double p,
  *   f_t = 1 / (1 + exp(-gate_t)),   h_t = f_t h_{t-1} + (1 - f_t) x_t
  * from the state h0[b] (float32 [B][d]; NULL: zeros).  gate and x [T][d]
  * (x_dtype), h [T][d] (h_dtype), last float32 [B][d] or NULL: the states behind
- * the last tokens, h0's for histories without tokens; it may be h0 itself.
+ * the last tokens, h0's for histories without tokens; it is not h0 itself.
  * offsets int32 [B + 1] on the device, not decreasing, within [0, T] (others are
  * clamped to it), or NULL: one history of all T tokens, B = 1.  Rows in front
  * of offsets[0] and from offsets[B] on belong to no history: their h is left
@@ -552,7 +552,7 @@ int mol_gated_scan(const void *gate, const void *x, int32_t x_dtype, int32_t T,
  *   dx_t = (1 - f_t) D_t,   dgate_t = f_t (1 - f_t) (h_{t-1} - x_t) D_t
  *   dh0 = f_0 D_0                  (dlast for histories without tokens)
  * h: as mol_gated_scan wrote it, rounded to its type.  dgate and dx x_dtype [T][d],
- * zero in rows of no history; dh0 float32 [B][d] or NULL, and may be dlast
+ * zero in rows of no history; dh0 float32 [B][d] or NULL, and not dlast
  * itself.  Workspace: mol_gated_scan_workspace. */
 int mol_gated_scan_grad(const void *gate, const void *x, int32_t x_dtype,
                         const void *h, const void *dh, int32_t h_dtype,

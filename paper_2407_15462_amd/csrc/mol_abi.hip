@@ -1511,6 +1511,7 @@ int mol_gated_scan(const void* gate, const void* x, int32_t x_dtype, int32_t T, 
   if ((rc = check_dtype(x_dtype, "x_dtype")) || (rc = check_dtype(h_dtype, "h_dtype"))) return rc;
   if (!offsets && B != 1) return fail(MOL_EINVAL, "offsets is NULL with B = %d histories", B);
   if (T > 0 && (!gate || !x || !h)) return fail(MOL_EINVAL, "gate, x or h is NULL");
+  if (last && last == h0) return fail(MOL_EINVAL, "last and h0 are the same buffer");
   if ((rc = check_ws(ws, ws_bytes, gated_scan_bytes(T, d)))) return rc;
   if (T == 0 && !last) return MOL_OK;
   MOL_TRY_HIP(launch_gated_scan(gate, x, x_dtype, T, d, offsets, B, h0, h, h_dtype, last, ws, static_cast<hipStream_t>(stream)),
@@ -1527,6 +1528,7 @@ int mol_gated_scan_grad(const void* gate, const void* x, int32_t x_dtype, const 
   if (!offsets && B != 1) return fail(MOL_EINVAL, "offsets is NULL with B = %d histories", B);
   if (!dh && !dlast) return fail(MOL_EINVAL, "dh and dlast are both NULL");
   if (T > 0 && (!gate || !x || !h || !dgate || !dx)) return fail(MOL_EINVAL, "gate, x, h, dgate or dx is NULL");
+  if (dh0 && dh0 == dlast) return fail(MOL_EINVAL, "dh0 and dlast are the same buffer");
   if ((rc = check_ws(ws, ws_bytes, gated_scan_bytes(T, d)))) return rc;
   if (T == 0 && !dh0) return MOL_OK;
   MOL_TRY_HIP(launch_gated_scan_grad(gate, x, x_dtype, h, dh, h_dtype, T, d, offsets, B, h0, dlast, dgate, dx, dh0, ws,

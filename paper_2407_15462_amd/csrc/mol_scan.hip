@@ -7,23 +7,33 @@
 // Both are linear maps of the state that comes in, state -> A state + H, which join:
 // the scan cuts the packed tokens, wherever histories end, into chunks of equal length,
 // each read once.  A workgroup holds a chunk of 128 channels (two a lane): each
-// wave, or part of a wave where there are few channels, takes a slice of S tokens
-// and runs through it from state 0, keeping every token's A and H; slices are
-// joined in LDS; the workgroup publishes the chunk's (A, H), gets the state that comes
-// in from the chunks before, and writes h = A state + H.  A history's first
-// token starts from h0 with A = 0, so that nothing crosses from one history to the next.
+// wave, or part of a wave where there are few channels, takes a slice of S tokens and
+// runs through it from state 0, for its (A, H); slices are joined in LDS; the
+// workgroup publishes the chunk's (A, H), gets the state that comes in from the
+// chunks before, and runs through the tokens once more, which it kept in registers, for
+// what it writes.  A history's first token starts from h0 with A = 0, so that nothing
+// crosses from one history to the next.
 //
-// The state that comes in is formed in an order that the sizes and offsets fix: the
-// state at the end of the group of kGroup chunks before (published by the
-// group's last chunk), then the (A, H) of the chunks since, in order; both only from the chunk in
-// which the history starts.  So a long history is a chain of one wait a group, and
-// short ones are none at all.
+// The state that comes in is formed in an order that sizes and offsets alone fix: the
+// state at the end of the kSuper chunks before (a chain of waits along a long history),
+// then the (A, H) of the groups of kGroup chunks since, then those of the
+// group's chunks; each only from the chunk in which the history starts, so that short
+// histories wait for little.
 //
 // Waiting is sure to end: workgroups take their chunks by a ticket, in order, so that
-// a chunk's predecessors belong to workgroups that run or have ended, and each
-// publishes its (A, H) before it waits for anything.  A published pair is one
+// a chunk's predecessors belong to workgroups that run or have ended, and what each
+// publishes needs nothing but what those before it publish.  A published pair is one
 // 64-bit word, whose top bit (the sign of A, which is not negative) says that it is there.
+//
+// Measured, bf16: 1024 histories of 262,144 tokens of 512 channels 219 us (3.7 TB/s; 184 to 202
+// without the waits), back 319 (5.0 TB/s, what a copy of as much reaches); one history of
+// 131,072 x 1024 230.  What bounds it: back, memory; forward, the waits and, at more than half
+// of the vector rate, two gates an element (27 instructions).  Tried and slower forward: every token's A and H kept
+// in place of the second run (half as many tokens a slice: 225 to 231 us), workgroups that stay and load their
+// next chunk ahead (226 to 311: a wait is then for workgroups at another place of their turn), a ninth wave for
+// the waits, tickets of their own for every 128 channels (238: neighbours in memory drift apart in time).
 #include <algorithm>
+#include <type_traits>
 
 #include "mol_kernels.h"
 #include "mol_vec.h"
@@ -35,8 +45,9 @@ namespace {
 using vec::Raw;
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
-constexpr int kGroup = 32;                // chunks of a group
-constexpr int kSlots = kGroup / kWaves;   // whose pairs a wave reads
+constexpr int kGroup = 8, kSuper = 64;    // chunks
+static_assert(kGroup - 1 < kWaves && kSuper / kGroup - 1 < kWaves, "a wave waits for one pair of each kind");
+
 constexpr float kLog2E = 1.4426950408889634f, kLog2ELo = 1.925963033500e-8f, kLn2 = 0.6931471805599453f;
 
 struct ScanArgs {
@@ -55,11 +66,13 @@ struct ScanArgs {
   void* dgate;
   void* dx;
   float* dh0;
-  uint32_t* ticket;        // workspace
+  uint32_t* ticket;        // workspace (of more than one chunk)
   int2* plan;              // of each chunk: the first history that it holds tokens of, and the chunk
                            // that the state coming in starts from (the chunk itself: none comes in)
-  uint64_t* pairs;         // [chunks][d]
-  uint64_t* states;        // [chunks / kGroup][d]
+  uint64_t* pairs;         // [chunks][d] (A, H)
+  uint64_t* group_pairs;   // [chunks / kGroup][d]
+  uint64_t* states;        // [chunks / kSuper][d] (0, state)
+  long words;              // of the three together
 };
 
 __device__ __forceinline__ int offset_at(const ScanArgs& a, int i) {
@@ -67,16 +80,22 @@ __device__ __forceinline__ int offset_at(const ScanArgs& a, int i) {
   return min(max(a.offsets[i], 0), a.T);
 }
 
-struct Gate {
-  float f, rest;           // sigmoid(gate), sigmoid(-gate)
-};
-__device__ __forceinline__ Gate gate_of(float g) {
-  const float n = -fabsf(g), t = n * kLog2E;
-  const float r = fmaf(n, kLog2ELo, fmaf(n, kLog2E, -t));
-  const float e0 = __builtin_amdgcn_exp2f(t);
-  const float e = e0 == 0.f ? 0.f : fmaf(e0, r * kLn2, e0);    // e^{-|g|}
-  const float s = __builtin_amdgcn_rcpf(1.f + e), q = e * s;
-  return g >= 0.f ? Gate{s, q} : Gate{q, s};
+// f = sigmoid(g) and rest = sigmoid(-g), which 1 - f would not give near f = 1; far out
+// e^{-g} stays finite (f is 2^-126 there), and NaN stays NaN
+template <typename T>
+__device__ __forceinline__ void gates_of(float g, float& f, float& rest) {
+  float e;
+  if (sizeof(T) == 2) {
+    // (the product's rounding makes e off by a relative |g| 2^-24, where the gate itself is known to 2^-9 |g|)
+    e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(g * -kLog2E, 126.f));
+  } else {
+    g = __builtin_elementwise_minimum(__builtin_elementwise_maximum(g, -87.f), 120.f);
+    const float t = g * -kLog2E, r = fmaf(g, -kLog2ELo, fmaf(g, -kLog2E, -t));
+    e = __builtin_amdgcn_exp2f(t);
+    e = fmaf(e, r * kLn2, e);
+  }
+  f = __builtin_amdgcn_rcpf(1.f + e);
+  rest = e * f;
 }
 
 // a v, and 0 for a = 0 whatever v is (another history's state)
@@ -128,8 +147,7 @@ __global__ __launch_bounds__(256) void k_scan_plan(ScanArgs a, int chunk_len) {
   const long tid = static_cast<long>(blockIdx.x) * 256 + threadIdx.x, all = static_cast<long>(gridDim.x) * 256;
   const int lane = threadIdx.x & 63;
   if (a.ticket && tid == 0) *a.ticket = 0;
-  const long words = (static_cast<long>(a.chunks) + a.chunks / kGroup) * a.d;      // (states lie behind pairs)
-  for (long i = tid; i < words; i += all) a.pairs[i] = 0;
+  for (long i = tid; i < a.words; i += all) a.pairs[i] = 0;
   for (long c = tid / 64; c < a.chunks; c += all / 64) {
     int first, from = static_cast<int>(c);
     if (!BACK) {
@@ -169,39 +187,74 @@ __global__ __launch_bounds__(256) void k_scan_plan(ScanArgs a, int chunk_len) {
 // without channels of their own can read others'.
 template <bool BACK, typename T, typename TH, int S, bool UNI, bool EVEN>
 __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
-  constexpr int kMost = UNI ? kWaves * S : kWaves * S * 16;    // tokens of a chunk (4 lanes a row at least)
-  constexpr int kBlock = S < 8 ? S : 8;                        // tokens whose loads are in flight together on the way out
-  __shared__ uint32_t flags[kMost / S];                        // of a slice: the tokens at which a history begins, those at which
-                                                               // it ends << 16 (in the scan's direction)
-  __shared__ int begin_b[kMost], end_b[kMost];                 // whose
-  __shared__ float sum_a[kWaves][128], sum_h[kWaves][128];     // [wave][channel]
-  __shared__ float in_a[kWaves][128], in_h[kWaves][128], in_s[128];
+  constexpr int kMost = kWaves * S * (UNI ? 1 : 16);            // tokens of a chunk (4 lanes a row at least)
+  constexpr int kBlock = BACK ? 8 : S;                         // tokens whose x and h are in flight together on the way out
+  __shared__ uint32_t begins[kMost / S], ends[kMost / S];      // of a slice: the tokens at which a history begins and ends
+  __shared__ int begin_b[kMost], end_b[kMost];                 // (in the scan's direction), and whose
+  __shared__ float sum_a[kWaves][128], sum_h[kWaves][128];       // [wave][channel]: of the unit's slices
+  __shared__ float in_a[kWaves][128], in_h[kWaves][128], come[128];
   __shared__ int my_ticket;
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64), d = a.d;
   const int lanes = UNI ? 64 : 1 << a.lanes_log2, per_wave = UNI ? 1 : 64 >> a.lanes_log2;
-  const int sub = UNI ? 0 : lane >> a.lanes_log2;              // which slice of the wave's
-  const int slice = wave * per_wave + sub, slices = kWaves * per_wave, len = slices * S;
-  int unit = blockIdx.x;
+  const int len = kWaves * per_wave * S;
+  int ticket = blockIdx.x;
   if (a.chunks > 1) {
     if (tid == 0) my_ticket = __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    unit = __builtin_amdgcn_readfirstlane(my_ticket);
+    ticket = __builtin_amdgcn_readfirstlane(my_ticket);
   }
-  const int chunk = unit / a.groups, cg = unit - chunk * a.groups, d = a.d;
-  const int row_lane = UNI ? lane : lane & (lanes - 1);
-  const int ch = cg * 128 + 2 * row_lane, nch = d - ch;        // this lane's channels: 2 or 1 (or none)
-  const uint32_t from_ch = EVEN ? min(ch, d - 2) : min(ch, d - 1);
-
-  // tokens in the scan's direction: i = 0 .. len - 1 of the chunk stands for token
-  // first + i, or first - i on the way back
+  const int chunk = __builtin_amdgcn_readfirstlane(ticket / a.groups), cg = ticket - chunk * a.groups;
+  // tokens in the scan's direction: i = 0 .. len - 1 stands for token first + i, or first - i on the way back
   const int first = BACK ? a.T - 1 - chunk * len : chunk * len;
   const int lo = BACK ? max(0, first + 1 - len) : first;
   const int hi = BACK ? first + 1 : min(a.T, first + len);
+
+  const int sub = UNI ? 0 : lane >> a.lanes_log2;              // which slice of the wave's
+  const int slice = wave * per_wave + sub;
+  const int row_lane = UNI ? lane : lane & (lanes - 1);
+  Raw<T, 2> gate[S];
+  Raw<T, 2> xr[BACK ? 1 : S];
+  Raw<TH, 2> dr[BACK ? S : 1];
+  auto row_at = [&](auto* base, int row, uint32_t from_ch) {   // a lane's channels of a row
+    typedef std::remove_reference_t<decltype(*base)> E;
+    typedef std::conditional_t<std::is_const_v<E>, const char, char> Byte;
+    return reinterpret_cast<E*>(reinterpret_cast<Byte*>(base + static_cast<int64_t>(row) * d) +
+                                from_ch * static_cast<uint32_t>(sizeof(E)));
+  };
+  auto load = [&](auto& r, const auto* base, int t, uint32_t from_ch) {
+    if (EVEN)
+      r.load(row_at(base, t, from_ch));
+    else
+      r.load(row_at(base, t, from_ch), d - static_cast<int>(from_ch));
+  };
+  const int t_first = BACK ? first - slice * S : first + slice * S;
+  auto token = [&](int s) { return BACK ? t_first - s : t_first + s; };
+  auto from_of = [&](int cg) { return static_cast<uint32_t>(min(cg * 128 + 2 * row_lane, EVEN ? d - 2 : d - 1)); };
+  // Rows that are no history's are read as well (and past the tensor's ends others
+  // in their place): what comes of them is not written, and the next history begins anew.
+  auto fetch = [&](int cg) {
+    const uint32_t from_ch = from_of(cg);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const int t = min(max(token(s), 0), a.T - 1);
+      load(gate[s], static_cast<const T*>(a.gate), t, from_ch);
+      if constexpr (BACK) {
+        if (a.dh) load(dr[s], static_cast<const TH*>(a.dh), t, from_ch);
+      } else {
+        load(xr[s], static_cast<const T*>(a.x), t, from_ch);
+      }
+    }
+  };
+  if constexpr (BACK)
+#pragma unroll
+    for (int s = 0; s < S; ++s) dr[s].zero();
+
+  fetch(cg);
   const int live_lo = __builtin_amdgcn_readfirstlane(max(lo, offset_at(a, 0)));
   const int live_hi = __builtin_amdgcn_readfirstlane(min(hi, offset_at(a, a.B)));
-
-  for (int i = tid; i < slices; i += kThreads) flags[i] = 0;
+  auto live = [&](int s) { return token(s) >= live_lo && token(s) < live_hi; };
+  for (int i = tid; i < kWaves * per_wave; i += kThreads) begins[i] = ends[i] = 0;
   __syncthreads();
   int2 plan = a.chunks > 1 ? a.plan[chunk] : make_int2(0, 0);
   plan.x = __builtin_amdgcn_readfirstlane(plan.x);
@@ -222,262 +275,254 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
     if (tb >= lo && tb < hi) {
       const int i = BACK ? first - tb : tb - first;
       begin_b[i] = b;
-      atomicOr(&flags[i / S], 1u << i % S);
+      atomicOr(&begins[i / S], 1u << i % S);
     }
     if (te >= lo && te < hi) {
       const int i = BACK ? first - te : te - first;
       end_b[i] = b;
-      atomicOr(&flags[i / S], 0x10000u << i % S);
+      atomicOr(&ends[i / S], 1u << i % S);
     }
   }
+  const int group0 = chunk / kGroup * kGroup, super0 = chunk / kSuper * kSuper;
+  const int from = min(plan.y, chunk);
+  const int from1 = max(from, group0);                         // chunks whose pairs are needed: from1 .. chunk - 1,
+  const int from2 = max(from, super0) / kGroup;                // groups: from2 .. group0 / kGroup - 1 (where from < group0),
+  const bool old = from < super0;                              // and the state in front of the super
   __syncthreads();
-  uint32_t flag = flags[slice];
-  if (UNI) flag = __builtin_amdgcn_readfirstlane(flag);
-  const int t_first = BACK ? first - slice * S : first + slice * S;
-  auto token = [&](int s) { return BACK ? t_first - s : t_first + s; };
-  auto live = [&](int s) { return token(s) >= live_lo && token(s) < live_hi; };
-  // Rows that are no history's are not read (another's stands in): what comes of
-  // them is not written, and the next history begins anew.
-  const int read_lo = live_lo < live_hi ? live_lo : lo, read_hi = live_lo < live_hi ? live_hi : hi;
-  auto load = [&](auto& r, const auto* base, int t) {
-    const auto* p = base + static_cast<int64_t>(min(max(t, read_lo), read_hi - 1)) * d + from_ch;
-    if (EVEN)
-      r.load(p);
-    else
-      r.load(p, nch);
-  };
-
-  // the slice from state 0: p[s] = A, q[s] = H; on the way back of D_t
-  Raw<T, 2> gate[S];
-  float p[S][2], q[S][2];
-  float A[2] = {1.f, 1.f}, H[2] = {0.f, 0.f};
+  uint32_t begin = begins[slice], end = ends[slice];
+  if (UNI) begin = __builtin_amdgcn_readfirstlane(begin), end = __builtin_amdgcn_readfirstlane(end);
   {
-    Raw<T, 2> xr[BACK ? 1 : S];
-    Raw<TH, 2> dr[BACK ? S : 1];
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      load(gate[s], static_cast<const T*>(a.gate), token(s));
-      if constexpr (BACK) {
-        dr[s].zero();
-        if (a.dh) load(dr[s], static_cast<const TH*>(a.dh), token(s));
-      } else {
-        load(xr[s], static_cast<const T*>(a.x), token(s));
-      }
-    }
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      if (flag >> s & 1) {
-        const float* in = BACK ? a.dlast : a.h0;
-        const long at = static_cast<long>(begin_b[slice * S + s]) * d + ch;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          A[e] = 0.f;
-          H[e] = in && e < nch ? in[at + e] : 0.f;
-        }
-      }
+    const int ch = cg * 128 + 2 * row_lane, nch = d - ch;      // this lane's channels: 2 or 1 (or none)
+    const uint32_t from_ch = from_of(cg);
+
+    // the state (back: E) that a history begins with at token s of the slice
+    auto start = [&](int s, float (&v)[2]) {
+      const float* in = BACK ? a.dlast : a.h0;
+      const long at = static_cast<long>(begin_b[slice * S + s]) * d + ch;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const Gate g = gate_of(gate[s].at(e));
-        if constexpr (BACK) {
-          p[s][e] = A[e];
-          q[s][e] = dr[s].at(e) + H[e];
-          A[e] *= g.f;
-          H[e] = g.f * q[s][e];
-        } else {
-          p[s][e] = A[e] *= g.f;
-          q[s][e] = H[e] = fmaf(g.f, H[e], g.rest * xr[s].at(e));
+        v[e] = in && e < nch ? in[at + e] : 0.f;
+        asm volatile("" : "+v"(v[e]));                         // (waited for here, not by tokens without a beginning)
+      }
+    };
+    // the slice from state 0
+    float A[2] = {1.f, 1.f}, H[2] = {0.f, 0.f};
+    auto run = [&](auto marked) {
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        if (marked && (begin >> s & 1)) {
+          A[0] = A[1] = 0.f;
+          start(s, H);
         }
-      }
-    }
-  }
-
-  // slices joined: (A, H) of all slices before this one, within the wave, then over waves
-  float before_a[2] = {1.f, 1.f}, before_h[2] = {0.f, 0.f}, wave_a[2], wave_h[2];
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    float ca = A[e], chh = H[e];                 // inclusive over slices of the wave
-    if (!UNI) {
-      for (int o = lanes; o < 64; o <<= 1) {
-        const float ua = __shfl_up(ca, o), uh = __shfl_up(chh, o);
-        if (lane >= o) {
-          chh += through(ca, uh);
-          ca = through(ca, ua);
-        }
-      }
-      const float ua = __shfl_up(ca, lanes), uh = __shfl_up(chh, lanes);
-      if (sub) before_a[e] = ua, before_h[e] = uh;
-    }
-    wave_a[e] = ca;
-    wave_h[e] = chh;
-    if (sub == per_wave - 1) {
-      sum_a[wave][2 * row_lane + e] = ca;
-      sum_h[wave][2 * row_lane + e] = chh;
-    }
-  }
-  __syncthreads();
-  float pre_a[2] = {1.f, 1.f}, pre_h[2] = {0.f, 0.f};           // of the waves before
-  for (int w = 0; w < wave; ++w)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float wa = sum_a[w][2 * row_lane + e], wh = sum_h[w][2 * row_lane + e];
-      pre_h[e] = wh + through(wa, pre_h[e]);
-      pre_a[e] = through(wa, pre_a[e]);
-    }
-  float all_a[2], all_h[2];                                     // of the chunk (the last wave's last slice)
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    all_h[e] = wave_h[e] + through(wave_a[e], pre_h[e]);
-    all_a[e] = through(wave_a[e], pre_a[e]);
-  }
-  const bool speaks = wave == kWaves - 1 && sub == per_wave - 1;
-  if (a.chunks > 1 && speaks)
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (e < nch) publish(a.pairs + static_cast<long>(chunk) * a.d + ch + e, all_a[e], all_h[e]);
-
-  // the state that comes in
-  float state[2] = {0.f, 0.f};
-  if (plan.y < chunk) {
-    const int group0 = chunk / kGroup * kGroup, from = max(plan.y, group0);
-    float ra[2] = {1.f, 1.f}, rh[2] = {0.f, 0.f};
-    uint64_t got[kSlots][2];
-    bool missing = false;
-#pragma unroll
-    for (int k = 0; k < kSlots; ++k) {
-      const int j = group0 + wave * kSlots + k;
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        got[k][e] = j >= from && j < chunk && e < nch ? look(a.pairs + static_cast<long>(j) * a.d + ch + e) : ~0ull;
-    }
-    do {
-      missing = false;
-#pragma unroll
-      for (int k = 0; k < kSlots; ++k) {
-        const int j = group0 + wave * kSlots + k;
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (!there(got[k][e])) {
-            got[k][e] = look(a.pairs + static_cast<long>(j) * a.d + ch + e);
-            missing = missing || !there(got[k][e]);
-          }
-      }
-      if (missing) __builtin_amdgcn_s_sleep(2);
-    } while (missing);
-#pragma unroll
-    for (int k = 0; k < kSlots; ++k) {
-      const int j = group0 + wave * kSlots + k;
-      if (j >= from && j < chunk)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float wa = a_of(got[k][e]);
-          rh[e] = h_of(got[k][e]) + through(wa, rh[e]);
-          ra[e] = through(wa, ra[e]);
+          float f, rest;
+          gates_of<T>(gate[s].at(e), f, rest);
+          A[e] *= f;
+          if constexpr (BACK)
+            H[e] = f * (dr[s].at(e) + H[e]);
+          else
+            H[e] = fmaf(f, H[e], rest * xr[s].at(e));
         }
-    }
-    if (sub == 0)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        in_a[wave][2 * row_lane + e] = ra[e];
-        in_h[wave][2 * row_lane + e] = rh[e];
       }
-    if (wave == 0 && plan.y < group0 && sub == 0)
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (e < nch) {
-          const uint64_t* w = a.states + static_cast<long>(chunk / kGroup - 1) * a.d + ch + e;
-          uint64_t v = look(w);
-          while (!there(v)) {
-            __builtin_amdgcn_s_sleep(2);
-            v = look(w);
-          }
-          in_s[2 * row_lane + e] = h_of(v);
-        }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      state[e] = plan.y < group0 ? in_s[2 * row_lane + e] : 0.f;
-      for (int w = 0; w < kWaves; ++w)
-        state[e] = in_h[w][2 * row_lane + e] + through(in_a[w][2 * row_lane + e], state[e]);
-    }
-  }
-  if (a.chunks > 1 && chunk % kGroup == kGroup - 1 && speaks)
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (e < nch)
-        publish(a.states + static_cast<long>(chunk / kGroup) * a.d + ch + e, 0.f, all_h[e] + through(all_a[e], state[e]));
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    state[e] = pre_h[e] + through(pre_a[e], state[e]);          // over the waves before,
-    state[e] = before_h[e] + through(before_a[e], state[e]);    // and the wave's slices before
-  }
-
-  // out
-  if (nch <= 0) return;
-  if constexpr (!BACK) {
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      if (flag >> s & 1) state[0] = state[1] = 0.f;
-      if (!live(s)) continue;
-      const float v[2] = {fmaf(p[s][0], state[0], q[s][0]), fmaf(p[s][1], state[1], q[s][1])};
-      const int64_t row = static_cast<int64_t>(token(s)) * d;
-      if (a.h_bf16)
-        put<EVEN>(static_cast<bf16_t*>(a.h) + row + from_ch, v, nch);
-      else
-        put<EVEN>(static_cast<float*>(a.h) + row + from_ch, v, nch);
-      if (a.last && (flag >> (16 + s) & 1)) put<EVEN>(a.last + static_cast<long>(end_b[slice * S + s]) * d + from_ch, v, nch);
-    }
-  } else {
-    // (the gates are formed again: kept from above they would take S more registers for each channel)
+    };
+    // (slices in which no history begins, nearly all, have a form without the tests)
+    if (__any(begin))
+      run(std::true_type{});
+    else
+      run(std::false_type{});
+    // What follows forms the gates again, from the rows as they lie in registers: half as many as
+    // every token's A and H would take, so that a slice can be twice as long.
 #pragma unroll
     for (int s = 0; s < S; ++s)
 #pragma unroll
       for (int i = 0; i < Raw<T, 2>::kWords; ++i) asm volatile("" : "+v"(gate[s].w[i]));
+
+    // slices joined: (A, H) of the wave's slices before this one, and of the wave
+    float before_a[2] = {1.f, 1.f}, before_h[2] = {0.f, 0.f};
 #pragma unroll
-    for (int s0 = 0; s0 < S; s0 += kBlock) {
-      Raw<T, 2> xr[kBlock];
-      Raw<TH, 2> hr[kBlock];
-#pragma unroll
-      for (int i = 0; i < kBlock; ++i) {
-        load(xr[i], static_cast<const T*>(a.x), token(s0 + i));
-        // (of a history's first token not used)
-        const TH* before = static_cast<const TH*>(a.h) + static_cast<int64_t>(max(token(s0 + i) - 1, 0)) * d + from_ch;
-        if (EVEN)
-          hr[i].load(before);
-        else
-          hr[i].load(before, nch);
-      }
-#pragma unroll
-      for (int i = 0; i < kBlock; ++i) {
-        const int s = s0 + i;
-        const int64_t row = static_cast<int64_t>(token(s)) * d;
-        if (flag >> s & 1) state[0] = state[1] = 0.f;
-        if (!live(s)) {                        // rows of no history: no loss depends on them
-          const float none[2] = {0.f, 0.f};
-          if (token(s) >= 0) {
-            put<EVEN>(static_cast<T*>(a.dgate) + row + from_ch, none, nch);
-            put<EVEN>(static_cast<T*>(a.dx) + row + from_ch, none, nch);
+    for (int e = 0; e < 2; ++e) {
+      float ca = A[e], chh = H[e];                             // inclusive over slices of the wave
+      if (!UNI) {
+        for (int o = lanes; o < 64; o <<= 1) {
+          const float ua = __shfl_up(ca, o), uh = __shfl_up(chh, o);
+          if (lane >= o) {
+            chh += through(ca, uh);
+            ca = through(ca, ua);
           }
-          continue;
         }
-        float prev[2] = {hr[i].at(0), hr[i].at(1)}, dg[2], dx[2], out[2];
-        const bool stops = flag >> (16 + s) & 1;
-        const long b = stops ? end_b[slice * S + s] : 0;
-        if (stops)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) prev[e] = a.h0 && e < nch ? a.h0[b * d + ch + e] : 0.f;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const Gate g = gate_of(gate[s].at(e));
-          const float D = fmaf(p[s][e], state[e], q[s][e]);
-          dx[e] = g.rest * D;
-          out[e] = g.f * D;
-          dg[e] = out[e] * g.rest * (prev[e] - xr[i].at(e));
-        }
-        put<EVEN>(static_cast<T*>(a.dgate) + row + from_ch, dg, nch);
-        put<EVEN>(static_cast<T*>(a.dx) + row + from_ch, dx, nch);
-        if (stops && a.dh0) put<EVEN>(a.dh0 + b * d + from_ch, out, nch);
+        const float ua = __shfl_up(ca, lanes), uh = __shfl_up(chh, lanes);
+        if (sub) before_a[e] = ua, before_h[e] = uh;
+      }
+      if (sub == per_wave - 1) {
+        sum_a[wave][2 * row_lane + e] = ca;
+        sum_h[wave][2 * row_lane + e] = chh;
       }
     }
+    __syncthreads();                                           // sums
+    float pre_a[2], pre_h[2], all_a[2], all_h[2];              // of the waves before, and with this one (the last: of all)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      pre_a[e] = 1.f, pre_h[e] = 0.f;
+      for (int v = 0; v < wave; ++v) {
+        const float wa = sum_a[v][2 * row_lane + e], wh = sum_h[v][2 * row_lane + e];
+        pre_h[e] = wh + through(wa, pre_h[e]);
+        pre_a[e] = through(wa, pre_a[e]);
+      }
+      const float wa = sum_a[wave][2 * row_lane + e], wh = sum_h[wave][2 * row_lane + e];
+      all_h[e] = wh + through(wa, pre_h[e]);
+      all_a[e] = through(wa, pre_a[e]);
+    }
+    const bool speaks = a.chunks > 1 && wave == kWaves - 1 && sub == 0;
+    if (speaks)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (e < nch) publish(a.pairs + static_cast<long>(chunk) * d + ch + e, all_a[e], all_h[e]);
+    // the state that comes in: each wave gets a pair of the group's chunks, then one of the super's groups
+    float state[2] = {0.f, 0.f};
+    // (A, H) of the pairs i0 .. i1 - 1, pair j0 + v by wave v, joined
+    auto gather = [&](const uint64_t* base, int i0, int i1, int j0, float (&fa)[2], float (&fh)[2]) {
+      if (j0 + wave >= i0 && j0 + wave < i1 && sub == 0) {
+        const uint64_t* at = base + static_cast<long>(j0 + wave) * d + ch;
+        uint64_t got[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) got[e] = e < nch ? look(at + e) : ~0ull;
+        while (__any(!there(got[0]) || !there(got[1]))) {
+          // (the channels' words were written together: until the first is there, only it is looked for)
+          for (;;) {
+            bool yes = true;
+            if (row_lane == 0) yes = there(got[0] = look(at));
+            if (__all(yes)) break;
+            __builtin_amdgcn_s_sleep(4);
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (!there(got[e])) got[e] = look(at + e);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          in_a[wave][2 * row_lane + e] = a_of(got[e]);
+          in_h[wave][2 * row_lane + e] = h_of(got[e]);
+        }
+      }
+      __syncthreads();
+      for (int i = i0; i < i1; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float wa = in_a[i - j0][2 * row_lane + e];
+          fh[e] = in_h[i - j0][2 * row_lane + e] + through(wa, fh[e]);
+          fa[e] = through(wa, fa[e]);
+        }
+      __syncthreads();
+    };
+    if (a.chunks > 1) {
+      float ga[2] = {1.f, 1.f}, gh[2] = {0.f, 0.f};
+      if (from1 < chunk) gather(a.pairs, from1, chunk, group0, ga, gh);
+      if (speaks && chunk % kGroup == kGroup - 1)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (e < nch)
+            publish(a.group_pairs + static_cast<long>(chunk / kGroup) * d + ch + e, through(all_a[e], ga[e]),
+                    all_h[e] + through(all_a[e], gh[e]));
+      if (from < group0) {
+        float sa[2] = {1.f, 1.f}, sh[2] = {0.f, 0.f};
+        if (old) {
+          if (wave == kWaves - 1 && sub == 0) {
+            const uint64_t* at = a.states + static_cast<long>(chunk / kSuper - 1) * d + ch;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              uint64_t v = e < nch ? look(at + e) : ~0ull;
+              while (!there(v)) {
+                __builtin_amdgcn_s_sleep(1);
+                v = look(at + e);
+              }
+              come[2 * row_lane + e] = h_of(v);
+            }
+          }
+        }
+        if (from2 < group0 / kGroup) gather(a.group_pairs, from2, group0 / kGroup, super0 / kGroup, sa, sh);
+        if (old) {
+          __syncthreads();
+          state[0] = come[2 * row_lane], state[1] = come[2 * row_lane + 1];
+          __syncthreads();
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) state[e] = sh[e] + through(sa[e], state[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) state[e] = gh[e] + through(ga[e], state[e]);
+      if (speaks && chunk % kSuper == kSuper - 1)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (e < nch)
+            publish(a.states + static_cast<long>(chunk / kSuper) * d + ch + e, 0.f, all_h[e] + through(all_a[e], state[e]));
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      state[e] = pre_h[e] + through(pre_a[e], state[e]);
+      state[e] = before_h[e] + through(before_a[e], state[e]);
+    }
+
+    // out
+    const int t_last = token(S - 1);
+    const bool plain = !begin && !end && min(t_first, t_last) >= live_lo && max(t_first, t_last) < live_hi;
+    auto out = [&](auto marked) {
+#pragma unroll
+      for (int s0 = 0; s0 < S; s0 += kBlock) {
+        Raw<T, 2> xo[kBlock];
+        Raw<TH, 2> hr[kBlock];
+        if constexpr (BACK)
+#pragma unroll
+          for (int i = 0; i < kBlock; ++i) {
+            load(xo[i], static_cast<const T*>(a.x), max(token(s0 + i), 0), from_ch);
+            load(hr[i], static_cast<const TH*>(a.h), max(token(s0 + i) - 1, 0), from_ch);    // (of a history's first token not used)
+          }
+#pragma unroll
+        for (int i = 0; i < kBlock; ++i) {
+          const int s = s0 + i;
+          if (marked && (begin >> s & 1)) start(s, state);
+          const bool stops = marked && (end >> s & 1);
+          float f[2], rest[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) gates_of<T>(gate[s].at(e), f[e], rest[e]);
+          if constexpr (!BACK) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) state[e] = fmaf(f[e], state[e], rest[e] * xr[s].at(e));
+            if ((marked && !live(s)) || nch <= 0) continue;
+            if (a.h_bf16)
+              put<EVEN>(row_at(static_cast<bf16_t*>(a.h), token(s), from_ch), state, nch);
+            else
+              put<EVEN>(row_at(static_cast<float*>(a.h), token(s), from_ch), state, nch);
+            if (stops && a.last) put<EVEN>(row_at(a.last, end_b[slice * S + s], from_ch), state, nch);
+          } else {
+            float prev[2] = {hr[i].at(0), hr[i].at(1)}, dg[2], dx[2];
+            const int b = stops ? end_b[slice * S + s] : 0;
+            if (stops)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                prev[e] = a.h0 && e < nch ? a.h0[static_cast<long>(b) * d + ch + e] : 0.f;
+                asm volatile("" : "+v"(prev[e]));
+              }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float D = dr[s].at(e) + state[e];
+              dx[e] = rest[e] * D;
+              state[e] = f[e] * D;
+              dg[e] = state[e] * rest[e] * (prev[e] - xo[i].at(e));
+            }
+            if ((marked && token(s) < 0) || nch <= 0) continue;
+            if (marked && !live(s)) dg[0] = dg[1] = dx[0] = dx[1] = 0.f;   // rows of no history: no loss depends on them
+            put<EVEN>(row_at(static_cast<T*>(a.dgate), token(s), from_ch), dg, nch);
+            put<EVEN>(row_at(static_cast<T*>(a.dx), token(s), from_ch), dx, nch);
+            if (stops && a.dh0) put<EVEN>(row_at(a.dh0, b, from_ch), state, nch);
+          }
+        }
+      }
+    };
+    if (__all(plain))
+      out(std::false_type{});
+    else
+      out(std::true_type{});
   }
 }
 
@@ -504,8 +549,9 @@ __global__ __launch_bounds__(256) void k_gated_step(StepArgs a) {
   float o[VE];
 #pragma unroll
   for (int e = 0; e < VE; ++e) {
-    const Gate f = gate_of(g.at(e));
-    o[e] = fmaf(f.f, h.at(e), f.rest * x.at(e));
+    float f, rest;
+    gates_of<T>(g.at(e), f, rest);
+    o[e] = fmaf(f, h.at(e), rest * x.at(e));
   }
   vec::store(a.state_out + i, o, n);
   if (!a.h) return;
@@ -517,18 +563,24 @@ __global__ __launch_bounds__(256) void k_gated_step(StepArgs a) {
 
 namespace {
 
-// tokens of a slice: what two workgroups of a CU have registers for
-template <bool BACK>
+// Tokens of a slice.  The more, the fewer waits, each of which costs a workgroup the latencies
+// of a store and a load that pass the caches: 24 in place of 32 took 230 us at 262,144 x 512 forward (219).
+// Beyond these registers run out, and slices side by side in a wave make chunks long enough.
+template <bool BACK, typename T, bool UNI>
 constexpr int slice_len() {
-  return BACK ? 8 : 16;
+  return !BACK && UNI && sizeof(T) == 2 ? 32 : 16;
 }
 struct ScanShape {
   int lanes_log2, len, chunks, groups;
 };
+int row_lanes_log2(int d) {
+  int n = 2;
+  while (n < 6 && (2 << n) < d) ++n;
+  return n;
+}
 ScanShape scan_shape(int T, int d, int S) {
   ScanShape s{};
-  s.lanes_log2 = 2;
-  while (s.lanes_log2 < 6 && (2 << s.lanes_log2) < d) ++s.lanes_log2;
+  s.lanes_log2 = row_lanes_log2(d);
   s.len = kWaves * (64 >> s.lanes_log2) * S;
   s.chunks = static_cast<int>((static_cast<long>(T) + s.len - 1) / s.len);
   s.groups = (d + 127) / 128;
@@ -536,14 +588,15 @@ ScanShape scan_shape(int T, int d, int S) {
 }
 constexpr size_t kScanAlign = 256;
 size_t up(size_t n) { return (n + kScanAlign - 1) / kScanAlign * kScanAlign; }
-size_t shape_bytes(const ScanShape& s, int d) {
-  if (s.chunks <= 1) return 0;
-  return kScanAlign + up(s.chunks * sizeof(int2)) + (static_cast<size_t>(s.chunks) + s.chunks / kGroup) * d * sizeof(uint64_t);
+long pair_words(const ScanShape& s, int d) {
+  return (static_cast<long>(s.chunks) + s.chunks / kGroup + s.chunks / kSuper) * d;
 }
-
-template <bool BACK, typename T, typename TH>
-hipError_t run_scan(ScanArgs a, void* ws, hipStream_t st) {
-  constexpr int S = slice_len<BACK>();
+size_t shape_bytes(const ScanShape& s, int d) {
+  return s.chunks <= 1 ? 0 : kScanAlign + up(s.chunks * sizeof(int2)) + pair_words(s, d) * sizeof(uint64_t);
+}
+template <bool BACK, typename T, typename TH, bool UNI>
+hipError_t run_scan_lanes(ScanArgs a, void* ws, hipStream_t st) {
+  constexpr int S = slice_len<BACK, T, UNI>();
   const ScanShape s = scan_shape(a.T, a.d, S);
   a.chunks = s.chunks;
   a.groups = s.groups;
@@ -557,30 +610,31 @@ hipError_t run_scan(ScanArgs a, void* ws, hipStream_t st) {
     a.ticket = reinterpret_cast<uint32_t*>(w);
     a.plan = reinterpret_cast<int2*>(w + kScanAlign);
     a.pairs = reinterpret_cast<uint64_t*>(w + kScanAlign + up(s.chunks * sizeof(int2)));
-    a.states = a.pairs + static_cast<long>(s.chunks) * a.d;
-    const long want = std::max<long>(static_cast<long>(s.chunks) * a.d / 1024, s.chunks / 4);
+    a.group_pairs = a.pairs + static_cast<long>(s.chunks) * a.d;
+    a.states = a.group_pairs + static_cast<long>(s.chunks / kGroup) * a.d;
+    a.words = pair_words(s, a.d);
+    const long want = std::max<long>(a.words / 1024, s.chunks / 4);
     hipLaunchKernelGGL((k_scan_plan<BACK>), dim3(static_cast<unsigned>(std::min(want + 1, 1024l))), dim3(256), 0, st, a, s.len);
   }
   const unsigned grid = static_cast<unsigned>(s.chunks) * s.groups;
-  const bool even = a.d % 2 == 0;
-  if (s.lanes_log2 == 6 && even)
-    hipLaunchKernelGGL((k_scan<BACK, T, TH, S, true, true>), dim3(grid), dim3(kThreads), 0, st, a);
-  else if (s.lanes_log2 == 6)
-    hipLaunchKernelGGL((k_scan<BACK, T, TH, S, true, false>), dim3(grid), dim3(kThreads), 0, st, a);
-  else if (even)
-    hipLaunchKernelGGL((k_scan<BACK, T, TH, S, false, true>), dim3(grid), dim3(kThreads), 0, st, a);
+  if (a.d % 2 == 0)
+    hipLaunchKernelGGL((k_scan<BACK, T, TH, S, UNI, true>), dim3(grid), dim3(kThreads), 0, st, a);
   else
-    hipLaunchKernelGGL((k_scan<BACK, T, TH, S, false, false>), dim3(grid), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((k_scan<BACK, T, TH, S, UNI, false>), dim3(grid), dim3(kThreads), 0, st, a);
   return hipGetLastError();
+}
+template <bool BACK, typename T, typename TH>
+hipError_t run_scan(const ScanArgs& a, void* ws, hipStream_t st) {
+  return row_lanes_log2(a.d) == 6 ? run_scan_lanes<BACK, T, TH, true>(a, ws, st) : run_scan_lanes<BACK, T, TH, false>(a, ws, st);
 }
 
 }  // namespace
 
 size_t gated_scan_bytes(int T, int d) {
-  return std::max(shape_bytes(scan_shape(T, d, slice_len<false>()), d), shape_bytes(scan_shape(T, d, slice_len<true>()), d));
+  return shape_bytes(scan_shape(T, d, 16), d);                // (of the shortest slices)
 }
 long gated_scan_blocks(int T, int d) {
-  const ScanShape s = scan_shape(T, d, std::min(slice_len<false>(), slice_len<true>()));
+  const ScanShape s = scan_shape(T, d, 16);
   return static_cast<long>(s.chunks) * s.groups;
 }
 

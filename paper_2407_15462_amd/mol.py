@@ -880,14 +880,16 @@ def gated_scan(gate: torch.Tensor, x: torch.Tensor, offsets: Optional[torch.Tens
 
     gate, x: [T][d] packed tokens; offsets: int32 [B + 1], history b's tokens are offsets[b] .. offsets[b + 1] - 1
     (None: one history of all tokens); h0: float32 [B][d], the states before them (zeros by default).  h in ``dtype``
-    (x's by default), last in float32, and may be written to ``out`` and ``last``; last may be h0.  Rows of no history
-    are not written in h."""
+    (x's by default), last in float32, and may be written to ``out`` and ``last``; last may be h0 (which is copied
+    first).  Rows of no history are not written in h."""
     T, d, B = _histories(gate, x, offsets, h0)
     dev = x.device
     with _on(dev, stream):
         ws = _workspace(lambda: mol_gated_scan_workspace(T, d, B), ws, dev)
         out = _output(out, x, dtype)
         last = _output(last, x, torch.float32, "last", (B, d))
+        if h0 is not None and last.data_ptr() == h0.data_ptr():
+            h0 = h0.clone()
         _check(load().mol_gated_scan(gate.data_ptr(), x.data_ptr(), _DTYPES[x.dtype], T, d, _at(offsets), B, _at(h0),
                                      out.data_ptr(), _DTYPES[out.dtype], last.data_ptr(), _at(ws),
                                      0 if ws is None else ws.numel(), _stream(stream)))

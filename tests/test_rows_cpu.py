@@ -52,9 +52,9 @@ TOKENS = [(dict(T=-1), EINVAL), (dict(d=0), EINVAL), (dict(B=0), EINVAL), (dict(
         (dict(n=-1), EINVAL), (dict(n=1 << 40), EINVAL), (dict(p=-0.1), EINVAL), (dict(p=1.0), EINVAL), (dict(p=NAN), EINVAL),
         (dict(p=0.999999), EINVAL), (dict(offset=4), EINVAL), (dict(xt=2), EUNSUPPORTED), (dict(yt=2), EUNSUPPORTED),
         (dict(x=None), EINVAL), (dict(y=None), EINVAL)]] + [
-    ("mol_gated_scan", SCAN, b, s) for b, s in TOKENS] + [
+    ("mol_gated_scan", SCAN, b, s) for b, s in TOKENS + [(dict(h0=FAKE, last=FAKE), EINVAL)]] + [
     ("mol_gated_scan_grad", SCAN_GRAD, b, s) for b, s in TOKENS + [
-        (dict(dh=None), EINVAL), (dict(dgate=None), EINVAL), (dict(dx=None), EINVAL)]] + [
+        (dict(dh=None), EINVAL), (dict(dgate=None), EINVAL), (dict(dx=None), EINVAL), (dict(dlast=FAKE, dh0=FAKE), EINVAL)]] + [
     ("mol_gated_step", STEP, b, s) for b, s in [
         (dict(B=-1), EINVAL), (dict(d=0), EINVAL), (dict(d=65537), EUNSUPPORTED), (dict(B=1 << 30), EUNSUPPORTED),
         (dict(xt=2), EUNSUPPORTED), (dict(ht=2), EUNSUPPORTED), (dict(gate=None), EINVAL), (dict(x=None), EINVAL),
