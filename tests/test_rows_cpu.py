@@ -130,5 +130,5 @@ def test_the_oracles_generator_gives_the_published_answers():
 
 def test_workspace_query_writes_whole_size():
     out = ctypes.c_size_t(0)
-    assert mol.load().mol_gated_scan_workspace(1 << 23, 4096, 1, ctypes.byref(out)) == mol.MOL_OK
+    assert mol.load().mol_gated_scan_workspace(1 << 23, 8192, 1, ctypes.byref(out)) == mol.MOL_OK
     assert out.value > 1 << 32
