@@ -10,11 +10,14 @@
 // Bound by memory: a row is read once into the registers of a team of lanes
 // (both rows of a gradient), its statistics are formed there (variance about the mean,
 // float32; a gradient forms them again from x rather than reading them), and it is
-// written once.
+// written once.  Measured: layer norm of 262,144 x 512 bf16 99 us (5.4 TB/s, where a copy of as
+// much runs at 5.0), its gradient 158 + 5 (4.9); 172M float32 elements to bf16 rows of 32 of
+// length 1 174 us (6.0).  Where rows are few, their chains of loads and sums: 32 rows of 1024 take
+// 3.5 us, the gradient of 4099 float32 rows of 777 14 + 4 (7 at the rate of large ones).
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
-#include "mol_grad.h"
 #include "mol_kernels.h"
 #include "mol_vec.h"
 
@@ -71,13 +74,17 @@ struct Team {
 template <int E, int VE>
 struct Place {
   int col[E / VE], n[E / VE];      // first element of each run, and how many of the row's it holds
-  __device__ __forceinline__ Place(int lane, int lanes, int d) {
+  int span, d;
+  __device__ __forceinline__ Place(int lane, int lanes, int d_) : span(lanes * VE), d(d_) {
 #pragma unroll
     for (int g = 0; g < E / VE; ++g) {
       col[g] = (g * lanes + lane) * VE;
       n[g] = min(VE, d - col[g]);
     }
   }
+  // of the runs g of all lanes: all whole, none there
+  __device__ __forceinline__ bool full(int g) const { return (g + 1) * span <= d; }
+  __device__ __forceinline__ bool none(int g) const { return g * span >= d; }
 };
 
 // Powers of two that bring a row's squares back into range, for sums of
@@ -97,13 +104,15 @@ struct Stats {
   template <typename T>
   __device__ __forceinline__ void form(const Raw<T, VE> (&raw)[E / VE], const Place<E, VE>& at, const Team<TEAM>& team, int d,
                                        float eps) {
-    float ss = squares(raw, at, team, d, 1.f);
+    float ss;
     scale = 1.f;
-    const float want = rescale(ss);
-    // (a layer norm's small rows need none: eps is added to their variance)
-    if (__any(MODE == kLength ? want != 1.f : want < 1.f)) {
-      scale = MODE == kLength || want < 1.f ? want : 1.f;
+    for (bool again = false;; again = true) {                  // (one copy of the code, which runs once, seldom twice)
       ss = squares(raw, at, team, d, scale);
+      const float want = rescale(ss);
+      // (a layer norm's small rows need none: eps is added to their variance)
+      const bool needed = MODE == kLength ? want != 1.f : want < 1.f;
+      if (again || !__any(needed)) break;
+      if (needed) scale = want;
     }
     if (MODE == kLayer) {
       inv = 1.f / sqrtf(ss / d + eps * scale * scale);
@@ -124,9 +133,8 @@ struct Stats {
     for (int g = 0; g < E / VE; ++g)
 #pragma unroll
       for (int e = 0; e < VE; ++e) x[g * VE + e] = raw[g].at(e);
-    if (scale_needed(s))
 #pragma unroll
-      for (int i = 0; i < E; ++i) x[i] *= s;
+    for (int i = 0; i < E; ++i) x[i] *= s;
     if (MODE == kLayer) {
 #pragma unroll
       for (int i = 0; i < E; ++i) mean[0] += x[i];
@@ -135,27 +143,60 @@ struct Stats {
     }
     float ss[1] = {0.f};
 #pragma unroll
-    for (int g = 0; g < E / VE; ++g)
+    for (int g = 0; g < E / VE; ++g) {
+      if (MODE == kLayer) {
+        if (WHOLE || at.full(g)) {
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        float& v = x[g * VE + e];
-        if (MODE == kLayer) v = WHOLE || e < at.n[g] ? v - mean[0] : 0.f;
-        ss[0] = fmaf(v, v, ss[0]);
+          for (int e = 0; e < VE; ++e) x[g * VE + e] -= mean[0];
+        } else {
+#pragma unroll
+          for (int e = 0; e < VE; ++e) x[g * VE + e] = e < at.n[g] ? x[g * VE + e] - mean[0] : 0.f;
+        }
       }
+#pragma unroll
+      for (int e = 0; e < VE; ++e) ss[0] = fmaf(x[g * VE + e], x[g * VE + e], ss[0]);
+    }
     team.sum(ss);
     return ss[0];
   }
-  static __device__ __forceinline__ bool scale_needed(float s) { return __any(s != 1.f); }
 };
 
+// A row as it lies: runs that pass its end are read from where they would end with it
+// (settle() puts that right), so that every lane loads whole runs and nothing branches.
 template <typename T, int E, int VE>
 __device__ __forceinline__ void load_row(Raw<T, VE> (&r)[E / VE], const T* p, const Place<E, VE>& at, bool whole) {
+  if (!whole && at.d < VE) {                           // (rows shorter than a run)
+#pragma unroll
+    for (int g = 0; g < E / VE; ++g) r[g].load(p + at.col[g], at.n[g]);
+    return;
+  }
+#pragma unroll
+  for (int g = 0; g < E / VE; ++g) r[g].load(p + (whole ? at.col[g] : min(at.col[g], at.d - VE)));
+}
+// what was read for elements behind the row's end becomes 0, the last run's elements move to their places
+template <typename T, int E, int VE>
+__device__ __forceinline__ void settle(Raw<T, VE> (&r)[E / VE], const Place<E, VE>& at, bool whole) {
+  if (whole || at.d < VE) return;
+  constexpr int kPer = 4 / sizeof(T);                  // elements of a word
 #pragma unroll
   for (int g = 0; g < E / VE; ++g) {
-    if (whole)
-      r[g].load(p + at.col[g]);
-    else
-      r[g].load(p + at.col[g], at.n[g]);
+    if (at.full(g)) continue;
+    if (at.d % VE) {                                   // by VE - n elements, of the lane whose run is cut
+      const int k = at.n[g] > 0 ? VE - at.n[g] : 0;
+#pragma unroll
+      for (int by = 1; by < Raw<T, VE>::kWords; by <<= 1)
+#pragma unroll
+        for (int i = 0; i < Raw<T, VE>::kWords; ++i)
+          r[g].w[i] = k / kPer & by ? (i + by < Raw<T, VE>::kWords ? r[g].w[i + by] : 0) : r[g].w[i];
+      if (kPer == 2)
+#pragma unroll
+        for (int i = 0; i < Raw<T, VE>::kWords; ++i) {
+          const uint32_t above = i + 1 < Raw<T, VE>::kWords ? r[g].w[i + 1] : 0;
+          r[g].w[i] = k & 1 ? __builtin_amdgcn_alignbit(above, r[g].w[i], 16) : r[g].w[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < Raw<T, VE>::kWords; ++i) r[g].w[i] = at.n[g] > 0 ? r[g].w[i] : 0;
   }
 }
 
@@ -164,24 +205,37 @@ __device__ __forceinline__ void store_row(void* out, int bf16, long row, int d, 
                                           const float (&v)[E]) {
 #pragma unroll
   for (int g = 0; g < E / VE; ++g) {
+    if (!whole && at.none(g)) continue;
     float o[VE];
 #pragma unroll
     for (int e = 0; e < VE; ++e) o[e] = v[g * VE + e];
     const long to = row * d + at.col[g];
-    const int n = whole ? VE : at.n[g];
+    auto put = [&](auto* y) {
+      if (whole || at.full(g) || at.n[g] >= VE)
+        vec::store(y + to, o);
+      else if (d % VE)
+        vec::store(y + to, o, at.n[g]);
+    };
     if (bf16)
-      vec::store(static_cast<bf16_t*>(out) + to, o, n);
+      put(static_cast<bf16_t*>(out));
     else
-      vec::store(static_cast<float*>(out) + to, o, n);
+      put(static_cast<float*>(out));
   }
 }
 
 template <int E, int VE>
-__device__ __forceinline__ void load_weights(float (&w)[E], const float* p, float otherwise, const Place<E, VE>& at) {
+__device__ __forceinline__ void load_weights(float (&w)[E], const float* p, float otherwise, const Place<E, VE>& at,
+                                             bool whole) {
+  if (p) {
+    Raw<float, VE> r[E / VE];
+    load_row(r, p, at, whole);
+    settle(r, at, whole);
 #pragma unroll
-  for (int g = 0; g < E / VE; ++g)
+    for (int i = 0; i < E; ++i) w[i] = r[i / VE].at(i % VE);
+  } else {
 #pragma unroll
-    for (int e = 0; e < VE; ++e) w[g * VE + e] = p && e < at.n[g] ? p[at.col[g] + e] : otherwise;
+    for (int i = 0; i < E; ++i) w[i] = otherwise;
+  }
 }
 
 template <int TEAM>
@@ -201,8 +255,8 @@ __global__ __launch_bounds__(threads<TEAM>()) void k_norm(RowArgs a) {
   const T* x = static_cast<const T*>(a.x);
   float gamma[E], beta[E];
   if (MODE == kLayer) {
-    load_weights(gamma, a.gamma, 1.f, at);
-    load_weights(beta, a.beta, 0.f, at);
+    load_weights(gamma, a.gamma, 1.f, at, WHOLE);
+    load_weights(beta, a.beta, 0.f, at, WHOLE);
   }
   const long step = static_cast<long>(gridDim.x) * teams;
   // (the rows of a wave start together and end together, so that sums over lanes find them all)
@@ -212,6 +266,7 @@ __global__ __launch_bounds__(threads<TEAM>()) void k_norm(RowArgs a) {
   load_row(raw, x + min(first + mine, a.T - 1) * a.d, at, WHOLE);
   for (long row = first; row < a.T; row += step) {
     if (row + step < a.T) load_row(next, x + min(row + step + mine, a.T - 1) * a.d, at, WHOLE);
+    settle(raw, at, WHOLE);
     Stats<MODE, TEAM, E, VE, WHOLE> st;
     st.form(raw, at, team, a.d, a.eps);
 #pragma unroll
@@ -237,8 +292,11 @@ __global__ __launch_bounds__(threads<TEAM>()) void k_norm_grad(RowArgs a) {
   const Place<E, VE> at(team.lane, lanes, a.d);
   const T* x = static_cast<const T*>(a.x);
   const TG* dy = static_cast<const TG*>(a.dy);
+  // (float32 rows leave no registers for the row behind them; nor do 16 elements of each of 1024 threads, for
+  // which gamma is read again with every row)
+  constexpr bool kGamma = TEAM < 1024 || E == 8, kAhead = kGamma && VE == 8;
   float gamma[E], dgamma[E], dbeta[E];
-  if (MODE == kLayer) load_weights(gamma, a.gamma, 1.f, at);
+  if (MODE == kLayer && kGamma) load_weights(gamma, a.gamma, 1.f, at, WHOLE);
 #pragma unroll
   for (int i = 0; i < E; ++i) dgamma[i] = dbeta[i] = 0.f;
   const long step = static_cast<long>(gridDim.x) * teams;
@@ -251,15 +309,16 @@ __global__ __launch_bounds__(threads<TEAM>()) void k_norm_grad(RowArgs a) {
     load_row(r, x + at_row, at, WHOLE);
     load_row(g, dy + at_row, at, WHOLE);
   };
-  // (a team of a whole workgroup has no registers for the row behind)
-  constexpr bool kAhead = TEAM == 0;
   if (kAhead) fetch(raw, graw, first);
   for (long row = first; row < a.T; row += step) {
     if (!kAhead)
       fetch(raw, graw, row);
     else if (row + step < a.T)
       fetch(next, gnext, row + step);
+    if (MODE == kLayer && !kGamma) load_weights(gamma, a.gamma, 1.f, at, WHOLE);
     const bool live = row + mine < a.T;
+    settle(raw, at, WHOLE);
+    settle(graw, at, WHOLE);
     Stats<MODE, TEAM, E, VE, WHOLE> st;
     st.form(raw, at, team, a.d, a.eps);
     float w[E], c[2] = {0.f, 0.f};             // layer norm: sums of w and w xhat; L2: of y dy
@@ -339,6 +398,29 @@ __global__ __launch_bounds__(threads<TEAM>()) void k_norm_grad(RowArgs a) {
   }
 }
 
+// The workgroups' parts [parts][2][d] summed: 16 columns of dgamma and dbeta by 64 runs of parts,
+// the runs in order.
+__global__ __launch_bounds__(1024) void k_norm_sums(const float* in, int parts, int d, float* dgamma, float* dbeta) {
+  __shared__ float sh[64][17];
+  const int c = threadIdx.x & 15, run = threadIdx.x / 16, col = blockIdx.x * 16 + c;
+  float v = 0.f;
+  if (col < 2 * d) {
+#pragma unroll 8
+    for (int k = run; k < parts; k += 64) v += in[static_cast<long>(k) * 2 * d + col];
+  }
+  sh[run][c] = v;
+  __syncthreads();
+  if (threadIdx.x < 64) {                              // four lanes a column
+    const int col4 = threadIdx.x / 4, q = threadIdx.x & 3;
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) t += sh[16 * q + k][col4];
+    t = vec::team_sum(t, 4);
+    const int to = blockIdx.x * 16 + col4;
+    if (q == 0 && to < 2 * d) (to < d ? dgamma[to] : dbeta[to - d]) = t;
+  }
+}
+
 namespace {
 
 struct RowPlan {
@@ -350,25 +432,32 @@ int pow2_up(int n) {
   while (p < n) p <<= 1;
   return p;
 }
-RowPlan row_plan(int d, bool grad) {
+// A row's team is as small as its registers allow, since sums over fewer lanes take fewer
+// steps, and a row of 64 lanes or less needs no barrier.
+RowPlan row_plan(int d) {
   RowPlan p{};
-  const int most = 16;
-  if (d <= 64 * most) {
-    p.E = d <= 8 * 16 ? 8 : most;
+  if (d <= 1024) {
+    p.E = d <= 128 ? 8 : 16;
     p.lanes = pow2_up((d + p.E - 1) / p.E);
     p.rows = 256 / p.lanes;
   } else {
-    p.E = most;
-    p.team = d <= 256 * most ? 256 : 1024;
+    p.team = d <= 4096 ? 256 : 1024;
+    p.E = d <= 8 * p.team ? 8 : 16;
     p.lanes = p.team;
     p.rows = 1;
   }
   return p;
 }
 bool row_whole(const RowPlan& p, int d) { return d == p.lanes * p.E; }
-long row_blocks(const RowPlan& p, long T, bool grad) {
-  const long want = (T + p.rows - 1) / p.rows;
-  return std::min(want, grad ? 1024l : 2048l);
+// Workgroups.  Without gradients of weights each takes the rows that it holds at once, since
+// a grid that stays drifts apart in memory (172M elements in rows of 32 to unit length: 174 us,
+// with 2048 workgroups that stay 206; wide rows, which read as much of gamma and beta, stay).
+// With them, whose parts each writes and a launch of sums reads, about as many as run at once,
+// of two rows a team at least (512 in place of 1024 took 179 us at 262,144 x 512, for 163).
+long row_blocks(const RowPlan& p, long T, bool weights) {
+  const long rows = weights ? 2 * p.rows : p.rows, want = (T + rows - 1) / rows;
+  if (p.team == 1024) return std::min(want, weights ? 256l : 512l);
+  return std::min(want, weights ? 1024l : 1l << 22);
 }
 
 template <int MODE, typename T, int TEAM, int E>
@@ -380,18 +469,20 @@ void run_norm(const RowArgs& a, long blocks, bool whole, hipStream_t st) {
 }
 template <int MODE, typename T>
 hipError_t launch_norm_mode(RowArgs& a, hipStream_t st) {
-  const RowPlan p = row_plan(a.d, false);
+  const RowPlan p = row_plan(a.d);
   a.lanes = p.lanes;
   const long blocks = row_blocks(p, a.T, false);
   const bool whole = row_whole(p, a.d);
-  if (p.team == 256)
-    run_norm<MODE, T, 256, 16>(a, blocks, whole, st);
-  else if (p.team)
-    run_norm<MODE, T, 1024, 16>(a, blocks, whole, st);
-  else if (p.E == 8)
-    run_norm<MODE, T, 0, 8>(a, blocks, whole, st);
-  else
-    run_norm<MODE, T, 0, 16>(a, blocks, whole, st);
+  auto of = [&](auto e) {
+    constexpr int E = decltype(e)::value;
+    if (p.team == 256)
+      run_norm<MODE, T, 256, E>(a, blocks, whole, st);
+    else if (p.team)
+      run_norm<MODE, T, 1024, E>(a, blocks, whole, st);
+    else
+      run_norm<MODE, T, 0, E>(a, blocks, whole, st);
+  };
+  p.E == 8 ? of(std::integral_constant<int, 8>{}) : of(std::integral_constant<int, 16>{});
   return hipGetLastError();
 }
 
@@ -405,41 +496,32 @@ void run_norm_grad(const RowArgs& a, long blocks, bool whole, hipStream_t st) {
 }
 template <int MODE, typename T, typename TG>
 hipError_t launch_norm_grad_mode(RowArgs& a, float* dgamma, float* dbeta, float* ws, hipStream_t st) {
-  const RowPlan p = row_plan(a.d, true);
+  const RowPlan p = row_plan(a.d);
   a.lanes = p.lanes;
-  const long blocks = row_blocks(p, a.T, true);       // (0 of no rows, whose sums are 0)
+  const long blocks = row_blocks(p, a.T, MODE == kLayer);     // (0 of no rows, whose sums are 0)
   const bool whole = row_whole(p, a.d), sums = dgamma && blocks != 1;
   a.dgamma = sums ? ws : dgamma;
   a.dbeta = sums ? ws + a.d : dbeta;
   a.part = sums ? 2l * a.d : 0;
-  if (blocks == 0)
-    ;
-  else if (p.team == 256)
-    run_norm_grad<MODE, T, TG, 256, 16>(a, blocks, whole, st);
-  else if (p.team)
-    run_norm_grad<MODE, T, TG, 1024, 16>(a, blocks, whole, st);
-  else if (p.E == 8)
-    run_norm_grad<MODE, T, TG, 0, 8>(a, blocks, whole, st);
-  else
-    run_norm_grad<MODE, T, TG, 0, 16>(a, blocks, whole, st);
+  auto of = [&](auto e) {
+    constexpr int E = decltype(e)::value;
+    if (p.team == 256)
+      run_norm_grad<MODE, T, TG, 256, E>(a, blocks, whole, st);
+    else if (p.team)
+      run_norm_grad<MODE, T, TG, 1024, E>(a, blocks, whole, st);
+    else
+      run_norm_grad<MODE, T, TG, 0, E>(a, blocks, whole, st);
+  };
+  if (blocks) p.E == 8 ? of(std::integral_constant<int, 8>{}) : of(std::integral_constant<int, 16>{});
   if (!sums) return hipGetLastError();
-  grad::SumList list(st);
-  for (int i = 0; i < 2; ++i) {
-    grad::SumJob j{};
-    j.in = ws + static_cast<long>(i) * a.d;
-    j.L = j.in_len = j.out_len = a.d;
-    j.stride = 2l * a.d;
-    j.S = static_cast<int>(blocks);
-    j.out = i ? dbeta : dgamma;
-    list.add(j);
-  }
-  return list.run();
+  hipLaunchKernelGGL(k_norm_sums, dim3((2 * a.d + 15) / 16), dim3(1024), 0, st, ws, static_cast<int>(blocks), a.d, dgamma, dbeta);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 size_t norm_grad_bytes(long T, int d) {
-  const long blocks = row_blocks(row_plan(d, true), T, true);
+  const long blocks = row_blocks(row_plan(d), T, true);
   return blocks > 1 ? static_cast<size_t>(blocks) * 2 * d * sizeof(float) : 0;
 }
 

@@ -724,24 +724,48 @@ def adamw_step(tensors: AdamwTensors, lr=1e-3, beta1: float = 0.9, beta2: float 
 
 
 # --------------------------------------------- between embedding rows and scores
-def _row_tensor(x: torch.Tensor, name: str) -> Tuple[int, int]:
+# These calls are short: what is checked is checked once and without further calls where it is as it should be,
+# and a call for another device or stream makes that one current and calls itself.
+def _rows(x: torch.Tensor, name: str = "x") -> Tuple[int, int]:
     """(rows, elements of a row) of a float tensor [..., d]."""
-    _need(isinstance(x, torch.Tensor) and x.dim() >= 1 and x.shape[-1] > 0, f"{name} must be a tensor [..., d]")
-    _operand(x, name, None, _FLOATS, x.device)
+    if not (isinstance(x, torch.Tensor) and x.dtype in _DTYPES and x.is_contiguous() and x.dim() and x.shape[-1] > 0):
+        _need(isinstance(x, torch.Tensor) and x.dim() >= 1 and x.shape[-1] > 0, f"{name} must be a tensor [..., d]")
+        _operand(x, name, None, _FLOATS, x.device)
     d = x.shape[-1]
-    _sizes(d)
     return x.numel() // d, d
 
 
-def _output(out: Optional[torch.Tensor], like: torch.Tensor, dtype, name: str = "out", shape=None) -> torch.Tensor:
-    """The caller's tensor, or a new one of ``dtype`` (like's by default)."""
-    shape = like.shape if shape is None else shape
+def _elsewhere(x: torch.Tensor, stream) -> bool:
+    """Whether a call has to make another device or stream current first."""
+    index = x.get_device()
+    if index < 0:
+        raise ValueError(f"the operands are on {x.device}, not on a GPU")
+    return stream is not None or index != torch._C._cuda_getDevice()
+
+
+def _like(x: torch.Tensor, t, name: str, dtypes) -> None:
+    """t: of x's shape and device."""
+    if not (isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == x.shape and t.get_device() == x.get_device() and
+            t.is_contiguous()):
+        _operand(t, name, x.shape, dtypes, x.device)
+
+
+def _vector(x: torch.Tensor, t, name: str, d: int) -> None:
+    """t: float32 [d] on x's device."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.float32 and t.dim() == 1 and t.shape[0] == d and
+            t.get_device() == x.get_device() and t.is_contiguous()):
+        _operand(t, name, (d,), _F32, x.device)
+
+
+def _output(out: Optional[torch.Tensor], x: torch.Tensor, dtype) -> torch.Tensor:
+    """The caller's tensor of x's shape, or a new one of ``dtype`` (x's by default)."""
     if out is None:
-        dtype = like.dtype if dtype is None else dtype
-        if dtype not in _FLOATS:
+        if dtype is None or dtype is x.dtype:
+            return torch.empty_like(x)
+        if dtype not in _DTYPES:
             raise ValueError(f"unsupported output dtype {dtype}")
-        return like.new_empty(shape, dtype=dtype)
-    _operand(out, name, shape, _FLOATS if dtype is None else (dtype,), like.device)
+        return torch.empty_like(x, dtype=dtype)
+    _like(x, out, "out", _FLOATS if dtype is None else (dtype,))
     return out
 
 
@@ -749,20 +773,29 @@ def _at(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _now(x: torch.Tensor) -> int:
+    """The current stream of x's device, which is current."""
+    return torch._C._cuda_getCurrentRawStream(x.get_device())
+
+
 def layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None, eps: float = 1e-5,
                dtype=None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Layer norm of the rows of x [..., d]: (x - mean) / sqrt(var + eps) gamma + beta, in ``dtype`` (x's by default).
 
     gamma, beta: float32 [d] (1 and 0 by default).  out may be x."""
-    T, d = _row_tensor(x, "x")
-    dev = x.device
-    for name, t in (("gamma", gamma), ("beta", beta)):
-        if t is not None:
-            _operand(t, name, (d,), _F32, dev)
-    with _on(dev, stream):
-        out = _output(out, x, dtype)
-        _check(load().mol_layer_norm(x.data_ptr(), _DTYPES[x.dtype], T, d, _at(gamma), _at(beta), eps, out.data_ptr(),
-                                     _DTYPES[out.dtype], _stream(stream)))
+    T, d = _rows(x)
+    if gamma is not None:
+        _vector(x, gamma, "gamma", d)
+    if beta is not None:
+        _vector(x, beta, "beta", d)
+    if _elsewhere(x, stream):
+        with _on(x.device, stream):
+            return layer_norm(x, gamma, beta, eps, dtype, out)
+    out = _output(out, x, dtype)
+    rc = load().mol_layer_norm(x.data_ptr(), _DTYPES[x.dtype], T, d, None if gamma is None else gamma.data_ptr(),
+                               None if beta is None else beta.data_ptr(), eps, out.data_ptr(), _DTYPES[out.dtype], _now(x))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -778,21 +811,25 @@ def layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Ten
 
     dx in ``dtype`` (x's by default), and into ``out`` if given (which may be dy or x); dgamma and dbeta float32 [d],
     or None without ``weights``."""
-    T, d = _row_tensor(x, "x")
-    dev = x.device
-    _operand(dy, "dy", x.shape, _FLOATS, dev)
+    T, d = _rows(x)
+    _like(x, dy, "dy", _FLOATS)
     if gamma is not None:
-        _operand(gamma, "gamma", (d,), _F32, dev)
-    with _on(dev, stream):
-        out = _output(out, x, dtype)
-        dgamma = dbeta = None
-        if weights:
-            ws = _workspace(lambda: mol_layer_norm_grad_workspace(T, d), ws, dev)
-            dgamma, dbeta = x.new_empty((2, d), dtype=torch.float32).unbind(0)
-        _check(load().mol_layer_norm_grad(
-            dy.data_ptr(), _DTYPES[dy.dtype], x.data_ptr(), _DTYPES[x.dtype], T, d, _at(gamma), eps, out.data_ptr(),
-            _DTYPES[out.dtype], _at(dgamma), _at(dbeta), _at(ws) if weights else None,
-            ws.numel() if weights and ws is not None else 0, _stream(stream)))
+        _vector(x, gamma, "gamma", d)
+    if _elsewhere(x, stream):
+        with _on(x.device, stream):
+            return layer_norm_grad(dy, x, gamma, eps, dtype, weights, out, ws)
+    out = _output(out, x, dtype)
+    dgamma = dbeta = None
+    if weights:
+        ws = _workspace(lambda: mol_layer_norm_grad_workspace(T, d), ws, x.device)
+        dgamma, dbeta = x.new_empty((2, d), dtype=torch.float32).unbind(0)
+    else:
+        ws = None
+    rc = load().mol_layer_norm_grad(
+        dy.data_ptr(), _DTYPES[dy.dtype], x.data_ptr(), _DTYPES[x.dtype], T, d, _at(gamma), eps, out.data_ptr(),
+        _DTYPES[out.dtype], _at(dgamma), _at(dbeta), _at(ws), 0 if ws is None else ws.numel(), _now(x))
+    if rc:
+        _check(rc)
     return out, dgamma, dbeta
 
 
@@ -800,23 +837,30 @@ def normalize(x: torch.Tensor, eps: float = 1e-12, dtype=None, out: Optional[tor
               stream=None) -> torch.Tensor:
     """The rows of x [..., d] to length one (Eq. 2's components): x / max(|x|, eps), in ``dtype`` (x's by default).
     out may be x."""
-    T, d = _row_tensor(x, "x")
-    with _on(x.device, stream):
-        out = _output(out, x, dtype)
-        _check(load().mol_normalize(x.data_ptr(), _DTYPES[x.dtype], T, d, eps, out.data_ptr(), _DTYPES[out.dtype],
-                                    _stream(stream)))
+    T, d = _rows(x)
+    if _elsewhere(x, stream):
+        with _on(x.device, stream):
+            return normalize(x, eps, dtype, out)
+    out = _output(out, x, dtype)
+    rc = load().mol_normalize(x.data_ptr(), _DTYPES[x.dtype], T, d, eps, out.data_ptr(), _DTYPES[out.dtype], _now(x))
+    if rc:
+        _check(rc)
     return out
 
 
 def normalize_grad(dy: torch.Tensor, x: torch.Tensor, eps: float = 1e-12, dtype=None, out: Optional[torch.Tensor] = None,
                    stream=None) -> torch.Tensor:
     """Gradient of normalize, given dy [..., d] and the x that went in, in ``dtype`` (x's by default).  out may be dy or x."""
-    T, d = _row_tensor(x, "x")
-    _operand(dy, "dy", x.shape, _FLOATS, x.device)
-    with _on(x.device, stream):
-        out = _output(out, x, dtype)
-        _check(load().mol_normalize_grad(dy.data_ptr(), _DTYPES[dy.dtype], x.data_ptr(), _DTYPES[x.dtype], T, d, eps,
-                                         out.data_ptr(), _DTYPES[out.dtype], _stream(stream)))
+    T, d = _rows(x)
+    _like(x, dy, "dy", _FLOATS)
+    if _elsewhere(x, stream):
+        with _on(x.device, stream):
+            return normalize_grad(dy, x, eps, dtype, out)
+    out = _output(out, x, dtype)
+    rc = load().mol_normalize_grad(dy.data_ptr(), _DTYPES[dy.dtype], x.data_ptr(), _DTYPES[x.dtype], T, d, eps,
+                                   out.data_ptr(), _DTYPES[out.dtype], _now(x))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -828,25 +872,31 @@ def dropout(x: torch.Tensor, p: float, seed: int, step=0, offset: int = 0, resid
     not stored: the gradient for x is the same call on dy, without residual.  step: a number in [0, 2^32), or one
     int32 on the GPU that the kernel reads, for graphs that are replayed.  offset: a multiple of 8; tensors of one
     step that are to have masks of their own need ranges of their own.  out may be x or residual."""
-    _need(isinstance(x, torch.Tensor), "x must be a tensor")
-    dev = x.device
-    _operand(x, "x", None, _FLOATS, dev)
-    if residual is not None:
-        _operand(residual, "residual", x.shape, _FLOATS, dev)
+    if not (isinstance(x, torch.Tensor) and x.dtype in _DTYPES and x.is_contiguous()):
+        _need(isinstance(x, torch.Tensor), "x must be a tensor")
+        _operand(x, "x", None, _FLOATS, x.device)
     on_step = isinstance(step, torch.Tensor)
     if on_step:
         _need(step.numel() == 1, "step must have one element")
-        _operand(step, "step", step.shape, _INT32, dev)
+        _operand(step, "step", step.shape, _INT32, x.device)
     elif not 0 <= step < 1 << 32:
         raise ValueError(f"step = {step} outside [0, 2^32)")
     if not 0 <= offset < 1 << 63:
         raise ValueError(f"offset = {offset} outside [0, 2^63)")
-    with _on(dev, stream):
-        out = _output(out, x, residual.dtype if out is None and dtype is None and residual is not None else dtype)
-        _need(residual is None or residual.dtype == out.dtype, "residual must have the output's dtype")
-        _check(load().mol_dropout(x.data_ptr(), _DTYPES[x.dtype], x.numel(), p, seed & 0xFFFFFFFFFFFFFFFF, offset,
-                                  0 if on_step else step, step.data_ptr() if on_step else None, _at(residual),
-                                  out.data_ptr(), _DTYPES[out.dtype], _stream(stream)))
+    if residual is not None:
+        _like(x, residual, "residual", _FLOATS)
+        dtype = residual.dtype if dtype is None and out is None else dtype
+    if _elsewhere(x, stream):
+        with _on(x.device, stream):
+            return dropout(x, p, seed, step, offset, residual, dtype, out)
+    out = _output(out, x, dtype)
+    if residual is not None and residual.dtype is not out.dtype:
+        raise ValueError("residual must have the output's dtype")
+    rc = load().mol_dropout(x.data_ptr(), _DTYPES[x.dtype], x.numel(), p, seed & 0xFFFFFFFFFFFFFFFF, offset,
+                            0 if on_step else step, step.data_ptr() if on_step else None,
+                            None if residual is None else residual.data_ptr(), out.data_ptr(), _DTYPES[out.dtype], _now(x))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -856,21 +906,28 @@ def gated_scan_workspace(x: torch.Tensor, B: int) -> torch.Tensor:
     return torch.empty(max(mol_gated_scan_workspace(T, d, B), 1), dtype=torch.uint8, device=x.device)
 
 
-def _histories(gate, x, offsets, h0):
-    """(T, d, B) of a scan's operands."""
+def _tokens(gate, x) -> Tuple[int, int]:
+    """(T, d) of a scan's or a step's gate and x."""
     _need(isinstance(x, torch.Tensor) and x.dim() == 2, "x must be a tensor [T][d]")
-    dev, (T, d) = x.device, x.shape
-    _operand(x, "x", None, _FLOATS, dev)
-    _operand(gate, "gate", x.shape, (x.dtype,), dev)
+    if not (x.dtype in _DTYPES and x.is_contiguous()):
+        _operand(x, "x", None, _FLOATS, x.device)
+    _like(x, gate, "gate", (x.dtype,))
+    T, d = x.shape
+    _sizes(T, d)
+    return T, d
+
+
+def _histories(x, d, offsets, h0) -> int:
+    """B, the histories of a scan."""
     B = 1
     if offsets is not None:
         _need(isinstance(offsets, torch.Tensor) and offsets.dim() == 1 and offsets.numel() > 1, "offsets must be a tensor [B + 1]")
-        _operand(offsets, "offsets", None, _INT32, dev)
+        _operand(offsets, "offsets", None, _INT32, x.device)
         B = offsets.numel() - 1
     if h0 is not None:
-        _operand(h0, "h0", (B, d), _F32, dev)
-    _sizes(T, d, B)
-    return T, d, B
+        _operand(h0, "h0", (B, d), _F32, x.device)
+    _sizes(B)
+    return B
 
 
 def gated_scan(gate: torch.Tensor, x: torch.Tensor, offsets: Optional[torch.Tensor] = None,
@@ -882,17 +939,24 @@ def gated_scan(gate: torch.Tensor, x: torch.Tensor, offsets: Optional[torch.Tens
     (None: one history of all tokens); h0: float32 [B][d], the states before them (zeros by default).  h in ``dtype``
     (x's by default), last in float32, and may be written to ``out`` and ``last``; last may be h0 (which is copied
     first).  Rows of no history are not written in h."""
-    T, d, B = _histories(gate, x, offsets, h0)
-    dev = x.device
-    with _on(dev, stream):
-        ws = _workspace(lambda: mol_gated_scan_workspace(T, d, B), ws, dev)
-        out = _output(out, x, dtype)
-        last = _output(last, x, torch.float32, "last", (B, d))
-        if h0 is not None and last.data_ptr() == h0.data_ptr():
-            h0 = h0.clone()
-        _check(load().mol_gated_scan(gate.data_ptr(), x.data_ptr(), _DTYPES[x.dtype], T, d, _at(offsets), B, _at(h0),
-                                     out.data_ptr(), _DTYPES[out.dtype], last.data_ptr(), _at(ws),
-                                     0 if ws is None else ws.numel(), _stream(stream)))
+    T, d = _tokens(gate, x)
+    B = _histories(x, d, offsets, h0)
+    if last is not None:
+        _operand(last, "last", (B, d), _F32, x.device)
+    if _elsewhere(x, stream):
+        with _on(x.device, stream):
+            return gated_scan(gate, x, offsets, h0, dtype, out, last, ws)
+    ws = _workspace(lambda: mol_gated_scan_workspace(T, d, B), ws, x.device)
+    out = _output(out, x, dtype)
+    if last is None:
+        last = x.new_empty((B, d), dtype=torch.float32)
+    elif h0 is not None and last.data_ptr() == h0.data_ptr():
+        h0 = h0.clone()
+    rc = load().mol_gated_scan(gate.data_ptr(), x.data_ptr(), _DTYPES[x.dtype], T, d, _at(offsets), B, _at(h0),
+                               out.data_ptr(), _DTYPES[out.dtype], last.data_ptr(), _at(ws), 0 if ws is None else ws.numel(),
+                               _now(x))
+    if rc:
+        _check(rc)
     return out, last
 
 
@@ -902,21 +966,24 @@ def gated_scan_grad(gate: torch.Tensor, x: torch.Tensor, h: torch.Tensor, dh: Op
     """Gradient of gated_scan, given its output h and the gradients dh [T][d] for h (of h's type) and dlast float32
     [B][d] for last (either may be None): (dgate, dx, dh0), of x's type and float32; dh0 is None without h0.
     Rows of no history have gradients of zero."""
-    T, d, B = _histories(gate, x, offsets, h0)
-    dev = x.device
-    _operand(h, "h", x.shape, _FLOATS, dev)
+    T, d = _tokens(gate, x)
+    B = _histories(x, d, offsets, h0)
+    _like(x, h, "h", _FLOATS)
     if dh is not None:
-        _operand(dh, "dh", x.shape, (h.dtype,), dev)
+        _like(x, dh, "dh", (h.dtype,))
     if dlast is not None:
-        _operand(dlast, "dlast", (B, d), _F32, dev)
-    with _on(dev, stream):
-        ws = _workspace(lambda: mol_gated_scan_workspace(T, d, B), ws, dev)
-        dgate, dx = torch.empty_like(x), torch.empty_like(x)
-        dh0 = None if h0 is None else torch.empty_like(h0)
-        _check(load().mol_gated_scan_grad(
-            gate.data_ptr(), x.data_ptr(), _DTYPES[x.dtype], h.data_ptr(), _at(dh), _DTYPES[h.dtype], T, d, _at(offsets), B,
-            _at(h0), _at(dlast), dgate.data_ptr(), dx.data_ptr(), _at(dh0), _at(ws), 0 if ws is None else ws.numel(),
-            _stream(stream)))
+        _operand(dlast, "dlast", (B, d), _F32, x.device)
+    if _elsewhere(x, stream):
+        with _on(x.device, stream):
+            return gated_scan_grad(gate, x, h, dh, offsets, h0, dlast, ws)
+    ws = _workspace(lambda: mol_gated_scan_workspace(T, d, B), ws, x.device)
+    dgate, dx = torch.empty_like(x), torch.empty_like(x)
+    dh0 = None if h0 is None else torch.empty_like(h0)
+    rc = load().mol_gated_scan_grad(
+        gate.data_ptr(), x.data_ptr(), _DTYPES[x.dtype], h.data_ptr(), _at(dh), _DTYPES[h.dtype], T, d, _at(offsets), B,
+        _at(h0), _at(dlast), dgate.data_ptr(), dx.data_ptr(), _at(dh0), _at(ws), 0 if ws is None else ws.numel(), _now(x))
+    if rc:
+        _check(rc)
     return dgate, dx, dh0
 
 
@@ -924,19 +991,20 @@ def gated_step(gate: torch.Tensor, x: torch.Tensor, state: torch.Tensor, new: Op
                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One more token of every history: gate, x [B][d] and the states float32 [B][d], which are updated in place (or
     written to ``new``).  Returns the new states in ``dtype`` (x's by default)."""
-    _need(isinstance(x, torch.Tensor) and x.dim() == 2, "x must be a tensor [B][d]")
-    dev, (B, d) = x.device, x.shape
-    _operand(x, "x", None, _FLOATS, dev)
-    _operand(gate, "gate", x.shape, (x.dtype,), dev)
-    _operand(state, "state", x.shape, _F32, dev)
-    if new is not None:
-        _operand(new, "new", x.shape, _F32, dev)
-    _sizes(B, d)
-    with _on(dev, stream):
-        out = _output(out, x, dtype)
-        _check(load().mol_gated_step(gate.data_ptr(), x.data_ptr(), _DTYPES[x.dtype], B, d, state.data_ptr(),
-                                     (state if new is None else new).data_ptr(), out.data_ptr(), _DTYPES[out.dtype],
-                                     _stream(stream)))
+    B, d = _tokens(gate, x)
+    _like(x, state, "state", _F32)
+    if new is None:
+        new = state
+    else:
+        _like(x, new, "new", _F32)
+    if _elsewhere(x, stream):
+        with _on(x.device, stream):
+            return gated_step(gate, x, state, new, dtype, out)
+    out = _output(out, x, dtype)
+    rc = load().mol_gated_step(gate.data_ptr(), x.data_ptr(), _DTYPES[x.dtype], B, d, state.data_ptr(), new.data_ptr(),
+                               out.data_ptr(), _DTYPES[out.dtype], _now(x))
+    if rc:
+        _check(rc)
     return out
 
 
