@@ -1017,8 +1017,7 @@ class Learner:
     masters; a_q [Vq][P], a_x [V][P]: the gating logits of every query and item;
     W1 [H][P], b1 [H], W2 [P][H], b2 [P]: the gating MLP, all float32 (they are
     updated in place).  weight_decay is for the embeddings and W1, W2.  The rows
-    are learned and served as they are: Eq. 2's L2 normalisation of the components is
-    not part of a step, so that it is a model of unnormalised dot products.
+    are learned and served as they are, a model of unnormalised dot products, unless ``normalize`` is given.
     states_8bit: AdamW states of the two embedding tables in 8 bits.  flags: the
     precision of the gating MLP in a step's scores (MOL_FLAG_*); float32 by default,
     since training moves its weights out of the range that the others are meant for
@@ -1027,8 +1026,15 @@ class Learner:
     gradients, whose chain has no such range; MOL_FLAG_F32_GATING keeps float32 up to
     their rounding to bf16 (see score_grad).
 
+    normalize: components, of queries and items, have length one in the scores (Eq. 2), in steps and in retrieval.
+    dropout: the chance by which a step drops each element of the rows that it reads (0: none).  gates [Vq][Pq][d]: a
+    query is a history of ids instead of one: their rows run through the gated recurrence of gated_scan, whose gates
+    are these rows, and the state behind the last is the query; its gating logits are the last id's.  norm: (gamma,
+    beta), float32 [Pq d] each: layer norm of the queries' rows or states.  All of these are learned as well.
+
     The copy of the items' table is laid out as a corpus: ``problem`` gives the
-    retrieval problem of the model as it is.
+    retrieval problem of the model as it is.  Of histories that go on, ``states`` keeps the state, ``advance``
+    takes one more event of each into it, and ``problem_of`` gives the problem of states.
 
     To save a learner: ``master``, ``state`` (m and v, and of 8-bit states
     m_scale and v_scale, by tensor) and ``steps``.  One made of the saved masters with
@@ -1036,7 +1042,8 @@ class Learner:
     """
 
     def __init__(self, queries, items, a_q, a_x, W1, b1, W2, b2, weight_decay: float = 0.0, states_8bit: bool = False,
-                 seed: int = 0, flags: int = MOL_FLAG_F32_GATING, grad_flags: int = 0):
+                 seed: int = 0, flags: int = MOL_FLAG_F32_GATING, grad_flags: int = 0, normalize: bool = False,
+                 dropout: float = 0.0, gates=None, norm=None):
         Vq, Pq, d = queries.shape
         Px, V, _ = items.shape
         P, dev = Pq * Px, queries.device
@@ -1045,7 +1052,19 @@ class Learner:
                                ("b1", b1, (H,)), ("W2", W2, (P, H)), ("b2", b2, (P,)), ("queries", queries, (Vq, Pq, d))):
             _operand(t, name, shape, (torch.float32,), dev)
         self.master = dict(queries=queries, items=items, a_q=a_q, a_x=a_x, W1=W1, b1=b1, W2=W2, b2=b2)
-        self.copy = {n: self.master[n].bfloat16() for n in ("queries", "items", "W1", "W2")}
+        if not 0 <= dropout <= 1 - 2.0 ** -16:
+            raise ValueError(f"dropout = {dropout} outside [0, 1 - 2^-16]")
+        if gates is not None:
+            _operand(gates, "gates", (Vq, Pq, d), (torch.float32,), dev)
+            self.master["gates"] = gates
+        if norm is not None:
+            _need(len(norm) == 2, "norm must be (gamma, beta)")
+            for name, t in zip(("gamma", "beta"), norm):
+                _operand(t, name, (Pq * d,), (torch.float32,), dev)
+                self.master[name] = t
+        self.normalize, self.dropout = bool(normalize), float(dropout)
+        decays = ("queries", "items", "W1", "W2")
+        self.copy = {n: self.master[n].bfloat16() for n in decays + ("gates",) if n in self.master}
         self.grad = {n: torch.empty_like(t, dtype=torch.bfloat16 if n in ("W1", "W2") else torch.float32)
                      for n, t in self.master.items()}
         eight = {n: states_8bit and n in ("queries", "items") for n in self.master}
@@ -1056,7 +1075,7 @@ class Learner:
         ms, vs = ([scale(n, t) for n, t in self.master.items()] for _ in range(2))
         self.tensors = AdamwTensors(
             list(self.master.values()), list(self.grad.values()), list(m.values()), list(v.values()), ms, vs,
-            weight_decay=[weight_decay if n in self.copy else 0.0 for n in self.master],
+            weight_decay=[weight_decay if n in decays else 0.0 for n in self.master],
             out=dict(copy=[self.copy.get(n) for n in self.master]))
         self.state = dict(m=m, v=v)
         if any(eight.values()):
@@ -1067,12 +1086,14 @@ class Learner:
         self.shape = (Vq, V, Pq, Px, P, d)
 
     def step(self, query_ids: torch.Tensor, item_ids: torch.Tensor, target: torch.Tensor, lr,
-             inv_temp: float = 20.0) -> torch.Tensor:
+             inv_temp: float = 20.0, offsets: Optional[torch.Tensor] = None) -> torch.Tensor:
         """One optimisation step on B queries and N sampled items: query_ids int32
         [B] (outside the table: a row of zeros, which adds to no gradient), item_ids
         int32 [N] (outside the table: an empty slot, no candidate), target int32 [B]:
         the column of each query's positive; lr: a number, or one float32 on the GPU
-        (which a captured step reads when it runs).  Returns the losses [B] from
+        (which a captured step reads when it runs).  With gates query_ids are the events
+        of all histories, [T], and offsets int32 [B + 1] says where each begins and ends (an
+        event outside the table leaves the state as it is).  Returns the losses [B] from
         before the step.  Allocates with torch and launches on the current stream
         only: it can be captured into a graph."""
         # (what AdamW and the loss would refuse, before anything is changed)
@@ -1082,35 +1103,132 @@ class Learner:
         elif not isinstance(lr, numbers.Real) or not 0 <= lr <= _F32_MAX:
             raise ValueError(f"lr = {lr!r} is not a rate: a number from 0 to {_F32_MAX:g}")
         _need(query_ids.numel() > 0 and item_ids.numel() > 0, "a step needs a query and an item")
+        self._check_offsets(offsets)
         with _on(self.steps.device, None):
-            return self._step(query_ids, item_ids, target, lr, inv_temp)
+            return self._step(query_ids, item_ids, target, lr, inv_temp, offsets)
 
-    def _step(self, query_ids, item_ids, target, lr, inv_temp) -> torch.Tensor:
+    def _check_offsets(self, offsets) -> None:
+        _need((offsets is not None) == ("gates" in self.master), "offsets go with gates")
+        if offsets is not None:
+            _need(isinstance(offsets, torch.Tensor) and offsets.dim() == 1 and offsets.numel() > 1,
+                  "offsets must be a tensor [B + 1]")
+            _operand(offsets, "offsets", offsets.shape, _INT32, self.steps.device)
+
+    def _drop(self, rows: torch.Tensor, of_items: bool) -> torch.Tensor:
+        """Dropout of a step's rows, and of their gradients: the mask is this step's, and the items' is their own."""
+        if not self.dropout:
+            return rows
+        return dropout(rows, self.dropout, self.seed, step=self.steps, offset=int(of_items) << 40)
+
+    def _gates(self, ids: torch.Tensor) -> torch.Tensor:
+        """The gates of events; one outside the table keeps the state."""
         Vq, V, Pq, Px, P, d = self.shape
-        B, N = query_ids.numel(), item_ids.numel()
+        g = embed_lookup(self.copy["gates"].view(1, Vq, Pq * d), ids).view(-1, Pq * d)
+        return g.masked_fill_(((ids < 0) | (ids >= Vq))[:, None], float("inf"))
+
+    def _components(self, v: torch.Tensor):
+        """(rows before normalize, Q [B][Pq][d]) of the queries' rows or states."""
+        Vq, V, Pq, Px, P, d = self.shape
+        M, B = self.master, v.shape[0]
+        last = None if self.normalize else torch.bfloat16
+        if "gamma" in M:
+            v = layer_norm(v, M["gamma"], M["beta"], dtype=torch.float32 if last is None else last)
+        elif last is not None:
+            v = v.to(last)
+        return v, (normalize(v.view(B, Pq, d), dtype=torch.bfloat16) if self.normalize else v.view(B, Pq, d))
+
+    def _step(self, query_ids, item_ids, target, lr, inv_temp, offsets) -> torch.Tensor:
+        Vq, V, Pq, Px, P, d = self.shape
+        T, N = query_ids.numel(), item_ids.numel()
         M, C, G = self.master, self.copy, self.grad
-        queries = C["queries"].view(1, Vq, Pq * d)
         item_ids = item_ids.masked_fill(item_ids >= V, -1)       # (the loss takes negative ids alone for empty slots)
-        tensors = (embed_lookup(queries, query_ids).view(B, Pq, d), embed_lookup(C["items"], item_ids),
-                   embed_lookup(M["a_q"].view(1, Vq, P), query_ids).view(B, P),
+        rows = self._drop(embed_lookup(C["queries"].view(1, Vq, Pq * d), query_ids).view(T, Pq * d), False)
+        if offsets is None:
+            v, of_query = rows, query_ids
+        else:
+            g = self._gates(query_ids)
+            ws = gated_scan_workspace(rows, offsets.numel() - 1)
+            h, v = gated_scan(g, rows, offsets, ws=ws)
+            of_query = self._last(query_ids, offsets)
+        B = v.shape[0]
+        u, Q = self._components(v)
+        x = self._drop(embed_lookup(C["items"], item_ids), True)
+        tensors = (Q, normalize(x) if self.normalize else x,
+                   embed_lookup(M["a_q"].view(1, Vq, P), of_query).view(B, P),
                    embed_lookup(M["a_x"].view(1, V, P), item_ids).view(N, P), C["W1"], M["b1"], C["W2"], M["b2"])
         phi = score(Problem(*tensors, flags=self.flags))
         weight = torch.full((B,), 1.0 / B, device=phi.device)
         loss, dphi = softmax_loss(phi, target, item_ids, inv_temp, weight, dphi=phi)
-        g = score_grad(Problem(*tensors, flags=self.grad_flags), dphi, out=dict(dW1=G["W1"], db1=G["b1"], dW2=G["W2"], db2=G["b2"]))
-        embed_grad(g["dQ"].view(1, B, Pq * d), query_ids, Vq, out=G["queries"].view(1, Vq, Pq * d))
-        embed_grad(g["dX"], item_ids, V, out=G["items"])
-        embed_grad(g["da_q"].view(1, B, P), query_ids, Vq, out=G["a_q"].view(1, Vq, P))
-        embed_grad(g["da_x"].view(1, N, P), item_ids, V, out=G["a_x"].view(1, V, P))
+        out = score_grad(Problem(*tensors, flags=self.grad_flags), dphi,
+                         out=dict(dW1=G["W1"], db1=G["b1"], dW2=G["W2"], db2=G["b2"]))
+        dq, dx = out["dQ"], out["dX"]
+        if self.normalize:
+            dq = normalize_grad(dq, u.view(B, Pq, d), dtype=torch.float32)
+            dx = normalize_grad(dx, x)
+        dq = dq.view(B, Pq * d)
+        if "gamma" in M:
+            dq, dgamma, dbeta = layer_norm_grad(dq, v, M["gamma"], dtype=torch.float32)
+            G["gamma"].copy_(dgamma)
+            G["beta"].copy_(dbeta)
+        if offsets is not None:
+            dg, dq, _ = gated_scan_grad(g, rows, h, offsets=offsets, dlast=dq.float(), ws=ws)
+            embed_grad(dg.view(1, T, Pq * d), query_ids, Vq, out=G["gates"].view(1, Vq, Pq * d))
+        embed_grad(self._drop(dq, False).view(1, T, Pq * d), query_ids, Vq, out=G["queries"].view(1, Vq, Pq * d))
+        embed_grad(self._drop(dx, True), item_ids, V, out=G["items"])
+        embed_grad(out["da_q"].view(1, B, P), of_query, Vq, out=G["a_q"].view(1, Vq, P))
+        embed_grad(out["da_x"].view(1, N, P), item_ids, V, out=G["a_x"].view(1, V, P))
         self.steps.add_(1)
         adamw_step(self.tensors, lr=lr, step=self.steps, seed=self.seed)
         return loss
 
-    def problem(self, query_ids: torch.Tensor, flags: int = 0) -> Problem:
-        """The retrieval problem of these queries against all items.  flags: 0 is
-        meant for gating weights of RMS up to 0.3 (see MOL_FLAG_*)."""
+    @staticmethod
+    def _last(ids: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:
+        """The last event of every history, -1 of none."""
+        if ids.numel() == 0:
+            return ids.new_full((offsets.numel() - 1,), -1)
+        some = offsets[1:] > offsets[:-1]
+        return torch.where(some, ids[(offsets[1:].long() - 1).clamp(min=0, max=ids.numel() - 1)], -1)
+
+    def states(self, query_ids: torch.Tensor, offsets: torch.Tensor, state: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The states float32 [B][Pq d] behind the events query_ids [T] of histories, which offsets int32 [B + 1] cuts
+        into, from ``state`` on (zeros by default)."""
+        self._check_offsets(offsets)
         Vq, V, Pq, Px, P, d = self.shape
-        B = query_ids.numel()
-        return Problem(embed_lookup(self.copy["queries"].view(1, Vq, Pq * d), query_ids).view(B, Pq, d), self.copy["items"],
-                       embed_lookup(self.master["a_q"].view(1, Vq, P), query_ids).view(B, P), self.master["a_x"],
-                       self.copy["W1"], self.master["b1"], self.copy["W2"], self.master["b2"], flags)
+        with _on(self.steps.device, None):
+            rows = embed_lookup(self.copy["queries"].view(1, Vq, Pq * d), query_ids).view(-1, Pq * d)
+            return gated_scan(self._gates(query_ids), rows, offsets, h0=state)[1]
+
+    def advance(self, state: torch.Tensor, ids: torch.Tensor) -> torch.Tensor:
+        """One more event of each of B histories, ids int32 [B], into their states [B][Pq d], in place."""
+        _need("gates" in self.master, "states go with gates")
+        Vq, V, Pq, Px, P, d = self.shape
+        with _on(self.steps.device, None):
+            rows = embed_lookup(self.copy["queries"].view(1, Vq, Pq * d), ids).view(-1, Pq * d)
+            gated_step(self._gates(ids), rows, state)
+        return state
+
+    def corpus(self) -> torch.Tensor:
+        """The items' rows as retrieval reads them [Px][V][d]: the model's copy, or with normalize one of length one."""
+        return normalize(self.copy["items"]) if self.normalize else self.copy["items"]
+
+    def problem_of(self, state: torch.Tensor, last_ids: torch.Tensor, flags: int = 0,
+                   corpus: Optional[torch.Tensor] = None) -> Problem:
+        """The retrieval problem of histories' states [B][Pq d] and last events [B] against all items.  corpus: what
+        ``corpus`` gave since the last step, to be spared another one."""
+        Vq, V, Pq, Px, P, d = self.shape
+        with _on(self.steps.device, None):
+            return Problem(self._components(state)[1], self.corpus() if corpus is None else corpus,
+                           embed_lookup(self.master["a_q"].view(1, Vq, P), last_ids).view(-1, P), self.master["a_x"],
+                           self.copy["W1"], self.master["b1"], self.copy["W2"], self.master["b2"], flags)
+
+    def problem(self, query_ids: torch.Tensor, flags: int = 0, offsets: Optional[torch.Tensor] = None,
+                corpus: Optional[torch.Tensor] = None) -> Problem:
+        """The retrieval problem of these queries (with gates: of the histories that offsets cuts them into) against all
+        items.  flags: 0 is meant for gating weights of RMS up to 0.3 (see MOL_FLAG_*).  corpus: see problem_of."""
+        self._check_offsets(offsets)
+        Vq, V, Pq, Px, P, d = self.shape
+        if offsets is not None:
+            return self.problem_of(self.states(query_ids, offsets), self._last(query_ids, offsets), flags, corpus)
+        with _on(self.steps.device, None):
+            rows = embed_lookup(self.copy["queries"].view(1, Vq, Pq * d), query_ids).view(-1, Pq * d)
+        return self.problem_of(rows, query_ids, flags, corpus)
