@@ -1423,7 +1423,7 @@ int mol_layer_norm_grad_workspace(int64_t T, int32_t d, size_t* bytes) {
   int rc;
   if ((rc = check_norm(T, d, 1.f, 1.f))) return rc;
   if (!bytes) return fail(MOL_EINVAL, "bytes is NULL");
-  *bytes = norm_grad_bytes(T, d);
+  *bytes = norm_grad_most(T, d);
   return MOL_OK;
 }
 

@@ -258,6 +258,7 @@ hipError_t launch_adamw(const mol_adamw& opt, const mol_adamw_tensor* tensors, i
 hipError_t launch_norm(int length, const void* x, int x_dtype, long T, int d, const float* gamma, const float* beta, float eps,
                        void* y, int y_dtype, hipStream_t st);
 size_t norm_grad_bytes(long T, int d);
+size_t norm_grad_most(long T, int d);      // of every call of no more rows and elements
 hipError_t launch_norm_grad(int length, const void* dy, int dy_dtype, const void* x, int x_dtype, long T, int d,
                             const float* gamma, float eps, void* dx, int dx_dtype, float* dgamma, float* dbeta, void* ws,
                             hipStream_t st);

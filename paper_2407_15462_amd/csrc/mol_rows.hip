@@ -524,6 +524,8 @@ size_t norm_grad_bytes(long T, int d) {
   const long blocks = row_blocks(row_plan(d), T, true);
   return blocks > 1 ? static_cast<size_t>(blocks) * 2 * d * sizeof(float) : 0;
 }
+// of every call of no more rows and elements (the widest rows have fewer workgroups)
+size_t norm_grad_most(long T, int d) { return std::max(norm_grad_bytes(T, d), norm_grad_bytes(T, std::min(d, 4096))); }
 
 hipError_t launch_norm(int length, const void* x, int x_dtype, long T, int d, const float* gamma, const float* beta, float eps,
                        void* y, int y_dtype, hipStream_t st) {

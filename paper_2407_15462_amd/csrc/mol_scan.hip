@@ -563,13 +563,13 @@ __global__ __launch_bounds__(256) void k_gated_step(StepArgs a) {
 
 namespace {
 
-// Tokens of a slice.  The more, the fewer waits, each of which costs a workgroup the latencies
-// of a store and a load that pass the caches: 24 in place of 32 took 230 us at 262,144 x 512 forward (219).
-// Beyond these registers run out, and slices side by side in a wave make chunks long enough.
-template <bool BACK, typename T, bool UNI>
-constexpr int slice_len() {
-  return !BACK && UNI && sizeof(T) == 2 ? 32 : 16;
-}
+// Tokens of a slice: 16, or 32 (as many as registers hold, forward in bfloat16) where that leaves
+// every CU a workgroup.  The longer, the fewer waits, each of which costs a workgroup the latencies of a store
+// and a load that pass the caches (262,144 x 512: 219 us, with 24 tokens 230; 20,000 x 512 32, with 16 33); the
+// shorter, the more workgroups (6400 x 256: 15 us a call, with 32 tokens 20).
+constexpr int kSlice = 16, kLongSlice = 32;
+constexpr long kManyUnits = 256;
+
 struct ScanShape {
   int lanes_log2, len, chunks, groups;
 };
@@ -594,9 +594,8 @@ long pair_words(const ScanShape& s, int d) {
 size_t shape_bytes(const ScanShape& s, int d) {
   return s.chunks <= 1 ? 0 : kScanAlign + up(s.chunks * sizeof(int2)) + pair_words(s, d) * sizeof(uint64_t);
 }
-template <bool BACK, typename T, typename TH, bool UNI>
-hipError_t run_scan_lanes(ScanArgs a, void* ws, hipStream_t st) {
-  constexpr int S = slice_len<BACK, T, UNI>();
+template <bool BACK, typename T, typename TH, bool UNI, int S>
+hipError_t run_scan_slices(ScanArgs a, void* ws, hipStream_t st) {
   const ScanShape s = scan_shape(a.T, a.d, S);
   a.chunks = s.chunks;
   a.groups = s.groups;
@@ -625,16 +624,22 @@ hipError_t run_scan_lanes(ScanArgs a, void* ws, hipStream_t st) {
 }
 template <bool BACK, typename T, typename TH>
 hipError_t run_scan(const ScanArgs& a, void* ws, hipStream_t st) {
-  return row_lanes_log2(a.d) == 6 ? run_scan_lanes<BACK, T, TH, true>(a, ws, st) : run_scan_lanes<BACK, T, TH, false>(a, ws, st);
+  if (row_lanes_log2(a.d) < 6) return run_scan_slices<BACK, T, TH, false, kSlice>(a, ws, st);
+  if constexpr (!BACK && sizeof(T) == 2) {
+    const ScanShape s = scan_shape(a.T, a.d, kLongSlice);
+    if (static_cast<long>(s.chunks) * s.groups >= kManyUnits)
+      return run_scan_slices<BACK, T, TH, true, kLongSlice>(a, ws, st);
+  }
+  return run_scan_slices<BACK, T, TH, true, kSlice>(a, ws, st);
 }
 
 }  // namespace
 
 size_t gated_scan_bytes(int T, int d) {
-  return shape_bytes(scan_shape(T, d, 16), d);                // (of the shortest slices)
+  return shape_bytes(scan_shape(T, d, kSlice), d);                // (of the shortest slices)
 }
 long gated_scan_blocks(int T, int d) {
-  const ScanShape s = scan_shape(T, d, 16);
+  const ScanShape s = scan_shape(T, d, kSlice);
   return static_cast<long>(s.chunks) * s.groups;
 }
 

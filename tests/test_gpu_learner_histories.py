@@ -100,6 +100,10 @@ def step64(learner, ids, inv_temp):
         Q = Q / Q.norm(dim=-1, keepdim=True).clamp(min=1e-12)
     kept.append(Q)
     Q = Rounded.apply(Q)
+    if "gamma" in w:                                     # a query without an event adds to no gradient of a query's
+        dead = ~inside if offsets is None else torch.tensor([not bool(inside[a:b].any()) for a, b in
+                                                             zip(offsets[:-1].tolist(), offsets[1:].tolist())])
+        Q = torch.where(dead[:, None, None], Q.detach(), Q)
     it = items.clamp(min=0)
     x = drop(w["items"][:, it] * (items >= 0)[None, :, None], 1 << 40)
     X = Rounded.apply(x / x.norm(dim=-1, keepdim=True).clamp(min=1e-12)) if learner.normalize else x
@@ -253,3 +257,22 @@ def test_refusals():
         mol.Learner(*(plain.master[n] for n in NAMES), gates=g[:, :3].contiguous())
     with pytest.raises(ValueError):
         mol.Learner(*(plain.master[n] for n in NAMES), norm=(g.view(-1)[:96], g.view(-1)[:95]))
+
+
+def test_a_history_without_events_moves_no_weights():
+    """Its state is zero, so that with beta = 0 its components have no length: neither it nor they reach gamma and beta."""
+    grads = []
+    for lens, events in (([3, 0, 5], None), ([3, 2, 5], -1)):
+        learner = make(20, 90, 4, 4, 24, 32, seed=1, **OPTIONS["all"])
+        learner.master["beta"].zero_()
+        learner.dropout = 0.0
+        ids = torch.arange(1, 11, dtype=torch.int32) % 7
+        offsets = torch.tensor([0, 3, 3 + lens[1], 8 + lens[1]], dtype=torch.int32)
+        ids = torch.cat([ids[:3], torch.full((lens[1],), -1, dtype=torch.int32), ids[3:8]])
+        _, items, target, _ = batch(learner, 8, 40, seed=4)
+        loss = learner.step(ids.cuda(), items.cuda(), target[:3].cuda(), 0.01, offsets=offsets.cuda())
+        assert torch.isfinite(loss).all()
+        for n in ("gamma", "beta", "queries", "gates"):
+            assert torch.isfinite(learner.grad[n]).all() and float(learner.grad[n].abs().max()) < 1e3, n
+        grads.append({n: learner.grad[n].clone() for n in learner.grad})
+    assert all(torch.equal(grads[0][n], grads[1][n]) for n in ("gamma", "beta", "queries", "gates", "items"))

@@ -105,6 +105,14 @@ def test_layer_norm_grad_over_many_rows():
     within(dgamma, (dy * xhat).sum(0), 160 * rh.U * xhat.abs().sum(0) + 60 * rh.U * T, "dgamma")
 
 
+def test_a_workspace_for_more_serves_fewer():
+    ws = mol.layer_norm_grad_workspace(torch.empty(6000, 8192, device="cuda"))
+    for T, d in ((6000, 4096), (5000, 4097), (6000, 30), (10, 8192)):
+        x, dy = rows(T, d, BF16), rows(T, d, BF16, seed=1)
+        ws.fill_(0x7F)
+        assert all(torch.equal(a, b) for a, b in zip(mol.layer_norm_grad(dy, x, ws=ws), mol.layer_norm_grad(dy, x)))
+
+
 def test_layer_norm_gradient_is_the_difference_quotient():
     T, d, h = 3, 21, 1e-3
     g = torch.Generator().manual_seed(8)
