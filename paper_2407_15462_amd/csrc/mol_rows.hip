@@ -10,9 +10,10 @@
 // Bound by memory: a row is read once into the registers of a team of lanes
 // (both rows of a gradient), its statistics are formed there (variance about the mean,
 // float32; a gradient forms them again from x rather than reading them), and it is
-// written once.  Measured: layer norm of 262,144 x 512 bf16 99 us (5.4 TB/s, where a copy of as
-// much runs at 5.0), its gradient 158 + 5 (4.9); 172M float32 elements to bf16 rows of 32 of
-// length 1 174 us (6.0).  Where rows are few, their chains of loads and sums: 32 rows of 1024 take
+// written once.  Measured: layer norm of 262,144 x 512 bf16 93 to 100 us (5.4 TB/s, where a copy of
+// as much runs at 5.0), its gradient 141 + 5 (5.5; through the caches 158 + 5); 172M float32 elements to bf16 rows
+// of 32 of length 1 172 us (6.0).  Reading past the caches gains in gradients of large tensors only (streams();
+// forwards it took 134 us for 100).  Where rows are few, their chains of loads and sums: 32 rows of 1024 take
 // 3.5 us, the gradient of 4099 float32 rows of 777 14 + 4 (7 at the rate of large ones).
 #include <algorithm>
 #include <cfloat>
@@ -44,6 +45,7 @@ struct RowArgs {
   float* dgamma;           // [2][d] of the workgroup, or of the call; NULL: not wanted
   float* dbeta;
   long part;               // floats from one workgroup's to the next
+  bool once;               // gradients, teams of lanes: read past the caches
 };
 
 template <int TEAM>
@@ -163,7 +165,7 @@ struct Stats {
 
 // A row as it lies: runs that pass its end are read from where they would end with it
 // (settle() puts that right), so that every lane loads whole runs and nothing branches.
-template <typename T, int E, int VE>
+template <bool ONCE = false, typename T, int E, int VE>
 __device__ __forceinline__ void load_row(Raw<T, VE> (&r)[E / VE], const T* p, const Place<E, VE>& at, bool whole) {
   if (!whole && at.d < VE) {                           // (rows shorter than a run)
 #pragma unroll
@@ -171,7 +173,7 @@ __device__ __forceinline__ void load_row(Raw<T, VE> (&r)[E / VE], const T* p, co
     return;
   }
 #pragma unroll
-  for (int g = 0; g < E / VE; ++g) r[g].load(p + (whole ? at.col[g] : min(at.col[g], at.d - VE)));
+  for (int g = 0; g < E / VE; ++g) r[g].template load<ONCE>(p + (whole ? at.col[g] : min(at.col[g], at.d - VE)));
 }
 // what was read for elements behind the row's end becomes 0, the last run's elements move to their places
 template <typename T, int E, int VE>
@@ -282,7 +284,7 @@ __global__ __launch_bounds__(threads<TEAM>()) void k_norm(RowArgs a) {
 
 // The weights' gradients are summed over a lane's rows in registers, over the
 // workgroup's teams at the end, and over workgroups by a launch of sums.
-template <int MODE, typename T, typename TG, int TEAM, int E, bool WHOLE>
+template <int MODE, typename T, typename TG, int TEAM, int E, bool WHOLE, bool ONCE>
 __global__ __launch_bounds__(threads<TEAM>()) void k_norm_grad(RowArgs a) {
   constexpr int VE = sizeof(T) == 2 && sizeof(TG) == 2 ? 8 : 4;
   extern __shared__ float dyn[];             // [4][2][d] where teams are joined
@@ -306,8 +308,8 @@ __global__ __launch_bounds__(threads<TEAM>()) void k_norm_grad(RowArgs a) {
   Raw<TG, VE> graw[E / VE], gnext[E / VE];
   auto fetch = [&](Raw<T, VE>(&r)[E / VE], Raw<TG, VE>(&g)[E / VE], long row) {
     const long at_row = min(row + mine, a.T - 1) * a.d;
-    load_row(r, x + at_row, at, WHOLE);
-    load_row(g, dy + at_row, at, WHOLE);
+    load_row<ONCE>(r, x + at_row, at, WHOLE);
+    load_row<ONCE>(g, dy + at_row, at, WHOLE);
   };
   if (kAhead) fetch(raw, graw, first);
   for (long row = first; row < a.T; row += step) {
@@ -453,7 +455,7 @@ bool row_whole(const RowPlan& p, int d) { return d == p.lanes * p.E; }
 // a grid that stays drifts apart in memory (172M elements in rows of 32 to unit length: 174 us,
 // with 2048 workgroups that stay 206; wide rows, which read as much of gamma and beta, stay).
 // With them, whose parts each writes and a launch of sums reads, about as many as run at once,
-// of two rows a team at least (512 in place of 1024 took 179 us at 262,144 x 512, for 163).
+// of two rows a team at least (512 in place of 1024 took 179 us at 262,144 x 512 through the caches, for 163).
 long row_blocks(const RowPlan& p, long T, bool weights) {
   const long rows = weights ? 2 * p.rows : p.rows, want = (T + rows - 1) / rows;
   if (p.team == 1024) return std::min(want, weights ? 256l : 512l);
@@ -489,10 +491,14 @@ hipError_t launch_norm_mode(RowArgs& a, hipStream_t st) {
 template <int MODE, typename T, typename TG, int TEAM, int E>
 void run_norm_grad(const RowArgs& a, long blocks, bool whole, hipStream_t st) {
   const size_t lds = TEAM == 0 && MODE == kLayer && a.dgamma ? 8 * a.d * sizeof(float) : 0;
-  if (whole)
-    hipLaunchKernelGGL((k_norm_grad<MODE, T, TG, TEAM, E, true>), dim3(blocks), dim3(threads<TEAM>()), lds, st, a);
-  else
-    hipLaunchKernelGGL((k_norm_grad<MODE, T, TG, TEAM, E, false>), dim3(blocks), dim3(threads<TEAM>()), lds, st, a);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads<TEAM>()), lds, st, a); };
+  if constexpr (TEAM == 0) {
+    if (a.once) {
+      whole ? go(k_norm_grad<MODE, T, TG, TEAM, E, true, true>) : go(k_norm_grad<MODE, T, TG, TEAM, E, false, true>);
+      return;
+    }
+  }
+  whole ? go(k_norm_grad<MODE, T, TG, TEAM, E, true, false>) : go(k_norm_grad<MODE, T, TG, TEAM, E, false, false>);
 }
 template <int MODE, typename T, typename TG>
 hipError_t launch_norm_grad_mode(RowArgs& a, float* dgamma, float* dbeta, float* ws, hipStream_t st) {
@@ -555,6 +561,7 @@ hipError_t launch_norm_grad(int length, const void* dy, int dy_dtype, const void
   a.gamma = gamma;
   a.y = dx;
   a.y_bf16 = dx_dtype == MOL_BF16;
+  a.once = vec::streams(static_cast<size_t>(T) * d * ((x_dtype == MOL_BF16 ? 2 : 4) + (dy_dtype == MOL_BF16 ? 2 : 4)));
   float* w = static_cast<float*>(ws);
   auto types = [&](auto t, auto tg) {
     using T_ = decltype(t);

@@ -25,13 +25,14 @@
 // publishes needs nothing but what those before it publish.  A published pair is one
 // 64-bit word, whose top bit (the sign of A, which is not negative) says that it is there.
 //
-// Measured, bf16: 1024 histories of 262,144 tokens of 512 channels 219 us (3.7 TB/s; 184 to 202
-// without the waits), back 319 (5.0 TB/s, what a copy of as much reaches); one history of
-// 131,072 x 1024 230.  What bounds it: back, memory; forward, the waits and, at more than half
-// of the vector rate, two gates an element (27 instructions).  Tried and slower forward: every token's A and H kept
-// in place of the second run (half as many tokens a slice: 225 to 231 us), workgroups that stay and load their
-// next chunk ahead (226 to 311: a wait is then for workgroups at another place of their turn), a ninth wave for
-// the waits, tickets of their own for every 128 channels (238: neighbours in memory drift apart in time).
+// Measured, bf16: 1024 histories of 262,144 tokens of 512 channels 205 to 209 us (3.9 TB/s), back 309 (5.2
+// TB/s, where a copy of as much reaches 5.0); one history of 131,072 x 1024 208, back (x 512) 180.  Inputs of
+// 256 MB and more are read and written past the caches (through them 217, 318, 225 and 182).  What bounds it: back,
+// memory; forward, the waits (27 to 45 us in a build without them) and, at more than half of the vector rate, two
+// gates an element (27 instructions).  Tried and slower forward: every token's A and H kept in place of the second
+// run (half as many tokens a slice: 225 to 231 where this took 219), workgroups that stay and load their next chunk
+// ahead (226 to 311: a wait is then for workgroups at another place of their turn), a ninth wave for the waits,
+// tickets of their own for every 128 channels (238: neighbours in memory drift apart in time).
 #include <algorithm>
 #include <type_traits>
 
@@ -73,6 +74,7 @@ struct ScanArgs {
   uint64_t* group_pairs;   // [chunks / kGroup][d]
   uint64_t* states;        // [chunks / kSuper][d] (0, state)
   long words;              // of the three together
+  bool once;               // rows are read past the caches
 };
 
 __device__ __forceinline__ int offset_at(const ScanArgs& a, int i) {
@@ -113,12 +115,12 @@ __device__ __forceinline__ float a_of(uint64_t v) { return __uint_as_float(stati
 __device__ __forceinline__ float h_of(uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v)); }
 
 // two channels, or the one that there is
-template <bool EVEN, typename T>
+template <bool EVEN, bool ONCE, typename T>
 __device__ __forceinline__ void put(T* p, const float (&v)[2], int n) {
   if (EVEN)
-    vec::store(p, v);
+    vec::store<ONCE>(p, v);
   else
-    vec::store(p, v, n);
+    vec::store<ONCE>(p, v, n);
 }
 
 // First history that has tokens at t or behind: the number of ends offsets[1 .. B] up to t,
@@ -184,8 +186,8 @@ __global__ __launch_bounds__(256) void k_scan_plan(ScanArgs a, int chunk_len) {
 
 // UNI: a wave's lanes share their slice (more than 64 channels), so that what depends on
 // the token alone is a scalar.  EVEN: an even number of channels, so that lanes
-// without channels of their own can read others'.
-template <bool BACK, typename T, typename TH, int S, bool UNI, bool EVEN>
+// without channels of their own can read others'.  ONCE: rows are read and written past the caches.
+template <bool BACK, typename T, typename TH, int S, bool UNI, bool EVEN, bool ONCE>
 __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
   constexpr int kMost = kWaves * S * (UNI ? 1 : 16);            // tokens of a chunk (4 lanes a row at least)
   constexpr int kBlock = BACK ? 8 : S;                         // tokens whose x and h are in flight together on the way out
@@ -224,9 +226,9 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
   };
   auto load = [&](auto& r, const auto* base, int t, uint32_t from_ch) {
     if (EVEN)
-      r.load(row_at(base, t, from_ch));
+      r.template load<ONCE>(row_at(base, t, from_ch));
     else
-      r.load(row_at(base, t, from_ch), d - static_cast<int>(from_ch));
+      r.template load<ONCE>(row_at(base, t, from_ch), d - static_cast<int>(from_ch));
   };
   const int t_first = BACK ? first - slice * S : first + slice * S;
   auto token = [&](int s) { return BACK ? t_first - s : t_first + s; };
@@ -490,10 +492,10 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
             for (int e = 0; e < 2; ++e) state[e] = fmaf(f[e], state[e], rest[e] * xr[s].at(e));
             if ((marked && !live(s)) || nch <= 0) continue;
             if (a.h_bf16)
-              put<EVEN>(row_at(static_cast<bf16_t*>(a.h), token(s), from_ch), state, nch);
+              put<EVEN, ONCE>(row_at(static_cast<bf16_t*>(a.h), token(s), from_ch), state, nch);
             else
-              put<EVEN>(row_at(static_cast<float*>(a.h), token(s), from_ch), state, nch);
-            if (stops && a.last) put<EVEN>(row_at(a.last, end_b[slice * S + s], from_ch), state, nch);
+              put<EVEN, ONCE>(row_at(static_cast<float*>(a.h), token(s), from_ch), state, nch);
+            if (stops && a.last) put<EVEN, false>(row_at(a.last, end_b[slice * S + s], from_ch), state, nch);
           } else {
             float prev[2] = {hr[i].at(0), hr[i].at(1)}, dg[2], dx[2];
             const int b = stops ? end_b[slice * S + s] : 0;
@@ -512,9 +514,9 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
             }
             if ((marked && token(s) < 0) || nch <= 0) continue;
             if (marked && !live(s)) dg[0] = dg[1] = dx[0] = dx[1] = 0.f;   // rows of no history: no loss depends on them
-            put<EVEN>(row_at(static_cast<T*>(a.dgate), token(s), from_ch), dg, nch);
-            put<EVEN>(row_at(static_cast<T*>(a.dx), token(s), from_ch), dx, nch);
-            if (stops && a.dh0) put<EVEN>(row_at(a.dh0, b, from_ch), state, nch);
+            put<EVEN, ONCE>(row_at(static_cast<T*>(a.dgate), token(s), from_ch), dg, nch);
+            put<EVEN, ONCE>(row_at(static_cast<T*>(a.dx), token(s), from_ch), dx, nch);
+            if (stops && a.dh0) put<EVEN, false>(row_at(a.dh0, b, from_ch), state, nch);
           }
         }
       }
@@ -565,7 +567,7 @@ namespace {
 
 // Tokens of a slice: 16, or 32 (as many as registers hold, forward in bfloat16) where that leaves
 // every CU a workgroup.  The longer, the fewer waits, each of which costs a workgroup the latencies of a store
-// and a load that pass the caches (262,144 x 512: 219 us, with 24 tokens 230; 20,000 x 512 32, with 16 33); the
+// and a load that pass the caches (262,144 x 512 through the caches: 219 us, with 24 tokens 230; 20,000 x 512 32, with 16 33); the
 // shorter, the more workgroups (6400 x 256: 15 us a call, with 32 tokens 20).
 constexpr int kSlice = 16, kLongSlice = 32;
 constexpr long kManyUnits = 256;
@@ -616,10 +618,14 @@ hipError_t run_scan_slices(ScanArgs a, void* ws, hipStream_t st) {
     hipLaunchKernelGGL((k_scan_plan<BACK>), dim3(static_cast<unsigned>(std::min(want + 1, 1024l))), dim3(256), 0, st, a, s.len);
   }
   const unsigned grid = static_cast<unsigned>(s.chunks) * s.groups;
-  if (a.d % 2 == 0)
-    hipLaunchKernelGGL((k_scan<BACK, T, TH, S, UNI, true>), dim3(grid), dim3(kThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL((k_scan<BACK, T, TH, S, UNI, false>), dim3(grid), dim3(kThreads), 0, st, a);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, st, a); };
+  if (a.d % 2) {
+    go(k_scan<BACK, T, TH, S, UNI, false, false>);
+  } else if constexpr (UNI) {
+    a.once ? go(k_scan<BACK, T, TH, S, UNI, true, true>) : go(k_scan<BACK, T, TH, S, UNI, true, false>);
+  } else {
+    go(k_scan<BACK, T, TH, S, UNI, true, false>);
+  }
   return hipGetLastError();
 }
 template <bool BACK, typename T, typename TH>
@@ -656,6 +662,7 @@ hipError_t launch_gated_scan(const void* gate, const void* x, int x_dtype, int T
   a.h = h;
   a.h_bf16 = h_dtype == MOL_BF16;
   a.last = last;
+  a.once = vec::streams(static_cast<size_t>(T) * d * (x_dtype == MOL_BF16 ? 4 : 8));
   return x_dtype == MOL_BF16 ? run_scan<false, bf16_t, bf16_t>(a, ws, st) : run_scan<false, float, float>(a, ws, st);
 }
 
@@ -676,6 +683,7 @@ hipError_t launch_gated_scan_grad(const void* gate, const void* x, int x_dtype, 
   a.dgate = dgate;
   a.dx = dx;
   a.dh0 = dh0;
+  a.once = vec::streams(static_cast<size_t>(T) * d * ((x_dtype == MOL_BF16 ? 4 : 8) + (h_dtype == MOL_BF16 ? 2 : 4) * (dh ? 2 : 1)));
   if (x_dtype == MOL_BF16)
     return h_dtype == MOL_BF16 ? run_scan<true, bf16_t, bf16_t>(a, ws, st) : run_scan<true, bf16_t, float>(a, ws, st);
   return h_dtype == MOL_BF16 ? run_scan<true, float, bf16_t>(a, ws, st) : run_scan<true, float, float>(a, ws, st);

@@ -34,6 +34,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
 }
 
+// Whether a call's inputs are to be read past the caches: if they are more than the last-level
+// cache's 256 MB.  Measured: dropout of 134M bfloat16 elements with residual (512 MB read) 117 us, 137
+// through the caches; of 30M float32 ones (114 MB) 46, and 36 through the caches, which hold them.
+inline bool streams(size_t bytes) { return bytes >= 256ul << 20; }
+
 // N elements as they lie in memory.
 template <typename T, int N>
 struct Raw {
@@ -49,12 +54,18 @@ struct Raw {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = 0;
   }
-  // all N
+  // all N; ONCE: past the caches, for tensors that they do not hold (see streams())
+  template <bool ONCE = false>
   __device__ __forceinline__ void load(const T* p) {
     constexpr int kStep = kWords < 4 ? kWords : 4;
 #pragma unroll
     for (int i = 0; i < kWords; i += kStep) {
-      const auto v = *reinterpret_cast<const typename Mem<kStep * 4, sizeof(T)>::type*>(p + i * 4 / sizeof(T));
+      const auto* at = reinterpret_cast<const typename Mem<kStep * 4, sizeof(T)>::type*>(p + i * 4 / sizeof(T));
+      typename Mem<kStep * 4, sizeof(T)>::type v;
+      if constexpr (ONCE)
+        v = __builtin_nontemporal_load(at);
+      else
+        v = *at;
       if constexpr (kStep == 1)
         w[i] = v;
       else
@@ -63,8 +74,9 @@ struct Raw {
     }
   }
   // the first n (none for n <= 0), zeros behind them
+  template <bool ONCE = false>
   __device__ __forceinline__ void load(const T* p, int n) {
-    if (n >= N) return load(p);
+    if (n >= N) return load<ONCE>(p);
     zero();
 #pragma unroll
     for (int e = 0; e < N; ++e)
@@ -78,7 +90,7 @@ struct Raw {
 };
 
 // N values to memory, each rounded once: all, or the first n
-template <typename T, int N>
+template <bool ONCE = false, typename T, int N>
 __device__ __forceinline__ void store(T* p, const float (&v)[N]) {
   constexpr int kWords = Raw<T, N>::kWords, kStep = kWords < 4 ? kWords : 4;
   uint32_t w[kWords];
@@ -97,12 +109,16 @@ __device__ __forceinline__ void store(T* p, const float (&v)[N]) {
     else
 #pragma unroll
       for (int j = 0; j < kStep; ++j) x[j] = w[i + j];
-    *reinterpret_cast<typename Mem<kStep * 4, sizeof(T)>::type*>(p + i * 4 / sizeof(T)) = x;
+    auto* to = reinterpret_cast<typename Mem<kStep * 4, sizeof(T)>::type*>(p + i * 4 / sizeof(T));
+    if constexpr (ONCE)
+      __builtin_nontemporal_store(x, to);
+    else
+      *to = x;
   }
 }
-template <typename T, int N>
+template <bool ONCE = false, typename T, int N>
 __device__ __forceinline__ void store(T* p, const float (&v)[N], int n) {
-  if (n >= N) return store(p, v);
+  if (n >= N) return store<ONCE>(p, v);
 #pragma unroll
   for (int e = 0; e < N; ++e)
     if (e < n) {
