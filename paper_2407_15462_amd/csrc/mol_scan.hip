@@ -215,44 +215,38 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
   const int sub = UNI ? 0 : lane >> a.lanes_log2;              // which slice of the wave's
   const int slice = wave * per_wave + sub;
   const int row_lane = UNI ? lane : lane & (lanes - 1);
+  const int ch = cg * 128 + 2 * row_lane, nch = d - ch;        // this lane's channels: 2 or 1 (or none)
+  const uint32_t from_ch = min(ch, EVEN ? d - 2 : d - 1);      // where it reads
   Raw<T, 2> gate[S];
   Raw<T, 2> xr[BACK ? 1 : S];
   Raw<TH, 2> dr[BACK ? S : 1];
-  auto row_at = [&](auto* base, int row, uint32_t from_ch) {   // a lane's channels of a row
+  auto row_at = [&](auto* base, int row) {                     // this lane's channels of a row
     typedef std::remove_reference_t<decltype(*base)> E;
     typedef std::conditional_t<std::is_const_v<E>, const char, char> Byte;
     return reinterpret_cast<E*>(reinterpret_cast<Byte*>(base + static_cast<int64_t>(row) * d) +
                                 from_ch * static_cast<uint32_t>(sizeof(E)));
   };
-  auto load = [&](auto& r, const auto* base, int t, uint32_t from_ch) {
+  auto load = [&](auto& r, const auto* base, int t) {
     if (EVEN)
-      r.template load<ONCE>(row_at(base, t, from_ch));
+      r.template load<ONCE>(row_at(base, t));
     else
-      r.template load<ONCE>(row_at(base, t, from_ch), d - static_cast<int>(from_ch));
+      r.template load<ONCE>(row_at(base, t), d - static_cast<int>(from_ch));
   };
   const int t_first = BACK ? first - slice * S : first + slice * S;
   auto token = [&](int s) { return BACK ? t_first - s : t_first + s; };
-  auto from_of = [&](int cg) { return static_cast<uint32_t>(min(cg * 128 + 2 * row_lane, EVEN ? d - 2 : d - 1)); };
   // Rows that are no history's are read as well (and past the tensor's ends others
   // in their place): what comes of them is not written, and the next history begins anew.
-  auto fetch = [&](int cg) {
-    const uint32_t from_ch = from_of(cg);
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const int t = min(max(token(s), 0), a.T - 1);
-      load(gate[s], static_cast<const T*>(a.gate), t, from_ch);
-      if constexpr (BACK) {
-        if (a.dh) load(dr[s], static_cast<const TH*>(a.dh), t, from_ch);
-      } else {
-        load(xr[s], static_cast<const T*>(a.x), t, from_ch);
-      }
+  for (int s = 0; s < S; ++s) {
+    const int t = min(max(token(s), 0), a.T - 1);
+    load(gate[s], static_cast<const T*>(a.gate), t);
+    if constexpr (BACK) {
+      dr[s].zero();
+      if (a.dh) load(dr[s], static_cast<const TH*>(a.dh), t);
+    } else {
+      load(xr[s], static_cast<const T*>(a.x), t);
     }
-  };
-  if constexpr (BACK)
-#pragma unroll
-    for (int s = 0; s < S; ++s) dr[s].zero();
-
-  fetch(cg);
+  }
   const int live_lo = __builtin_amdgcn_readfirstlane(max(lo, offset_at(a, 0)));
   const int live_hi = __builtin_amdgcn_readfirstlane(min(hi, offset_at(a, a.B)));
   auto live = [&](int s) { return token(s) >= live_lo && token(s) < live_hi; };
@@ -293,239 +287,234 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
   __syncthreads();
   uint32_t begin = begins[slice], end = ends[slice];
   if (UNI) begin = __builtin_amdgcn_readfirstlane(begin), end = __builtin_amdgcn_readfirstlane(end);
-  {
-    const int ch = cg * 128 + 2 * row_lane, nch = d - ch;      // this lane's channels: 2 or 1 (or none)
-    const uint32_t from_ch = from_of(cg);
-
-    // the state (back: E) that a history begins with at token s of the slice
-    auto start = [&](int s, float (&v)[2]) {
-      const float* in = BACK ? a.dlast : a.h0;
-      const long at = static_cast<long>(begin_b[slice * S + s]) * d + ch;
+  // the state (back: E) that a history begins with at token s of the slice
+  auto start = [&](int s, float (&v)[2]) {
+    const float* in = BACK ? a.dlast : a.h0;
+    const long at = static_cast<long>(begin_b[slice * S + s]) * d + ch;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      v[e] = in && e < nch ? in[at + e] : 0.f;
+      asm volatile("" : "+v"(v[e]));                         // (waited for here, not by tokens without a beginning)
+    }
+  };
+  // the slice from state 0
+  float A[2] = {1.f, 1.f}, H[2] = {0.f, 0.f};
+  auto run = [&](auto marked) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      if (marked && (begin >> s & 1)) {
+        A[0] = A[1] = 0.f;
+        start(s, H);
+      }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        v[e] = in && e < nch ? in[at + e] : 0.f;
-        asm volatile("" : "+v"(v[e]));                         // (waited for here, not by tokens without a beginning)
+        float f, rest;
+        gates_of<T>(gate[s].at(e), f, rest);
+        A[e] *= f;
+        if constexpr (BACK)
+          H[e] = f * (dr[s].at(e) + H[e]);
+        else
+          H[e] = fmaf(f, H[e], rest * xr[s].at(e));
       }
-    };
-    // the slice from state 0
-    float A[2] = {1.f, 1.f}, H[2] = {0.f, 0.f};
-    auto run = [&](auto marked) {
+    }
+  };
+  // (slices in which no history begins, nearly all, have a form without the tests)
+  if (__any(begin))
+    run(std::true_type{});
+  else
+    run(std::false_type{});
+  // What follows forms the gates again, from the rows as they lie in registers: half as many as
+  // every token's A and H would take, so that a slice can be twice as long.
 #pragma unroll
-      for (int s = 0; s < S; ++s) {
-        if (marked && (begin >> s & 1)) {
-          A[0] = A[1] = 0.f;
-          start(s, H);
-        }
+  for (int s = 0; s < S; ++s)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float f, rest;
-          gates_of<T>(gate[s].at(e), f, rest);
-          A[e] *= f;
-          if constexpr (BACK)
-            H[e] = f * (dr[s].at(e) + H[e]);
-          else
-            H[e] = fmaf(f, H[e], rest * xr[s].at(e));
-        }
-      }
-    };
-    // (slices in which no history begins, nearly all, have a form without the tests)
-    if (__any(begin))
-      run(std::true_type{});
-    else
-      run(std::false_type{});
-    // What follows forms the gates again, from the rows as they lie in registers: half as many as
-    // every token's A and H would take, so that a slice can be twice as long.
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-      for (int i = 0; i < Raw<T, 2>::kWords; ++i) asm volatile("" : "+v"(gate[s].w[i]));
+    for (int i = 0; i < Raw<T, 2>::kWords; ++i) asm volatile("" : "+v"(gate[s].w[i]));
 
-    // slices joined: (A, H) of the wave's slices before this one, and of the wave
-    float before_a[2] = {1.f, 1.f}, before_h[2] = {0.f, 0.f};
+  // slices joined: (A, H) of the wave's slices before this one, and of the wave
+  float before_a[2] = {1.f, 1.f}, before_h[2] = {0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float ca = A[e], chh = H[e];                             // inclusive over slices of the wave
-      if (!UNI) {
-        for (int o = lanes; o < 64; o <<= 1) {
-          const float ua = __shfl_up(ca, o), uh = __shfl_up(chh, o);
-          if (lane >= o) {
-            chh += through(ca, uh);
-            ca = through(ca, ua);
-          }
+  for (int e = 0; e < 2; ++e) {
+    float ca = A[e], chh = H[e];                             // inclusive over slices of the wave
+    if (!UNI) {
+      for (int o = lanes; o < 64; o <<= 1) {
+        const float ua = __shfl_up(ca, o), uh = __shfl_up(chh, o);
+        if (lane >= o) {
+          chh += through(ca, uh);
+          ca = through(ca, ua);
         }
-        const float ua = __shfl_up(ca, lanes), uh = __shfl_up(chh, lanes);
-        if (sub) before_a[e] = ua, before_h[e] = uh;
       }
-      if (sub == per_wave - 1) {
-        sum_a[wave][2 * row_lane + e] = ca;
-        sum_h[wave][2 * row_lane + e] = chh;
-      }
+      const float ua = __shfl_up(ca, lanes), uh = __shfl_up(chh, lanes);
+      if (sub) before_a[e] = ua, before_h[e] = uh;
     }
-    __syncthreads();                                           // sums
-    float pre_a[2], pre_h[2], all_a[2], all_h[2];              // of the waves before, and with this one (the last: of all)
+    if (sub == per_wave - 1) {
+      sum_a[wave][2 * row_lane + e] = ca;
+      sum_h[wave][2 * row_lane + e] = chh;
+    }
+  }
+  __syncthreads();                                           // sums
+  float pre_a[2], pre_h[2], all_a[2], all_h[2];              // of the waves before, and with this one (the last: of all)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      pre_a[e] = 1.f, pre_h[e] = 0.f;
-      for (int v = 0; v < wave; ++v) {
-        const float wa = sum_a[v][2 * row_lane + e], wh = sum_h[v][2 * row_lane + e];
-        pre_h[e] = wh + through(wa, pre_h[e]);
-        pre_a[e] = through(wa, pre_a[e]);
-      }
-      const float wa = sum_a[wave][2 * row_lane + e], wh = sum_h[wave][2 * row_lane + e];
-      all_h[e] = wh + through(wa, pre_h[e]);
-      all_a[e] = through(wa, pre_a[e]);
+  for (int e = 0; e < 2; ++e) {
+    pre_a[e] = 1.f, pre_h[e] = 0.f;
+    for (int v = 0; v < wave; ++v) {
+      const float wa = sum_a[v][2 * row_lane + e], wh = sum_h[v][2 * row_lane + e];
+      pre_h[e] = wh + through(wa, pre_h[e]);
+      pre_a[e] = through(wa, pre_a[e]);
     }
-    const bool speaks = a.chunks > 1 && wave == kWaves - 1 && sub == 0;
-    if (speaks)
+    const float wa = sum_a[wave][2 * row_lane + e], wh = sum_h[wave][2 * row_lane + e];
+    all_h[e] = wh + through(wa, pre_h[e]);
+    all_a[e] = through(wa, pre_a[e]);
+  }
+  const bool speaks = a.chunks > 1 && wave == kWaves - 1 && sub == 0;
+  if (speaks)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (e < nch) publish(a.pairs + static_cast<long>(chunk) * d + ch + e, all_a[e], all_h[e]);
+  // the state that comes in: each wave gets a pair of the group's chunks, then one of the super's groups
+  float state[2] = {0.f, 0.f};
+  // (A, H) of the pairs i0 .. i1 - 1, pair j0 + v by wave v, joined
+  auto gather = [&](const uint64_t* base, int i0, int i1, int j0, float (&fa)[2], float (&fh)[2]) {
+    if (j0 + wave >= i0 && j0 + wave < i1 && sub == 0) {
+      const uint64_t* at = base + static_cast<long>(j0 + wave) * d + ch;
+      uint64_t got[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) got[e] = e < nch ? look(at + e) : ~0ull;
+      while (__any(!there(got[0]) || !there(got[1]))) {
+        // (the channels' words were written together: until the first is there, only it is looked for)
+        for (;;) {
+          bool yes = true;
+          if (row_lane == 0) yes = there(got[0] = look(at));
+          if (__all(yes)) break;
+          __builtin_amdgcn_s_sleep(4);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (!there(got[e])) got[e] = look(at + e);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        in_a[wave][2 * row_lane + e] = a_of(got[e]);
+        in_h[wave][2 * row_lane + e] = h_of(got[e]);
+      }
+    }
+    __syncthreads();
+    for (int i = i0; i < i1; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float wa = in_a[i - j0][2 * row_lane + e];
+        fh[e] = in_h[i - j0][2 * row_lane + e] + through(wa, fh[e]);
+        fa[e] = through(wa, fa[e]);
+      }
+    __syncthreads();
+  };
+  if (a.chunks > 1) {
+    float ga[2] = {1.f, 1.f}, gh[2] = {0.f, 0.f};
+    if (from1 < chunk) gather(a.pairs, from1, chunk, group0, ga, gh);
+    if (speaks && chunk % kGroup == kGroup - 1)
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        if (e < nch) publish(a.pairs + static_cast<long>(chunk) * d + ch + e, all_a[e], all_h[e]);
-    // the state that comes in: each wave gets a pair of the group's chunks, then one of the super's groups
-    float state[2] = {0.f, 0.f};
-    // (A, H) of the pairs i0 .. i1 - 1, pair j0 + v by wave v, joined
-    auto gather = [&](const uint64_t* base, int i0, int i1, int j0, float (&fa)[2], float (&fh)[2]) {
-      if (j0 + wave >= i0 && j0 + wave < i1 && sub == 0) {
-        const uint64_t* at = base + static_cast<long>(j0 + wave) * d + ch;
-        uint64_t got[2];
+        if (e < nch)
+          publish(a.group_pairs + static_cast<long>(chunk / kGroup) * d + ch + e, through(all_a[e], ga[e]),
+                  all_h[e] + through(all_a[e], gh[e]));
+    if (from < group0) {
+      float sa[2] = {1.f, 1.f}, sh[2] = {0.f, 0.f};
+      if (old) {
+        if (wave == kWaves - 1 && sub == 0) {
+          const uint64_t* at = a.states + static_cast<long>(chunk / kSuper - 1) * d + ch;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) got[e] = e < nch ? look(at + e) : ~0ull;
-        while (__any(!there(got[0]) || !there(got[1]))) {
-          // (the channels' words were written together: until the first is there, only it is looked for)
-          for (;;) {
-            bool yes = true;
-            if (row_lane == 0) yes = there(got[0] = look(at));
-            if (__all(yes)) break;
-            __builtin_amdgcn_s_sleep(4);
-          }
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (!there(got[e])) got[e] = look(at + e);
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          in_a[wave][2 * row_lane + e] = a_of(got[e]);
-          in_h[wave][2 * row_lane + e] = h_of(got[e]);
-        }
-      }
-      __syncthreads();
-      for (int i = i0; i < i1; ++i)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float wa = in_a[i - j0][2 * row_lane + e];
-          fh[e] = in_h[i - j0][2 * row_lane + e] + through(wa, fh[e]);
-          fa[e] = through(wa, fa[e]);
-        }
-      __syncthreads();
-    };
-    if (a.chunks > 1) {
-      float ga[2] = {1.f, 1.f}, gh[2] = {0.f, 0.f};
-      if (from1 < chunk) gather(a.pairs, from1, chunk, group0, ga, gh);
-      if (speaks && chunk % kGroup == kGroup - 1)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (e < nch)
-            publish(a.group_pairs + static_cast<long>(chunk / kGroup) * d + ch + e, through(all_a[e], ga[e]),
-                    all_h[e] + through(all_a[e], gh[e]));
-      if (from < group0) {
-        float sa[2] = {1.f, 1.f}, sh[2] = {0.f, 0.f};
-        if (old) {
-          if (wave == kWaves - 1 && sub == 0) {
-            const uint64_t* at = a.states + static_cast<long>(chunk / kSuper - 1) * d + ch;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              uint64_t v = e < nch ? look(at + e) : ~0ull;
-              while (!there(v)) {
-                __builtin_amdgcn_s_sleep(1);
-                v = look(at + e);
-              }
-              come[2 * row_lane + e] = h_of(v);
+          for (int e = 0; e < 2; ++e) {
+            uint64_t v = e < nch ? look(at + e) : ~0ull;
+            while (!there(v)) {
+              __builtin_amdgcn_s_sleep(1);
+              v = look(at + e);
             }
+            come[2 * row_lane + e] = h_of(v);
           }
         }
-        if (from2 < group0 / kGroup) gather(a.group_pairs, from2, group0 / kGroup, super0 / kGroup, sa, sh);
-        if (old) {
-          __syncthreads();
-          state[0] = come[2 * row_lane], state[1] = come[2 * row_lane + 1];
-          __syncthreads();
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) state[e] = sh[e] + through(sa[e], state[e]);
+      }
+      if (from2 < group0 / kGroup) gather(a.group_pairs, from2, group0 / kGroup, super0 / kGroup, sa, sh);
+      if (old) {
+        __syncthreads();
+        state[0] = come[2 * row_lane], state[1] = come[2 * row_lane + 1];
+        __syncthreads();
       }
 #pragma unroll
-      for (int e = 0; e < 2; ++e) state[e] = gh[e] + through(ga[e], state[e]);
-      if (speaks && chunk % kSuper == kSuper - 1)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (e < nch)
-            publish(a.states + static_cast<long>(chunk / kSuper) * d + ch + e, 0.f, all_h[e] + through(all_a[e], state[e]));
+      for (int e = 0; e < 2; ++e) state[e] = sh[e] + through(sa[e], state[e]);
     }
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      state[e] = pre_h[e] + through(pre_a[e], state[e]);
-      state[e] = before_h[e] + through(before_a[e], state[e]);
-    }
+    for (int e = 0; e < 2; ++e) state[e] = gh[e] + through(ga[e], state[e]);
+    if (speaks && chunk % kSuper == kSuper - 1)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (e < nch)
+          publish(a.states + static_cast<long>(chunk / kSuper) * d + ch + e, 0.f, all_h[e] + through(all_a[e], state[e]));
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    state[e] = pre_h[e] + through(pre_a[e], state[e]);
+    state[e] = before_h[e] + through(before_a[e], state[e]);
+  }
 
-    // out
-    const int t_last = token(S - 1);
-    const bool plain = !begin && !end && min(t_first, t_last) >= live_lo && max(t_first, t_last) < live_hi;
-    auto out = [&](auto marked) {
+  // out
+  const int t_last = token(S - 1);
+  const bool plain = !begin && !end && min(t_first, t_last) >= live_lo && max(t_first, t_last) < live_hi;
+  auto out = [&](auto marked) {
 #pragma unroll
-      for (int s0 = 0; s0 < S; s0 += kBlock) {
-        Raw<T, 2> xo[kBlock];
-        Raw<TH, 2> hr[kBlock];
-        if constexpr (BACK)
-#pragma unroll
-          for (int i = 0; i < kBlock; ++i) {
-            load(xo[i], static_cast<const T*>(a.x), max(token(s0 + i), 0), from_ch);
-            load(hr[i], static_cast<const TH*>(a.h), max(token(s0 + i) - 1, 0), from_ch);    // (of a history's first token not used)
-          }
+    for (int s0 = 0; s0 < S; s0 += kBlock) {
+      Raw<T, 2> xo[kBlock];
+      Raw<TH, 2> hr[kBlock];
+      if constexpr (BACK)
 #pragma unroll
         for (int i = 0; i < kBlock; ++i) {
-          const int s = s0 + i;
-          if (marked && (begin >> s & 1)) start(s, state);
-          const bool stops = marked && (end >> s & 1);
-          float f[2], rest[2];
+          load(xo[i], static_cast<const T*>(a.x), max(token(s0 + i), 0));
+          load(hr[i], static_cast<const TH*>(a.h), max(token(s0 + i) - 1, 0));    // (of a history's first token not used)
+        }
 #pragma unroll
-          for (int e = 0; e < 2; ++e) gates_of<T>(gate[s].at(e), f[e], rest[e]);
-          if constexpr (!BACK) {
+      for (int i = 0; i < kBlock; ++i) {
+        const int s = s0 + i;
+        if (marked && (begin >> s & 1)) start(s, state);
+        const bool stops = marked && (end >> s & 1);
+        float f[2], rest[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) state[e] = fmaf(f[e], state[e], rest[e] * xr[s].at(e));
-            if ((marked && !live(s)) || nch <= 0) continue;
-            if (a.h_bf16)
-              put<EVEN, ONCE>(row_at(static_cast<bf16_t*>(a.h), token(s), from_ch), state, nch);
-            else
-              put<EVEN, ONCE>(row_at(static_cast<float*>(a.h), token(s), from_ch), state, nch);
-            if (stops && a.last) put<EVEN, false>(row_at(a.last, end_b[slice * S + s], from_ch), state, nch);
-          } else {
-            float prev[2] = {hr[i].at(0), hr[i].at(1)}, dg[2], dx[2];
-            const int b = stops ? end_b[slice * S + s] : 0;
-            if (stops)
+        for (int e = 0; e < 2; ++e) gates_of<T>(gate[s].at(e), f[e], rest[e]);
+        if constexpr (!BACK) {
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                prev[e] = a.h0 && e < nch ? a.h0[static_cast<long>(b) * d + ch + e] : 0.f;
-                asm volatile("" : "+v"(prev[e]));
-              }
+          for (int e = 0; e < 2; ++e) state[e] = fmaf(f[e], state[e], rest[e] * xr[s].at(e));
+          if ((marked && !live(s)) || nch <= 0) continue;
+          if (a.h_bf16)
+            put<EVEN, ONCE>(row_at(static_cast<bf16_t*>(a.h), token(s)), state, nch);
+          else
+            put<EVEN, ONCE>(row_at(static_cast<float*>(a.h), token(s)), state, nch);
+          if (stops && a.last) put<EVEN, false>(row_at(a.last, end_b[slice * S + s]), state, nch);
+        } else {
+          float prev[2] = {hr[i].at(0), hr[i].at(1)}, dg[2], dx[2];
+          const int b = stops ? end_b[slice * S + s] : 0;
+          if (stops)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float D = dr[s].at(e) + state[e];
-              dx[e] = rest[e] * D;
-              state[e] = f[e] * D;
-              dg[e] = state[e] * rest[e] * (prev[e] - xo[i].at(e));
+              prev[e] = a.h0 && e < nch ? a.h0[static_cast<long>(b) * d + ch + e] : 0.f;
+              asm volatile("" : "+v"(prev[e]));
             }
-            if ((marked && token(s) < 0) || nch <= 0) continue;
-            if (marked && !live(s)) dg[0] = dg[1] = dx[0] = dx[1] = 0.f;   // rows of no history: no loss depends on them
-            put<EVEN, ONCE>(row_at(static_cast<T*>(a.dgate), token(s), from_ch), dg, nch);
-            put<EVEN, ONCE>(row_at(static_cast<T*>(a.dx), token(s), from_ch), dx, nch);
-            if (stops && a.dh0) put<EVEN, false>(row_at(a.dh0, b, from_ch), state, nch);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float D = dr[s].at(e) + state[e];
+            dx[e] = rest[e] * D;
+            state[e] = f[e] * D;
+            dg[e] = state[e] * rest[e] * (prev[e] - xo[i].at(e));
           }
+          if ((marked && token(s) < 0) || nch <= 0) continue;
+          if (marked && !live(s)) dg[0] = dg[1] = dx[0] = dx[1] = 0.f;   // rows of no history: no loss depends on them
+          put<EVEN, ONCE>(row_at(static_cast<T*>(a.dgate), token(s)), dg, nch);
+          put<EVEN, ONCE>(row_at(static_cast<T*>(a.dx), token(s)), dx, nch);
+          if (stops && a.dh0) put<EVEN, false>(row_at(a.dh0, b), state, nch);
         }
       }
-    };
-    if (__all(plain))
-      out(std::false_type{});
-    else
-      out(std::true_type{});
-  }
+    }
+  };
+  if (__all(plain))
+    out(std::false_type{});
+  else
+    out(std::true_type{});
 }
 
 // One token of every history: the new states, and h in its type.
