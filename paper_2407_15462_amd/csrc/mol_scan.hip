@@ -75,6 +75,7 @@ struct ScanArgs {
   uint64_t* states;        // [chunks / kSuper][d] (0, state)
   long words;              // of the three together
   bool once;               // rows are read past the caches
+  bool empties;            // the scan's own launch sees to histories without tokens
 };
 
 __device__ __forceinline__ int offset_at(const ScanArgs& a, int i) {
@@ -174,11 +175,13 @@ __global__ __launch_bounds__(256) void k_scan_plan(ScanArgs a, int chunk_len) {
   float* out = BACK ? a.dh0 : a.last;
   const float* in = BACK ? a.dlast : a.h0;
   if (!out) return;
-  for (long b0 = tid / 64 * 64; b0 < a.B; b0 += all) {
+  // (eight histories a wave and turn: enough waves for rows of many that are empty, few turns for many that are not)
+  for (long b0 = tid / 64 * 8; b0 < a.B; b0 += all / 8) {
     const int b = static_cast<int>(b0) + lane;
-    uint64_t m = __ballot(b < a.B && offset_at(a, b) >= offset_at(a, b + 1));
+    uint64_t m = __ballot(lane < 8 && b < a.B && offset_at(a, b) >= offset_at(a, b + 1));
     for (; m; m &= m - 1) {
       const long at = (b0 + __builtin_ctzll(m)) * a.d;
+#pragma unroll 4
       for (int c = lane; c < a.d; c += 64) out[at + c] = in ? in[at + c] : 0.f;
     }
   }
@@ -255,29 +258,31 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
   int2 plan = a.chunks > 1 ? a.plan[chunk] : make_int2(0, 0);
   plan.x = __builtin_amdgcn_readfirstlane(plan.x);
   plan.y = __builtin_amdgcn_readfirstlane(plan.y);
-  for (int b = plan.x + tid; b < a.B; b += kThreads) {
-    const int s = offset_at(a, b), e = offset_at(a, b + 1);
-    if (a.chunks > 1 && s >= hi) break;
-    if (s >= e) {
-      // (without a plan's launch, histories without tokens are seen to here)
-      float* out = BACK ? a.dh0 : a.last;
-      const float* in = BACK ? a.dlast : a.h0;
-      if (a.chunks == 1 && out)
-        for (int c = cg * 128; c < min(d, cg * 128 + 128); ++c)
-          out[static_cast<long>(b) * d + c] = in ? in[static_cast<long>(b) * d + c] : 0.f;
-      continue;
+  for (int b0 = plan.x + wave * 64; b0 < a.B; b0 += kThreads) {
+    const int b = b0 + lane;
+    const int s = b < a.B ? offset_at(a, b) : a.T, e = b < a.B ? offset_at(a, b + 1) : a.T;
+    if (a.chunks > 1 && __all(s >= hi)) break;
+    if (s < e) {
+      const int tb = BACK ? e - 1 : s, te = BACK ? s : e - 1;
+      if (tb >= lo && tb < hi) {
+        const int i = BACK ? first - tb : tb - first;
+        begin_b[i] = b;
+        atomicOr(&begins[i / S], 1u << i % S);
+      }
+      if (te >= lo && te < hi) {
+        const int i = BACK ? first - te : te - first;
+        end_b[i] = b;
+        atomicOr(&ends[i / S], 1u << i % S);
+      }
     }
-    const int tb = BACK ? e - 1 : s, te = BACK ? s : e - 1;
-    if (tb >= lo && tb < hi) {
-      const int i = BACK ? first - tb : tb - first;
-      begin_b[i] = b;
-      atomicOr(&begins[i / S], 1u << i % S);
-    }
-    if (te >= lo && te < hi) {
-      const int i = BACK ? first - te : te - first;
-      end_b[i] = b;
-      atomicOr(&ends[i / S], 1u << i % S);
-    }
+    // (histories without tokens, unless a launch of the plan's sees to them)
+    float* out = BACK ? a.dh0 : a.last;
+    const float* in = BACK ? a.dlast : a.h0;
+    if (a.empties && out)
+      for (uint64_t m = __ballot(b < a.B && s >= e); m; m &= m - 1) {
+        const long at = static_cast<long>(b0 + __builtin_ctzll(m)) * d;
+        for (int c = cg * 128 + lane; c < min(d, cg * 128 + 128); c += 64) out[at + c] = in ? in[at + c] : 0.f;
+      }
   }
   const int group0 = chunk / kGroup * kGroup, super0 = chunk / kSuper * kSuper;
   const int from = min(plan.y, chunk);
@@ -591,10 +596,12 @@ hipError_t run_scan_slices(ScanArgs a, void* ws, hipStream_t st) {
   a.chunks = s.chunks;
   a.groups = s.groups;
   a.lanes_log2 = s.lanes_log2;
-  if (s.chunks == 0) {                       // no tokens: no history has any
-    hipLaunchKernelGGL((k_scan_plan<BACK>), dim3(static_cast<unsigned>(std::min(a.B / 64 + 1, 1024))), dim3(256), 0, st, a, s.len);
-    return hipGetLastError();
-  }
+  // The plan's launch: of one chunk, and of no tokens, there is none to make, but histories without tokens.  A few
+  // of these the scan's workgroups see to (4096 histories with 100 tokens x 512: 33 us a call, with theirs 194).
+  ScanArgs plan = a;
+  plan.words = 0;
+  bool wanted = s.chunks != 1 || a.B > 32;
+  a.empties = !wanted;
   if (s.chunks > 1) {
     char* w = static_cast<char*>(ws);
     a.ticket = reinterpret_cast<uint32_t*>(w);
@@ -603,9 +610,16 @@ hipError_t run_scan_slices(ScanArgs a, void* ws, hipStream_t st) {
     a.group_pairs = a.pairs + static_cast<long>(s.chunks) * a.d;
     a.states = a.group_pairs + static_cast<long>(s.chunks / kGroup) * a.d;
     a.words = pair_words(s, a.d);
-    const long want = std::max<long>(a.words / 1024, s.chunks / 4);
-    hipLaunchKernelGGL((k_scan_plan<BACK>), dim3(static_cast<unsigned>(std::min(want + 1, 1024l))), dim3(256), 0, st, a, s.len);
+    plan = a;
+  } else {
+    plan.chunks = 0;
+    wanted = wanted && (BACK ? a.dh0 : a.last);
   }
+  if (wanted) {
+    const long want = std::max({plan.words / 1024, plan.chunks / 4l, a.B / 32l});
+    hipLaunchKernelGGL((k_scan_plan<BACK>), dim3(static_cast<unsigned>(std::min(want + 1, 1024l))), dim3(256), 0, st, plan, s.len);
+  }
+  if (s.chunks == 0) return hipGetLastError();
   const unsigned grid = static_cast<unsigned>(s.chunks) * s.groups;
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, st, a); };
   if (a.d % 2) {

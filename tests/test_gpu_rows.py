@@ -105,6 +105,22 @@ def test_layer_norm_grad_over_many_rows():
     within(dgamma, (dy * xhat).sum(0), 160 * rh.U * xhat.abs().sum(0) + 60 * rh.U * T, "dgamma")
 
 
+def test_norms_past_32_bits():
+    """More than 2^31 elements: the last rows are as they are alone."""
+    T, d = 4200001, 520
+    x = torch.empty(T, d, dtype=BF16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    dy = x.flip(0)
+    rows_ = [0, T // 2, T - 2, T - 1]
+    some, dsome = x[rows_].contiguous(), dy[rows_].contiguous()
+    assert torch.equal(mol.layer_norm(x)[rows_], mol.layer_norm(some))
+    assert torch.equal(mol.normalize(x)[rows_], mol.normalize(some))
+    assert torch.equal(mol.normalize_grad(dy, x)[rows_], mol.normalize_grad(dsome, some))
+    dx, dgamma, dbeta = mol.layer_norm_grad(dy, x)
+    assert torch.equal(dx[rows_], mol.layer_norm_grad(dsome, some)[0])
+    # dbeta: a lane's 4102 rows at most, then as in the helpers, of magnitudes 0.8 on average
+    assert float((dbeta.double() - dy.double().sum(0)).abs().max()) < (4102 + 128) * rh.U * T
+
+
 def test_a_workspace_for_more_serves_fewer():
     ws = mol.layer_norm_grad_workspace(torch.empty(6000, 8192, device="cuda"))
     for T, d in ((6000, 4096), (5000, 4097), (6000, 30), (10, 8192)):

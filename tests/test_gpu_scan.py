@@ -178,6 +178,26 @@ def test_no_tokens():
     assert torch.equal(mol.gated_scan_grad(x, x, x, offsets=off, h0=h0, dlast=h0 + 1)[2], h0 + 1)
 
 
+@pytest.mark.parametrize("T", [60, 3000])
+def test_mostly_empty_histories(T):
+    """Far more histories than tokens: each one's state, in one chunk and in several."""
+    B, d = 5001, 140
+    g = torch.Generator().manual_seed(T)
+    offsets = torch.sort((torch.rand(B + 1, generator=g) * (T + 1)).int().clamp(max=T)).values
+    offsets[0], offsets[-1] = 0, T
+    lens = (offsets[1:] - offsets[:-1]).tolist()
+    gate, x = (torch.randn(T, d, generator=g).cuda() for _ in range(2))
+    h0 = torch.randn(B, d, generator=g)
+    want, bound, _, last, lb = rh.gated_scan(gate, x, lens, 0, h0, F32)
+    h, end = mol.gated_scan(gate, x, offsets.cuda(), h0=h0.cuda())
+    within(h, want, bound, "h")
+    within(end, last, lb, "last")
+    dlast = torch.randn(B, d, generator=g)
+    ref = rh.gated_scan_grad(gate, x, h, None, lens, 0, h0, dlast, F32)
+    for name, a, b in zip(("dgate", "dx", "dh0"), mol.gated_scan_grad(gate, x, h, offsets=offsets.cuda(), h0=h0.cuda(), dlast=dlast.cuda()), ref):
+        within(a, *b, name)
+
+
 def test_gradient_is_the_difference_quotient():
     lens, d, h = [3, 0, 9], 5, 1e-3
     g = torch.Generator().manual_seed(2)
