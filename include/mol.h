@@ -537,7 +537,8 @@ int mol_dropout(const void *x, int32_t x_dtype, int64_t n, double p,
  * offsets int32 [B + 1] on the device, not decreasing, within [0, T] (others are
  * clamped to it), or NULL: one history of all T tokens, B = 1.  Rows in front
  * of offsets[0] and from offsets[B] on belong to no history: their h is left
- * as it is.  States are float32 throughout.  Needs mol_gated_scan_workspace bytes
+ * as it is.  States are float32 throughout; one that is not finite stays so to its
+ * history's end, and is no other history's.  Needs mol_gated_scan_workspace bytes
  * (256-byte aligned), which serve every scan and gradient of no more tokens,
  * channels and histories.  d up to MOL_MAX_ROW, T and B up to MOL_MAX_TOKENS. */
 int mol_gated_scan_workspace(int32_t T, int32_t d, int32_t B, size_t *bytes);

@@ -11,8 +11,9 @@
 // runs through it from state 0, for its (A, H); slices are joined in LDS; the
 // workgroup publishes the chunk's (A, H), gets the state that comes in from the
 // chunks before, and runs through the tokens once more, which it kept in registers, for
-// what it writes.  A history's first token starts from h0 with A = 0, so that nothing
-// crosses from one history to the next.
+// what it writes.  A history's first token starts from h0, with a mark for A, so that
+// nothing crosses from one history to the next.  (A = 0 is no such mark: it is a product of gates
+// below float32's range, through which a NaN or an infinity stays what it is, since f is never 0.)
 //
 // The state that comes in is formed in an order that sizes and offsets alone fix: the
 // state at the end of the kSuper chunks before (a chain of waits along a long history),
@@ -34,6 +35,7 @@
 // ahead (226 to 311: a wait is then for workgroups at another place of their turn), a ninth wave for the waits,
 // tickets of their own for every 128 channels (238: neighbours in memory drift apart in time).
 #include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 #include "mol_kernels.h"
@@ -101,8 +103,12 @@ __device__ __forceinline__ void gates_of(float g, float& f, float& rest) {
   rest = e * f;
 }
 
-// a v, and 0 for a = 0 whatever v is (another history's state)
-__device__ __forceinline__ float through(float a, float v) { return a == 0.f ? 0.f : a * v; }
+// The A of tokens among which a history begins is NaN, as it is behind a NaN gate (whose H is NaN as well, so that what
+// comes in changes nothing); others' are from 0 to 1.  So the A of tokens behind others is the product of both.
+constexpr float kBegins = __builtin_nanf("");
+// What is left of v behind tokens of A = a: a v; nothing where a history begins there, whatever v is (another
+// history's state); and a v that is not finite as it is, since no product of gates is 0.
+__device__ __forceinline__ float through(float a, float v) { return a != a ? 0.f : fabsf(v) <= FLT_MAX ? a * v : v; }
 
 __device__ __forceinline__ void publish(uint64_t* p, float a, float h) {
   const uint64_t v = static_cast<uint64_t>(__float_as_uint(a) | 0x80000000u) << 32 | __float_as_uint(h);
@@ -308,7 +314,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       if (marked && (begin >> s & 1)) {
-        A[0] = A[1] = 0.f;
+        A[0] = A[1] = kBegins;
         start(s, H);
       }
 #pragma unroll
@@ -345,7 +351,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
         const float ua = __shfl_up(ca, o), uh = __shfl_up(chh, o);
         if (lane >= o) {
           chh += through(ca, uh);
-          ca = through(ca, ua);
+          ca *= ua;
         }
       }
       const float ua = __shfl_up(ca, lanes), uh = __shfl_up(chh, lanes);
@@ -364,11 +370,11 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
     for (int v = 0; v < wave; ++v) {
       const float wa = sum_a[v][2 * row_lane + e], wh = sum_h[v][2 * row_lane + e];
       pre_h[e] = wh + through(wa, pre_h[e]);
-      pre_a[e] = through(wa, pre_a[e]);
+      pre_a[e] *= wa;
     }
     const float wa = sum_a[wave][2 * row_lane + e], wh = sum_h[wave][2 * row_lane + e];
     all_h[e] = wh + through(wa, pre_h[e]);
-    all_a[e] = through(wa, pre_a[e]);
+    all_a[e] = wa * pre_a[e];
   }
   const bool speaks = a.chunks > 1 && wave == kWaves - 1 && sub == 0;
   if (speaks)
@@ -408,7 +414,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
       for (int e = 0; e < 2; ++e) {
         const float wa = in_a[i - j0][2 * row_lane + e];
         fh[e] = in_h[i - j0][2 * row_lane + e] + through(wa, fh[e]);
-        fa[e] = through(wa, fa[e]);
+        fa[e] *= wa;
       }
     __syncthreads();
   };
@@ -419,7 +425,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_scan(ScanArgs a) {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         if (e < nch)
-          publish(a.group_pairs + static_cast<long>(chunk / kGroup) * d + ch + e, through(all_a[e], ga[e]),
+          publish(a.group_pairs + static_cast<long>(chunk / kGroup) * d + ch + e, all_a[e] * ga[e],
                   all_h[e] + through(all_a[e], gh[e]));
     if (from < group0) {
       float sa[2] = {1.f, 1.f}, sh[2] = {0.f, 0.f};
