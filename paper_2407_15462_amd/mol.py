@@ -1167,8 +1167,9 @@ class Learner:
         if self.normalize:
             u = u.view(B, Pq, d)
             dq = normalize_grad(dq, u, dtype=torch.float32)
-            dq.masked_fill_((u == 0).all(-1, keepdim=True), 0)    # (no length, no direction: the formula's 1 / eps is of no use)
             dx = normalize_grad(dx, x)
+            for dy, of in ((dq, u), (dx, x)):                     # (no length, no direction: the formula's 1 / eps is of no use)
+                dy.masked_fill_((of == 0).all(-1, keepdim=True), 0)
         dq = dq.view(B, Pq * d)
         if "gamma" in M:
             dq, dgamma, dbeta = layer_norm_grad(dq, v, M["gamma"], dtype=torch.float32)
