@@ -1088,7 +1088,8 @@ class Learner:
     def step(self, query_ids: torch.Tensor, item_ids: torch.Tensor, target: torch.Tensor, lr,
              inv_temp: float = 20.0, offsets: Optional[torch.Tensor] = None) -> torch.Tensor:
         """One optimisation step on B queries and N sampled items: query_ids int32
-        [B] (outside the table: a row of zeros, which adds to no gradient of a query's), item_ids
+        [B] (outside the table: a row of zeros, which adds to no gradient of a row's; behind a norm
+        such a query is beta, which learns from its loss), item_ids
         int32 [N] (outside the table: an empty slot, no candidate), target int32 [B]:
         the column of each query's positive; lr: a number, or one float32 on the GPU
         (which a captured step reads when it runs).  With gates query_ids are the events
@@ -1162,8 +1163,6 @@ class Learner:
         out = score_grad(Problem(*tensors, flags=self.grad_flags), dphi,
                          out=dict(dW1=G["W1"], db1=G["b1"], dW2=G["W2"], db2=G["b2"]))
         dq, dx = out["dQ"], out["dX"]
-        if "gamma" in M:                                          # (a query without an event is gamma's and beta's alone)
-            dq.masked_fill_(self._without_events(query_ids, offsets)[:, None, None], 0)
         if self.normalize:
             u = u.view(B, Pq, d)
             dq = normalize_grad(dq, u, dtype=torch.float32)
@@ -1185,15 +1184,6 @@ class Learner:
         self.steps.add_(1)
         adamw_step(self.tensors, lr=lr, step=self.steps, seed=self.seed)
         return loss
-
-    def _without_events(self, ids: torch.Tensor, offsets) -> torch.Tensor:
-        """Which queries have no event of the table."""
-        inside = (ids >= 0) & (ids < self.shape[0])
-        if offsets is None:
-            return ~inside
-        count = torch.nn.functional.pad(inside.cumsum(0), (1, 0))
-        ends = offsets.long().clamp(0, ids.numel())
-        return count[ends[1:]] <= count[ends[:-1]]
 
     @staticmethod
     def _last(ids: torch.Tensor, offsets: torch.Tensor) -> torch.Tensor:

@@ -3,7 +3,8 @@ a row, a component or a history holds nothing (MI355X only)."""
 import pytest
 import torch
 
-from test_gpu_learner_histories import batch, make, step64
+import rows_helpers as rh
+from test_gpu_learner_histories import OPTIONS, Rounded, batch, make, step64
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +34,60 @@ def test_an_items_component_of_length_zero_has_no_gradient(options):
     assert float((got - want).norm() / want.norm()) < (4e-3 + 1e-4 + 3 * 2.0 ** -8) * amp
     if "states_8bit" in options:
         assert float(learner.state["m_scale"]["items"].max()) < 1.0 and float(learner.state["v_scale"]["items"].max()) < 1.0
+
+
+def beta_of_queries_without_events(learner, ids, inv_temp):
+    """What these queries' losses, of all queries' mean, are to beta, which is their row behind the norm: the gradient, and
+    its size before normalize takes what lies along a component away."""
+    q, items, target, offsets = ids
+    Vq, V, Pq, Px, P, d = learner.shape
+    inside = (q >= 0) & (q < Vq)
+    dead = [b for b in range(len(target)) if not (inside[b] if offsets is None else inside[offsets[b]:offsets[b + 1]].any())]
+    assert dead
+    w = {n: learner.copy.get(n, t).double().cpu() for n, t in learner.master.items()}
+    beta = w["beta"].requires_grad_()
+    u = beta.view(Pq, d).expand(len(dead), Pq, d)
+    r = u.norm(dim=-1, keepdim=True) if learner.normalize else torch.ones(1, dtype=torch.float64)
+    Q = Rounded.apply(u / r)
+    at = items.long().clamp(min=0)
+    x = w["items"][:, at] * (items >= 0)[None, :, None]
+    if learner.dropout:
+        share = 1 - int(learner.dropout * 65536 + 0.5) / 65536
+        x = Rounded.apply(x * rh.kept(x.numel(), learner.dropout, learner.seed, int(learner.steps), 1 << 40).view(x.shape) / share)
+    X = Rounded.apply(x / x.norm(dim=-1, keepdim=True).clamp(min=1e-12)) if learner.normalize else x
+    # (the gating logits are the last id's, where that is one of the table's: none of a query without an event is)
+    s = torch.einsum("bqd,xnd->bnqx", Q, X).reshape(len(dead), len(items), P)
+    lg = (w["a_x"][at] * (items >= 0)[:, None])[None] + torch.nn.functional.silu(s @ w["W1"].t() + w["b1"]) @ w["W2"].t() + w["b2"]
+    hot = target[dead].long()
+    keep = (items >= 0)[None] & (items[None] != items[hot][:, None])
+    keep[torch.arange(len(dead)), hot] = True
+    z = ((torch.softmax(lg, -1) * s).sum(-1) * inv_temp).masked_fill(~keep, -torch.inf)
+    loss = (torch.logsumexp(z, 1) - z[torch.arange(len(dead)), hot]).sum() / len(target)
+    gb, gq = torch.autograd.grad(loss, [beta, Q])
+    return gb, float((gq.norm(dim=-1, keepdim=True) / r.detach()).sum(0).norm())
+
+
+@pytest.mark.parametrize("name", ["norm", "gates norm", "all"])
+@pytest.mark.parametrize("Vq,V,Pq,Px,d,H,B,N", [(50, 300, 8, 4, 64, 64, 40, 120), (20, 90, 4, 4, 24, 32, 9, 33)])
+def test_beta_learns_from_queries_without_events(name, Vq, V, Pq, Px, d, H, B, N):
+    """Behind the norm a query without an event is beta: its loss is one of the losses, so that a step's gradient of beta
+    holds its part, and that of nothing else of a query's does."""
+    learner = make(Vq, V, Pq, Px, d, H, seed=1, **OPTIONS[name])
+    for step in range(1, 3):
+        ids = batch(learner, B, N, seed=step)
+        if ids[3] is None:
+            ids[0][3], ids[0][6] = -1, Vq                  # (of queries without histories: ids outside the table)
+        loss, want, amp_q, amp_x = step64(learner, ids, 20.0)          # (which takes these queries for constants)
+        part, size = beta_of_queries_without_events(learner, ids, 20.0)
+        assert float(part.norm()) > 0.1 * float(want["beta"].norm())
+        got = learner.step(*(x.cuda() for x in ids[:3]), 0.01, offsets=None if ids[3] is None else ids[3].cuda())
+        # the bounds of a step (scores within 1e-4, 20 times that in z, twice in the loss, once a component that falls to
+        # the other side of its rounding; softmax within 4e-3 of itself, and the roundings on a gradient's way)
+        assert float((got.double().cpu() - loss).abs().max()) < 4e-3 + 20 * 2.0 ** -8 / 24
+        for n in learner.master:
+            roundings = dict(queries=3, items=3, gates=4).get(n, 1)
+            rel = 4e-3 + 1e-4 + roundings * 2.0 ** -8
+            bound = rel * (amp_x if n == "items" else amp_q if roundings > 1 or n in ("gamma", "beta") else 1.0) * float(want[n].norm())
+            if n == "beta":
+                want[n], bound = want[n] + part, bound + rel * size
+            assert float((learner.grad[n].double().cpu() - want[n]).norm()) < bound, n
