@@ -732,6 +732,8 @@ def _rows(x: torch.Tensor, name: str = "x") -> Tuple[int, int]:
         _need(isinstance(x, torch.Tensor) and x.dim() >= 1 and x.shape[-1] > 0, f"{name} must be a tensor [..., d]")
         _operand(x, name, None, _FLOATS, x.device)
     d = x.shape[-1]
+    if d >= 1 << 31:
+        _sizes(d)
     return x.numel() // d, d
 
 
