@@ -117,6 +117,7 @@ struct Stats {
       if (needed) scale = want;
     }
     if (MODE == kLayer) {
+      if (ss == 0.f) scale = 1.f;                              // (a constant row: x is 0 in any scale, and eps is left of the variance)
       inv = 1.f / sqrtf(ss / d + eps * scale * scale);
       flat = false;
     } else {
