@@ -110,8 +110,8 @@ struct Stats {
     scale = 1.f;
     for (bool again = false;; again = true) {                  // (one copy of the code, which runs once, seldom twice)
       ss = squares(raw, at, team, d, scale);
-      const float want = rescale(ss);
-      // (a layer norm's small rows need none: eps is added to their variance)
+      const float want = rescale(MODE == kLayer ? ss + eps : ss);
+      // (a layer norm's small rows need none: eps is added to their variance, in range as well)
       const bool needed = MODE == kLength ? want != 1.f : want < 1.f;
       if (again || !__any(needed)) break;
       if (needed) scale = want;

@@ -33,3 +33,20 @@ def test_layer_norm_of_constant_rows_whose_sum_overflows(d, t, sign):
     (dx, dgamma, dbeta), bounds = rh.layer_norm_grad(dy, small, gamma, 1e-5, F32)
     for name, a, b, c in zip(("dx", "dgamma", "dbeta"), got, (dx, dgamma, dbeta), bounds):
         within(a, b, c, name)
+
+
+@pytest.mark.parametrize("d", [2, 3, 7, 64, 300])
+def test_layer_norm_of_large_variance_and_eps(d):
+    """A variance and an eps that float32 holds, whose sum it does not."""
+    eps, half = 3.4e38, d // 2
+    a = (2.9e38 / (2 * half)) ** 0.5                         # (the sum of squares, 2.9e38, is in range too)
+    x = torch.zeros(4, d)
+    x[:, :half], x[:, half:2 * half] = a, -a
+    x[2] *= 1e-19
+    x, dy = x.cuda(), rows(4, d, F32, seed=2)
+    want, bound = rh.layer_norm(x, None, None, eps, F32)
+    within(mol.layer_norm(x, eps=eps), want, bound, "y")
+    (dx, dgamma, _), (bx, bg, _) = rh.layer_norm_grad(dy, x, None, eps, F32)
+    got = mol.layer_norm_grad(dy, x, eps=eps)
+    within(got[0], dx, bx, "dx")
+    within(got[1], dgamma, bg, "dgamma")
