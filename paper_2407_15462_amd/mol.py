@@ -1192,8 +1192,8 @@ class Learner:
         """The last event of every history, -1 of none."""
         if ids.numel() == 0:
             return ids.new_full((offsets.numel() - 1,), -1)
-        some = offsets[1:] > offsets[:-1]
-        return torch.where(some, ids[(offsets[1:].long() - 1).clamp(min=0, max=ids.numel() - 1)], -1)
+        ends = offsets.long().clamp(0, ids.numel())              # (as the scan takes them)
+        return torch.where(ends[1:] > ends[:-1], ids[(ends[1:] - 1).clamp(min=0)], -1)
 
     def states(self, query_ids: torch.Tensor, offsets: torch.Tensor, state: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The states float32 [B][Pq d] behind the events query_ids [T] of histories, which offsets int32 [B + 1] cuts

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import rows_helpers as rh
-from test_gpu_learner_histories import OPTIONS, Rounded, batch, make, step64
+from test_gpu_learner_histories import OPTIONS, Rounded, batch, everything, make, step64
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +91,17 @@ def test_beta_learns_from_queries_without_events(name, Vq, V, Pq, Px, d, H, B, N
             if n == "beta":
                 want[n], bound = want[n] + part, bound + rel * size
             assert float((learner.grad[n].double().cpu() - want[n]).norm()) < bound, n
+
+
+def test_offsets_past_the_events_are_clamped_throughout():
+    """As the scan clamps them: a history that starts behind the last event has no last event either."""
+    a, b = (make(20, 90, 4, 4, 24, 32, seed=1, **OPTIONS["all"]) for _ in range(2))
+    ids = (torch.arange(12, dtype=torch.int32) % 7).cuda()
+    over, inside = (torch.tensor(o, dtype=torch.int32, device="cuda") for o in ([-3, 4, 9, 40, 50], [0, 4, 9, 12, 12]))
+    _, items, target, _ = batch(a, 8, 40, seed=4)
+    p, q = a.problem(ids, offsets=over), b.problem(ids, offsets=inside)
+    assert all(torch.equal(x, y) for x, y in zip(p.tensors, q.tensors))
+    assert not p.tensors[2][3].any(), "the gating logits of a history without events"
+    losses = [m.step(ids, items.cuda(), target[:4].cuda(), 0.01, offsets=o) for m, o in ((a, over), (b, inside))]
+    assert torch.equal(*losses)
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(everything(a), everything(b)))
