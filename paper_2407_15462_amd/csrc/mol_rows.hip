@@ -355,9 +355,14 @@ __global__ __launch_bounds__(threads<TEAM>()) void k_norm_grad(RowArgs a) {
     } else if (st.flat) {
       c[1] = 0.f;
     }
-    const float inv = st.inv * st.scale;
+    // (L2 in two factors: 1 / |x| may be 2^-135 where dx is a normal number; layer norm's is 2^-128 and more)
+    const bool two = MODE == kLength && st.scale < 1.f;
+    const float inv = two ? st.inv : st.inv * st.scale, then = two ? st.scale : 1.f;
 #pragma unroll
-    for (int i = 0; i < E; ++i) w[i] = inv * fmaf(-st.x[i], c[1], MODE == kLayer ? w[i] - c[0] : w[i]);
+    for (int i = 0; i < E; ++i) {
+      w[i] = inv * fmaf(-st.x[i], c[1], MODE == kLayer ? w[i] - c[0] : w[i]);
+      if (MODE == kLength) w[i] *= then;
+    }
     if (live) store_row(a.y, a.y_bf16, row + mine, a.d, at, WHOLE, w);
     if (kAhead)
 #pragma unroll

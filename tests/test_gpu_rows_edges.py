@@ -50,3 +50,25 @@ def test_layer_norm_of_large_variance_and_eps(d):
     got = mol.layer_norm_grad(dy, x, eps=eps)
     within(got[0], dx, bx, "dx")
     within(got[1], dgamma, bg, "dgamma")
+
+
+@pytest.mark.parametrize("d", [9, 64, 300, 5000])
+@pytest.mark.parametrize("to", [F32, BF16])
+def test_gradients_of_rows_as_large_as_float32_holds(d, to):
+    """1 / |x| is below float32's normal numbers, dy / |x| is not."""
+    x, dy = rows(5, d, F32), rows(5, d, F32, seed=2)
+    x = x / x.abs().amax(1, keepdim=True)
+    x[1] *= 3e38
+    x[3] *= 1.5e38
+    dy *= 1e30
+    want, bound = rh.normalize_grad(dy, x, 1e-12, to)
+    within(mol.normalize_grad(dy, x, dtype=to), want, bound, "unit rows")
+    (want, _, _), (bound, _, _) = rh.layer_norm_grad(dy, x, None, 1e-5, to)
+    within(mol.layer_norm_grad(dy, x, dtype=to)[0], want, bound, "layer norm")
+    # and the smallest: |x| of 2^-60 and below, of dy far smaller and larger than it
+    x[1] = x[1] * 2.0 ** -128 * 1e-30
+    x[3] = x[3] * 2.0 ** -128 * 2.0 ** -60
+    for scale in (1e-60, 1e-25):
+        small = dy * scale
+        want, bound = rh.normalize_grad(small, x, 1e-37, to)
+        within(mol.normalize_grad(small, x, eps=1e-37, dtype=to), want, bound + 1e-44, f"unit rows, dy of {scale}")
