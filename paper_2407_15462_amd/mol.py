@@ -761,12 +761,10 @@ def _vector(x: torch.Tensor, t, name: str, d: int) -> None:
 
 def _output(out: Optional[torch.Tensor], x: torch.Tensor, dtype) -> torch.Tensor:
     """The caller's tensor of x's shape, or a new one of ``dtype`` (x's by default)."""
+    if dtype is not None and dtype not in _DTYPES:
+        raise ValueError(f"unsupported output dtype {dtype}")
     if out is None:
-        if dtype is None or dtype is x.dtype:
-            return torch.empty_like(x)
-        if dtype not in _DTYPES:
-            raise ValueError(f"unsupported output dtype {dtype}")
-        return torch.empty_like(x, dtype=dtype)
+        return torch.empty_like(x) if dtype is None or dtype is x.dtype else torch.empty_like(x, dtype=dtype)
     _like(x, out, "out", _FLOATS if dtype is None else (dtype,))
     return out
 

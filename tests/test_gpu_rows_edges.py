@@ -72,3 +72,16 @@ def test_gradients_of_rows_as_large_as_float32_holds(d, to):
         small = dy * scale
         want, bound = rh.normalize_grad(small, x, 1e-37, to)
         within(mol.normalize_grad(small, x, eps=1e-37, dtype=to), want, bound + 1e-44, f"unit rows, dy of {scale}")
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64])
+def test_output_types_are_refused_with_an_output_too(dtype):
+    x = torch.zeros(3, 8, device="cuda")
+    out = torch.full((3, 8), 7.0, dtype=dtype, device="cuda")
+    for call in (lambda **k: mol.layer_norm(x, **k), lambda **k: mol.normalize(x, **k), lambda **k: mol.normalize_grad(x, x, **k),
+                 lambda **k: mol.layer_norm_grad(x, x, **k), lambda **k: mol.dropout(x, 0.5, 1, **k), lambda **k: mol.gated_scan(x, x, **k),
+                 lambda **k: mol.gated_step(x, x, x.clone(), **k)):
+        for given in (dict(dtype=dtype), dict(out=out), dict(dtype=dtype, out=out)):
+            with pytest.raises(ValueError, match="dtype"):
+                call(**given)
+    assert bool((out == 7).all())
