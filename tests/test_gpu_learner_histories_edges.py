@@ -105,3 +105,16 @@ def test_offsets_past_the_events_are_clamped_throughout():
     losses = [m.step(ids, items.cuda(), target[:4].cuda(), 0.01, offsets=o) for m, o in ((a, over), (b, inside))]
     assert torch.equal(*losses)
     assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(everything(a), everything(b)))
+
+
+def test_no_events_at_all():
+    learner = make(20, 90, 4, 4, 24, 32, seed=1, **OPTIONS["all"])
+    none, offsets = torch.empty(0, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    assert learner.states(none, offsets).shape == (3, 96) and not learner.states(none, offsets).any()
+    kept = torch.rand(3, 96, device="cuda")
+    assert torch.equal(learner.states(none, offsets, state=kept), kept)
+    prob = learner.problem(none, offsets=offsets)
+    unit = learner.master["beta"].view(4, 24)
+    unit = unit / unit.norm(dim=-1, keepdim=True)
+    # (one rounding to bfloat16, and float32's of the length)
+    assert float((prob.tensors[0].float() - unit).abs().max()) < 2.0 ** -8 and not prob.tensors[2].any()

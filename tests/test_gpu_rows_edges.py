@@ -1,4 +1,5 @@
-"""Norms of rows whose sums leave float32's range (MI355X only)."""
+"""Norms of rows at the ends of float32's range, refusals, and operators whose inputs are
+read past the caches, in float32 and with a residual (MI355X only)."""
 import pytest
 import torch
 
@@ -85,3 +86,42 @@ def test_output_types_are_refused_with_an_output_too(dtype):
             with pytest.raises(ValueError, match="dtype"):
                 call(**given)
     assert bool((out == 7).all())
+
+
+@pytest.mark.parametrize("T,d", [(70001, 512), (300007, 131)])
+def test_float32_norms_back_past_the_caches(T, d):
+    """256 MB and more of float32 rows: rows as they are alone, and the weights' sums."""
+    assert T * d * 8 >= 1 << 28
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x, dy = (torch.randn(T, d, generator=g, device="cuda") for _ in range(2))
+    some = [0, 1, T // 2, T - 2, T - 1]
+    xs, ds = x[some].contiguous(), dy[some].contiguous()
+    dx, dgamma, dbeta = mol.layer_norm_grad(dy, x)
+    (want, _, _), (bound, _, _) = rh.layer_norm_grad(ds, xs, None, 1e-5, F32)
+    within(dx[some], want, bound, "dx")
+    assert torch.equal(dx[some], mol.layer_norm_grad(ds, xs)[0])
+    unit = mol.normalize_grad(dy, x)
+    within(unit[some], *rh.normalize_grad(ds, xs, 1e-12, F32), "dx of unit rows")
+    assert torch.equal(unit[some], mol.normalize_grad(ds, xs))
+    c = x.double() - x.double().mean(1, keepdim=True)
+    xhat = c / (c.square().mean(1, keepdim=True) + 1e-5).sqrt()
+    # a lane's rows are at most T / 1024 of a workgroup's, then 6 additions over lanes, 3 over waves, 80 over workgroups;
+    # xhat is off by 2 PATH U of its row's largest at most
+    n = T / 1024 + 128
+    within(dbeta, dy.double().sum(0), n * rh.U * dy.double().abs().sum(0), "dbeta")
+    within(dgamma, (dy * xhat).sum(0), (n + 2 * rh.PATH) * rh.U * dy.double().abs().sum(0) * float(xhat.abs().max()), "dgamma")
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("p", [0.3, 0.9])
+def test_dropout_with_residual_past_the_caches(t, p):
+    n = (1 << 28) // (2 * (4 if t == F32 else 2)) + 16003
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x, res = (torch.empty(n, dtype=t, device="cuda").normal_(generator=g) for _ in range(2))
+    got = mol.dropout(x, p, 5, step=3, offset=1 << 33, residual=res)
+    for at in (0, n // 16 * 8, n // 8 * 8 - 4000):
+        piece = slice(at, min(at + 5000, n))
+        _, want, bound = rh.dropout(x[piece], p, 5, 3, (1 << 33) + at, res[piece], t)
+        # (of a sum that cancels, the bound counts the terms)
+        within(got[piece], want, bound + 3 * rh.U * (x[piece].double().cpu().abs() / (1 - p) + res[piece].double().cpu().abs()), f"at {at}")
+    assert torch.equal(mol.dropout(x, p, 5, step=3, offset=1 << 33, residual=res, out=res), got), "in place differs"
