@@ -471,11 +471,13 @@ int mol_adamw_step(const mol_adamw *opt, const mol_adamw_tensor *tensors,
  * Between embedding rows and scores: a query formed from a user's history,
  * rows and components normalised, dropout in training.  Reductions, states
  * and statistics are float32, outputs are rounded once, and all of it is
- * deterministic.  Tensors need the alignment of their elements only. */
+ * deterministic.  Tensors need the alignment of their elements only; an output
+ * overlaps an input in no other way than is said. */
 
 /* Layer norm of every row of x [T][d]:
  *   y = (x - mean) / sqrt(var + eps) * gamma + beta
- * with the row's mean and (biased) variance, formed about the mean; gamma and
+ * with the row's mean and (biased) variance, formed about the mean (a float32
+ * sum: x - mean is off by up to 2^-18 of the row's mean magnitude); gamma and
  * beta float32 [d], NULL for 1 and 0.  eps from FLT_MIN to FLT_MAX, d up to
  * MOL_MAX_NORM.  y may be x itself where their types are the same.  T == 0 is
  * a no-op. */
@@ -540,7 +542,9 @@ int mol_dropout(const void *x, int32_t x_dtype, int64_t n, double p,
  * as it is.  States are float32 throughout; one that is not finite stays so to its
  * history's end, and is no other history's.  Needs mol_gated_scan_workspace bytes
  * (256-byte aligned), which serve every scan and gradient of no more tokens,
- * channels and histories.  d up to MOL_MAX_ROW, T and B up to MOL_MAX_TOKENS. */
+ * channels and histories.  d up to MOL_MAX_ROW, T and B up to MOL_MAX_TOKENS, and
+ * for d above 64 ceil(T / 128) ceil(d / 128) below 2^23 (a launch's workgroups):
+ * at d = 512 T up to 268,435,328.  MOL_EUNSUPPORTED beyond. */
 int mol_gated_scan_workspace(int32_t T, int32_t d, int32_t B, size_t *bytes);
 int mol_gated_scan(const void *gate, const void *x, int32_t x_dtype, int32_t T,
                    int32_t d, const int32_t *offsets, int32_t B,

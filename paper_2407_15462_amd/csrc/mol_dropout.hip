@@ -8,8 +8,8 @@
 //
 // Bound by memory: a thread takes 8 elements, one counter, at a time.  Its 10
 // rounds are 20 64-bit products, which for 32 bits an element would take as long as the
-// memory does (bfloat16).  Measured: 134M bf16 elements 81 to 86 us (6.3 TB/s), with a residual 121 (6.6), both read
-// past the caches (91 and 137 through them; see streams()); 524,288 in 2.7 us, of a call's 6.4.
+// memory does (bfloat16).  Measured: 134M bf16 elements 81 to 86 us (6.3 TB/s), with a residual 121 to 129 (6.2 to
+// 6.6), both read past the caches (91 and 137 through them; see streams()); 524,288 in 2.7 us, of a call's 6.4.
 #include <algorithm>
 
 #include "mol_kernels.h"

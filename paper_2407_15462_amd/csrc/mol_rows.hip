@@ -11,10 +11,10 @@
 // (both rows of a gradient), its statistics are formed there (variance about the mean,
 // float32; a gradient forms them again from x rather than reading them), and it is
 // written once.  Measured: layer norm of 262,144 x 512 bf16 93 to 100 us (5.4 TB/s, where a copy of
-// as much runs at 5.0), its gradient 141 + 5 (5.5; through the caches 158 + 5); 172M float32 elements to bf16 rows
+// as much runs at 5.0), its gradient 137 to 141 + 5 (5.5; through the caches 158 + 5); 172M float32 elements to bf16 rows
 // of 32 of length 1 172 us (6.0).  Reading past the caches gains in gradients of large tensors only (streams();
 // forwards it took 134 us for 100).  Where rows are few, their chains of loads and sums: 32 rows of 1024 take
-// 3.5 us, the gradient of 4099 float32 rows of 777 14 + 4 (7 at the rate of large ones).
+// 3.5 us, the gradient of 4099 float32 rows of 777 14 to 16 + 4 (7 at the rate of large ones).
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
@@ -117,7 +117,7 @@ struct Stats {
       if (needed) scale = want;
     }
     if (MODE == kLayer) {
-      if (ss == 0.f) scale = 1.f;                              // (a constant row: x is 0 in any scale, and eps is left of the variance)
+      if (ss == 0.f) scale = 1.f;                              // (a constant row: x is 0 in any scale, and all that counts is eps)
       inv = 1.f / sqrtf(ss / d + eps * scale * scale);
       flat = false;
     } else {

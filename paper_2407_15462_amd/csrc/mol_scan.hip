@@ -26,9 +26,10 @@
 // publishes needs nothing but what those before it publish.  A published pair is one
 // 64-bit word, whose top bit (the sign of A, which is not negative) says that it is there.
 //
-// Measured, bf16: 1024 histories of 262,144 tokens of 512 channels 205 to 209 us (3.9 TB/s), back 309 (5.2
-// TB/s, where a copy of as much reaches 5.0); one history of 131,072 x 1024 208, back (x 512) 180.  Inputs of
-// 256 MB and more are read and written past the caches (through them 217, 318, 225 and 182).  What bounds it: back,
+// Measured, bf16: 1024 histories of 262,144 tokens of 512 channels 191 to 207 us (3.9 to 4.2 TB/s), back 305 to 309
+// (5.2 TB/s, where a copy of as much reaches 5.0); one history of 131,072 x 1024 200 to 208, back (x 512) 173 to 180; 64
+// histories of 20,000 x 512 32.  Inputs of 256 MB and more are read and written past the caches (through them 217, 318,
+// 225 and 182, where these took the larger figures).  What bounds it: back,
 // memory; forward, the waits (27 to 45 us in a build without them) and, at more than half of the vector rate, two
 // gates an element (27 instructions).  Tried and slower forward: every token's A and H kept in place of the second
 // run (half as many tokens a slice: 225 to 231 where this took 219), workgroups that stay and load their next chunk

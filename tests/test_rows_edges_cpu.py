@@ -15,3 +15,12 @@ def test_rows_past_int32_are_refused(d):
                  lambda: mol.layer_norm_grad_workspace(x), lambda: mol.gated_scan(x, x), lambda: mol.gated_step(x, x, x)):
         with pytest.raises(ValueError, match="2.31"):
             call()
+
+
+@pytest.mark.parametrize("d,most", [(1, 1 << 30), (64, 1 << 30), (65, (1 << 30) - 128), (128, (1 << 30) - 128), (129, (1 << 29) - 128),
+                                    (512, 268435328), (65536, 128 * ((1 << 14) - 1))])
+def test_the_largest_scans_are_those_that_the_header_names(d, most):
+    assert mol.mol_gated_scan_workspace(most, d, 1) > 0
+    for T in (most + 1, 1 << 31 if most == 1 << 30 else 1 << 30):
+        with pytest.raises((mol.MolError, ValueError)):
+            mol.mol_gated_scan_workspace(T, d, 1)
